@@ -486,6 +486,57 @@ gb_status gb_scorer_step(gb_pool* step_pool, const gb_scorer_config* cfg, const 
                          void* workspace_dev, const void* hidden_dev, float* score_out_dev,
                          gb_stream_t stream);
 
+/*
+ * Causal attention over whole prompts (the prefill whose keys and values gb_pool_seed takes):
+ * sequences packed one after the other, sequence s holding rows cu_seqlens[s] .. cu_seqlens[s+1]-1,
+ *   out[i][h] = sum_{j <= i, j in i's sequence} softmax_j(scale * q[i][h] . k[j][h / G]) v[j][h / G]
+ * with G = num_q_heads / num_kv_heads.  Algorithm 1 starts from "C initial traces from P": this
+ * computes the prompt P's own attention.
+ *   q, k, v, out:  rows of num_q_heads (k, v: num_kv_heads) heads of head_dim values in dtype, heads
+ *                  contiguous, *_stride elements from one token to the next; 16-byte aligned, strides
+ *                  a multiple of 16 bytes (so q, k and v may be columns of one fused projection).  The
+ *                  span of out's rows must not meet that of q, k or v.
+ *   cu_seqlens:    int32 [num_seqs + 1], non-decreasing, within [0, num_tokens]; a sequence may be empty
+ *   num_tokens:    rows of q, k, v and out; rows outside every sequence are left as they were
+ *   workspace:     gb_prompt_workspace_bytes, 256-byte aligned; calls using one workspace must be ordered
+ * Values in rows a query does not see (later tokens, other sequences) do not reach its result, whatever
+ * they are.  Two launches: a planner that lists the work longest first, and the attention.
+ * Errors: GB_ERR_INVALID for bad sizes, alignment, strides, overlap, a workspace that is too small or a
+ * scale that is not positive and finite; GB_ERR_UNSUPPORTED unless (dtype, head_dim) is (GB_BF16, 128)
+ * or (GB_F32, 64) and G one of 1, 2, 4, 8, 16; GB_ERR_TOO_LARGE when the work list passes 2^31 entries.  A
+ * sequence whose bounds are out of order or range is not computed and recorded as GB_ERR_INVALID
+ * in the workspace's status (gb_prompt_status).
+ */
+typedef struct {
+  const void* q;
+  const void* k;
+  const void* v;
+  void* out;
+  const int32_t* cu_seqlens;
+  void* workspace;
+  size_t workspace_bytes;
+  int64_t q_stride;
+  int64_t k_stride;
+  int64_t v_stride;
+  int64_t out_stride;
+  int num_seqs;
+  int num_tokens;
+  int num_q_heads;
+  int num_kv_heads;
+  int head_dim;
+  int dtype;
+  float scale;
+} gb_prompt_args;
+gb_status gb_prompt_workspace_bytes(int num_tokens, int num_seqs, int num_q_heads, int num_kv_heads, int head_dim,
+                                    int dtype, size_t* bytes);
+gb_status gb_prompt_attention(const gb_prompt_args* args, gb_stream_t stream);
+
+/*
+ * Device status of the last gb_prompt_attention call with this workspace (GB_OK, GB_ERR_INVALID for a
+ * sequence out of order or range, GB_ERR_TIMEOUT for a bounded wait that ran out).  Synchronises `stream`.
+ */
+gb_status gb_prompt_status(const void* workspace_dev, int* device_status, gb_stream_t stream);
+
 /* Short description of the pool's last host-side failure ("" if none); static storage. */
 const char* gb_last_error(gb_pool* pool);
 

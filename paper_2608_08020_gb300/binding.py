@@ -29,7 +29,7 @@ EXPORTS = ["gb_pool_workspace_bytes", "gb_pool_init", "gb_pool_destroy", "gb_poo
            "gb_append_kv", "gb_score_probe", "gb_push_scores", "gb_prune_branch", "gb_release", "gb_pool_status",
            "gb_pool_clear_status", "gb_pool_wait_selftest", "gb_pool_read_state", "gb_pool_set_profile_events", "gb_pool_launch_count",
            "gb_paged_decode_noalloc", "gb_paged_decode_noalloc_status", "gb_pool_read_step_stats", "gb_pool_set_capacity", "gb_pool_last_ranked", "gb_score_mlp", "gb_fork_slots", "gb_scorer_sizes", "gb_scorer_seed",
-           "gb_scorer_step", "gb_last_error"]
+           "gb_scorer_step", "gb_prompt_workspace_bytes", "gb_prompt_attention", "gb_prompt_status", "gb_last_error"]
 GB_PROF_DECODE, GB_PROF_PROBE, GB_PROF_PRUNE, GB_PROF_GROUPED = 0, 1, 2, 3
 GB_PROF_PLAN, GB_PROF_APPEND, GB_PROF_COMBINE, GB_PROF_ATTENTION = 4, 5, 6, 7
 
@@ -54,6 +54,15 @@ class GbPagedDecodeArgs(ctypes.Structure):
                 ("num_q_heads", ctypes.c_int), ("num_kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int),
                 ("page_size", ctypes.c_int), ("kv_dtype", ctypes.c_int), ("max_pages_per_beam", ctypes.c_int),
                 ("num_pages", ctypes.c_int64), ("scale", ctypes.c_float)]
+
+
+class GbPromptArgs(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("out", ctypes.c_void_p),
+                ("cu_seqlens", ctypes.c_void_p), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+                ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
+                ("out_stride", ctypes.c_int64), ("num_seqs", ctypes.c_int), ("num_tokens", ctypes.c_int),
+                ("num_q_heads", ctypes.c_int), ("num_kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int),
+                ("dtype", ctypes.c_int), ("scale", ctypes.c_float)]
 
 
 class GambitError(RuntimeError):
@@ -102,6 +111,9 @@ def load(path: Path | None = None) -> ctypes.CDLL:
         "gb_scorer_sizes": [V, P, P, P, P, I, P],
         "gb_scorer_seed": [V, P, V, V, V, I, V],
         "gb_scorer_step": [V, P, V, V, V, V, V],
+        "gb_prompt_workspace_bytes": [I, I, I, I, I, I, P],
+        "gb_prompt_attention": [P, V],
+        "gb_prompt_status": [V, P, V],
         "gb_last_error": [V],
     }
     for name, args in sig.items():
@@ -318,6 +330,25 @@ def gb_paged_decode_noalloc_status(stream=None) -> int:
     st = ctypes.c_int()
     _check(None, load().gb_paged_decode_noalloc_status(ctypes.byref(st), stream_handle(stream)),
            "gb_paged_decode_noalloc_status")
+    return st.value
+
+
+def gb_prompt_workspace_bytes(num_tokens: int, num_seqs: int, num_q_heads: int, num_kv_heads: int, head_dim: int,
+                              dtype: int) -> int:
+    n = ctypes.c_size_t()
+    _check(None, load().gb_prompt_workspace_bytes(num_tokens, num_seqs, num_q_heads, num_kv_heads, head_dim, dtype,
+                                                  ctypes.byref(n)), "gb_prompt_workspace_bytes")
+    return n.value
+
+
+def gb_prompt_attention(args: GbPromptArgs, stream=None) -> None:
+    _check(None, load().gb_prompt_attention(ctypes.byref(args), stream_handle(stream)), "gb_prompt_attention")
+
+
+def gb_prompt_status(workspace, stream=None) -> int:
+    """Device status of the last gb_prompt_attention call with this workspace (synchronises)."""
+    st = ctypes.c_int()
+    _check(None, load().gb_prompt_status(ptr(workspace), ctypes.byref(st), stream_handle(stream)), "gb_prompt_status")
     return st.value
 
 

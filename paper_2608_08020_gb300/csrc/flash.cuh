@@ -1,0 +1,470 @@
+// Attention of up to 256 query rows over a run of keys on the tcgen05 tensor cores: bf16 inputs, 128
+// dims, fp32 sums.  The pipeline shared by the prompt and the draft-tree kernels; a Job says which
+// units of work there are, where their rows lie, which keys a row sees and where its result goes.
+//
+//   S = Q K^T (128 x 128, fp32 in tensor memory),  P = 2^(scale' S - m) (bf16),  O += P V
+// with the running maximum m and sum l of each row's softmax, one pass over the keys.
+//
+// A unit has one head's query rows and nt tiles of 128 keys.  Two groups of four softmax warps each hold
+// a Q tile of 128 rows, an accumulator O and an S tile in tensor memory (512 columns in all).  In a dual
+// unit (129 to 256 rows) the groups have the two halves of the rows and every K/V tile serves
+// both; otherwise both have the same rows, group g takes tiles g, g + 2, ..., and the groups' sums are
+// joined at the unit's end, so a unit of few rows has the same two chains in flight.  While one group
+// takes the exponentials of its S tile the tensor core works for the other: per tile 1024 cycles of
+// products (128^3 x 2 at 4096 multiply-adds a cycle) against 512 of ex2 (32 a cycle) and about 600 of
+// other instructions.
+//
+// P is rounded to bf16 for the tensor core (relative 2^-9 each, independent, so a result's error
+// is about that of its own rounding to bf16); the sum l is of the unrounded values.
+//
+// Warp roles (320 threads):
+//   warps 0-7  softmax: thread r of group g owns row r of its tile (tensor-memory lane r); also loads
+//              the row's query and writes its result
+//   warp 8     takes units from a grid-wide counter, publishes them in a ring of four, and streams
+//              K and V tiles through a ring of five 32 KiB stages (K0 V0 K1 V1 ...)
+//   warp 9     issues the products: S(i), then P.V(i - 2) before S(i) of the same group, whose S tile
+//              P overwrites; a CTA's products run in issue order
+// P overwrites the first half of its S tile.  O is rescaled by its own group, and only when a maximum
+// grows by more than 8 (p <= 2^8 meanwhile): when S(i) is complete so is P.V(i - 2), issued before it.
+//
+// Every wait is bounded; when one runs out the CTA records the timeout, every role stops issuing and waits
+// (bounded) for its own copies and products, the tensor memory is freed and the CTA leaves.
+#pragma once
+#include <cuda.h>
+
+#include "internal.cuh"
+#include "ptx.cuh"
+#include "tc.cuh"
+
+namespace gb {
+namespace flash {
+
+constexpr int kRows = 128, kTok = 128, kD = 128;
+constexpr int kThreads = 320;
+constexpr int kLoadWarp = 8, kMmaWarp = 9;
+constexpr int kStages = 5;
+constexpr int kTile = 32768;           // Q, K or V tile: 128 x 128 bf16
+constexpr int kRing = 2 * kTile;       // after the two Q tiles
+constexpr int kBar = kRing + kStages * kTile;
+constexpr int kXch = kBar + 1024;      // float2 [2 groups][128 rows]: (m, l) of a unit's groups
+constexpr int kSmem = kXch + 2048;
+static_assert(kSmem <= 232448, "shared memory per block");
+constexpr uint32_t kTmemS = 0, kTmemO = 256;  // column of group 0; group 1 is 128 further
+
+constexpr int kSlots = 4, kUnitWords = 16;
+constexpr int kBarFull = 0;                       // [kStages]
+constexpr int kBarEmpty = kBarFull + 8 * kStages; // [kStages]
+constexpr int kBarQ = kBarEmpty + 8 * kStages;    // [2] the group's query rows are in
+constexpr int kBarS = kBarQ + 16;                 // [2] S of the group's next tile is complete
+constexpr int kBarP = kBarS + 16;                 // [2] P of it is written (and O rescaled)
+constexpr int kBarO = kBarP + 16;                 // [2] the unit's last P.V of the group is complete
+constexpr int kBarOFree = kBarO + 16;             // [2] the group's O has been read
+constexpr int kBarX = kBarOFree + 16;             // the groups' (m, l) are in
+constexpr int kBarPatch = kBarX + 8;              // a V tile that is mended before it is handed on
+constexpr int kBarSched = kBarPatch + 8;          // [kSlots]
+constexpr int kBarSchedFree = kBarSched + 8 * kSlots;
+constexpr int kUnits = kBarSchedFree + 8 * kSlots;  // int [kSlots][kUnitWords]
+constexpr int kWordTmem = kUnits + 4 * kSlots * kUnitWords;
+constexpr int kWordAbort = kWordTmem + 4;
+static_assert(kUnits % 16 == 0 && kWordAbort + 4 <= 1024, "control area");
+constexpr int kSchedReaders = 9;  // eight softmax warps, the MMA warp
+
+// What every role knows of a unit; w is the job's own.
+struct Unit {
+  int nt;    // tiles of 128 keys; -1: no more units
+  int dual;  // 129 to 256 rows
+  int head;  // KV head
+  int w[kUnitWords - 3];
+};
+static_assert(sizeof(Unit) == 4 * kUnitWords, "unit words");
+
+// The columns are handed out only after the wait: the registers pass through it.
+__device__ __forceinline__ void ld32_issue(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+        "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+        "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr));
+}
+__device__ __forceinline__ void ld32_wait(uint32_t* r) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                 "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]),
+                 "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]),
+                 "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]),
+                 "+r"(r[30]), "+r"(r[31])
+               :
+               : "memory");
+}
+
+__device__ __forceinline__ void st16(uint32_t taddr, const uint32_t* u) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(
+          taddr),
+      "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]), "r"(u[8]), "r"(u[9]),
+      "r"(u[10]), "r"(u[11]), "r"(u[12]), "r"(u[13]), "r"(u[14]), "r"(u[15])
+      : "memory");
+}
+__device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// 32 columns of a row's result: O of one group, or of both with their weights.
+__device__ __forceinline__ void read_o(uint32_t a, uint32_t b, bool two, float wa, float wb, float* o) {
+  uint32_t u[32];
+  ld32_issue(a, u);
+  if (two) {
+    uint32_t v[32];
+    ld32_issue(b, v);
+    ld32_wait(u);
+    ld32_wait(v);
+    // A weight of 0 belongs to a group that saw no key of the row: what it summed is 0 x V.
+#pragma unroll
+    for (int c = 0; c < 32; ++c)
+      o[c] = (wa == 0.f ? 0.f : wa * __uint_as_float(u[c])) + (wb == 0.f ? 0.f : wb * __uint_as_float(v[c]));
+  } else {
+    ld32_wait(u);
+#pragma unroll
+    for (int c = 0; c < 32; ++c) o[c] = __uint_as_float(u[c]);
+  }
+}
+
+// Keys of a tile a row sees: the first `limit` and, from column 64 on, those of `bits`.
+struct Sees {
+  bool all;                 // every key of the tile, for every row of the warp
+  int limit;                // columns below this
+  unsigned long long bits;  // columns 64 + i for bit i
+};
+
+// Columns [c0, c0 + cols) of sum_j 2^(qscale q.k_j - m) v_j over the keys that key(j, k, v) says are seen, by a
+// warp: lane l gets columns c0 + l cols / 32 on.  A product with P takes every key of a tile, with p = 0 for those
+// the row does not see, and 0 x inf is NaN: a row whose result is not finite although its maximum is, is summed
+// again here where one of those keys' values is not finite.
+template <class Key>
+__device__ __forceinline__ void sum_seen(const __nv_bfloat16* q, int nkeys, Key key, float qscale, float m, int c0,
+                                         int cols, float* acc) {
+  const int lane = threadIdx.x & 31, per = cols / 32;
+  float qv[4];
+  for (int i = 0; i < 4; ++i) {
+    qv[i] = __bfloat162float(q[4 * lane + i]);
+    acc[i] = 0.f;
+  }
+  for (int j = 0; j < nkeys; ++j) {
+    const __nv_bfloat16 *k, *v;
+    if (!key(j, k, v)) continue;
+    float s = 0.f;
+    for (int i = 0; i < 4; ++i) s = fmaf(qv[i], __bfloat162float(k[4 * lane + i]), s);
+    for (int w = 16; w > 0; w >>= 1) s += __shfl_xor_sync(0xffffffffu, s, w);
+    const float p = exp2f(fmaf(s, qscale, -m));
+    for (int i = 0; i < per; ++i) acc[i] = fmaf(p, __bfloat162float(v[c0 + per * lane + i]), acc[i]);
+  }
+}
+// Whether v has a value that is not finite in columns [c0, c0 + cols) (a warp's answer).
+__device__ __forceinline__ bool not_finite(const __nv_bfloat16* v, int c0, int cols) {
+  const int lane = threadIdx.x & 31, per = cols / 32;
+  bool bad = false;
+  for (int i = 0; i < per; ++i) bad |= !isfinite(__bfloat162float(v[c0 + per * lane + i]));
+  return __any_sync(0xffffffffu, bad);
+}
+
+template <class Job>
+__device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t sbase = smem_addr(sm), ctl = sbase + kBar;
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(sm + kBar + kWordAbort);
+  Unit* units = reinterpret_cast<Unit*>(sm + kBar + kUnits);
+  if (sbase & 1023) {  // the swizzled layouts need a 1024-byte aligned base
+    if (tid == 0) job.error(GB_ERR_UNSUPPORTED);
+    return;
+  }
+  if (tid == 0) {
+    for (int i = 0; i < kStages; ++i) {
+      mbar_init(ctl + kBarFull + 8 * i, 1);
+      mbar_init(ctl + kBarEmpty + 8 * i, 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(ctl + kBarQ + 8 * i, Job::kQArrivals);
+      mbar_init(ctl + kBarS + 8 * i, 1);
+      mbar_init(ctl + kBarP + 8 * i, 4);
+      mbar_init(ctl + kBarO + 8 * i, 1);
+      mbar_init(ctl + kBarOFree + 8 * i, 8);
+    }
+    mbar_init(ctl + kBarX, 8);
+    mbar_init(ctl + kBarPatch, 1);
+    for (int i = 0; i < kSlots; ++i) {
+      mbar_init(ctl + kBarSched + 8 * i, 1);
+      mbar_init(ctl + kBarSchedFree + 8 * i, kSchedReaders);
+    }
+    *abort_flag = 0;
+    fence_mbar_init();
+  }
+  if (warp == kMmaWarp) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(ctl + kWordTmem), "r"(512));
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(sm + kBar + kWordTmem);
+  pdl_wait();
+  pdl_launch_dependents();
+
+  if (warp == kLoadWarp) {
+    // ---------------------------------------------------------------- units, K and V tiles
+    uint32_t n = 0;  // stages filled
+    uint32_t patches = 0;
+    bool ok = true;
+    const int total = job.total();
+    int next = 0;
+    if (lane == 0) next = job.ticket();
+    for (int u = 0;; ++u) {
+      const int id = __shfl_sync(0xffffffffu, next, 0);
+      if (lane == 0 && id < total) next = job.ticket();
+      const int slot = u & (kSlots - 1);
+      if (lane == 0 && u >= kSlots)
+        ok = wait_or_abort(ctl + kBarSchedFree + 8 * slot, (u / kSlots - 1) & 1, abort_flag);
+      ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
+      if (!ok || *abort_flag) break;
+      Unit x;
+      x.nt = -1;
+      if (id < total) job.unit(id, x);
+      if (lane == 0) {
+        units[slot] = x;
+        mbar_arrive(ctl + kBarSched + 8 * slot);
+      }
+      if (x.nt < 0) break;
+      for (int t = 0; t < 2 * x.nt && ok; ++t, ++n) {
+        const uint32_t st = n % kStages, dst = sbase + kRing + st * kTile;
+        const int kv = t & 1, j = t >> 1;
+        if (lane == 0 && n >= (uint32_t)kStages)
+          ok = wait_or_abort(ctl + kBarEmpty + 8 * st, (n / kStages - 1) & 1, abort_flag);
+        ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
+        if (!ok) break;
+        const uint32_t full = ctl + kBarFull + 8 * st;
+        // Rows [z0, z1) of a V tile hold no token: whatever lies in them is made 0, since 0 x NaN is NaN.
+        int z0 = 0, z1 = 0;
+        if (kv) job.stale_rows(x, j, z0, z1);
+        const uint32_t bar = z0 < z1 ? ctl + kBarPatch : full;
+        if (lane == 0) mbar_arrive_expect_tx(bar, kTile);
+        __syncwarp();
+        job.load_tile(x, j, kv, dst, bar, lane);
+        if (z0 < z1) {
+          if (lane == 0) ok = wait_or_abort(bar, patches++ & 1, abort_flag);
+          ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
+          if (!ok) break;
+          for (int i = lane; i < (z1 - z0) * 16; i += 32)
+            *reinterpret_cast<uint4*>(sm + (dst - sbase) + Job::v_row(z0 + (i >> 4), (i >> 3) & 1) + (i & 7) * 16) =
+                make_uint4(0, 0, 0, 0);
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(full);
+        }
+      }
+      if (!ok) break;
+    }
+    // Copies in flight land before the CTA leaves (bounded).
+    if (lane == 0 && *abort_flag)
+      for (uint32_t k = n > (uint32_t)kStages ? n - kStages : 0; k < n; ++k)
+        mbar_wait_bounded(ctl + kBarFull + 8 * (k % kStages), (k / kStages) & 1, kWaitLimitNs / 8);
+  } else if (warp == kMmaWarp) {
+    // ---------------------------------------------------------------- products
+    if (lane == 0) {
+      constexpr uint32_t ID_S = idesc(kRows, kTok, false), ID_PV = idesc(kRows, kD, true);
+      uint32_t ring = 0;               // stage count of the unit's first tile
+      uint32_t np[2] = {0, 0};         // P tiles consumed per group
+      uint32_t ns[2] = {0, 0};
+      bool ok = true;
+      for (int u = 0; ok; ++u) {
+        const int slot = u & (kSlots - 1);
+        ok = wait_or_abort(ctl + kBarSched + 8 * slot, (u / kSlots) & 1, abort_flag);
+        if (!ok) break;
+        const int nt = units[slot].nt, dual = units[slot].dual;
+        mbar_arrive(ctl + kBarSchedFree + 8 * slot);
+        if (nt < 0) break;
+        const int items = dual ? 2 * nt : nt;
+        for (int i = 0; i < items + 2 && ok; ++i) {
+          const int g = i & 1;
+          if (i >= 2) {  // P.V of item i - 2
+            const int it = i - 2;
+            const uint32_t pos = ring + 2 * (dual ? it >> 1 : it) + 1, st = pos % kStages;
+            ok = wait_or_abort(ctl + kBarP + 8 * g, np[g] & 1, abort_flag) &&
+                 wait_or_abort(ctl + kBarFull + 8 * st, (pos / kStages) & 1, abort_flag) &&
+                 (it >= 2 || u == 0 || wait_or_abort(ctl + kBarOFree + 8 * g, (u - 1) & 1, abort_flag));
+            if (!ok) break;
+            ++np[g];
+            tc_fence_after();
+            const uint32_t vb = sbase + kRing + st * kTile;
+#pragma unroll
+            for (int kk = 0; kk < kTok / 16; ++kk)
+              mma_ts(tmem + kTmemO + g * 128, tmem + kTmemS + g * 128 + kk * 8,
+                     sdesc(vb + kk * Job::kVStep, Job::kVLbo, Job::kVSbo), ID_PV, (it >= 2 || kk > 0) ? 1u : 0u);
+            if (!dual || g == 1) mma_commit(ctl + kBarEmpty + 8 * st);
+            if (it + 2 >= items) mma_commit(ctl + kBarO + 8 * g);
+          }
+          if (i < items) {  // S of item i
+            const uint32_t pos = ring + 2 * (dual ? i >> 1 : i), st = pos % kStages;
+            ok = (i >= 2 || wait_or_abort(ctl + kBarQ + 8 * g, u & 1, abort_flag)) &&
+                 wait_or_abort(ctl + kBarFull + 8 * st, (pos / kStages) & 1, abort_flag);
+            if (!ok) break;
+            ++ns[g];
+            tc_fence_after();
+            const uint32_t kb = sbase + kRing + st * kTile;
+#pragma unroll
+            for (int kk = 0; kk < kD / 16; ++kk)
+              mma(tmem + kTmemS + g * 128, sdesc(sbase + g * kTile + (kk >> 2) * 16384 + (kk & 3) * 32, 16, 1024),
+                  sdesc(kb + (kk >> 2) * Job::kKHalf + (kk & 3) * 32, 16, Job::kKSbo), ID_S, kk > 0);
+            if (!dual || g == 1) mma_commit(ctl + kBarEmpty + 8 * st);
+            mma_commit(ctl + kBarS + 8 * g);
+          }
+        }
+        if (ok && items == 1) mma_commit(ctl + kBarO + 8);  // group 1 had no tile
+        ring += 2 * nt;
+      }
+      if (*abort_flag)  // products in flight end before the tensor memory is freed (bounded)
+        for (int g = 0; g < 2; ++g)
+          if (ns[g]) mbar_wait_bounded(ctl + kBarS + 8 * g, (ns[g] - 1) & 1, kWaitLimitNs / 8);
+    }
+    __syncwarp();
+  } else {
+    // ---------------------------------------------------------------- softmax
+    const int g = warp >> 2, r = tid & 127;
+    const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t s_addr = tmem + kTmemS + g * 128 + lane_base, o_addr = tmem + kTmemO + lane_base;
+    float2* xch = reinterpret_cast<float2*>(sm + kXch);
+    const float qscale = job.qscale;
+    uint32_t n = 0, nx = 0;  // tiles of this group, joined units
+    bool alive = true;
+    Unit x, y;
+    auto fetch = [&](int u, Unit& to) {  // unit u, once it is known
+      const int slot = u & (kSlots - 1);
+      if (!wait_or_abort(ctl + kBarSched + 8 * slot, (u / kSlots) & 1, abort_flag)) return false;
+      to = units[slot];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(ctl + kBarSchedFree + 8 * slot);
+      return true;
+    };
+    alive = fetch(0, x);
+    typename Job::Row row;
+    if (alive && x.nt >= 0) job.load_q(x, g, r, sbase + g * kTile, ctl + kBarQ + 8 * g, row);
+    for (int u = 0; alive && x.nt >= 0; ++u) {
+      const int mine = x.dual ? x.nt : (x.nt + 1 - g) / 2;  // this group's tiles
+      float m_ref = -INFINITY, l = 0.f;
+      for (int i = 0; i < mine; ++i, ++n) {
+        const int t = x.dual ? i : 2 * i + g;
+        if (!wait_or_abort(ctl + kBarS + 8 * g, n & 1, abort_flag)) { alive = false; break; }
+        tc_fence_after();
+        uint32_t su[128];
+#pragma unroll
+        for (int c = 0; c < 128; c += 32) ld32_issue(s_addr + c, su + c);
+#pragma unroll
+        for (int c = 0; c < 128; c += 32) ld32_wait(su + c);
+        float* s = reinterpret_cast<float*>(su);
+        const Sees see = job.sees(x, row, t);
+        if (!see.all) {
+#pragma unroll
+          for (int c = 0; c < 128; ++c) {
+            const bool on = c < see.limit || (c >= 64 && ((see.bits >> (c - 64)) & 1));
+            s[c] = on ? s[c] : -INFINITY;
+          }
+        }
+        float mx[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+        for (int c = 4; c < 128; c += 4) {
+          mx[0] = fmaxf(mx[0], s[c]);
+          mx[1] = fmaxf(mx[1], s[c + 1]);
+          mx[2] = fmaxf(mx[2], s[c + 2]);
+          mx[3] = fmaxf(mx[3], s[c + 3]);
+        }
+        const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * qscale;
+        const bool raise = mt > m_ref + 8.f;
+        if (i > 0 && __any_sync(0xffffffffu, raise)) {
+          const float alpha = raise ? exp2f(m_ref - mt) : 1.f;
+#pragma unroll 1
+          for (int c0 = 0; c0 < 128; c0 += 32) {
+            float o[32];
+            tmem_ld32(o_addr + g * 128 + c0, o);
+#pragma unroll
+            for (int c = 0; c < 32; ++c) o[c] *= alpha;
+            tmem_st32(o_addr + g * 128 + c0, o);
+          }
+          l *= alpha;
+        }
+        if (raise) m_ref = mt;
+        const float neg_m = m_ref == -INFINITY ? 0.f : -m_ref;  // no key seen yet: every p is 0
+        float ls[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < 128; c += 32) {
+          uint32_t pw[16];
+#pragma unroll
+          for (int k = 0; k < 32; k += 4) {
+            const float p0 = ex2_approx(fmaf(s[c + k], qscale, neg_m));
+            const float p1 = ex2_approx(fmaf(s[c + k + 1], qscale, neg_m));
+            const float p2 = ex2_approx(fmaf(s[c + k + 2], qscale, neg_m));
+            const float p3 = ex2_approx(fmaf(s[c + k + 3], qscale, neg_m));
+            const __nv_bfloat162 a = __floats2bfloat162_rn(p0, p1), b = __floats2bfloat162_rn(p2, p3);
+            pw[k / 2] = *reinterpret_cast<const uint32_t*>(&a);
+            pw[k / 2 + 1] = *reinterpret_cast<const uint32_t*>(&b);
+            ls[0] += p0;
+            ls[1] += p1;
+            ls[2] += p2;
+            ls[3] += p3;
+          }
+          st16(s_addr + c / 2, pw);
+        }
+        st_wait();
+        l += (ls[0] + ls[1]) + (ls[2] + ls[3]);
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(ctl + kBarP + 8 * g);
+      }
+      if (!alive) break;
+      // The next unit's query rows: S of this unit's last tile has been read.
+      if (!(alive = fetch(u + 1, y))) break;
+      typename Job::Row row_y;
+      if (y.nt >= 0) job.load_q(y, g, r, sbase + g * kTile, ctl + kBarQ + 8 * g, row_y);
+      if (x.dual) {
+        if (!(alive = wait_or_abort(ctl + kBarO + 8 * g, u & 1, abort_flag))) break;
+        tc_fence_after();
+        job.out(x, row, o_addr + g * 128, 0, false, 1.f, 0.f, 0, 128, m_ref, l);
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], 2;" ::"r"(ctl + kBarOFree + 8 * g) : "memory");
+      } else {
+        // Join the two groups' sums; group g writes columns [64 g, 64 g + 64).
+        xch[g * 128 + r] = make_float2(m_ref, l);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(ctl + kBarX);
+        if (!(alive = wait_or_abort(ctl + kBarX, nx & 1, abort_flag) && wait_or_abort(ctl + kBarO, u & 1, abort_flag) &&
+                      wait_or_abort(ctl + kBarO + 8, u & 1, abort_flag)))
+          break;
+        ++nx;
+        const float2 other = xch[(1 - g) * 128 + r];
+        const float m = fmaxf(m_ref, other.x), ref = m == -INFINITY ? 0.f : m;
+        const float mine_w = exp2f(m_ref - ref), other_w = exp2f(other.x - ref);
+        tc_fence_after();
+        job.out(x, row, o_addr + 64 * g, o_addr + 128 + 64 * g, x.nt > 1, g == 0 ? mine_w : other_w,
+                g == 0 ? other_w : mine_w, 64 * g, 64, m, l * mine_w + other.y * other_w);
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(ctl + kBarOFree);
+          mbar_arrive(ctl + kBarOFree + 8);
+        }
+        // Both groups have read the exchange before either writes it again.
+        if (!(alive = wait_or_abort(ctl + kBarOFree, u & 1, abort_flag))) break;
+      }
+      x = y;
+      row = row_y;
+    }
+    job.drain_q(ctl + kBarQ + 8 * g, *abort_flag != 0);
+  }
+  if (*abort_flag && tid == 0) job.error(GB_ERR_TIMEOUT);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == kMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));
+}
+
+}  // namespace flash
+}  // namespace gb

@@ -1,6 +1,7 @@
 // Internal definitions shared by the library's translation units.
 #pragma once
 
+#include <cuda.h>
 #include <cuda_runtime.h>
 #include <cuda_bf16.h>
 #include <stdint.h>
@@ -347,6 +348,10 @@ struct gb_pool {
   bool have_dtmap = false;
   int tmap_oob = 0;                          // first row group past the tensor map (loads zeros)
   std::string last_error;
+  unsigned long long epoch = 0;             // calls that changed the beams' contexts
+  unsigned long long draft_epoch = ~0ull;   // the epoch, workspace and tree size of the round planned last
+  const void* draft_ws = nullptr;
+  int draft_tokens = 0;
   unsigned long long launches = 0;          // kernels launched by this pool
   cudaEvent_t prof_start[GB_PROF_SLOTS] = {};  // caller-owned instrumentation events
   cudaEvent_t prof_stop[GB_PROF_SLOTS] = {};
@@ -389,6 +394,9 @@ cudaError_t launch_attention(gb_pool* pool, int layer, const void* q, const void
                              float* out, bool allow_local, cudaStream_t s);
 cudaError_t launch_wait_selftest(gb_pool* pool, cudaStream_t s);
 void make_kv_tensor_maps(gb_pool* pool);
+// A bf16 tensor map with the 128-byte swizzle, zeros out of bounds (grouped.cu); strides in bytes.
+bool encode_tensor_map(void* map, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides,
+                       const cuuint32_t* box);
 cudaError_t launch_probe(gb_pool* pool, const void* hidden, int hidden_dtype, int H, const float* w,
                          float bias, const uint8_t* mask, float* score_out, const float* scores_in,
                          cudaStream_t s);

@@ -776,6 +776,7 @@ static gb_status append_layer(gb_pool* pool, int layer, int n_tokens, const void
     return fail(pool, GB_ERR_INVALID, "append: bad arguments");
   if (layer != pool->next_layer) return fail(pool, GB_ERR_STATE, "layers of a step must be called in order");
   if (layer == 0) {
+    ++pool->epoch;
     prof_begin(pool, GB_PROF_PLAN, s);
     // One thread per slot (rounded up to a warp): the planner's block scans span only the pool's slots.
     launch_pdl(k_step_begin, 1, std::max(32, (pool->cfg.max_beams + 31) / 32 * 32), 0, s, pool->view, n_tokens,
@@ -851,6 +852,7 @@ extern "C" gb_status gb_release(gb_pool* pool, const int32_t* slots_dev, int n, 
   if (n < 0 || (n > 0 && !slots_dev)) return fail(pool, GB_ERR_INVALID, "release: bad arguments");
   if (pool->next_layer != 0) return fail(pool, GB_ERR_STATE, "release inside an open step");
   if (n == 0) return GB_OK;
+  ++pool->epoch;
   k_release<<<1, 1024, 0, reinterpret_cast<cudaStream_t>(stream)>>>(pool->view, slots_dev, n);
   pool->launches += 1;
   gb_status st = check_launch(pool, "release");

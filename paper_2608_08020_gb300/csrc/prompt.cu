@@ -1,0 +1,361 @@
+// Causal attention over whole prompts, packed one after the other (gb_prompt_attention).
+//
+//   out[i][h] = sum_{j <= i} p_j v[j][h / G],  p = softmax_j(scale q[i][h] . k[j][h / G])
+// for the tokens i, j of one sequence.  The rows of one KV head are (token, query head of the group), token
+// by token, so a tile of 128 rows has 128 / G tokens and all G heads that read the same K and V.
+//
+// Bound by the tensor cores from a few hundred tokens on (2 D Hq n^2 flops against 4 D (Hq + Hkv) n bytes).
+// A planner CTA lists the units (sequence, run of tokens), longest first; a CTA per SM takes (unit, KV head)
+// from a counter.  bf16: flash.cuh; fp32: tile.cuh.
+#include <algorithm>
+#include <mutex>
+
+#include "flash.cuh"
+#include "tile.cuh"
+#include "worklist.cuh"
+
+namespace gb {
+namespace {
+
+// Workspace: control words, then the units.
+enum PromptCtl : int { kPrStatus = 0, kPrUnits = 1, kPrNext = 2, kPrWords = 64 };
+
+struct PromptUnit {
+  int start, len;   // the sequence's first row and length
+  int t0, ntok;     // its tokens [t0, t0 + ntok)
+};
+
+// Tokens per unit: the most rows a unit of the kernel holds.
+__global__ void __launch_bounds__(kListThreads) k_prompt_plan(const int* cu, int num_seqs, int num_tokens, int tokens,
+                                                              int small_tokens, int few, int max_units, int* ctl) {
+  pdl_wait();
+  pdl_launch_dependents();
+  __shared__ ListSmem sm;
+  PromptUnit* units = reinterpret_cast<PromptUnit*>(ctl + kPrWords);
+  auto length = [&](int s) {
+    const int a = cu[s], e = cu[s + 1];
+    return a >= 0 && a <= e && e <= num_tokens ? e - a : -1;
+  };
+  if (threadIdx.x == 0) ctl[kPrStatus] = GB_OK;
+  __syncthreads();
+  int mine = 0;
+  bool bad = false;
+  for (int s = threadIdx.x; s < num_seqs; s += kListThreads) {
+    const int n = length(s);
+    bad |= n < 0;
+    mine += n > 0 ? (n + tokens - 1) / tokens : 0;
+  }
+  int all;
+  block_exclusive_scan(mine, sm.tmp, &all);
+  if (bad) ctl[kPrStatus] = GB_ERR_INVALID;
+  const int per = all <= few ? small_tokens : tokens;
+  const int n = emit_sorted(
+      sm, num_seqs, [&](int s) { return (max(length(s), 0) + per - 1) / per; },
+      [&](int s, int i) { return (min((i + 1) * per, length(s)) + flash::kTok - 1) / flash::kTok; },
+      [&](int s, int i, int at) {
+        if (at >= max_units) return;
+        const int len = length(s);
+        units[at] = {cu[s], len, i * per, min(per, len - i * per)};
+      });
+  if (threadIdx.x == 0) {
+    ctl[kPrUnits] = min(n, max_units);
+    ctl[kPrNext] = 0;
+  }
+}
+
+struct PromptView {
+  int* ctl;
+  int Hkv, G, num_tokens;
+  float qscale;
+  long long q_stride, k_stride, v_stride, out_stride;  // elements between tokens
+};
+
+struct PromptJob : PromptView {
+  CUtensorMap tq, tk, tv;
+  const __nv_bfloat16 *q, *k, *v;
+  __nv_bfloat16* o;
+
+  static constexpr int kQArrivals = 1;
+  // Tiles land as [half of D][128 tokens][64 dims].
+  static constexpr int kKHalf = 16384, kKSbo = 1024, kVLbo = 16384, kVSbo = 1024, kVStep = 2048;
+  static __device__ __forceinline__ int v_row(int row, int half) { return half * 16384 + row * 128; }
+
+  struct Row {
+    int tok;        // row r's token in its sequence
+    int head;       // its query head
+    int first;      // the warp's first token
+    bool valid;
+  };
+
+  __device__ __forceinline__ void error(int code) const { atomicCAS(&ctl[kPrStatus], GB_OK, code); }
+  __device__ __forceinline__ int total() const { return ctl[kPrUnits] * Hkv; }
+  __device__ __forceinline__ int ticket() const { return atomicAdd(&ctl[kPrNext], 1); }
+  __device__ __forceinline__ void unit(int id, flash::Unit& x) const {
+    const PromptUnit e = reinterpret_cast<const PromptUnit*>(ctl + kPrWords)[id / Hkv];
+    x.head = id % Hkv;
+    x.nt = (e.t0 + e.ntok + flash::kTok - 1) / flash::kTok;
+    x.dual = e.ntok * G > flash::kRows;
+    x.w[0] = e.start;
+    x.w[1] = e.t0;
+    x.w[2] = e.ntok;
+    x.w[3] = e.len;
+  }
+  // A tile's rows past the sequence are the next one's, or past the tensor and zeros.
+  __device__ __forceinline__ void stale_rows(const flash::Unit&, int, int&, int&) const {}
+  __device__ __forceinline__ void load_tile(const flash::Unit& x, int j, int kv, uint32_t dst, uint32_t bar,
+                                            int lane) const {
+    if (lane == 0) tma4(dst, kv ? &tv : &tk, 0, x.w[0] + j * flash::kTok, 0, x.head, bar);
+  }
+  static __device__ __forceinline__ void tma4(uint32_t dst, const CUtensorMap* tm, int c0, int c1, int c2, int c3,
+                                              uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(
+            dst),
+        "l"(tm), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar)
+        : "memory");
+  }
+  __device__ __forceinline__ void load_q(const flash::Unit& x, int g, int r, uint32_t dst, uint32_t bar,
+                                         Row& row) const {
+    const int base = x.w[1] + (x.dual ? g * (flash::kRows / G) : 0);
+    row.tok = base + r / G;
+    row.head = x.head * G + r % G;
+    row.first = base + (r & ~31) / G;
+    row.valid = row.tok < x.w[1] + x.w[2];
+    if (r == 0) {
+      mbar_arrive_expect_tx(bar, flash::kTile);
+      tma4(dst, &tq, 0, x.head * G, x.w[0] + base, 0, bar);
+    }
+  }
+  __device__ __forceinline__ flash::Sees sees(const flash::Unit&, const Row& row, int t) const {
+    const int k0 = t * flash::kTok;
+    return {k0 + flash::kTok - 1 <= row.first, row.tok - k0 + 1, 0ull};
+  }
+  __device__ __forceinline__ void out(const flash::Unit& x, const Row& row, uint32_t a, uint32_t b, bool two, float wa,
+                                      float wb, int c0, int cols, float m, float l) const {
+    const float inv = 1.f / l;
+    __nv_bfloat16* dst = o + (x.w[0] + row.tok) * out_stride + row.head * flash::kD + c0;
+    bool fine = true;
+#pragma unroll 1
+    for (int c = 0; c < cols; c += 32) {
+      float f[32];
+      flash::read_o(a + c, b + c, two, wa, wb, f);
+      uint32_t u[16];
+#pragma unroll
+      for (int i = 0; i < 32; i += 2) {
+        const float f0 = f[i] * inv, f1 = f[i + 1] * inv;
+        fine = fine && isfinite(f0) && isfinite(f1);
+        const __nv_bfloat162 p = __floats2bfloat162_rn(f0, f1);
+        u[i / 2] = *reinterpret_cast<const uint32_t*>(&p);
+      }
+      if (row.valid)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          *reinterpret_cast<uint4*>(dst + c + 8 * i) = make_uint4(u[4 * i], u[4 * i + 1], u[4 * i + 2], u[4 * i + 3]);
+    }
+    unsigned redo = __ballot_sync(0xffffffffu, row.valid && !fine && isfinite(m) && isfinite(l));
+    while (redo) {  // see sum_seen
+      const int src = __ffs(redo) - 1;
+      redo &= redo - 1;
+      const int tok = __shfl_sync(0xffffffffu, row.tok, src), head = __shfl_sync(0xffffffffu, row.head, src);
+      const float mr = __shfl_sync(0xffffffffu, m, src), ir = __shfl_sync(0xffffffffu, inv, src);
+      const long long s0 = x.w[0];
+      const __nv_bfloat16 *kh = k + s0 * k_stride + x.head * flash::kD, *vh = v + s0 * v_stride + x.head * flash::kD;
+      bool unseen = false;
+      for (long long j = tok + 1; j < (long long)x.nt * flash::kTok && s0 + j < num_tokens && !unseen; ++j)
+        unseen = flash::not_finite(vh + j * v_stride, c0, cols);
+      if (!unseen) continue;
+      float acc[4];
+      flash::sum_seen(
+          q + (s0 + tok) * q_stride + head * flash::kD, tok + 1,
+          [&](int j, const __nv_bfloat16*& kj, const __nv_bfloat16*& vj) {
+            kj = kh + j * k_stride;
+            vj = vh + j * v_stride;
+            return true;
+          },
+          qscale, mr, c0, cols, acc);
+      const int lane = threadIdx.x & 31, per = cols / 32;
+      for (int i = 0; i < per; ++i)
+        o[(s0 + tok) * out_stride + head * flash::kD + c0 + per * lane + i] = __float2bfloat16(acc[i] * ir);
+    }
+  }
+  __device__ __forceinline__ void drain_q(uint32_t bar, bool aborted) const {
+    // A copy in flight lands before the CTA leaves; without one the barrier's last phase passes at once.
+    if (aborted && (threadIdx.x & 127) == 0) {
+      mbar_wait_bounded(bar, 0, kWaitLimitNs / 16);
+      mbar_wait_bounded(bar, 1, kWaitLimitNs / 16);
+    }
+  }
+};
+
+__global__ void __launch_bounds__(flash::kThreads, 1) k_prompt(const __grid_constant__ PromptJob job) {
+  extern __shared__ __align__(1024) unsigned char sm[];
+  flash::body(job, sm);
+}
+
+// fp32: a CTA per (unit, KV head).
+struct PromptTile {
+  const float *qp, *kp, *vp;  // the sequence's first row, this head
+  float* op;
+  long long q_stride, k_stride, v_stride, out_stride;
+  int G, t0, ntok;
+  __device__ __forceinline__ int tok(int r) const { return t0 + r / G; }
+  __device__ __forceinline__ bool valid(int r) const { return r / G < ntok; }
+  __device__ __forceinline__ const float* q(int r) const {
+    return valid(r) ? qp + tok(r) * q_stride + (r % G) * kTileD : nullptr;
+  }
+  __device__ __forceinline__ const float* key(int j) const { return kp + j * k_stride; }
+  __device__ __forceinline__ const float* val(int j) const { return vp + j * v_stride; }
+  __device__ __forceinline__ bool on(int r, int j) const { return j <= tok(r); }
+  __device__ __forceinline__ void out(int r, int c, float4 o, float, float l) const {
+    if (!valid(r)) return;
+    const float inv = 1.f / l;
+    *reinterpret_cast<float4*>(op + tok(r) * out_stride + (r % G) * kTileD + c) =
+        make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+  }
+};
+
+__global__ void __launch_bounds__(kTileThreads) k_prompt_f32(PromptView p, const float* q, const float* k,
+                                                             const float* v, float* o) {
+  pdl_wait();
+  pdl_launch_dependents();
+  extern __shared__ __align__(16) unsigned char raw[];
+  TileSmem& sm = *reinterpret_cast<TileSmem*>(raw);
+  const int total = p.ctl[kPrUnits] * p.Hkv;
+  for (int id = blockIdx.x; id < total; id += gridDim.x) {
+    const PromptUnit e = reinterpret_cast<const PromptUnit*>(p.ctl + kPrWords)[id / p.Hkv];
+    const int h = id % p.Hkv;
+    const long long s0 = e.start;
+    const PromptTile src{q + s0 * p.q_stride + h * p.G * kTileD,
+                         k + s0 * p.k_stride + h * kTileD,
+                         v + s0 * p.v_stride + h * kTileD,
+                         o + s0 * p.out_stride + h * p.G * kTileD,
+                         p.q_stride, p.k_stride, p.v_stride, p.out_stride, p.G, e.t0, e.ntok};
+    tile_attention(sm, src, e.t0 + e.ntok, p.qscale);
+    __syncthreads();
+  }
+}
+
+// The rows of a unit: two tiles of 128 for the tensor cores, or one where few units leave SMs without
+// work; 64 for the CUDA cores.
+int unit_tokens(int dtype, int G) { return (dtype == GB_BF16 ? 2 * flash::kRows : kTileRows) / G; }
+
+bool shape_ok(int dtype, int D, int Hq, int Hkv) {
+  const int G = Hkv > 0 && Hq > 0 && Hq % Hkv == 0 ? Hq / Hkv : 0;
+  return (G == 1 || G == 2 || G == 4 || G == 8 || G == 16) &&
+         ((dtype == GB_BF16 && D == flash::kD) || (dtype == GB_F32 && D == kTileD));
+}
+
+long long max_units(int dtype, int G, int num_tokens, int num_seqs) {
+  const int least = dtype == GB_BF16 ? flash::kRows / G : kTileRows / G;
+  return (long long)num_tokens / least + num_seqs;
+}
+
+}  // namespace
+}  // namespace gb
+
+using namespace gb;
+
+extern "C" gb_status gb_prompt_workspace_bytes(int num_tokens, int num_seqs, int num_q_heads, int num_kv_heads,
+                                               int head_dim, int dtype, size_t* bytes) {
+  if (!bytes || num_tokens < 0 || num_seqs < 0 || num_kv_heads < 1 || num_q_heads < 1 || num_q_heads % num_kv_heads)
+    return GB_ERR_INVALID;
+  if (dtype != GB_F32 && dtype != GB_BF16) return GB_ERR_INVALID;
+  if (!shape_ok(dtype, head_dim, num_q_heads, num_kv_heads)) return GB_ERR_UNSUPPORTED;
+  const long long n = max_units(dtype, num_q_heads / num_kv_heads, num_tokens, num_seqs);
+  if (n * num_kv_heads >= (1ll << 31)) return GB_ERR_TOO_LARGE;
+  *bytes = (size_t)(kPrWords * sizeof(int) + n * sizeof(PromptUnit) + 255) & ~(size_t)255;
+  return GB_OK;
+}
+
+namespace {
+
+bool aligned(const void* p, int64_t stride, int esize) { return !((uintptr_t)p & 15) && !((stride * esize) & 15); }
+
+// [first, last) byte addresses of `rows` rows of `width` elements.
+bool meets(const void* a, int64_t as, int aw, const void* b, int64_t bs, int bw, int rows, int esize) {
+  const uintptr_t a0 = (uintptr_t)a, b0 = (uintptr_t)b;
+  const uintptr_t a1 = a0 + ((uintptr_t)(rows - 1) * as + aw) * esize, b1 = b0 + ((uintptr_t)(rows - 1) * bs + bw) * esize;
+  return a0 < b1 && b0 < a1;
+}
+
+}  // namespace
+
+extern "C" gb_status gb_prompt_attention(const gb_prompt_args* a, gb_stream_t stream) {
+  if (!a) return GB_ERR_INVALID;
+  size_t need = 0;
+  const gb_status st = gb_prompt_workspace_bytes(a->num_tokens, a->num_seqs, a->num_q_heads, a->num_kv_heads,
+                                                 a->head_dim, a->dtype, &need);
+  if (st != GB_OK) return st;
+  if (!a->workspace || ((uintptr_t)a->workspace & 255) || a->workspace_bytes < need || !a->cu_seqlens ||
+      !(a->scale > 0.f) || a->scale > 3e38f)
+    return GB_ERR_INVALID;
+  if (a->num_tokens == 0) return GB_OK;
+  const int es = a->dtype == GB_BF16 ? 2 : 4, D = a->head_dim, qw = a->num_q_heads * D, kw = a->num_kv_heads * D;
+  if (!a->q || !a->k || !a->v || !a->out || a->q_stride < qw || a->k_stride < kw || a->v_stride < kw ||
+      a->out_stride < qw || !aligned(a->q, a->q_stride, es) || !aligned(a->k, a->k_stride, es) ||
+      !aligned(a->v, a->v_stride, es) || !aligned(a->out, a->out_stride, es))
+    return GB_ERR_INVALID;
+  const int64_t widest = std::max(std::max(a->q_stride, a->k_stride), std::max(a->v_stride, a->out_stride));
+  if (widest > (int64_t)1 << 31) return GB_ERR_INVALID;
+  if (meets(a->out, a->out_stride, qw, a->q, a->q_stride, qw, a->num_tokens, es) ||
+      meets(a->out, a->out_stride, qw, a->k, a->k_stride, kw, a->num_tokens, es) ||
+      meets(a->out, a->out_stride, qw, a->v, a->v_stride, kw, a->num_tokens, es))
+    return GB_ERR_INVALID;
+  int device = 0, sms = 0;
+  if (cudaGetDevice(&device) != cudaSuccess ||
+      cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess)
+    return GB_ERR_CUDA;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  const int G = a->num_q_heads / a->num_kv_heads, tokens = unit_tokens(a->dtype, G);
+  int* ctl = static_cast<int*>(a->workspace);
+  // Few units (a short prompt): half the rows each, so that twice as many SMs have work and a unit's two
+  // groups share its keys.
+  const int few = a->dtype == GB_BF16 ? sms / a->num_kv_heads : 0;
+  const long long most = max_units(a->dtype, G, a->num_tokens, a->num_seqs);
+  PromptView view{ctl, a->num_kv_heads, G, a->num_tokens, a->scale * 1.4426950408889634f,
+                  a->q_stride, a->k_stride, a->v_stride, a->out_stride};
+  // The tensor maps first: nothing is enqueued when one cannot be made.
+  PromptJob job;
+  if (a->dtype == GB_BF16) {
+    static_cast<PromptView&>(job) = view;
+    job.q = static_cast<const __nv_bfloat16*>(a->q);
+    job.k = static_cast<const __nv_bfloat16*>(a->k);
+    job.v = static_cast<const __nv_bfloat16*>(a->v);
+    job.o = static_cast<__nv_bfloat16*>(a->out);
+    const cuuint64_t n = (cuuint64_t)a->num_tokens;
+    const cuuint64_t qd[4] = {64, (cuuint64_t)a->num_q_heads, n, 2}, kd[4] = {64, n, 2, (cuuint64_t)a->num_kv_heads};
+    const cuuint64_t qs[3] = {256, (cuuint64_t)a->q_stride * 2, 128};
+    const cuuint64_t ks[3] = {(cuuint64_t)a->k_stride * 2, 128, 256}, vs[3] = {(cuuint64_t)a->v_stride * 2, 128, 256};
+    const cuuint32_t qb[4] = {64, (cuuint32_t)G, (cuuint32_t)(flash::kRows / G), 2}, kb[4] = {64, flash::kTok, 2, 1};
+    if (!encode_tensor_map(&job.tq, a->q, 4, qd, qs, qb) || !encode_tensor_map(&job.tk, a->k, 4, kd, ks, kb) ||
+        !encode_tensor_map(&job.tv, a->v, 4, kd, vs, kb))
+      return GB_ERR_CUDA;
+  }
+  if (launch_pdl(k_prompt_plan, 1, kListThreads, 0, s, a->cu_seqlens, a->num_seqs, a->num_tokens, tokens,
+                 few ? flash::kRows / G : tokens, few, (int)most, ctl) != cudaSuccess)
+    return GB_ERR_CUDA;
+  cudaError_t e;
+  if (a->dtype == GB_BF16) {
+    e = set_max_dynamic_smem(reinterpret_cast<const void*>(k_prompt), flash::kSmem);
+    if (e == cudaSuccess) e = launch_pdl(k_prompt, (unsigned)std::min<long long>(sms, most * a->num_kv_heads), flash::kThreads, flash::kSmem, s, job);
+  } else {
+    e = set_max_dynamic_smem(reinterpret_cast<const void*>(k_prompt_f32), (int)sizeof(TileSmem));
+    if (e == cudaSuccess)
+      e = launch_pdl(k_prompt_f32, (unsigned)std::min<long long>(most * a->num_kv_heads, sms * 16), kTileThreads,
+                     sizeof(TileSmem), s, view, static_cast<const float*>(a->q), static_cast<const float*>(a->k),
+                     static_cast<const float*>(a->v), static_cast<float*>(a->out));
+  }
+  return e == cudaSuccess ? GB_OK : GB_ERR_CUDA;
+}
+
+extern "C" gb_status gb_prompt_status(const void* workspace_dev, int* device_status, gb_stream_t stream) {
+  if (!workspace_dev || !device_status) return GB_ERR_INVALID;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  int v = GB_OK;
+  if (cudaMemcpyAsync(&v, static_cast<const int*>(workspace_dev) + kPrStatus, sizeof(int), cudaMemcpyDeviceToHost, s) !=
+          cudaSuccess ||
+      cudaStreamSynchronize(s) != cudaSuccess)
+    return GB_ERR_CUDA;
+  *device_status = v;
+  return GB_OK;
+}

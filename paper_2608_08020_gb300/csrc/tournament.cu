@@ -691,6 +691,7 @@ cudaError_t launch_prune_branch(gb_pool* pool, int K, int fanout, int warmup, co
   a.pruned_out = pruned_out;
   a.lineage_out = reinterpret_cast<unsigned*>(lineage_out);
   pool->launches += 1;
+  ++pool->epoch;
   return launch_pdl(k_tournament, tournament_grid(pool), kTourThreads, 0, s, pool->view, a);
 }
 
@@ -704,6 +705,7 @@ cudaError_t launch_forks(gb_pool* pool, const int32_t* parent_of, cudaStream_t s
   TourArgs a{};
   a.parent_of = parent_of;
   pool->launches += 1;
+  ++pool->epoch;
   return launch_pdl(k_tournament, tournament_grid(pool), kTourThreads, 0, s, pool->view, a);
 }
 

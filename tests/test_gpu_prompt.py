@@ -1,0 +1,95 @@
+"""Attention over packed prompts against the definition in 64 bits.
+
+Bounds, elementwise, with A = sum_j p_j |v_j|: bf16 rounds each p and the result by at most eps / 2 = 2^-8 of
+the value, so |err| <= 2^-8 (A + |o|); the sums in fp32 and the exponentials (2^-22 relative in ex2, and
+an exponent off by 2^-23 of its size, |exponent| <= 64 here) stay below 2e-5 A.  fp32: the scores' sums of 64
+products and the exponents are off by at most 64 x 2^-24 x sum |q k| (below 2e-5 here), so 4e-5 A."""
+import math
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+
+def attend(q, k, v, cu, scale):
+    """(out, sum p |v|) in 64 bits, sequence by sequence; zeros outside them."""
+    import torch
+    o = torch.zeros(q.shape, dtype=torch.float64, device=q.device)
+    a = torch.zeros_like(o)
+    g = q.shape[1] // k.shape[1]
+    for s, e in zip(cu, cu[1:]):
+        n = e - s
+        if n <= 0:
+            continue
+        kk, vv = (x[s:e].double().repeat_interleave(g, 1).transpose(0, 1) for x in (k, v))
+        x = q[s:e].double().transpose(0, 1) @ kk.transpose(1, 2) * scale
+        x.masked_fill_(torch.ones(n, n, dtype=torch.bool, device=q.device).triu(1), -math.inf)
+        p = torch.softmax(x, -1)
+        o[s:e] = (p @ vv).transpose(0, 1)
+        a[s:e] = (p @ vv.abs()).transpose(0, 1)
+    return o, a
+
+
+def bound(o, a, dtype):
+    return (a + o.abs()) * 2.0 ** -8 + 2e-5 * a if dtype == "bf16" else 4e-5 * a
+
+
+def make(dtype, total, hq, hkv, seed, fused=False, scale_q=1.0):
+    import torch
+    from paper_2608_08020_gb300.pool import TORCH_DT
+    d = 128 if dtype == "bf16" else 64
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    x = torch.randn(total, hq + 2 * hkv, d, generator=g, device="cuda")
+    x[:, :hq] *= scale_q
+    x = x.to(TORCH_DT[dtype])
+    parts = x.split([hq, hkv, hkv], 1)
+    return parts if fused else [t.contiguous() for t in parts]
+
+
+def run(dtype, lengths, hq, hkv, *, seed=0, fused=False, pad=0, scale=None, scale_q=1.0):
+    import torch
+    from paper_2608_08020_gb300.prompt import PromptAttention
+    cu = [0]
+    for n in lengths:
+        cu.append(cu[-1] + n)
+    total = cu[-1] + pad
+    q, k, v = make(dtype, total, hq, hkv, seed, fused, scale_q)
+    d = q.shape[2]
+    scale = 1 / math.sqrt(d) if scale is None else scale
+    op = PromptAttention(hq, hkv, d, dtype, max_tokens=total, max_seqs=len(lengths))
+    out = torch.full((total, hq, d), 7.0, dtype=q.dtype, device="cuda")
+    assert op(q, k, v, torch.tensor(cu, dtype=torch.int32, device="cuda"), scale, out) is out
+    assert op.status() == 0
+    o, a = attend(q, k, v, cu, scale)
+    err = (out.double() - o).abs()[:cu[-1]]
+    lim = bound(o, a, dtype)[:cu[-1]]
+    assert bool((err <= lim).all()), float((err / lim).nan_to_num(9e9).max())
+    assert bool((out[cu[-1]:] == 7).all())
+    return out
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [1, 2, 31, 63, 64, 65, 127, 128, 129, 255, 256, 257, 500, 1025])
+def test_one_prompt(cuda, dtype, n):
+    run(dtype, [n], 8, 2, seed=n)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("hq,hkv", [(1, 1), (5, 5), (2, 1), (6, 3), (32, 8), (8, 1), (16, 1)])
+def test_head_layouts(cuda, dtype, hq, hkv):
+    run(dtype, [1, 40, 0, 300, 17, 129], hq, hkv, seed=hq, fused=True, pad=5)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_packed(cuda, dtype):
+    run(dtype, [0, 0, 3, 700, 1, 1, 64, 0, 1300, 128, 33, 0], 16, 4, seed=3, pad=200)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_many_short_sequences(cuda, dtype):
+    run(dtype, [i % 4 for i in range(2500)], 4, 2, seed=4)
+
+
+@pytest.mark.parametrize("scale_q", [0.0, 1e-3, 6.0])
+def test_flat_and_sharp_scores(cuda, scale_q):
+    run("bf16", [900], 8, 2, seed=5, scale_q=scale_q)
