@@ -537,6 +537,79 @@ gb_status gb_prompt_attention(const gb_prompt_args* args, gb_stream_t stream);
  */
 gb_status gb_prompt_status(const void* workspace_dev, int* device_status, gb_stream_t stream);
 
+/*
+ * Trees of drafted tokens (speculative decoding over the beams).  A round: a drafter proposes up to
+ * n_draft tokens for every active slot, each the continuation of the context or of an earlier
+ * drafted token; the model runs them all at once (gb_draft_attention, layer by layer); the caller picks a
+ * path; gb_accept_draft appends it.  Drafted keys and values stay in the caller's arrays until then: the
+ * pool does not change, and what is rejected costs no page.  (One decode step of Algorithm 1's "Generate"
+ * then advances every trace by several tokens.)
+ *   parent_dev:  int32 [max_beams][n_draft]: token i's parent, an earlier token of the slot, or -1
+ *                for the context's end; an entry that is neither records GB_ERR_INVALID in the device status
+ *                and counts as -1
+ *   count_dev:   int32 [max_beams] drafted tokens of each slot, 0 .. n_draft, or NULL for n_draft each;
+ *                a count out of range records GB_ERR_INVALID and is clamped
+ *   n_draft:     1 .. 64, the second dimension of every array below
+ *   workspace_dev: gb_draft_workspace_bytes, 256-byte aligned, the caller's; calls using one workspace
+ *                must be ordered, and a round uses one
+ */
+typedef struct {
+  const int32_t* parent_dev;
+  const int32_t* count_dev;
+  void* workspace_dev;
+  size_t workspace_bytes;
+  int n_draft;
+} gb_draft;
+
+/* Workspace of a pool's draft rounds of n_draft tokens (work lists and partial results). */
+gb_status gb_draft_workspace_bytes(gb_pool* pool, int n_draft, size_t* bytes);
+
+/*
+ * Attention of one layer for every drafted token of every active slot:
+ *   out[b][i][h] = sum_j p_j v_j,  p = softmax_j(scale * q[b][i][h] . k_j)
+ * over the tokens j of slot b's context (this layer's pages) and over i and its ancestors.
+ *   q_dev, out_dev: [max_beams][n_draft][Hq][D] in kv_dtype;  k_dev, v_dev: [max_beams][n_draft][Hkv][D]
+ * all 16-byte aligned, out_dev apart from the others.  Rows of inactive slots and of tokens from the
+ * count on are zero in out_dev and ignored in the inputs; values that a row does not see do not reach its
+ * result, whatever they are.  The pool's contexts are not changed.
+ * Layer 0 plans the round; the other layers may follow in any order, and again, until the pool changes
+ * (append, decode, accept, truncate, fork, prune, release).  Launches: the attention and the join of its partial
+ * results, for layer 0 the planner first.
+ * Errors: GB_ERR_INVALID for bad sizes, pointers or a scale that is not positive and finite; GB_ERR_STATE for an unseeded pool,
+ * inside an open step, a layer above 0 without a plan, or when the pool is on another device than the current one.
+ */
+gb_status gb_draft_attention(gb_pool* pool, int layer, const gb_draft* draft, const void* q_dev, const void* k_dev,
+                             const void* v_dev, float scale, void* out_dev, gb_stream_t stream);
+
+/*
+ * Append the accepted path of every active slot, every layer: the tokens from the tree's root to
+ * token accepted_dev[b] (int32 [max_beams]; -1: none), in that order, at the slot's next positions.
+ *   k_dev, v_dev:  [num_layers][max_beams][n_draft][Hkv][D] in kv_dtype, 16-byte aligned
+ *   count_out_dev: int32 [max_beams] tokens appended (may be NULL)
+ *   path_out_dev:  int32 [max_beams][n_draft] the path, then -1 (may be NULL)
+ * Pages as a sequence of decode steps would take them, the k-th advancing the slots whose path has a
+ * k-th token: lowest free page first, slots ascending, a shared partial tail page copied first.  Slots
+ * whose path is empty are unchanged.  Two launches.
+ * Errors: as gb_draft_attention; out of pages, or a block table that is full, is recorded as GB_ERR_OOM in the
+ * device status and nothing is appended to any slot; a slot whose accepted token is no token of its tree, or whose
+ * tree has a bad parent, is left out (GB_ERR_INVALID in the device status).
+ */
+gb_status gb_accept_draft(gb_pool* pool, const gb_draft* draft, const void* k_dev, const void* v_dev,
+                          const int32_t* accepted_dev, int32_t* count_out_dev, int32_t* path_out_dev,
+                          gb_stream_t stream);
+
+/*
+ * Cut contexts short: active slot b keeps its first lengths_dev[b] tokens (int32 [max_beams]; negative: all of
+ * them), drops its references to the pages past them (pages reaching 0 become free), and gen falls by as many
+ * tokens, to 0 at least.  Rewinds a trace to an earlier thought boundary, or takes accepted tokens back.
+ * A slot cut inside a page that other slots hold gets its own copy of the page's rows (every layer; the lowest
+ * free page, slots ascending); where all of a page's holders are cut inside it the last one keeps it.
+ * Running means are left.  Errors: GB_ERR_STATE for an unseeded pool, an open step or another device; a length above
+ * the slot's records GB_ERR_INVALID in the device status and leaves the slot; GB_ERR_OOM is recorded, and nothing cut,
+ * unless the pool has a free page before the call for every slot cut inside a page that then has several holders.
+ */
+gb_status gb_truncate(gb_pool* pool, const int32_t* lengths_dev, gb_stream_t stream);
+
 /* Short description of the pool's last host-side failure ("" if none); static storage. */
 const char* gb_last_error(gb_pool* pool);
 

@@ -34,6 +34,7 @@ This module is oracle code (test infrastructure), see ``oracle/__init__.py``.
 """
 from __future__ import annotations
 
+import copy
 import heapq
 
 import numpy as np
@@ -237,6 +238,66 @@ class PoolOracle:
             self.seq_len[s] = 0
             self.gen[s] = 0
             self.history[s] = []
+
+    def accept(self, counts) -> bool:
+        """Append counts[slot] tokens to each active slot (an accepted drafted path): as decode steps, the k-th
+        advancing the slots that have a k-th token; all or nothing."""
+        trial = copy.deepcopy(self)
+        todo = [int(c) if self.active[s] else 0 for s, c in enumerate(counts)]
+        for k in range(max(todo, default=0)):
+            for b in (s for s, c in enumerate(todo) if c > k):
+                L = int(trial.seq_len[b])
+                new_page = L % trial.P == 0
+                if (new_page and L // trial.P >= trial.max_pages) or not trial._grow(b, L, new_page):
+                    self._set_error(ERR_OOM)
+                    return False
+                trial.seq_len[b] = L + 1
+                trial.gen[b] += 1
+        self.__dict__ = trial.__dict__
+        return True
+
+    def _grow(self, b: int, L: int, new_page: bool) -> bool:
+        """The page of slot b's position L, a shared tail page copied first; False without a free page."""
+        if not new_page and self.refcnt[self.tables[b][L // self.P]] == 1:
+            return True
+        if not self._free:
+            return False
+        page = self._alloc()
+        if new_page:
+            self.tables[b].append(page)
+        else:
+            self.refcnt[self.tables[b][L // self.P]] -= 1
+            self.tables[b][L // self.P] = page
+        return True
+
+    def truncate(self, lengths) -> bool:
+        """Each active slot keeps its first lengths[slot] tokens (negative: all).  The pages past them lose a reference
+        first; then, in slot order, a slot cut inside a page that others hold gets a copy of it.  Nothing changes
+        unless there is a free page for every slot cut inside a page with several holders."""
+        cut = {}
+        for s, n in enumerate(int(x) for x in lengths):
+            if self.active[s] and n > self.seq_len[s]:
+                self._set_error(ERR_INVALID)
+            elif self.active[s] and 0 <= n < self.seq_len[s]:
+                cut[s] = n
+        inside = [s for s, n in cut.items() if n % self.P and self.refcnt[self.tables[s][n // self.P]] > 1]
+        if len(inside) > self.num_free():
+            self._set_error(ERR_OOM)
+            return False
+        for s, n in cut.items():
+            keep = -(-n // self.P)
+            for p in self.tables[s][keep:]:
+                self._unref(p)
+            del self.tables[s][keep:]
+            self.gen[s] = max(0, self.gen[s] - (self.seq_len[s] - n))
+            self.seq_len[s] = n
+        for s in sorted(inside):
+            old = self.tables[s][-1]
+            if self.refcnt[old] > 1:
+                page = self._alloc()
+                self.refcnt[old] -= 1
+                self.tables[s][-1] = page
+        return True
 
     # -- invariants ----------------------------------------------------------
     def check_invariants(self) -> None:

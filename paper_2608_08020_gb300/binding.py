@@ -29,7 +29,8 @@ EXPORTS = ["gb_pool_workspace_bytes", "gb_pool_init", "gb_pool_destroy", "gb_poo
            "gb_append_kv", "gb_score_probe", "gb_push_scores", "gb_prune_branch", "gb_release", "gb_pool_status",
            "gb_pool_clear_status", "gb_pool_wait_selftest", "gb_pool_read_state", "gb_pool_set_profile_events", "gb_pool_launch_count",
            "gb_paged_decode_noalloc", "gb_paged_decode_noalloc_status", "gb_pool_read_step_stats", "gb_pool_set_capacity", "gb_pool_last_ranked", "gb_score_mlp", "gb_fork_slots", "gb_scorer_sizes", "gb_scorer_seed",
-           "gb_scorer_step", "gb_prompt_workspace_bytes", "gb_prompt_attention", "gb_prompt_status", "gb_last_error"]
+           "gb_scorer_step", "gb_prompt_workspace_bytes", "gb_prompt_attention", "gb_prompt_status",
+           "gb_draft_workspace_bytes", "gb_draft_attention", "gb_accept_draft", "gb_truncate", "gb_last_error"]
 GB_PROF_DECODE, GB_PROF_PROBE, GB_PROF_PRUNE, GB_PROF_GROUPED = 0, 1, 2, 3
 GB_PROF_PLAN, GB_PROF_APPEND, GB_PROF_COMBINE, GB_PROF_ATTENTION = 4, 5, 6, 7
 
@@ -63,6 +64,11 @@ class GbPromptArgs(ctypes.Structure):
                 ("out_stride", ctypes.c_int64), ("num_seqs", ctypes.c_int), ("num_tokens", ctypes.c_int),
                 ("num_q_heads", ctypes.c_int), ("num_kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int),
                 ("dtype", ctypes.c_int), ("scale", ctypes.c_float)]
+
+
+class GbDraft(ctypes.Structure):
+    _fields_ = [("parent_dev", ctypes.c_void_p), ("count_dev", ctypes.c_void_p), ("workspace_dev", ctypes.c_void_p),
+                ("workspace_bytes", ctypes.c_size_t), ("n_draft", ctypes.c_int)]
 
 
 class GambitError(RuntimeError):
@@ -114,6 +120,10 @@ def load(path: Path | None = None) -> ctypes.CDLL:
         "gb_prompt_workspace_bytes": [I, I, I, I, I, I, P],
         "gb_prompt_attention": [P, V],
         "gb_prompt_status": [V, P, V],
+        "gb_draft_workspace_bytes": [V, I, P],
+        "gb_draft_attention": [V, I, P, V, V, V, F, V, V],
+        "gb_accept_draft": [V, P, V, V, V, V, V, V],
+        "gb_truncate": [V, V, V],
         "gb_last_error": [V],
     }
     for name, args in sig.items():
@@ -350,6 +360,26 @@ def gb_prompt_status(workspace, stream=None) -> int:
     st = ctypes.c_int()
     _check(None, load().gb_prompt_status(ptr(workspace), ctypes.byref(st), stream_handle(stream)), "gb_prompt_status")
     return st.value
+
+
+def gb_draft_workspace_bytes(pool: int, n_draft: int) -> int:
+    n = ctypes.c_size_t()
+    _check(pool, load().gb_draft_workspace_bytes(pool, n_draft, ctypes.byref(n)), "gb_draft_workspace_bytes")
+    return n.value
+
+
+def gb_draft_attention(pool: int, layer: int, draft: GbDraft, q, k, v, scale: float, out, stream=None) -> None:
+    _check(pool, load().gb_draft_attention(pool, layer, ctypes.byref(draft), ptr(q), ptr(k), ptr(v), float(scale),
+                                           ptr(out), stream_handle(stream)), "gb_draft_attention")
+
+
+def gb_accept_draft(pool: int, draft: GbDraft, k, v, accepted, count_out=None, path_out=None, stream=None) -> None:
+    _check(pool, load().gb_accept_draft(pool, ctypes.byref(draft), ptr(k), ptr(v), ptr(accepted), ptr(count_out),
+                                        ptr(path_out), stream_handle(stream)), "gb_accept_draft")
+
+
+def gb_truncate(pool: int, lengths, stream=None) -> None:
+    _check(pool, load().gb_truncate(pool, ptr(lengths), stream_handle(stream)), "gb_truncate")
 
 
 def gb_last_error(pool: int) -> str:

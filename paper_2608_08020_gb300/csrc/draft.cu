@@ -1,0 +1,1081 @@
+// Trees of drafted tokens over a beam pool: their attention (gb_draft_attention), the append of an accepted
+// path (gb_accept_draft) and cutting a beam short (gb_truncate).
+//
+//   out[b][i][h] = sum_j p_j v_j,  p = softmax_j(scale q[b][i][h] . k_j)
+// where j runs over beam b's context (through its block table) and over i and its ancestors in the beam's
+// tree, whose keys and values are the caller's.
+//
+// A round's plan, made with layer 0: every shared-prefix segment's pages are read once for all drafted
+// tokens of the beams that share them (rows (beam, token, query head), 256 to a unit), every beam's remainder
+// and its drafts by units of its own; long runs of keys are split.  A beam whose rows one unit answers gets
+// its result from it; the others' units leave records (sum, maximum, row sum) that k_draft_merge joins.
+// bf16: flash.cuh; fp32: tile.cuh, without segments.
+//
+// Bound by the reads of the cache while rows x 2 flops a byte stay below the machine's ~280, i.e. up to some
+// 100 rows a shared token, and by the tensor cores beyond.
+#include <algorithm>
+
+#include "flash.cuh"
+#include "tile.cuh"
+#include "worklist.cuh"
+
+namespace gb {
+namespace {
+
+constexpr int kMaxDraft = 64;   // tokens of a tree: a row's ancestors are one 64-bit word
+constexpr int kTailRec = kMaxSegDepth;  // rec_off column of a beam's own units
+constexpr int kRecOffs = kMaxSegDepth + 1;
+
+// Workspace words of control.
+enum DraftCtl : int { kDrUnits = 0, kDrNext = 1, kDrList = 2, kDrOk = 3, kDrWords = 64 };
+
+struct DraftUnit {
+  int seg;         // -1: a beam's own unit
+  int beam;        // whose table lists the pages
+  int e0, ntok;    // rows: entries [e0, e0 + ntok) of the token list, or the beam's tokens
+  int tok0, tok1;  // context positions
+  int drafts;      // 1: then the drafted tokens
+  int split;       // its record among the beam's for this segment
+};
+
+// Byte offsets of the workspace.
+struct DraftLayout {
+  size_t units, anc, cnt, nrec, rec_base, rec_off, seg_cnt, seg_list, off, list, acc, ml, rec, total;
+  int rec_cap, max_units;
+};
+
+int ws_rows(const gb_pool_config& c, int T) { return T * (c.num_q_heads / c.num_kv_heads); }
+
+DraftLayout draft_layout(const gb_pool_config& c, int num_sms, int T) {
+  DraftLayout d{};
+  const size_t B = (size_t)c.max_beams;
+  size_t o = 0;
+  auto take = [&](size_t bytes) { const size_t at = o; o = (o + bytes + 255) & ~(size_t)255; return at; };
+  // Records: six a beam (shared segments and its own units; the plan stops splitting, then
+  // leaves the deepest segments to the beams, when there would be more), and what splits a few long
+  // beams over all SMs.
+  d.rec_cap = (int)(6 * B) + 2 * num_sms;
+  d.max_units = d.rec_cap * ((ws_rows(c, T) + kTileRows - 1) / kTileRows + 1);
+  take(kDrWords * sizeof(int));
+  d.units = take((size_t)d.max_units * sizeof(DraftUnit));
+  d.anc = take(B * T * sizeof(unsigned long long));
+  d.cnt = take(B * sizeof(int));
+  d.nrec = take(B * sizeof(int));
+  d.rec_base = take(B * sizeof(int));
+  d.rec_off = take(B * kRecOffs * sizeof(int));
+  d.seg_cnt = take(B * kMaxSegDepth * sizeof(int));
+  d.seg_list = take(B * kMaxSegDepth * sizeof(int));
+  d.off = take(B * kMaxSegDepth * sizeof(int));
+  d.list = take(B * kMaxSegDepth * T * sizeof(int));
+  d.acc = take(B * 4 * sizeof(int) + B * sizeof(unsigned long long));
+  const size_t rows = (size_t)d.rec_cap * c.num_kv_heads * ws_rows(c, T);
+  d.ml = take(rows * sizeof(float2));
+  d.rec = take(rows * c.head_dim * sizeof(float));
+  d.total = o;
+  return d;
+}
+
+// The workspace's parts, by value to the kernels.
+struct DraftView {
+  int T, rows;              // tokens of a tree, rows of a beam and KV head (T x G)
+  int rec_cap, max_units;
+  int* ctl;
+  DraftUnit* units;
+  unsigned long long* anc;  // [max_beams][T] ancestors and self
+  int* cnt;                 // [max_beams] drafted tokens, 0 for an inactive slot
+  int* nrec;                // [max_beams] records
+  int* rec_base;            // [max_beams] the first of them
+  int* rec_off;             // [max_beams][kRecOffs] those of the k-th segment, and of the beam's own units
+  int* seg_cnt;             // [segments] drafted tokens of its beams
+  int* seg_list;            // [segments] where its token list begins
+  int* off;                 // [max_beams][kMaxSegDepth] the beam's place in that list
+  int* list;                // beam | depth << 10 | token << 14
+  int* acc_n;               // [max_beams] accept: tokens appended,
+  int* acc_pos;             //   the position of the first,
+  int* acc_old;             //   the shared tail page they moved away from, or -1
+  unsigned long long* acc_path;  // the path's tokens
+  float2* ml;               // [rec_cap][Hkv][rows] (maximum, sum)
+  float* rec;               // [rec_cap][Hkv][rows][D]
+};
+
+DraftView draft_view(const gb_pool* p, const DraftLayout& d, int T, void* ws) {
+  char* m = static_cast<char*>(ws);
+  const size_t B = (size_t)p->cfg.max_beams;
+  DraftView v{};
+  v.T = T;
+  v.rows = ws_rows(p->cfg, T);
+  v.rec_cap = d.rec_cap;
+  v.max_units = d.max_units;
+  v.ctl = reinterpret_cast<int*>(m);
+  v.units = reinterpret_cast<DraftUnit*>(m + d.units);
+  v.anc = reinterpret_cast<unsigned long long*>(m + d.anc);
+  v.cnt = reinterpret_cast<int*>(m + d.cnt);
+  v.nrec = reinterpret_cast<int*>(m + d.nrec);
+  v.rec_base = reinterpret_cast<int*>(m + d.rec_base);
+  v.rec_off = reinterpret_cast<int*>(m + d.rec_off);
+  v.seg_cnt = reinterpret_cast<int*>(m + d.seg_cnt);
+  v.seg_list = reinterpret_cast<int*>(m + d.seg_list);
+  v.off = reinterpret_cast<int*>(m + d.off);
+  v.list = reinterpret_cast<int*>(m + d.list);
+  v.acc_path = reinterpret_cast<unsigned long long*>(m + d.acc);
+  v.acc_n = reinterpret_cast<int*>(v.acc_path + B);
+  v.acc_pos = v.acc_n + B;
+  v.acc_old = v.acc_pos + B;
+  v.ml = reinterpret_cast<float2*>(m + d.ml);
+  v.rec = reinterpret_cast<float*>(m + d.rec);
+  return v;
+}
+
+// A warp's slot b: lane l's masks of tokens l and l + 32 (ancestors and self; 0 from `count` on), by
+// doubling the paths.  A parent that is no earlier token counts as none and makes *bad true.
+__device__ __forceinline__ void ancestors(const int* parent, int T, int count, unsigned long long* lo,
+                                          unsigned long long* hi, bool* bad) {
+  const int lane = threadIdx.x & 31;
+  unsigned long long a[2];
+  int up[2];
+  bool wrong = false;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int i = lane + 32 * k;
+    const bool on = i < count;
+    int p = on ? parent[i] : -1;
+    if (p < -1 || p >= i) {
+      wrong |= on;
+      p = -1;
+    }
+    up[k] = p;
+    a[k] = on ? 1ull << i : 0ull;
+  }
+#pragma unroll
+  for (int s = 0; s < 6; ++s) {  // paths of up to 2^6 tokens
+    unsigned long long na[2];
+    int nu[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int from = up[k] & 31;
+      const unsigned long long a0 = __shfl_sync(0xffffffffu, a[0], from), a1 = __shfl_sync(0xffffffffu, a[1], from);
+      const int u0 = __shfl_sync(0xffffffffu, up[0], from), u1 = __shfl_sync(0xffffffffu, up[1], from);
+      na[k] = up[k] < 0 ? a[k] : a[k] | (up[k] < 32 ? a0 : a1);
+      nu[k] = up[k] < 0 ? -1 : (up[k] < 32 ? u0 : u1);
+    }
+    a[0] = na[0];
+    a[1] = na[1];
+    up[0] = nu[0];
+    up[1] = nu[1];
+  }
+  *lo = a[0];
+  *hi = a[1];
+  *bad = __any_sync(0xffffffffu, wrong);
+}
+
+// Tiles of 128 keys of n context tokens and the drafts: the drafted tokens lie in the second half of the
+// last tile, beside at most 64 context tokens.
+__device__ __forceinline__ int tail_tiles(int n) { return n / flash::kTok + (n % flash::kTok <= 64 ? 1 : 2); }
+
+__device__ __forceinline__ int drafted(const int* count, int b, int T, bool act, bool* bad) {
+  const int n = !act ? 0 : count ? count[b] : T;
+  if (n < 0 || n > T) {
+    *bad = true;
+    return n < 0 ? 0 : T;
+  }
+  return n;
+}
+
+// CTA 0 makes the work list, the others the ancestor masks, a warp per slot.  `tokens`: of a unit's rows;
+// `least`: tiles below which a run of keys is not split.
+__global__ void __launch_bounds__(kListThreads) k_draft_plan(PoolView v, DraftView w, const int* parent,
+                                                             const int* count, int tokens, int least, bool segs) {
+  pdl_wait();
+  pdl_launch_dependents();
+  const int tid = threadIdx.x;
+  if (blockIdx.x > 0) {
+    const int b = (blockIdx.x - 1) * 32 + (tid >> 5), lane = tid & 31;
+    if (b >= v.max_beams) return;
+    bool bad = false;
+    const int n = drafted(count, b, w.T, v.active[b] != 0, &bad);
+    unsigned long long lo, hi;
+    bool wrong;
+    ancestors(parent + (size_t)b * w.T, w.T, n, &lo, &hi, &wrong);
+    if (lane < w.T) w.anc[(size_t)b * w.T + lane] = lo;
+    if (lane + 32 < w.T) w.anc[(size_t)b * w.T + lane + 32] = hi;
+    if ((bad || wrong) && lane == 0) set_status(v.ctl, GB_ERR_INVALID);
+    return;
+  }
+  __shared__ ListSmem sm;
+  __shared__ short s_cnt[kMaxBeams];
+  __shared__ int s_sum;
+  const int b = tid, cap = v.max_beams;
+  const bool act = b < cap && v.active[b] != 0;
+  const int L = act ? v.seq_len[b] : 0;
+  bool bad = false;
+  const int cnt = b < cap ? drafted(count, b, w.T, act, &bad) : 0;
+  const int nseg = segs ? v.ctl[kCtlSegCount] : 0;
+  int nd = segs && cnt > 0 ? v.seg_nseg[b] : 0;
+  s_cnt[b] = (short)cnt;
+  if (b < cap) w.cnt[b] = cnt;
+  if (tid == 0) {
+    w.ctl[kDrList] = 0;
+    w.ctl[kDrNext] = 0;
+  }
+  for (int s = tid; s < nseg; s += kListThreads) w.seg_cnt[s] = 0;
+  // The depth down to which segments are used: a record each, and one for the rest, must fit.
+  int dmax = kMaxSegDepth, all;
+  for (; dmax > 0; --dmax) {
+    block_exclusive_scan(cnt > 0 ? min(nd, dmax) + 1 : 0, sm.tmp, &all);
+    if (all <= w.rec_cap) break;
+  }
+  nd = min(nd, dmax);
+  __syncthreads();
+  // Segments: their drafted tokens, and each beam's place among them.
+  for (int e = tid; e < (segs ? cap * kMaxSegDepth : 0); e += kListThreads) {
+    const int c = s_cnt[e / kMaxSegDepth], k = e % kMaxSegDepth;
+    if (c > 0 && k < min(v.seg_nseg[e / kMaxSegDepth], dmax)) w.off[e] = atomicAdd(&w.seg_cnt[v.seg_bid[e]], c);
+  }
+  int start = 0;
+  for (int k = 0; k < nd; ++k) start += v.seg_len[v.seg_bid[b * kMaxSegDepth + k]] * v.P;
+  const int tail = cnt > 0 ? tail_tiles(L - start) : 0, btiles = (cnt + tokens - 1) / tokens;
+  __threadfence_block();
+  __syncthreads();
+  auto seg_tiles = [&](int s) { return (v.seg_len[s] * v.P + flash::kTok - 1) / flash::kTok; };
+  int work = tail * btiles;
+  for (int s = tid; s < nseg; s += kListThreads) {
+    const int c = w.seg_cnt[s];
+    work += (c + tokens - 1) / tokens * seg_tiles(s);
+    if (c > 0) w.seg_list[s] = atomicAdd(&w.ctl[kDrList], c);
+  }
+  block_exclusive_scan(work, sm.tmp, &all);
+  // Tiles per unit: some units per SM, but not too short ones, and no more records than there is room for.
+  int per = max(least, (int)(((long long)all * v.Hkv + 2 * v.num_sms - 1) / (2 * v.num_sms)));
+  int mine, base;
+  for (;; per *= 2) {
+    mine = cnt > 0 ? (tail + per - 1) / per : 0;
+    for (int k = 0; k < nd; ++k) mine += (seg_tiles(v.seg_bid[b * kMaxSegDepth + k]) + per - 1) / per;
+    base = block_exclusive_scan(mine, sm.tmp, &all);
+    if (all <= w.rec_cap || per > (1 << 24)) break;
+  }
+  if (b < cap) {
+    w.nrec[b] = mine;
+    w.rec_base[b] = base;
+    int at = 0;
+    for (int k = 0; k < nd; ++k) {
+      w.rec_off[b * kRecOffs + k] = at;
+      at += (seg_tiles(v.seg_bid[b * kMaxSegDepth + k]) + per - 1) / per;
+    }
+    w.rec_off[b * kRecOffs + kTailRec] = at;
+  }
+  // The beams' own sizes, for the list's other threads.
+  __shared__ int s_start[kMaxBeams], s_len[kMaxBeams];
+  s_start[b] = start;
+  s_len[b] = L;
+  __syncthreads();
+  struct Piece {
+    int tiles, splits, share, row_tiles, rows;
+  };
+  auto piece = [&](int src) {  // sources: the segments, then the slots
+    Piece p;
+    if (src < nseg) {
+      p.rows = w.seg_cnt[src];
+      p.tiles = p.rows > 0 ? seg_tiles(src) : 0;
+    } else {
+      p.rows = s_cnt[src - nseg];
+      p.tiles = p.rows > 0 ? tail_tiles(s_len[src - nseg] - s_start[src - nseg]) : 0;
+    }
+    p.splits = (p.tiles + per - 1) / per;
+    p.share = p.splits > 0 ? (p.tiles + p.splits - 1) / p.splits : 1;
+    p.row_tiles = (p.rows + tokens - 1) / tokens;
+    return p;
+  };
+  const int n = emit_sorted(
+      sm, nseg + cap,
+      [&](int src) {
+        const Piece p = piece(src);
+        return p.splits * p.row_tiles;
+      },
+      [&](int src, int i) {
+        const Piece p = piece(src);
+        const int sp = i / p.row_tiles, t = i % p.row_tiles;
+        const int rows = min(tokens, p.rows - t * tokens);
+        return (min(p.share, p.tiles - sp * p.share) + 1) * (2 * rows > tokens ? 2 : 1);
+      },
+      [&](int src, int i, int at) {
+        if (at >= w.max_units) return;
+        const Piece p = piece(src);
+        const int sp = i / p.row_tiles, t = i % p.row_tiles;
+        const int rows = max(0, min(tokens, p.rows - t * tokens));
+        DraftUnit u;
+        u.split = sp;
+        u.ntok = rows;
+        if (src < nseg) {
+          const int len = v.seg_len[src] * v.P, first = v.seg_i0[src] * v.P;
+          u.seg = src;
+          u.beam = v.seg_rep[src];
+          u.e0 = w.seg_list[src] + t * tokens;
+          u.tok0 = first + sp * p.share * flash::kTok;
+          u.tok1 = first + min((sp + 1) * p.share * flash::kTok, len);
+          u.drafts = 0;
+        } else {
+          const int beam = src - nseg, n = s_len[beam];
+          u.seg = -1;
+          u.beam = beam;
+          u.e0 = t * tokens;
+          u.tok0 = min(s_start[beam] + sp * p.share * flash::kTok, n);
+          u.tok1 = min(s_start[beam] + (sp + 1) * p.share * flash::kTok, n);
+          u.drafts = sp == p.splits - 1;
+        }
+        w.units[at] = u;
+      });
+  if (tid == 0) w.ctl[kDrUnits] = min(n, w.max_units);
+  // Token lists of the segments.
+  for (int e = tid >> 5; e < (segs ? cap * kMaxSegDepth : 0); e += kListThreads / 32) {
+    const int c = s_cnt[e / kMaxSegDepth], k = e % kMaxSegDepth;
+    if (c == 0 || k >= min(v.seg_nseg[e / kMaxSegDepth], dmax)) continue;
+    int* to = w.list + w.seg_list[v.seg_bid[e]] + w.off[e];
+    for (int i = tid & 31; i < c; i += 32) to[i] = (e / kMaxSegDepth) | k << 10 | i << 14;
+  }
+}
+
+// Where a row's result goes: the output itself when the beam has one record, else its record.
+struct DraftRow {
+  int beam, tok, rec;  // rec: the record, or -1 for the output
+  bool valid;
+};
+__device__ __forceinline__ DraftRow draft_row(const DraftView& w, int seg, int beam, int e, int split, bool valid) {
+  DraftRow r{beam, 0, -1, valid};
+  if (!valid) return r;
+  int k = kTailRec;
+  if (seg >= 0) {
+    const int x = w.list[e];
+    r.beam = x & 1023;
+    k = (x >> 10) & 15;
+    r.tok = x >> 14;
+  } else {
+    r.tok = e;
+  }
+  if (w.nrec[r.beam] > 1) r.rec = w.rec_base[r.beam] + w.rec_off[r.beam * kRecOffs + k] + split;
+  return r;
+}
+
+struct DraftJob {
+  CUtensorMap tp, tk, tv;  // the pool's pages; the drafted keys and values
+  PoolView v;
+  DraftView w;
+  int layer, oob;
+  float qscale;
+  const __nv_bfloat16 *q, *k, *vv;  // this layer's [max_beams][T][heads][128]
+  __nv_bfloat16* o;
+
+  static constexpr int kQArrivals = 4;
+  // Tiles land as [16 groups of 8 tokens][half of D][8][64 dims].
+  static constexpr int kKHalf = 1024, kKSbo = 2048, kVLbo = 1024, kVSbo = 2048, kVStep = 4096;
+  static __device__ __forceinline__ int v_row(int row, int half) {
+    return (row >> 3) * 2048 + half * 1024 + (row & 7) * 128;
+  }
+
+  struct Row : DraftRow {
+    int gg;  // query head of the KV head
+    unsigned long long anc;
+  };
+
+  __device__ __forceinline__ void error(int code) const { set_status(v.ctl, code); }
+  __device__ __forceinline__ int total() const { return w.ctl[kDrUnits] * v.Hkv; }
+  __device__ __forceinline__ int ticket() const { return atomicAdd(&w.ctl[kDrNext], 1); }
+  // Words of a unit: those of its DraftUnit, in order.
+  enum { kSeg, kBeam, kE0, kNtok, kTok0, kTok1, kDrafts, kSplit, kCount };
+  __device__ __forceinline__ void unit(int id, flash::Unit& x) const {
+    const DraftUnit e = w.units[id / v.Hkv];
+    const int n = e.tok1 - e.tok0;
+    x.head = id % v.Hkv;
+    x.nt = e.drafts ? tail_tiles(n) : (n + flash::kTok - 1) / flash::kTok;
+    x.dual = e.ntok * v.G > flash::kRows;
+    x.w[kSeg] = e.seg;
+    x.w[kBeam] = e.beam;
+    x.w[kE0] = e.e0;
+    x.w[kNtok] = e.ntok;
+    x.w[kTok0] = e.tok0;
+    x.w[kTok1] = e.tok1;
+    x.w[kDrafts] = e.drafts;
+    x.w[kSplit] = e.split;
+    x.w[kCount] = e.seg < 0 ? w.cnt[e.beam] : 0;
+  }
+  __device__ __forceinline__ bool draft_tile(const flash::Unit& x, int j) const { return x.w[kDrafts] && j == x.nt - 1; }
+  // Rows of the context's last page past its end hold whatever the pool's memory did.
+  __device__ __forceinline__ void stale_rows(const flash::Unit& x, int j, int& z0, int& z1) const {
+    const int n = x.w[kTok1] - x.w[kTok0] - j * flash::kTok;
+    if (n > 0 && n < flash::kTok && n % v.P) {
+      z0 = n;
+      z1 = (n + v.P - 1) / v.P * v.P;
+    }
+  }
+  static __device__ __forceinline__ void tma5(uint32_t dst, const CUtensorMap* tm, int c1, int c2, int c3, int c4,
+                                              uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(
+            dst),
+        "l"(tm), "r"(0), "r"(c1), "r"(c2), "r"(c3), "r"(c4), "r"(bar)
+        : "memory");
+  }
+  __device__ __forceinline__ void load_tile(const flash::Unit& x, int j, int kv, uint32_t dst, uint32_t bar,
+                                            int lane) const {
+    const int c0 = x.w[kTok0] + j * flash::kTok, at = lane * v.P;
+    const bool last = draft_tile(x, j);
+    if (at < (last ? 64 : flash::kTok)) {
+      int row = oob;
+      if (c0 + at < x.w[kTok1]) {
+        int page = v.tables[(size_t)x.w[kBeam] * v.max_pages + (c0 + at) / v.P];
+        if (page < 0 || page >= v.num_pages) {
+          set_status(v.ctl, GB_ERR_INVALID);
+          page = 0;
+        }
+        row = (int)((((long long)layer * v.num_pages + page) * 2 * v.Hkv + x.head) * v.P / 8);
+      }
+      tma5(dst + lane * v.P * 256, &tp, 0, 0, kv, row, bar);
+    }
+    if (last && lane >= 16 && lane < 24) {
+      const int t = (lane - 16) * 8;
+      tma5(dst + (lane - 8) * 2048, kv ? &tv : &tk, t < x.w[kCount] ? t : kMaxDraft, 0, x.head, x.w[kBeam], bar);
+    }
+  }
+  __device__ __forceinline__ void load_q(const flash::Unit& x, int g, int r, uint32_t dst, uint32_t bar,
+                                         Row& row) const {
+    const int i = (x.dual ? g * flash::kRows + r : r) / v.G;
+    static_cast<DraftRow&>(row) = draft_row(w, x.w[kSeg], x.w[kBeam], x.w[kE0] + i, x.w[kSplit], i < x.w[kNtok]);
+    row.gg = r % v.G;
+    const char* src =
+        reinterpret_cast<const char*>(q + (((size_t)row.beam * w.T + row.tok) * v.Hq + x.head * v.G + row.gg) * flash::kD);
+#pragma unroll
+    for (int c = 0; c < 16; ++c) {
+      const uint32_t to = dst + (c >> 3) * 16384 + swz(r, (c & 7) * 8);
+      if (row.valid)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(src + 16 * c) : "memory");
+      else
+        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(to), "r"(0) : "memory");
+    }
+    row.anc = row.valid && x.w[kDrafts] ? w.anc[(size_t)row.beam * w.T + row.tok] : 0ull;
+    asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory");
+    fence_proxy_async_smem();
+    __syncwarp();
+    if ((r & 31) == 0) mbar_arrive(bar);
+  }
+  __device__ __forceinline__ flash::Sees sees(const flash::Unit& x, const Row& row, int t) const {
+    const int n = x.w[kTok1] - x.w[kTok0] - t * flash::kTok;
+    const bool last = draft_tile(x, t);
+    return {!last && n >= flash::kTok, n, last ? row.anc : 0ull};
+  }
+  __device__ __forceinline__ void out(const flash::Unit& x, const Row& row, uint32_t a, uint32_t b, bool two, float wa,
+                                      float wb, int c0, int cols, float m, float l) const {
+    const bool final = row.rec < 0;
+    const float inv = final ? 1.f / l : 1.f;
+    const int head = x.head * v.G + row.gg;
+    __nv_bfloat16* dst = o + (((size_t)row.beam * w.T + row.tok) * v.Hq + head) * flash::kD + c0;
+    const size_t rr = ((size_t)max(row.rec, 0) * v.Hkv + x.head) * w.rows + row.tok * v.G + row.gg;
+    float* rec = w.rec + rr * flash::kD + c0;
+    bool fine = true;
+#pragma unroll 1
+    for (int c = 0; c < cols; c += 32) {
+      float f[32];
+      flash::read_o(a + c, b + c, two, wa, wb, f);
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
+        f[i] *= inv;
+        fine = fine && isfinite(f[i]);
+      }
+      if (!row.valid) continue;
+      if (final) {
+#pragma unroll
+        for (int i = 0; i < 32; i += 8) {
+          uint32_t u[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const __nv_bfloat162 p = __floats2bfloat162_rn(f[i + 2 * k], f[i + 2 * k + 1]);
+            u[k] = *reinterpret_cast<const uint32_t*>(&p);
+          }
+          *reinterpret_cast<uint4*>(dst + c + i) = make_uint4(u[0], u[1], u[2], u[3]);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 32; i += 4)
+          *reinterpret_cast<float4*>(rec + c + i) = make_float4(f[i], f[i + 1], f[i + 2], f[i + 3]);
+      }
+    }
+    if (row.valid && !final && c0 == 0) w.ml[rr] = make_float2(m, l);
+    unsigned redo = __ballot_sync(0xffffffffu, row.valid && x.w[kDrafts] && !fine && isfinite(m) && isfinite(l));
+    while (redo) {  // see sum_seen; only drafted tokens off the row's path share a tile with what it sees
+      const int src = __ffs(redo) - 1;
+      redo &= redo - 1;
+      const int tok = __shfl_sync(0xffffffffu, row.tok, src), gg = __shfl_sync(0xffffffffu, row.gg, src);
+      const float mr = __shfl_sync(0xffffffffu, m, src), ir = __shfl_sync(0xffffffffu, inv, src);
+      const unsigned long long anc = __shfl_sync(0xffffffffu, row.anc, src);
+      const bool fin = __shfl_sync(0xffffffffu, final, src);
+      const size_t at = __shfl_sync(0xffffffffu, rr, src);
+      const size_t kv0 = ((size_t)x.w[kBeam] * w.T * v.Hkv + x.head) * flash::kD;
+      const int nctx = x.w[kTok1] - x.w[kTok0];
+      bool unseen = false;
+      for (int j = 0; j < min(w.T, (x.w[kCount] + 7) & ~7) && !unseen; ++j)
+        if (!((anc >> j) & 1)) unseen = flash::not_finite(vv + kv0 + (size_t)j * v.Hkv * flash::kD, c0, cols);
+      if (!unseen) continue;
+      const size_t qo = (((size_t)x.w[kBeam] * w.T + tok) * v.Hq + x.head * v.G + gg) * flash::kD;
+      float acc[4];
+      flash::sum_seen(
+          q + qo, nctx + w.T,
+          [&](int j, const __nv_bfloat16*& kj, const __nv_bfloat16*& vj) {
+            if (j >= nctx) {
+              kj = k + kv0 + (size_t)(j - nctx) * v.Hkv * flash::kD;
+              vj = vv + kv0 + (size_t)(j - nctx) * v.Hkv * flash::kD;
+              return ((anc >> (j - nctx)) & 1) != 0;
+            }
+            const int pos = x.w[kTok0] + j, page = v.tables[(size_t)x.w[kBeam] * v.max_pages + pos / v.P];
+            if (page < 0 || page >= v.num_pages) return false;
+            const __nv_bfloat16* pool = reinterpret_cast<const __nv_bfloat16*>(v.kv);
+            kj = pool + kv_elem_offset(v, layer, page, 0, x.head, pos % v.P);
+            vj = pool + kv_elem_offset(v, layer, page, 1, x.head, pos % v.P);
+            return true;
+          },
+          qscale, mr, c0, cols, acc);
+      const int lane = threadIdx.x & 31, per = cols / 32;
+      for (int i = 0; i < per; ++i) {
+        const int c = c0 + per * lane + i;
+        if (fin) o[qo + c] = __float2bfloat16(acc[i] * ir);
+        else w.rec[at * flash::kD + c] = acc[i];
+      }
+    }
+  }
+  __device__ __forceinline__ void drain_q(uint32_t, bool) const {}
+};
+
+__global__ void __launch_bounds__(flash::kThreads, 1) k_draft(const __grid_constant__ DraftJob job) {
+  extern __shared__ __align__(1024) unsigned char sm[];
+  flash::body(job, sm);
+}
+
+// fp32: a CTA per (unit, KV head).
+struct DraftTile {
+  const PoolView& v;
+  const DraftView& w;
+  const DraftUnit& u;
+  int layer, head, nctx;
+  const float *qp, *kp, *vp;
+  float* op;
+  __device__ __forceinline__ int tok(int r) const { return u.e0 + r / v.G; }
+  __device__ __forceinline__ bool valid(int r) const { return r / v.G < u.ntok; }
+  __device__ __forceinline__ size_t row(int r) const {
+    return (((size_t)u.beam * w.T + tok(r)) * v.Hq + head * v.G + r % v.G) * kTileD;
+  }
+  __device__ __forceinline__ const float* q(int r) const { return valid(r) ? qp + row(r) : nullptr; }
+  __device__ __forceinline__ const float* token(int j, int kv) const {
+    if (j >= nctx) return (kv ? vp : kp) + (((size_t)u.beam * w.T + j - nctx) * v.Hkv + head) * kTileD;
+    const int pos = u.tok0 + j, page = v.tables[(size_t)u.beam * v.max_pages + pos / v.P];
+    if (page < 0 || page >= v.num_pages) {
+      set_status(v.ctl, GB_ERR_INVALID);
+      return nullptr;
+    }
+    return reinterpret_cast<const float*>(v.kv) + kv_elem_offset(v, layer, page, kv, head, pos % v.P);
+  }
+  __device__ __forceinline__ const float* key(int j) const { return token(j, 0); }
+  __device__ __forceinline__ const float* val(int j) const { return token(j, 1); }
+  __device__ __forceinline__ bool on(int r, int j) const {
+    return j < nctx || (valid(r) && ((w.anc[(size_t)u.beam * w.T + tok(r)] >> (j - nctx)) & 1));
+  }
+  __device__ __forceinline__ void out(int r, int c, float4 x, float m, float l) const {
+    if (!valid(r)) return;
+    const DraftRow d = draft_row(w, -1, u.beam, tok(r), u.split, true);
+    if (d.rec < 0) {
+      const float inv = 1.f / l;
+      *reinterpret_cast<float4*>(op + row(r) + c) = make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv);
+    } else {
+      const size_t rr = ((size_t)d.rec * v.Hkv + head) * w.rows + tok(r) * v.G + r % v.G;
+      *reinterpret_cast<float4*>(w.rec + rr * kTileD + c) = x;
+      if (c == 0) w.ml[rr] = make_float2(m, l);
+    }
+  }
+};
+
+__global__ void __launch_bounds__(kTileThreads) k_draft_f32(PoolView v, DraftView w, int layer, const float* q,
+                                                            const float* k, const float* vv, float* o, float qscale) {
+  pdl_wait();
+  pdl_launch_dependents();
+  extern __shared__ __align__(16) unsigned char raw[];
+  TileSmem& sm = *reinterpret_cast<TileSmem*>(raw);
+  const int total = w.ctl[kDrUnits] * v.Hkv;
+  for (int id = blockIdx.x; id < total; id += gridDim.x) {
+    const DraftUnit u = w.units[id / v.Hkv];
+    const int nctx = u.tok1 - u.tok0;
+    const DraftTile src{v, w, u, layer, id % v.Hkv, nctx, q, k, vv, o};
+    tile_attention(sm, src, nctx + (u.drafts ? w.cnt[u.beam] : 0), qscale);
+    __syncthreads();
+  }
+}
+
+// A warp per (slot, token, query head): joins the row's records, sum 2^(m_k - m) (o_k, l_k), or
+// writes the zeros of a row that holds no token.
+template <typename T, int D>
+__global__ void __launch_bounds__(256) k_draft_merge(PoolView v, DraftView w, T* o) {
+  pdl_wait();
+  pdl_launch_dependents();
+  if (blockIdx.x == 0 && threadIdx.x == 0) w.ctl[kDrNext] = 0;  // for the next layer
+  constexpr int per = D / 32;
+  const int lane = threadIdx.x & 31;
+  const long long rows = (long long)v.max_beams * w.T * v.Hq, step = (long long)gridDim.x * 8;
+  for (long long r = blockIdx.x * 8ll + (threadIdx.x >> 5); r < rows; r += step) {
+    const int hq = (int)(r % v.Hq), i = (int)(r / v.Hq % w.T), b = (int)(r / v.Hq / w.T);
+    float acc[per] = {};
+    if (i < w.cnt[b]) {
+      const int n = w.nrec[b];
+      if (n <= 1) continue;
+      const size_t step_r = (size_t)v.Hkv * w.rows;
+      const size_t r0 = ((size_t)w.rec_base[b] * v.Hkv + hq / v.G) * w.rows + i * v.G + hq % v.G;
+      float m = -INFINITY;
+      for (int k = lane; k < n; k += 32) m = fmaxf(m, w.ml[r0 + k * step_r].x);
+#pragma unroll
+      for (int s = 16; s > 0; s >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, s));
+      const float ref = m == -INFINITY ? 0.f : m;
+      float l = 0.f;
+#pragma unroll 4
+      for (int k = 0; k < n; ++k) {
+        const float2 ml = w.ml[r0 + k * step_r];
+        const float f = exp2f(ml.x - ref);
+        l = fmaf(ml.y, f, l);
+        const float* x = w.rec + (r0 + k * step_r) * D + lane * per;
+#pragma unroll
+        for (int c = 0; c < per; ++c) acc[c] = fmaf(x[c], f, acc[c]);
+      }
+      const float inv = 1.f / l;
+#pragma unroll
+      for (int c = 0; c < per; ++c) acc[c] *= inv;
+    }
+    T* dst = o + r * D + lane * per;
+#pragma unroll
+    for (int c = 0; c < per; ++c) {
+      if constexpr (sizeof(T) == 2) dst[c] = __float2bfloat16(acc[c]);
+      else dst[c] = acc[c];
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Accepting a path
+// ---------------------------------------------------------------------------
+
+// One CTA, thread = slot.  The rule of a step that appends one token after another, each to the slots whose
+// path is that long: lowest free page first, slots ascending; a partial tail page that others still hold is
+// left to them and copied.  All or nothing.
+__global__ void __launch_bounds__(1024) k_accept_plan(PoolView v, DraftView w, const int* parent, const int* count,
+                                                      const int* accepted, int* n_out, int* path_out) {
+  pdl_wait();
+  pdl_launch_dependents();
+  constexpr int kMaxNeeds = kMaxDraft / 16 + 1;  // pages a slot can need
+  __shared__ int tmp[33];
+  __shared__ unsigned long long s_path[kMaxBeams];
+  __shared__ int s_tail[kMaxBeams];
+  __shared__ unsigned s_bits[kMaxDraft][kMaxBeams / 32];  // slots that need a page with their k-th token
+  __shared__ int s_first[kMaxDraft];                      // needs of earlier tokens
+  __shared__ int s_pages[kMaxBeams * kMaxNeeds];
+  const int tid = threadIdx.x, b = tid, lane = tid & 31;
+  // Paths, a warp per slot.
+  for (int s = tid >> 5; s < v.max_beams; s += 32) {
+    bool bad = false, wrong;
+    const int n = drafted(count, s, w.T, v.active[s] != 0, &bad), to = v.active[s] ? accepted[s] : -1;
+    unsigned long long lo, hi;
+    ancestors(parent + (size_t)s * w.T, w.T, n, &lo, &hi, &wrong);
+    const bool odd = wrong || to < -1 || to >= n;
+    const unsigned long long p = __shfl_sync(0xffffffffu, to < 32 ? lo : hi, max(to, 0) & 31);
+    if (lane == 0) {
+      s_path[s] = odd || to < 0 ? 0ull : p;
+      if (odd || bad) set_status(v.ctl, GB_ERR_INVALID);
+    }
+  }
+  for (int i = tid; i < kMaxDraft * (kMaxBeams / 32); i += 1024) (&s_bits[0][0])[i] = 0;
+  __syncthreads();
+  const bool act = b < v.max_beams && v.active[b] != 0;
+  unsigned long long path = act ? s_path[b] : 0ull;
+  int n = __popcll(path);
+  const int L = act ? v.seq_len[b] : 0;
+  // Copy-on-write: a slot that appends leaves a tail page that another still holds after the lower
+  // slots have left it.
+  int tail = -1;
+  if (n > 0 && L % v.P && v.ctl[kCtlTailShared]) tail = v.tables[(size_t)b * v.max_pages + L / v.P];
+  s_tail[b] = tail;
+  __syncthreads();
+  bool cow = false;
+  if (tail >= 0) {
+    int before = 0;
+    const int R = v.refcnt[tail];
+    if (R > 1)
+      for (int s = 0; s < b; ++s) before += s_tail[s] == tail;
+    cow = R - before > 1;
+  }
+  const int first_new = (L + v.P - 1) / v.P;
+  const int fresh = n > 0 ? max(0, (L + n - 1) / v.P - first_new + 1) : 0;
+  const int need = fresh + (cow ? 1 : 0);
+  const bool too_long = n > 0 && (L + n - 1) / v.P >= v.max_pages;
+  int total;
+  block_exclusive_scan(need, tmp, &total);
+  const bool fails = __syncthreads_or(too_long) || total > v.ctl[kCtlFree];
+  if (fails) {
+    if (tid == 0) set_status(v.ctl, GB_ERR_OOM);
+    n = 0;
+    path = 0;
+    cow = false;
+    total = 0;
+  } else {
+    if (cow) atomicOr(&s_bits[0][b >> 5], 1u << (b & 31));
+    for (int j = 0; j < fresh; ++j) atomicOr(&s_bits[(first_new + j) * v.P - L][b >> 5], 1u << (b & 31));
+  }
+  __syncthreads();
+  // The r-th need, token by token and slots ascending, gets the r-th lowest free page.
+  {
+    int c = 0;
+    if (tid < kMaxDraft)
+      for (int i = 0; i < kMaxBeams / 32; ++i) c += __popc(s_bits[tid][i]);
+    int all;
+    const int at = block_exclusive_scan(c, tmp, &all);
+    if (tid < kMaxDraft) s_first[tid] = at;
+  }
+  int found = 0, w0 = max(v.ctl[kCtlCursor], 0);
+  __syncthreads();
+  while (found < total && w0 < v.words) {
+    const int word = w0 + tid;
+    unsigned bits = word < v.words ? v.free_bits[word] : 0u;
+    if (word == v.words - 1 && (v.num_pages & 31)) bits &= (1u << (v.num_pages & 31)) - 1u;
+    int here;
+    int r = found + block_exclusive_scan(__popc(bits), tmp, &here);
+    const unsigned before = bits;
+    while (bits && r < total) {
+      s_pages[r] = word * 32 + __ffs(bits) - 1;
+      bits &= bits - 1u;
+      if (++r == total) v.ctl[kCtlCursor] = word;
+    }
+    if (bits != before) v.free_bits[word] = (v.free_bits[word] & ~before) | bits;
+    found += here;
+    w0 += 1024;
+  }
+  __syncthreads();
+  if (tid == 0 && total > 0) v.ctl[kCtlFree] -= total;
+  auto page_of = [&](int k) {
+    int r = s_first[k] + __popc(s_bits[k][b >> 5] & ((1u << (b & 31)) - 1u));
+    for (int i = 0; i < (b >> 5); ++i) r += __popc(s_bits[k][i]);
+    return s_pages[r];
+  };
+  if (!fails) {
+    if (cow) {
+      const int p = page_of(0);
+      atomicSub(&v.refcnt[tail], 1);
+      v.refcnt[p] = 1;
+      v.tables[(size_t)b * v.max_pages + L / v.P] = p;
+    }
+    for (int j = 0; j < fresh; ++j) {
+      const int p = page_of((first_new + j) * v.P - L);
+      v.refcnt[p] = 1;
+      v.tables[(size_t)b * v.max_pages + first_new + j] = p;
+    }
+  }
+  if (b < v.max_beams) {
+    w.acc_n[b] = n;
+    w.acc_pos[b] = L;
+    w.acc_old[b] = cow ? tail : -1;
+    w.acc_path[b] = path;
+    if (n > 0) {
+      v.seq_len[b] = L + n;
+      v.gen[b] += n;
+    }
+    if (n_out) n_out[b] = n;
+    if (path_out) {
+      int* to = path_out + (size_t)b * w.T;
+      for (int i = 0; i < w.T; ++i) {
+        to[i] = path ? __ffsll((long long)path) - 1 : -1;
+        path &= path - 1;
+      }
+    }
+  }
+}
+
+// A CTA per (slot, layer): the rows of a copied tail page, then the path's rows.
+__global__ void __launch_bounds__(256) k_accept_copy(PoolView v, DraftView w, const char* k, const char* vv) {
+  pdl_wait();
+  pdl_launch_dependents();
+  __shared__ short s_tok[kMaxDraft];
+  const int b = blockIdx.x, layer = blockIdx.y, tid = threadIdx.x;
+  const int n = w.acc_n[b];
+  if (n == 0) return;
+  const int L = w.acc_pos[b], old = w.acc_old[b], rows = v.Hkv * 16;  // 16-byte pieces of a token's K (or V)
+  if (tid < 64) {
+    const unsigned long long path = w.acc_path[b];
+    if ((path >> tid) & 1) s_tok[__popcll(path & ((1ull << tid) - 1))] = (short)tid;
+  }
+  const int* table = v.tables + (size_t)b * v.max_pages;
+  if (old >= 0) {
+    const int page = table[L / v.P], have = L % v.P;
+    for (int i = tid; i < 2 * v.Hkv * have * 16; i += 256) {
+      const int c = i & 15, row = (i >> 4) % have, kvh = (i >> 4) / have;
+      const int kv = kvh / v.Hkv, h = kvh % v.Hkv;
+      reinterpret_cast<uint4*>(v.kv + kv_elem_offset(v, layer, page, kv, h, row) * v.esize)[c] =
+          reinterpret_cast<const uint4*>(v.kv + kv_elem_offset(v, layer, old, kv, h, row) * v.esize)[c];
+    }
+  }
+  __syncthreads();
+  const size_t src0 = ((size_t)layer * v.max_beams + b) * w.T * rows;
+  for (int i = tid; i < 2 * n * rows; i += 256) {
+    const int kv = i >= n * rows, j = kv ? i - n * rows : i, t = j / rows, c = j % rows, pos = L + t;
+    const int page = table[pos / v.P];
+    if (page < 0 || page >= v.num_pages) {
+      set_status(v.ctl, GB_ERR_INVALID);
+      continue;
+    }
+    const uint4 x = __ldcs(reinterpret_cast<const uint4*>(kv ? vv : k) + src0 + (size_t)s_tok[t] * rows + c);
+    reinterpret_cast<uint4*>(v.kv + kv_elem_offset(v, layer, page, kv, c >> 4, pos % v.P) * v.esize)[c & 15] = x;
+  }
+}
+
+// One CTA, thread = slot.  The pages past a slot's new length lose a reference.  A slot that is cut inside a page
+// that others hold (theirs goes on, or was cut elsewhere) gets a copy, so that a shared page keeps one
+// meaning for all its holders; slots decide in order against the current references, so when all of a page's
+// holders are cut inside it the last one keeps it.  All or nothing: when there is not a free page for every
+// slot cut inside a page that has several holders before the call, nothing changes.
+__global__ void __launch_bounds__(1024) k_truncate(PoolView v, const int* lengths) {
+  pdl_wait();
+  pdl_launch_dependents();
+  constexpr int kShort = 8;  // pages a thread drops by itself; longer runs go to a warp each
+  __shared__ int tmp[33];
+  __shared__ int s_tail[kMaxBeams], s_pages[kMaxBeams], s_long[kMaxBeams];
+  __shared__ int s_nlong;
+  const int tid = threadIdx.x, b = tid;
+  const bool act = b < v.max_beams && v.active[b] != 0;
+  const int L = act ? v.seq_len[b] : 0, want = act ? lengths[b] : -1;
+  if (want > L) set_status(v.ctl, GB_ERR_INVALID);
+  const bool cut = want >= 0 && want < L;
+  const int* table = v.tables + (size_t)b * v.max_pages;
+  const int tail = cut && want % v.P ? table[want / v.P] : -1;
+  const bool shared = tail >= 0 && v.refcnt[tail] > 1;
+  if (tid == 0) s_nlong = 0;
+  s_tail[b] = tail;
+  int need;
+  block_exclusive_scan(shared ? 1 : 0, tmp, &need);
+  if (need > v.ctl[kCtlFree]) {
+    if (tid == 0) {
+      set_status(v.ctl, GB_ERR_OOM);
+      v.ctl[kCtlCowJobs] = 0;
+    }
+    return;
+  }
+  __syncthreads();
+  const int j0 = cut ? (want + v.P - 1) / v.P : 0, j1 = cut ? (L + v.P - 1) / v.P : 0;
+  if (j1 - j0 <= kShort) {
+    for (int j = j0; j < j1; ++j) unref_page(v, table[j]);
+  } else {
+    s_long[atomicAdd(&s_nlong, 1)] = b;
+  }
+  if (cut) {
+    v.seq_len[b] = want;
+    v.gen[b] = max(0, v.gen[b] - (L - want));
+  }
+  __syncthreads();
+  s_pages[b] = j1;  // the run's end, for the warps that take the long ones
+  __syncthreads();
+  for (int i = tid >> 5; i < s_nlong; i += 32) {
+    const int s = s_long[i], n = v.seq_len[s];
+    for (int j = (n + v.P - 1) / v.P + (tid & 31); j < s_pages[s]; j += 32)
+      unref_page(v, v.tables[(size_t)s * v.max_pages + j]);
+  }
+  __threadfence_block();
+  __syncthreads();
+  // Who copies: references as they are now, less the lower slots that copied before.
+  bool cow = false;
+  if (shared) {
+    const int R = *reinterpret_cast<volatile int*>(&v.refcnt[tail]);
+    int before = 0;
+    if (R > 1)
+      for (int s = 0; s < b; ++s) before += s_tail[s] == tail;
+    cow = R - before > 1;
+  }
+  int total;
+  const int rank = block_exclusive_scan(cow ? 1 : 0, tmp, &total);
+  int found = 0, w0 = max(*reinterpret_cast<volatile int*>(&v.ctl[kCtlCursor]), 0);
+  __syncthreads();
+  while (found < total && w0 < v.words) {
+    const int word = w0 + tid;
+    unsigned bits = word < v.words ? *reinterpret_cast<volatile unsigned*>(&v.free_bits[word]) : 0u;
+    if (word == v.words - 1 && (v.num_pages & 31)) bits &= (1u << (v.num_pages & 31)) - 1u;
+    int here;
+    int r = found + block_exclusive_scan(__popc(bits), tmp, &here);
+    const unsigned before = bits;
+    while (bits && r < total) {
+      s_pages[r] = word * 32 + __ffs(bits) - 1;
+      bits &= bits - 1u;
+      if (++r == total) v.ctl[kCtlCursor] = word;
+    }
+    if (bits != before) v.free_bits[word] = (*reinterpret_cast<volatile unsigned*>(&v.free_bits[word]) & ~before) | bits;
+    found += here;
+    w0 += 1024;
+  }
+  __syncthreads();
+  if (cow) {
+    const int p = s_pages[rank];
+    atomicSub(&v.refcnt[tail], 1);
+    v.refcnt[p] = 1;
+    v.tables[(size_t)b * v.max_pages + want / v.P] = p;
+    v.cow[3 * rank] = tail;
+    v.cow[3 * rank + 1] = p;
+    v.cow[3 * rank + 2] = want % v.P;
+  }
+  if (tid == 0) {
+    v.ctl[kCtlCowJobs] = total;
+    if (total > 0) atomicSub(&v.ctl[kCtlFree], total);
+  }
+}
+
+// The rows of the pages that k_truncate replaced: a CTA per (layer, job).
+__global__ void __launch_bounds__(256) k_cow_rows(PoolView v) {
+  pdl_wait();
+  pdl_launch_dependents();
+  const int jobs = v.ctl[kCtlCowJobs], layer = blockIdx.y;
+  for (int j = blockIdx.x; j < jobs; j += gridDim.x) {
+    const int old = v.cow[3 * j], page = v.cow[3 * j + 1], have = v.cow[3 * j + 2];
+    for (int i = threadIdx.x; i < 2 * v.Hkv * have * 16; i += 256) {
+      const int c = i & 15, row = (i >> 4) % have, kvh = (i >> 4) / have;
+      reinterpret_cast<uint4*>(v.kv + kv_elem_offset(v, layer, page, kvh / v.Hkv, kvh % v.Hkv, row) * v.esize)[c] =
+          reinterpret_cast<const uint4*>(v.kv + kv_elem_offset(v, layer, old, kvh / v.Hkv, kvh % v.Hkv, row) * v.esize)[c];
+    }
+  }
+}
+
+bool on_device(const gb_pool* pool) {
+  int d = -1;
+  return cudaGetDevice(&d) == cudaSuccess && d == pool->device;
+}
+
+gb_status check_draft(gb_pool* pool, const gb_draft* d, const char* what) {
+  if (!d || d->n_draft < 1 || d->n_draft > kMaxDraft || !d->parent_dev || !d->workspace_dev ||
+      ((uintptr_t)d->workspace_dev & 255))
+    return fail(pool, GB_ERR_INVALID, what);
+  if (d->workspace_bytes < draft_layout(pool->cfg, pool->num_sms, d->n_draft).total)
+    return fail(pool, GB_ERR_INVALID, "draft: the workspace is too small");
+  if (!on_device(pool)) return fail(pool, GB_ERR_STATE, "draft: the pool is on another device than the current one");
+  if (!pool->seeded) return fail(pool, GB_ERR_STATE, "pool not seeded");
+  if (pool->next_layer != 0) return fail(pool, GB_ERR_STATE, "draft: inside an open step");
+  return GB_OK;
+}
+
+bool meets(const void* a, size_t an, const void* b, size_t bn) {
+  const char *x = static_cast<const char*>(a), *y = static_cast<const char*>(b);
+  return x < y + bn && y < x + an;
+}
+
+}  // namespace
+}  // namespace gb
+
+using namespace gb;
+
+extern "C" gb_status gb_draft_workspace_bytes(gb_pool* pool, int n_draft, size_t* bytes) {
+  if (!pool || !bytes) return GB_ERR_INVALID;
+  if (n_draft < 1 || n_draft > kMaxDraft) return fail(pool, GB_ERR_INVALID, "draft: 1 to 64 tokens");
+  *bytes = draft_layout(pool->cfg, pool->num_sms, n_draft).total;
+  return GB_OK;
+}
+
+extern "C" gb_status gb_draft_attention(gb_pool* pool, int layer, const gb_draft* d, const void* q_dev,
+                                        const void* k_dev, const void* v_dev, float scale, void* out_dev,
+                                        gb_stream_t stream) {
+  if (!pool) return GB_ERR_INVALID;
+  gb_status st = check_draft(pool, d, "draft: bad arguments");
+  if (st != GB_OK) return st;
+  if (layer < 0 || layer >= pool->cfg.num_layers || !q_dev || !k_dev || !v_dev || !out_dev || !(scale > 0.f) ||
+      scale > 3e38f || (((uintptr_t)q_dev | (uintptr_t)k_dev | (uintptr_t)v_dev | (uintptr_t)out_dev) & 15))
+    return fail(pool, GB_ERR_INVALID, "draft: bad arguments");
+  const PoolView& v = pool->view;
+  const int T = d->n_draft;
+  const size_t qb = (size_t)v.max_beams * T * v.Hq * v.D * v.esize, kb = qb / v.G;
+  if (meets(out_dev, qb, q_dev, qb) || meets(out_dev, qb, k_dev, kb) || meets(out_dev, qb, v_dev, kb))
+    return fail(pool, GB_ERR_INVALID, "draft: the output overlaps an input");
+  const bool bf16 = v.dtype == GB_BF16;
+  if (bf16 && !pool->have_tmap) return fail(pool, GB_ERR_UNSUPPORTED, "draft: no tensor map over the pool");
+  if (layer > 0 && (pool->draft_epoch != pool->epoch || pool->draft_ws != d->workspace_dev || pool->draft_tokens != T))
+    return fail(pool, GB_ERR_STATE, "draft: layer 0 plans the round, on the pool as it is and in this workspace");
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  const DraftView w = draft_view(pool, draft_layout(pool->cfg, pool->num_sms, T), T, d->workspace_dev);
+  const float qscale = scale * 1.4426950408889634f;
+  DraftJob job;
+  if (bf16) {
+    job.v = v;
+    job.w = w;
+    job.layer = layer;
+    job.oob = pool->tmap_oob;
+    job.qscale = qscale;
+    job.q = static_cast<const __nv_bfloat16*>(q_dev);
+    job.k = static_cast<const __nv_bfloat16*>(k_dev);
+    job.vv = static_cast<const __nv_bfloat16*>(v_dev);
+    job.o = static_cast<__nv_bfloat16*>(out_dev);
+    job.tp = *reinterpret_cast<const CUtensorMap*>(pool->tmap);
+    const cuuint64_t dims[5] = {64, (cuuint64_t)T, 2, (cuuint64_t)v.Hkv, (cuuint64_t)v.max_beams};
+    const cuuint64_t strides[4] = {(cuuint64_t)v.Hkv * 256, 128, 256, (cuuint64_t)T * v.Hkv * 256};
+    const cuuint32_t box[5] = {64, 8, 2, 1, 1};
+    if (!encode_tensor_map(&job.tk, k_dev, 5, dims, strides, box) ||
+        !encode_tensor_map(&job.tv, v_dev, 5, dims, strides, box))
+      return fail(pool, GB_ERR_CUDA, "draft: tensor map");
+  }
+  if (layer == 0) {
+    const int tokens = (bf16 ? 2 * flash::kRows : kTileRows) / v.G;
+    launch_pdl(k_draft_plan, 1 + (v.max_beams + 31) / 32, kListThreads, 0, s, v, w, d->parent_dev, d->count_dev, tokens,
+               2, bf16 && v.grouped);
+    pool->launches += 1;
+    if ((st = check_launch(pool, "draft_plan")) != GB_OK) return st;
+    pool->draft_epoch = pool->epoch;
+    pool->draft_ws = d->workspace_dev;
+    pool->draft_tokens = T;
+  }
+  cudaError_t e;
+  const long long rows = (long long)v.max_beams * T * v.Hq;
+  const unsigned merge = (unsigned)std::min<long long>((rows + 7) / 8, pool->num_sms * 16);
+  if (bf16) {
+    e = set_max_dynamic_smem(reinterpret_cast<const void*>(k_draft), flash::kSmem);
+    if (e == cudaSuccess) e = launch_pdl(k_draft, pool->num_sms, flash::kThreads, flash::kSmem, s, job);
+    if (e == cudaSuccess) e = launch_pdl(k_draft_merge<__nv_bfloat16, 128>, merge, 256, 0, s, v, w, job.o);
+  } else {
+    e = set_max_dynamic_smem(reinterpret_cast<const void*>(k_draft_f32), (int)sizeof(TileSmem));
+    if (e == cudaSuccess)
+      e = launch_pdl(k_draft_f32, pool->num_sms * 3, kTileThreads, sizeof(TileSmem), s, v, w, layer,
+                     static_cast<const float*>(q_dev), static_cast<const float*>(k_dev), static_cast<const float*>(v_dev),
+                     static_cast<float*>(out_dev), qscale);
+    if (e == cudaSuccess) e = launch_pdl(k_draft_merge<float, 64>, merge, 256, 0, s, v, w, static_cast<float*>(out_dev));
+  }
+  pool->launches += 2;
+  if (e != cudaSuccess) return fail(pool, GB_ERR_CUDA, cudaGetErrorString(e));
+  return check_launch(pool, "draft");
+}
+
+extern "C" gb_status gb_accept_draft(gb_pool* pool, const gb_draft* d, const void* k_dev, const void* v_dev,
+                                     const int32_t* accepted_dev, int32_t* count_out_dev, int32_t* path_out_dev,
+                                     gb_stream_t stream) {
+  if (!pool) return GB_ERR_INVALID;
+  gb_status st = check_draft(pool, d, "accept: bad arguments");
+  if (st != GB_OK) return st;
+  if (!k_dev || !v_dev || !accepted_dev || (((uintptr_t)k_dev | (uintptr_t)v_dev) & 15))
+    return fail(pool, GB_ERR_INVALID, "accept: bad arguments");
+  const DraftView w =
+      draft_view(pool, draft_layout(pool->cfg, pool->num_sms, d->n_draft), d->n_draft, d->workspace_dev);
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  launch_pdl(k_accept_plan, 1, 1024, 0, s, pool->view, w, d->parent_dev, d->count_dev, accepted_dev, count_out_dev,
+             path_out_dev);
+  pool->launches += 1;
+  if ((st = check_launch(pool, "accept_plan")) != GB_OK) return st;
+  ++pool->epoch;
+  launch_pdl(k_accept_copy, dim3(pool->cfg.max_beams, pool->cfg.num_layers), 256, 0, s, pool->view, w,
+             static_cast<const char*>(k_dev), static_cast<const char*>(v_dev));
+  pool->launches += 1;
+  return check_launch(pool, "accept_copy");
+}
+
+extern "C" gb_status gb_truncate(gb_pool* pool, const int32_t* lengths_dev, gb_stream_t stream) {
+  if (!pool) return GB_ERR_INVALID;
+  if (!lengths_dev) return fail(pool, GB_ERR_INVALID, "truncate: null pointer");
+  if (!on_device(pool)) return fail(pool, GB_ERR_STATE, "truncate: the pool is on another device than the current one");
+  if (!pool->seeded) return fail(pool, GB_ERR_STATE, "pool not seeded");
+  if (pool->next_layer != 0) return fail(pool, GB_ERR_STATE, "truncate inside an open step");
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  ++pool->epoch;
+  launch_pdl(k_truncate, 1, 1024, 0, s, pool->view, lengths_dev);
+  launch_pdl(k_cow_rows, dim3(std::min(pool->cfg.max_beams, 64), pool->cfg.num_layers), 256, 0, s, pool->view);
+  pool->launches += 2;
+  const gb_status st = check_launch(pool, "truncate");
+  if (st != GB_OK) return st;
+  if (rebuild_segments(pool, s) != cudaSuccess) return check_launch(pool, "segments");
+  return GB_OK;
+}

@@ -108,7 +108,24 @@ __device__ __forceinline__ void tile_attention(TileSmem& sm, const Src& src, int
   for (int i = 0; i < 4; ++i) {
 #pragma unroll
     for (int w = 8; w > 0; w >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], w);
-    src.out(4 * ty + i, 4 * tx, make_float4(o[i][0], o[i][1], o[i][2], o[i][3]), m[i], l[i]);
+    const int row = 4 * ty + i, c = 4 * tx;
+    const float* qr = src.q(row);
+    // P V takes every key of a tile, with p = 0 for those the row does not see, and 0 x inf is NaN: columns that are
+    // not finite although the row's sum is, are summed again over the keys it sees.
+    if (qr && isfinite(m[i]) && isfinite(l[i]) &&
+        !(isfinite(o[i][0]) && isfinite(o[i][1]) && isfinite(o[i][2]) && isfinite(o[i][3]))) {
+      float acc[4] = {};
+      for (int j = 0; j < nkeys; ++j) {
+        const float *k = src.on(row, j) ? src.key(j) : nullptr, *v = k ? src.val(j) : nullptr;
+        if (!v) continue;
+        float sc = 0.f;
+        for (int d = 0; d < kTileD; ++d) sc = fmaf(qr[d] * qscale, k[d], sc);
+        const float p = exp2f(sc - m[i]);
+        for (int e = 0; e < 4; ++e) acc[e] = fmaf(p, v[c + e], acc[e]);
+      }
+      for (int e = 0; e < 4; ++e) o[i][e] = acc[e];
+    }
+    src.out(row, c, make_float4(o[i][0], o[i][1], o[i][2], o[i][3]), m[i], l[i]);
   }
 }
 

@@ -1,0 +1,59 @@
+"""``DraftTrees``: trees of drafted tokens over a ``BeamPool`` (speculative decoding of every trace at once).
+
+A round: ``attention`` layer by layer lets every drafted token attend to its beam's context and to its own
+ancestors in the beam's tree; the caller picks a path per beam; ``accept`` appends the path's keys and values to the
+pool.  The pool does not change until then.  ``BeamPool.truncate`` takes tokens back.
+
+Every operation is one call into ``libgambit.so``; the object keeps the workspace, so its calls belong on one stream.
+"""
+from __future__ import annotations
+
+import torch
+
+from paper_2608_08020_gb300 import binding as B
+from paper_2608_08020_gb300.pool import BeamPool, TORCH_DT
+
+
+class DraftTrees:
+    def __init__(self, pool: BeamPool, n_draft: int):
+        self.pool, self.n_draft = pool, n_draft
+        c = pool.cfg
+        n = B.gb_draft_workspace_bytes(pool.handle, n_draft)
+        self.workspace = torch.empty(n, dtype=torch.uint8, device=pool.kv.device)
+        self.dtype = TORCH_DT[pool.kv_dtype]
+        self.q_shape = (pool.max_beams, n_draft, c.num_q_heads, c.head_dim)
+        self.kv_shape = (pool.max_beams, n_draft, c.num_kv_heads, c.head_dim)
+
+    def _check(self, name, x, shape, dtype):
+        if tuple(x.shape) != shape or x.dtype != dtype or not x.is_contiguous() or x.device != self.workspace.device:
+            raise ValueError(f"{name}: {tuple(x.shape)} {x.dtype} on {x.device}, expected contiguous {shape} {dtype} on "
+                             f"{self.workspace.device}")
+
+    def _draft(self, parent, count):
+        self._check("parent", parent, self.kv_shape[:2], torch.int32)
+        if count is not None:
+            self._check("count", count, self.kv_shape[:1], torch.int32)
+        return B.GbDraft(parent.data_ptr(), None if count is None else count.data_ptr(), self.workspace.data_ptr(),
+                         self.workspace.numel(), self.n_draft)
+
+    def attention(self, layer: int, q, k, v, parent, scale: float, out=None, count=None, stream=None):
+        """One layer: q [max_beams][n_draft][q heads][D], k and v [max_beams][n_draft][kv heads][D], parent int32
+        [max_beams][n_draft] (-1: the context's end), count int32 [max_beams] (None: n_draft each); returns out, like q."""
+        if out is None:
+            out = torch.empty_like(q)
+        for name, x, shape in (("q", q, self.q_shape), ("k", k, self.kv_shape), ("v", v, self.kv_shape), ("out", out, self.q_shape)):
+            self._check(name, x, shape, self.dtype)
+        B.gb_draft_attention(self.pool.handle, layer, self._draft(parent, count), q, k, v, scale, out, stream)
+        return out
+
+    def accept(self, k, v, parent, accepted, count=None, stream=None):
+        """Append each slot's path from its tree's root to token accepted[slot] (int32 [max_beams]; -1: none), all
+        layers: k and v [layers][max_beams][n_draft][kv heads][D].  Returns (tokens appended int32 [max_beams], their
+        indices in order int32 [max_beams][n_draft], then -1)."""
+        for name, x in (("k", k), ("v", v)):
+            self._check(name, x, (self.pool.cfg.num_layers, *self.kv_shape), self.dtype)
+        self._check("accepted", accepted, self.kv_shape[:1], torch.int32)
+        n = torch.empty_like(accepted)
+        path = torch.empty_like(parent)
+        B.gb_accept_draft(self.pool.handle, self._draft(parent, count), k, v, accepted, n, path, stream)
+        return n, path

@@ -83,6 +83,17 @@ class BeamPool:
     def release(self, slots, stream=None):
         B.gb_release(self.handle, slots, int(slots.numel()), stream)
 
+    def fork_slots(self, parent_of, stream=None):
+        """Apply a tournament decided elsewhere (parent_of int32 [max_beams]; see gb_fork_slots)."""
+        B.gb_fork_slots(self.handle, parent_of, stream)
+
+    def truncate(self, lengths, stream=None):
+        """Each active slot keeps its first lengths[slot] tokens (int32 [max_beams]; negative: all)."""
+        if lengths.dtype != torch.int32 or lengths.numel() != self.max_beams or not lengths.is_contiguous() \
+                or lengths.device != self.kv.device:
+            raise ValueError("lengths: contiguous int32 [max_beams] on the pool's device expected")
+        B.gb_truncate(self.handle, lengths, stream)
+
     def status(self, stream=None) -> int:
         return B.gb_pool_status(self.handle, stream)
 

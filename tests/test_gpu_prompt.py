@@ -93,3 +93,88 @@ def test_many_short_sequences(cuda, dtype):
 @pytest.mark.parametrize("scale_q", [0.0, 1e-3, 6.0])
 def test_flat_and_sharp_scores(cuda, scale_q):
     run("bf16", [900], 8, 2, seed=5, scale_q=scale_q)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_values_out_of_sight(cuda, dtype):
+    """Infinities and NaN in later tokens and in other sequences do not reach a row; where it sees them they do."""
+    import torch
+    from paper_2608_08020_gb300.prompt import PromptAttention
+    q, k, v = make(dtype, 400, 8, 2, 9)
+    d = q.shape[2]
+    v[100, 0, 5] = float("inf")                # sequence 0: rows from 100 on
+    v[130, :, d - 1] = float("nan")
+    k[250] = float("nan")                      # sequence 1: rows from 250 on
+    v[251] = float("nan")
+    q[390:], k[390:], v[390:] = float("nan"), float("nan"), float("nan")
+    cu = [0, 160, 300, 380]
+    op = PromptAttention(8, 2, d, dtype, max_tokens=400, max_seqs=3)
+    out = op(q, k, v, torch.tensor(cu, dtype=torch.int32, device="cuda"), 1 / math.sqrt(d))
+    clean = [x.clone() for x in (k, v)]
+    clean[1][100, 0, 5], clean[1][130, :, d - 1], clean[0][250], clean[1][251] = 0, 0, 0, 0
+    for s, e in zip(cu, cu[1:]):
+        for i in range(s, e):
+            # What row i sees, in 64 bits.
+            kk, vv = (x[s:i + 1].double().repeat_interleave(4, 1) for x in (k, v))
+            p = torch.softmax(torch.einsum("hd,thd->ht", q[i].double(), kk) / math.sqrt(d), -1)
+            o, a = torch.einsum("ht,thd->hd", p, vv), torch.einsum("ht,thd->hd", p, vv.abs())
+            ok = o.isfinite()
+            assert torch.equal(out[i].isfinite(), ok), i
+            assert bool(((out[i].double() - o).abs() <= bound(o, a, dtype))[ok].all()), i
+    assert op.status() == 0
+
+
+def test_bad_sequences_are_left_out(cuda):
+    import torch
+    from paper_2608_08020_gb300 import binding as B
+    from paper_2608_08020_gb300.prompt import PromptAttention
+    q, k, v = make("bf16", 300, 4, 2, 10)
+    op = PromptAttention(4, 2, 128, "bf16", max_tokens=300, max_seqs=4)
+    for cu, fine in (([0, 100, 90, 200, 300], [(0, 100), (90, 200), (200, 300)]), ([-5, 100, 200, 300, 400], [(100, 200), (200, 300)])):
+        out = torch.full_like(q, 7.0)
+        op(q, k, v, torch.tensor(cu, dtype=torch.int32, device="cuda"), 0.1, out)
+        assert B.STATUS_NAMES[op.status()] == "GB_ERR_INVALID"
+        assert bool(out.isfinite().all())
+        for s, e in fine[-1:]:
+            o, a = attend(q, k, v, [s, e], 0.1)
+            assert bool(((out.double() - o).abs() <= bound(o, a, "bf16"))[s:e].all())
+    op(q, k, v, torch.tensor([0, 300], dtype=torch.int32, device="cuda"), 0.1)
+    assert op.status() == 0
+
+
+def test_streams_and_graphs(cuda):
+    """On another stream, and captured once and replayed with other lengths and values."""
+    import torch
+    from paper_2608_08020_gb300.prompt import PromptAttention
+    q, k, v = make("bf16", 700, 8, 2, 11)
+    op = PromptAttention(8, 2, 128, "bf16", max_tokens=700, max_seqs=5)
+    cu = torch.tensor([0, 1, 300, 300, 650, 700], dtype=torch.int32, device="cuda")
+    out = torch.empty_like(q)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        op(q, k, v, cu, 0.1, out)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        op(q, k, v, cu, 0.1, out)
+    for lengths in ([0, 1, 300, 300, 650, 700], [0, 0, 0, 64, 600, 700], [0, 700, 700, 700, 700, 700]):
+        cu.copy_(torch.tensor(lengths, dtype=torch.int32))
+        for x, y in zip((q, k, v), make("bf16", 700, 8, 2, lengths[3])):
+            x.copy_(y)
+        graph.replay()
+        torch.cuda.synchronize()
+        o, a = attend(q, k, v, lengths, 0.1)
+        assert bool(((out.double() - o).abs() <= bound(o, a, "bf16")).all())
+
+
+def test_wrapper_refuses(cuda):
+    import torch
+    from paper_2608_08020_gb300.prompt import PromptAttention
+    q, k, v = make("bf16", 64, 4, 2, 12)
+    op = PromptAttention(4, 2, 128, "bf16", max_tokens=64, max_seqs=2)
+    cu = torch.tensor([0, 64], dtype=torch.int32, device="cuda")
+    for args in ((q[:, :2], k, v, cu), (q.float(), k, v, cu), (q, k[:60], v, cu), (q, k, v.transpose(0, 1).contiguous().transpose(0, 1), cu),
+                 (q, k, v, cu.long()), (q, k, v, cu.cpu()), (q, k, v, torch.zeros(4, dtype=torch.int32, device="cuda"))):
+        with pytest.raises(ValueError):
+            op(*args, 0.1)
