@@ -203,7 +203,6 @@ __global__ void __launch_bounds__(kListThreads) k_draft_plan(PoolView v, DraftVi
   }
   __shared__ ListSmem sm;
   __shared__ short s_cnt[kMaxBeams];
-  __shared__ int s_sum;
   const int b = tid, cap = v.max_beams;
   const bool act = b < cap && v.active[b] != 0;
   const int L = act ? v.seq_len[b] : 0;

@@ -110,6 +110,26 @@ __device__ __forceinline__ void st16(uint32_t taddr, const uint32_t* u) {
 }
 __device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+// Products with the accumulate flag known (tc.cuh's take it as a value).
+__device__ __forceinline__ void mma_set(uint32_t d, uint64_t a, uint64_t b, uint32_t id) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, 0, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+               "l"(a), "l"(b), "r"(id));
+}
+__device__ __forceinline__ void mma_add(uint32_t d, uint64_t a, uint64_t b, uint32_t id) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.eq.b32 p, 0, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+               "l"(a), "l"(b), "r"(id));
+}
+__device__ __forceinline__ void mma_ts_add(uint32_t d, uint32_t a, uint64_t b, uint32_t id) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.eq.b32 p, 0, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+               "r"(a), "l"(b), "r"(id));
+}
+// One lane of the warp, the same each time.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+  return p != 0;
+}
+
 // 32 columns of a row's result: O of one group, or of both with their weights.
 __device__ __forceinline__ void read_o(uint32_t a, uint32_t b, bool two, float wa, float wb, float* o) {
   uint32_t u[32];
@@ -269,62 +289,74 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
         mbar_wait_bounded(ctl + kBarFull + 8 * (k % kStages), (k / kStages) & 1, kWaitLimitNs / 8);
   } else if (warp == kMmaWarp) {
     // ---------------------------------------------------------------- products
-    if (lane == 0) {
-      constexpr uint32_t ID_S = idesc(kRows, kTok, false), ID_PV = idesc(kRows, kD, true);
-      uint32_t ring = 0;               // stage count of the unit's first tile
-      uint32_t np[2] = {0, 0};         // P tiles consumed per group
-      uint32_t ns[2] = {0, 0};
-      bool ok = true;
-      for (int u = 0; ok; ++u) {
-        const int slot = u & (kSlots - 1);
-        ok = wait_or_abort(ctl + kBarSched + 8 * slot, (u / kSlots) & 1, abort_flag);
-        if (!ok) break;
-        const int nt = units[slot].nt, dual = units[slot].dual;
-        mbar_arrive(ctl + kBarSchedFree + 8 * slot);
-        if (nt < 0) break;
-        const int items = dual ? 2 * nt : nt;
-        for (int i = 0; i < items + 2 && ok; ++i) {
-          const int g = i & 1;
-          if (i >= 2) {  // P.V of item i - 2
-            const int it = i - 2;
-            const uint32_t pos = ring + 2 * (dual ? it >> 1 : it) + 1, st = pos % kStages;
-            ok = wait_or_abort(ctl + kBarP + 8 * g, np[g] & 1, abort_flag) &&
-                 wait_or_abort(ctl + kBarFull + 8 * st, (pos / kStages) & 1, abort_flag) &&
-                 (it >= 2 || u == 0 || wait_or_abort(ctl + kBarOFree + 8 * g, (u - 1) & 1, abort_flag));
-            if (!ok) break;
-            ++np[g];
-            tc_fence_after();
-            const uint32_t vb = sbase + kRing + st * kTile;
+    // The whole warp walks the items and one lane issues: operands that are the same in every lane stay in
+    // uniform registers, where the instruction takes them from.
+    constexpr uint32_t ID_S = idesc(kRows, kTok, false), ID_PV = idesc(kRows, kD, true);
+    const bool leader = elect_one();
+    const uint32_t base = __shfl_sync(0xffffffffu, sbase, 0), tm = __shfl_sync(0xffffffffu, tmem, 0);
+    const uint32_t bars = base + kBar;
+    uint32_t ring = 0;               // stage count of the unit's first tile
+    uint32_t np[2] = {0, 0};         // S and P tiles so far, per group
+    uint32_t ns[2] = {0, 0};
+    bool ok = true;
+    auto wait = [&](uint32_t bar, uint32_t parity) {
+      ok = __all_sync(0xffffffffu, wait_or_abort(bar, parity, abort_flag));
+      return ok;
+    };
+    for (int u = 0; ok; ++u) {
+      const int slot = u & (kSlots - 1);
+      if (!wait(bars + kBarSched + 8 * slot, (u / kSlots) & 1)) break;
+      const int nt = __shfl_sync(0xffffffffu, units[slot].nt, 0), dual = __shfl_sync(0xffffffffu, units[slot].dual, 0);
+      if (leader) mbar_arrive(bars + kBarSchedFree + 8 * slot);
+      if (nt < 0) break;
+      const int items = dual ? 2 * nt : nt;
+      for (int i = 0; i < items + 2 && ok; ++i) {
+        const int g = i & 1;
+        if (i >= 2) {  // P.V of item i - 2
+          const int it = i - 2;
+          const uint32_t pos = ring + 2 * (dual ? it >> 1 : it) + 1, st = pos % kStages;
+          if (!wait(bars + kBarFull + 8 * st, (pos / kStages) & 1)) break;
+          if (it < 2 && u > 0 && !wait(bars + kBarOFree + 8 * g, (u - 1) & 1)) break;
+          if (!wait(bars + kBarP + 8 * g, np[g] & 1)) break;
+          ++np[g];
+          tc_fence_after();
+          if (leader) {
+            const uint64_t v0 = sdesc(base + kRing + st * kTile, Job::kVLbo, Job::kVSbo);
+            const uint32_t o = tm + kTmemO + g * 128, p = tm + kTmemS + g * 128;
+            mma_ts(o, p, v0, ID_PV, it >= 2 ? 1u : 0u);
 #pragma unroll
-            for (int kk = 0; kk < kTok / 16; ++kk)
-              mma_ts(tmem + kTmemO + g * 128, tmem + kTmemS + g * 128 + kk * 8,
-                     sdesc(vb + kk * Job::kVStep, Job::kVLbo, Job::kVSbo), ID_PV, (it >= 2 || kk > 0) ? 1u : 0u);
-            if (!dual || g == 1) mma_commit(ctl + kBarEmpty + 8 * st);
-            if (it + 2 >= items) mma_commit(ctl + kBarO + 8 * g);
+            for (int kk = 1; kk < kTok / 16; ++kk) mma_ts_add(o, p + kk * 8, v0 + ((kk * Job::kVStep) >> 4), ID_PV);
+            if (!dual || g == 1) mma_commit(bars + kBarEmpty + 8 * st);
+            if (it + 2 >= items) mma_commit(bars + kBarO + 8 * g);
           }
-          if (i < items) {  // S of item i
-            const uint32_t pos = ring + 2 * (dual ? i >> 1 : i), st = pos % kStages;
-            ok = (i >= 2 || wait_or_abort(ctl + kBarQ + 8 * g, u & 1, abort_flag)) &&
-                 wait_or_abort(ctl + kBarFull + 8 * st, (pos / kStages) & 1, abort_flag);
-            if (!ok) break;
-            ++ns[g];
-            tc_fence_after();
-            const uint32_t kb = sbase + kRing + st * kTile;
-#pragma unroll
-            for (int kk = 0; kk < kD / 16; ++kk)
-              mma(tmem + kTmemS + g * 128, sdesc(sbase + g * kTile + (kk >> 2) * 16384 + (kk & 3) * 32, 16, 1024),
-                  sdesc(kb + (kk >> 2) * Job::kKHalf + (kk & 3) * 32, 16, Job::kKSbo), ID_S, kk > 0);
-            if (!dual || g == 1) mma_commit(ctl + kBarEmpty + 8 * st);
-            mma_commit(ctl + kBarS + 8 * g);
-          }
+          __syncwarp();
         }
-        if (ok && items == 1) mma_commit(ctl + kBarO + 8);  // group 1 had no tile
-        ring += 2 * nt;
+        if (i < items) {  // S of item i
+          const uint32_t pos = ring + 2 * (dual ? i >> 1 : i), st = pos % kStages;
+          if (i < 2 && !wait(bars + kBarQ + 8 * g, u & 1)) break;
+          if (!wait(bars + kBarFull + 8 * st, (pos / kStages) & 1)) break;
+          ++ns[g];
+          tc_fence_after();
+          if (leader) {
+            const uint64_t q0 = sdesc(base + g * kTile, 16, 1024), k0 = sdesc(base + kRing + st * kTile, 16, Job::kKSbo);
+            const uint32_t d = tm + kTmemS + g * 128;
+            mma_set(d, q0, k0, ID_S);
+#pragma unroll
+            for (int kk = 1; kk < kD / 16; ++kk)
+              mma_add(d, q0 + (((kk >> 2) * 16384 + (kk & 3) * 32) >> 4),
+                      k0 + (((kk >> 2) * Job::kKHalf + (kk & 3) * 32) >> 4), ID_S);
+            if (!dual || g == 1) mma_commit(bars + kBarEmpty + 8 * st);
+            mma_commit(bars + kBarS + 8 * g);
+          }
+          __syncwarp();
+        }
       }
-      if (*abort_flag)  // products in flight end before the tensor memory is freed (bounded)
-        for (int g = 0; g < 2; ++g)
-          if (ns[g]) mbar_wait_bounded(ctl + kBarS + 8 * g, (ns[g] - 1) & 1, kWaitLimitNs / 8);
+      if (ok && items == 1 && leader) mma_commit(bars + kBarO + 8);  // group 1 had no tile
+      ring += 2 * nt;
     }
+    if (leader && *abort_flag)  // products in flight end before the tensor memory is freed (bounded)
+      for (int g = 0; g < 2; ++g)
+        if (ns[g]) mbar_wait_bounded(bars + kBarS + 8 * g, (ns[g] - 1) & 1, kWaitLimitNs / 8);
     __syncwarp();
   } else {
     // ---------------------------------------------------------------- softmax
