@@ -434,11 +434,14 @@ struct DraftJob {
       tma5(dst + (lane - 8) * 2048, kv ? &tv : &tk, t < x.w[kCount] ? t : kMaxDraft, 0, x.head, x.w[kBeam], bar);
     }
   }
-  __device__ __forceinline__ void load_q(const flash::Unit& x, int g, int r, uint32_t dst, uint32_t bar,
-                                         Row& row) const {
+  __device__ __forceinline__ void find_row(const flash::Unit& x, int g, int r, Row& row) const {
     const int i = (x.dual ? g * flash::kRows + r : r) / v.G;
     static_cast<DraftRow&>(row) = draft_row(w, x.w[kSeg], x.w[kBeam], x.w[kE0] + i, x.w[kSplit], i < x.w[kNtok]);
     row.gg = r % v.G;
+    row.anc = row.valid && x.w[kDrafts] ? w.anc[(size_t)row.beam * w.T + row.tok] : 0ull;
+  }
+  __device__ __forceinline__ void load_q(const flash::Unit& x, int g, int r, uint32_t dst, uint32_t bar,
+                                         const Row& row) const {
     const char* src =
         reinterpret_cast<const char*>(q + (((size_t)row.beam * w.T + row.tok) * v.Hq + x.head * v.G + row.gg) * flash::kD);
 #pragma unroll
@@ -449,7 +452,6 @@ struct DraftJob {
       else
         asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(to), "r"(0) : "memory");
     }
-    row.anc = row.valid && x.w[kDrafts] ? w.anc[(size_t)row.beam * w.T + row.tok] : 0ull;
     asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory");
     fence_proxy_async_smem();
     __syncwarp();
@@ -985,6 +987,8 @@ extern "C" gb_status gb_draft_attention(gb_pool* pool, int layer, const gb_draft
   if (meets(out_dev, qb, q_dev, qb) || meets(out_dev, qb, k_dev, kb) || meets(out_dev, qb, v_dev, kb))
     return fail(pool, GB_ERR_INVALID, "draft: the output overlaps an input");
   const bool bf16 = v.dtype == GB_BF16;
+  if (bf16 && !flash::launches_with(reinterpret_cast<const void*>(k_draft)))
+    return fail(pool, GB_ERR_UNSUPPORTED, "draft: the kernel's registers");
   if (bf16 && !pool->have_tmap) return fail(pool, GB_ERR_UNSUPPORTED, "draft: no tensor map over the pool");
   if (layer > 0 && (pool->draft_epoch != pool->epoch || pool->draft_ws != d->workspace_dev || pool->draft_tokens != T))
     return fail(pool, GB_ERR_STATE, "draft: layer 0 plans the round, on the pool as it is and in this workspace");

@@ -17,7 +17,7 @@
 // P is rounded to bf16 for the tensor core (relative 2^-9 each, independent, so a result's error
 // is about that of its own rounding to bf16); the sum l is of the unrounded values.
 //
-// Warp roles (320 threads):
+// Warp roles (384 threads; warps 10 and 11 idle):
 //   warps 0-7  softmax: thread r of group g owns row r of its tile (tensor-memory lane r); also loads
 //              the row's query and writes its result
 //   warp 8     takes units from a grid-wide counter, publishes them in a ring of four, and streams
@@ -31,6 +31,9 @@
 // (bounded) for its own copies and products, the tensor memory is freed and the CTA leaves.
 #pragma once
 #include <cuda.h>
+#include <mutex>
+#include <set>
+#include <utility>
 
 #include "internal.cuh"
 #include "ptx.cuh"
@@ -40,7 +43,10 @@ namespace gb {
 namespace flash {
 
 constexpr int kRows = 128, kTok = 128, kD = 128;
-constexpr int kThreads = 320;
+constexpr int kThreads = 384;          // three warpgroups: the two softmax groups, and the others
+constexpr int kLaunchRegs = 168;       // registers a thread at launch (65536 / 384, in eights); the softmax groups then
+constexpr int kSoftmaxRegs = 216, kOtherRegs = 72;  // hold a tile's row of 128 scores, the others give theirs
+static_assert(256 * kSoftmaxRegs + 128 * kOtherRegs <= kThreads * kLaunchRegs, "the shares come from the launch's total");
 constexpr int kLoadWarp = 8, kMmaWarp = 9;
 constexpr int kStages = 5;
 constexpr int kTile = 32768;           // Q, K or V tile: 128 x 128 bf16
@@ -56,8 +62,8 @@ constexpr int kBarFull = 0;                       // [kStages]
 constexpr int kBarEmpty = kBarFull + 8 * kStages; // [kStages]
 constexpr int kBarQ = kBarEmpty + 8 * kStages;    // [2] the group's query rows are in
 constexpr int kBarS = kBarQ + 16;                 // [2] S of the group's next tile is complete
-constexpr int kBarP = kBarS + 16;                 // [2] P of it is written (and O rescaled)
-constexpr int kBarO = kBarP + 16;                 // [2] the unit's last P.V of the group is complete
+constexpr int kBarP = kBarS + 16;                 // [2 groups][2 halves] P of 64 of its keys is written (and O rescaled)
+constexpr int kBarO = kBarP + 32;                 // [2] the unit's last P.V of the group is complete
 constexpr int kBarOFree = kBarO + 16;             // [2] the group's O has been read
 constexpr int kBarX = kBarOFree + 16;             // the groups' (m, l) are in
 constexpr int kBarPatch = kBarX + 8;              // a V tile that is mended before it is handed on
@@ -108,6 +114,34 @@ __device__ __forceinline__ void st16(uint32_t taddr, const uint32_t* u) {
       "r"(u[10]), "r"(u[11]), "r"(u[12]), "r"(u[13]), "r"(u[14]), "r"(u[15])
       : "memory");
 }
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ uint64_t pack2(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t x, float& a, float& b) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x));
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+template <int N>
+__device__ __forceinline__ void regs_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void regs_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 __device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // Products with the accumulate flag known (tc.cuh's take it as a value).
@@ -122,6 +156,19 @@ __device__ __forceinline__ void mma_add(uint32_t d, uint64_t a, uint64_t b, uint
 __device__ __forceinline__ void mma_ts_add(uint32_t d, uint32_t a, uint64_t b, uint32_t id) {
   asm volatile("{\n\t.reg .pred p;\n\tsetp.eq.b32 p, 0, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
                "r"(a), "l"(b), "r"(id));
+}
+// Whether a kernel of this pipeline has the registers at launch that its warps then share out.
+inline bool launches_with(const void* kernel) {
+  static std::mutex mu;
+  static std::set<std::pair<const void*, int>> fine;  // (kernel, device)
+  int device = 0;
+  if (cudaGetDevice(&device) != cudaSuccess) return false;
+  std::lock_guard<std::mutex> lock(mu);
+  if (fine.count({kernel, device})) return true;
+  cudaFuncAttributes a{};
+  if (cudaFuncGetAttributes(&a, kernel) != cudaSuccess || a.numRegs != kLaunchRegs) return false;
+  fine.insert({kernel, device});
+  return true;
 }
 // One lane of the warp, the same each time.
 __device__ __forceinline__ bool elect_one() {
@@ -206,7 +253,8 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(ctl + kBarQ + 8 * i, Job::kQArrivals);
       mbar_init(ctl + kBarS + 8 * i, 1);
-      mbar_init(ctl + kBarP + 8 * i, 4);
+      mbar_init(ctl + kBarP + 16 * i, 4);
+      mbar_init(ctl + kBarP + 16 * i + 8, 4);
       mbar_init(ctl + kBarO + 8 * i, 1);
       mbar_init(ctl + kBarOFree + 8 * i, 8);
     }
@@ -230,135 +278,9 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
   pdl_wait();
   pdl_launch_dependents();
 
-  if (warp == kLoadWarp) {
-    // ---------------------------------------------------------------- units, K and V tiles
-    uint32_t n = 0;  // stages filled
-    uint32_t patches = 0;
-    bool ok = true;
-    const int total = job.total();
-    int next = 0;
-    if (lane == 0) next = job.ticket();
-    for (int u = 0;; ++u) {
-      const int id = __shfl_sync(0xffffffffu, next, 0);
-      if (lane == 0 && id < total) next = job.ticket();
-      const int slot = u & (kSlots - 1);
-      if (lane == 0 && u >= kSlots)
-        ok = wait_or_abort(ctl + kBarSchedFree + 8 * slot, (u / kSlots - 1) & 1, abort_flag);
-      ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
-      if (!ok || *abort_flag) break;
-      Unit x;
-      x.nt = -1;
-      if (id < total) job.unit(id, x);
-      if (lane == 0) {
-        units[slot] = x;
-        mbar_arrive(ctl + kBarSched + 8 * slot);
-      }
-      if (x.nt < 0) break;
-      for (int t = 0; t < 2 * x.nt && ok; ++t, ++n) {
-        const uint32_t st = n % kStages, dst = sbase + kRing + st * kTile;
-        const int kv = t & 1, j = t >> 1;
-        if (lane == 0 && n >= (uint32_t)kStages)
-          ok = wait_or_abort(ctl + kBarEmpty + 8 * st, (n / kStages - 1) & 1, abort_flag);
-        ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
-        if (!ok) break;
-        const uint32_t full = ctl + kBarFull + 8 * st;
-        // Rows [z0, z1) of a V tile hold no token: whatever lies in them is made 0, since 0 x NaN is NaN.
-        int z0 = 0, z1 = 0;
-        if (kv) job.stale_rows(x, j, z0, z1);
-        const uint32_t bar = z0 < z1 ? ctl + kBarPatch : full;
-        if (lane == 0) mbar_arrive_expect_tx(bar, kTile);
-        __syncwarp();
-        job.load_tile(x, j, kv, dst, bar, lane);
-        if (z0 < z1) {
-          if (lane == 0) ok = wait_or_abort(bar, patches++ & 1, abort_flag);
-          ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
-          if (!ok) break;
-          for (int i = lane; i < (z1 - z0) * 16; i += 32)
-            *reinterpret_cast<uint4*>(sm + (dst - sbase) + Job::v_row(z0 + (i >> 4), (i >> 3) & 1) + (i & 7) * 16) =
-                make_uint4(0, 0, 0, 0);
-          fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(full);
-        }
-      }
-      if (!ok) break;
-    }
-    // Copies in flight land before the CTA leaves (bounded).
-    if (lane == 0 && *abort_flag)
-      for (uint32_t k = n > (uint32_t)kStages ? n - kStages : 0; k < n; ++k)
-        mbar_wait_bounded(ctl + kBarFull + 8 * (k % kStages), (k / kStages) & 1, kWaitLimitNs / 8);
-  } else if (warp == kMmaWarp) {
-    // ---------------------------------------------------------------- products
-    // The whole warp walks the items and one lane issues: operands that are the same in every lane stay in
-    // uniform registers, where the instruction takes them from.
-    constexpr uint32_t ID_S = idesc(kRows, kTok, false), ID_PV = idesc(kRows, kD, true);
-    const bool leader = elect_one();
-    const uint32_t base = __shfl_sync(0xffffffffu, sbase, 0), tm = __shfl_sync(0xffffffffu, tmem, 0);
-    const uint32_t bars = base + kBar;
-    uint32_t ring = 0;               // stage count of the unit's first tile
-    uint32_t np[2] = {0, 0};         // S and P tiles so far, per group
-    uint32_t ns[2] = {0, 0};
-    bool ok = true;
-    auto wait = [&](uint32_t bar, uint32_t parity) {
-      ok = __all_sync(0xffffffffu, wait_or_abort(bar, parity, abort_flag));
-      return ok;
-    };
-    for (int u = 0; ok; ++u) {
-      const int slot = u & (kSlots - 1);
-      if (!wait(bars + kBarSched + 8 * slot, (u / kSlots) & 1)) break;
-      const int nt = __shfl_sync(0xffffffffu, units[slot].nt, 0), dual = __shfl_sync(0xffffffffu, units[slot].dual, 0);
-      if (leader) mbar_arrive(bars + kBarSchedFree + 8 * slot);
-      if (nt < 0) break;
-      const int items = dual ? 2 * nt : nt;
-      for (int i = 0; i < items + 2 && ok; ++i) {
-        const int g = i & 1;
-        if (i >= 2) {  // P.V of item i - 2
-          const int it = i - 2;
-          const uint32_t pos = ring + 2 * (dual ? it >> 1 : it) + 1, st = pos % kStages;
-          if (!wait(bars + kBarFull + 8 * st, (pos / kStages) & 1)) break;
-          if (it < 2 && u > 0 && !wait(bars + kBarOFree + 8 * g, (u - 1) & 1)) break;
-          if (!wait(bars + kBarP + 8 * g, np[g] & 1)) break;
-          ++np[g];
-          tc_fence_after();
-          if (leader) {
-            const uint64_t v0 = sdesc(base + kRing + st * kTile, Job::kVLbo, Job::kVSbo);
-            const uint32_t o = tm + kTmemO + g * 128, p = tm + kTmemS + g * 128;
-            mma_ts(o, p, v0, ID_PV, it >= 2 ? 1u : 0u);
-#pragma unroll
-            for (int kk = 1; kk < kTok / 16; ++kk) mma_ts_add(o, p + kk * 8, v0 + ((kk * Job::kVStep) >> 4), ID_PV);
-            if (!dual || g == 1) mma_commit(bars + kBarEmpty + 8 * st);
-            if (it + 2 >= items) mma_commit(bars + kBarO + 8 * g);
-          }
-          __syncwarp();
-        }
-        if (i < items) {  // S of item i
-          const uint32_t pos = ring + 2 * (dual ? i >> 1 : i), st = pos % kStages;
-          if (i < 2 && !wait(bars + kBarQ + 8 * g, u & 1)) break;
-          if (!wait(bars + kBarFull + 8 * st, (pos / kStages) & 1)) break;
-          ++ns[g];
-          tc_fence_after();
-          if (leader) {
-            const uint64_t q0 = sdesc(base + g * kTile, 16, 1024), k0 = sdesc(base + kRing + st * kTile, 16, Job::kKSbo);
-            const uint32_t d = tm + kTmemS + g * 128;
-            mma_set(d, q0, k0, ID_S);
-#pragma unroll
-            for (int kk = 1; kk < kD / 16; ++kk)
-              mma_add(d, q0 + (((kk >> 2) * 16384 + (kk & 3) * 32) >> 4),
-                      k0 + (((kk >> 2) * Job::kKHalf + (kk & 3) * 32) >> 4), ID_S);
-            if (!dual || g == 1) mma_commit(bars + kBarEmpty + 8 * st);
-            mma_commit(bars + kBarS + 8 * g);
-          }
-          __syncwarp();
-        }
-      }
-      if (ok && items == 1 && leader) mma_commit(bars + kBarO + 8);  // group 1 had no tile
-      ring += 2 * nt;
-    }
-    if (leader && *abort_flag)  // products in flight end before the tensor memory is freed (bounded)
-      for (int g = 0; g < 2; ++g)
-        if (ns[g]) mbar_wait_bounded(bars + kBarS + 8 * g, (ns[g] - 1) & 1, kWaitLimitNs / 8);
-    __syncwarp();
-  } else {
+  // The warpgroups share out the launch's registers; the others give theirs at once, so the groups' waits for them end.
+  if (warp < kLoadWarp) {
+    regs_inc<kSoftmaxRegs>();
     // ---------------------------------------------------------------- softmax
     const int g = warp >> 2, r = tid & 127;
     const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
@@ -378,9 +300,15 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
     };
     alive = fetch(0, x);
     typename Job::Row row;
-    if (alive && x.nt >= 0) job.load_q(x, g, r, sbase + g * kTile, ctl + kBarQ + 8 * g, row);
+    auto tiles = [&](const Unit& z) { return z.nt < 0 ? 0 : z.dual ? z.nt : (z.nt + 1 - g) / 2; };  // this group's
+    // A group without a tile loads no queries: nothing would wait for them.
+    auto begin = [&](const Unit& z, typename Job::Row& zr) {
+      if (z.nt >= 0) job.find_row(z, g, r, zr);
+      if (tiles(z) > 0) job.load_q(z, g, r, sbase + g * kTile, ctl + kBarQ + 8 * g, zr);
+    };
+    if (alive) begin(x, row);
     for (int u = 0; alive && x.nt >= 0; ++u) {
-      const int mine = x.dual ? x.nt : (x.nt + 1 - g) / 2;  // this group's tiles
+      const int mine = tiles(x);
       float m_ref = -INFINITY, l = 0.f;
       for (int i = 0; i < mine; ++i, ++n) {
         const int t = x.dual ? i : 2 * i + g;
@@ -400,14 +328,11 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
             s[c] = on ? s[c] : -INFINITY;
           }
         }
-        float mx[4] = {s[0], s[1], s[2], s[3]};
+        float mx[4] = {fmaxf(s[0], s[1]), fmaxf(s[2], s[3]), fmaxf(s[4], s[5]), fmaxf(s[6], s[7])};
 #pragma unroll
-        for (int c = 4; c < 128; c += 4) {
-          mx[0] = fmaxf(mx[0], s[c]);
-          mx[1] = fmaxf(mx[1], s[c + 1]);
-          mx[2] = fmaxf(mx[2], s[c + 2]);
-          mx[3] = fmaxf(mx[3], s[c + 3]);
-        }
+        for (int c = 8; c < 128; c += 8)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) mx[k] = max3(mx[k], s[c + 2 * k], s[c + 2 * k + 1]);
         const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * qscale;
         const bool raise = mt > m_ref + 8.f;
         if (i > 0 && __any_sync(0xffffffffu, raise)) {
@@ -424,37 +349,38 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
         }
         if (raise) m_ref = mt;
         const float neg_m = m_ref == -INFINITY ? 0.f : -m_ref;  // no key seen yet: every p is 0
-        float ls[4] = {0.f, 0.f, 0.f, 0.f};
+        const uint64_t sc2 = pack2(qscale, qscale), nm2 = pack2(neg_m, neg_m);
+        uint64_t ls[4] = {0ull, 0ull, 0ull, 0ull};  // pairs of fp32 sums
 #pragma unroll
         for (int c = 0; c < 128; c += 32) {
           uint32_t pw[16];
 #pragma unroll
-          for (int k = 0; k < 32; k += 4) {
-            const float p0 = ex2_approx(fmaf(s[c + k], qscale, neg_m));
-            const float p1 = ex2_approx(fmaf(s[c + k + 1], qscale, neg_m));
-            const float p2 = ex2_approx(fmaf(s[c + k + 2], qscale, neg_m));
-            const float p3 = ex2_approx(fmaf(s[c + k + 3], qscale, neg_m));
-            const __nv_bfloat162 a = __floats2bfloat162_rn(p0, p1), b = __floats2bfloat162_rn(p2, p3);
+          for (int k = 0; k < 32; k += 2) {
+            float p0, p1;
+            unpack2(fma2(pack2(s[c + k], s[c + k + 1]), sc2, nm2), p0, p1);
+            p0 = ex2_approx(p0);
+            p1 = ex2_approx(p1);
+            ls[(k >> 1) & 3] = add2(ls[(k >> 1) & 3], pack2(p0, p1));
+            const __nv_bfloat162 a = __floats2bfloat162_rn(p0, p1);
             pw[k / 2] = *reinterpret_cast<const uint32_t*>(&a);
-            pw[k / 2 + 1] = *reinterpret_cast<const uint32_t*>(&b);
-            ls[0] += p0;
-            ls[1] += p1;
-            ls[2] += p2;
-            ls[3] += p3;
           }
           st16(s_addr + c / 2, pw);
+          if (c == 32 || c == 96) {  // half of the tile's keys: the tensor core may begin on them
+            st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(ctl + kBarP + 16 * g + (c == 96 ? 8 : 0));
+          }
         }
-        st_wait();
-        l += (ls[0] + ls[1]) + (ls[2] + ls[3]);
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(ctl + kBarP + 8 * g);
+        float l0, l1;
+        unpack2(add2(add2(ls[0], ls[1]), add2(ls[2], ls[3])), l0, l1);
+        l += l0 + l1;
       }
       if (!alive) break;
       // The next unit's query rows: S of this unit's last tile has been read.
       if (!(alive = fetch(u + 1, y))) break;
       typename Job::Row row_y;
-      if (y.nt >= 0) job.load_q(y, g, r, sbase + g * kTile, ctl + kBarQ + 8 * g, row_y);
+      begin(y, row_y);
       if (x.dual) {
         if (!(alive = wait_or_abort(ctl + kBarO + 8 * g, u & 1, abort_flag))) break;
         tc_fence_after();
@@ -490,6 +416,147 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       row = row_y;
     }
     job.drain_q(ctl + kBarQ + 8 * g, *abort_flag != 0);
+  } else {
+    regs_dec<kOtherRegs>();
+    if (warp == kLoadWarp) {
+      // ---------------------------------------------------------------- units, K and V tiles
+      uint32_t n = 0;  // stages filled
+      uint32_t patches = 0;
+      bool ok = true;
+      const int total = job.total();
+      int next = 0;
+      if (lane == 0) next = job.ticket();
+      for (int u = 0;; ++u) {
+        const int id = __shfl_sync(0xffffffffu, next, 0);
+        if (lane == 0 && id < total) next = job.ticket();
+        const int slot = u & (kSlots - 1);
+        if (lane == 0 && u >= kSlots)
+          ok = wait_or_abort(ctl + kBarSchedFree + 8 * slot, (u / kSlots - 1) & 1, abort_flag);
+        ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
+        if (!ok || *abort_flag) break;
+        Unit x;
+        x.nt = -1;
+        if (id < total) job.unit(id, x);
+        if (lane == 0) {
+          units[slot] = x;
+          mbar_arrive(ctl + kBarSched + 8 * slot);
+        }
+        if (x.nt < 0) break;
+        for (int t = 0; t < 2 * x.nt && ok; ++t, ++n) {
+          const uint32_t st = n % kStages, dst = sbase + kRing + st * kTile;
+          const int kv = t & 1, j = t >> 1;
+          if (lane == 0 && n >= (uint32_t)kStages)
+            ok = wait_or_abort(ctl + kBarEmpty + 8 * st, (n / kStages - 1) & 1, abort_flag);
+          ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
+          if (!ok) break;
+          const uint32_t full = ctl + kBarFull + 8 * st;
+          // Rows [z0, z1) of a V tile hold no token: whatever lies in them is made 0, since 0 x NaN is NaN.
+          int z0 = 0, z1 = 0;
+          if (kv) job.stale_rows(x, j, z0, z1);
+          const uint32_t bar = z0 < z1 ? ctl + kBarPatch : full;
+          if (lane == 0) mbar_arrive_expect_tx(bar, kTile);
+          __syncwarp();
+          job.load_tile(x, j, kv, dst, bar, lane);
+          if (z0 < z1) {
+            if (lane == 0) ok = wait_or_abort(bar, patches++ & 1, abort_flag);
+            ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
+            if (!ok) break;
+            for (int i = lane; i < (z1 - z0) * 16; i += 32)
+              *reinterpret_cast<uint4*>(sm + (dst - sbase) + Job::v_row(z0 + (i >> 4), (i >> 3) & 1) + (i & 7) * 16) =
+                  make_uint4(0, 0, 0, 0);
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(full);
+          }
+        }
+        if (!ok) break;
+      }
+      // Copies in flight land before the CTA leaves (bounded).
+      if (lane == 0 && *abort_flag)
+        for (uint32_t k = n > (uint32_t)kStages ? n - kStages : 0; k < n; ++k)
+          mbar_wait_bounded(ctl + kBarFull + 8 * (k % kStages), (k / kStages) & 1, kWaitLimitNs / 8);
+    } else if (warp == kMmaWarp) {
+      // ---------------------------------------------------------------- products
+      // The whole warp walks the items and one lane issues: operands that are the same in every lane stay in
+      // uniform registers, where the instruction takes them from.
+      constexpr uint32_t ID_S = idesc(kRows, kTok, false), ID_PV = idesc(kRows, kD, true);
+      const bool leader = elect_one();
+      const uint32_t base = __shfl_sync(0xffffffffu, sbase, 0), tm = __shfl_sync(0xffffffffu, tmem, 0);
+      const uint32_t bars = base + kBar;
+      uint32_t ring = 0;               // stage count of the unit's first tile
+      uint32_t np[2] = {0, 0};         // S and P tiles so far, per group
+      uint32_t ns[2] = {0, 0};
+      uint32_t nq[2] = {0, 0};         // units in which the group had tiles
+      bool ok = true;
+      auto wait = [&](uint32_t bar, uint32_t parity) {
+        ok = __all_sync(0xffffffffu, wait_or_abort(bar, parity, abort_flag));
+        return ok;
+      };
+      for (int u = 0; ok; ++u) {
+        const int slot = u & (kSlots - 1);
+        if (!wait(bars + kBarSched + 8 * slot, (u / kSlots) & 1)) break;
+        const int nt = __shfl_sync(0xffffffffu, units[slot].nt, 0), dual = __shfl_sync(0xffffffffu, units[slot].dual, 0);
+        if (leader) mbar_arrive(bars + kBarSchedFree + 8 * slot);
+        if (nt < 0) break;
+        const int items = dual ? 2 * nt : nt;
+        for (int i = 0; i < items + 2 && ok; ++i) {
+          const int g = i & 1;
+          const uint32_t v_pos = ring + 2 * (dual ? (i - 2) >> 1 : i - 2) + 1, v_st = v_pos % kStages;
+          const uint32_t k_pos = ring + 2 * (dual ? i >> 1 : i), k_st = k_pos % kStages;
+          // The tiles first: once P is there nothing else is waited for between it and the next S.
+          if (i < items && !wait(bars + kBarFull + 8 * k_st, (k_pos / kStages) & 1)) break;
+          if (i < 2 && i < items && !wait(bars + kBarQ + 8 * g, nq[g]++ & 1)) break;
+          if (i >= 2) {  // P.V of item i - 2
+            const int it = i - 2;
+            if (!wait(bars + kBarFull + 8 * v_st, (v_pos / kStages) & 1)) break;
+            if (it < 2 && u > 0 && !wait(bars + kBarOFree + 8 * g, (u - 1) & 1)) break;
+            const uint64_t v0 = sdesc(base + kRing + v_st * kTile, Job::kVLbo, Job::kVSbo);
+            const uint32_t o = tm + kTmemO + g * 128, p = tm + kTmemS + g * 128;
+            if (!wait(bars + kBarP + 16 * g, np[g] & 1)) break;
+            tc_fence_after();
+            if (leader) {
+              mma_ts(o, p, v0, ID_PV, it >= 2 ? 1u : 0u);
+#pragma unroll
+              for (int kk = 1; kk < kTok / 32; ++kk) mma_ts_add(o, p + kk * 8, v0 + ((kk * Job::kVStep) >> 4), ID_PV);
+            }
+            __syncwarp();
+            if (!wait(bars + kBarP + 16 * g + 8, np[g] & 1)) break;
+            tc_fence_after();
+            ++np[g];
+            if (leader) {
+#pragma unroll
+              for (int kk = kTok / 32; kk < kTok / 16; ++kk)
+                mma_ts_add(o, p + kk * 8, v0 + ((kk * Job::kVStep) >> 4), ID_PV);
+              if (!dual || g == 1) mma_commit(bars + kBarEmpty + 8 * v_st);
+              if (it + 2 >= items) mma_commit(bars + kBarO + 8 * g);
+            }
+            __syncwarp();
+          }
+          if (i < items) {  // S of item i
+            ++ns[g];
+            tc_fence_after();
+            if (leader) {
+              const uint64_t q0 = sdesc(base + g * kTile, 16, 1024), k0 = sdesc(base + kRing + k_st * kTile, 16, Job::kKSbo);
+              const uint32_t d = tm + kTmemS + g * 128;
+              mma_set(d, q0, k0, ID_S);
+#pragma unroll
+              for (int kk = 1; kk < kD / 16; ++kk)
+                mma_add(d, q0 + (((kk >> 2) * 16384 + (kk & 3) * 32) >> 4),
+                        k0 + (((kk >> 2) * Job::kKHalf + (kk & 3) * 32) >> 4), ID_S);
+              if (!dual || g == 1) mma_commit(bars + kBarEmpty + 8 * k_st);
+              mma_commit(bars + kBarS + 8 * g);
+            }
+            __syncwarp();
+          }
+        }
+        if (ok && items == 1 && leader) mma_commit(bars + kBarO + 8);  // group 1 had no tile
+        ring += 2 * nt;
+      }
+      if (leader && *abort_flag)  // products in flight end before the tensor memory is freed (bounded)
+        for (int g = 0; g < 2; ++g)
+          if (ns[g]) mbar_wait_bounded(bars + kBarS + 8 * g, (ns[g] - 1) & 1, kWaitLimitNs / 8);
+      __syncwarp();
+    }
   }
   if (*abort_flag && tid == 0) job.error(GB_ERR_TIMEOUT);
   tc_fence_before();

@@ -114,16 +114,21 @@ struct PromptJob : PromptView {
         "l"(tm), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar)
         : "memory");
   }
-  __device__ __forceinline__ void load_q(const flash::Unit& x, int g, int r, uint32_t dst, uint32_t bar,
-                                         Row& row) const {
-    const int base = x.w[1] + (x.dual ? g * (flash::kRows / G) : 0);
+  __device__ __forceinline__ int first_token(const flash::Unit& x, int g) const {
+    return x.w[1] + (x.dual ? g * (flash::kRows / G) : 0);
+  }
+  __device__ __forceinline__ void find_row(const flash::Unit& x, int g, int r, Row& row) const {
+    const int base = first_token(x, g);
     row.tok = base + r / G;
     row.head = x.head * G + r % G;
     row.first = base + (r & ~31) / G;
     row.valid = row.tok < x.w[1] + x.w[2];
+  }
+  __device__ __forceinline__ void load_q(const flash::Unit& x, int g, int r, uint32_t dst, uint32_t bar,
+                                         const Row&) const {
     if (r == 0) {
       mbar_arrive_expect_tx(bar, flash::kTile);
-      tma4(dst, &tq, 0, x.head * G, x.w[0] + base, 0, bar);
+      tma4(dst, &tq, 0, x.head * G, x.w[0] + first_token(x, g), 0, bar);
     }
   }
   __device__ __forceinline__ flash::Sees sees(const flash::Unit&, const Row& row, int t) const {
@@ -314,6 +319,7 @@ extern "C" gb_status gb_prompt_attention(const gb_prompt_args* a, gb_stream_t st
   const long long most = max_units(a->dtype, G, a->num_tokens, a->num_seqs);
   PromptView view{ctl, a->num_kv_heads, G, a->num_tokens, a->scale * 1.4426950408889634f,
                   a->q_stride, a->k_stride, a->v_stride, a->out_stride};
+  if (a->dtype == GB_BF16 && !flash::launches_with(reinterpret_cast<const void*>(k_prompt))) return GB_ERR_UNSUPPORTED;
   // The tensor maps first: nothing is enqueued when one cannot be made.
   PromptJob job;
   if (a->dtype == GB_BF16) {

@@ -178,3 +178,23 @@ def test_wrapper_refuses(cuda):
                  (q, k, v, cu.long()), (q, k, v, cu.cpu()), (q, k, v, torch.zeros(4, dtype=torch.int32, device="cuda"))):
         with pytest.raises(ValueError):
             op(*args, 0.1)
+
+
+def test_units_of_one_tile_in_a_row(cuda):
+    """Many sequences within one tile of keys, where one of a unit's two groups has nothing to do, over and over: the
+    same result each time."""
+    import torch
+    from paper_2608_08020_gb300.prompt import PromptAttention
+    lengths = [1 + (7 * i) % 32 for i in range(900)]
+    cu = [0]
+    for n in lengths:
+        cu.append(cu[-1] + n)
+    q, k, v = make("bf16", cu[-1], 8, 2, 13)
+    op = PromptAttention(8, 2, 128, "bf16", max_tokens=cu[-1], max_seqs=900)
+    at = torch.tensor(cu, dtype=torch.int32, device="cuda")
+    first = op(q, k, v, at, 0.1)
+    o, a = attend(q, k, v, cu, 0.1)
+    assert bool(((first.double() - o).abs() <= bound(o, a, "bf16")).all())
+    for _ in range(200):
+        out = op(q, k, v, at, 0.1)
+    assert torch.equal(out, first) and op.status() == 0
