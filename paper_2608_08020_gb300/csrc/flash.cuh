@@ -17,15 +17,15 @@
 // P is rounded to bf16 for the tensor core (relative 2^-9 each, independent, so a result's error
 // is about that of its own rounding to bf16); the sum l is of the unrounded values.
 //
-// Warp roles (384 threads; warps 10 and 11 idle):
+// Warp roles (384 threads; warp 11 idles):
 //   warps 0-7  softmax: thread r of group g owns row r of its tile (tensor-memory lane r); also loads
 //              the row's query and writes its result
 //   warp 8     takes units from a grid-wide counter, publishes them in a ring of four, and streams
 //              K and V tiles through a ring of five 32 KiB stages (K0 V0 K1 V1 ...)
-//   warp 9     issues the products: S(i), then P.V(i - 2) before S(i) of the same group, whose S tile
-//              P overwrites; a CTA's products run in issue order
+//   warps 9-10 issue the products of a group each: S(i), then P.V(i) before S(i + 1), whose tile
+//              P overwrites; a thread's products run in issue order
 // P overwrites the first half of its S tile.  O is rescaled by its own group, and only when a maximum
-// grows by more than 8 (p <= 2^8 meanwhile): when S(i) is complete so is P.V(i - 2), issued before it.
+// grows by more than 8 (p <= 2^8 meanwhile): when S(i) is complete so is P.V(i - 1), issued before it.
 //
 // Every wait is bounded; when one runs out the CTA records the timeout, every role stops issuing and waits
 // (bounded) for its own copies and products, the tensor memory is freed and the CTA leaves.
@@ -73,7 +73,7 @@ constexpr int kUnits = kBarSchedFree + 8 * kSlots;  // int [kSlots][kUnitWords]
 constexpr int kWordTmem = kUnits + 4 * kSlots * kUnitWords;
 constexpr int kWordAbort = kWordTmem + 4;
 static_assert(kUnits % 16 == 0 && kWordAbort + 4 <= 1024, "control area");
-constexpr int kSchedReaders = 9;  // eight softmax warps, the MMA warp
+constexpr int kSchedReaders = 10;  // eight softmax warps, the two that issue products
 
 // What every role knows of a unit; w is the job's own.
 struct Unit {
@@ -248,7 +248,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
   if (tid == 0) {
     for (int i = 0; i < kStages; ++i) {
       mbar_init(ctl + kBarFull + 8 * i, 1);
-      mbar_init(ctl + kBarEmpty + 8 * i, 1);
+      mbar_init(ctl + kBarEmpty + 8 * i, 2);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(ctl + kBarQ + 8 * i, Job::kQArrivals);
@@ -475,18 +475,18 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       if (lane == 0 && *abort_flag)
         for (uint32_t k = n > (uint32_t)kStages ? n - kStages : 0; k < n; ++k)
           mbar_wait_bounded(ctl + kBarFull + 8 * (k % kStages), (k / kStages) & 1, kWaitLimitNs / 8);
-    } else if (warp == kMmaWarp) {
-      // ---------------------------------------------------------------- products
-      // The whole warp walks the items and one lane issues: operands that are the same in every lane stay in
-      // uniform registers, where the instruction takes them from.
+    } else if (warp == kMmaWarp || warp == kMmaWarp + 1) {
+      // ---------------------------------------------------------------- products, a warp per group
+      // The whole warp walks the group's tiles and one lane issues: operands that are the same in every lane
+      // stay in uniform registers, where the instruction takes them from.
       constexpr uint32_t ID_S = idesc(kRows, kTok, false), ID_PV = idesc(kRows, kD, true);
+      const int g = warp - kMmaWarp;
       const bool leader = elect_one();
       const uint32_t base = __shfl_sync(0xffffffffu, sbase, 0), tm = __shfl_sync(0xffffffffu, tmem, 0);
-      const uint32_t bars = base + kBar;
-      uint32_t ring = 0;               // stage count of the unit's first tile
-      uint32_t np[2] = {0, 0};         // S and P tiles so far, per group
-      uint32_t ns[2] = {0, 0};
-      uint32_t nq[2] = {0, 0};         // units in which the group had tiles
+      const uint32_t bars = base + kBar, s_t = tm + kTmemS + g * 128, o_t = tm + kTmemO + g * 128;
+      const uint64_t q0 = sdesc(base + g * kTile, 16, 1024);
+      uint32_t ring = 0;        // stage count of the unit's first tile
+      uint32_t n = 0, nq = 0;   // the group's tiles, and units in which it had any
       bool ok = true;
       auto wait = [&](uint32_t bar, uint32_t parity) {
         ok = __all_sync(0xffffffffu, wait_or_abort(bar, parity, abort_flag));
@@ -498,63 +498,66 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
         const int nt = __shfl_sync(0xffffffffu, units[slot].nt, 0), dual = __shfl_sync(0xffffffffu, units[slot].dual, 0);
         if (leader) mbar_arrive(bars + kBarSchedFree + 8 * slot);
         if (nt < 0) break;
-        const int items = dual ? 2 * nt : nt;
-        for (int i = 0; i < items + 2 && ok; ++i) {
-          const int g = i & 1;
-          const uint32_t v_pos = ring + 2 * (dual ? (i - 2) >> 1 : i - 2) + 1, v_st = v_pos % kStages;
-          const uint32_t k_pos = ring + 2 * (dual ? i >> 1 : i), k_st = k_pos % kStages;
+        const int mine = dual ? nt : (nt + 1 - g) / 2;
+        // A stage is free after both groups' use of it; a tile of one group's alone counts twice.
+        auto done_with = [&](uint32_t st) {
+          mma_commit(bars + kBarEmpty + 8 * st);
+          if (!dual) mma_commit(bars + kBarEmpty + 8 * st);
+        };
+        for (int i = -1; i < mine && ok; ++i) {  // P.V of tile i, then S of tile i + 1
+          const uint32_t v_pos = ring + 2 * (dual ? i : 2 * i + g) + 1, v_st = v_pos % kStages;
+          const uint32_t k_pos = ring + 2 * (dual ? i + 1 : 2 * (i + 1) + g), k_st = k_pos % kStages;
           // The tiles first: once P is there nothing else is waited for between it and the next S.
-          if (i < items && !wait(bars + kBarFull + 8 * k_st, (k_pos / kStages) & 1)) break;
-          if (i < 2 && i < items && !wait(bars + kBarQ + 8 * g, nq[g]++ & 1)) break;
-          if (i >= 2) {  // P.V of item i - 2
-            const int it = i - 2;
+          if (i + 1 < mine && !wait(bars + kBarFull + 8 * k_st, (k_pos / kStages) & 1)) break;
+          if (i < 0) {
+            if (mine > 0 && !wait(bars + kBarQ + 8 * g, nq++ & 1)) break;
+          } else {
             if (!wait(bars + kBarFull + 8 * v_st, (v_pos / kStages) & 1)) break;
-            if (it < 2 && u > 0 && !wait(bars + kBarOFree + 8 * g, (u - 1) & 1)) break;
+            if (i == 0 && u > 0 && !wait(bars + kBarOFree + 8 * g, (u - 1) & 1)) break;
             const uint64_t v0 = sdesc(base + kRing + v_st * kTile, Job::kVLbo, Job::kVSbo);
-            const uint32_t o = tm + kTmemO + g * 128, p = tm + kTmemS + g * 128;
-            if (!wait(bars + kBarP + 16 * g, np[g] & 1)) break;
+            if (!wait(bars + kBarP + 16 * g, (n - 1) & 1)) break;
             tc_fence_after();
             if (leader) {
-              mma_ts(o, p, v0, ID_PV, it >= 2 ? 1u : 0u);
+              mma_ts(o_t, s_t, v0, ID_PV, i > 0 ? 1u : 0u);
 #pragma unroll
-              for (int kk = 1; kk < kTok / 32; ++kk) mma_ts_add(o, p + kk * 8, v0 + ((kk * Job::kVStep) >> 4), ID_PV);
+              for (int kk = 1; kk < kTok / 32; ++kk) mma_ts_add(o_t, s_t + kk * 8, v0 + ((kk * Job::kVStep) >> 4), ID_PV);
             }
             __syncwarp();
-            if (!wait(bars + kBarP + 16 * g + 8, np[g] & 1)) break;
+            if (!wait(bars + kBarP + 16 * g + 8, (n - 1) & 1)) break;
             tc_fence_after();
-            ++np[g];
             if (leader) {
 #pragma unroll
               for (int kk = kTok / 32; kk < kTok / 16; ++kk)
-                mma_ts_add(o, p + kk * 8, v0 + ((kk * Job::kVStep) >> 4), ID_PV);
-              if (!dual || g == 1) mma_commit(bars + kBarEmpty + 8 * v_st);
-              if (it + 2 >= items) mma_commit(bars + kBarO + 8 * g);
+                mma_ts_add(o_t, s_t + kk * 8, v0 + ((kk * Job::kVStep) >> 4), ID_PV);
+              done_with(v_st);
+              if (i + 1 == mine) mma_commit(bars + kBarO + 8 * g);
             }
             __syncwarp();
           }
-          if (i < items) {  // S of item i
-            ++ns[g];
+          if (i + 1 < mine) {
+            ++n;
             tc_fence_after();
             if (leader) {
-              const uint64_t q0 = sdesc(base + g * kTile, 16, 1024), k0 = sdesc(base + kRing + k_st * kTile, 16, Job::kKSbo);
-              const uint32_t d = tm + kTmemS + g * 128;
-              mma_set(d, q0, k0, ID_S);
+              const uint64_t k0 = sdesc(base + kRing + k_st * kTile, 16, Job::kKSbo);
+              mma_set(s_t, q0, k0, ID_S);
 #pragma unroll
               for (int kk = 1; kk < kD / 16; ++kk)
-                mma_add(d, q0 + (((kk >> 2) * 16384 + (kk & 3) * 32) >> 4),
+                mma_add(s_t, q0 + (((kk >> 2) * 16384 + (kk & 3) * 32) >> 4),
                         k0 + (((kk >> 2) * Job::kKHalf + (kk & 3) * 32) >> 4), ID_S);
-              if (!dual || g == 1) mma_commit(bars + kBarEmpty + 8 * k_st);
               mma_commit(bars + kBarS + 8 * g);
+              done_with(k_st);
             }
             __syncwarp();
           }
         }
-        if (ok && items == 1 && leader) mma_commit(bars + kBarO + 8);  // group 1 had no tile
+        if (ok && mine == 0) {  // nothing to wait for, but no sooner than the last unit's has been taken
+          if (u > 0 && !wait(bars + kBarOFree + 8 * g, (u - 1) & 1)) break;
+          if (leader) mbar_arrive(bars + kBarO + 8 * g);
+        }
         ring += 2 * nt;
       }
-      if (leader && *abort_flag)  // products in flight end before the tensor memory is freed (bounded)
-        for (int g = 0; g < 2; ++g)
-          if (ns[g]) mbar_wait_bounded(bars + kBarS + 8 * g, (ns[g] - 1) & 1, kWaitLimitNs / 8);
+      if (leader && *abort_flag && n > 0)  // products in flight end before the tensor memory is freed (bounded)
+        mbar_wait_bounded(bars + kBarS + 8 * g, (n - 1) & 1, kWaitLimitNs / 8);
       __syncwarp();
     }
   }
