@@ -35,7 +35,7 @@ struct DraftUnit {
   int e0, ntok;    // rows: entries [e0, e0 + ntok) of the token list, or the beam's tokens
   int tok0, tok1;  // context positions
   int drafts;      // 1: then the drafted tokens
-  int split;       // its record among the beam's for this segment
+  int rec;         // a segment's: which of its pieces; a beam's own: the record, -1: the output itself
 };
 
 // Byte offsets of the workspace.
@@ -66,7 +66,7 @@ DraftLayout draft_layout(const gb_pool_config& c, int num_sms, int T) {
   d.seg_cnt = take(B * kMaxSegDepth * sizeof(int));
   d.seg_list = take(B * kMaxSegDepth * sizeof(int));
   d.off = take(B * kMaxSegDepth * sizeof(int));
-  d.list = take(B * kMaxSegDepth * T * sizeof(int));
+  d.list = take(B * kMaxSegDepth * T * sizeof(int2));
   d.acc = take(B * 4 * sizeof(int) + B * sizeof(unsigned long long));
   const size_t rows = (size_t)d.rec_cap * c.num_kv_heads * ws_rows(c, T);
   d.ml = take(rows * sizeof(float2));
@@ -89,7 +89,7 @@ struct DraftView {
   int* seg_cnt;             // [segments] drafted tokens of its beams
   int* seg_list;            // [segments] where its token list begins
   int* off;                 // [max_beams][kMaxSegDepth] the beam's place in that list
-  int* list;                // beam | depth << 10 | token << 14
+  int2* list;               // (beam | token << 10, record of the beam's first piece of the segment)
   int* acc_n;               // [max_beams] accept: tokens appended,
   int* acc_pos;             //   the position of the first,
   int* acc_old;             //   the shared tail page they moved away from, or -1
@@ -116,7 +116,7 @@ DraftView draft_view(const gb_pool* p, const DraftLayout& d, int T, void* ws) {
   v.seg_cnt = reinterpret_cast<int*>(m + d.seg_cnt);
   v.seg_list = reinterpret_cast<int*>(m + d.seg_list);
   v.off = reinterpret_cast<int*>(m + d.off);
-  v.list = reinterpret_cast<int*>(m + d.list);
+  v.list = reinterpret_cast<int2*>(m + d.list);
   v.acc_path = reinterpret_cast<unsigned long long*>(m + d.acc);
   v.acc_n = reinterpret_cast<int*>(v.acc_path + B);
   v.acc_pos = v.acc_n + B;
@@ -302,7 +302,6 @@ __global__ void __launch_bounds__(kListThreads) k_draft_plan(PoolView v, DraftVi
         const int sp = i / p.row_tiles, t = i % p.row_tiles;
         const int rows = max(0, min(tokens, p.rows - t * tokens));
         DraftUnit u;
-        u.split = sp;
         u.ntok = rows;
         if (src < nseg) {
           const int len = v.seg_len[src] * v.P, first = v.seg_i0[src] * v.P;
@@ -312,6 +311,7 @@ __global__ void __launch_bounds__(kListThreads) k_draft_plan(PoolView v, DraftVi
           u.tok0 = first + sp * p.share * flash::kTok;
           u.tok1 = first + min((sp + 1) * p.share * flash::kTok, len);
           u.drafts = 0;
+          u.rec = sp;
         } else {
           const int beam = src - nseg, n = s_len[beam];
           u.seg = -1;
@@ -320,6 +320,7 @@ __global__ void __launch_bounds__(kListThreads) k_draft_plan(PoolView v, DraftVi
           u.tok0 = min(s_start[beam] + sp * p.share * flash::kTok, n);
           u.tok1 = min(s_start[beam] + (sp + 1) * p.share * flash::kTok, n);
           u.drafts = sp == p.splits - 1;
+          u.rec = w.nrec[beam] > 1 ? w.rec_base[beam] + w.rec_off[beam * kRecOffs + kTailRec] + sp : -1;
         }
         w.units[at] = u;
       });
@@ -328,8 +329,9 @@ __global__ void __launch_bounds__(kListThreads) k_draft_plan(PoolView v, DraftVi
   for (int e = tid >> 5; e < (segs ? cap * kMaxSegDepth : 0); e += kListThreads / 32) {
     const int c = s_cnt[e / kMaxSegDepth], k = e % kMaxSegDepth;
     if (c == 0 || k >= min(v.seg_nseg[e / kMaxSegDepth], dmax)) continue;
-    int* to = w.list + w.seg_list[v.seg_bid[e]] + w.off[e];
-    for (int i = tid & 31; i < c; i += 32) to[i] = (e / kMaxSegDepth) | k << 10 | i << 14;
+    int2* to = w.list + w.seg_list[v.seg_bid[e]] + w.off[e];
+    const int beam = e / kMaxSegDepth, rec = w.rec_base[beam] + w.rec_off[beam * kRecOffs + k];
+    for (int i = tid & 31; i < c; i += 32) to[i] = make_int2(beam | i << 10, rec);
   }
 }
 
@@ -338,20 +340,11 @@ struct DraftRow {
   int beam, tok, rec;  // rec: the record, or -1 for the output
   bool valid;
 };
-__device__ __forceinline__ DraftRow draft_row(const DraftView& w, int seg, int beam, int e, int split, bool valid) {
-  DraftRow r{beam, 0, -1, valid};
-  if (!valid) return r;
-  int k = kTailRec;
-  if (seg >= 0) {
-    const int x = w.list[e];
-    r.beam = x & 1023;
-    k = (x >> 10) & 15;
-    r.tok = x >> 14;
-  } else {
-    r.tok = e;
-  }
-  if (w.nrec[r.beam] > 1) r.rec = w.rec_base[r.beam] + w.rec_off[r.beam * kRecOffs + k] + split;
-  return r;
+// Row of entry e of a segment's token list, or of a beam's own token e.
+__device__ __forceinline__ DraftRow draft_row(const DraftView& w, int seg, int beam, int e, int rec, bool valid) {
+  if (!valid || seg < 0) return {beam, valid ? e : 0, rec, valid};
+  const int2 x = w.list[e];  // a beam with a segment has a record of its own units too
+  return {x.x & 1023, x.x >> 10, x.y + rec, true};
 }
 
 struct DraftJob {
@@ -363,6 +356,7 @@ struct DraftJob {
   const __nv_bfloat16 *q, *k, *vv;  // this layer's [max_beams][T][heads][128]
   __nv_bfloat16* o;
 
+  static constexpr bool kEarlyQ = true;
   static constexpr int kQArrivals = 4;
   // Tiles land as [16 groups of 8 tokens][half of D][8][64 dims].
   static constexpr int kKHalf = 1024, kKSbo = 2048, kVLbo = 1024, kVSbo = 2048, kVStep = 4096;
@@ -379,7 +373,7 @@ struct DraftJob {
   __device__ __forceinline__ int total() const { return w.ctl[kDrUnits] * v.Hkv; }
   __device__ __forceinline__ int ticket() const { return atomicAdd(&w.ctl[kDrNext], 1); }
   // Words of a unit: those of its DraftUnit, in order.
-  enum { kSeg, kBeam, kE0, kNtok, kTok0, kTok1, kDrafts, kSplit, kCount };
+  enum { kSeg, kBeam, kE0, kNtok, kTok0, kTok1, kDrafts, kRec, kCount };
   __device__ __forceinline__ void unit(int id, flash::Unit& x) const {
     const DraftUnit e = w.units[id / v.Hkv];
     const int n = e.tok1 - e.tok0;
@@ -393,7 +387,7 @@ struct DraftJob {
     x.w[kTok0] = e.tok0;
     x.w[kTok1] = e.tok1;
     x.w[kDrafts] = e.drafts;
-    x.w[kSplit] = e.split;
+    x.w[kRec] = e.rec;
     x.w[kCount] = e.seg < 0 ? w.cnt[e.beam] : 0;
   }
   __device__ __forceinline__ bool draft_tile(const flash::Unit& x, int j) const { return x.w[kDrafts] && j == x.nt - 1; }
@@ -413,14 +407,18 @@ struct DraftJob {
         "l"(tm), "r"(0), "r"(c1), "r"(c2), "r"(c3), "r"(c4), "r"(bar)
         : "memory");
   }
-  __device__ __forceinline__ void load_tile(const flash::Unit& x, int j, int kv, uint32_t dst, uint32_t bar,
+  // The lane's page of tile j, -1: none.
+  __device__ __forceinline__ int page(const flash::Unit& x, int j, int lane) const {
+    const int pos = x.w[kTok0] + j * flash::kTok + lane * v.P;
+    if (lane * v.P >= flash::kTok || pos >= x.w[kTok1]) return -1;
+    return v.tables[(size_t)x.w[kBeam] * v.max_pages + pos / v.P];
+  }
+  __device__ __forceinline__ void load_tile(const flash::Unit& x, int j, int kv, int page, uint32_t dst, uint32_t bar,
                                             int lane) const {
-    const int c0 = x.w[kTok0] + j * flash::kTok, at = lane * v.P;
     const bool last = draft_tile(x, j);
-    if (at < (last ? 64 : flash::kTok)) {
+    if (lane * v.P < (last ? 64 : flash::kTok)) {
       int row = oob;
-      if (c0 + at < x.w[kTok1]) {
-        int page = v.tables[(size_t)x.w[kBeam] * v.max_pages + (c0 + at) / v.P];
+      if (x.w[kTok0] + j * flash::kTok + lane * v.P < x.w[kTok1]) {
         if (page < 0 || page >= v.num_pages) {
           set_status(v.ctl, GB_ERR_INVALID);
           page = 0;
@@ -436,7 +434,7 @@ struct DraftJob {
   }
   __device__ __forceinline__ void find_row(const flash::Unit& x, int g, int r, Row& row) const {
     const int i = (x.dual ? g * flash::kRows + r : r) / v.G;
-    static_cast<DraftRow&>(row) = draft_row(w, x.w[kSeg], x.w[kBeam], x.w[kE0] + i, x.w[kSplit], i < x.w[kNtok]);
+    static_cast<DraftRow&>(row) = draft_row(w, x.w[kSeg], x.w[kBeam], x.w[kE0] + i, x.w[kRec], i < x.w[kNtok]);
     row.gg = r % v.G;
     row.anc = row.valid && x.w[kDrafts] ? w.anc[(size_t)row.beam * w.T + row.tok] : 0ull;
   }
@@ -452,7 +450,10 @@ struct DraftJob {
       else
         asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(to), "r"(0) : "memory");
     }
-    asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory");
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  }
+  __device__ __forceinline__ void loaded_q(int r, uint32_t bar) const {
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
     fence_proxy_async_smem();
     __syncwarp();
     if ((r & 31) == 0) mbar_arrive(bar);
@@ -540,7 +541,7 @@ struct DraftJob {
       }
     }
   }
-  __device__ __forceinline__ void drain_q(uint32_t, bool) const {}
+  __device__ __forceinline__ void drain_q(uint32_t, bool) const { asm volatile("cp.async.wait_all;" ::: "memory"); }
 };
 
 __global__ void __launch_bounds__(flash::kThreads, 1) k_draft(const __grid_constant__ DraftJob job) {
@@ -578,7 +579,7 @@ struct DraftTile {
   }
   __device__ __forceinline__ void out(int r, int c, float4 x, float m, float l) const {
     if (!valid(r)) return;
-    const DraftRow d = draft_row(w, -1, u.beam, tok(r), u.split, true);
+    const DraftRow d = draft_row(w, -1, u.beam, tok(r), u.rec, true);
     if (d.rec < 0) {
       const float inv = 1.f / l;
       *reinterpret_cast<float4*>(op + row(r) + c) = make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv);

@@ -8,22 +8,23 @@
 // A unit has one head's query rows and nt tiles of 128 keys.  Two groups of four softmax warps each hold
 // a Q tile of 128 rows, an accumulator O and an S tile in tensor memory (512 columns in all).  In a dual
 // unit (129 to 256 rows) the groups have the two halves of the rows and every K/V tile serves
-// both; otherwise both have the same rows, group g takes tiles g, g + 2, ..., and the groups' sums are
-// joined at the unit's end, so a unit of few rows has the same two chains in flight.  While one group
-// takes the exponentials of its S tile the tensor core works for the other: per tile 1024 cycles of
-// products (128^3 x 2 at 4096 multiply-adds a cycle) against 512 of ex2 (32 a cycle) and about 600 of
+// both.  A joint unit (up to 128 rows, more than one tile) has the same rows in both groups: group g takes
+// tiles g, g + 2, ..., and the groups' sums are joined at its end.  A unit of up to 128 rows and one tile is one
+// group's alone, the groups taking turns.  So there are two chains in flight: while one group
+// takes the exponentials of its S tile the tensor core works for the other.  Per tile 1024 cycles of
+// products (128^3 x 2 at 4096 multiply-adds a cycle) stand against 512 of ex2 (32 a cycle) and about 400 of
 // other instructions.
 //
 // P is rounded to bf16 for the tensor core (relative 2^-9 each, independent, so a result's error
 // is about that of its own rounding to bf16); the sum l is of the unrounded values.
 //
-// Warp roles (384 threads; warp 11 idles):
-//   warps 0-7  softmax: thread r of group g owns row r of its tile (tensor-memory lane r); also loads
-//              the row's query and writes its result
-//   warp 8     takes units from a grid-wide counter, publishes them in a ring of four, and streams
-//              K and V tiles through a ring of five 32 KiB stages (K0 V0 K1 V1 ...)
-//   warps 9-10 issue the products of a group each: S(i), then P.V(i) before S(i + 1), whose tile
-//              P overwrites; a thread's products run in issue order
+// Warp roles (384 threads):
+//   warps 0-7   softmax: thread r of group g owns row r of its tile (tensor-memory lane r); also loads
+//               the row's query and writes its result
+//   warp 8      streams K and V tiles through a ring of five 32 KiB stages (K0 V0 K1 V1 ...)
+//   warps 9-10  issue the products of a group each: S(i), then P.V(i) before S(i + 1), whose tile
+//               P overwrites; a thread's products run in issue order
+//   warp 11     takes units from a grid-wide counter and publishes them in a ring of eight, ahead of the others
 // P overwrites the first half of its S tile.  O is rescaled by its own group, and only when a maximum
 // grows by more than 8 (p <= 2^8 meanwhile): when S(i) is complete so is P.V(i - 1), issued before it.
 //
@@ -47,7 +48,7 @@ constexpr int kThreads = 384;          // three warpgroups: the two softmax grou
 constexpr int kLaunchRegs = 168;       // registers a thread at launch (65536 / 384, in eights); the softmax groups then
 constexpr int kSoftmaxRegs = 216, kOtherRegs = 72;  // hold a tile's row of 128 scores, the others give theirs
 static_assert(256 * kSoftmaxRegs + 128 * kOtherRegs <= kThreads * kLaunchRegs, "the shares come from the launch's total");
-constexpr int kLoadWarp = 8, kMmaWarp = 9;
+constexpr int kLoadWarp = 8, kMmaWarp = 9, kUnitWarp = 11;
 constexpr int kStages = 5;
 constexpr int kTile = 32768;           // Q, K or V tile: 128 x 128 bf16
 constexpr int kRing = 2 * kTile;       // after the two Q tiles
@@ -57,23 +58,30 @@ constexpr int kSmem = kXch + 2048;
 static_assert(kSmem <= 232448, "shared memory per block");
 constexpr uint32_t kTmemS = 0, kTmemO = 256;  // column of group 0; group 1 is 128 further
 
-constexpr int kSlots = 4, kUnitWords = 16;
-constexpr int kBarFull = 0;                       // [kStages]
-constexpr int kBarEmpty = kBarFull + 8 * kStages; // [kStages]
+constexpr int kSlots = 8, kUnitWords = 16;  // units known ahead
+// Three "full" barriers a stage, used in turn (ring position mod 15).  A group that has no tile of a unit goes on to the
+// next one and may wait for a position up to 8 past the last one it saw filled.  A wait on a barrier whose phase before
+// last has not ended would pass at once; position p - 15 has been consumed, since p - 10, which is before the one seen, was
+// issued into its stage.
+constexpr int kFulls = 3 * kStages;
+constexpr int kBarFull = 0;                       // [kFulls]
+constexpr int kBarEmpty = kBarFull + 8 * kFulls;  // [kStages]
 constexpr int kBarQ = kBarEmpty + 8 * kStages;    // [2] the group's query rows are in
 constexpr int kBarS = kBarQ + 16;                 // [2] S of the group's next tile is complete
 constexpr int kBarP = kBarS + 16;                 // [2 groups][2 halves] P of 64 of its keys is written (and O rescaled)
 constexpr int kBarO = kBarP + 32;                 // [2] the unit's last P.V of the group is complete
 constexpr int kBarOFree = kBarO + 16;             // [2] the group's O has been read
-constexpr int kBarX = kBarOFree + 16;             // the groups' (m, l) are in
-constexpr int kBarPatch = kBarX + 8;              // a V tile that is mended before it is handed on
-constexpr int kBarSched = kBarPatch + 8;          // [kSlots]
+constexpr int kBarX = kBarOFree + 16;             // a joint unit's (m, l) are in
+constexpr int kBarXDone = kBarX + 8;              // and have been read
+constexpr int kBarPatch = kBarXDone + 8;              // a V tile that is mended before it is handed on
+constexpr int kBarTake = kBarPatch + 8;           // the loading warp has begun on a unit: the next may be taken
+constexpr int kBarSched = kBarTake + 8;           // [kSlots]
 constexpr int kBarSchedFree = kBarSched + 8 * kSlots;
-constexpr int kUnits = kBarSchedFree + 8 * kSlots;  // int [kSlots][kUnitWords]
+constexpr int kUnits = (kBarSchedFree + 8 * kSlots + 15) / 16 * 16;  // int [kSlots][kUnitWords]
 constexpr int kWordTmem = kUnits + 4 * kSlots * kUnitWords;
 constexpr int kWordAbort = kWordTmem + 4;
 static_assert(kUnits % 16 == 0 && kWordAbort + 4 <= 1024, "control area");
-constexpr int kSchedReaders = 10;  // eight softmax warps, the two that issue products
+constexpr int kSchedReaders = 11;  // eight softmax warps, the two that issue products, the one that loads
 
 // What every role knows of a unit; w is the job's own.
 struct Unit {
@@ -83,6 +91,11 @@ struct Unit {
   int w[kUnitWords - 3];
 };
 static_assert(sizeof(Unit) == 4 * kUnitWords, "unit words");
+
+// Whether group g has tiles of a CTA's u-th unit, and how many.
+__device__ __forceinline__ bool takes_part(int nt, int dual, int u, int g) { return dual || nt > 1 || (u & 1) == g; }
+__device__ __forceinline__ int group_tiles(int nt, int dual, int g) { return dual || nt == 1 ? nt : (nt + 1 - g) / 2; }
+__device__ __forceinline__ int group_tile(int nt, int dual, int g, int i) { return dual || nt == 1 ? i : 2 * i + g; }
 
 // The columns are handed out only after the wait: the registers pass through it.
 __device__ __forceinline__ void ld32_issue(uint32_t taddr, uint32_t* r) {
@@ -170,6 +183,21 @@ inline bool launches_with(const void* kernel) {
   fine.insert({kernel, device});
   return true;
 }
+// A whole warp's wait_or_abort, whose lanes stay together.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  uint64_t t0 = 0;
+  for (uint32_t it = 1;; ++it) {
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+    if ((it & 63) == 0) {
+      const uint64_t now = globaltimer_ns();
+      if (t0 == 0) t0 = now;
+      if (__any_sync(0xffffffffu, *abort_flag != 0 || now - t0 > kWaitLimitNs)) {
+        *abort_flag = 1;
+        return false;
+      }
+    }
+  }
+}
 // One lane of the warp, the same each time.
 __device__ __forceinline__ bool elect_one() {
   uint32_t p;
@@ -237,7 +265,8 @@ __device__ __forceinline__ bool not_finite(const __nv_bfloat16* v, int c0, int c
 
 template <class Job>
 __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  // (the warp by a shuffle: what follows from it is then known to be the same in every lane)
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const uint32_t sbase = smem_addr(sm), ctl = sbase + kBar;
   volatile int* abort_flag = reinterpret_cast<volatile int*>(sm + kBar + kWordAbort);
   Unit* units = reinterpret_cast<Unit*>(sm + kBar + kUnits);
@@ -246,8 +275,8 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
     return;
   }
   if (tid == 0) {
+    for (int i = 0; i < kFulls; ++i) mbar_init(ctl + kBarFull + 8 * i, 1);
     for (int i = 0; i < kStages; ++i) {
-      mbar_init(ctl + kBarFull + 8 * i, 1);
       mbar_init(ctl + kBarEmpty + 8 * i, 2);
     }
     for (int i = 0; i < 2; ++i) {
@@ -259,7 +288,9 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       mbar_init(ctl + kBarOFree + 8 * i, 8);
     }
     mbar_init(ctl + kBarX, 8);
+    mbar_init(ctl + kBarXDone, 8);
     mbar_init(ctl + kBarPatch, 1);
+    mbar_init(ctl + kBarTake, 1);
     for (int i = 0; i < kSlots; ++i) {
       mbar_init(ctl + kBarSched + 8 * i, 1);
       mbar_init(ctl + kBarSchedFree + 8 * i, kSchedReaders);
@@ -287,32 +318,54 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
     const uint32_t s_addr = tmem + kTmemS + g * 128 + lane_base, o_addr = tmem + kTmemO + lane_base;
     float2* xch = reinterpret_cast<float2*>(sm + kXch);
     const float qscale = job.qscale;
-    uint32_t n = 0, nx = 0;  // tiles of this group, joined units
+    uint32_t n = 0, nx = 0;       // tiles of this group, joint units
+    int u_next = 0;               // the unit read next
+    uint32_t taken[2] = {0, 0};   // units so far in which each group had tiles
     bool alive = true;
-    Unit x, y;
-    auto fetch = [&](int u, Unit& to) {  // unit u, once it is known
-      const int slot = u & (kSlots - 1);
-      if (!wait_or_abort(ctl + kBarSched + 8 * slot, (u / kSlots) & 1, abort_flag)) return false;
-      to = units[slot];
-      __syncwarp();
-      if (lane == 0) mbar_arrive(ctl + kBarSchedFree + 8 * slot);
+    typename Job::Row row, row_y;
+    // The group's next unit: its words stay in shared memory until the group is done with it.
+    auto next_unit = [&](int& slot) {
+      for (;; ++u_next) {
+        slot = u_next & (kSlots - 1);
+        if (!wait_or_abort(ctl + kBarSched + 8 * slot, (u_next / kSlots) & 1, abort_flag)) return false;
+        const int nt = units[slot].nt, dual = units[slot].dual;
+        if (nt < 0) return true;
+        const bool in0 = takes_part(nt, dual, u_next, 0), in1 = takes_part(nt, dual, u_next, 1);
+        taken[0] += in0;
+        taken[1] += in1;
+        if (g == 0 ? in0 : in1) {
+          ++u_next;
+          return true;
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(ctl + kBarSchedFree + 8 * slot);
+      }
+    };
+    int sx = 0, sy = 0;
+    alive = next_unit(sx);
+    if (alive && units[sx].nt >= 0) {
+      job.find_row(units[sx], g, r, row);
+      job.load_q(units[sx], g, r, sbase + g * kTile, ctl + kBarQ + 8 * g, row);
+      job.loaded_q(r, ctl + kBarQ + 8 * g);
+    }
+    // The group's last S of a unit is complete: the next unit's query rows may come.
+    auto begin_next = [&]() {
+      if (!next_unit(sy)) return false;
+      if (units[sy].nt >= 0) {
+        job.find_row(units[sy], g, r, row_y);
+        job.load_q(units[sy], g, r, sbase + g * kTile, ctl + kBarQ + 8 * g, row_y);
+      }
       return true;
     };
-    alive = fetch(0, x);
-    typename Job::Row row;
-    auto tiles = [&](const Unit& z) { return z.nt < 0 ? 0 : z.dual ? z.nt : (z.nt + 1 - g) / 2; };  // this group's
-    // A group without a tile loads no queries: nothing would wait for them.
-    auto begin = [&](const Unit& z, typename Job::Row& zr) {
-      if (z.nt >= 0) job.find_row(z, g, r, zr);
-      if (tiles(z) > 0) job.load_q(z, g, r, sbase + g * kTile, ctl + kBarQ + 8 * g, zr);
-    };
-    if (alive) begin(x, row);
-    for (int u = 0; alive && x.nt >= 0; ++u) {
-      const int mine = tiles(x);
+    while (alive && units[sx].nt >= 0) {
+      const Unit& x = units[sx];
+      const int nt = x.nt, dual = x.dual, mine = group_tiles(nt, dual, g);
+      const uint32_t c0 = taken[0] - 1, c1 = taken[1] - 1;  // this unit's number among each group's
       float m_ref = -INFINITY, l = 0.f;
       for (int i = 0; i < mine; ++i, ++n) {
-        const int t = x.dual ? i : 2 * i + g;
+        const int t = group_tile(nt, dual, g, i);
         if (!wait_or_abort(ctl + kBarS + 8 * g, n & 1, abort_flag)) { alive = false; break; }
+        if (Job::kEarlyQ && i + 1 == mine && !(alive = begin_next())) break;
         tc_fence_after();
         uint32_t su[128];
 #pragma unroll
@@ -377,12 +430,10 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
         l += l0 + l1;
       }
       if (!alive) break;
-      // The next unit's query rows: S of this unit's last tile has been read.
-      if (!(alive = fetch(u + 1, y))) break;
-      typename Job::Row row_y;
-      begin(y, row_y);
-      if (x.dual) {
-        if (!(alive = wait_or_abort(ctl + kBarO + 8 * g, u & 1, abort_flag))) break;
+      if (!Job::kEarlyQ && !(alive = begin_next())) break;
+      if (units[sy].nt >= 0) job.loaded_q(r, ctl + kBarQ + 8 * g);
+      if (dual || nt == 1) {
+        if (!(alive = wait_or_abort(ctl + kBarO + 8 * g, (g == 0 ? c0 : c1) & 1, abort_flag))) break;
         tc_fence_after();
         job.out(x, row, o_addr + g * 128, 0, false, 1.f, 0.f, 0, 128, m_ref, l);
         tc_fence_before();
@@ -393,88 +444,159 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
         xch[g * 128 + r] = make_float2(m_ref, l);
         __syncwarp();
         if (lane == 0) mbar_arrive(ctl + kBarX);
-        if (!(alive = wait_or_abort(ctl + kBarX, nx & 1, abort_flag) && wait_or_abort(ctl + kBarO, u & 1, abort_flag) &&
-                      wait_or_abort(ctl + kBarO + 8, u & 1, abort_flag)))
+        if (!(alive = wait_or_abort(ctl + kBarX, nx & 1, abort_flag) && wait_or_abort(ctl + kBarO, c0 & 1, abort_flag) &&
+                      wait_or_abort(ctl + kBarO + 8, c1 & 1, abort_flag)))
           break;
-        ++nx;
         const float2 other = xch[(1 - g) * 128 + r];
         const float m = fmaxf(m_ref, other.x), ref = m == -INFINITY ? 0.f : m;
         const float mine_w = exp2f(m_ref - ref), other_w = exp2f(other.x - ref);
         tc_fence_after();
-        job.out(x, row, o_addr + 64 * g, o_addr + 128 + 64 * g, x.nt > 1, g == 0 ? mine_w : other_w,
+        job.out(x, row, o_addr + 64 * g, o_addr + 128 + 64 * g, true, g == 0 ? mine_w : other_w,
                 g == 0 ? other_w : mine_w, 64 * g, 64, m, l * mine_w + other.y * other_w);
         tc_fence_before();
         __syncwarp();
         if (lane == 0) {
           mbar_arrive(ctl + kBarOFree);
           mbar_arrive(ctl + kBarOFree + 8);
+          mbar_arrive(ctl + kBarXDone);
         }
         // Both groups have read the exchange before either writes it again.
-        if (!(alive = wait_or_abort(ctl + kBarOFree, u & 1, abort_flag))) break;
+        if (!(alive = wait_or_abort(ctl + kBarXDone, nx & 1, abort_flag))) break;
+        ++nx;
       }
-      x = y;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(ctl + kBarSchedFree + 8 * sx);
+      sx = sy;
       row = row_y;
     }
     job.drain_q(ctl + kBarQ + 8 * g, *abort_flag != 0);
   } else {
     regs_dec<kOtherRegs>();
-    if (warp == kLoadWarp) {
-      // ---------------------------------------------------------------- units, K and V tiles
-      uint32_t n = 0;  // stages filled
-      uint32_t patches = 0;
-      bool ok = true;
+    if (warp == kUnitWarp) {
+      // ---------------------------------------------------------------- units
+      // One unit ahead of the loading warp: its words are there when that warp gets to it, and no CTA sits on units that
+      // another could begin (taking four ahead cost 40% of a long prompt, whose CTAs have seven units each).
       const int total = job.total();
-      int next = 0;
-      if (lane == 0) next = job.ticket();
+      bool ok = true;
       for (int u = 0;; ++u) {
-        const int id = __shfl_sync(0xffffffffu, next, 0);
-        if (lane == 0 && id < total) next = job.ticket();
-        const int slot = u & (kSlots - 1);
-        if (lane == 0 && u >= kSlots)
-          ok = wait_or_abort(ctl + kBarSchedFree + 8 * slot, (u / kSlots - 1) & 1, abort_flag);
-        ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
-        if (!ok || *abort_flag) break;
+        if (lane == 0 && u > 0) ok = wait_or_abort(ctl + kBarTake, (u - 1) & 1, abort_flag);
+        int id = 0;
+        if (lane == 0 && ok) id = job.ticket();
+        id = __shfl_sync(0xffffffffu, id, 0);
         Unit x;
         x.nt = -1;
         if (id < total) job.unit(id, x);
+        const int slot = u & (kSlots - 1);
+        if (lane == 0 && ok && u >= kSlots)
+          ok = wait_or_abort(ctl + kBarSchedFree + 8 * slot, (u / kSlots - 1) & 1, abort_flag);
+        ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
+        if (!ok || *abort_flag) break;
         if (lane == 0) {
           units[slot] = x;
           mbar_arrive(ctl + kBarSched + 8 * slot);
         }
         if (x.nt < 0) break;
-        for (int t = 0; t < 2 * x.nt && ok; ++t, ++n) {
-          const uint32_t st = n % kStages, dst = sbase + kRing + st * kTile;
+      }
+    } else if (warp == kLoadWarp) {
+      // ---------------------------------------------------------------- K and V tiles
+      uint32_t n = 0;  // stages filled
+      uint32_t patches = 0;
+      uint32_t p_dst = 0, p_full = 0;  // the V tile that waits to be mended
+      int z0 = 0, z1 = 0;              // its rows that hold no token
+      bool ok = true;
+      Unit x;
+      auto fetch = [&](int u) {
+        const int slot = u & (kSlots - 1);
+        if (lane == 0) ok = wait_or_abort(ctl + kBarSched + 8 * slot, (u / kSlots) & 1, abort_flag);
+        ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
+        if (!ok) return;
+        __syncwarp();
+        x = units[slot];
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(ctl + kBarSchedFree + 8 * slot);
+          mbar_arrive(ctl + kBarTake);
+        }
+      };
+      // Whatever lies in the rows of a V tile that hold no token is made 0, since 0 x NaN is NaN.
+      auto mend = [&]() {
+        for (int i = lane; i < (z1 - z0) * 16; i += 32)
+          *reinterpret_cast<uint4*>(sm + (p_dst - sbase) + Job::v_row(z0 + (i >> 4), (i >> 3) & 1) + (i & 7) * 16) =
+              make_uint4(0, 0, 0, 0);
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_full);
+        ++patches;
+        z0 = z1 = 0;
+      };
+      // A stage's release, or with `landed` only the tile to be mended, which meanwhile is mended as soon as it is in.
+      auto wait = [&](uint32_t bar, uint32_t parity, bool landed) {
+        if (z0 >= z1) {  // (a suspended wait leaves the issue slots to the softmax)
+          const bool in = lane != 0 || wait_or_abort(bar, parity, abort_flag);
+          return __shfl_sync(0xffffffffu, in ? 1 : 0, 0) != 0;
+        }
+        uint64_t t0 = 0;
+        for (uint32_t it = 1;; ++it) {
+          int f = 0;
+          if (lane == 0) {
+            if (z0 < z1 && mbar_test(ctl + kBarPatch, patches & 1)) f = 2;
+            else if (!landed && mbar_test(bar, parity)) f = 1;
+            else if ((it & 63) == 0) {
+              const uint64_t now = globaltimer_ns();
+              if (t0 == 0) t0 = now;
+              if (*abort_flag || now - t0 > kWaitLimitNs) {
+                *abort_flag = 1;
+                f = 3;
+              }
+            }
+          }
+          f = __shfl_sync(0xffffffffu, f, 0);
+          if (f == 3) return false;
+          if (f == 2) mend();
+          if (f == 1 || (landed && f == 2)) return true;
+        }
+      };
+      fetch(0);
+      int page = ok && x.nt >= 0 ? job.page(x, 0, lane) : 0;  // pages of the next tile, a tile ahead
+      for (int u = 0; ok && x.nt >= 0; ++u) {
+        const Unit now = x;
+        for (int t = 0; t < 2 * now.nt && ok; ++t, ++n) {
+          const uint32_t st = n % kStages, dst = sbase + kRing + st * kTile, full = ctl + kBarFull + 8 * (n % kFulls);
           const int kv = t & 1, j = t >> 1;
-          if (lane == 0 && n >= (uint32_t)kStages)
-            ok = wait_or_abort(ctl + kBarEmpty + 8 * st, (n / kStages - 1) & 1, abort_flag);
-          ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
+          if (n >= (uint32_t)kStages) ok = wait(ctl + kBarEmpty + 8 * st, (n / kStages - 1) & 1, false);
           if (!ok) break;
-          const uint32_t full = ctl + kBarFull + 8 * st;
-          // Rows [z0, z1) of a V tile hold no token: whatever lies in them is made 0, since 0 x NaN is NaN.
-          int z0 = 0, z1 = 0;
-          if (kv) job.stale_rows(x, j, z0, z1);
-          const uint32_t bar = z0 < z1 ? ctl + kBarPatch : full;
+          uint32_t bar = full;
+          int s0 = 0, s1 = 0;
+          if (kv) job.stale_rows(now, j, s0, s1);
+          if (s0 < s1) {
+            if (z0 < z1 && !(ok = wait(0, 0, true))) break;  // one at a time
+            z0 = s0;
+            z1 = s1;
+            p_dst = dst;
+            p_full = full;
+            bar = ctl + kBarPatch;
+          }
           if (lane == 0) mbar_arrive_expect_tx(bar, kTile);
           __syncwarp();
-          job.load_tile(x, j, kv, dst, bar, lane);
-          if (z0 < z1) {
-            if (lane == 0) ok = wait_or_abort(bar, patches++ & 1, abort_flag);
-            ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
-            if (!ok) break;
-            for (int i = lane; i < (z1 - z0) * 16; i += 32)
-              *reinterpret_cast<uint4*>(sm + (dst - sbase) + Job::v_row(z0 + (i >> 4), (i >> 3) & 1) + (i & 7) * 16) =
-                  make_uint4(0, 0, 0, 0);
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(full);
+          job.load_tile(now, j, kv, page, dst, bar, lane);
+          if (kv) {
+            if (j + 1 < now.nt) {
+              page = job.page(now, j + 1, lane);
+            } else {
+              fetch(u + 1);
+              if (ok && x.nt >= 0) page = job.page(x, 0, lane);
+            }
           }
         }
-        if (!ok) break;
       }
+      if (ok && z0 < z1) ok = wait(0, 0, true);
       // Copies in flight land before the CTA leaves (bounded).
-      if (lane == 0 && *abort_flag)
+      if (lane == 0 && *abort_flag) {
+        if (z0 < z1) mbar_wait_bounded(ctl + kBarPatch, patches & 1, kWaitLimitNs / 8);
         for (uint32_t k = n > (uint32_t)kStages ? n - kStages : 0; k < n; ++k)
-          mbar_wait_bounded(ctl + kBarFull + 8 * (k % kStages), (k / kStages) & 1, kWaitLimitNs / 8);
+          if (ctl + kBarFull + 8 * (k % kFulls) != p_full || z0 >= z1)
+            mbar_wait_bounded(ctl + kBarFull + 8 * (k % kFulls), (k / kFulls) & 1, kWaitLimitNs / 8);
+      }
     } else if (warp == kMmaWarp || warp == kMmaWarp + 1) {
       // ---------------------------------------------------------------- products, a warp per group
       // The whole warp walks the group's tiles and one lane issues: operands that are the same in every lane
@@ -486,10 +608,10 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       const uint32_t bars = base + kBar, s_t = tm + kTmemS + g * 128, o_t = tm + kTmemO + g * 128;
       const uint64_t q0 = sdesc(base + g * kTile, 16, 1024);
       uint32_t ring = 0;        // stage count of the unit's first tile
-      uint32_t n = 0, nq = 0;   // the group's tiles, and units in which it had any
+      uint32_t n = 0, c = 0;    // the group's tiles, and units in which it had any
       bool ok = true;
       auto wait = [&](uint32_t bar, uint32_t parity) {
-        ok = __all_sync(0xffffffffu, wait_or_abort(bar, parity, abort_flag));
+        ok = warp_wait(bar, parity, abort_flag);
         return ok;
       };
       for (int u = 0; ok; ++u) {
@@ -498,22 +620,26 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
         const int nt = __shfl_sync(0xffffffffu, units[slot].nt, 0), dual = __shfl_sync(0xffffffffu, units[slot].dual, 0);
         if (leader) mbar_arrive(bars + kBarSchedFree + 8 * slot);
         if (nt < 0) break;
-        const int mine = dual ? nt : (nt + 1 - g) / 2;
+        if (!takes_part(nt, dual, u, g)) {
+          ring += 2 * nt;
+          continue;
+        }
+        const int mine = group_tiles(nt, dual, g);
         // A stage is free after both groups' use of it; a tile of one group's alone counts twice.
         auto done_with = [&](uint32_t st) {
           mma_commit(bars + kBarEmpty + 8 * st);
           if (!dual) mma_commit(bars + kBarEmpty + 8 * st);
         };
         for (int i = -1; i < mine && ok; ++i) {  // P.V of tile i, then S of tile i + 1
-          const uint32_t v_pos = ring + 2 * (dual ? i : 2 * i + g) + 1, v_st = v_pos % kStages;
-          const uint32_t k_pos = ring + 2 * (dual ? i + 1 : 2 * (i + 1) + g), k_st = k_pos % kStages;
+          const uint32_t v_pos = ring + 2 * group_tile(nt, dual, g, i) + 1, v_st = v_pos % kStages;
+          const uint32_t k_pos = ring + 2 * group_tile(nt, dual, g, i + 1), k_st = k_pos % kStages;
           // The tiles first: once P is there nothing else is waited for between it and the next S.
-          if (i + 1 < mine && !wait(bars + kBarFull + 8 * k_st, (k_pos / kStages) & 1)) break;
+          if (i + 1 < mine && !wait(bars + kBarFull + 8 * (k_pos % kFulls), (k_pos / kFulls) & 1)) break;
           if (i < 0) {
-            if (mine > 0 && !wait(bars + kBarQ + 8 * g, nq++ & 1)) break;
+            if (!wait(bars + kBarQ + 8 * g, c & 1)) break;
           } else {
-            if (!wait(bars + kBarFull + 8 * v_st, (v_pos / kStages) & 1)) break;
-            if (i == 0 && u > 0 && !wait(bars + kBarOFree + 8 * g, (u - 1) & 1)) break;
+            if (!wait(bars + kBarFull + 8 * (v_pos % kFulls), (v_pos / kFulls) & 1)) break;
+            if (i == 0 && c > 0 && !wait(bars + kBarOFree + 8 * g, (c - 1) & 1)) break;
             const uint64_t v0 = sdesc(base + kRing + v_st * kTile, Job::kVLbo, Job::kVSbo);
             if (!wait(bars + kBarP + 16 * g, (n - 1) & 1)) break;
             tc_fence_after();
@@ -550,10 +676,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
             __syncwarp();
           }
         }
-        if (ok && mine == 0) {  // nothing to wait for, but no sooner than the last unit's has been taken
-          if (u > 0 && !wait(bars + kBarOFree + 8 * g, (u - 1) & 1)) break;
-          if (leader) mbar_arrive(bars + kBarO + 8 * g);
-        }
+        ++c;
         ring += 2 * nt;
       }
       if (leader && *abort_flag && n > 0)  // products in flight end before the tensor memory is freed (bounded)

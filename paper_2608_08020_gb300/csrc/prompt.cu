@@ -75,6 +75,7 @@ struct PromptJob : PromptView {
   const __nv_bfloat16 *q, *k, *v;
   __nv_bfloat16* o;
 
+  static constexpr bool kEarlyQ = false;
   static constexpr int kQArrivals = 1;
   // Tiles land as [half of D][128 tokens][64 dims].
   static constexpr int kKHalf = 16384, kKSbo = 1024, kVLbo = 16384, kVSbo = 1024, kVStep = 2048;
@@ -102,7 +103,8 @@ struct PromptJob : PromptView {
   }
   // A tile's rows past the sequence are the next one's, or past the tensor and zeros.
   __device__ __forceinline__ void stale_rows(const flash::Unit&, int, int&, int&) const {}
-  __device__ __forceinline__ void load_tile(const flash::Unit& x, int j, int kv, uint32_t dst, uint32_t bar,
+  __device__ __forceinline__ int page(const flash::Unit&, int, int) const { return 0; }
+  __device__ __forceinline__ void load_tile(const flash::Unit& x, int j, int kv, int, uint32_t dst, uint32_t bar,
                                             int lane) const {
     if (lane == 0) tma4(dst, kv ? &tv : &tk, 0, x.w[0] + j * flash::kTok, 0, x.head, bar);
   }
@@ -131,6 +133,7 @@ struct PromptJob : PromptView {
       tma4(dst, &tq, 0, x.head * G, x.w[0] + first_token(x, g), 0, bar);
     }
   }
+  __device__ __forceinline__ void loaded_q(int, uint32_t) const {}
   __device__ __forceinline__ flash::Sees sees(const flash::Unit&, const Row& row, int t) const {
     const int k0 = t * flash::kTok;
     return {k0 + flash::kTok - 1 <= row.first, row.tok - k0 + 1, 0ull};
