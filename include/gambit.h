@@ -569,7 +569,7 @@ gb_status gb_draft_workspace_bytes(gb_pool* pool, int n_draft, size_t* bytes);
  *   out[b][i][h] = sum_j p_j v_j,  p = softmax_j(scale * q[b][i][h] . k_j)
  * over the tokens j of slot b's context (this layer's pages) and over i and its ancestors.
  *   q_dev, out_dev: [max_beams][n_draft][Hq][D] in kv_dtype;  k_dev, v_dev: [max_beams][n_draft][Hkv][D]
- * all 16-byte aligned, out_dev apart from the others.  Rows of inactive slots and of tokens from the
+ * 16-byte aligned (out_dev: 32), out_dev apart from the others.  Rows of inactive slots and of tokens from the
  * count on are zero in out_dev and ignored in the inputs; values that a row does not see do not reach its
  * result, whatever they are.  The pool's contexts are not changed.
  * Layer 0 plans the round; the other layers may follow in any order, and again, until the pool changes

@@ -14,6 +14,7 @@
 // Bound by the reads of the cache while rows x 2 flops a byte stay below the machine's ~280, i.e. up to some
 // 100 rows a shared token, and by the tensor cores beyond.
 #include <algorithm>
+#include <type_traits>
 
 #include "flash.cuh"
 #include "tile.cuh"
@@ -27,20 +28,20 @@ constexpr int kTailRec = kMaxSegDepth;  // rec_off column of a beam's own units
 constexpr int kRecOffs = kMaxSegDepth + 1;
 
 // Workspace words of control.
-enum DraftCtl : int { kDrUnits = 0, kDrNext = 1, kDrList = 2, kDrOk = 3, kDrWords = 64 };
+enum DraftCtl : int { kDrUnits = 0, kDrList = 1, kDrWords = 64 };
 
 struct DraftUnit {
   int seg;         // -1: a beam's own unit
   int beam;        // whose table lists the pages
   int e0, ntok;    // rows: entries [e0, e0 + ntok) of the token list, or the beam's tokens
   int tok0, tok1;  // context positions
-  int drafts;      // 1: then the drafted tokens
+  int drafts;      // the beam's drafted tokens, which follow; 0: none
   int rec;         // a segment's: which of its pieces; a beam's own: the record, -1: the output itself
 };
 
 // Byte offsets of the workspace.
 struct DraftLayout {
-  size_t units, anc, cnt, nrec, rec_base, rec_off, seg_cnt, seg_list, off, list, acc, ml, rec, total;
+  size_t units, anc, cnt, nrec, rec_base, rec_off, depth, seg_cnt, seg_list, off, list, acc, ml, rec, total;
   int rec_cap, max_units;
 };
 
@@ -63,6 +64,7 @@ DraftLayout draft_layout(const gb_pool_config& c, int num_sms, int T) {
   d.nrec = take(B * sizeof(int));
   d.rec_base = take(B * sizeof(int));
   d.rec_off = take(B * kRecOffs * sizeof(int));
+  d.depth = take(B * sizeof(int));
   d.seg_cnt = take(B * kMaxSegDepth * sizeof(int));
   d.seg_list = take(B * kMaxSegDepth * sizeof(int));
   d.off = take(B * kMaxSegDepth * sizeof(int));
@@ -86,6 +88,7 @@ struct DraftView {
   int* nrec;                // [max_beams] records
   int* rec_base;            // [max_beams] the first of them
   int* rec_off;             // [max_beams][kRecOffs] those of the k-th segment, and of the beam's own units
+  int* depth;               // [max_beams] segments used
   int* seg_cnt;             // [segments] drafted tokens of its beams
   int* seg_list;            // [segments] where its token list begins
   int* off;                 // [max_beams][kMaxSegDepth] the beam's place in that list
@@ -113,6 +116,7 @@ DraftView draft_view(const gb_pool* p, const DraftLayout& d, int T, void* ws) {
   v.nrec = reinterpret_cast<int*>(m + d.nrec);
   v.rec_base = reinterpret_cast<int*>(m + d.rec_base);
   v.rec_off = reinterpret_cast<int*>(m + d.rec_off);
+  v.depth = reinterpret_cast<int*>(m + d.depth);
   v.seg_cnt = reinterpret_cast<int*>(m + d.seg_cnt);
   v.seg_list = reinterpret_cast<int*>(m + d.seg_list);
   v.off = reinterpret_cast<int*>(m + d.off);
@@ -181,28 +185,27 @@ __device__ __forceinline__ int drafted(const int* count, int b, int T, bool act,
   return n;
 }
 
-// CTA 0 makes the work list, the others the ancestor masks, a warp per slot.  `tokens`: of a unit's rows;
-// `least`: tiles below which a run of keys is not split.
-__global__ void __launch_bounds__(kListThreads) k_draft_plan(PoolView v, DraftView w, const int* parent,
-                                                             const int* count, int tokens, int least, bool segs) {
+// What the plan counts a unit as, in eighths of the time of a 128-key tile of up to 128 rows: a tile of more rows is
+// twice that, a unit's start and end (queries, pipeline, result) kUnitCost more per 128 rows, and a record that has to be written
+// and joined kRecCost per 128 rows.
+constexpr int kTileCost = 8, kUnitCost = 10, kRecCost = 14;
+
+// The work list (one CTA).  `tokens`: of a unit's rows; `least`: tiles below which a run of keys is not split.
+//
+// Down to which depth the shared segments are used is chosen by the cost above: a segment's unit reads
+// its pages once for up to 256 rows, but every piece of a beam's context beyond the first costs a record.  64 beams of 50 rows
+// over 64 shared and 130 own tokens run without segments; 64 beams of 50 rows at 4000 tokens use them all.
+__global__ void __launch_bounds__(kListThreads) k_draft_plan(PoolView v, DraftView w, const int* count, int tokens, int least,
+                                                             bool segs) {
   pdl_wait();
   pdl_launch_dependents();
-  const int tid = threadIdx.x;
-  if (blockIdx.x > 0) {
-    const int b = (blockIdx.x - 1) * 32 + (tid >> 5), lane = tid & 31;
-    if (b >= v.max_beams) return;
-    bool bad = false;
-    const int n = drafted(count, b, w.T, v.active[b] != 0, &bad);
-    unsigned long long lo, hi;
-    bool wrong;
-    ancestors(parent + (size_t)b * w.T, w.T, n, &lo, &hi, &wrong);
-    if (lane < w.T) w.anc[(size_t)b * w.T + lane] = lo;
-    if (lane + 32 < w.T) w.anc[(size_t)b * w.T + lane + 32] = hi;
-    if ((bad || wrong) && lane == 0) set_status(v.ctl, GB_ERR_INVALID);
-    return;
-  }
+  constexpr int kCached = 4096;         // segments whose rows and tiles fit in shared memory
   __shared__ ListSmem sm;
   __shared__ short s_cnt[kMaxBeams];
+  __shared__ unsigned s_src[kCached];   // rows | tiles << 16, each clamped (a source with more is read from memory)
+  __shared__ int s_cost[kMaxSegDepth + 1];
+  __shared__ int s_start[kMaxBeams], s_len[kMaxBeams];
+  const int tid = threadIdx.x;
   const int b = tid, cap = v.max_beams;
   const bool act = b < cap && v.active[b] != 0;
   const int L = act ? v.seq_len[b] : 0;
@@ -212,39 +215,76 @@ __global__ void __launch_bounds__(kListThreads) k_draft_plan(PoolView v, DraftVi
   int nd = segs && cnt > 0 ? v.seg_nseg[b] : 0;
   s_cnt[b] = (short)cnt;
   if (b < cap) w.cnt[b] = cnt;
-  if (tid == 0) {
-    w.ctl[kDrList] = 0;
-    w.ctl[kDrNext] = 0;
-  }
+  if (tid == 0) w.ctl[kDrList] = 0;
+  if (tid <= kMaxSegDepth) s_cost[tid] = 0;
   for (int s = tid; s < nseg; s += kListThreads) w.seg_cnt[s] = 0;
-  // The depth down to which segments are used: a record each, and one for the rest, must fit.
-  int dmax = kMaxSegDepth, all;
-  for (; dmax > 0; --dmax) {
-    block_exclusive_scan(cnt > 0 ? min(nd, dmax) + 1 : 0, sm.tmp, &all);
-    if (all <= w.rec_cap) break;
-  }
-  nd = min(nd, dmax);
   __syncthreads();
   // Segments: their drafted tokens, and each beam's place among them.
   for (int e = tid; e < (segs ? cap * kMaxSegDepth : 0); e += kListThreads) {
     const int c = s_cnt[e / kMaxSegDepth], k = e % kMaxSegDepth;
-    if (c > 0 && k < min(v.seg_nseg[e / kMaxSegDepth], dmax)) w.off[e] = atomicAdd(&w.seg_cnt[v.seg_bid[e]], c);
+    if (c > 0 && k < v.seg_nseg[e / kMaxSegDepth]) w.off[e] = atomicAdd(&w.seg_cnt[v.seg_bid[e]], c);
   }
-  int start = 0;
-  for (int k = 0; k < nd; ++k) start += v.seg_len[v.seg_bid[b * kMaxSegDepth + k]] * v.P;
-  const int tail = cnt > 0 ? tail_tiles(L - start) : 0, btiles = (cnt + tokens - 1) / tokens;
+  auto seg_tiles = [&](int s) { return (v.seg_len[s] * v.P + flash::kTok - 1) / flash::kTok; };
+  auto unit_cost = [&](int rows, int tiles, int rec) {  // of `rows` tokens over `tiles` tiles
+    const int full = rows / tokens, rest = rows - full * tokens, halves = 2 * full + (rest > 0) + (2 * rest > tokens);
+    return halves * (tiles * kTileCost + kUnitCost + rec);
+  };
+  // Cost of the beams' own units by depth, for the beams that reach it; then the segments'.
+  {
+    int at = 0;
+    if (cnt > 0) {
+      atomicAdd(&s_cost[0], unit_cost(cnt, tail_tiles(L), 0));
+      for (int k = 0; k < nd; ++k) {
+        // What using the k-th segment too changes: a shorter rest, and for the first one a record.
+        const int from = tail_tiles(L - at), rec = k == 0 ? kRecCost : 0;
+        at += v.seg_len[v.seg_bid[b * kMaxSegDepth + k]] * v.P;
+        atomicAdd(&s_cost[k + 1], unit_cost(cnt, tail_tiles(L - at), rec) - unit_cost(cnt, from, 0));
+      }
+    }
+  }
   __threadfence_block();
   __syncthreads();
-  auto seg_tiles = [&](int s) { return (v.seg_len[s] * v.P + flash::kTok - 1) / flash::kTok; };
-  int work = tail * btiles;
   for (int s = tid; s < nseg; s += kListThreads) {
     const int c = w.seg_cnt[s];
-    work += (c + tokens - 1) / tokens * seg_tiles(s);
+    if (c > 0) atomicAdd(&s_cost[v.seg_members[v.seg_mem_off[s]] % kMaxSegDepth + 1], unit_cost(c, seg_tiles(s), kRecCost));
+  }
+  int dmax = 0, all;
+  __syncthreads();
+  {
+    int cost = s_cost[0], best = cost;
+    for (int d = 1; d <= kMaxSegDepth; ++d) {
+      cost += s_cost[d];
+      if (cost < best) {
+        best = cost;
+        dmax = d;
+      }
+    }
+  }
+  for (; dmax > 0; --dmax) {  // a record each, and one for the rest, must fit
+    block_exclusive_scan(cnt > 0 ? min(nd, dmax) + 1 : 0, sm.tmp, &all);
+    if (all <= w.rec_cap) break;
+  }
+  nd = min(nd, dmax);
+  int start = 0;
+  for (int k = 0; k < nd; ++k) start += v.seg_len[v.seg_bid[b * kMaxSegDepth + k]] * v.P;
+  const int tail = cnt > 0 ? tail_tiles(L - start) : 0;
+  auto seg_rows = [&](int s) { return v.seg_members[v.seg_mem_off[s]] % kMaxSegDepth < dmax ? w.seg_cnt[s] : 0; };
+  int work = tail * ((cnt + tokens - 1) / tokens);
+  for (int s = tid; s < nseg; s += kListThreads) {
+    const int c = seg_rows(s), t = seg_tiles(s);
+    if (s < kCached) s_src[s] = (unsigned)min(c, 65535) | (unsigned)min(t, 65535) << 16;
+    work += (c + tokens - 1) / tokens * t;
     if (c > 0) w.seg_list[s] = atomicAdd(&w.ctl[kDrList], c);
   }
   block_exclusive_scan(work, sm.tmp, &all);
-  // Tiles per unit: some units per SM, but not too short ones, and no more records than there is room for.
-  int per = max(least, (int)(((long long)all * v.Hkv + 2 * v.num_sms - 1) / (2 * v.num_sms)));
+  // Tiles per unit.  Few sources: one unit per SM, of equal length (two shorter ones leave SMs idle in the second
+  // wave: a 20000-token beam of 8 KV heads in 256 units of 5 tiles took as long as 144 of 9 would in two waves).  More: half an
+  // SM's share at most, which the sorted list evens out.  Not too short ones, and no more records than there is room for.
+  const long long heads_work = (long long)all * v.Hkv;
+  int whole;
+  block_exclusive_scan((cnt > 0 ? (cnt + tokens - 1) / tokens : 0), sm.tmp, &whole);
+  const int waves = whole * v.Hkv < v.num_sms ? 1 : 2;
+  int per = max(least, (int)((heads_work + waves * v.num_sms - 1) / (waves * v.num_sms)));
   int mine, base;
   for (;; per *= 2) {
     mine = cnt > 0 ? (tail + per - 1) / per : 0;
@@ -252,32 +292,35 @@ __global__ void __launch_bounds__(kListThreads) k_draft_plan(PoolView v, DraftVi
     base = block_exclusive_scan(mine, sm.tmp, &all);
     if (all <= w.rec_cap || per > (1 << 24)) break;
   }
+  int tail_rec = 0;
   if (b < cap) {
     w.nrec[b] = mine;
     w.rec_base[b] = base;
-    int at = 0;
     for (int k = 0; k < nd; ++k) {
-      w.rec_off[b * kRecOffs + k] = at;
-      at += (seg_tiles(v.seg_bid[b * kMaxSegDepth + k]) + per - 1) / per;
+      w.rec_off[b * kRecOffs + k] = tail_rec;
+      tail_rec += (seg_tiles(v.seg_bid[b * kMaxSegDepth + k]) + per - 1) / per;
     }
-    w.rec_off[b * kRecOffs + kTailRec] = at;
+    w.rec_off[b * kRecOffs + kTailRec] = tail_rec;
+    w.depth[b] = nd;
   }
   // The beams' own sizes, for the list's other threads.
-  __shared__ int s_start[kMaxBeams], s_len[kMaxBeams];
+  __shared__ int s_rec[kMaxBeams];
   s_start[b] = start;
   s_len[b] = L;
+  s_rec[b] = mine > 1 ? base + tail_rec : -1;
   __syncthreads();
   struct Piece {
     int tiles, splits, share, row_tiles, rows;
   };
   auto piece = [&](int src) {  // sources: the segments, then the slots
     Piece p;
-    if (src < nseg) {
-      p.rows = w.seg_cnt[src];
-      p.tiles = p.rows > 0 ? seg_tiles(src) : 0;
-    } else {
+    if (src >= nseg) {
       p.rows = s_cnt[src - nseg];
       p.tiles = p.rows > 0 ? tail_tiles(s_len[src - nseg] - s_start[src - nseg]) : 0;
+    } else {
+      const unsigned x = src < kCached ? s_src[src] : ~0u;
+      p.rows = (x & 0xffff) == 0xffff ? seg_rows(src) : x & 0xffff;
+      p.tiles = p.rows == 0 ? 0 : x >> 16 == 0xffff ? seg_tiles(src) : x >> 16;
     }
     p.splits = (p.tiles + per - 1) / per;
     p.share = p.splits > 0 ? (p.tiles + p.splits - 1) / p.splits : 1;
@@ -319,19 +362,37 @@ __global__ void __launch_bounds__(kListThreads) k_draft_plan(PoolView v, DraftVi
           u.e0 = t * tokens;
           u.tok0 = min(s_start[beam] + sp * p.share * flash::kTok, n);
           u.tok1 = min(s_start[beam] + (sp + 1) * p.share * flash::kTok, n);
-          u.drafts = sp == p.splits - 1;
-          u.rec = w.nrec[beam] > 1 ? w.rec_base[beam] + w.rec_off[beam * kRecOffs + kTailRec] + sp : -1;
+          u.drafts = sp == p.splits - 1 ? s_cnt[beam] : 0;
+          u.rec = s_rec[beam] < 0 ? -1 : s_rec[beam] + sp;
         }
         w.units[at] = u;
       });
   if (tid == 0) w.ctl[kDrUnits] = min(n, w.max_units);
-  // Token lists of the segments.
-  for (int e = tid >> 5; e < (segs ? cap * kMaxSegDepth : 0); e += kListThreads / 32) {
-    const int c = s_cnt[e / kMaxSegDepth], k = e % kMaxSegDepth;
-    if (c == 0 || k >= min(v.seg_nseg[e / kMaxSegDepth], dmax)) continue;
-    int2* to = w.list + w.seg_list[v.seg_bid[e]] + w.off[e];
-    const int beam = e / kMaxSegDepth, rec = w.rec_base[beam] + w.rec_off[beam * kRecOffs + k];
-    for (int i = tid & 31; i < c; i += 32) to[i] = make_int2(beam | i << 10, rec);
+}
+
+// A warp per slot: the ancestor masks of its tokens, and their entries in the lists of the slot's segments.
+__global__ void __launch_bounds__(256) k_draft_rows(PoolView v, DraftView w, const int* parent, const int* count) {
+  pdl_wait();
+  pdl_launch_dependents();
+  const int b = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (b >= v.max_beams) return;
+  bool bad = false;
+  const int n = drafted(count, b, w.T, v.active[b] != 0, &bad), nd = w.depth[b], base = w.rec_base[b];
+  int at = 0, rec = 0;
+  if (lane < nd && n > 0) {  // lane k: the slot's k-th segment
+    at = w.seg_list[v.seg_bid[b * kMaxSegDepth + lane]] + w.off[b * kMaxSegDepth + lane];
+    rec = base + w.rec_off[b * kRecOffs + lane];
+  }
+  unsigned long long lo, hi;
+  bool wrong;
+  ancestors(parent + (size_t)b * w.T, w.T, n, &lo, &hi, &wrong);
+  if (lane < w.T) w.anc[(size_t)b * w.T + lane] = lo;
+  if (lane + 32 < w.T) w.anc[(size_t)b * w.T + lane + 32] = hi;
+  if ((bad || wrong) && lane == 0) set_status(v.ctl, GB_ERR_INVALID);
+  for (int k = 0; k < nd; ++k) {
+    int2* to = w.list + __shfl_sync(0xffffffffu, at, k);
+    const int r = __shfl_sync(0xffffffffu, rec, k);
+    for (int i = lane; i < n; i += 32) to[i] = make_int2(b | i << 10, r);
   }
 }
 
@@ -352,11 +413,12 @@ struct DraftJob {
   PoolView v;
   DraftView w;
   int layer, oob;
+  int page_shift, group0;   // log2 of the page size; the layer's first row group in the tensor map
   float qscale;
   const __nv_bfloat16 *q, *k, *vv;  // this layer's [max_beams][T][heads][128]
   __nv_bfloat16* o;
 
-  static constexpr bool kEarlyQ = true;
+  static constexpr bool kEarlyQ = true, kBits = true;
   static constexpr int kQArrivals = 4;
   // Tiles land as [16 groups of 8 tokens][half of D][8][64 dims].
   static constexpr int kKHalf = 1024, kKSbo = 2048, kVLbo = 1024, kVSbo = 2048, kVStep = 4096;
@@ -371,9 +433,8 @@ struct DraftJob {
 
   __device__ __forceinline__ void error(int code) const { set_status(v.ctl, code); }
   __device__ __forceinline__ int total() const { return w.ctl[kDrUnits] * v.Hkv; }
-  __device__ __forceinline__ int ticket() const { return atomicAdd(&w.ctl[kDrNext], 1); }
-  // Words of a unit: those of its DraftUnit, in order.
-  enum { kSeg, kBeam, kE0, kNtok, kTok0, kTok1, kDrafts, kRec, kCount };
+  // Words of a unit, those of its loads first.
+  enum { kBeam, kTok0, kTok1, kDrafts, kSeg, kE0, kNtok, kRec };
   __device__ __forceinline__ void unit(int id, flash::Unit& x) const {
     const DraftUnit e = w.units[id / v.Hkv];
     const int n = e.tok1 - e.tok0;
@@ -388,15 +449,14 @@ struct DraftJob {
     x.w[kTok1] = e.tok1;
     x.w[kDrafts] = e.drafts;
     x.w[kRec] = e.rec;
-    x.w[kCount] = e.seg < 0 ? w.cnt[e.beam] : 0;
   }
   __device__ __forceinline__ bool draft_tile(const flash::Unit& x, int j) const { return x.w[kDrafts] && j == x.nt - 1; }
   // Rows of the context's last page past its end hold whatever the pool's memory did.
   __device__ __forceinline__ void stale_rows(const flash::Unit& x, int j, int& z0, int& z1) const {
     const int n = x.w[kTok1] - x.w[kTok0] - j * flash::kTok;
-    if (n > 0 && n < flash::kTok && n % v.P) {
+    if (n > 0 && n < flash::kTok && (n & (v.P - 1))) {
       z0 = n;
-      z1 = (n + v.P - 1) / v.P * v.P;
+      z1 = (n + v.P - 1) & ~(v.P - 1);
     }
   }
   static __device__ __forceinline__ void tma5(uint32_t dst, const CUtensorMap* tm, int c1, int c2, int c3, int c4,
@@ -407,29 +467,25 @@ struct DraftJob {
         "l"(tm), "r"(0), "r"(c1), "r"(c2), "r"(c3), "r"(c4), "r"(bar)
         : "memory");
   }
-  // The lane's page of tile j, -1: none.
+  // The lane's page of tile j: its first row group in the pool's tensor map, or one past it (zeros).
   __device__ __forceinline__ int page(const flash::Unit& x, int j, int lane) const {
-    const int pos = x.w[kTok0] + j * flash::kTok + lane * v.P;
-    if (lane * v.P >= flash::kTok || pos >= x.w[kTok1]) return -1;
-    return v.tables[(size_t)x.w[kBeam] * v.max_pages + pos / v.P];
+    const int pos = x.w[kTok0] + j * flash::kTok + (lane << page_shift);
+    if ((lane << page_shift) >= flash::kTok || pos >= x.w[kTok1]) return oob;
+    int p = v.tables[(size_t)x.w[kBeam] * v.max_pages + (pos >> page_shift)];
+    if (p < 0 || p >= v.num_pages) {
+      set_status(v.ctl, GB_ERR_INVALID);
+      p = 0;
+    }
+    return group0 + x.head * (v.P / 8) + p * (2 * v.Hkv * v.P / 8);
   }
+  // A page to a lane: the copies' issue overlaps.
   __device__ __forceinline__ void load_tile(const flash::Unit& x, int j, int kv, int page, uint32_t dst, uint32_t bar,
                                             int lane) const {
     const bool last = draft_tile(x, j);
-    if (lane * v.P < (last ? 64 : flash::kTok)) {
-      int row = oob;
-      if (x.w[kTok0] + j * flash::kTok + lane * v.P < x.w[kTok1]) {
-        if (page < 0 || page >= v.num_pages) {
-          set_status(v.ctl, GB_ERR_INVALID);
-          page = 0;
-        }
-        row = (int)((((long long)layer * v.num_pages + page) * 2 * v.Hkv + x.head) * v.P / 8);
-      }
-      tma5(dst + lane * v.P * 256, &tp, 0, 0, kv, row, bar);
-    }
+    if ((lane << page_shift) < (last ? 64 : flash::kTok)) tma5(dst + (lane << (page_shift + 8)), &tp, 0, 0, kv, page, bar);
     if (last && lane >= 16 && lane < 24) {
       const int t = (lane - 16) * 8;
-      tma5(dst + (lane - 8) * 2048, kv ? &tv : &tk, t < x.w[kCount] ? t : kMaxDraft, 0, x.head, x.w[kBeam], bar);
+      tma5(dst + (lane - 8) * 2048, kv ? &tv : &tk, t < x.w[kDrafts] ? t : kMaxDraft, 0, x.head, x.w[kBeam], bar);
     }
   }
   __device__ __forceinline__ void find_row(const flash::Unit& x, int g, int r, Row& row) const {
@@ -464,42 +520,38 @@ struct DraftJob {
     return {!last && n >= flash::kTok, n, last ? row.anc : 0ull};
   }
   __device__ __forceinline__ void out(const flash::Unit& x, const Row& row, uint32_t a, uint32_t b, bool two, float wa,
-                                      float wb, int c0, int cols, float m, float l) const {
+                                      float wb, float m, float l) const {
     const bool final = row.rec < 0;
     const float inv = final ? 1.f / l : 1.f;
     const int head = x.head * v.G + row.gg;
-    __nv_bfloat16* dst = o + (((size_t)row.beam * w.T + row.tok) * v.Hq + head) * flash::kD + c0;
+    __nv_bfloat16* dst = o + (((size_t)row.beam * w.T + row.tok) * v.Hq + head) * flash::kD;
     const size_t rr = ((size_t)max(row.rec, 0) * v.Hkv + x.head) * w.rows + row.tok * v.G + row.gg;
-    float* rec = w.rec + rr * flash::kD + c0;
+    float* rec = w.rec + rr * flash::kD;
     bool fine = true;
 #pragma unroll 1
-    for (int c = 0; c < cols; c += 32) {
-      float f[32];
+    for (int c = 0; c < flash::kD; c += 16) {
+      float f[16];
       flash::read_o(a + c, b + c, two, wa, wb, f);
 #pragma unroll
-      for (int i = 0; i < 32; ++i) {
+      for (int i = 0; i < 16; ++i) {
         f[i] *= inv;
         fine = fine && isfinite(f[i]);
       }
       if (!row.valid) continue;
       if (final) {
+        uint32_t u[8];
 #pragma unroll
-        for (int i = 0; i < 32; i += 8) {
-          uint32_t u[4];
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const __nv_bfloat162 p = __floats2bfloat162_rn(f[i + 2 * k], f[i + 2 * k + 1]);
-            u[k] = *reinterpret_cast<const uint32_t*>(&p);
-          }
-          *reinterpret_cast<uint4*>(dst + c + i) = make_uint4(u[0], u[1], u[2], u[3]);
+        for (int k = 0; k < 8; ++k) {
+          const __nv_bfloat162 p = __floats2bfloat162_rn(f[2 * k], f[2 * k + 1]);
+          u[k] = *reinterpret_cast<const uint32_t*>(&p);
         }
+        flash::st32(dst + c, u);
       } else {
-#pragma unroll
-        for (int i = 0; i < 32; i += 4)
-          *reinterpret_cast<float4*>(rec + c + i) = make_float4(f[i], f[i + 1], f[i + 2], f[i + 3]);
+        flash::st32(rec + c, reinterpret_cast<const uint32_t*>(f));
+        flash::st32(rec + c + 8, reinterpret_cast<const uint32_t*>(f + 8));
       }
     }
-    if (row.valid && !final && c0 == 0) w.ml[rr] = make_float2(m, l);
+    if (row.valid && !final) w.ml[rr] = make_float2(m, l);
     unsigned redo = __ballot_sync(0xffffffffu, row.valid && x.w[kDrafts] && !fine && isfinite(m) && isfinite(l));
     while (redo) {  // see sum_seen; only drafted tokens off the row's path share a tile with what it sees
       const int src = __ffs(redo) - 1;
@@ -512,8 +564,8 @@ struct DraftJob {
       const size_t kv0 = ((size_t)x.w[kBeam] * w.T * v.Hkv + x.head) * flash::kD;
       const int nctx = x.w[kTok1] - x.w[kTok0];
       bool unseen = false;
-      for (int j = 0; j < min(w.T, (x.w[kCount] + 7) & ~7) && !unseen; ++j)
-        if (!((anc >> j) & 1)) unseen = flash::not_finite(vv + kv0 + (size_t)j * v.Hkv * flash::kD, c0, cols);
+      for (int j = 0; j < min(w.T, (x.w[kDrafts] + 7) & ~7) && !unseen; ++j)
+        if (!((anc >> j) & 1)) unseen = flash::not_finite(vv + kv0 + (size_t)j * v.Hkv * flash::kD);
       if (!unseen) continue;
       const size_t qo = (((size_t)x.w[kBeam] * w.T + tok) * v.Hq + x.head * v.G + gg) * flash::kD;
       float acc[4];
@@ -532,10 +584,9 @@ struct DraftJob {
             vj = pool + kv_elem_offset(v, layer, page, 1, x.head, pos % v.P);
             return true;
           },
-          qscale, mr, c0, cols, acc);
-      const int lane = threadIdx.x & 31, per = cols / 32;
-      for (int i = 0; i < per; ++i) {
-        const int c = c0 + per * lane + i;
+          qscale, mr, acc);
+      for (int i = 0; i < 4; ++i) {
+        const int c = 4 * (threadIdx.x & 31) + i;
         if (fin) o[qo + c] = __float2bfloat16(acc[i] * ir);
         else w.rec[at * flash::kD + c] = acc[i];
       }
@@ -602,53 +653,69 @@ __global__ void __launch_bounds__(kTileThreads) k_draft_f32(PoolView v, DraftVie
     const DraftUnit u = w.units[id / v.Hkv];
     const int nctx = u.tok1 - u.tok0;
     const DraftTile src{v, w, u, layer, id % v.Hkv, nctx, q, k, vv, o};
-    tile_attention(sm, src, nctx + (u.drafts ? w.cnt[u.beam] : 0), qscale);
+    tile_attention(sm, src, nctx + u.drafts, qscale);
     __syncthreads();
   }
 }
 
-// A warp per (slot, token, query head): joins the row's records, sum 2^(m_k - m) (o_k, l_k), or
-// writes the zeros of a row that holds no token.
+// A CTA per (slot, token), or one for every 8 of its query heads where those are few, a warp per row: joins the row's records, sum 2^(m_k - m) (o_k, l_k), or
+// writes the zeros of a row that holds no token; a row that has its result already is left.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) k_draft_merge(PoolView v, DraftView w, T* o) {
   pdl_wait();
   pdl_launch_dependents();
-  if (blockIdx.x == 0 && threadIdx.x == 0) w.ctl[kDrNext] = 0;  // for the next layer
   constexpr int per = D / 32;
-  const int lane = threadIdx.x & 31;
-  const long long rows = (long long)v.max_beams * w.T * v.Hq, step = (long long)gridDim.x * 8;
-  for (long long r = blockIdx.x * 8ll + (threadIdx.x >> 5); r < rows; r += step) {
-    const int hq = (int)(r % v.Hq), i = (int)(r / v.Hq % w.T), b = (int)(r / v.Hq / w.T);
+  using Vec = typename std::conditional<per == 4, float4, float2>::type;
+  const int lane = threadIdx.x & 31, i = blockIdx.x, b = blockIdx.y;
+  const int n = i < w.cnt[b] ? w.nrec[b] : 0;
+  if (n == 1) return;
+  const size_t step = (size_t)v.Hkv * w.rows;
+  const size_t r1 = n > 0 ? (size_t)w.rec_base[b] * step + i * v.G : 0;
+  for (int hq = blockIdx.z * 8 + (threadIdx.x >> 5); hq < v.Hq; hq += 8 * gridDim.z) {
     float acc[per] = {};
-    if (i < w.cnt[b]) {
-      const int n = w.nrec[b];
-      if (n <= 1) continue;
-      const size_t step_r = (size_t)v.Hkv * w.rows;
-      const size_t r0 = ((size_t)w.rec_base[b] * v.Hkv + hq / v.G) * w.rows + i * v.G + hq % v.G;
+    if (n > 0) {
+      const size_t r0 = r1 + (size_t)(hq / v.G) * w.rows + hq % v.G;
       float m = -INFINITY;
-      for (int k = lane; k < n; k += 32) m = fmaxf(m, w.ml[r0 + k * step_r].x);
+      for (int k = lane; k < n; k += 32) m = fmaxf(m, w.ml[r0 + k * step].x);
 #pragma unroll
       for (int s = 16; s > 0; s >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, s));
       const float ref = m == -INFINITY ? 0.f : m;
       float l = 0.f;
-#pragma unroll 4
-      for (int k = 0; k < n; ++k) {
-        const float2 ml = w.ml[r0 + k * step_r];
+      for (int k0 = 0; k0 < n; k0 += 32) {
+        // Lane k has the weight of record k0 + k, so that the records' loads wait for nothing but their addresses.
+        float2 ml = make_float2(-INFINITY, 0.f);
+        if (k0 + lane < n) ml = w.ml[r0 + (k0 + lane) * step];
         const float f = exp2f(ml.x - ref);
         l = fmaf(ml.y, f, l);
-        const float* x = w.rec + (r0 + k * step_r) * D + lane * per;
+        const int m32 = min(32, n - k0);
+        const Vec* x = reinterpret_cast<const Vec*>(w.rec + (r0 + k0 * step) * D) + lane;
+        for (int k = 0; k < m32; k += 8) {
+          Vec y[8];
 #pragma unroll
-        for (int c = 0; c < per; ++c) acc[c] = fmaf(x[c], f, acc[c]);
+          for (int e = 0; e < 8; ++e)
+            if (k + e < m32) y[e] = x[(size_t)(k + e) * step * 32];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float g = __shfl_sync(0xffffffffu, f, (k + e) & 31);
+            if (k + e < m32)
+#pragma unroll
+              for (int c = 0; c < per; ++c) acc[c] = fmaf(reinterpret_cast<const float*>(&y[e])[c], g, acc[c]);
+          }
+        }
       }
+#pragma unroll
+      for (int s = 16; s > 0; s >>= 1) l += __shfl_xor_sync(0xffffffffu, l, s);
       const float inv = 1.f / l;
 #pragma unroll
       for (int c = 0; c < per; ++c) acc[c] *= inv;
     }
-    T* dst = o + r * D + lane * per;
+    T* dst = o + (((size_t)b * w.T + i) * v.Hq + hq) * D + lane * per;
+    if constexpr (sizeof(T) == 2) {
 #pragma unroll
-    for (int c = 0; c < per; ++c) {
-      if constexpr (sizeof(T) == 2) dst[c] = __float2bfloat16(acc[c]);
-      else dst[c] = acc[c];
+      for (int c = 0; c < per; c += 2)
+        *reinterpret_cast<__nv_bfloat162*>(dst + c) = __floats2bfloat162_rn(acc[c], acc[c + 1]);
+    } else {
+      *reinterpret_cast<Vec*>(dst) = *reinterpret_cast<const Vec*>(acc);
     }
   }
 }
@@ -855,6 +922,7 @@ __global__ void __launch_bounds__(1024) k_truncate(PoolView v, const int* length
     if (tid == 0) {
       set_status(v.ctl, GB_ERR_OOM);
       v.ctl[kCtlCowJobs] = 0;
+      v.ctl[kCtlSegStale] = 0;
     }
     return;
   }
@@ -865,6 +933,8 @@ __global__ void __launch_bounds__(1024) k_truncate(PoolView v, const int* length
   } else {
     s_long[atomicAdd(&s_nlong, 1)] = b;
   }
+  // Only pages of shared segments matter to them: those past a slot's cover are its own.
+  const bool stale = __syncthreads_or(cut && v.grouped && want / v.P < v.seg_cover[b]);
   if (cut) {
     v.seq_len[b] = want;
     v.gen[b] = max(0, v.gen[b] - (L - want));
@@ -920,6 +990,7 @@ __global__ void __launch_bounds__(1024) k_truncate(PoolView v, const int* length
   }
   if (tid == 0) {
     v.ctl[kCtlCowJobs] = total;
+    v.ctl[kCtlSegStale] = stale;
     if (total > 0) atomicSub(&v.ctl[kCtlFree], total);
   }
 }
@@ -980,7 +1051,7 @@ extern "C" gb_status gb_draft_attention(gb_pool* pool, int layer, const gb_draft
   gb_status st = check_draft(pool, d, "draft: bad arguments");
   if (st != GB_OK) return st;
   if (layer < 0 || layer >= pool->cfg.num_layers || !q_dev || !k_dev || !v_dev || !out_dev || !(scale > 0.f) ||
-      scale > 3e38f || (((uintptr_t)q_dev | (uintptr_t)k_dev | (uintptr_t)v_dev | (uintptr_t)out_dev) & 15))
+      scale > 3e38f || (((uintptr_t)q_dev | (uintptr_t)k_dev | (uintptr_t)v_dev) & 15) || ((uintptr_t)out_dev & 31))
     return fail(pool, GB_ERR_INVALID, "draft: bad arguments");
   const PoolView& v = pool->view;
   const int T = d->n_draft;
@@ -1002,6 +1073,8 @@ extern "C" gb_status gb_draft_attention(gb_pool* pool, int layer, const gb_draft
     job.w = w;
     job.layer = layer;
     job.oob = pool->tmap_oob;
+    job.page_shift = v.P == 16 ? 4 : v.P == 32 ? 5 : 6;
+    job.group0 = (int)((long long)layer * v.num_pages * 2 * v.Hkv * v.P / 8);
     job.qscale = qscale;
     job.q = static_cast<const __nv_bfloat16*>(q_dev);
     job.k = static_cast<const __nv_bfloat16*>(k_dev);
@@ -1017,17 +1090,16 @@ extern "C" gb_status gb_draft_attention(gb_pool* pool, int layer, const gb_draft
   }
   if (layer == 0) {
     const int tokens = (bf16 ? 2 * flash::kRows : kTileRows) / v.G;
-    launch_pdl(k_draft_plan, 1 + (v.max_beams + 31) / 32, kListThreads, 0, s, v, w, d->parent_dev, d->count_dev, tokens,
-               2, bf16 && v.grouped);
-    pool->launches += 1;
+    launch_pdl(k_draft_plan, 1, kListThreads, 0, s, v, w, d->count_dev, tokens, 2, bf16 && v.grouped);
+    launch_pdl(k_draft_rows, (v.max_beams + 7) / 8, 256, 0, s, v, w, d->parent_dev, d->count_dev);
+    pool->launches += 2;
     if ((st = check_launch(pool, "draft_plan")) != GB_OK) return st;
     pool->draft_epoch = pool->epoch;
     pool->draft_ws = d->workspace_dev;
     pool->draft_tokens = T;
   }
   cudaError_t e;
-  const long long rows = (long long)v.max_beams * T * v.Hq;
-  const unsigned merge = (unsigned)std::min<long long>((rows + 7) / 8, pool->num_sms * 16);
+  const dim3 merge(T, v.max_beams, (long long)T * v.max_beams < 2 * pool->num_sms ? (v.Hq + 7) / 8 : 1);
   if (bf16) {
     e = set_max_dynamic_smem(reinterpret_cast<const void*>(k_draft), flash::kSmem);
     if (e == cudaSuccess) e = launch_pdl(k_draft, pool->num_sms, flash::kThreads, flash::kSmem, s, job);
@@ -1080,6 +1152,6 @@ extern "C" gb_status gb_truncate(gb_pool* pool, const int32_t* lengths_dev, gb_s
   pool->launches += 2;
   const gb_status st = check_launch(pool, "truncate");
   if (st != GB_OK) return st;
-  if (rebuild_segments(pool, s) != cudaSuccess) return check_launch(pool, "segments");
+  if (rebuild_segments(pool, s, pool->view.ctl + kCtlSegStale) != cudaSuccess) return check_launch(pool, "segments");
   return GB_OK;
 }

@@ -18,13 +18,16 @@
 // P is rounded to bf16 for the tensor core (relative 2^-9 each, independent, so a result's error
 // is about that of its own rounding to bf16); the sum l is of the unrounded values.
 //
-// Warp roles (384 threads):
-//   warps 0-7   softmax: thread r of group g owns row r of its tile (tensor-memory lane r); also loads
-//               the row's query and writes its result
-//   warp 8      streams K and V tiles through a ring of five 32 KiB stages (K0 V0 K1 V1 ...)
-//   warps 9-10  issue the products of a group each: S(i), then P.V(i) before S(i + 1), whose tile
-//               P overwrites; a thread's products run in issue order
-//   warp 11     takes units from a grid-wide counter and publishes them in a ring of eight, ahead of the others
+// Warp roles (512 threads):
+//   warps 0-7    softmax: thread r of group g owns row r of its tile (tensor-memory lane r); also loads
+//                the row's query
+//   warp 8       takes the CTA's units from the sorted list, publishes them in a ring of eight and streams K
+//   warp 11      streams V; both go through one ring of five 32 KiB stages (K0 V0 K1 V1 ...)
+//   warps 9-10   issue the products of a group each: S(i), then P.V(i) before S(i + 1), whose tile
+//                P overwrites; a thread's products run in issue order
+//   warps 12-15  write the results: while they read O the softmax groups are in the next unit
+// CTA b takes entries b, 2 n - 1 - b, 2 n + b, ... of the list (n CTAs, longest first), so the shares come out even
+// without a counter that every unit has to wait for.
 // P overwrites the first half of its S tile.  O is rescaled by its own group, and only when a maximum
 // grows by more than 8 (p <= 2^8 meanwhile): when S(i) is complete so is P.V(i - 1), issued before it.
 //
@@ -44,11 +47,11 @@ namespace gb {
 namespace flash {
 
 constexpr int kRows = 128, kTok = 128, kD = 128;
-constexpr int kThreads = 384;          // three warpgroups: the two softmax groups, and the others
-constexpr int kLaunchRegs = 168;       // registers a thread at launch (65536 / 384, in eights); the softmax groups then
-constexpr int kSoftmaxRegs = 216, kOtherRegs = 72;  // hold a tile's row of 128 scores, the others give theirs
-static_assert(256 * kSoftmaxRegs + 128 * kOtherRegs <= kThreads * kLaunchRegs, "the shares come from the launch's total");
-constexpr int kLoadWarp = 8, kMmaWarp = 9, kUnitWarp = 11;
+constexpr int kThreads = 512;          // four warpgroups: the two softmax groups, loads and products, results
+constexpr int kLaunchRegs = 128;       // registers a thread at launch (65536 / 512); the softmax groups then hold a
+constexpr int kSoftmaxRegs = 192, kOtherRegs = 64;  // tile's row of 128 scores, the others give theirs
+static_assert(256 * (kSoftmaxRegs + kOtherRegs) <= kThreads * kLaunchRegs, "the shares come from the launch's total");
+constexpr int kKWarp = 8, kMmaWarp = 9, kVWarp = 11, kOutWarp = 12;
 constexpr int kStages = 5;
 constexpr int kTile = 32768;           // Q, K or V tile: 128 x 128 bf16
 constexpr int kRing = 2 * kTile;       // after the two Q tiles
@@ -59,29 +62,28 @@ static_assert(kSmem <= 232448, "shared memory per block");
 constexpr uint32_t kTmemS = 0, kTmemO = 256;  // column of group 0; group 1 is 128 further
 
 constexpr int kSlots = 8, kUnitWords = 16;  // units known ahead
-// Three "full" barriers a stage, used in turn (ring position mod 15).  A group that has no tile of a unit goes on to the
-// next one and may wait for a position up to 8 past the last one it saw filled.  A wait on a barrier whose phase before
-// last has not ended would pass at once; position p - 15 has been consumed, since p - 10, which is before the one seen, was
-// issued into its stage.
+// Three "full" and three "empty" barriers a stage, used in turn (ring position mod 15).  The warps do not keep step: a
+// group that has no tile of a unit goes on to the next one and may wait for a position up to 8 past the last one it saw
+// filled, and a loading warp may wait for a position whose predecessor in the stage the other one has yet to fill.  A
+// wait on a barrier whose phase before last has not ended would pass at once; for a waiter at position p that is the phase of
+// p - 15 (full) or p - 20 (empty), both consumed: p - 10, which is issued by then, came into a stage that was free.
 constexpr int kFulls = 3 * kStages;
 constexpr int kBarFull = 0;                       // [kFulls]
-constexpr int kBarEmpty = kBarFull + 8 * kFulls;  // [kStages]
-constexpr int kBarQ = kBarEmpty + 8 * kStages;    // [2] the group's query rows are in
+constexpr int kBarEmpty = kBarFull + 8 * kFulls;  // [kFulls]
+constexpr int kBarQ = kBarEmpty + 8 * kFulls;     // [2] the group's query rows are in
 constexpr int kBarS = kBarQ + 16;                 // [2] S of the group's next tile is complete
 constexpr int kBarP = kBarS + 16;                 // [2 groups][2 halves] P of 64 of its keys is written (and O rescaled)
 constexpr int kBarO = kBarP + 32;                 // [2] the unit's last P.V of the group is complete
 constexpr int kBarOFree = kBarO + 16;             // [2] the group's O has been read
-constexpr int kBarX = kBarOFree + 16;             // a joint unit's (m, l) are in
-constexpr int kBarXDone = kBarX + 8;              // and have been read
-constexpr int kBarPatch = kBarXDone + 8;              // a V tile that is mended before it is handed on
-constexpr int kBarTake = kBarPatch + 8;           // the loading warp has begun on a unit: the next may be taken
-constexpr int kBarSched = kBarTake + 8;           // [kSlots]
+constexpr int kBarML = kBarOFree + 16;            // [2] the group's (m, l) are in
+constexpr int kBarPatch = kBarML + 16;            // a V tile that is mended before it is handed on
+constexpr int kBarSched = kBarPatch + 8;          // [kSlots]
 constexpr int kBarSchedFree = kBarSched + 8 * kSlots;
 constexpr int kUnits = (kBarSchedFree + 8 * kSlots + 15) / 16 * 16;  // int [kSlots][kUnitWords]
 constexpr int kWordTmem = kUnits + 4 * kSlots * kUnitWords;
 constexpr int kWordAbort = kWordTmem + 4;
 static_assert(kUnits % 16 == 0 && kWordAbort + 4 <= 1024, "control area");
-constexpr int kSchedReaders = 11;  // eight softmax warps, the two that issue products, the one that loads
+constexpr int kSchedReaders = 15;  // eight softmax warps, two that issue products, one that loads V, four that write
 
 // What every role knows of a unit; w is the job's own.
 struct Unit {
@@ -170,6 +172,13 @@ __device__ __forceinline__ void mma_ts_add(uint32_t d, uint32_t a, uint64_t b, u
   asm volatile("{\n\t.reg .pred p;\n\tsetp.eq.b32 p, 0, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
                "r"(a), "l"(b), "r"(id));
 }
+// 32 bytes of a row.  A thread writes its own row, so a store of a warp meets 32 lines however wide it is: the wider, the
+// fewer.
+__device__ __forceinline__ void st32(void* p, const uint32_t* u) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(u[0]), "r"(u[1]), "r"(u[2]),
+               "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7])
+               : "memory");
+}
 // Whether a kernel of this pipeline has the registers at launch that its warps then share out.
 inline bool launches_with(const void* kernel) {
   static std::mutex mu;
@@ -205,23 +214,37 @@ __device__ __forceinline__ bool elect_one() {
   return p != 0;
 }
 
-// 32 columns of a row's result: O of one group, or of both with their weights.
+__device__ __forceinline__ void ld16_issue(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr));
+}
+__device__ __forceinline__ void ld16_wait(uint32_t* r) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                 "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+               :
+               : "memory");
+}
+// 16 columns of a row's result: O of one group, or of both with their weights.
 __device__ __forceinline__ void read_o(uint32_t a, uint32_t b, bool two, float wa, float wb, float* o) {
-  uint32_t u[32];
-  ld32_issue(a, u);
+  uint32_t u[16];
+  ld16_issue(a, u);
   if (two) {
-    uint32_t v[32];
-    ld32_issue(b, v);
-    ld32_wait(u);
-    ld32_wait(v);
+    uint32_t v[16];
+    ld16_issue(b, v);
+    ld16_wait(u);
+    ld16_wait(v);
     // A weight of 0 belongs to a group that saw no key of the row: what it summed is 0 x V.
 #pragma unroll
-    for (int c = 0; c < 32; ++c)
+    for (int c = 0; c < 16; ++c)
       o[c] = (wa == 0.f ? 0.f : wa * __uint_as_float(u[c])) + (wb == 0.f ? 0.f : wb * __uint_as_float(v[c]));
   } else {
-    ld32_wait(u);
+    ld16_wait(u);
 #pragma unroll
-    for (int c = 0; c < 32; ++c) o[c] = __uint_as_float(u[c]);
+    for (int c = 0; c < 16; ++c) o[c] = __uint_as_float(u[c]);
   }
 }
 
@@ -232,14 +255,13 @@ struct Sees {
   unsigned long long bits;  // columns 64 + i for bit i
 };
 
-// Columns [c0, c0 + cols) of sum_j 2^(qscale q.k_j - m) v_j over the keys that key(j, k, v) says are seen, by a
-// warp: lane l gets columns c0 + l cols / 32 on.  A product with P takes every key of a tile, with p = 0 for those
-// the row does not see, and 0 x inf is NaN: a row whose result is not finite although its maximum is, is summed
-// again here where one of those keys' values is not finite.
+// sum_j 2^(qscale q.k_j - m) v_j over the keys that key(j, k, v) says are seen, by a warp: lane l gets
+// columns 4 l on.  A product with P takes every key of a tile, with p = 0 for those the row does not see, and 0 x inf is
+// NaN: a row whose result is not finite although its maximum is, is summed again here where one of those keys' values is
+// not finite.
 template <class Key>
-__device__ __forceinline__ void sum_seen(const __nv_bfloat16* q, int nkeys, Key key, float qscale, float m, int c0,
-                                         int cols, float* acc) {
-  const int lane = threadIdx.x & 31, per = cols / 32;
+__device__ __forceinline__ void sum_seen(const __nv_bfloat16* q, int nkeys, Key key, float qscale, float m, float* acc) {
+  const int lane = threadIdx.x & 31;
   float qv[4];
   for (int i = 0; i < 4; ++i) {
     qv[i] = __bfloat162float(q[4 * lane + i]);
@@ -252,14 +274,13 @@ __device__ __forceinline__ void sum_seen(const __nv_bfloat16* q, int nkeys, Key 
     for (int i = 0; i < 4; ++i) s = fmaf(qv[i], __bfloat162float(k[4 * lane + i]), s);
     for (int w = 16; w > 0; w >>= 1) s += __shfl_xor_sync(0xffffffffu, s, w);
     const float p = exp2f(fmaf(s, qscale, -m));
-    for (int i = 0; i < per; ++i) acc[i] = fmaf(p, __bfloat162float(v[c0 + per * lane + i]), acc[i]);
+    for (int i = 0; i < 4; ++i) acc[i] = fmaf(p, __bfloat162float(v[4 * lane + i]), acc[i]);
   }
 }
-// Whether v has a value that is not finite in columns [c0, c0 + cols) (a warp's answer).
-__device__ __forceinline__ bool not_finite(const __nv_bfloat16* v, int c0, int cols) {
-  const int lane = threadIdx.x & 31, per = cols / 32;
+// Whether v has a value that is not finite (a warp's answer).
+__device__ __forceinline__ bool not_finite(const __nv_bfloat16* v) {
   bool bad = false;
-  for (int i = 0; i < per; ++i) bad |= !isfinite(__bfloat162float(v[c0 + per * lane + i]));
+  for (int i = 0; i < 4; ++i) bad |= !isfinite(__bfloat162float(v[4 * (threadIdx.x & 31) + i]));
   return __any_sync(0xffffffffu, bad);
 }
 
@@ -275,8 +296,8 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
     return;
   }
   if (tid == 0) {
-    for (int i = 0; i < kFulls; ++i) mbar_init(ctl + kBarFull + 8 * i, 1);
-    for (int i = 0; i < kStages; ++i) {
+    for (int i = 0; i < kFulls; ++i) {
+      mbar_init(ctl + kBarFull + 8 * i, 1);
       mbar_init(ctl + kBarEmpty + 8 * i, 2);
     }
     for (int i = 0; i < 2; ++i) {
@@ -285,12 +306,10 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       mbar_init(ctl + kBarP + 16 * i, 4);
       mbar_init(ctl + kBarP + 16 * i + 8, 4);
       mbar_init(ctl + kBarO + 8 * i, 1);
-      mbar_init(ctl + kBarOFree + 8 * i, 8);
+      mbar_init(ctl + kBarOFree + 8 * i, 4);
+      mbar_init(ctl + kBarML + 8 * i, 4);
     }
-    mbar_init(ctl + kBarX, 8);
-    mbar_init(ctl + kBarXDone, 8);
     mbar_init(ctl + kBarPatch, 1);
-    mbar_init(ctl + kBarTake, 1);
     for (int i = 0; i < kSlots; ++i) {
       mbar_init(ctl + kBarSched + 8 * i, 1);
       mbar_init(ctl + kBarSchedFree + 8 * i, kSchedReaders);
@@ -310,7 +329,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
   pdl_launch_dependents();
 
   // The warpgroups share out the launch's registers; the others give theirs at once, so the groups' waits for them end.
-  if (warp < kLoadWarp) {
+  if (warp < kKWarp) {
     regs_inc<kSoftmaxRegs>();
     // ---------------------------------------------------------------- softmax
     const int g = warp >> 2, r = tid & 127;
@@ -318,9 +337,8 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
     const uint32_t s_addr = tmem + kTmemS + g * 128 + lane_base, o_addr = tmem + kTmemO + lane_base;
     float2* xch = reinterpret_cast<float2*>(sm + kXch);
     const float qscale = job.qscale;
-    uint32_t n = 0, nx = 0;       // tiles of this group, joint units
+    uint32_t n = 0, c_done = 0;   // tiles of this group, units it is done with
     int u_next = 0;               // the unit read next
-    uint32_t taken[2] = {0, 0};   // units so far in which each group had tiles
     bool alive = true;
     typename Job::Row row, row_y;
     // The group's next unit: its words stay in shared memory until the group is done with it.
@@ -328,12 +346,9 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       for (;; ++u_next) {
         slot = u_next & (kSlots - 1);
         if (!wait_or_abort(ctl + kBarSched + 8 * slot, (u_next / kSlots) & 1, abort_flag)) return false;
-        const int nt = units[slot].nt, dual = units[slot].dual;
+        const int nt = units[slot].nt;
         if (nt < 0) return true;
-        const bool in0 = takes_part(nt, dual, u_next, 0), in1 = takes_part(nt, dual, u_next, 1);
-        taken[0] += in0;
-        taken[1] += in1;
-        if (g == 0 ? in0 : in1) {
+        if (takes_part(nt, units[slot].dual, u_next, g)) {
           ++u_next;
           return true;
         }
@@ -360,7 +375,6 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
     while (alive && units[sx].nt >= 0) {
       const Unit& x = units[sx];
       const int nt = x.nt, dual = x.dual, mine = group_tiles(nt, dual, g);
-      const uint32_t c0 = taken[0] - 1, c1 = taken[1] - 1;  // this unit's number among each group's
       float m_ref = -INFINITY, l = 0.f;
       for (int i = 0; i < mine; ++i, ++n) {
         const int t = group_tile(nt, dual, g, i);
@@ -376,9 +390,17 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
         const Sees see = job.sees(x, row, t);
         if (!see.all) {
 #pragma unroll
-          for (int c = 0; c < 128; ++c) {
-            const bool on = c < see.limit || (c >= 64 && ((see.bits >> (c - 64)) & 1));
-            s[c] = on ? s[c] : -INFINITY;
+          for (int c = 0; c < 64; ++c) s[c] = c < see.limit ? s[c] : -INFINITY;
+          if (Job::kBits) {
+            const uint32_t half[2] = {(uint32_t)see.bits, (uint32_t)(see.bits >> 32)};
+#pragma unroll
+            for (int c = 64; c < 128; ++c) {
+              const bool bit = (int32_t)(half[(c - 64) >> 5] << (31 - (c & 31))) < 0;
+              s[c] = bit || c < see.limit ? s[c] : -INFINITY;
+            }
+          } else {
+#pragma unroll
+            for (int c = 64; c < 128; ++c) s[c] = c < see.limit ? s[c] : -INFINITY;
           }
         }
         float mx[4] = {fmaxf(s[0], s[1]), fmaxf(s[2], s[3]), fmaxf(s[4], s[5]), fmaxf(s[6], s[7])};
@@ -432,38 +454,12 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       if (!alive) break;
       if (!Job::kEarlyQ && !(alive = begin_next())) break;
       if (units[sy].nt >= 0) job.loaded_q(r, ctl + kBarQ + 8 * g);
-      if (dual || nt == 1) {
-        if (!(alive = wait_or_abort(ctl + kBarO + 8 * g, (g == 0 ? c0 : c1) & 1, abort_flag))) break;
-        tc_fence_after();
-        job.out(x, row, o_addr + g * 128, 0, false, 1.f, 0.f, 0, 128, m_ref, l);
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], 2;" ::"r"(ctl + kBarOFree + 8 * g) : "memory");
-      } else {
-        // Join the two groups' sums; group g writes columns [64 g, 64 g + 64).
-        xch[g * 128 + r] = make_float2(m_ref, l);
-        __syncwarp();
-        if (lane == 0) mbar_arrive(ctl + kBarX);
-        if (!(alive = wait_or_abort(ctl + kBarX, nx & 1, abort_flag) && wait_or_abort(ctl + kBarO, c0 & 1, abort_flag) &&
-                      wait_or_abort(ctl + kBarO + 8, c1 & 1, abort_flag)))
-          break;
-        const float2 other = xch[(1 - g) * 128 + r];
-        const float m = fmaxf(m_ref, other.x), ref = m == -INFINITY ? 0.f : m;
-        const float mine_w = exp2f(m_ref - ref), other_w = exp2f(other.x - ref);
-        tc_fence_after();
-        job.out(x, row, o_addr + 64 * g, o_addr + 128 + 64 * g, true, g == 0 ? mine_w : other_w,
-                g == 0 ? other_w : mine_w, 64 * g, 64, m, l * mine_w + other.y * other_w);
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) {
-          mbar_arrive(ctl + kBarOFree);
-          mbar_arrive(ctl + kBarOFree + 8);
-          mbar_arrive(ctl + kBarXDone);
-        }
-        // Both groups have read the exchange before either writes it again.
-        if (!(alive = wait_or_abort(ctl + kBarXDone, nx & 1, abort_flag))) break;
-        ++nx;
-      }
+      // (m, l) go to the warps that write, once they have those of the group's unit before.
+      if (c_done > 0 && !(alive = wait_or_abort(ctl + kBarOFree + 8 * g, (c_done - 1) & 1, abort_flag))) break;
+      ++c_done;
+      xch[g * 128 + r] = make_float2(m_ref, l);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(ctl + kBarML + 8 * g);
       __syncwarp();
       if (lane == 0) mbar_arrive(ctl + kBarSchedFree + 8 * sx);
       sx = sy;
@@ -472,34 +468,61 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
     job.drain_q(ctl + kBarQ + 8 * g, *abort_flag != 0);
   } else {
     regs_dec<kOtherRegs>();
-    if (warp == kUnitWarp) {
-      // ---------------------------------------------------------------- units
-      // One unit ahead of the loading warp: its words are there when that warp gets to it, and no CTA sits on units that
-      // another could begin (taking four ahead cost 40% of a long prompt, whose CTAs have seven units each).
+    if (warp == kKWarp) {
+      // ---------------------------------------------------------------- units and K tiles
       const int total = job.total();
+      uint32_t n = 0;  // ring position
       bool ok = true;
-      for (int u = 0;; ++u) {
-        if (lane == 0 && u > 0) ok = wait_or_abort(ctl + kBarTake, (u - 1) & 1, abort_flag);
-        int id = 0;
-        if (lane == 0 && ok) id = job.ticket();
-        id = __shfl_sync(0xffffffffu, id, 0);
-        Unit x;
+      auto id_of = [&](int u) {  // b, 2 n - 1 - b, 2 n + b, ...
+        return u * (int)gridDim.x + ((u & 1) ? (int)gridDim.x - 1 - (int)blockIdx.x : (int)blockIdx.x);
+      };
+      auto find = [&](int u, Unit& x) {
         x.nt = -1;
-        if (id < total) job.unit(id, x);
+        if (id_of(u) < total) job.unit(id_of(u), x);
+      };
+      auto publish = [&](int u, const Unit& x) {
         const int slot = u & (kSlots - 1);
-        if (lane == 0 && ok && u >= kSlots)
-          ok = wait_or_abort(ctl + kBarSchedFree + 8 * slot, (u / kSlots - 1) & 1, abort_flag);
-        ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
-        if (!ok || *abort_flag) break;
-        if (lane == 0) {
+        if (u >= kSlots) ok = warp_wait(ctl + kBarSchedFree + 8 * slot, (u / kSlots - 1) & 1, abort_flag);
+        if (ok && lane == 0) {
           units[slot] = x;
           mbar_arrive(ctl + kBarSched + 8 * slot);
         }
-        if (x.nt < 0) break;
+        __syncwarp();
+      };
+      Unit x, y;
+      find(0, x);
+      publish(0, x);
+      int page = x.nt >= 0 ? job.page(x, 0, lane) : 0;  // the lane's page of the next tile
+      for (int u = 0; ok && x.nt >= 0; ++u) {
+        Unit z;
+        z.nt = -1;
+        for (int j = 0; j < x.nt && ok; ++j, n += 2) {
+          const uint32_t st = n % kStages;
+          if (n >= (uint32_t)kStages && !(ok = warp_wait(ctl + kBarEmpty + 8 * ((n - kStages) % kFulls), ((n - kStages) / kFulls) & 1, abort_flag))) break;
+          const uint32_t bar = ctl + kBarFull + 8 * (n % kFulls);
+          if (lane == 0) mbar_arrive_expect_tx(bar, kTile);
+          __syncwarp();
+          job.load_tile(x, j, 0, page, sbase + kRing + st * kTile, bar, lane);
+          if (j == 0) {  // units are known two ahead
+            if (u == 0) {
+              find(1, y);
+              publish(1, y);
+            }
+            if (y.nt >= 0) find(u + 2, z);
+          }
+          page = j + 1 < x.nt ? job.page(x, j + 1, lane) : y.nt >= 0 ? job.page(y, 0, lane) : 0;
+        }
+        if (!ok) break;
+        if (y.nt >= 0) publish(u + 2, z);
+        x = y;
+        y = z;
       }
-    } else if (warp == kLoadWarp) {
-      // ---------------------------------------------------------------- K and V tiles
-      uint32_t n = 0;  // stages filled
+      if (lane == 0 && *abort_flag)  // copies in flight land before the CTA leaves (bounded)
+        for (uint32_t k = n > 2 * kStages ? n - 2 * kStages : 0; k < n; k += 2)
+          mbar_wait_bounded(ctl + kBarFull + 8 * (k % kFulls), (k / kFulls) & 1, kWaitLimitNs / 8);
+    } else if (warp == kVWarp) {
+      // ---------------------------------------------------------------- V tiles
+      uint32_t n = 1;  // ring position
       uint32_t patches = 0;
       uint32_t p_dst = 0, p_full = 0;  // the V tile that waits to be mended
       int z0 = 0, z1 = 0;              // its rows that hold no token
@@ -507,16 +530,10 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       Unit x;
       auto fetch = [&](int u) {
         const int slot = u & (kSlots - 1);
-        if (lane == 0) ok = wait_or_abort(ctl + kBarSched + 8 * slot, (u / kSlots) & 1, abort_flag);
-        ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
-        if (!ok) return;
-        __syncwarp();
+        if (!(ok = warp_wait(ctl + kBarSched + 8 * slot, (u / kSlots) & 1, abort_flag))) return;
         x = units[slot];
         __syncwarp();
-        if (lane == 0) {
-          mbar_arrive(ctl + kBarSchedFree + 8 * slot);
-          mbar_arrive(ctl + kBarTake);
-        }
+        if (lane == 0) mbar_arrive(ctl + kBarSchedFree + 8 * slot);
       };
       // Whatever lies in the rows of a V tile that hold no token is made 0, since 0 x NaN is NaN.
       auto mend = [&]() {
@@ -531,10 +548,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       };
       // A stage's release, or with `landed` only the tile to be mended, which meanwhile is mended as soon as it is in.
       auto wait = [&](uint32_t bar, uint32_t parity, bool landed) {
-        if (z0 >= z1) {  // (a suspended wait leaves the issue slots to the softmax)
-          const bool in = lane != 0 || wait_or_abort(bar, parity, abort_flag);
-          return __shfl_sync(0xffffffffu, in ? 1 : 0, 0) != 0;
-        }
+        if (z0 >= z1) return warp_wait(bar, parity, abort_flag);  // (a suspended wait leaves the issue slots to others)
         uint64_t t0 = 0;
         for (uint32_t it = 1;; ++it) {
           int f = 0;
@@ -557,17 +571,16 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
         }
       };
       fetch(0);
-      int page = ok && x.nt >= 0 ? job.page(x, 0, lane) : 0;  // pages of the next tile, a tile ahead
+      int page = ok && x.nt >= 0 ? job.page(x, 0, lane) : 0;
       for (int u = 0; ok && x.nt >= 0; ++u) {
         const Unit now = x;
-        for (int t = 0; t < 2 * now.nt && ok; ++t, ++n) {
+        for (int j = 0; j < now.nt && ok; ++j, n += 2) {
           const uint32_t st = n % kStages, dst = sbase + kRing + st * kTile, full = ctl + kBarFull + 8 * (n % kFulls);
-          const int kv = t & 1, j = t >> 1;
-          if (n >= (uint32_t)kStages) ok = wait(ctl + kBarEmpty + 8 * st, (n / kStages - 1) & 1, false);
+          if (n >= (uint32_t)kStages) ok = wait(ctl + kBarEmpty + 8 * ((n - kStages) % kFulls), ((n - kStages) / kFulls) & 1, false);
           if (!ok) break;
           uint32_t bar = full;
           int s0 = 0, s1 = 0;
-          if (kv) job.stale_rows(now, j, s0, s1);
+          job.stale_rows(now, j, s0, s1);
           if (s0 < s1) {
             if (z0 < z1 && !(ok = wait(0, 0, true))) break;  // one at a time
             z0 = s0;
@@ -578,14 +591,12 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
           }
           if (lane == 0) mbar_arrive_expect_tx(bar, kTile);
           __syncwarp();
-          job.load_tile(now, j, kv, page, dst, bar, lane);
-          if (kv) {
-            if (j + 1 < now.nt) {
-              page = job.page(now, j + 1, lane);
-            } else {
-              fetch(u + 1);
-              if (ok && x.nt >= 0) page = job.page(x, 0, lane);
-            }
+          job.load_tile(now, j, 1, page, dst, bar, lane);
+          if (j + 1 < now.nt) {
+            page = job.page(now, j + 1, lane);
+          } else {
+            fetch(u + 1);
+            if (ok && x.nt >= 0) page = job.page(x, 0, lane);
           }
         }
       }
@@ -593,9 +604,57 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       // Copies in flight land before the CTA leaves (bounded).
       if (lane == 0 && *abort_flag) {
         if (z0 < z1) mbar_wait_bounded(ctl + kBarPatch, patches & 1, kWaitLimitNs / 8);
-        for (uint32_t k = n > (uint32_t)kStages ? n - kStages : 0; k < n; ++k)
+        for (uint32_t k = n > 2 * kStages ? n - 2 * kStages : 1; k < n; k += 2)
           if (ctl + kBarFull + 8 * (k % kFulls) != p_full || z0 >= z1)
             mbar_wait_bounded(ctl + kBarFull + 8 * (k % kFulls), (k / kFulls) & 1, kWaitLimitNs / 8);
+      }
+    } else if (warp >= kOutWarp) {
+      // ---------------------------------------------------------------- results
+      const int r = tid & 127;
+      const uint32_t o_addr = tmem + kTmemO + ((uint32_t)((warp & 3) * 32) << 16);
+      const float2* xch = reinterpret_cast<const float2*>(sm + kXch);
+      uint32_t c[2] = {0, 0};  // each group's units so far
+      for (int u = 0;; ++u) {
+        const int slot = u & (kSlots - 1);
+        if (!wait_or_abort(ctl + kBarSched + 8 * slot, (u / kSlots) & 1, abort_flag)) break;
+        const Unit& x = units[slot];
+        const int nt = x.nt, dual = x.dual;
+        if (nt < 0) break;
+        bool ok = true;
+        typename Job::Row row;
+        if (!dual && nt > 1) {  // the two groups' sums, joined
+          job.find_row(x, 0, r, row);
+          for (int g = 0; g < 2 && ok; ++g)
+            ok = wait_or_abort(ctl + kBarML + 8 * g, c[g] & 1, abort_flag) && wait_or_abort(ctl + kBarO + 8 * g, c[g] & 1, abort_flag);
+          if (!ok) break;
+          const float2 p = xch[r], q = xch[128 + r];
+          const float m = fmaxf(p.x, q.x), ref = m == -INFINITY ? 0.f : m, wp = exp2f(p.x - ref), wq = exp2f(q.x - ref);
+          tc_fence_after();
+          job.out(x, row, o_addr, o_addr + 128, true, wp, wq, m, p.y * wp + q.y * wq);
+          tc_fence_before();
+          __syncwarp();
+          for (int g = 0; g < 2; ++g, __syncwarp()) {
+            if (lane == 0) mbar_arrive(ctl + kBarOFree + 8 * g);
+            ++c[g];
+          }
+        } else {
+          for (int g = 0; g < 2; ++g) {
+            if (!takes_part(nt, dual, u, g)) continue;
+            job.find_row(x, g, r, row);
+            ok = wait_or_abort(ctl + kBarML + 8 * g, c[g] & 1, abort_flag) && wait_or_abort(ctl + kBarO + 8 * g, c[g] & 1, abort_flag);
+            if (!ok) break;
+            const float2 p = xch[g * 128 + r];
+            tc_fence_after();
+            job.out(x, row, o_addr + g * 128, 0, false, 1.f, 0.f, p.x, p.y);
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(ctl + kBarOFree + 8 * g);
+            ++c[g];
+          }
+          if (!ok) break;
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(ctl + kBarSchedFree + 8 * slot);
       }
     } else if (warp == kMmaWarp || warp == kMmaWarp + 1) {
       // ---------------------------------------------------------------- products, a warp per group
@@ -626,9 +685,9 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
         }
         const int mine = group_tiles(nt, dual, g);
         // A stage is free after both groups' use of it; a tile of one group's alone counts twice.
-        auto done_with = [&](uint32_t st) {
-          mma_commit(bars + kBarEmpty + 8 * st);
-          if (!dual) mma_commit(bars + kBarEmpty + 8 * st);
+        auto done_with = [&](uint32_t pos) {
+          mma_commit(bars + kBarEmpty + 8 * (pos % kFulls));
+          if (!dual) mma_commit(bars + kBarEmpty + 8 * (pos % kFulls));
         };
         for (int i = -1; i < mine && ok; ++i) {  // P.V of tile i, then S of tile i + 1
           const uint32_t v_pos = ring + 2 * group_tile(nt, dual, g, i) + 1, v_st = v_pos % kStages;
@@ -655,7 +714,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
 #pragma unroll
               for (int kk = kTok / 32; kk < kTok / 16; ++kk)
                 mma_ts_add(o_t, s_t + kk * 8, v0 + ((kk * Job::kVStep) >> 4), ID_PV);
-              done_with(v_st);
+              done_with(v_pos);
               if (i + 1 == mine) mma_commit(bars + kBarO + 8 * g);
             }
             __syncwarp();
@@ -671,7 +730,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
                 mma_add(s_t, q0 + (((kk >> 2) * 16384 + (kk & 3) * 32) >> 4),
                         k0 + (((kk >> 2) * Job::kKHalf + (kk & 3) * 32) >> 4), ID_S);
               mma_commit(bars + kBarS + 8 * g);
-              done_with(k_st);
+              done_with(k_pos);
             }
             __syncwarp();
           }

@@ -54,6 +54,7 @@ enum Ctl : int {
   kCtlSegGen = 19,     // segment rebuilds so far (stamps the per-page claim words)
   kCtlSegAlloc = 20,   // words 20-21: (segments << 32 | member slots) handed out by the running rebuild
   kCtlTailShared = 22, // 1 when a partial tail page may be shared (set by seed and forks, cleared by the planner)
+  kCtlSegStale = 23,   // 1 when the last truncation took pages that segments cover
   kCtlCounters = 24,   // words 24-26 and 28-30: the two counter sets of the attention launches (Counters)
   kCtlWords = 32
 };
@@ -388,7 +389,7 @@ cudaError_t set_max_dynamic_smem(const void* kernel, int bytes);
 cudaError_t launch_decode(gb_pool* pool, int layer, const void* q, const void* k_new, const void* v_new, float scale,
                           float* out, int mode, bool allow_local, cudaStream_t s);
 cudaError_t launch_decode_view(const PoolView& v, int W, const void* q, float scale, float* out, cudaStream_t s);
-cudaError_t rebuild_segments(gb_pool* pool, cudaStream_t s);
+cudaError_t rebuild_segments(gb_pool* pool, cudaStream_t s, const int* if_set = nullptr);  // if_set: a device word
 cudaError_t launch_forks(gb_pool* pool, const int32_t* parent_of, cudaStream_t s);
 cudaError_t launch_attention(gb_pool* pool, int layer, const void* q, const void* k_new, const void* v_new, float scale,
                              float* out, bool allow_local, cudaStream_t s);

@@ -18,7 +18,7 @@ namespace gb {
 namespace {
 
 // Workspace: control words, then the units.
-enum PromptCtl : int { kPrStatus = 0, kPrUnits = 1, kPrNext = 2, kPrWords = 64 };
+enum PromptCtl : int { kPrStatus = 0, kPrUnits = 1, kPrWords = 64 };
 
 struct PromptUnit {
   int start, len;   // the sequence's first row and length
@@ -57,10 +57,7 @@ __global__ void __launch_bounds__(kListThreads) k_prompt_plan(const int* cu, int
         const int len = length(s);
         units[at] = {cu[s], len, i * per, min(per, len - i * per)};
       });
-  if (threadIdx.x == 0) {
-    ctl[kPrUnits] = min(n, max_units);
-    ctl[kPrNext] = 0;
-  }
+  if (threadIdx.x == 0) ctl[kPrUnits] = min(n, max_units);
 }
 
 struct PromptView {
@@ -75,7 +72,7 @@ struct PromptJob : PromptView {
   const __nv_bfloat16 *q, *k, *v;
   __nv_bfloat16* o;
 
-  static constexpr bool kEarlyQ = false;
+  static constexpr bool kEarlyQ = false, kBits = false;
   static constexpr int kQArrivals = 1;
   // Tiles land as [half of D][128 tokens][64 dims].
   static constexpr int kKHalf = 16384, kKSbo = 1024, kVLbo = 16384, kVSbo = 1024, kVStep = 2048;
@@ -90,7 +87,6 @@ struct PromptJob : PromptView {
 
   __device__ __forceinline__ void error(int code) const { atomicCAS(&ctl[kPrStatus], GB_OK, code); }
   __device__ __forceinline__ int total() const { return ctl[kPrUnits] * Hkv; }
-  __device__ __forceinline__ int ticket() const { return atomicAdd(&ctl[kPrNext], 1); }
   __device__ __forceinline__ void unit(int id, flash::Unit& x) const {
     const PromptUnit e = reinterpret_cast<const PromptUnit*>(ctl + kPrWords)[id / Hkv];
     x.head = id % Hkv;
@@ -139,26 +135,26 @@ struct PromptJob : PromptView {
     return {k0 + flash::kTok - 1 <= row.first, row.tok - k0 + 1, 0ull};
   }
   __device__ __forceinline__ void out(const flash::Unit& x, const Row& row, uint32_t a, uint32_t b, bool two, float wa,
-                                      float wb, int c0, int cols, float m, float l) const {
+                                      float wb, float m, float l) const {
     const float inv = 1.f / l;
-    __nv_bfloat16* dst = o + (x.w[0] + row.tok) * out_stride + row.head * flash::kD + c0;
+    __nv_bfloat16* dst = o + (x.w[0] + row.tok) * out_stride + row.head * flash::kD;
     bool fine = true;
 #pragma unroll 1
-    for (int c = 0; c < cols; c += 32) {
-      float f[32];
+    for (int c = 0; c < flash::kD; c += 16) {
+      float f[16];
       flash::read_o(a + c, b + c, two, wa, wb, f);
-      uint32_t u[16];
+      uint32_t u[8];
 #pragma unroll
-      for (int i = 0; i < 32; i += 2) {
+      for (int i = 0; i < 16; i += 2) {
         const float f0 = f[i] * inv, f1 = f[i + 1] * inv;
         fine = fine && isfinite(f0) && isfinite(f1);
         const __nv_bfloat162 p = __floats2bfloat162_rn(f0, f1);
         u[i / 2] = *reinterpret_cast<const uint32_t*>(&p);
       }
-      if (row.valid)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          *reinterpret_cast<uint4*>(dst + c + 8 * i) = make_uint4(u[4 * i], u[4 * i + 1], u[4 * i + 2], u[4 * i + 3]);
+      if (row.valid) {
+        *reinterpret_cast<uint4*>(dst + c) = make_uint4(u[0], u[1], u[2], u[3]);
+        *reinterpret_cast<uint4*>(dst + c + 8) = make_uint4(u[4], u[5], u[6], u[7]);
+      }
     }
     unsigned redo = __ballot_sync(0xffffffffu, row.valid && !fine && isfinite(m) && isfinite(l));
     while (redo) {  // see sum_seen
@@ -170,7 +166,7 @@ struct PromptJob : PromptView {
       const __nv_bfloat16 *kh = k + s0 * k_stride + x.head * flash::kD, *vh = v + s0 * v_stride + x.head * flash::kD;
       bool unseen = false;
       for (long long j = tok + 1; j < (long long)x.nt * flash::kTok && s0 + j < num_tokens && !unseen; ++j)
-        unseen = flash::not_finite(vh + j * v_stride, c0, cols);
+        unseen = flash::not_finite(vh + j * v_stride);
       if (!unseen) continue;
       float acc[4];
       flash::sum_seen(
@@ -180,10 +176,9 @@ struct PromptJob : PromptView {
             vj = vh + j * v_stride;
             return true;
           },
-          qscale, mr, c0, cols, acc);
-      const int lane = threadIdx.x & 31, per = cols / 32;
-      for (int i = 0; i < per; ++i)
-        o[(s0 + tok) * out_stride + head * flash::kD + c0 + per * lane + i] = __float2bfloat16(acc[i] * ir);
+          qscale, mr, acc);
+      for (int i = 0; i < 4; ++i)
+        o[(s0 + tok) * out_stride + head * flash::kD + 4 * (threadIdx.x & 31) + i] = __float2bfloat16(acc[i] * ir);
     }
   }
   __device__ __forceinline__ void drain_q(uint32_t bar, bool aborted) const {

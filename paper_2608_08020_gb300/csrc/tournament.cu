@@ -54,6 +54,7 @@ struct TourArgs {
   int* parent_out;
   uint8_t* pruned_out;
   unsigned* lineage_out;
+  const int* if_set;        // when given, nothing is done unless this word is set
 };
 
 // Unsigned key whose ascending order is: larger mean first, +0 == -0, NaN last.
@@ -123,6 +124,7 @@ __device__ __forceinline__ void write_child(const PoolView& v, int s, int p, uns
 
 __global__ void __launch_bounds__(kTourThreads, 1) k_tournament(PoolView v, TourArgs a) {
   pdl_wait();
+  if (a.if_set && *a.if_set == 0) return;  // no CTA arrives at a barrier
   __shared__ unsigned long long s_keys[kMaxBeams];
   __shared__ int ord[kMaxBeams];      // rank -> slot
   __shared__ int blist[kMaxBeams];    // eligible parents in rank order
@@ -695,12 +697,15 @@ cudaError_t launch_prune_branch(gb_pool* pool, int K, int fanout, int warmup, co
   return launch_pdl(k_tournament, tournament_grid(pool), kTourThreads, 0, s, pool->view, a);
 }
 
-cudaError_t rebuild_segments(gb_pool* pool, cudaStream_t s) {
+cudaError_t rebuild_segments(gb_pool* pool, cudaStream_t s, const int* if_set) {
   if (!pool->view.grouped) return cudaSuccess;
-  return launch_forks(pool, nullptr, s);
+  TourArgs a{};
+  a.if_set = if_set;
+  pool->launches += 1;
+  return launch_pdl(k_tournament, tournament_grid(pool), kTourThreads, 0, s, pool->view, a);
 }
 
-// Apply parent_of's forks (nullptr: none) and rebuild the segments.
+// Apply parent_of's forks and rebuild the segments.
 cudaError_t launch_forks(gb_pool* pool, const int32_t* parent_of, cudaStream_t s) {
   TourArgs a{};
   a.parent_of = parent_of;

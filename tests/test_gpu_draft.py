@@ -518,7 +518,7 @@ def test_refusals(cuda):
                dict(workspace_dev=t.workspace.data_ptr() + 16), dict(workspace_bytes=t.workspace.numel() - 1), dict(n_draft=5)):
         assert attention(**kw) == accept(**kw) == "GB_ERR_INVALID", kw
     for kw in (dict(layer=-1), dict(layer=2), dict(q=None), dict(k=None), dict(v=None), dict(out=None), dict(q=q.data_ptr() + 8),
-               dict(k=k.data_ptr() + 2), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")),
+               dict(k=k.data_ptr() + 2), dict(out=out.data_ptr() + 16), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")),
                dict(out=q.data_ptr()), dict(out=k.data_ptr() + 256)):
         assert attention(**kw) == "GB_ERR_INVALID", kw
     for kw in (dict(k=None), dict(v=None), dict(a=None), dict(v=v.data_ptr() + 4)):
