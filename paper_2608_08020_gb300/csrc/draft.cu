@@ -625,8 +625,8 @@ struct DraftTile {
   }
   __device__ __forceinline__ const float* key(int j) const { return token(j, 0); }
   __device__ __forceinline__ const float* val(int j) const { return token(j, 1); }
-  __device__ __forceinline__ bool on(int r, int j) const {
-    return j < nctx || (valid(r) && ((w.anc[(size_t)u.beam * w.T + tok(r)] >> (j - nctx)) & 1));
+  __device__ __forceinline__ TileSees sees(int r) const {
+    return {nctx, nctx, valid(r) ? w.anc[(size_t)u.beam * w.T + tok(r)] : 0ull};
   }
   __device__ __forceinline__ void out(int r, int c, float4 x, float m, float l) const {
     if (!valid(r)) return;
@@ -642,7 +642,7 @@ struct DraftTile {
   }
 };
 
-__global__ void __launch_bounds__(kTileThreads) k_draft_f32(PoolView v, DraftView w, int layer, const float* q,
+__global__ void __launch_bounds__(kTileThreads, 1) k_draft_f32(PoolView v, DraftView w, int layer, const float* q,
                                                             const float* k, const float* vv, float* o, float qscale) {
   pdl_wait();
   pdl_launch_dependents();
@@ -1090,7 +1090,7 @@ extern "C" gb_status gb_draft_attention(gb_pool* pool, int layer, const gb_draft
   }
   if (layer == 0) {
     const int tokens = (bf16 ? 2 * flash::kRows : kTileRows) / v.G;
-    launch_pdl(k_draft_plan, 1, kListThreads, 0, s, v, w, d->count_dev, tokens, 2, bf16 && v.grouped);
+    launch_pdl(k_draft_plan, 1, kListThreads, 0, s, v, w, d->count_dev, tokens, bf16 ? 2 : 1, bf16 && v.grouped);
     launch_pdl(k_draft_rows, (v.max_beams + 7) / 8, 256, 0, s, v, w, d->parent_dev, d->count_dev);
     pool->launches += 2;
     if ((st = check_launch(pool, "draft_plan")) != GB_OK) return st;
@@ -1107,7 +1107,7 @@ extern "C" gb_status gb_draft_attention(gb_pool* pool, int layer, const gb_draft
   } else {
     e = set_max_dynamic_smem(reinterpret_cast<const void*>(k_draft_f32), (int)sizeof(TileSmem));
     if (e == cudaSuccess)
-      e = launch_pdl(k_draft_f32, pool->num_sms * 3, kTileThreads, sizeof(TileSmem), s, v, w, layer,
+      e = launch_pdl(k_draft_f32, pool->num_sms, kTileThreads, sizeof(TileSmem), s, v, w, layer,
                      static_cast<const float*>(q_dev), static_cast<const float*>(k_dev), static_cast<const float*>(v_dev),
                      static_cast<float*>(out_dev), qscale);
     if (e == cudaSuccess) e = launch_pdl(k_draft_merge<float, 64>, merge, 256, 0, s, v, w, static_cast<float*>(out_dev));

@@ -208,7 +208,7 @@ struct PromptTile {
   }
   __device__ __forceinline__ const float* key(int j) const { return kp + j * k_stride; }
   __device__ __forceinline__ const float* val(int j) const { return vp + j * v_stride; }
-  __device__ __forceinline__ bool on(int r, int j) const { return j <= tok(r); }
+  __device__ __forceinline__ TileSees sees(int r) const { return {tok(r) + 1, 0, 0ull}; }
   __device__ __forceinline__ void out(int r, int c, float4 o, float, float l) const {
     if (!valid(r)) return;
     const float inv = 1.f / l;
@@ -217,7 +217,7 @@ struct PromptTile {
   }
 };
 
-__global__ void __launch_bounds__(kTileThreads) k_prompt_f32(PromptView p, const float* q, const float* k,
+__global__ void __launch_bounds__(kTileThreads, 1) k_prompt_f32(PromptView p, const float* q, const float* k,
                                                              const float* v, float* o) {
   pdl_wait();
   pdl_launch_dependents();
@@ -239,7 +239,7 @@ __global__ void __launch_bounds__(kTileThreads) k_prompt_f32(PromptView p, const
 }
 
 // The rows of a unit: two tiles of 128 for the tensor cores, or one where few units leave SMs without
-// work; 64 for the CUDA cores.
+// work; 32 for the CUDA cores.
 int unit_tokens(int dtype, int G) { return (dtype == GB_BF16 ? 2 * flash::kRows : kTileRows) / G; }
 
 bool shape_ok(int dtype, int D, int Hq, int Hkv) {
