@@ -20,30 +20,33 @@ class DraftTrees:
         c = pool.cfg
         n = B.gb_draft_workspace_bytes(pool.handle, n_draft)
         self.workspace = torch.empty(n, dtype=torch.uint8, device=pool.kv.device)
+        self.device = self.workspace.device
+        self._args = B.GbDraft(workspace_dev=self.workspace.data_ptr(), workspace_bytes=n, n_draft=n_draft)
         self.dtype = TORCH_DT[pool.kv_dtype]
         self.q_shape = (pool.max_beams, n_draft, c.num_q_heads, c.head_dim)
         self.kv_shape = (pool.max_beams, n_draft, c.num_kv_heads, c.head_dim)
 
     def _check(self, name, x, shape, dtype):
-        if tuple(x.shape) != shape or x.dtype != dtype or not x.is_contiguous() or x.device != self.workspace.device:
+        if x.shape != shape or x.dtype is not dtype or x.device != self.device or not x.is_contiguous():
             raise ValueError(f"{name}: {tuple(x.shape)} {x.dtype} on {x.device}, expected contiguous {shape} {dtype} on "
-                             f"{self.workspace.device}")
+                             f"{self.device}")
+        return x.data_ptr()
 
     def _draft(self, parent, count):
-        self._check("parent", parent, self.kv_shape[:2], torch.int32)
-        if count is not None:
-            self._check("count", count, self.kv_shape[:1], torch.int32)
-        return B.GbDraft(parent.data_ptr(), None if count is None else count.data_ptr(), self.workspace.data_ptr(),
-                         self.workspace.numel(), self.n_draft)
+        d = self._args
+        d.parent_dev = self._check("parent", parent, self.kv_shape[:2], torch.int32)
+        d.count_dev = None if count is None else self._check("count", count, self.kv_shape[:1], torch.int32)
+        return d
 
     def attention(self, layer: int, q, k, v, parent, scale: float, out=None, count=None, stream=None):
         """One layer: q [max_beams][n_draft][q heads][D], k and v [max_beams][n_draft][kv heads][D], parent int32
         [max_beams][n_draft] (-1: the context's end), count int32 [max_beams] (None: n_draft each); returns out, like q."""
         if out is None:
-            out = torch.empty_like(q)
-        for name, x, shape in (("q", q, self.q_shape), ("k", k, self.kv_shape), ("v", v, self.kv_shape), ("out", out, self.q_shape)):
-            self._check(name, x, shape, self.dtype)
-        B.gb_draft_attention(self.pool.handle, layer, self._draft(parent, count), q, k, v, scale, out, stream)
+            out = torch.empty(self.q_shape, dtype=self.dtype, device=self.device)
+        check = self._check
+        B.gb_draft_attention(self.pool.handle, layer, self._draft(parent, count), check("q", q, self.q_shape, self.dtype),
+                             check("k", k, self.kv_shape, self.dtype), check("v", v, self.kv_shape, self.dtype), scale,
+                             check("out", out, self.q_shape, self.dtype), stream)
         return out
 
     def accept(self, k, v, parent, accepted, count=None, stream=None):
@@ -53,7 +56,8 @@ class DraftTrees:
         for name, x in (("k", k), ("v", v)):
             self._check(name, x, (self.pool.cfg.num_layers, *self.kv_shape), self.dtype)
         self._check("accepted", accepted, self.kv_shape[:1], torch.int32)
+        draft = self._draft(parent, count)
         n = torch.empty_like(accepted)
         path = torch.empty_like(parent)
-        B.gb_accept_draft(self.pool.handle, self._draft(parent, count), k, v, accepted, n, path, stream)
+        B.gb_accept_draft(self.pool.handle, draft, k, v, accepted, n, path, stream)
         return n, path
