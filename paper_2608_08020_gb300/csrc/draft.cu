@@ -418,7 +418,7 @@ struct DraftJob {
   const __nv_bfloat16 *q, *k, *vv;  // this layer's [max_beams][T][heads][128]
   __nv_bfloat16* o;
 
-  static constexpr bool kEarlyQ = true, kBits = true;
+  static constexpr bool kEarlyQ = true;
   static constexpr int kQArrivals = 4;
   // Tiles land as [16 groups of 8 tokens][half of D][8][64 dims].
   static constexpr int kKHalf = 1024, kKSbo = 2048, kVLbo = 1024, kVSbo = 2048, kVStep = 4096;
@@ -440,7 +440,7 @@ struct DraftJob {
     const int n = e.tok1 - e.tok0;
     x.head = id % v.Hkv;
     x.nt = e.drafts ? tail_tiles(n) : (n + flash::kTok - 1) / flash::kTok;
-    x.dual = e.ntok * v.G > flash::kRows;
+    x.mode = e.ntok * v.G > flash::kRows ? flash::kDual : flash::kJoint;
     x.w[kSeg] = e.seg;
     x.w[kBeam] = e.beam;
     x.w[kE0] = e.e0;
@@ -489,20 +489,25 @@ struct DraftJob {
     }
   }
   __device__ __forceinline__ void find_row(const flash::Unit& x, int g, int r, Row& row) const {
-    const int i = (x.dual ? g * flash::kRows + r : r) / v.G;
+    const int i = (x.mode == flash::kDual ? g * flash::kRows + r : r) / v.G;
     static_cast<DraftRow&>(row) = draft_row(w, x.w[kSeg], x.w[kBeam], x.w[kE0] + i, x.w[kRec], i < x.w[kNtok]);
     row.gg = r % v.G;
     row.anc = row.valid && x.w[kDrafts] ? w.anc[(size_t)row.beam * w.T + row.tok] : 0ull;
   }
   __device__ __forceinline__ void load_q(const flash::Unit& x, int g, int r, uint32_t dst, uint32_t bar,
                                          const Row& row) const {
-    const char* src =
-        reinterpret_cast<const char*>(q + (((size_t)row.beam * w.T + row.tok) * v.Hq + x.head * v.G + row.gg) * flash::kD);
+    // Half a warp to a row, so that a copy of the warp meets four lines (a row to a thread met 32).
+    const int lane = r & 31, c = lane & 15;
+    const unsigned long long mine = reinterpret_cast<unsigned long long>(
+        q + (((size_t)row.beam * w.T + row.tok) * v.Hq + x.head * v.G + row.gg) * flash::kD);
+    const unsigned there = __ballot_sync(0xffffffffu, row.valid);
 #pragma unroll
-    for (int c = 0; c < 16; ++c) {
-      const uint32_t to = dst + (c >> 3) * 16384 + swz(r, (c & 7) * 8);
-      if (row.valid)
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(src + 16 * c) : "memory");
+    for (int i = 0; i < 32; i += 2) {
+      const int l = i + (lane >> 4);
+      const char* src = reinterpret_cast<const char*>(__shfl_sync(0xffffffffu, mine, l)) + 16 * c;
+      const uint32_t to = dst + (c >> 3) * 16384 + swz((r & ~31) + l, (c & 7) * 8);
+      if ((there >> l) & 1)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(src) : "memory");
       else
         asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(to), "r"(0) : "memory");
     }
@@ -517,7 +522,7 @@ struct DraftJob {
   __device__ __forceinline__ flash::Sees sees(const flash::Unit& x, const Row& row, int t) const {
     const int n = x.w[kTok1] - x.w[kTok0] - t * flash::kTok;
     const bool last = draft_tile(x, t);
-    return {!last && n >= flash::kTok, n, last ? row.anc : 0ull};
+    return {!last && n >= flash::kTok, last, n, row.anc};
   }
   __device__ __forceinline__ void out(const flash::Unit& x, const Row& row, uint32_t a, uint32_t b, bool two, float wa,
                                       float wb, float m, float l) const {

@@ -6,14 +6,15 @@
 // with the running maximum m and sum l of each row's softmax, one pass over the keys.
 //
 // A unit has one head's query rows and nt tiles of 128 keys.  Two groups of four softmax warps each hold
-// a Q tile of 128 rows, an accumulator O and an S tile in tensor memory (512 columns in all).  In a dual
-// unit (129 to 256 rows) the groups have the two halves of the rows and every K/V tile serves
-// both.  A joint unit (up to 128 rows, more than one tile) has the same rows in both groups: group g takes
-// tiles g, g + 2, ..., and the groups' sums are joined at its end.  A unit of up to 128 rows and one tile is one
-// group's alone, the groups taking turns.  So there are two chains in flight: while one group
-// takes the exponentials of its S tile the tensor core works for the other.  Per tile 1024 cycles of
-// products (128^3 x 2 at 4096 multiply-adds a cycle) stand against 512 of ex2 (32 a cycle) and about 400 of
-// other instructions.
+// a Q tile of 128 rows, an accumulator O and an S tile in tensor memory (512 columns in all), so that two chains are in flight:
+// while one group takes the exponentials of its S tile the tensor core works for the other.  Per tile 1024
+// cycles of products (128^3 x 2 at 4096 multiply-adds a cycle) stand against 512 of ex2 (32 a cycle) and about 400 of
+// other instructions.  What a group works on:
+//   dual          129 to 256 rows: each group half of the rows, every K/V tile serves both
+//   first, second up to 128 rows: two units of the CTA's list, a group each, their tiles coming by turns
+//   joint         up to 128 rows and no second unit: the same rows in both groups, group g takes tiles g, g + 2, ...,
+//                 and their sums are joined at the end
+//   alone         the same with a single tile: group 0
 //
 // P is rounded to bf16 for the tensor core (relative 2^-9 each, independent, so a result's error
 // is about that of its own rounding to bf16); the sum l is of the unrounded values.
@@ -61,12 +62,13 @@ constexpr int kSmem = kXch + 2048;
 static_assert(kSmem <= 232448, "shared memory per block");
 constexpr uint32_t kTmemS = 0, kTmemO = 256;  // column of group 0; group 1 is 128 further
 
-constexpr int kSlots = 8, kUnitWords = 16;  // units known ahead
-// Three "full" and three "empty" barriers a stage, used in turn (ring position mod 15).  The warps do not keep step: a
-// group that has no tile of a unit goes on to the next one and may wait for a position up to 8 past the last one it saw
-// filled, and a loading warp may wait for a position whose predecessor in the stage the other one has yet to fill.  A
-// wait on a barrier whose phase before last has not ended would pass at once; for a waiter at position p that is the phase of
-// p - 15 (full) or p - 20 (empty), both consumed: p - 10, which is issued by then, came into a stage that was free.
+constexpr int kSlots = 8, kUnitWords = 12;  // units known ahead
+enum Mode : int { kJoint, kDual, kFirst, kSecond, kAlone };
+// Three "full" and three "empty" barriers a stage, used in turn (ring position mod 15), since the warps do not keep step: a wait
+// on a barrier whose phase before last has not ended would pass at once.  For a group that waits for K at position p that
+// phase is of p - 15, which has been consumed: K at p - 10 came into its stage, and is out before p's unit begins (kBarBegin)
+// or p - 4 was seen.  The V after a K that was seen follows in the same way, and a loading warp's wait, for the consumption of
+// p - 5, has p - 20 behind it.
 constexpr int kFulls = 3 * kStages;
 constexpr int kBarFull = 0;                       // [kFulls]
 constexpr int kBarEmpty = kBarFull + 8 * kFulls;  // [kFulls]
@@ -78,7 +80,8 @@ constexpr int kBarOFree = kBarO + 16;             // [2] the group's O has been 
 constexpr int kBarML = kBarOFree + 16;            // [2] the group's (m, l) are in
 constexpr int kBarPatch = kBarML + 16;            // a V tile that is mended before it is handed on
 constexpr int kBarSched = kBarPatch + 8;          // [kSlots]
-constexpr int kBarSchedFree = kBarSched + 8 * kSlots;
+constexpr int kBarBegin = kBarSched + 8 * kSlots;  // [kSlots] K of the unit is on its way
+constexpr int kBarSchedFree = kBarBegin + 8 * kSlots;
 constexpr int kUnits = (kBarSchedFree + 8 * kSlots + 15) / 16 * 16;  // int [kSlots][kUnitWords]
 constexpr int kWordTmem = kUnits + 4 * kSlots * kUnitWords;
 constexpr int kWordAbort = kWordTmem + 4;
@@ -88,16 +91,28 @@ constexpr int kSchedReaders = 15;  // eight softmax warps, two that issue produc
 // What every role knows of a unit; w is the job's own.
 struct Unit {
   int nt;    // tiles of 128 keys; -1: no more units
-  int dual;  // 129 to 256 rows
+  int mode;  // (the job says kDual or kJoint)
+  int mate;  // tiles of the other unit of a first or second one
   int head;  // KV head
-  int w[kUnitWords - 3];
+  int w[kUnitWords - 4];
 };
 static_assert(sizeof(Unit) == 4 * kUnitWords, "unit words");
 
-// Whether group g has tiles of a CTA's u-th unit, and how many.
-__device__ __forceinline__ bool takes_part(int nt, int dual, int u, int g) { return dual || nt > 1 || (u & 1) == g; }
-__device__ __forceinline__ int group_tiles(int nt, int dual, int g) { return dual || nt == 1 ? nt : (nt + 1 - g) / 2; }
-__device__ __forceinline__ int group_tile(int nt, int dual, int g, int i) { return dual || nt == 1 ? i : 2 * i + g; }
+__device__ __forceinline__ bool takes_part(int mode, int g) {
+  return mode <= kDual || (g == 0) != (mode == kSecond);
+}
+// Group g's tiles of a unit, and the ring position of the K of its i-th, counted from where the unit (or the pair) begins.
+__device__ __forceinline__ int group_tiles(int nt, int mode, int g) { return mode == kJoint ? (nt + 1 - g) / 2 : nt; }
+__device__ __forceinline__ int group_tile(int mode, int g, int i) { return mode == kJoint ? 2 * i + g : i; }
+__device__ __forceinline__ int tile_position(int mode, int mate, int g, int i) {
+  if (mode == kFirst) return 2 * (i + min(i, mate));
+  if (mode == kSecond) return 2 * (i + min(i + 1, mate));
+  return 2 * group_tile(mode, g, i);
+}
+// Ring positions of a unit, a pair's counted with its second.
+__device__ __forceinline__ int positions(int nt, int mode, int mate) {
+  return mode == kFirst ? 0 : mode == kSecond ? 2 * (nt + mate) : 2 * nt;
+}
 
 // The columns are handed out only after the wait: the registers pass through it.
 __device__ __forceinline__ void ld32_issue(uint32_t taddr, uint32_t* r) {
@@ -248,11 +263,12 @@ __device__ __forceinline__ void read_o(uint32_t a, uint32_t b, bool two, float w
   }
 }
 
-// Keys of a tile a row sees: the first `limit` and, from column 64 on, those of `bits`.
+// Keys of a tile a row sees: all of them, the first `limit`, or the first `limit` (up to 64) and those of `bits`.
 struct Sees {
-  bool all;                 // every key of the tile, for every row of the warp
+  bool all;                 // (the same for the warp)
+  bool by_bits;             // (the same for the warp)
   int limit;                // columns below this
-  unsigned long long bits;  // columns 64 + i for bit i
+  unsigned long long bits;  // column 64 + i for bit i
 };
 
 // sum_j 2^(qscale q.k_j - m) v_j over the keys that key(j, k, v) says are seen, by a warp: lane l gets
@@ -312,6 +328,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
     mbar_init(ctl + kBarPatch, 1);
     for (int i = 0; i < kSlots; ++i) {
       mbar_init(ctl + kBarSched + 8 * i, 1);
+      mbar_init(ctl + kBarBegin + 8 * i, 1);
       mbar_init(ctl + kBarSchedFree + 8 * i, kSchedReaders);
     }
     *abort_flag = 0;
@@ -346,9 +363,8 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       for (;; ++u_next) {
         slot = u_next & (kSlots - 1);
         if (!wait_or_abort(ctl + kBarSched + 8 * slot, (u_next / kSlots) & 1, abort_flag)) return false;
-        const int nt = units[slot].nt;
-        if (nt < 0) return true;
-        if (takes_part(nt, units[slot].dual, u_next, g)) {
+        if (units[slot].nt < 0) return true;
+        if (takes_part(units[slot].mode, g)) {
           ++u_next;
           return true;
         }
@@ -374,10 +390,10 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
     };
     while (alive && units[sx].nt >= 0) {
       const Unit& x = units[sx];
-      const int nt = x.nt, dual = x.dual, mine = group_tiles(nt, dual, g);
+      const int mode = x.mode, mine = group_tiles(x.nt, mode, g);
       float m_ref = -INFINITY, l = 0.f;
       for (int i = 0; i < mine; ++i, ++n) {
-        const int t = group_tile(nt, dual, g, i);
+        const int t = group_tile(mode, g, i);
         if (!wait_or_abort(ctl + kBarS + 8 * g, n & 1, abort_flag)) { alive = false; break; }
         if (Job::kEarlyQ && i + 1 == mine && !(alive = begin_next())) break;
         tc_fence_after();
@@ -391,13 +407,10 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
         if (!see.all) {
 #pragma unroll
           for (int c = 0; c < 64; ++c) s[c] = c < see.limit ? s[c] : -INFINITY;
-          if (Job::kBits) {
+          if (see.by_bits) {
             const uint32_t half[2] = {(uint32_t)see.bits, (uint32_t)(see.bits >> 32)};
 #pragma unroll
-            for (int c = 64; c < 128; ++c) {
-              const bool bit = (int32_t)(half[(c - 64) >> 5] << (31 - (c & 31))) < 0;
-              s[c] = bit || c < see.limit ? s[c] : -INFINITY;
-            }
+            for (int c = 64; c < 128; ++c) s[c] = (half[(c - 64) >> 5] & (1u << (c & 31))) ? s[c] : -INFINITY;
           } else {
 #pragma unroll
             for (int c = 64; c < 128; ++c) s[c] = c < see.limit ? s[c] : -INFINITY;
@@ -478,6 +491,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       };
       auto find = [&](int u, Unit& x) {
         x.nt = -1;
+        x.mate = 0;
         if (id_of(u) < total) job.unit(id_of(u), x);
       };
       auto publish = [&](int u, const Unit& x) {
@@ -489,33 +503,70 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
         }
         __syncwarp();
       };
-      Unit x, y;
-      find(0, x);
-      publish(0, x);
-      int page = x.nt >= 0 ? job.page(x, 0, lane) : 0;  // the lane's page of the next tile
-      for (int u = 0; ok && x.nt >= 0; ++u) {
-        Unit z;
-        z.nt = -1;
-        for (int j = 0; j < x.nt && ok; ++j, n += 2) {
-          const uint32_t st = n % kStages;
-          if (n >= (uint32_t)kStages && !(ok = warp_wait(ctl + kBarEmpty + 8 * ((n - kStages) % kFulls), ((n - kStages) / kFulls) & 1, abort_flag))) break;
-          const uint32_t bar = ctl + kBarFull + 8 * (n % kFulls);
-          if (lane == 0) mbar_arrive_expect_tx(bar, kTile);
-          __syncwarp();
-          job.load_tile(x, j, 0, page, sbase + kRing + st * kTile, bar, lane);
-          if (j == 0) {  // units are known two ahead
-            if (u == 0) {
-              find(1, y);
-              publish(1, y);
-            }
-            if (y.nt >= 0) find(u + 2, z);
-          }
-          page = j + 1 < x.nt ? job.page(x, j + 1, lane) : y.nt >= 0 ? job.page(y, 0, lane) : 0;
+      auto begin = [&](int u) {
+        if (lane == 0) mbar_arrive(ctl + kBarBegin + 8 * (u & (kSlots - 1)));
+      };
+      auto load = [&](const Unit& z, int j, int page) {
+        const uint32_t st = n % kStages;
+        if (n >= (uint32_t)kStages)
+          ok = warp_wait(ctl + kBarEmpty + 8 * ((n - kStages) % kFulls), ((n - kStages) / kFulls) & 1, abort_flag);
+        if (!ok) return;
+        const uint32_t bar = ctl + kBarFull + 8 * (n % kFulls);
+        if (lane == 0) mbar_arrive_expect_tx(bar, kTile);
+        __syncwarp();
+        job.load_tile(z, j, 0, page, sbase + kRing + st * kTile, bar, lane);
+        n += 2;
+      };
+      // Modes of a unit and the one after it: two of up to 128 rows make a pair.
+      auto match = [&](Unit& p, Unit& q) {
+        if (p.nt < 0 || p.mode == kDual) return false;
+        if (q.nt < 0 || q.mode == kDual) {
+          if (p.nt == 1) p.mode = kAlone;
+          return false;
         }
-        if (!ok) break;
-        if (y.nt >= 0) publish(u + 2, z);
-        x = y;
-        y = z;
+        p.mode = kFirst;
+        p.mate = q.nt;
+        q.mode = kSecond;
+        q.mate = p.nt;
+        return true;
+      };
+      // x, and y where they are a pair, are known to all and next to be loaded; what follows is looked up meanwhile.
+      Unit x, y, a, c;
+      find(0, x);
+      find(1, y);
+      bool pair = match(x, y);
+      publish(0, x);
+      if (pair && ok) publish(1, y);
+      int page_x = x.nt >= 0 ? job.page(x, 0, lane) : 0, page_y = pair ? job.page(y, 0, lane) : 0;  // the lane's pages
+      for (int u = 0; ok && x.nt >= 0;) {
+        const int step = pair ? 2 : 1, tiles = pair ? max(x.nt, y.nt) : x.nt;
+        bool next_pair = false;
+        begin(u);
+        if (pair) begin(u + 1);
+        for (int j = 0; j < tiles && ok; ++j) {
+          if (j < x.nt) {
+            load(x, j, page_x);
+            if (j + 1 < x.nt) page_x = job.page(x, j + 1, lane);
+          }
+          if (pair && j < y.nt && ok) {
+            load(y, j, page_y);
+            if (j + 1 < y.nt) page_y = job.page(y, j + 1, lane);
+          }
+          if (j == 0 && ok) {
+            if (pair) find(u + 2, a);
+            else a = y;
+            find(u + step + 1, c);
+            next_pair = match(a, c);
+            publish(u + step, a);
+            if (next_pair && ok) publish(u + step + 1, c);
+          }
+        }
+        u += step;
+        pair = next_pair;
+        x = a;
+        y = c;
+        page_x = ok && x.nt >= 0 ? job.page(x, 0, lane) : 0;
+        page_y = ok && pair ? job.page(y, 0, lane) : 0;
       }
       if (lane == 0 && *abort_flag)  // copies in flight land before the CTA leaves (bounded)
         for (uint32_t k = n > 2 * kStages ? n - 2 * kStages : 0; k < n; k += 2)
@@ -527,11 +578,11 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       uint32_t p_dst = 0, p_full = 0;  // the V tile that waits to be mended
       int z0 = 0, z1 = 0;              // its rows that hold no token
       bool ok = true;
-      Unit x;
-      auto fetch = [&](int u) {
+      auto fetch = [&](int u, Unit& to) {
         const int slot = u & (kSlots - 1);
+        to.nt = -1;
         if (!(ok = warp_wait(ctl + kBarSched + 8 * slot, (u / kSlots) & 1, abort_flag))) return;
-        x = units[slot];
+        to = units[slot];
         __syncwarp();
         if (lane == 0) mbar_arrive(ctl + kBarSchedFree + 8 * slot);
       };
@@ -570,35 +621,53 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
           if (f == 1 || (landed && f == 2)) return true;
         }
       };
-      fetch(0);
-      int page = ok && x.nt >= 0 ? job.page(x, 0, lane) : 0;
-      for (int u = 0; ok && x.nt >= 0; ++u) {
-        const Unit now = x;
-        for (int j = 0; j < now.nt && ok; ++j, n += 2) {
-          const uint32_t st = n % kStages, dst = sbase + kRing + st * kTile, full = ctl + kBarFull + 8 * (n % kFulls);
-          if (n >= (uint32_t)kStages) ok = wait(ctl + kBarEmpty + 8 * ((n - kStages) % kFulls), ((n - kStages) / kFulls) & 1, false);
-          if (!ok) break;
-          uint32_t bar = full;
-          int s0 = 0, s1 = 0;
-          job.stale_rows(now, j, s0, s1);
-          if (s0 < s1) {
-            if (z0 < z1 && !(ok = wait(0, 0, true))) break;  // one at a time
-            z0 = s0;
-            z1 = s1;
-            p_dst = dst;
-            p_full = full;
-            bar = ctl + kBarPatch;
+      auto load = [&](const Unit& now, int j, int page) {
+        const uint32_t st = n % kStages, dst = sbase + kRing + st * kTile, full = ctl + kBarFull + 8 * (n % kFulls);
+        if (n >= (uint32_t)kStages)
+          ok = wait(ctl + kBarEmpty + 8 * ((n - kStages) % kFulls), ((n - kStages) / kFulls) & 1, false);
+        if (!ok) return;
+        uint32_t bar = full;
+        int s0 = 0, s1 = 0;
+        job.stale_rows(now, j, s0, s1);
+        if (s0 < s1) {
+          if (z0 < z1 && !(ok = wait(0, 0, true))) return;  // one at a time
+          z0 = s0;
+          z1 = s1;
+          p_dst = dst;
+          p_full = full;
+          bar = ctl + kBarPatch;
+        }
+        if (lane == 0) mbar_arrive_expect_tx(bar, kTile);
+        __syncwarp();
+        job.load_tile(now, j, 1, page, dst, bar, lane);
+        n += 2;
+      };
+      Unit x, y;
+      fetch(0, x);
+      bool pair = ok && x.nt >= 0 && x.mode == kFirst;
+      if (pair) fetch(1, y);
+      int page_x = ok && x.nt >= 0 ? job.page(x, 0, lane) : 0, page_y = ok && pair ? job.page(y, 0, lane) : 0;
+      for (int u = 0; ok && x.nt >= 0;) {
+        const int tiles = pair ? max(x.nt, y.nt) : x.nt;
+        for (int j = 0; j < tiles && ok; ++j) {
+          if (j < x.nt) {
+            load(x, j, page_x);
+            if (j + 1 < x.nt) page_x = job.page(x, j + 1, lane);
           }
-          if (lane == 0) mbar_arrive_expect_tx(bar, kTile);
-          __syncwarp();
-          job.load_tile(now, j, 1, page, dst, bar, lane);
-          if (j + 1 < now.nt) {
-            page = job.page(now, j + 1, lane);
-          } else {
-            fetch(u + 1);
-            if (ok && x.nt >= 0) page = job.page(x, 0, lane);
+          if (pair && j < y.nt && ok) {
+            load(y, j, page_y);
+            if (j + 1 < y.nt) page_y = job.page(y, j + 1, lane);
           }
         }
+        if (!ok) break;
+        u += pair ? 2 : 1;
+        fetch(u, x);
+        if (!ok) break;
+        pair = x.nt >= 0 && x.mode == kFirst;
+        if (pair) fetch(u + 1, y);
+        if (!ok) break;
+        page_x = x.nt >= 0 ? job.page(x, 0, lane) : 0;
+        page_y = pair ? job.page(y, 0, lane) : 0;
       }
       if (ok && z0 < z1) ok = wait(0, 0, true);
       // Copies in flight land before the CTA leaves (bounded).
@@ -618,11 +687,11 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
         const int slot = u & (kSlots - 1);
         if (!wait_or_abort(ctl + kBarSched + 8 * slot, (u / kSlots) & 1, abort_flag)) break;
         const Unit& x = units[slot];
-        const int nt = x.nt, dual = x.dual;
-        if (nt < 0) break;
+        const int mode = x.mode;
+        if (x.nt < 0) break;
         bool ok = true;
         typename Job::Row row;
-        if (!dual && nt > 1) {  // the two groups' sums, joined
+        if (mode == kJoint) {  // the two groups' sums
           job.find_row(x, 0, r, row);
           for (int g = 0; g < 2 && ok; ++g)
             ok = wait_or_abort(ctl + kBarML + 8 * g, c[g] & 1, abort_flag) && wait_or_abort(ctl + kBarO + 8 * g, c[g] & 1, abort_flag);
@@ -639,7 +708,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
           }
         } else {
           for (int g = 0; g < 2; ++g) {
-            if (!takes_part(nt, dual, u, g)) continue;
+            if (!takes_part(mode, g)) continue;
             job.find_row(x, g, r, row);
             ok = wait_or_abort(ctl + kBarML + 8 * g, c[g] & 1, abort_flag) && wait_or_abort(ctl + kBarO + 8 * g, c[g] & 1, abort_flag);
             if (!ok) break;
@@ -676,22 +745,23 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       for (int u = 0; ok; ++u) {
         const int slot = u & (kSlots - 1);
         if (!wait(bars + kBarSched + 8 * slot, (u / kSlots) & 1)) break;
-        const int nt = __shfl_sync(0xffffffffu, units[slot].nt, 0), dual = __shfl_sync(0xffffffffu, units[slot].dual, 0);
+        const int nt = __shfl_sync(0xffffffffu, units[slot].nt, 0), mode = __shfl_sync(0xffffffffu, units[slot].mode, 0),
+                  mate = __shfl_sync(0xffffffffu, units[slot].mate, 0);
         if (leader) mbar_arrive(bars + kBarSchedFree + 8 * slot);
         if (nt < 0) break;
-        if (!takes_part(nt, dual, u, g)) {
-          ring += 2 * nt;
-          continue;
-        }
-        const int mine = group_tiles(nt, dual, g);
+        const uint32_t from = ring;
+        ring += positions(nt, mode, mate);
+        if (!takes_part(mode, g)) continue;
+        if (!wait(bars + kBarBegin + 8 * slot, (u / kSlots) & 1)) break;
+        const int mine = group_tiles(nt, mode, g);
         // A stage is free after both groups' use of it; a tile of one group's alone counts twice.
         auto done_with = [&](uint32_t pos) {
           mma_commit(bars + kBarEmpty + 8 * (pos % kFulls));
-          if (!dual) mma_commit(bars + kBarEmpty + 8 * (pos % kFulls));
+          if (mode != kDual) mma_commit(bars + kBarEmpty + 8 * (pos % kFulls));
         };
         for (int i = -1; i < mine && ok; ++i) {  // P.V of tile i, then S of tile i + 1
-          const uint32_t v_pos = ring + 2 * group_tile(nt, dual, g, i) + 1, v_st = v_pos % kStages;
-          const uint32_t k_pos = ring + 2 * group_tile(nt, dual, g, i + 1), k_st = k_pos % kStages;
+          const uint32_t v_pos = from + tile_position(mode, mate, g, i) + 1, v_st = v_pos % kStages;
+          const uint32_t k_pos = from + tile_position(mode, mate, g, i + 1), k_st = k_pos % kStages;
           // The tiles first: once P is there nothing else is waited for between it and the next S.
           if (i + 1 < mine && !wait(bars + kBarFull + 8 * (k_pos % kFulls), (k_pos / kFulls) & 1)) break;
           if (i < 0) {
@@ -736,7 +806,6 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
           }
         }
         ++c;
-        ring += 2 * nt;
       }
       if (leader && *abort_flag && n > 0)  // products in flight end before the tensor memory is freed (bounded)
         mbar_wait_bounded(bars + kBarS + 8 * g, (n - 1) & 1, kWaitLimitNs / 8);

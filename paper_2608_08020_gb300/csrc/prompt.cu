@@ -72,7 +72,7 @@ struct PromptJob : PromptView {
   const __nv_bfloat16 *q, *k, *v;
   __nv_bfloat16* o;
 
-  static constexpr bool kEarlyQ = false, kBits = false;
+  static constexpr bool kEarlyQ = false;
   static constexpr int kQArrivals = 1;
   // Tiles land as [half of D][128 tokens][64 dims].
   static constexpr int kKHalf = 16384, kKSbo = 1024, kVLbo = 16384, kVSbo = 1024, kVStep = 2048;
@@ -91,7 +91,7 @@ struct PromptJob : PromptView {
     const PromptUnit e = reinterpret_cast<const PromptUnit*>(ctl + kPrWords)[id / Hkv];
     x.head = id % Hkv;
     x.nt = (e.t0 + e.ntok + flash::kTok - 1) / flash::kTok;
-    x.dual = e.ntok * G > flash::kRows;
+    x.mode = e.ntok * G > flash::kRows ? flash::kDual : flash::kJoint;
     x.w[0] = e.start;
     x.w[1] = e.t0;
     x.w[2] = e.ntok;
@@ -113,7 +113,7 @@ struct PromptJob : PromptView {
         : "memory");
   }
   __device__ __forceinline__ int first_token(const flash::Unit& x, int g) const {
-    return x.w[1] + (x.dual ? g * (flash::kRows / G) : 0);
+    return x.w[1] + (x.mode == flash::kDual ? g * (flash::kRows / G) : 0);
   }
   __device__ __forceinline__ void find_row(const flash::Unit& x, int g, int r, Row& row) const {
     const int base = first_token(x, g);
@@ -132,7 +132,7 @@ struct PromptJob : PromptView {
   __device__ __forceinline__ void loaded_q(int, uint32_t) const {}
   __device__ __forceinline__ flash::Sees sees(const flash::Unit&, const Row& row, int t) const {
     const int k0 = t * flash::kTok;
-    return {k0 + flash::kTok - 1 <= row.first, row.tok - k0 + 1, 0ull};
+    return {k0 + flash::kTok - 1 <= row.first, false, row.tok - k0 + 1, 0ull};
   }
   __device__ __forceinline__ void out(const flash::Unit& x, const Row& row, uint32_t a, uint32_t b, bool two, float wa,
                                       float wb, float m, float l) const {
