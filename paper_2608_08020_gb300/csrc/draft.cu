@@ -524,8 +524,9 @@ struct DraftJob {
     const bool last = draft_tile(x, t);
     return {!last && n >= flash::kTok, last, n, row.anc};
   }
+  template <class Done>
   __device__ __forceinline__ void out(const flash::Unit& x, const Row& row, uint32_t a, uint32_t b, bool two, float wa,
-                                      float wb, float m, float l) const {
+                                      float wb, float m, float l, Done done) const {
     const bool final = row.rec < 0;
     const float inv = final ? 1.f / l : 1.f;
     const int head = x.head * v.G + row.gg;
@@ -533,29 +534,31 @@ struct DraftJob {
     const size_t rr = ((size_t)max(row.rec, 0) * v.Hkv + x.head) * w.rows + row.tok * v.G + row.gg;
     float* rec = w.rec + rr * flash::kD;
     bool fine = true;
-#pragma unroll 1
-    for (int c = 0; c < flash::kD; c += 16) {
-      float f[16];
-      flash::read_o(a + c, b + c, two, wa, wb, f);
+    flash::walk_o(
+        a, b, two, wa, wb,
+        [&](int c, auto count, float* f) {
+          constexpr int N = decltype(count)::value;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        f[i] *= inv;
-        fine = fine && isfinite(f[i]);
-      }
-      if (!row.valid) continue;
-      if (final) {
-        uint32_t u[8];
+          for (int i = 0; i < N; ++i) {
+            f[i] *= inv;
+            fine = fine && isfinite(f[i]);
+          }
+          if (!row.valid) return;
+          if (final) {
+            uint32_t u[N / 2];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const __nv_bfloat162 p = __floats2bfloat162_rn(f[2 * k], f[2 * k + 1]);
-          u[k] = *reinterpret_cast<const uint32_t*>(&p);
-        }
-        flash::st32(dst + c, u);
-      } else {
-        flash::st32(rec + c, reinterpret_cast<const uint32_t*>(f));
-        flash::st32(rec + c + 8, reinterpret_cast<const uint32_t*>(f + 8));
-      }
-    }
+            for (int k = 0; k < N / 2; ++k) {
+              const __nv_bfloat162 p = __floats2bfloat162_rn(f[2 * k], f[2 * k + 1]);
+              u[k] = *reinterpret_cast<const uint32_t*>(&p);
+            }
+#pragma unroll
+            for (int k = 0; k < N / 2; k += 8) flash::st32(dst + c + 2 * k, u + k);
+          } else {
+#pragma unroll
+            for (int k = 0; k < N; k += 8) flash::st32(rec + c + k, reinterpret_cast<const uint32_t*>(f + k));
+          }
+        },
+        done);
     if (row.valid && !final) w.ml[rr] = make_float2(m, l);
     unsigned redo = __ballot_sync(0xffffffffu, row.valid && x.w[kDrafts] && !fine && isfinite(m) && isfinite(l));
     while (redo) {  // see sum_seen; only drafted tokens off the row's path share a tile with what it sees

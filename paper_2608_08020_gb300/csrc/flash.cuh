@@ -38,6 +38,7 @@
 #include <cuda.h>
 #include <mutex>
 #include <set>
+#include <type_traits>
 #include <utility>
 
 #include "internal.cuh"
@@ -243,23 +244,47 @@ __device__ __forceinline__ void ld16_wait(uint32_t* r) {
                :
                : "memory");
 }
-// 16 columns of a row's result: O of one group, or of both with their weights.
-__device__ __forceinline__ void read_o(uint32_t a, uint32_t b, bool two, float wa, float wb, float* o) {
-  uint32_t u[16];
+// Columns of a row's result, N = 16 or 32 of one group's O, or 16 of both with their weights.
+template <int N>
+__device__ __forceinline__ void read_o(uint32_t a, float* o) {
+  uint32_t u[N];
+#pragma unroll
+  for (int c = 0; c < N; c += 16) ld16_issue(a + c, u + c);
+#pragma unroll
+  for (int c = 0; c < N; c += 16) ld16_wait(u + c);
+#pragma unroll
+  for (int c = 0; c < N; ++c) o[c] = __uint_as_float(u[c]);
+}
+__device__ __forceinline__ void read_both(uint32_t a, uint32_t b, float wa, float wb, float* o) {
+  uint32_t u[16], v[16];
   ld16_issue(a, u);
+  ld16_issue(b, v);
+  ld16_wait(u);
+  ld16_wait(v);
+  // A weight of 0 belongs to a group that saw no key of the row: what it summed is 0 x V.
+#pragma unroll
+  for (int c = 0; c < 16; ++c)
+    o[c] = (wa == 0.f ? 0.f : wa * __uint_as_float(u[c])) + (wb == 0.f ? 0.f : wb * __uint_as_float(v[c]));
+}
+// The 128 columns in turn, 32 at a time (16 of a joint unit): use(c, N, values).  done() once all have been read.
+template <class Use, class Done>
+__device__ __forceinline__ void walk_o(uint32_t a, uint32_t b, bool two, float wa, float wb, Use use, Done done) {
   if (two) {
-    uint32_t v[16];
-    ld16_issue(b, v);
-    ld16_wait(u);
-    ld16_wait(v);
-    // A weight of 0 belongs to a group that saw no key of the row: what it summed is 0 x V.
-#pragma unroll
-    for (int c = 0; c < 16; ++c)
-      o[c] = (wa == 0.f ? 0.f : wa * __uint_as_float(u[c])) + (wb == 0.f ? 0.f : wb * __uint_as_float(v[c]));
+#pragma unroll 1
+    for (int c = 0; c < kD; c += 16) {
+      float f[16];
+      read_both(a + c, b + c, wa, wb, f);
+      if (c + 16 == kD) done();
+      use(c, std::integral_constant<int, 16>{}, f);
+    }
   } else {
-    ld16_wait(u);
-#pragma unroll
-    for (int c = 0; c < 16; ++c) o[c] = __uint_as_float(u[c]);
+#pragma unroll 1
+    for (int c = 0; c < kD; c += 32) {
+      float f[32];
+      read_o<32>(a + c, f);
+      if (c + 32 == kD) done();
+      use(c, std::integral_constant<int, 32>{}, f);
+    }
   }
 }
 
@@ -699,13 +724,13 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
           const float2 p = xch[r], q = xch[128 + r];
           const float m = fmaxf(p.x, q.x), ref = m == -INFINITY ? 0.f : m, wp = exp2f(p.x - ref), wq = exp2f(q.x - ref);
           tc_fence_after();
-          job.out(x, row, o_addr, o_addr + 128, true, wp, wq, m, p.y * wp + q.y * wq);
-          tc_fence_before();
-          __syncwarp();
-          for (int g = 0; g < 2; ++g, __syncwarp()) {
-            if (lane == 0) mbar_arrive(ctl + kBarOFree + 8 * g);
-            ++c[g];
-          }
+          job.out(x, row, o_addr, o_addr + 128, true, wp, wq, m, p.y * wp + q.y * wq, [&]() {
+            tc_fence_before();
+            __syncwarp();
+            if (lane < 2) mbar_arrive(ctl + kBarOFree + 8 * lane);
+          });
+          ++c[0];
+          ++c[1];
         } else {
           for (int g = 0; g < 2; ++g) {
             if (!takes_part(mode, g)) continue;
@@ -714,10 +739,11 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
             if (!ok) break;
             const float2 p = xch[g * 128 + r];
             tc_fence_after();
-            job.out(x, row, o_addr + g * 128, 0, false, 1.f, 0.f, p.x, p.y);
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(ctl + kBarOFree + 8 * g);
+            job.out(x, row, o_addr + g * 128, 0, false, 1.f, 0.f, p.x, p.y, [&]() {
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(ctl + kBarOFree + 8 * g);
+            });
             ++c[g];
           }
           if (!ok) break;

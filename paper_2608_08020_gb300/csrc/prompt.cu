@@ -134,28 +134,30 @@ struct PromptJob : PromptView {
     const int k0 = t * flash::kTok;
     return {k0 + flash::kTok - 1 <= row.first, false, row.tok - k0 + 1, 0ull};
   }
+  template <class Done>
   __device__ __forceinline__ void out(const flash::Unit& x, const Row& row, uint32_t a, uint32_t b, bool two, float wa,
-                                      float wb, float m, float l) const {
+                                      float wb, float m, float l, Done done) const {
     const float inv = 1.f / l;
     __nv_bfloat16* dst = o + (x.w[0] + row.tok) * out_stride + row.head * flash::kD;
     bool fine = true;
-#pragma unroll 1
-    for (int c = 0; c < flash::kD; c += 16) {
-      float f[16];
-      flash::read_o(a + c, b + c, two, wa, wb, f);
-      uint32_t u[8];
+    flash::walk_o(
+        a, b, two, wa, wb,
+        [&](int c, auto count, const float* f) {
+          constexpr int N = decltype(count)::value;
+          uint32_t u[N / 2];
 #pragma unroll
-      for (int i = 0; i < 16; i += 2) {
-        const float f0 = f[i] * inv, f1 = f[i + 1] * inv;
-        fine = fine && isfinite(f0) && isfinite(f1);
-        const __nv_bfloat162 p = __floats2bfloat162_rn(f0, f1);
-        u[i / 2] = *reinterpret_cast<const uint32_t*>(&p);
-      }
-      if (row.valid) {
-        *reinterpret_cast<uint4*>(dst + c) = make_uint4(u[0], u[1], u[2], u[3]);
-        *reinterpret_cast<uint4*>(dst + c + 8) = make_uint4(u[4], u[5], u[6], u[7]);
-      }
-    }
+          for (int i = 0; i < N; i += 2) {
+            const float f0 = f[i] * inv, f1 = f[i + 1] * inv;
+            fine = fine && isfinite(f0) && isfinite(f1);
+            const __nv_bfloat162 p = __floats2bfloat162_rn(f0, f1);
+            u[i / 2] = *reinterpret_cast<const uint32_t*>(&p);
+          }
+          if (row.valid)
+#pragma unroll
+            for (int i = 0; i < N / 2; i += 4)
+              *reinterpret_cast<uint4*>(dst + c + 2 * i) = make_uint4(u[i], u[i + 1], u[i + 2], u[i + 3]);
+        },
+        done);
     unsigned redo = __ballot_sync(0xffffffffu, row.valid && !fine && isfinite(m) && isfinite(l));
     while (redo) {  // see sum_seen
       const int src = __ffs(redo) - 1;
