@@ -190,13 +190,42 @@ __device__ __forceinline__ int drafted(const int* count, int b, int T, bool act,
 // and joined kRecCost per 128 rows.
 constexpr int kTileCost = 8, kUnitCost = 10, kRecCost = 14;
 
+// Slots up to which the planner's CTA also writes the rows (two slots a warp), without a launch of its own.
+constexpr int kOneLaunch = 64;
+
+// A warp per slot of [first, first + step, ...): the ancestor masks of its tokens, and their entries in the lists of the
+// slot's segments.
+__device__ __forceinline__ void draft_rows(const PoolView& v, const DraftView& w, const int* parent, const int* count,
+                                           int first, int step) {
+  const int lane = threadIdx.x & 31;
+  for (int b = first; b < v.max_beams; b += step) {
+    bool bad = false;
+    const int n = drafted(count, b, w.T, v.active[b] != 0, &bad), nd = w.depth[b], base = w.rec_base[b];
+    int at = 0, rec = 0;
+    if (lane < nd && n > 0) {  // lane k: the slot's k-th segment
+      at = w.seg_list[v.seg_bid[b * kMaxSegDepth + lane]] + w.off[b * kMaxSegDepth + lane];
+      rec = base + w.rec_off[b * kRecOffs + lane];
+    }
+    unsigned long long lo, hi;
+    bool wrong;
+    ancestors(parent + (size_t)b * w.T, w.T, n, &lo, &hi, &wrong);
+    if (lane < w.T) w.anc[(size_t)b * w.T + lane] = lo;
+    if (lane + 32 < w.T) w.anc[(size_t)b * w.T + lane + 32] = hi;
+    if ((bad || wrong) && lane == 0) set_status(v.ctl, GB_ERR_INVALID);
+    for (int k = 0; k < nd; ++k) {
+      int2* to = w.list + __shfl_sync(0xffffffffu, at, k);
+      const int r = __shfl_sync(0xffffffffu, rec, k);
+      for (int i = lane; i < n; i += 32) to[i] = make_int2(b | i << 10, r);
+    }
+  }
+}
 // The work list (one CTA).  `tokens`: of a unit's rows; `least`: tiles below which a run of keys is not split.
 //
 // Down to which depth the shared segments are used is chosen by the cost above: a segment's unit reads
 // its pages once for up to 256 rows, but every piece of a beam's context beyond the first costs a record.  64 beams of 50 rows
 // over 64 shared and 130 own tokens run without segments; 64 beams of 50 rows at 4000 tokens use them all.
-__global__ void __launch_bounds__(kListThreads) k_draft_plan(PoolView v, DraftView w, const int* count, int tokens, int least,
-                                                             bool segs) {
+__global__ void __launch_bounds__(kListThreads) k_draft_plan(PoolView v, DraftView w, const int* parent, const int* count,
+                                                             int tokens, int least, bool segs) {
   pdl_wait();
   pdl_launch_dependents();
   constexpr int kCached = 4096;         // segments whose rows and tiles fit in shared memory
@@ -368,32 +397,17 @@ __global__ void __launch_bounds__(kListThreads) k_draft_plan(PoolView v, DraftVi
         w.units[at] = u;
       });
   if (tid == 0) w.ctl[kDrUnits] = min(n, w.max_units);
+  if (cap <= kOneLaunch) {
+    __threadfence_block();
+    __syncthreads();
+    draft_rows(v, w, parent, count, tid >> 5, kListThreads / 32);
+  }
 }
 
-// A warp per slot: the ancestor masks of its tokens, and their entries in the lists of the slot's segments.
 __global__ void __launch_bounds__(256) k_draft_rows(PoolView v, DraftView w, const int* parent, const int* count) {
   pdl_wait();
   pdl_launch_dependents();
-  const int b = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-  if (b >= v.max_beams) return;
-  bool bad = false;
-  const int n = drafted(count, b, w.T, v.active[b] != 0, &bad), nd = w.depth[b], base = w.rec_base[b];
-  int at = 0, rec = 0;
-  if (lane < nd && n > 0) {  // lane k: the slot's k-th segment
-    at = w.seg_list[v.seg_bid[b * kMaxSegDepth + lane]] + w.off[b * kMaxSegDepth + lane];
-    rec = base + w.rec_off[b * kRecOffs + lane];
-  }
-  unsigned long long lo, hi;
-  bool wrong;
-  ancestors(parent + (size_t)b * w.T, w.T, n, &lo, &hi, &wrong);
-  if (lane < w.T) w.anc[(size_t)b * w.T + lane] = lo;
-  if (lane + 32 < w.T) w.anc[(size_t)b * w.T + lane + 32] = hi;
-  if ((bad || wrong) && lane == 0) set_status(v.ctl, GB_ERR_INVALID);
-  for (int k = 0; k < nd; ++k) {
-    int2* to = w.list + __shfl_sync(0xffffffffu, at, k);
-    const int r = __shfl_sync(0xffffffffu, rec, k);
-    for (int i = lane; i < n; i += 32) to[i] = make_int2(b | i << 10, r);
-  }
+  draft_rows(v, w, parent, count, blockIdx.x * 8 + (threadIdx.x >> 5), gridDim.x * 8);
 }
 
 // Where a row's result goes: the output itself when the beam has one record, else its record.
@@ -432,10 +446,14 @@ struct DraftJob {
   };
 
   __device__ __forceinline__ void error(int code) const { set_status(v.ctl, code); }
-  __device__ __forceinline__ int total() const { return w.ctl[kDrUnits] * v.Hkv; }
+  struct Units {
+    int count;
+    __device__ __forceinline__ explicit Units(const DraftJob& j) : count(j.w.ctl[kDrUnits]) {}
+  };
+  __device__ __forceinline__ int total(const Units& all) const { return all.count * v.Hkv; }
   // Words of a unit, those of its loads first.
   enum { kBeam, kTok0, kTok1, kDrafts, kSeg, kE0, kNtok, kRec };
-  __device__ __forceinline__ void unit(int id, flash::Unit& x) const {
+  __device__ __forceinline__ void unit(const Units&, int id, flash::Unit& x) const {
     const DraftUnit e = w.units[id / v.Hkv];
     const int n = e.tok1 - e.tok0;
     x.head = id % v.Hkv;
@@ -1098,9 +1116,12 @@ extern "C" gb_status gb_draft_attention(gb_pool* pool, int layer, const gb_draft
   }
   if (layer == 0) {
     const int tokens = (bf16 ? 2 * flash::kRows : kTileRows) / v.G;
-    launch_pdl(k_draft_plan, 1, kListThreads, 0, s, v, w, d->count_dev, tokens, bf16 ? 2 : 1, bf16 && v.grouped);
-    launch_pdl(k_draft_rows, (v.max_beams + 7) / 8, 256, 0, s, v, w, d->parent_dev, d->count_dev);
-    pool->launches += 2;
+    launch_pdl(k_draft_plan, 1, kListThreads, 0, s, v, w, d->parent_dev, d->count_dev, tokens, bf16 ? 2 : 1, bf16 && v.grouped);
+    pool->launches += 1;
+    if (v.max_beams > kOneLaunch) {
+      launch_pdl(k_draft_rows, (v.max_beams + 7) / 8, 256, 0, s, v, w, d->parent_dev, d->count_dev);
+      pool->launches += 1;
+    }
     if ((st = check_launch(pool, "draft_plan")) != GB_OK) return st;
     pool->draft_epoch = pool->epoch;
     pool->draft_ws = d->workspace_dev;

@@ -508,7 +508,8 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
     regs_dec<kOtherRegs>();
     if (warp == kKWarp) {
       // ---------------------------------------------------------------- units and K tiles
-      const int total = job.total();
+      const typename Job::Units all(job);
+      const int total = job.total(all);
       uint32_t n = 0;  // ring position
       bool ok = true;
       auto id_of = [&](int u) {  // b, 2 n - 1 - b, 2 n + b, ...
@@ -517,7 +518,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       auto find = [&](int u, Unit& x) {
         x.nt = -1;
         x.mate = 0;
-        if (id_of(u) < total) job.unit(id_of(u), x);
+        if (id_of(u) < total) job.unit(all, id_of(u), x);
       };
       auto publish = [&](int u, const Unit& x) {
         const int slot = u & (kSlots - 1);

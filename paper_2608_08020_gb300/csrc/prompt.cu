@@ -62,9 +62,34 @@ __global__ void __launch_bounds__(kListThreads) k_prompt_plan(const int* cu, int
 
 struct PromptView {
   int* ctl;
+  const int* cu;
+  int num_seqs, tokens, small_tokens, few;  // tokens of a unit, where there are at most `few` of them small_tokens
   int Hkv, G, num_tokens;
   float qscale;
   long long q_stride, k_stride, v_stride, out_stride;  // elements between tokens
+};
+
+// The units.  One prompt's are known from its bounds, longest first, without the planner's launch (5 us of a 16 us call
+// of 333 tokens).
+struct PromptUnits {
+  int start, len, per, count;
+  __device__ __forceinline__ explicit PromptUnits(const PromptView& p) {
+    if (p.num_seqs != 1) {
+      count = p.ctl[kPrUnits];
+      return;
+    }
+    start = p.cu[0];
+    const int end = p.cu[1];
+    len = start >= 0 && start <= end && end <= p.num_tokens ? end - start : 0;
+    per = (len + p.tokens - 1) / p.tokens <= p.few ? p.small_tokens : p.tokens;
+    count = (len + per - 1) / per;
+    if (blockIdx.x == 0 && threadIdx.x % 32 == 0) p.ctl[kPrStatus] = start >= 0 && start <= end && end <= p.num_tokens ? GB_OK : GB_ERR_INVALID;
+  }
+  __device__ __forceinline__ PromptUnit operator()(const PromptView& p, int i) const {
+    if (p.num_seqs != 1) return reinterpret_cast<const PromptUnit*>(p.ctl + kPrWords)[i];
+    const int t0 = (count - 1 - i) * per;
+    return {start, len, t0, min(per, len - t0)};
+  }
 };
 
 struct PromptJob : PromptView {
@@ -86,9 +111,10 @@ struct PromptJob : PromptView {
   };
 
   __device__ __forceinline__ void error(int code) const { atomicCAS(&ctl[kPrStatus], GB_OK, code); }
-  __device__ __forceinline__ int total() const { return ctl[kPrUnits] * Hkv; }
-  __device__ __forceinline__ void unit(int id, flash::Unit& x) const {
-    const PromptUnit e = reinterpret_cast<const PromptUnit*>(ctl + kPrWords)[id / Hkv];
+  using Units = PromptUnits;  // what the warp that takes the units holds
+  __device__ __forceinline__ int total(const Units& all) const { return all.count * Hkv; }
+  __device__ __forceinline__ void unit(const Units& all, int id, flash::Unit& x) const {
+    const PromptUnit e = all(*this, id / Hkv);
     x.head = id % Hkv;
     x.nt = (e.t0 + e.ntok + flash::kTok - 1) / flash::kTok;
     x.mode = e.ntok * G > flash::kRows ? flash::kDual : flash::kJoint;
@@ -225,9 +251,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_prompt_f32(PromptView p, co
   pdl_launch_dependents();
   extern __shared__ __align__(16) unsigned char raw[];
   TileSmem& sm = *reinterpret_cast<TileSmem*>(raw);
-  const int total = p.ctl[kPrUnits] * p.Hkv;
+  const PromptUnits all(p);
+  const int total = all.count * p.Hkv;
   for (int id = blockIdx.x; id < total; id += gridDim.x) {
-    const PromptUnit e = reinterpret_cast<const PromptUnit*>(p.ctl + kPrWords)[id / p.Hkv];
+    const PromptUnit e = all(p, id / p.Hkv);
     const int h = id % p.Hkv;
     const long long s0 = e.start;
     const PromptTile src{q + s0 * p.q_stride + h * p.G * kTileD,
@@ -317,7 +344,7 @@ extern "C" gb_status gb_prompt_attention(const gb_prompt_args* a, gb_stream_t st
   // groups share its keys.
   const int few = a->dtype == GB_BF16 ? sms / a->num_kv_heads : 0;
   const long long most = max_units(a->dtype, G, a->num_tokens, a->num_seqs);
-  PromptView view{ctl, a->num_kv_heads, G, a->num_tokens, a->scale * 1.4426950408889634f,
+  PromptView view{ctl, a->cu_seqlens, a->num_seqs, tokens, few ? flash::kRows / G : tokens, few, a->num_kv_heads, G, a->num_tokens, a->scale * 1.4426950408889634f,
                   a->q_stride, a->k_stride, a->v_stride, a->out_stride};
   if (a->dtype == GB_BF16 && !flash::launches_with(reinterpret_cast<const void*>(k_prompt))) return GB_ERR_UNSUPPORTED;
   // The tensor maps first: nothing is enqueued when one cannot be made.
@@ -337,8 +364,9 @@ extern "C" gb_status gb_prompt_attention(const gb_prompt_args* a, gb_stream_t st
         !encode_tensor_map(&job.tv, a->v, 4, kd, vs, kb))
       return GB_ERR_CUDA;
   }
-  if (launch_pdl(k_prompt_plan, 1, kListThreads, 0, s, a->cu_seqlens, a->num_seqs, a->num_tokens, tokens,
-                 few ? flash::kRows / G : tokens, few, (int)most, ctl) != cudaSuccess)
+  if (a->num_seqs != 1 &&
+      launch_pdl(k_prompt_plan, 1, kListThreads, 0, s, a->cu_seqlens, a->num_seqs, a->num_tokens, tokens,
+                 view.small_tokens, few, (int)most, ctl) != cudaSuccess)
     return GB_ERR_CUDA;
   cudaError_t e;
   if (a->dtype == GB_BF16) {
