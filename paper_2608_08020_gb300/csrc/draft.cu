@@ -232,6 +232,8 @@ __global__ void __launch_bounds__(kListThreads) k_draft_plan(PoolView v, DraftVi
   __shared__ ListSmem sm;
   __shared__ short s_cnt[kMaxBeams];
   __shared__ unsigned s_src[kCached];   // rows | tiles << 16, each clamped (a source with more is read from memory)
+  constexpr int kStaged = 512;          // slots whose segments' lengths do
+  __shared__ unsigned short s_seg[kStaged * kMaxSegDepth];
   __shared__ int s_cost[kMaxSegDepth + 1];
   __shared__ int s_start[kMaxBeams], s_len[kMaxBeams];
   const int tid = threadIdx.x;
@@ -251,8 +253,18 @@ __global__ void __launch_bounds__(kListThreads) k_draft_plan(PoolView v, DraftVi
   // Segments: their drafted tokens, and each beam's place among them.
   for (int e = tid; e < (segs ? cap * kMaxSegDepth : 0); e += kListThreads) {
     const int c = s_cnt[e / kMaxSegDepth], k = e % kMaxSegDepth;
-    if (c > 0 && k < v.seg_nseg[e / kMaxSegDepth]) w.off[e] = atomicAdd(&w.seg_cnt[v.seg_bid[e]], c);
+    if (c > 0 && k < v.seg_nseg[e / kMaxSegDepth]) {
+      const int s = v.seg_bid[e];
+      if (cap <= kStaged) s_seg[e] = (unsigned short)v.seg_len[s];  // (a table has at most 65535 entries then)
+      w.off[e] = atomicAdd(&w.seg_cnt[s], c);
+    }
   }
+  const bool staged = cap <= kStaged && v.max_pages < 65536;
+  __syncthreads();
+  auto depth_pages = [&](int k) {  // pages of this slot's k-th segment
+    return staged ? (int)s_seg[b * kMaxSegDepth + k] : v.seg_len[v.seg_bid[b * kMaxSegDepth + k]];
+  };
+  auto depth_tiles = [&](int k) { return (depth_pages(k) * v.P + flash::kTok - 1) / flash::kTok; };
   auto seg_tiles = [&](int s) { return (v.seg_len[s] * v.P + flash::kTok - 1) / flash::kTok; };
   auto unit_cost = [&](int rows, int tiles, int rec) {  // of `rows` tokens over `tiles` tiles
     const int full = rows / tokens, rest = rows - full * tokens, halves = 2 * full + (rest > 0) + (2 * rest > tokens);
@@ -266,7 +278,7 @@ __global__ void __launch_bounds__(kListThreads) k_draft_plan(PoolView v, DraftVi
       for (int k = 0; k < nd; ++k) {
         // What using the k-th segment too changes: a shorter rest, and for the first one a record.
         const int from = tail_tiles(L - at), rec = k == 0 ? kRecCost : 0;
-        at += v.seg_len[v.seg_bid[b * kMaxSegDepth + k]] * v.P;
+        at += depth_pages(k) * v.P;
         atomicAdd(&s_cost[k + 1], unit_cost(cnt, tail_tiles(L - at), rec) - unit_cost(cnt, from, 0));
       }
     }
@@ -295,7 +307,7 @@ __global__ void __launch_bounds__(kListThreads) k_draft_plan(PoolView v, DraftVi
   }
   nd = min(nd, dmax);
   int start = 0;
-  for (int k = 0; k < nd; ++k) start += v.seg_len[v.seg_bid[b * kMaxSegDepth + k]] * v.P;
+  for (int k = 0; k < nd; ++k) start += depth_pages(k) * v.P;
   const int tail = cnt > 0 ? tail_tiles(L - start) : 0;
   auto seg_rows = [&](int s) { return v.seg_members[v.seg_mem_off[s]] % kMaxSegDepth < dmax ? w.seg_cnt[s] : 0; };
   int work = tail * ((cnt + tokens - 1) / tokens);
@@ -317,7 +329,7 @@ __global__ void __launch_bounds__(kListThreads) k_draft_plan(PoolView v, DraftVi
   int mine, base;
   for (;; per *= 2) {
     mine = cnt > 0 ? (tail + per - 1) / per : 0;
-    for (int k = 0; k < nd; ++k) mine += (seg_tiles(v.seg_bid[b * kMaxSegDepth + k]) + per - 1) / per;
+    for (int k = 0; k < nd; ++k) mine += (depth_tiles(k) + per - 1) / per;
     base = block_exclusive_scan(mine, sm.tmp, &all);
     if (all <= w.rec_cap || per > (1 << 24)) break;
   }
@@ -327,7 +339,7 @@ __global__ void __launch_bounds__(kListThreads) k_draft_plan(PoolView v, DraftVi
     w.rec_base[b] = base;
     for (int k = 0; k < nd; ++k) {
       w.rec_off[b * kRecOffs + k] = tail_rec;
-      tail_rec += (seg_tiles(v.seg_bid[b * kMaxSegDepth + k]) + per - 1) / per;
+      tail_rec += (depth_tiles(k) + per - 1) / per;
     }
     w.rec_off[b * kRecOffs + kTailRec] = tail_rec;
     w.depth[b] = nd;
@@ -451,6 +463,7 @@ struct DraftJob {
     __device__ __forceinline__ explicit Units(const DraftJob& j) : count(j.w.ctl[kDrUnits]) {}
   };
   __device__ __forceinline__ int total(const Units& all) const { return all.count * v.Hkv; }
+  __device__ __forceinline__ int capacity() const { return w.max_units * v.Hkv; }
   // Words of a unit, those of its loads first.
   enum { kBeam, kTok0, kTok1, kDrafts, kSeg, kE0, kNtok, kRec };
   __device__ __forceinline__ void unit(const Units&, int id, flash::Unit& x) const {
@@ -765,8 +778,23 @@ __global__ void __launch_bounds__(1024) k_accept_plan(PoolView v, DraftView w, c
   __shared__ int s_first[kMaxDraft];                      // needs of earlier tokens
   __shared__ int s_pages[kMaxBeams * kMaxNeeds];
   const int tid = threadIdx.x, b = tid, lane = tid & 31;
-  // Paths, a warp per slot.
-  for (int s = tid >> 5; s < v.max_beams; s += 32) {
+  const int nodes = v.max_beams * w.T;
+  const bool staged = nodes <= kMaxBeams * kMaxNeeds;
+  if (staged) {  // the trees fit in shared memory (in s_pages, before its use): a thread walks its slot's path up
+    for (int i = tid; i < nodes; i += 1024) s_pages[i] = parent[i];
+    bool bad = false;
+    const bool on = b < v.max_beams && v.active[b] != 0;
+    const int n = b < v.max_beams ? drafted(count, b, w.T, on, &bad) : 0, to = on ? accepted[b] : -1;
+    __syncthreads();
+    unsigned long long p = 0;
+    bool odd = to < -1 || to >= n;
+    for (int i = 0; i < n; ++i) odd |= s_pages[b * w.T + i] < -1 || s_pages[b * w.T + i] >= i;
+    for (int i = odd ? -1 : to; i >= 0; i = s_pages[b * w.T + i]) p |= 1ull << i;
+    if (b < v.max_beams) s_path[b] = p;
+    if (odd || bad) set_status(v.ctl, GB_ERR_INVALID);
+  }
+  // Larger ones: a warp per slot.
+  for (int s = tid >> 5; s < (staged ? 0 : v.max_beams); s += 32) {
     bool bad = false, wrong;
     const int n = drafted(count, s, w.T, v.active[s] != 0, &bad), to = v.active[s] ? accepted[s] : -1;
     unsigned long long lo, hi;

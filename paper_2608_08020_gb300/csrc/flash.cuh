@@ -336,12 +336,12 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
     if (tid == 0) job.error(GB_ERR_UNSUPPORTED);
     return;
   }
-  if (tid == 0) {
-    for (int i = 0; i < kFulls; ++i) {
-      mbar_init(ctl + kBarFull + 8 * i, 1);
-      mbar_init(ctl + kBarEmpty + 8 * i, 2);
-    }
-    for (int i = 0; i < 2; ++i) {
+  if (warp == 0) {  // a barrier to a lane
+    if (lane < kFulls) {
+      mbar_init(ctl + kBarFull + 8 * lane, 1);
+      mbar_init(ctl + kBarEmpty + 8 * lane, 2);
+    } else if (lane < kFulls + 2) {
+      const int i = lane - kFulls;
       mbar_init(ctl + kBarQ + 8 * i, Job::kQArrivals);
       mbar_init(ctl + kBarS + 8 * i, 1);
       mbar_init(ctl + kBarP + 16 * i, 4);
@@ -349,14 +349,16 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       mbar_init(ctl + kBarO + 8 * i, 1);
       mbar_init(ctl + kBarOFree + 8 * i, 4);
       mbar_init(ctl + kBarML + 8 * i, 4);
-    }
-    mbar_init(ctl + kBarPatch, 1);
-    for (int i = 0; i < kSlots; ++i) {
+    } else if (lane < kFulls + 2 + kSlots) {
+      const int i = lane - kFulls - 2;
       mbar_init(ctl + kBarSched + 8 * i, 1);
       mbar_init(ctl + kBarBegin + 8 * i, 1);
       mbar_init(ctl + kBarSchedFree + 8 * i, kSchedReaders);
+    } else if (lane == 31) {
+      mbar_init(ctl + kBarPatch, 1);
+      *abort_flag = 0;
     }
-    *abort_flag = 0;
+    static_assert(kFulls + 2 + kSlots <= 31, "a lane each");
     fence_mbar_init();
   }
   if (warp == kMmaWarp) {
@@ -509,7 +511,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
     if (warp == kKWarp) {
       // ---------------------------------------------------------------- units and K tiles
       const typename Job::Units all(job);
-      const int total = job.total(all);
+      const int total = job.total(all), cap = job.capacity();
       uint32_t n = 0;  // ring position
       bool ok = true;
       auto id_of = [&](int u) {  // b, 2 n - 1 - b, 2 n + b, ...
@@ -518,7 +520,9 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       auto find = [&](int u, Unit& x) {
         x.nt = -1;
         x.mate = 0;
-        if (id_of(u) < total) job.unit(all, id_of(u), x);
+        const int id = id_of(u);
+        if (id < cap) job.unit(all, id, x);  // (before the count of units is in: the list is there to its capacity)
+        if (id >= total) x.nt = -1;
       };
       auto publish = [&](int u, const Unit& x) {
         const int slot = u & (kSlots - 1);

@@ -43,10 +43,14 @@ class DraftTrees:
         [max_beams][n_draft] (-1: the context's end), count int32 [max_beams] (None: n_draft each); returns out, like q."""
         if out is None:
             out = torch.empty(self.q_shape, dtype=self.dtype, device=self.device)
-        check = self._check
-        B.gb_draft_attention(self.pool.handle, layer, self._draft(parent, count), check("q", q, self.q_shape, self.dtype),
-                             check("k", k, self.kv_shape, self.dtype), check("v", v, self.kv_shape, self.dtype), scale,
-                             check("out", out, self.q_shape, self.dtype), stream)
+        qs, ks, dt, dev = self.q_shape, self.kv_shape, self.dtype, self.device
+        if not (q.shape == qs and k.shape == ks and v.shape == ks and out.shape == qs and q.dtype is dt and k.dtype is dt
+                and v.dtype is dt and out.dtype is dt and q.is_contiguous() and k.is_contiguous() and v.is_contiguous()
+                and out.is_contiguous() and q.device == dev and k.device == dev and v.device == dev and out.device == dev):
+            for name, x, shape in (("q", q, qs), ("k", k, ks), ("v", v, ks), ("out", out, qs)):
+                self._check(name, x, shape, dt)
+        B.gb_draft_attention(self.pool.handle, layer, self._draft(parent, count), q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                             scale, out.data_ptr(), stream)
         return out
 
     def accept(self, k, v, parent, accepted, count=None, stream=None):
