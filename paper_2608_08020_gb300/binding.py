@@ -161,6 +161,26 @@ def _bind_torch(torch) -> None:
     _torch = torch
 
 
+def current_device() -> int:
+    """Index of the current torch device."""
+    if _torch is None:
+        import torch
+        _bind_torch(torch)
+    get = getattr(_torch._C, "_cuda_getDevice", None)
+    return get() if get is not None else _torch.cuda.current_device()
+
+
+def new_on(stream, make):
+    """make() with its memory belonging to `stream` (None: the current stream; else a torch.cuda.Stream)."""
+    if stream is None:
+        return make()
+    import torch
+    if not isinstance(stream, torch.cuda.Stream):
+        raise ValueError("outputs have to be given with a raw stream")
+    with torch.cuda.stream(stream):
+        return make()
+
+
 def stream_handle(s) -> int | None:
     if s is None:
         try:

@@ -28,7 +28,7 @@ constexpr int kTailRec = kMaxSegDepth;  // rec_off column of a beam's own units
 constexpr int kRecOffs = kMaxSegDepth + 1;
 
 // Workspace words of control.
-enum DraftCtl : int { kDrUnits = 0, kDrList = 1, kDrWords = 64 };
+enum DraftCtl : int { kDrUnits = 0, kDrList = 1, kDrFew = 2, kDrWords = 64 };
 
 struct DraftUnit {
   int seg;         // -1: a beam's own unit
@@ -190,8 +190,8 @@ __device__ __forceinline__ int drafted(const int* count, int b, int T, bool act,
 // and joined kRecCost per 128 rows.
 constexpr int kTileCost = 8, kUnitCost = 10, kRecCost = 14;
 
-// Slots up to which the planner's CTA also writes the rows (two slots a warp), without a launch of its own.
-constexpr int kOneLaunch = 64;
+// Slots up to which the planner's CTA also writes the rows (a slot to a warp), without a launch of its own.
+constexpr int kOneLaunch = 16;
 
 // A warp per slot of [first, first + step, ...): the ancestor masks of its tokens, and their entries in the lists of the
 // slot's segments.
@@ -219,13 +219,13 @@ __device__ __forceinline__ void draft_rows(const PoolView& v, const DraftView& w
     }
   }
 }
-// The work list (one CTA).  `tokens`: of a unit's rows; `least`: tiles below which a run of keys is not split.
+// The work list (one CTA).  `tokens`: of a unit's rows, `small`: where there are few units; `least`: tiles below which a run of keys is not split.
 //
 // Down to which depth the shared segments are used is chosen by the cost above: a segment's unit reads
 // its pages once for up to 256 rows, but every piece of a beam's context beyond the first costs a record.  64 beams of 50 rows
 // over 64 shared and 130 own tokens run without segments; 64 beams of 50 rows at 4000 tokens use them all.
 __global__ void __launch_bounds__(kListThreads) k_draft_plan(PoolView v, DraftView w, const int* parent, const int* count,
-                                                             int tokens, int least, bool segs) {
+                                                             int tokens, int small, int least, bool segs) {
   pdl_wait();
   pdl_launch_dependents();
   constexpr int kCached = 4096;         // segments whose rows and tiles fit in shared memory
@@ -310,23 +310,47 @@ __global__ void __launch_bounds__(kListThreads) k_draft_plan(PoolView v, DraftVi
   for (int k = 0; k < nd; ++k) start += depth_pages(k) * v.P;
   const int tail = cnt > 0 ? tail_tiles(L - start) : 0;
   auto seg_rows = [&](int s) { return v.seg_members[v.seg_mem_off[s]] % kMaxSegDepth < dmax ? w.seg_cnt[s] : 0; };
-  int work = tail * ((cnt + tokens - 1) / tokens);
+  // Few units of 128 rows: that many rows to a unit, and one unit per SM (two shorter ones leave SMs idle in the second
+  // wave: a 20000-token beam of 8 KV heads in 256 units of 5 tiles took as long as 144 of 9 would in two waves).
+  int mine, base, work = 0, whole = 0;
   for (int s = tid; s < nseg; s += kListThreads) {
     const int c = seg_rows(s), t = seg_tiles(s);
     if (s < kCached) s_src[s] = (unsigned)min(c, 65535) | (unsigned)min(t, 65535) << 16;
-    work += (c + tokens - 1) / tokens * t;
+    whole += (c + small - 1) / small;
     if (c > 0) w.seg_list[s] = atomicAdd(&w.ctl[kDrList], c);
   }
+  block_exclusive_scan(whole + (cnt + small - 1) / small, sm.tmp, &all);
+  const bool few = (long long)all * v.Hkv <= v.num_sms;
+  if (few) tokens = small;
+  auto tiles_of = [&](int s, int* rows) {  // of a segment, and its row tiles
+    const unsigned x = s < kCached ? s_src[s] : ~0u;
+    const int c = (x & 0xffff) == 0xffff ? seg_rows(s) : x & 0xffff;
+    *rows = (c + tokens - 1) / tokens;
+    return c == 0 ? 0 : x >> 16 == 0xffff ? seg_tiles(s) : x >> 16;
+  };
+  const int rows_b = (cnt + tokens - 1) / tokens;
+  work = tail * rows_b;
+  for (int s = tid; s < nseg; s += kListThreads) {
+    int rows;
+    const int t = tiles_of(s, &rows);
+    work += rows * t;
+  }
   block_exclusive_scan(work, sm.tmp, &all);
-  // Tiles per unit.  Few sources: one unit per SM, of equal length (two shorter ones leave SMs idle in the second
-  // wave: a 20000-token beam of 8 KV heads in 256 units of 5 tiles took as long as 144 of 9 would in two waves).  More: half an
-  // SM's share at most, which the sorted list evens out.  Not too short ones, and no more records than there is room for.
-  const long long heads_work = (long long)all * v.Hkv;
-  int whole;
-  block_exclusive_scan((cnt > 0 ? (cnt + tokens - 1) / tokens : 0), sm.tmp, &whole);
-  const int waves = whole * v.Hkv < v.num_sms ? 1 : 2;
-  int per = max(least, (int)((heads_work + waves * v.num_sms - 1) / (waves * v.num_sms)));
-  int mine, base;
+  // Tiles per unit: half an SM's share at most, which the sorted list evens out, but not too short ones, and no more
+  // records than there is room for.
+  const int share = (few ? 1 : 2) * v.num_sms;
+  int per = max(least, (int)(((long long)all * v.Hkv + share - 1) / share));
+  for (; few; per += 1 + per / 8) {  // until the pieces fit too
+    int n = rows_b * ((tail + per - 1) / per);
+    for (int s = tid; s < nseg; s += kListThreads) {
+      int rows;
+      const int t = tiles_of(s, &rows);
+      n += rows * ((t + per - 1) / per);
+    }
+    block_exclusive_scan(n, sm.tmp, &all);
+    if ((long long)all * v.Hkv <= v.num_sms || per > (1 << 24)) break;
+  }
+  if (tid == 0) w.ctl[kDrFew] = few;
   for (;; per *= 2) {
     mine = cnt > 0 ? (tail + per - 1) / per : 0;
     for (int k = 0; k < nd; ++k) mine += (depth_tiles(k) + per - 1) / per;
@@ -459,9 +483,12 @@ struct DraftJob {
 
   __device__ __forceinline__ void error(int code) const { set_status(v.ctl, code); }
   struct Units {
-    int count;
-    __device__ __forceinline__ explicit Units(const DraftJob& j) : count(j.w.ctl[kDrUnits]) {}
+    int count, few;
+    __device__ __forceinline__ explicit Units(const DraftJob& j) : count(j.w.ctl[kDrUnits]), few(j.w.ctl[kDrFew]) {}
   };
+  // Which rows share a unit, and where it stands in the list, follows the order in which segments were found, which may
+  // differ from run to run: a row's result may not depend on it.  Where there are few units all of more than a tile are joint.
+  __device__ __forceinline__ bool joins(const Units& all) const { return all.few != 0; }
   __device__ __forceinline__ int total(const Units& all) const { return all.count * v.Hkv; }
   __device__ __forceinline__ int capacity() const { return w.max_units * v.Hkv; }
   // Words of a unit, those of its loads first.
@@ -1144,7 +1171,8 @@ extern "C" gb_status gb_draft_attention(gb_pool* pool, int layer, const gb_draft
   }
   if (layer == 0) {
     const int tokens = (bf16 ? 2 * flash::kRows : kTileRows) / v.G;
-    launch_pdl(k_draft_plan, 1, kListThreads, 0, s, v, w, d->parent_dev, d->count_dev, tokens, bf16 ? 2 : 1, bf16 && v.grouped);
+    launch_pdl(k_draft_plan, 1, kListThreads, 0, s, v, w, d->parent_dev, d->count_dev, tokens,
+               bf16 ? tokens / 2 : tokens, bf16 ? 2 : 1, bf16 && v.grouped);
     pool->launches += 1;
     if (v.max_beams > kOneLaunch) {
       launch_pdl(k_draft_rows, (v.max_beams + 7) / 8, 256, 0, s, v, w, d->parent_dev, d->count_dev);

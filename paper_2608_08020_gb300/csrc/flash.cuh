@@ -14,7 +14,8 @@
 //   first, second up to 128 rows: two units of the CTA's list, a group each, their tiles coming by turns
 //   joint         up to 128 rows and no second unit: the same rows in both groups, group g takes tiles g, g + 2, ...,
 //                 and their sums are joined at the end
-//   alone         the same with a single tile: group 0
+//   alone         the same with a single tile, or where the job does not allow joint units: group 0
+// A row's sum goes over the keys in the same order in every mode but joint.
 //
 // P is rounded to bf16 for the tensor core (relative 2^-9 each, independent, so a result's error
 // is about that of its own rounding to bf16); the sum l is of the unrounded values.
@@ -196,7 +197,7 @@ __device__ __forceinline__ void st32(void* p, const uint32_t* u) {
                : "memory");
 }
 // Whether a kernel of this pipeline has the registers at launch that its warps then share out.
-inline bool launches_with(const void* kernel) {
+inline bool launches_with(const void* kernel) try {
   static std::mutex mu;
   static std::set<std::pair<const void*, int>> fine;  // (kernel, device)
   int device = 0;
@@ -207,6 +208,8 @@ inline bool launches_with(const void* kernel) {
   if (cudaFuncGetAttributes(&a, kernel) != cudaSuccess || a.numRegs != kLaunchRegs) return false;
   fine.insert({kernel, device});
   return true;
+} catch (...) {
+  return false;
 }
 // A whole warp's wait_or_abort, whose lanes stay together.
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
@@ -386,30 +389,41 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
     bool alive = true;
     typename Job::Row row, row_y;
     // The group's next unit: its words stay in shared memory until the group is done with it.
-    auto next_unit = [&](int& slot) {
+    bool known = false;  // the next unit has been found (the same in a warp)
+    auto next_unit = [&](int& slot, bool patient) {
       for (;; ++u_next) {
         slot = u_next & (kSlots - 1);
-        if (!wait_or_abort(ctl + kBarSched + 8 * slot, (u_next / kSlots) & 1, abort_flag)) return false;
-        if (units[slot].nt < 0) return true;
+        const uint32_t bar = ctl + kBarSched + 8 * slot, parity = (u_next / kSlots) & 1;
+        if (!patient) {
+          if (!__all_sync(0xffffffffu, mbar_test(bar, parity))) return true;
+        } else if (!wait_or_abort(bar, parity, abort_flag)) {
+          return false;
+        }
+        if (units[slot].nt < 0) break;
         if (takes_part(units[slot].mode, g)) {
           ++u_next;
-          return true;
+          break;
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(ctl + kBarSchedFree + 8 * slot);
       }
+      known = true;
+      return true;
     };
     int sx = 0, sy = 0;
-    alive = next_unit(sx);
+    alive = next_unit(sx, true);
     if (alive && units[sx].nt >= 0) {
       job.find_row(units[sx], g, r, row);
       job.load_q(units[sx], g, r, sbase + g * kTile, ctl + kBarQ + 8 * g, row);
       job.loaded_q(r, ctl + kBarQ + 8 * g);
     }
-    // The group's last S of a unit is complete: the next unit's query rows may come.
-    auto begin_next = [&]() {
-      if (!next_unit(sy)) return false;
-      if (units[sy].nt >= 0) {
+    // The group's last S of a unit is complete: the next unit's query rows may come.  While P of that tile is due the
+    // group does not wait for the unit: where others without the group come first, it is made known only when they are
+    // loaded, to which the ring may need the stage of this tile's V.
+    auto begin_next = [&](bool patient) {
+      if (known) return true;
+      if (!next_unit(sy, patient)) return false;
+      if (known && units[sy].nt >= 0) {
         job.find_row(units[sy], g, r, row_y);
         job.load_q(units[sy], g, r, sbase + g * kTile, ctl + kBarQ + 8 * g, row_y);
       }
@@ -419,10 +433,11 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       const Unit& x = units[sx];
       const int mode = x.mode, mine = group_tiles(x.nt, mode, g);
       float m_ref = -INFINITY, l = 0.f;
+      known = false;
       for (int i = 0; i < mine; ++i, ++n) {
         const int t = group_tile(mode, g, i);
         if (!wait_or_abort(ctl + kBarS + 8 * g, n & 1, abort_flag)) { alive = false; break; }
-        if (Job::kEarlyQ && i + 1 == mine && !(alive = begin_next())) break;
+        if (Job::kEarlyQ && i + 1 == mine && !(alive = begin_next(false))) break;
         tc_fence_after();
         uint32_t su[128];
 #pragma unroll
@@ -492,7 +507,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
         l += l0 + l1;
       }
       if (!alive) break;
-      if (!Job::kEarlyQ && !(alive = begin_next())) break;
+      if (!(alive = begin_next(true))) break;
       if (units[sy].nt >= 0) job.loaded_q(r, ctl + kBarQ + 8 * g);
       // (m, l) go to the warps that write, once they have those of the group's unit before.
       if (c_done > 0 && !(alive = wait_or_abort(ctl + kBarOFree + 8 * g, (c_done - 1) & 1, abort_flag))) break;
@@ -551,7 +566,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       auto match = [&](Unit& p, Unit& q) {
         if (p.nt < 0 || p.mode == kDual) return false;
         if (q.nt < 0 || q.mode == kDual) {
-          if (p.nt == 1) p.mode = kAlone;
+          if (p.nt == 1 || !job.joins(all)) p.mode = kAlone;
           return false;
         }
         p.mode = kFirst;

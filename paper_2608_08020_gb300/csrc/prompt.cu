@@ -115,6 +115,7 @@ struct PromptJob : PromptView {
   using Units = PromptUnits;  // what the warp that takes the units holds
   __device__ __forceinline__ int total(const Units& all) const { return all.count * Hkv; }
   __device__ __forceinline__ int capacity() const { return most_units * Hkv; }
+  __device__ __forceinline__ bool joins(const Units&) const { return true; }  // (the list is the same each time)
   __device__ __forceinline__ void unit(const Units& all, int id, flash::Unit& x) const {
     const PromptUnit e = all(*this, id / Hkv);
     x.head = id % Hkv;
@@ -339,9 +340,10 @@ extern "C" gb_status gb_prompt_attention(const gb_prompt_args* a, gb_stream_t st
   if (cudaGetDevice(&device) != cudaSuccess ||
       cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess)
     return GB_ERR_CUDA;
+  if (a->num_seqs == 0) return GB_OK;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  const int G = a->num_q_heads / a->num_kv_heads, tokens = unit_tokens(a->dtype, G);
   int* ctl = static_cast<int*>(a->workspace);
+  const int G = a->num_q_heads / a->num_kv_heads, tokens = unit_tokens(a->dtype, G);
   // Few units (a short prompt): half the rows each, so that twice as many SMs have work and the longest ends sooner.  Up to
   // one and a half units per SM: 1300 tokens of 8 KV heads 25.5 -> 22.2 us, 1600 tokens 29.9 -> 27.7, but 2000 tokens 34.7 -> 36.1.
   const int few = a->dtype == GB_BF16 ? 3 * sms / (2 * a->num_kv_heads) : 0;

@@ -40,9 +40,10 @@ class DraftTrees:
 
     def attention(self, layer: int, q, k, v, parent, scale: float, out=None, count=None, stream=None):
         """One layer: q [max_beams][n_draft][q heads][D], k and v [max_beams][n_draft][kv heads][D], parent int32
-        [max_beams][n_draft] (-1: the context's end), count int32 [max_beams] (None: n_draft each); returns out, like q."""
+        [max_beams][n_draft] (-1: the context's end), count int32 [max_beams] (None: n_draft each); returns out, like q (a new
+        one belongs to `stream`, which then has to be a torch.cuda.Stream or None)."""
         if out is None:
-            out = torch.empty(self.q_shape, dtype=self.dtype, device=self.device)
+            out = B.new_on(stream, lambda: torch.empty(self.q_shape, dtype=self.dtype, device=self.device))
         qs, ks, dt, dev = self.q_shape, self.kv_shape, self.dtype, self.device
         if not (q.shape == qs and k.shape == ks and v.shape == ks and out.shape == qs and q.dtype is dt and k.dtype is dt
                 and v.dtype is dt and out.dtype is dt and q.is_contiguous() and k.is_contiguous() and v.is_contiguous()
@@ -61,7 +62,6 @@ class DraftTrees:
             self._check(name, x, (self.pool.cfg.num_layers, *self.kv_shape), self.dtype)
         self._check("accepted", accepted, self.kv_shape[:1], torch.int32)
         draft = self._draft(parent, count)
-        n = torch.empty_like(accepted)
-        path = torch.empty_like(parent)
+        n, path = B.new_on(stream, lambda: (torch.empty_like(accepted), torch.empty_like(parent)))
         B.gb_accept_draft(self.pool.handle, draft, k, v, accepted, n, path, stream)
         return n, path

@@ -18,7 +18,9 @@ class PromptAttention:
         self.num_q_heads, self.num_kv_heads, self.head_dim, self.dtype = num_q_heads, num_kv_heads, head_dim, dtype
         self.max_tokens, self.max_seqs = max_tokens, max_seqs
         n = B.gb_prompt_workspace_bytes(max_tokens, max_seqs, num_q_heads, num_kv_heads, head_dim, _DT[dtype])
-        self.workspace = torch.zeros(n, dtype=torch.uint8, device=torch.device(device))
+        self.workspace = torch.zeros(n, dtype=torch.uint8, device=torch.device(device))   # status: GB_OK
+        if not torch.cuda.is_current_stream_capturing():
+            torch.cuda.current_stream(self.workspace.device).synchronize()                # calls may be on any stream
         self.device, self.torch_dtype = self.workspace.device, TORCH_DT[dtype]
         # The call's arguments, but for what changes from call to call.
         self._args = B.GbPromptArgs(workspace=self.workspace.data_ptr(), workspace_bytes=n, num_q_heads=num_q_heads,
@@ -27,10 +29,13 @@ class PromptAttention:
     def __call__(self, q, k, v, cu_seqlens, scale: float, out=None, stream=None):
         """q [tokens][q heads][head_dim], k and v [tokens][kv heads][head_dim] (each token's heads contiguous, tokens
         at any stride), cu_seqlens int32 [seqs + 1]; returns out [tokens][q heads][head_dim] (new unless given; the
-        rows outside every sequence are left as they were)."""
+        rows outside every sequence are left as they were).  A new out belongs to `stream`, which then has to be a
+        torch.cuda.Stream or None."""
         n, seqs, d = q.shape[0], cu_seqlens.numel() - 1, self.head_dim
         if out is None:
-            out = torch.empty((n, self.num_q_heads, d), dtype=self.torch_dtype, device=self.device)
+            out = B.new_on(stream, lambda: torch.empty((n, self.num_q_heads, d), dtype=self.torch_dtype, device=self.device))
+        if B.current_device() != self.device.index:
+            raise ValueError(f"the current device is not the workspace's, {self.device}")
         if n > self.max_tokens or not 0 <= seqs <= self.max_seqs:
             raise ValueError(f"{n} tokens in {seqs} sequences, the workspace holds {self.max_tokens} in {self.max_seqs}")
         a = self._args
@@ -56,4 +61,5 @@ class PromptAttention:
         return x.data_ptr(), token if n > 1 else heads * d
 
     def status(self, stream=None) -> int:
+        """Device status of the last call (synchronises)."""
         return B.gb_prompt_status(self.workspace, stream)

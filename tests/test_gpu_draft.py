@@ -548,3 +548,59 @@ def test_refusals(cuda):
         u.attention(0, q, k[0], v[0], parent, 0.1)
     with pytest.raises(B.GambitError, match="GB_ERR_STATE"):
         pool.truncate(acc)
+
+
+@pytest.mark.parametrize("beams,hq,hkv,t", [(3, 8, 2, 6), (40, 16, 2, 16), (24, 32, 8, 9)])
+def test_the_same_each_time(cuda, beams, hq, hkv, t):
+    """Segments are found in an order that may differ; the results may not."""
+    import torch
+    from paper_2608_08020_gb300.draft import DraftTrees
+    x = Trees("bf16", hq=hq, hkv=hkv, slots=beams, beams=beams, prompt=300, room=80, seed=9)
+    trees = DraftTrees(x.pool, t)
+    for n in (130, 200, 77):
+        x.append(n)
+        x.fork([b if b % 3 else (b + 1) % beams if (b + 1) % 3 else b for b in range(beams)])
+    x.append(50)
+    parent, count = x.trees(t, True)
+    q, k, v = x.rand(beams, t, hq, 128), x.rand(beams, t, hkv, 128), x.rand(beams, t, hkv, 128)
+    out = None
+    for _ in range(12):
+        got = trees.attention(0, q, k, v, x.ints(parent), x.scale, count=x.ints(count))
+        assert out is None or torch.equal(got, out)
+        out = got
+        x.fork(list(range(beams)))       # nothing moves, the segments are found again
+    assert x.pool.status() == 0
+
+
+@pytest.mark.parametrize("long,short,beams", [(1200, 40, 1000), (1200, 130, 1000), (700, 10, 935), (0, 0, 900), (0, 0, 1024)])
+def test_units_of_unequal_lengths(cuda, long, short, beams):
+    """Five long beams to an SM, then short ones: pairs whose halves differ, single units behind them (0: lengths drawn)."""
+    import torch
+    from paper_2608_08020_gb300.draft import DraftTrees
+    sms, t, room = torch.cuda.get_device_properties(0).multi_processor_count, 8, max(long, 600)
+    x = Trees("bf16", hq=8, hkv=1, slots=beams, beams=beams, prompt=1, room=room // 16 + 2, seed=beams)
+    trees = DraftTrees(x.pool, t)
+    k, v = x.rand(room, beams, 1, 128), x.rand(room, beams, 1, 128)
+    x.pool.append_kv(0, room, k, v)
+    lengths = np.where(np.arange(beams) < 5 * sms, long, short) if long else x.rng.integers(0, room, beams)
+    x.pool.truncate(x.ints(lengths + 1))
+    q, dk, dv = x.rand(beams, t, 8, 128), x.rand(beams, t, 1, 128), x.rand(beams, t, 1, 128)
+    parent = np.tile(np.arange(t) - 1, (beams, 1))
+    parent[::2, 3] = 0
+    out = trees.attention(0, q, dk, dv, x.ints(parent), x.scale)
+    assert x.pool.status() == 0
+    assert torch.equal(out, trees.attention(0, q, dk, dv, x.ints(parent), x.scale))
+    sees = torch.zeros(beams, t, 1 + room + t, dtype=torch.bool, device="cuda")
+    sees[:, :, 1:1 + room] = (torch.arange(room, device="cuda") < torch.tensor(lengths, device="cuda")[:, None])[:, None]
+    sees[:, :, 0] = True
+    for kind in (0, 1):
+        sees[kind::2, :, 1 + room:] = seen(parent[kind], 0)
+    for b in range(0, beams, 100):
+        at = slice(b, min(b + 100, beams))
+        K, V = (torch.cat([c[0].expand(at.stop - b, -1, -1, -1), y[:, at].transpose(0, 1), d[at]], 1).double()[:, :, 0]
+                for c, y, d in zip(x.ctx[0], (k, v), (dk, dv)))
+        p = torch.einsum("bthd,bkd->bthk", q[at].double(), K) * x.scale
+        p = torch.softmax(p.masked_fill(~sees[at, :, None], -math.inf), -1)
+        o, a = torch.einsum("bthk,bkd->bthd", p, V), torch.einsum("bthk,bkd->bthd", p, V.abs())
+        err = (out[at].double() - o).abs()
+        assert bool((err <= bound(o, a, "bf16")).all()), (b, float((err / bound(o, a, "bf16")).max()))

@@ -198,3 +198,52 @@ def test_units_of_one_tile_in_a_row(cuda):
     for _ in range(200):
         out = op(q, k, v, at, 0.1)
     assert torch.equal(out, first) and op.status() == 0
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_no_sequence_and_empty_ones(cuda, dtype):
+    run(dtype, [], 4, 2, pad=7)
+    run(dtype, [0], 4, 2, pad=7)
+    run(dtype, [0, 0, 0], 4, 2, pad=300)
+    run(dtype, [5], 4, 2, pad=300)
+    run(dtype, [], 4, 2)
+
+
+def test_one_bad_sequence(cuda):
+    import torch
+    from paper_2608_08020_gb300 import binding as B
+    from paper_2608_08020_gb300.prompt import PromptAttention
+    for dtype in ("bf16", "f32"):
+        q, k, v = make(dtype, 200, 4, 2, 14)
+        op = PromptAttention(4, 2, q.shape[2], dtype, max_tokens=200, max_seqs=1)
+        assert op.status() == 0
+        out = torch.full_like(q, 7.0)
+        for cu, code in (([0, 201], "GB_ERR_INVALID"), ([10, 5], "GB_ERR_INVALID"), ([-1, 100], "GB_ERR_INVALID"), ([3, 3], "GB_OK")):
+            op(q, k, v, torch.tensor(cu, dtype=torch.int32, device="cuda"), 0.1, out)
+            assert B.STATUS_NAMES[op.status()] == code and bool((out == 7).all()), (dtype, cu)
+        op(q, k, v, torch.tensor([50, 200], dtype=torch.int32, device="cuda"), 0.1, out)   # not from the first row
+        o, a = attend(q, k, v, [50, 200], 0.1)
+        assert op.status() == 0 and bool((out[:50] == 7).all())
+        assert bool(((out.double() - o).abs() <= bound(o, a, dtype))[50:].all())
+
+
+def test_the_same_each_time(cuda):
+    """Lists of many units of one length: the same bits from every call, on any stream, with a new output."""
+    import torch
+    from paper_2608_08020_gb300.prompt import PromptAttention
+    lengths = [37 * (1 + i % 9) for i in range(70)]
+    cu = [0]
+    for n in lengths:
+        cu.append(cu[-1] + n)
+    q, k, v = make("bf16", cu[-1], 8, 2, 15)
+    op = PromptAttention(8, 2, 128, "bf16", max_tokens=cu[-1], max_seqs=70)
+    at = torch.tensor(cu, dtype=torch.int32, device="cuda")
+    first = op(q, k, v, at, 0.1)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for _ in range(20):
+        out = op(q, k, v, at, 0.1, stream=side)
+        side.synchronize()
+        assert torch.equal(out, first)
+    with pytest.raises(ValueError):
+        op(q, k, v, at, 0.1, stream=side.cuda_stream)
