@@ -500,12 +500,13 @@ gb_status gb_scorer_step(gb_pool* step_pool, const gb_scorer_config* cfg, const 
  *   num_tokens:    rows of q, k, v and out; rows outside every sequence are left as they were
  *   workspace:     gb_prompt_workspace_bytes, 256-byte aligned; calls using one workspace must be ordered
  * Values in rows a query does not see (later tokens, other sequences) do not reach its result, whatever
- * they are.  Two launches: a planner that lists the work longest first, and the attention.
+ * they are.  Launches: the attention, and before it, unless num_seqs is 1, a planner that lists the work longest first;
+ * none, and the status stays, without tokens or sequences.
  * Errors: GB_ERR_INVALID for bad sizes, alignment, strides, overlap, a workspace that is too small or a
  * scale that is not positive and finite; GB_ERR_UNSUPPORTED unless (dtype, head_dim) is (GB_BF16, 128)
  * or (GB_F32, 64) and G one of 1, 2, 4, 8, 16; GB_ERR_TOO_LARGE when the work list passes 2^31 entries.  A
- * sequence whose bounds are out of order or range is not computed and recorded as GB_ERR_INVALID
- * in the workspace's status (gb_prompt_status).
+ * sequence whose bounds are out of range, out of order or before an earlier sequence's is not computed and
+ * recorded as GB_ERR_INVALID in the workspace's status (gb_prompt_status).
  */
 typedef struct {
   const void* q;
@@ -573,8 +574,9 @@ gb_status gb_draft_workspace_bytes(gb_pool* pool, int n_draft, size_t* bytes);
  * count on are zero in out_dev and ignored in the inputs; values that a row does not see do not reach its
  * result, whatever they are.  The pool's contexts are not changed.
  * Layer 0 plans the round; the other layers may follow in any order, and again, until the pool changes
- * (append, decode, accept, truncate, fork, prune, release).  Launches: the attention and the join of its partial
- * results, for layer 0 the planner first.
+ * (append, decode, accept, truncate, fork, prune, release); a plan captured into a graph serves that capture's calls.
+ * Results are the same from call to call.  Launches: the attention and the join of its partial results, for layer 0 the
+ * planner first (two launches in pools of more than 16 slots).
  * Errors: GB_ERR_INVALID for bad sizes, pointers or a scale that is not positive and finite; GB_ERR_STATE for an unseeded pool,
  * inside an open step, a layer above 0 without a plan, or when the pool is on another device than the current one.
  */
@@ -604,7 +606,8 @@ gb_status gb_accept_draft(gb_pool* pool, const gb_draft* draft, const void* k_de
  * tokens, to 0 at least.  Rewinds a trace to an earlier thought boundary, or takes accepted tokens back.
  * A slot cut inside a page that other slots hold gets its own copy of the page's rows (every layer; the lowest
  * free page, slots ascending); where all of a page's holders are cut inside it the last one keeps it.
- * Running means are left.  Errors: GB_ERR_STATE for an unseeded pool, an open step or another device; a length above
+ * Running means are left.  Three launches, the last one empty unless a shared-prefix segment was cut into.
+ * Errors: GB_ERR_STATE for an unseeded pool, an open step or another device; a length above
  * the slot's records GB_ERR_INVALID in the device status and leaves the slot; GB_ERR_OOM is recorded, and nothing cut,
  * unless the pool has a free page before the call for every slot cut inside a page that then has several holders.
  */

@@ -5,8 +5,8 @@
 // where j runs over beam b's context (through its block table) and over i and its ancestors in the beam's
 // tree, whose keys and values are the caller's.
 //
-// A round's plan, made with layer 0: every shared-prefix segment's pages are read once for all drafted
-// tokens of the beams that share them (rows (beam, token, query head), 256 to a unit), every beam's remainder
+// A round's plan, made with layer 0: every shared-prefix segment's pages, down to the depth that pays, are read once for
+// all drafted tokens of the beams that share them (rows (beam, token, query head), up to 256 to a unit), every beam's remainder
 // and its drafts by units of its own; long runs of keys are split.  A beam whose rows one unit answers gets
 // its result from it; the others' units leave records (sum, maximum, row sum) that k_draft_merge joins.
 // bf16: flash.cuh; fp32: tile.cuh, without segments.
@@ -219,13 +219,14 @@ __device__ __forceinline__ void draft_rows(const PoolView& v, const DraftView& w
     }
   }
 }
-// The work list (one CTA).  `tokens`: of a unit's rows, `small`: where there are few units; `least`: tiles below which a run of keys is not split.
+// The work list (one CTA).  `tokens`: of a unit's rows, `small`: where there are few units; `least`: tiles below which a run of keys is not split;
+// `coarse`: bits dropped from the costs, so that their sums stay in range.
 //
 // Down to which depth the shared segments are used is chosen by the cost above: a segment's unit reads
 // its pages once for up to 256 rows, but every piece of a beam's context beyond the first costs a record.  64 beams of 50 rows
 // over 64 shared and 130 own tokens run without segments; 64 beams of 50 rows at 4000 tokens use them all.
 __global__ void __launch_bounds__(kListThreads) k_draft_plan(PoolView v, DraftView w, const int* parent, const int* count,
-                                                             int tokens, int small, int least, bool segs) {
+                                                             int tokens, int small, int least, int coarse, bool segs) {
   pdl_wait();
   pdl_launch_dependents();
   constexpr int kCached = 4096;         // segments whose rows and tiles fit in shared memory
@@ -268,7 +269,7 @@ __global__ void __launch_bounds__(kListThreads) k_draft_plan(PoolView v, DraftVi
   auto seg_tiles = [&](int s) { return (v.seg_len[s] * v.P + flash::kTok - 1) / flash::kTok; };
   auto unit_cost = [&](int rows, int tiles, int rec) {  // of `rows` tokens over `tiles` tiles
     const int full = rows / tokens, rest = rows - full * tokens, halves = 2 * full + (rest > 0) + (2 * rest > tokens);
-    return halves * (tiles * kTileCost + kUnitCost + rec);
+    return (int)((long long)halves * (tiles * kTileCost + kUnitCost + rec) >> coarse);
   };
   // Cost of the beams' own units by depth, for the beams that reach it; then the segments'.
   {
@@ -1143,9 +1144,15 @@ extern "C" gb_status gb_draft_attention(gb_pool* pool, int layer, const gb_draft
   if (bf16 && !flash::launches_with(reinterpret_cast<const void*>(k_draft)))
     return fail(pool, GB_ERR_UNSUPPORTED, "draft: the kernel's registers");
   if (bf16 && !pool->have_tmap) return fail(pool, GB_ERR_UNSUPPORTED, "draft: no tensor map over the pool");
-  if (layer > 0 && (pool->draft_epoch != pool->epoch || pool->draft_ws != d->workspace_dev || pool->draft_tokens != T))
-    return fail(pool, GB_ERR_STATE, "draft: layer 0 plans the round, on the pool as it is and in this workspace");
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  // A captured plan is made when its graph runs: it serves the calls of the same capture only.
+  cudaStreamCaptureStatus capturing = cudaStreamCaptureStatusNone;
+  unsigned long long capture = 0;
+  if (cudaStreamGetCaptureInfo(s, &capturing, &capture) != cudaSuccess) return check_launch(pool, "draft: capture");
+  if (capturing != cudaStreamCaptureStatusActive) capture = 0;
+  if (layer > 0 && (pool->draft_epoch != pool->epoch || pool->draft_ws != d->workspace_dev || pool->draft_tokens != T ||
+                    pool->draft_capture != capture))
+    return fail(pool, GB_ERR_STATE, "draft: layer 0 plans the round, on the pool as it is, in this workspace and graph");
   const DraftView w = draft_view(pool, draft_layout(pool->cfg, pool->num_sms, T), T, d->workspace_dev);
   const float qscale = scale * 1.4426950408889634f;
   DraftJob job;
@@ -1171,8 +1178,11 @@ extern "C" gb_status gb_draft_attention(gb_pool* pool, int layer, const gb_draft
   }
   if (layer == 0) {
     const int tokens = (bf16 ? 2 * flash::kRows : kTileRows) / v.G;
+    const long long dearest = 2ll * v.max_beams * ((T + tokens - 1) / tokens) * (kTileCost * ((long long)v.max_pages * v.P / flash::kTok + 2) + kUnitCost + kRecCost);
+    int coarse = 0;
+    while (dearest >> coarse >= 1 << 28) ++coarse;
     launch_pdl(k_draft_plan, 1, kListThreads, 0, s, v, w, d->parent_dev, d->count_dev, tokens,
-               bf16 ? tokens / 2 : tokens, bf16 ? 2 : 1, bf16 && v.grouped);
+               bf16 ? tokens / 2 : tokens, bf16 ? 2 : 1, coarse, bf16 && v.grouped);
     pool->launches += 1;
     if (v.max_beams > kOneLaunch) {
       launch_pdl(k_draft_rows, (v.max_beams + 7) / 8, 256, 0, s, v, w, d->parent_dev, d->count_dev);
@@ -1182,6 +1192,7 @@ extern "C" gb_status gb_draft_attention(gb_pool* pool, int layer, const gb_draft
     pool->draft_epoch = pool->epoch;
     pool->draft_ws = d->workspace_dev;
     pool->draft_tokens = T;
+    pool->draft_capture = capture;
   }
   cudaError_t e;
   const dim3 merge(T, v.max_beams, (long long)T * v.max_beams < 2 * pool->num_sms ? (v.Hq + 7) / 8 : 1);

@@ -350,6 +350,7 @@ struct gb_pool {
   int tmap_oob = 0;                          // first row group past the tensor map (loads zeros)
   std::string last_error;
   unsigned long long epoch = 0;             // calls that changed the beams' contexts
+  unsigned long long draft_capture = 0;     // the graph capture it belongs to, 0: none
   unsigned long long draft_epoch = ~0ull;   // the epoch, workspace and tree size of the round planned last
   const void* draft_ws = nullptr;
   int draft_tokens = 0;

@@ -5,8 +5,8 @@
 // by token, so a tile of 128 rows has 128 / G tokens and all G heads that read the same K and V.
 //
 // Bound by the tensor cores from a few hundred tokens on (2 D Hq n^2 flops against 4 D (Hq + Hkv) n bytes).
-// A planner CTA lists the units (sequence, run of tokens), longest first; a CTA per SM takes (unit, KV head)
-// from a counter.  bf16: flash.cuh; fp32: tile.cuh.
+// A planner CTA lists the units (sequence, run of tokens), longest first; a CTA per SM takes its (unit, KV head) pairs
+// in turn.  One prompt's units need no list.  bf16: flash.cuh; fp32: tile.cuh.
 #include <algorithm>
 #include <mutex>
 
@@ -17,7 +17,7 @@
 namespace gb {
 namespace {
 
-// Workspace: control words, then the units.
+// Workspace: control words, the units, then a word per sequence.
 enum PromptCtl : int { kPrStatus = 0, kPrUnits = 1, kPrWords = 64 };
 
 struct PromptUnit {
@@ -25,39 +25,53 @@ struct PromptUnit {
   int t0, ntok;     // its tokens [t0, t0 + ntok)
 };
 
-// Tokens per unit: the most rows a unit of the kernel holds.
+// `tokens` of a unit, or where that makes `few` units at most `small_tokens`.  lens: a word per sequence, used only when some
+// bounds are out of order or range: then a sequence counts if its own bounds are in range, in order and not before an
+// earlier one that is in range, so no row belongs to two and the list has room for all units.
 __global__ void __launch_bounds__(kListThreads) k_prompt_plan(const int* cu, int num_seqs, int num_tokens, int tokens,
-                                                              int small_tokens, int few, int max_units, int* ctl) {
+                                                              int small_tokens, int few, int max_units, int* ctl, int* lens) {
   pdl_wait();
   pdl_launch_dependents();
   __shared__ ListSmem sm;
   PromptUnit* units = reinterpret_cast<PromptUnit*>(ctl + kPrWords);
-  auto length = [&](int s) {
-    const int a = cu[s], e = cu[s + 1];
-    return a >= 0 && a <= e && e <= num_tokens ? e - a : -1;
-  };
-  if (threadIdx.x == 0) ctl[kPrStatus] = GB_OK;
-  __syncthreads();
-  int mine = 0;
+  const int tid = threadIdx.x, lane = tid & 31;
+  auto in_range = [&](int x) { return x >= 0 && x <= num_tokens; };
   bool bad = false;
-  for (int s = threadIdx.x; s < num_seqs; s += kListThreads) {
-    const int n = length(s);
-    bad |= n < 0;
-    mine += n > 0 ? (n + tokens - 1) / tokens : 0;
+  for (int s = tid; s < num_seqs; s += kListThreads) bad |= !in_range(cu[s]) || !in_range(cu[s + 1]) || cu[s] > cu[s + 1];
+  bad = __syncthreads_or(bad);
+  if (tid == 0) ctl[kPrStatus] = bad ? GB_ERR_INVALID : GB_OK;
+  for (int base = 0, top = 0; bad && base < num_seqs; base += kListThreads) {  // top: the highest bound so far
+    const int s = base + tid, x = s < num_seqs && in_range(cu[s]) ? cu[s] : 0;
+    int high = max(x, top);  // of the bounds up to this one
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, high, o);
+      if (lane >= o) high = max(high, y);
+    }
+    if (lane == 31) sm.tmp[tid >> 5] = high;
+    __syncthreads();
+    for (int w = 0; w < tid >> 5; ++w) high = max(high, sm.tmp[w]);
+    if (s < num_seqs) lens[s] = in_range(cu[s]) && in_range(cu[s + 1]) && cu[s] >= high ? max(cu[s + 1] - cu[s], 0) : 0;
+    __syncthreads();
+    if (tid == kListThreads - 1) sm.tmp[0] = high;
+    __syncthreads();
+    top = sm.tmp[0];
+    __syncthreads();
   }
-  int all;
+  auto length = [&](int s) { return bad ? lens[s] : cu[s + 1] - cu[s]; };
+  int mine = 0, all;
+  for (int s = tid; s < num_seqs; s += kListThreads) mine += (length(s) + tokens - 1) / tokens;
   block_exclusive_scan(mine, sm.tmp, &all);
-  if (bad) ctl[kPrStatus] = GB_ERR_INVALID;
   const int per = all <= few ? small_tokens : tokens;
   const int n = emit_sorted(
-      sm, num_seqs, [&](int s) { return (max(length(s), 0) + per - 1) / per; },
+      sm, num_seqs, [&](int s) { return (length(s) + per - 1) / per; },
       [&](int s, int i) { return (min((i + 1) * per, length(s)) + flash::kTok - 1) / flash::kTok; },
       [&](int s, int i, int at) {
         if (at >= max_units) return;
         const int len = length(s);
         units[at] = {cu[s], len, i * per, min(per, len - i * per)};
       });
-  if (threadIdx.x == 0) ctl[kPrUnits] = min(n, max_units);
+  if (tid == 0) ctl[kPrUnits] = min(n, max_units);
 }
 
 struct PromptView {
@@ -298,7 +312,7 @@ extern "C" gb_status gb_prompt_workspace_bytes(int num_tokens, int num_seqs, int
   if (!shape_ok(dtype, head_dim, num_q_heads, num_kv_heads)) return GB_ERR_UNSUPPORTED;
   const long long n = max_units(dtype, num_q_heads / num_kv_heads, num_tokens, num_seqs);
   if (n * num_kv_heads >= (1ll << 31)) return GB_ERR_TOO_LARGE;
-  *bytes = (size_t)(kPrWords * sizeof(int) + n * sizeof(PromptUnit) + 255) & ~(size_t)255;
+  *bytes = (size_t)(kPrWords * sizeof(int) + n * sizeof(PromptUnit) + num_seqs * sizeof(int) + 255) & ~(size_t)255;
   return GB_OK;
 }
 
@@ -370,7 +384,8 @@ extern "C" gb_status gb_prompt_attention(const gb_prompt_args* a, gb_stream_t st
   }
   if (a->num_seqs != 1 &&
       launch_pdl(k_prompt_plan, 1, kListThreads, 0, s, a->cu_seqlens, a->num_seqs, a->num_tokens, tokens,
-                 view.small_tokens, few, (int)most, ctl) != cudaSuccess)
+                 view.small_tokens, few, (int)most, ctl,
+                 reinterpret_cast<int*>(reinterpret_cast<PromptUnit*>(ctl + kPrWords) + most)) != cudaSuccess)
     return GB_ERR_CUDA;
   cudaError_t e;
   if (a->dtype == GB_BF16) {

@@ -1,6 +1,5 @@
 // Sorted work lists built by one CTA: the units of many sources (sequences, shared segments, beams)
-// in descending order of cost, so that units handed out from a counter make a
-// longest-processing-time-first schedule.
+// in descending order of cost, so that taken in turn they make even shares, the longest begun first.
 #pragma once
 #include "internal.cuh"
 

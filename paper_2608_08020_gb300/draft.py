@@ -20,6 +20,8 @@ class DraftTrees:
         c = pool.cfg
         n = B.gb_draft_workspace_bytes(pool.handle, n_draft)
         self.workspace = torch.empty(n, dtype=torch.uint8, device=pool.kv.device)
+        if not torch.cuda.is_current_stream_capturing():   # whatever had this memory before is done: calls may be on any stream
+            torch.cuda.current_stream(pool.kv.device).synchronize()
         self.device = self.workspace.device
         self._args = B.GbDraft(workspace_dev=self.workspace.data_ptr(), workspace_bytes=n, n_draft=n_draft)
         self.dtype = TORCH_DT[pool.kv_dtype]

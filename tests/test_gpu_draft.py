@@ -604,3 +604,65 @@ def test_units_of_unequal_lengths(cuda, long, short, beams):
         o, a = torch.einsum("bthk,bkd->bthd", p, V), torch.einsum("bthk,bkd->bthd", p, V.abs())
         err = (out[at].double() - o).abs()
         assert bool((err <= bound(o, a, "bf16")).all()), (b, float((err / bound(o, a, "bf16")).max()))
+
+
+def test_a_captured_plan_stays_in_its_graph(cuda):
+    import torch
+    from paper_2608_08020_gb300 import binding as B
+    from paper_2608_08020_gb300.draft import DraftTrees
+    x = Trees("bf16", layers=2, seed=4)
+    trees = DraftTrees(x.pool, 4)
+    q, k, v = x.rand(x.slots, 4, x.hq, x.d), x.rand(x.slots, 4, x.hkv, x.d), x.rand(x.slots, 4, x.hkv, x.d)
+    parent, out = x.ints([[-1, 0, 1, 2]] * x.slots), x.rand(x.slots, 4, x.hq, x.d)
+    want = [trees.attention(layer, q, k, v, parent, x.scale) for layer in (0, 1)]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        with pytest.raises(B.GambitError, match="GB_ERR_STATE"):
+            trees.attention(1, q, k, v, parent, x.scale, out)
+        trees.attention(0, q, k, v, parent, x.scale, out)
+        trees.attention(1, q, k, v, parent, x.scale, out)
+    with pytest.raises(B.GambitError, match="GB_ERR_STATE"):
+        trees.attention(1, q, k, v, parent, x.scale, out)
+    graph.replay()
+    assert torch.equal(out, want[1])
+    assert torch.equal(trees.attention(0, q, k, v, parent, x.scale), want[0])
+    assert x.pool.status() == 0
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_the_largest_pool(cuda, dtype):
+    """1024 slots of 64 drafted tokens, tables of millions of tokens: sizes at which sums of the plan's costs are kept in range,
+    lists are not staged and trees do not fit in shared memory."""
+    from paper_2608_08020_gb300.draft import DraftTrees
+    x = Trees(dtype, hq=8, hkv=1, page=16, slots=1024, beams=1000, prompt=30, room=70000, pages=16000, seed=7)
+    trees = DraftTrees(x.pool, 64)
+    x.append(5)
+    x.fork([s if s % 7 else s + 3 for s in range(994)] + list(range(994, 1000)) + [1 + 7 * (s % 5) for s in range(24)])
+    x.append(3)
+    rnd = x.attention(trees, 64)
+    x.accept(trees, rnd, x.pick(rnd))
+    assert x.pool.status() == 0
+    x.same_pages()
+
+
+def test_streams(cuda):
+    """New results belong to the stream of the call; a raw stream needs them given."""
+    import torch
+    from paper_2608_08020_gb300.draft import DraftTrees
+    x = Trees("bf16", seed=4)
+    trees = DraftTrees(x.pool, 4)
+    q, k, v = x.rand(x.slots, 4, x.hq, x.d), x.rand(x.slots, 4, x.hkv, x.d), x.rand(1, x.slots, 4, x.hkv, x.d)
+    parent, acc = x.ints([[-1, 0, 1, 2]] * x.slots), x.ints([2] * x.slots)
+    want = trees.attention(0, q, k, v[0], parent, x.scale)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = [trees.attention(0, q, k, v[0], parent, x.scale, stream=side) for _ in range(5)]
+    n, path = trees.accept(v, v, parent, acc, stream=side)
+    side.synchronize()
+    assert all(torch.equal(y, want) for y in got)
+    assert n.tolist() == [3] * 4 + [0] * 2 and path.tolist() == [[0, 1, 2, -1]] * 4 + [[-1] * 4] * 2
+    for call in (lambda s: trees.attention(0, q, k, v[0], parent, x.scale, stream=s), lambda s: trees.accept(v, v, parent, acc, stream=s)):
+        with pytest.raises(ValueError):
+            call(side.cuda_stream)
+    assert x.pool.status() == 0

@@ -247,3 +247,30 @@ def test_the_same_each_time(cuda):
         assert torch.equal(out, first)
     with pytest.raises(ValueError):
         op(q, k, v, at, 0.1, stream=side.cuda_stream)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_bounds_that_name_rows_again(cuda, dtype):
+    """Sequences that begin before an earlier one's end are left out, thousands of them too."""
+    import torch
+    from paper_2608_08020_gb300 import binding as B
+    from paper_2608_08020_gb300.prompt import PromptAttention
+    q, k, v = make(dtype, 2000, 4, 2, 16)
+    op = PromptAttention(4, 2, q.shape[2], dtype, max_tokens=2000, max_seqs=200000)
+    out = torch.full_like(q, 7.0)
+    op(q, k, v, torch.tensor([0, 2000] * 100000, dtype=torch.int32, device="cuda"), 0.1, out)
+    assert B.STATUS_NAMES[op.status()] == "GB_ERR_INVALID"
+    o, a = attend(q, k, v, [0, 2000], 0.1)
+    assert bool(((out.double() - o).abs() <= bound(o, a, dtype)).all())
+    op(q, k, v, torch.tensor([0, 2000, 1000, 1500], dtype=torch.int32, device="cuda"), 0.1, out)
+    assert B.STATUS_NAMES[op.status()] == "GB_ERR_INVALID"
+    assert bool(((out.double() - o).abs() <= bound(o, a, dtype)).all())
+    cu = [-1, 0] + [2 * i // 3 for i in range(1500)] + [9999, 500, 1000, 1200, 1100, 1150, 1200, 2000]   # ... 999, then past the end
+    out.fill_(7.0)
+    op(q, k, v, torch.tensor(cu, dtype=torch.int32, device="cuda"), 0.1, out)
+    assert B.STATUS_NAMES[op.status()] == "GB_ERR_INVALID"
+    o, a = attend(q, k, v, sorted({2 * i // 3 for i in range(1500)}), 0.1)
+    fine = (out.double() - o).abs() <= bound(o, a, dtype)
+    assert bool(fine[:999].all()) and bool((out[999] == 7).all())
+    o, a = attend(q, k, v, [1000, 1200, 2000], 0.1)
+    assert bool(((out.double() - o).abs() <= bound(o, a, dtype))[1000:].all())
