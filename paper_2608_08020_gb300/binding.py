@@ -137,37 +137,38 @@ def load(path: Path | None = None) -> ctypes.CDLL:
 
 def ptr(x) -> int | None:
     """Device address of a tensor / int, or None."""
-    if x is None:
-        return None
-    if isinstance(x, int):
+    if x is None or isinstance(x, int):
         return x
     return x.data_ptr()
 
 
 _torch = None         # the torch module once it has been imported
 _raw_stream = None    # () -> cudaStream_t of the current torch stream
+_device = None        # () -> index of the current torch device
 
 
 def _bind_torch(torch) -> None:
     """Pick the cheapest way to the current stream: the raw-handle query where torch has it (0.3 us a
     call; building a torch.cuda.Stream object costs 3 us, as much as the library call itself)."""
-    global _torch, _raw_stream
+    global _torch, _raw_stream, _device
     get_raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
     get_device = getattr(torch._C, "_cuda_getDevice", None)
     if get_raw is not None and get_device is not None:
         _raw_stream = lambda: get_raw(get_device())  # noqa: E731
     else:
         _raw_stream = lambda: torch.cuda.current_stream().cuda_stream  # noqa: E731
+    _device = get_device or torch.cuda.current_device
     _torch = torch
 
 
-def current_device() -> int:
-    """Index of the current torch device."""
+def stream_on(device: int, s) -> int | None:
+    """stream_handle, for work that belongs on device `device`: refused when another one is current."""
     if _torch is None:
         import torch
         _bind_torch(torch)
-    get = getattr(_torch._C, "_cuda_getDevice", None)
-    return get() if get is not None else _torch.cuda.current_device()
+    if _device() != device:
+        raise ValueError(f"the current device is {_device()}, the workspace is on {device}")
+    return _raw_stream() if s is None else s if isinstance(s, int) else s.cuda_stream
 
 
 def new_on(stream, make):
@@ -371,8 +372,11 @@ def gb_prompt_workspace_bytes(num_tokens: int, num_seqs: int, num_q_heads: int, 
     return n.value
 
 
-def gb_prompt_attention(args: GbPromptArgs, stream=None) -> None:
-    _check(None, load().gb_prompt_attention(ctypes.byref(args), stream_handle(stream)), "gb_prompt_attention")
+def gb_prompt_attention(args: GbPromptArgs, stream=None, device: int | None = None) -> None:
+    """`device`: refuse when it is not the current one."""
+    code = load().gb_prompt_attention(ctypes.byref(args), stream_handle(stream) if device is None else stream_on(device, stream))
+    if code:
+        _check(None, code, "gb_prompt_attention")
 
 
 def gb_prompt_status(workspace, stream=None) -> int:
@@ -389,8 +393,9 @@ def gb_draft_workspace_bytes(pool: int, n_draft: int) -> int:
 
 
 def gb_draft_attention(pool: int, layer: int, draft: GbDraft, q, k, v, scale: float, out, stream=None) -> None:
-    _check(pool, load().gb_draft_attention(pool, layer, ctypes.byref(draft), ptr(q), ptr(k), ptr(v), float(scale),
-                                           ptr(out), stream_handle(stream)), "gb_draft_attention")
+    code = load().gb_draft_attention(pool, layer, ctypes.byref(draft), ptr(q), ptr(k), ptr(v), scale, ptr(out), stream_handle(stream))
+    if code:
+        _check(pool, code, "gb_draft_attention")
 
 
 def gb_accept_draft(pool: int, draft: GbDraft, k, v, accepted, count_out=None, path_out=None, stream=None) -> None:

@@ -22,6 +22,7 @@ class PromptAttention:
         if not torch.cuda.is_current_stream_capturing():
             torch.cuda.current_stream(self.workspace.device).synchronize()                # calls may be on any stream
         self.device, self.torch_dtype = self.workspace.device, TORCH_DT[dtype]
+        self._index = self.device.index
         # The call's arguments, but for what changes from call to call.
         self._args = B.GbPromptArgs(workspace=self.workspace.data_ptr(), workspace_bytes=n, num_q_heads=num_q_heads,
                                     num_kv_heads=num_kv_heads, head_dim=head_dim, dtype=_DT[dtype])
@@ -31,11 +32,9 @@ class PromptAttention:
         at any stride), cu_seqlens int32 [seqs + 1]; returns out [tokens][q heads][head_dim] (new unless given; the
         rows outside every sequence are left as they were).  A new out belongs to `stream`, which then has to be a
         torch.cuda.Stream or None."""
-        n, seqs, d = q.shape[0], cu_seqlens.numel() - 1, self.head_dim
+        n, seqs = q.shape[0], cu_seqlens.numel() - 1
         if out is None:
-            out = B.new_on(stream, lambda: torch.empty((n, self.num_q_heads, d), dtype=self.torch_dtype, device=self.device))
-        if B.current_device() != self.device.index:
-            raise ValueError(f"the current device is not the workspace's, {self.device}")
+            out = torch.empty_like(q) if stream is None else B.new_on(stream, lambda: torch.empty_like(q))
         if n > self.max_tokens or not 0 <= seqs <= self.max_seqs:
             raise ValueError(f"{n} tokens in {seqs} sequences, the workspace holds {self.max_tokens} in {self.max_seqs}")
         a = self._args
@@ -43,16 +42,16 @@ class PromptAttention:
         a.k, a.k_stride = self._rows("k", k, n, self.num_kv_heads)
         a.v, a.v_stride = self._rows("v", v, n, self.num_kv_heads)
         a.out, a.out_stride = self._rows("out", out, n, self.num_q_heads)
-        if cu_seqlens.dtype is not torch.int32 or cu_seqlens.device != self.device or not cu_seqlens.is_contiguous():
+        if cu_seqlens.dtype is not torch.int32 or cu_seqlens.get_device() != self._index or not cu_seqlens.is_contiguous():
             raise ValueError("cu_seqlens: contiguous int32 on the workspace's device expected")
         a.cu_seqlens, a.num_seqs, a.num_tokens, a.scale = cu_seqlens.data_ptr(), seqs, n, scale
-        B.gb_prompt_attention(a, stream)
+        B.gb_prompt_attention(a, stream, self._index)
         return out
 
     def _rows(self, name, x, n, heads):
         """Address and token stride of a tensor of rows."""
         d = self.head_dim
-        if x.shape != (n, heads, d) or x.dtype is not self.torch_dtype or x.device != self.device:
+        if x.shape != (n, heads, d) or x.dtype is not self.torch_dtype or x.get_device() != self._index:
             raise ValueError(f"{name}: {tuple(x.shape)} {x.dtype} on {x.device}, expected {(n, heads, d)} {self.torch_dtype} "
                              f"on {self.device}")
         token, head, one = x.stride()
