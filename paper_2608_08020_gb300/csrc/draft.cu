@@ -28,7 +28,7 @@ constexpr int kTailRec = kMaxSegDepth;  // rec_off column of a beam's own units
 constexpr int kRecOffs = kMaxSegDepth + 1;
 
 // Workspace words of control.
-enum DraftCtl : int { kDrUnits = 0, kDrList = 1, kDrFew = 2, kDrWords = 64 };
+enum DraftCtl : int { kDrUnits = 0, kDrFew = 1, kDrWords = 64 };
 
 struct DraftUnit {
   int seg;         // -1: a beam's own unit
@@ -219,76 +219,102 @@ __device__ __forceinline__ void draft_rows(const PoolView& v, const DraftView& w
     }
   }
 }
-// The work list (one CTA).  `tokens`: of a unit's rows, `small`: where there are few units; `least`: tiles below which a run of keys is not split;
-// `coarse`: bits dropped from the costs, so that their sums stay in range.
+// The work list (one CTA).  2^`shift` tokens to a unit, 2^`small` where there are few units; `least`: tiles below which a
+// run of keys is not split; `coarse`: bits dropped from the costs, so that their sums stay in range.
 //
 // Down to which depth the shared segments are used is chosen by the cost above: a segment's unit reads
 // its pages once for up to 256 rows, but every piece of a beam's context beyond the first costs a record.  64 beams of 50 rows
 // over 64 shared and 130 own tokens run without segments; 64 beams of 50 rows at 4000 tokens use them all.
+//
+// The time is latency, nothing else runs meanwhile: loads are issued together, counts and sums stay in shared memory.
 __global__ void __launch_bounds__(kListThreads) k_draft_plan(PoolView v, DraftView w, const int* parent, const int* count,
-                                                             int tokens, int small, int least, int coarse, bool segs) {
+                                                             int shift, int small, int least, int coarse, bool segs) {
   pdl_wait();
   pdl_launch_dependents();
-  constexpr int kCached = 4096;         // segments whose rows and tiles fit in shared memory
+  constexpr int kCached = 4096;         // segments whose rows, tiles and depth fit in shared memory
   __shared__ ListSmem sm;
   __shared__ short s_cnt[kMaxBeams];
-  __shared__ unsigned s_src[kCached];   // rows | tiles << 16, each clamped (a source with more is read from memory)
+  __shared__ unsigned s_src[kCached];   // rows, then rows | tiles << 16, each clamped (a source with more is read from memory)
   constexpr int kStaged = 512;          // slots whose segments' lengths do
   __shared__ unsigned short s_seg[kStaged * kMaxSegDepth];
   __shared__ int s_cost[kMaxSegDepth + 1];
   __shared__ int s_start[kMaxBeams], s_len[kMaxBeams];
+  constexpr int kFewTries = 24;
+  enum { kSumFew, kSumWork, kSumWorkFew, kSumList, kSumTry, kSums = kSumTry + kFewTries };
+  __shared__ int s_sum[kSums];
   const int tid = threadIdx.x;
   const int b = tid, cap = v.max_beams;
-  const bool act = b < cap && v.active[b] != 0;
-  const int L = act ? v.seq_len[b] : 0;
+  bool act = false;
+  int L = 0, nd = 0;
+  if (b < cap) {
+    const int on = v.active[b], len = v.seq_len[b], deep = segs ? v.seg_nseg[b] : 0;
+    act = on != 0;
+    L = act ? len : 0;
+    nd = deep;
+  }
   bool bad = false;
   const int cnt = b < cap ? drafted(count, b, w.T, act, &bad) : 0;
   const int nseg = segs ? v.ctl[kCtlSegCount] : 0;
-  int nd = segs && cnt > 0 ? v.seg_nseg[b] : 0;
+  if (cnt <= 0) nd = 0;
   s_cnt[b] = (short)cnt;
   if (b < cap) w.cnt[b] = cnt;
-  if (tid == 0) w.ctl[kDrList] = 0;
+  if (tid < kSums) s_sum[tid] = 0;
   if (tid <= kMaxSegDepth) s_cost[tid] = 0;
-  for (int s = tid; s < nseg; s += kListThreads) w.seg_cnt[s] = 0;
+  for (int s = tid; s < nseg; s += kListThreads) {
+    if (s < kCached) s_src[s] = 0;
+    else w.seg_cnt[s] = 0;
+  }
+  // The depth and tiles of the thread's first segment.
+  int depth0 = 0, tiles0 = 0;
+  auto seg_tiles = [&](int s) { return (v.seg_len[s] * v.P + flash::kTok - 1) / flash::kTok; };
+  if (tid < nseg) {
+    tiles0 = seg_tiles(tid);
+    depth0 = v.seg_members[v.seg_mem_off[tid]] % kMaxSegDepth;
+  }
+  auto seg_depth = [&](int s) { return s < kListThreads ? depth0 : v.seg_members[v.seg_mem_off[s]] % kMaxSegDepth; };
+  auto own_tiles = [&](int s) { return s < kListThreads ? tiles0 : seg_tiles(s); };  // (s: of this thread)
   __syncthreads();
   // Segments: their drafted tokens, and each beam's place among them.
+#pragma unroll 1
   for (int e = tid; e < (segs ? cap * kMaxSegDepth : 0); e += kListThreads) {
-    const int c = s_cnt[e / kMaxSegDepth], k = e % kMaxSegDepth;
-    if (c > 0 && k < v.seg_nseg[e / kMaxSegDepth]) {
-      const int s = v.seg_bid[e];
+    const int c = s_cnt[e / kMaxSegDepth], k = e % kMaxSegDepth, deep = v.seg_nseg[e / kMaxSegDepth], s = v.seg_bid[e];
+    if (c > 0 && k < deep) {
       if (cap <= kStaged) s_seg[e] = (unsigned short)v.seg_len[s];  // (a table has at most 65535 entries then)
-      w.off[e] = atomicAdd(&w.seg_cnt[s], c);
+      w.off[e] = s < kCached ? (int)atomicAdd(&s_src[s], (unsigned)c) : atomicAdd(&w.seg_cnt[s], c);
     }
   }
   const bool staged = cap <= kStaged && v.max_pages < 65536;
   __syncthreads();
+  // Drafted tokens of segment s; until its tiles are noted beside them.
+  auto seg_count = [&](int s) { return s < kCached ? (int)s_src[s] : w.seg_cnt[s]; };
   auto depth_pages = [&](int k) {  // pages of this slot's k-th segment
     return staged ? (int)s_seg[b * kMaxSegDepth + k] : v.seg_len[v.seg_bid[b * kMaxSegDepth + k]];
   };
   auto depth_tiles = [&](int k) { return (depth_pages(k) * v.P + flash::kTok - 1) / flash::kTok; };
-  auto seg_tiles = [&](int s) { return (v.seg_len[s] * v.P + flash::kTok - 1) / flash::kTok; };
   auto unit_cost = [&](int rows, int tiles, int rec) {  // of `rows` tokens over `tiles` tiles
-    const int full = rows / tokens, rest = rows - full * tokens, halves = 2 * full + (rest > 0) + (2 * rest > tokens);
+    const int full = rows >> shift, rest = rows & ((1 << shift) - 1), halves = 2 * full + (rest > 0) + (rest > 1 << shift >> 1);
     return (int)((long long)halves * (tiles * kTileCost + kUnitCost + rec) >> coarse);
   };
   // Cost of the beams' own units by depth, for the beams that reach it; then the segments'.
   {
     int at = 0;
     if (cnt > 0) {
-      atomicAdd(&s_cost[0], unit_cost(cnt, tail_tiles(L), 0));
+      int before = unit_cost(cnt, tail_tiles(L), 0);
+      atomicAdd(&s_cost[0], before);
+#pragma unroll 1
       for (int k = 0; k < nd; ++k) {
         // What using the k-th segment too changes: a shorter rest, and for the first one a record.
-        const int from = tail_tiles(L - at), rec = k == 0 ? kRecCost : 0;
         at += depth_pages(k) * v.P;
-        atomicAdd(&s_cost[k + 1], unit_cost(cnt, tail_tiles(L - at), rec) - unit_cost(cnt, from, 0));
+        const int after = unit_cost(cnt, tail_tiles(L - at), kRecCost);
+        atomicAdd(&s_cost[k + 1], after - before);
+        before = after;
       }
     }
   }
-  __threadfence_block();
-  __syncthreads();
+#pragma unroll 1
   for (int s = tid; s < nseg; s += kListThreads) {
-    const int c = w.seg_cnt[s];
-    if (c > 0) atomicAdd(&s_cost[v.seg_members[v.seg_mem_off[s]] % kMaxSegDepth + 1], unit_cost(c, seg_tiles(s), kRecCost));
+    const int c = seg_count(s);
+    if (c > 0) atomicAdd(&s_cost[seg_depth(s) + 1], unit_cost(c, own_tiles(s), kRecCost));
   }
   int dmax = 0, all;
   __syncthreads();
@@ -302,7 +328,8 @@ __global__ void __launch_bounds__(kListThreads) k_draft_plan(PoolView v, DraftVi
       }
     }
   }
-  for (; dmax > 0; --dmax) {  // a record each, and one for the rest, must fit
+#pragma unroll 1
+  for (; (dmax + 1) * cap > w.rec_cap && dmax > 0; --dmax) {  // a record each, and one for the rest, must fit
     block_exclusive_scan(cnt > 0 ? min(nd, dmax) + 1 : 0, sm.tmp, &all);
     if (all <= w.rec_cap) break;
   }
@@ -310,53 +337,73 @@ __global__ void __launch_bounds__(kListThreads) k_draft_plan(PoolView v, DraftVi
   int start = 0;
   for (int k = 0; k < nd; ++k) start += depth_pages(k) * v.P;
   const int tail = cnt > 0 ? tail_tiles(L - start) : 0;
-  auto seg_rows = [&](int s) { return v.seg_members[v.seg_mem_off[s]] % kMaxSegDepth < dmax ? w.seg_cnt[s] : 0; };
+  auto up = [&](int rows, int sh) { return (rows + (1 << sh) - 1) >> sh; };
   // Few units of 128 rows: that many rows to a unit, and one unit per SM (two shorter ones leave SMs idle in the second
   // wave: a 20000-token beam of 8 KV heads in 256 units of 5 tiles took as long as 144 of 9 would in two waves).
-  int mine, base, work = 0, whole = 0;
+  int whole = up(cnt, small), work = tail * up(cnt, shift), work_few = tail * whole;
+#pragma unroll 1
   for (int s = tid; s < nseg; s += kListThreads) {
-    const int c = seg_rows(s), t = seg_tiles(s);
+    const int c = seg_depth(s) < dmax ? seg_count(s) : 0, t = own_tiles(s);
     if (s < kCached) s_src[s] = (unsigned)min(c, 65535) | (unsigned)min(t, 65535) << 16;
-    whole += (c + small - 1) / small;
-    if (c > 0) w.seg_list[s] = atomicAdd(&w.ctl[kDrList], c);
+    if (s >= kCached || c >= 65535) w.seg_cnt[s] = c;
+    whole += up(c, small);
+    work += t * up(c, shift);
+    work_few += t * up(c, small);
+    if (c > 0) w.seg_list[s] = atomicAdd(&s_sum[kSumList], c);
   }
-  block_exclusive_scan(whole + (cnt + small - 1) / small, sm.tmp, &all);
-  const bool few = (long long)all * v.Hkv <= v.num_sms;
-  if (few) tokens = small;
-  auto tiles_of = [&](int s, int* rows) {  // of a segment, and its row tiles
-    const unsigned x = s < kCached ? s_src[s] : ~0u;
-    const int c = (x & 0xffff) == 0xffff ? seg_rows(s) : x & 0xffff;
-    *rows = (c + tokens - 1) / tokens;
-    return c == 0 ? 0 : x >> 16 == 0xffff ? seg_tiles(s) : x >> 16;
+  work = __reduce_add_sync(0xffffffffu, work);
+  work_few = __reduce_add_sync(0xffffffffu, work_few);
+  if ((tid & 31) == 0) {
+    atomicAdd(&s_sum[kSumWork], work);
+    atomicAdd(&s_sum[kSumWorkFew], work_few);
+  }
+  const bool few = (long long)block_sum(whole, &s_sum[kSumFew]) * v.Hkv <= v.num_sms;
+  if (few) shift = small;
+  const int tokens = 1 << shift;
+  struct Source {
+    int rows, tiles;
   };
-  const int rows_b = (cnt + tokens - 1) / tokens;
-  work = tail * rows_b;
-  for (int s = tid; s < nseg; s += kListThreads) {
-    int rows;
-    const int t = tiles_of(s, &rows);
-    work += rows * t;
-  }
-  block_exclusive_scan(work, sm.tmp, &all);
+  auto segment = [&](int s) {  // rows 0: not used
+    const unsigned x = s < kCached ? s_src[s] : ~0u;
+    Source r;
+    r.rows = (x & 0xffff) == 0xffff ? w.seg_cnt[s] : x & 0xffff;
+    r.tiles = r.rows == 0 ? 0 : x >> 16 == 0xffff ? seg_tiles(s) : x >> 16;
+    return r;
+  };
   // Tiles per unit: half an SM's share at most, which the sorted list evens out, but not too short ones, and no more
   // records than there is room for.
   const int share = (few ? 1 : 2) * v.num_sms;
-  int per = max(least, (int)(((long long)all * v.Hkv + share - 1) / share));
-  for (; few; per += 1 + per / 8) {  // until the pieces fit too
-    int n = rows_b * ((tail + per - 1) / per);
-    for (int s = tid; s < nseg; s += kListThreads) {
-      int rows;
-      const int t = tiles_of(s, &rows);
-      n += rows * ((t + per - 1) / per);
+  all = s_sum[few ? kSumWorkFew : kSumWork];
+  constexpr int kLongest = 1 << 20;  // no run of keys has more tiles
+  int mine, base, per = min(kLongest, max(least, (int)(((long long)all * v.Hkv + share - 1) / share)));
+  float inv;  // 1 / per, for quotients of counts of tiles: (x + 1/2) / per is at least 1 / (2 per) from a whole number, more than its error
+  auto pieces = [&](int tiles) { return (int)(((float)(tiles + per - 1) + 0.5f) * inv); };
+  inv = 1.f / (float)per;
+#pragma unroll 1
+  for (int k = 0; few; ++k) {  // until the pieces fit too
+    if (k == kFewTries) {      // (a piece each does)
+      per = kLongest;
+      inv = 1.f / (float)per;
+      break;
     }
-    block_exclusive_scan(n, sm.tmp, &all);
-    if ((long long)all * v.Hkv <= v.num_sms || per > (1 << 24)) break;
+    int n = up(cnt, shift) * pieces(tail);
+    for (int s = tid; s < nseg; s += kListThreads) {
+      const Source r = segment(s);
+      n += up(r.rows, shift) * pieces(r.tiles);
+    }
+    if ((long long)block_sum(n, &s_sum[kSumTry + k]) * v.Hkv <= v.num_sms) break;
+    per += 1 + per / 8;
+    inv = 1.f / (float)per;
   }
   if (tid == 0) w.ctl[kDrFew] = few;
-  for (;; per *= 2) {
-    mine = cnt > 0 ? (tail + per - 1) / per : 0;
-    for (int k = 0; k < nd; ++k) mine += (depth_tiles(k) + per - 1) / per;
+#pragma unroll 1
+  for (;;) {
+    mine = cnt > 0 ? pieces(tail) : 0;
+    for (int k = 0; k < nd; ++k) mine += pieces(depth_tiles(k));
     base = block_exclusive_scan(mine, sm.tmp, &all);
-    if (all <= w.rec_cap || per > (1 << 24)) break;
+    if (all <= w.rec_cap || per >= kLongest) break;
+    per *= 2;
+    inv = 1.f / (float)per;
   }
   int tail_rec = 0;
   if (b < cap) {
@@ -364,7 +411,7 @@ __global__ void __launch_bounds__(kListThreads) k_draft_plan(PoolView v, DraftVi
     w.rec_base[b] = base;
     for (int k = 0; k < nd; ++k) {
       w.rec_off[b * kRecOffs + k] = tail_rec;
-      tail_rec += (depth_tiles(k) + per - 1) / per;
+      tail_rec += pieces(depth_tiles(k));
     }
     w.rec_off[b * kRecOffs + kTailRec] = tail_rec;
     w.depth[b] = nd;
@@ -384,13 +431,13 @@ __global__ void __launch_bounds__(kListThreads) k_draft_plan(PoolView v, DraftVi
       p.rows = s_cnt[src - nseg];
       p.tiles = p.rows > 0 ? tail_tiles(s_len[src - nseg] - s_start[src - nseg]) : 0;
     } else {
-      const unsigned x = src < kCached ? s_src[src] : ~0u;
-      p.rows = (x & 0xffff) == 0xffff ? seg_rows(src) : x & 0xffff;
-      p.tiles = p.rows == 0 ? 0 : x >> 16 == 0xffff ? seg_tiles(src) : x >> 16;
+      const Source r = segment(src);
+      p.rows = r.rows;
+      p.tiles = r.tiles;
     }
-    p.splits = (p.tiles + per - 1) / per;
-    p.share = p.splits > 0 ? (p.tiles + p.splits - 1) / p.splits : 1;
-    p.row_tiles = (p.rows + tokens - 1) / tokens;
+    p.splits = pieces(p.tiles);
+    p.share = p.splits > 1 ? (p.tiles + p.splits - 1) / p.splits : max(p.tiles, 1);
+    p.row_tiles = up(p.rows, shift);
     return p;
   };
   const int n = emit_sorted(
@@ -401,14 +448,14 @@ __global__ void __launch_bounds__(kListThreads) k_draft_plan(PoolView v, DraftVi
       },
       [&](int src, int i) {
         const Piece p = piece(src);
-        const int sp = i / p.row_tiles, t = i % p.row_tiles;
+        const int sp = p.row_tiles == 1 ? i : i / p.row_tiles, t = i - sp * p.row_tiles;
         const int rows = min(tokens, p.rows - t * tokens);
         return (min(p.share, p.tiles - sp * p.share) + 1) * (2 * rows > tokens ? 2 : 1);
       },
       [&](int src, int i, int at) {
         if (at >= w.max_units) return;
         const Piece p = piece(src);
-        const int sp = i / p.row_tiles, t = i % p.row_tiles;
+        const int sp = p.row_tiles == 1 ? i : i / p.row_tiles, t = i - sp * p.row_tiles;
         const int rows = max(0, min(tokens, p.rows - t * tokens));
         DraftUnit u;
         u.ntok = rows;
@@ -1177,12 +1224,14 @@ extern "C" gb_status gb_draft_attention(gb_pool* pool, int layer, const gb_draft
       return fail(pool, GB_ERR_CUDA, "draft: tensor map");
   }
   if (layer == 0) {
-    const int tokens = (bf16 ? 2 * flash::kRows : kTileRows) / v.G;
+    const int tokens = (bf16 ? 2 * flash::kRows : kTileRows) / v.G;  // (G is a power of two)
+    int shift = 0;
+    while (1 << shift < tokens) ++shift;
     const long long dearest = 2ll * v.max_beams * ((T + tokens - 1) / tokens) * (kTileCost * ((long long)v.max_pages * v.P / flash::kTok + 2) + kUnitCost + kRecCost);
     int coarse = 0;
     while (dearest >> coarse >= 1 << 28) ++coarse;
-    launch_pdl(k_draft_plan, 1, kListThreads, 0, s, v, w, d->parent_dev, d->count_dev, tokens,
-               bf16 ? tokens / 2 : tokens, bf16 ? 2 : 1, coarse, bf16 && v.grouped);
+    launch_pdl(k_draft_plan, 1, kListThreads, 0, s, v, w, d->parent_dev, d->count_dev, shift,
+               bf16 ? shift - 1 : shift, bf16 ? 2 : 1, coarse, bf16 && v.grouped);
     pool->launches += 1;
     if (v.max_beams > kOneLaunch) {
       launch_pdl(k_draft_rows, (v.max_beams + 7) / 8, 256, 0, s, v, w, d->parent_dev, d->count_dev);
