@@ -780,7 +780,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_draft_f32(PoolView v, Draft
 // records, sum 2^(m_k - m) (o_k, l_k), or writes the zeros of a row that holds no token; a row that has its result
 // already is left.  Bound by the records' reads; many small CTAs (a third as many, looping: 128 beams of short contexts 46
 // -> 51 us a layer).
-template <typename T, int D>
+// kBatch records at a time: 4 where there are many CTAs, whose registers then let more of them run (48 instead of 74; 64 beams
+// x 4k 269 -> 260 us, a 36-layer round 1700 -> 1674), 8 where there are few (one beam of 20000 tokens 71 us, 74 with 4).
+template <typename T, int D, int kBatch>
 __global__ void __launch_bounds__(256) k_draft_merge(PoolView v, DraftView w, T* o) {
   pdl_wait();
   pdl_launch_dependents();
@@ -809,13 +811,14 @@ __global__ void __launch_bounds__(256) k_draft_merge(PoolView v, DraftView w, T*
         l = fmaf(ml.y, f, l);
         const int m32 = min(32, n - k0);
         const Vec* x = reinterpret_cast<const Vec*>(w.rec + (r0 + k0 * step) * D) + lane;
-        for (int k = 0; k < m32; k += 8) {
-          Vec y[8];
+#pragma unroll 1
+        for (int k = 0; k < m32; k += kBatch) {
+          Vec y[kBatch];
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
+          for (int e = 0; e < kBatch; ++e)
             if (k + e < m32) y[e] = x[(size_t)(k + e) * step * 32];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
+          for (int e = 0; e < kBatch; ++e) {
             const float g = __shfl_sync(0xffffffffu, f, (k + e) & 31);
             if (k + e < m32)
 #pragma unroll
@@ -1257,18 +1260,19 @@ extern "C" gb_status gb_draft_attention(gb_pool* pool, int layer, const gb_draft
     pool->draft_capture = capture;
   }
   cudaError_t e;
-  const dim3 merge(T, v.max_beams, (long long)T * v.max_beams < 2 * pool->num_sms ? (v.Hq + 7) / 8 : 1);
+  const bool sparse = (long long)T * v.max_beams < 2 * pool->num_sms;
+  const dim3 merge(T, v.max_beams, sparse ? (v.Hq + 7) / 8 : 1);
   if (bf16) {
     e = set_max_dynamic_smem(reinterpret_cast<const void*>(k_draft), flash::kSmem);
     if (e == cudaSuccess) e = launch_pdl(k_draft, pool->num_sms, flash::kThreads, flash::kSmem, s, job);
-    if (e == cudaSuccess) e = launch_pdl(k_draft_merge<__nv_bfloat16, 128>, merge, 256, 0, s, v, w, job.o);
+    if (e == cudaSuccess) e = launch_pdl(sparse ? k_draft_merge<__nv_bfloat16, 128, 8> : k_draft_merge<__nv_bfloat16, 128, 4>, merge, 256, 0, s, v, w, job.o);
   } else {
     e = set_max_dynamic_smem(reinterpret_cast<const void*>(k_draft_f32), (int)sizeof(TileSmem));
     if (e == cudaSuccess)
       e = launch_pdl(k_draft_f32, pool->num_sms, kTileThreads, sizeof(TileSmem), s, v, w, layer,
                      static_cast<const float*>(q_dev), static_cast<const float*>(k_dev), static_cast<const float*>(v_dev),
                      static_cast<float*>(out_dev), qscale);
-    if (e == cudaSuccess) e = launch_pdl(k_draft_merge<float, 64>, merge, 256, 0, s, v, w, static_cast<float*>(out_dev));
+    if (e == cudaSuccess) e = launch_pdl(sparse ? k_draft_merge<float, 64, 8> : k_draft_merge<float, 64, 4>, merge, 256, 0, s, v, w, static_cast<float*>(out_dev));
   }
   pool->launches += 2;
   if (e != cudaSuccess) return fail(pool, GB_ERR_CUDA, cudaGetErrorString(e));
