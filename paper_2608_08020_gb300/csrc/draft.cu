@@ -13,7 +13,7 @@
 //
 // Bound by the reads of the cache while rows x 2 flops a byte stay below the machine's ~280, i.e. up to some
 // 100 rows a shared token, and by the tensor cores beyond.  Measured (bf16): a layer of 64 traces at 4000 tokens, trees of up to
-// 16, 127 us with its plan and join (387 MB in 105 us inside the attention, 3.7 TB/s); 198 traces at 8000 tokens 288 us; a
+// 16, 116 us with its plan and join (387 MB in 95 us inside the attention, 4.1 TB/s); 198 traces at 8000 tokens 258 us; a
 // layer of 128 traces of 190 tokens 46 us.
 #include <algorithm>
 #include <type_traits>
@@ -522,6 +522,8 @@ struct DraftJob {
   __nv_bfloat16* o;
 
   static constexpr bool kEarlyQ = true;
+  // 64 traces x 4k 260 -> 240 us, 198 x 8k 295 -> 265; from two tiles on, 128 traces of 2 and 3 tiles a unit 1663 -> 1736 us.
+  static constexpr int kLongPair = 4;
   static constexpr int kQArrivals = 4;
   // Tiles land as [16 groups of 8 tokens][half of D][8][64 dims].
   static constexpr int kKHalf = 1024, kKSbo = 2048, kVLbo = 1024, kVSbo = 2048, kVStep = 4096;

@@ -24,7 +24,7 @@
 //   warps 0-7    softmax: thread r of group g owns row r of its tile (tensor-memory lane r); also loads
 //                the row's query
 //   warp 8       takes the CTA's units from the sorted list, publishes them in a ring of eight and streams K
-//   warp 11      streams V; both go through one ring of five 32 KiB stages (K0 V0 K1 V1 ...)
+//   warp 11      streams V; both go through one ring of five 32 KiB stages (K0 V0 K1 V1 ..., of a pair K K V V)
 //   warps 9-10   issue the products of a group each: S(i), then P.V(i) before S(i + 1), whose tile
 //                P overwrites; a thread's products run in issue order
 //   warps 12-15  write the results: while they read O the softmax groups are in the next unit
@@ -67,10 +67,12 @@ constexpr uint32_t kTmemS = 0, kTmemO = 256;  // column of group 0; group 1 is 1
 constexpr int kSlots = 8, kUnitWords = 12;  // units known ahead
 enum Mode : int { kJoint, kDual, kFirst, kSecond, kAlone };
 // Three "full" and three "empty" barriers a stage, used in turn (ring position mod 15), since the warps do not keep step: a wait
-// on a barrier whose phase before last has not ended would pass at once.  For a group that waits for K at position p that
-// phase is of p - 15, which has been consumed: K at p - 10 came into its stage, and is out before p's unit begins (kBarBegin)
-// or p - 4 was seen.  The V after a K that was seen follows in the same way, and a loading warp's wait, for the consumption of
-// p - 5, has p - 20 behind it.
+// on a barrier whose phase before last has not ended would pass at once.  For a group that waits for position p that phase is
+// of p - 15.  It has ended if the load of p - 10 into its stage has been issued, and that follows from what the group has seen:
+// the K and V of its tiles before, or that p's unit has begun (kBarBegin), so that every K before it is out.  Each warp loads in
+// order, and a load at q says that q - 5 was consumed, hence landed, hence that all loads of its kind before it are out.  The
+// blocks K V and K K V V, in any order, leave no p without such a chain (all sequences over the last ten positions gone through);
+// a loading warp's wait, for the consumption of p - 5, has p - 20 behind it in the same way.
 constexpr int kFulls = 3 * kStages;
 constexpr int kBarFull = 0;                       // [kFulls]
 constexpr int kBarEmpty = kBarFull + 8 * kFulls;  // [kFulls]
@@ -103,13 +105,28 @@ static_assert(sizeof(Unit) == 4 * kUnitWords, "unit words");
 __device__ __forceinline__ bool takes_part(int mode, int g) {
   return mode <= kDual || (g == 0) != (mode == kSecond);
 }
-// Group g's tiles of a unit, and the ring position of the K of its i-th, counted from where the unit (or the pair) begins.
+// Group g's tiles of a unit.
 __device__ __forceinline__ int group_tiles(int nt, int mode, int g) { return mode == kJoint ? (nt + 1 - g) / 2 : nt; }
 __device__ __forceinline__ int group_tile(int mode, int g, int i) { return mode == kJoint ? 2 * i + g : i; }
+// Ring positions of the K of a group's tiles i = 0, 1, ..., counted from where the unit (or the pair) begins; V follows its K.
 __device__ __forceinline__ int tile_position(int mode, int mate, int g, int i) {
   if (mode == kFirst) return 2 * (i + min(i, mate));
   if (mode == kSecond) return 2 * (i + min(i + 1, mate));
   return 2 * group_tile(mode, g, i);
+}
+// The same for a job with long pairs (kLongPair tiles or more by turns): while both units of one have tiles they come as K K V V, so
+// that a group's next K is in the ring a step before it is due.  Those of short ones come as K V K V, which puts the groups half
+// a step apart from the start.
+struct Places {
+  int both, first, v_after;  // tiles that come by turns, the first's position, and how far behind its K a V lies meanwhile
+  __device__ __forceinline__ int k(int i) const { return i < both ? 4 * i + first : 2 * (i + both); }
+  __device__ __forceinline__ int v(int i) const { return k(i) + (i < both ? v_after : 1); }
+};
+// Of the first or second unit of a pair with that many tiles by turns (0: of a unit by itself).
+template <class Job>
+__device__ __forceinline__ Places places(int both, bool second) {
+  const bool far = both >= Job::kLongPair;
+  return {both, second ? (far ? 1 : 2) : 0, far ? 2 : 1};
 }
 // Ring positions of a unit, a pair's counted with its second.
 __device__ __forceinline__ int positions(int nt, int mode, int mate) {
@@ -527,7 +544,8 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       // ---------------------------------------------------------------- units and K tiles
       const typename Job::Units all(job);
       const int total = job.total(all), cap = job.capacity();
-      uint32_t n = 0;  // ring position
+      uint32_t from = 0;            // ring position of the unit's (or pair's) first tile; without long pairs, of the next
+      uint32_t last = 0, seen = 0;  // position loaded last; bit i: so was the one i before it
       bool ok = true;
       auto id_of = [&](int u) {  // b, 2 n - 1 - b, 2 n + b, ...
         return u * (int)gridDim.x + ((u & 1) ? (int)gridDim.x - 1 - (int)blockIdx.x : (int)blockIdx.x);
@@ -551,8 +569,8 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       auto begin = [&](int u) {
         if (lane == 0) mbar_arrive(ctl + kBarBegin + 8 * (u & (kSlots - 1)));
       };
-      auto load = [&](const Unit& z, int j, int page) {
-        const uint32_t st = n % kStages;
+      auto load = [&](const Unit& z, const Places& at, int j, int page) {
+        const uint32_t n = Job::kLongPair > 0 ? from + at.k(j) : from, st = n % kStages;
         if (n >= (uint32_t)kStages)
           ok = warp_wait(ctl + kBarEmpty + 8 * ((n - kStages) % kFulls), ((n - kStages) / kFulls) & 1, abort_flag);
         if (!ok) return;
@@ -560,7 +578,12 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
         if (lane == 0) mbar_arrive_expect_tx(bar, kTile);
         __syncwarp();
         job.load_tile(z, j, 0, page, sbase + kRing + st * kTile, bar, lane);
-        n += 2;
+        if (Job::kLongPair > 0) {
+          seen = seen << (n - last) | 1;
+          last = n;
+        } else {
+          from += 2;
+        }
       };
       // Modes of a unit and the one after it: two of up to 128 rows make a pair.
       auto match = [&](Unit& p, Unit& q) {
@@ -584,17 +607,18 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       if (pair && ok) publish(1, y);
       int page_x = x.nt >= 0 ? job.page(x, 0, lane) : 0, page_y = pair ? job.page(y, 0, lane) : 0;  // the lane's pages
       for (int u = 0; ok && x.nt >= 0;) {
-        const int step = pair ? 2 : 1, tiles = pair ? max(x.nt, y.nt) : x.nt;
+        const int step = pair ? 2 : 1, tiles = pair ? max(x.nt, y.nt) : x.nt, both = pair ? min(x.nt, y.nt) : 0;
+        const Places at_x = places<Job>(both, false), at_y = places<Job>(both, true);
         bool next_pair = false;
         begin(u);
         if (pair) begin(u + 1);
         for (int j = 0; j < tiles && ok; ++j) {
           if (j < x.nt) {
-            load(x, j, page_x);
+            load(x, at_x, j, page_x);
             if (j + 1 < x.nt) page_x = job.page(x, j + 1, lane);
           }
           if (pair && j < y.nt && ok) {
-            load(y, j, page_y);
+            load(y, at_y, j, page_y);
             if (j + 1 < y.nt) page_y = job.page(y, j + 1, lane);
           }
           if (j == 0 && ok) {
@@ -606,6 +630,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
             if (next_pair && ok) publish(u + step + 1, c);
           }
         }
+        if (Job::kLongPair > 0) from += 2 * (x.nt + (pair ? y.nt : 0));
         u += step;
         pair = next_pair;
         x = a;
@@ -613,12 +638,17 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
         page_x = ok && x.nt >= 0 ? job.page(x, 0, lane) : 0;
         page_y = ok && pair ? job.page(y, 0, lane) : 0;
       }
+      if (Job::kLongPair == 0) {
+        last = from - 2;
+        seen = 0x155u & ((1u << min(from, 31u)) - 1);
+      }
       if (lane == 0 && *abort_flag)  // copies in flight land before the CTA leaves (bounded)
-        for (uint32_t k = n > 2 * kStages ? n - 2 * kStages : 0; k < n; k += 2)
-          mbar_wait_bounded(ctl + kBarFull + 8 * (k % kFulls), (k / kFulls) & 1, kWaitLimitNs / 8);
+        for (uint32_t i = 0; i < 2 * kStages; ++i)
+          if ((seen >> i) & 1)
+            mbar_wait_bounded(ctl + kBarFull + 8 * ((last - i) % kFulls), ((last - i) / kFulls) & 1, kWaitLimitNs / 8);
     } else if (warp == kVWarp) {
       // ---------------------------------------------------------------- V tiles
-      uint32_t n = 1;  // ring position
+      uint32_t from = 0, last = 0, seen = 0;  // as above
       uint32_t patches = 0;
       uint32_t p_dst = 0, p_full = 0;  // the V tile that waits to be mended
       int z0 = 0, z1 = 0;              // its rows that hold no token
@@ -666,7 +696,8 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
           if (f == 1 || (landed && f == 2)) return true;
         }
       };
-      auto load = [&](const Unit& now, int j, int page) {
+      auto load = [&](const Unit& now, const Places& at, int j, int page) {
+        const uint32_t n = Job::kLongPair > 0 ? from + at.v(j) : from + 1;
         const uint32_t st = n % kStages, dst = sbase + kRing + st * kTile, full = ctl + kBarFull + 8 * (n % kFulls);
         if (n >= (uint32_t)kStages)
           ok = wait(ctl + kBarEmpty + 8 * ((n - kStages) % kFulls), ((n - kStages) / kFulls) & 1, false);
@@ -685,7 +716,12 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
         if (lane == 0) mbar_arrive_expect_tx(bar, kTile);
         __syncwarp();
         job.load_tile(now, j, 1, page, dst, bar, lane);
-        n += 2;
+        if (Job::kLongPair > 0) {
+          seen = seen << (n - last) | 1;
+          last = n;
+        } else {
+          from += 2;
+        }
       };
       Unit x, y;
       fetch(0, x);
@@ -693,18 +729,20 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       if (pair) fetch(1, y);
       int page_x = ok && x.nt >= 0 ? job.page(x, 0, lane) : 0, page_y = ok && pair ? job.page(y, 0, lane) : 0;
       for (int u = 0; ok && x.nt >= 0;) {
-        const int tiles = pair ? max(x.nt, y.nt) : x.nt;
+        const int tiles = pair ? max(x.nt, y.nt) : x.nt, both = pair ? min(x.nt, y.nt) : 0;
+        const Places at_x = places<Job>(both, false), at_y = places<Job>(both, true);
         for (int j = 0; j < tiles && ok; ++j) {
           if (j < x.nt) {
-            load(x, j, page_x);
+            load(x, at_x, j, page_x);
             if (j + 1 < x.nt) page_x = job.page(x, j + 1, lane);
           }
           if (pair && j < y.nt && ok) {
-            load(y, j, page_y);
+            load(y, at_y, j, page_y);
             if (j + 1 < y.nt) page_y = job.page(y, j + 1, lane);
           }
         }
         if (!ok) break;
+        if (Job::kLongPair > 0) from += 2 * (x.nt + (pair ? y.nt : 0));
         u += pair ? 2 : 1;
         fetch(u, x);
         if (!ok) break;
@@ -715,12 +753,16 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
         page_y = pair ? job.page(y, 0, lane) : 0;
       }
       if (ok && z0 < z1) ok = wait(0, 0, true);
+      if (Job::kLongPair == 0) {
+        last = from - 1;
+        seen = 0x155u & ((1u << min(from, 31u)) - 1);
+      }
       // Copies in flight land before the CTA leaves (bounded).
       if (lane == 0 && *abort_flag) {
         if (z0 < z1) mbar_wait_bounded(ctl + kBarPatch, patches & 1, kWaitLimitNs / 8);
-        for (uint32_t k = n > 2 * kStages ? n - 2 * kStages : 1; k < n; k += 2)
-          if (ctl + kBarFull + 8 * (k % kFulls) != p_full || z0 >= z1)
-            mbar_wait_bounded(ctl + kBarFull + 8 * (k % kFulls), (k / kFulls) & 1, kWaitLimitNs / 8);
+        for (uint32_t i = 0; i < 2 * kStages; ++i)
+          if (((seen >> i) & 1) && (ctl + kBarFull + 8 * ((last - i) % kFulls) != p_full || z0 >= z1))
+            mbar_wait_bounded(ctl + kBarFull + 8 * ((last - i) % kFulls), ((last - i) / kFulls) & 1, kWaitLimitNs / 8);
       }
     } else if (warp >= kOutWarp) {
       // ---------------------------------------------------------------- results
@@ -800,14 +842,18 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
         if (!takes_part(mode, g)) continue;
         if (!wait(bars + kBarBegin + 8 * slot, (u / kSlots) & 1)) break;
         const int mine = group_tiles(nt, mode, g);
+        Places at = places<Job>(mode == kFirst || mode == kSecond ? min(nt, mate) : 0, mode == kSecond);
+        if (mode == kJoint) at = {mine, 2 * g, 1};  // every other tile
         // A stage is free after both groups' use of it; a tile of one group's alone counts twice.
-        auto done_with = [&](uint32_t pos) {
-          mma_commit(bars + kBarEmpty + 8 * (pos % kFulls));
-          if (mode != kDual) mma_commit(bars + kBarEmpty + 8 * (pos % kFulls));
+        auto done_with = [&](uint32_t bar) {
+          mma_commit(bar);
+          if (mode != kDual) mma_commit(bar);
         };
         for (int i = -1; i < mine && ok; ++i) {  // P.V of tile i, then S of tile i + 1
-          const uint32_t v_pos = from + tile_position(mode, mate, g, i) + 1, v_st = v_pos % kStages;
-          const uint32_t k_pos = from + tile_position(mode, mate, g, i + 1), k_st = k_pos % kStages;
+          const uint32_t v_pos = from + (Job::kLongPair > 0 ? at.v(i) : tile_position(mode, mate, g, i) + 1);
+          const uint32_t k_pos = from + (Job::kLongPair > 0 ? at.k(i + 1) : tile_position(mode, mate, g, i + 1));
+          const uint32_t v_st = v_pos % kStages, k_st = k_pos % kStages;
+          const uint32_t v_done = bars + kBarEmpty + 8 * (v_pos % kFulls), k_done = bars + kBarEmpty + 8 * (k_pos % kFulls);
           // The tiles first: once P is there nothing else is waited for between it and the next S.
           if (i + 1 < mine && !wait(bars + kBarFull + 8 * (k_pos % kFulls), (k_pos / kFulls) & 1)) break;
           if (i < 0) {
@@ -830,7 +876,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
 #pragma unroll
               for (int kk = kTok / 32; kk < kTok / 16; ++kk)
                 mma_ts_add(o_t, s_t + kk * 8, v0 + ((kk * Job::kVStep) >> 4), ID_PV);
-              done_with(v_pos);
+              done_with(v_done);
               if (i + 1 == mine) mma_commit(bars + kBarO + 8 * g);
             }
             __syncwarp();
@@ -846,7 +892,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
                 mma_add(s_t, q0 + (((kk >> 2) * 16384 + (kk & 3) * 32) >> 4),
                         k0 + (((kk >> 2) * Job::kKHalf + (kk & 3) * 32) >> 4), ID_S);
               mma_commit(bars + kBarS + 8 * g);
-              done_with(k_pos);
+              done_with(k_done);
             }
             __syncwarp();
           }
