@@ -666,3 +666,20 @@ def test_streams(cuda):
         with pytest.raises(ValueError):
             call(side.cuda_stream)
     assert x.pool.status() == 0
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_offsets_past_32_bits(cuda, dtype):
+    """A pool whose last layer begins behind 2^31 elements."""
+    from paper_2608_08020_gb300.draft import DraftTrees
+    x = Trees(dtype, layers=3, hq=16, hkv=8, slots=3, beams=2, prompt=200, room=40, pages=70000, seed=12)
+    trees = DraftTrees(x.pool, 7)
+    x.append(30)
+    x.fork([0, 1, 1])
+    rnd = x.attention(trees, 7)
+    x.accept(trees, rnd, [6 if c == 7 else c - 1 for c in rnd[1]])
+    x.truncate([225, -1, 210])
+    x.attention(trees, 7)
+    x.decode()
+    assert x.pool.status() == 0
+    x.same_pages()

@@ -274,3 +274,24 @@ def test_bounds_that_name_rows_again(cuda, dtype):
     assert bool(fine[:999].all()) and bool((out[999] == 7).all())
     o, a = attend(q, k, v, [1000, 1200, 2000], 0.1)
     assert bool(((out.double() - o).abs() <= bound(o, a, dtype))[1000:].all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_offsets_past_32_bits(cuda, dtype):
+    """Token strides with which the last rows lie behind 2^31 elements."""
+    import torch
+    from paper_2608_08020_gb300.prompt import PromptAttention
+    n, stride = 2300, 1 << 20
+    q, k, v = make(dtype, n, 4, 2, 17)
+    d = q.shape[2]
+    rows, res = (torch.zeros(n, stride, dtype=q.dtype, device="cuda") for _ in range(2))
+    wide = [rows[:, a * d:b * d].unflatten(1, (-1, d)) for a, b in ((0, 4), (4, 6), (6, 8))]
+    for x, y in zip(wide, (q, k, v)):
+        x.copy_(y)
+    out = res[:, :4 * d].unflatten(1, (-1, d))
+    op = PromptAttention(4, 2, d, dtype, max_tokens=n, max_seqs=2)
+    op(*wide, torch.tensor([0, 100, n], dtype=torch.int32, device="cuda"), 0.1, out)
+    o, a = attend(q, k, v, [0, 100, n], 0.1)
+    assert op.status() == 0
+    assert bool(((out.double() - o).abs() <= bound(o, a, dtype)).all())
+    assert not bool(res[:, 4 * d:5 * d].any())
