@@ -396,7 +396,7 @@ cudaError_t launch_attention(gb_pool* pool, int layer, const void* q, const void
                              float* out, bool allow_local, cudaStream_t s);
 cudaError_t launch_wait_selftest(gb_pool* pool, cudaStream_t s);
 void make_kv_tensor_maps(gb_pool* pool);
-// A bf16 tensor map with the 128-byte swizzle, zeros out of bounds (grouped.cu); strides in bytes.
+// A bf16 tensor map with the 128-byte swizzle, zeros out of bounds (tensor_map.cu); strides in bytes.
 bool encode_tensor_map(void* map, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides,
                        const cuuint32_t* box);
 cudaError_t launch_probe(gb_pool* pool, const void* hidden, int hidden_dtype, int H, const float* w,
