@@ -85,14 +85,16 @@ class BeamPool:
 
     def fork_slots(self, parent_of, stream=None):
         """Apply a tournament decided elsewhere (parent_of int32 [max_beams]; see gb_fork_slots)."""
-        B.gb_fork_slots(self.handle, parent_of, stream)
+        B.gb_fork_slots(self.handle, self._slots("parent_of", parent_of), stream)
 
     def truncate(self, lengths, stream=None):
         """Each active slot keeps its first lengths[slot] tokens (int32 [max_beams]; negative: all)."""
-        if lengths.dtype != torch.int32 or lengths.numel() != self.max_beams or not lengths.is_contiguous() \
-                or lengths.device != self.kv.device:
-            raise ValueError("lengths: contiguous int32 [max_beams] on the pool's device expected")
-        B.gb_truncate(self.handle, lengths, stream)
+        B.gb_truncate(self.handle, self._slots("lengths", lengths), stream)
+
+    def _slots(self, name, x):
+        if x.dtype != torch.int32 or x.numel() != self.max_beams or not x.is_contiguous() or x.device != self.kv.device:
+            raise ValueError(f"{name}: contiguous int32 [max_beams] on the pool's device expected")
+        return x
 
     def status(self, stream=None) -> int:
         return B.gb_pool_status(self.handle, stream)

@@ -683,3 +683,14 @@ def test_offsets_past_32_bits(cuda, dtype):
     x.decode()
     assert x.pool.status() == 0
     x.same_pages()
+
+
+def test_fork_refusals(cuda):
+    x = Trees("bf16", seed=4)
+    good = x.ints([0, 1, 2, 3, 0, 1])
+    for bad in (good.long(), good[:5], good.cpu(), good.repeat(2)[::2]):
+        with pytest.raises(ValueError):
+            x.pool.fork_slots(bad)
+    x.fork([0, 1, 2, 3, 0, 1])
+    assert x.pool.status() == 0
+    x.same_pages()
