@@ -1252,7 +1252,8 @@ extern "C" gb_status gb_draft_attention(gb_pool* pool, int layer, const gb_draft
     const int tokens = (bf16 ? 2 * flash::kRows : kTileRows) / v.G;  // (G is a power of two)
     int shift = 0;
     while (1 << shift < tokens) ++shift;
-    const long long dearest = 2ll * v.max_beams * ((T + tokens - 1) / tokens) * (kTileCost * ((long long)v.max_pages * v.P / flash::kTok + 2) + kUnitCost + kRecCost);
+    const long long tiles = (long long)v.max_pages * v.P / flash::kTok + 2;
+    const long long dearest = 2 * v.max_beams * ((T + tokens - 1ll) / tokens) * (kTileCost * tiles + kUnitCost + kRecCost);
     int coarse = 0;
     while (dearest >> coarse >= 1 << 28) ++coarse;
     launch_pdl(k_draft_plan, 1, kListThreads, 0, s, v, w, d->parent_dev, d->count_dev, shift,
@@ -1274,14 +1275,18 @@ extern "C" gb_status gb_draft_attention(gb_pool* pool, int layer, const gb_draft
   if (bf16) {
     e = set_max_dynamic_smem(reinterpret_cast<const void*>(k_draft), flash::kSmem);
     if (e == cudaSuccess) e = launch_pdl(k_draft, pool->num_sms, flash::kThreads, flash::kSmem, s, job);
-    if (e == cudaSuccess) e = launch_pdl(sparse ? k_draft_merge<__nv_bfloat16, 128, 8> : k_draft_merge<__nv_bfloat16, 128, 4>, merge, 256, 0, s, v, w, job.o);
+    if (e == cudaSuccess)
+      e = launch_pdl(sparse ? k_draft_merge<__nv_bfloat16, 128, 8> : k_draft_merge<__nv_bfloat16, 128, 4>, merge, 256, 0, s, v,
+                     w, job.o);
   } else {
     e = set_max_dynamic_smem(reinterpret_cast<const void*>(k_draft_f32), (int)sizeof(TileSmem));
     if (e == cudaSuccess)
       e = launch_pdl(k_draft_f32, pool->num_sms, kTileThreads, sizeof(TileSmem), s, v, w, layer,
                      static_cast<const float*>(q_dev), static_cast<const float*>(k_dev), static_cast<const float*>(v_dev),
                      static_cast<float*>(out_dev), qscale);
-    if (e == cudaSuccess) e = launch_pdl(sparse ? k_draft_merge<float, 64, 8> : k_draft_merge<float, 64, 4>, merge, 256, 0, s, v, w, static_cast<float*>(out_dev));
+    if (e == cudaSuccess)
+      e = launch_pdl(sparse ? k_draft_merge<float, 64, 8> : k_draft_merge<float, 64, 4>, merge, 256, 0, s, v, w,
+                     static_cast<float*>(out_dev));
   }
   pool->launches += 2;
   if (e != cudaSuccess) return fail(pool, GB_ERR_CUDA, cudaGetErrorString(e));

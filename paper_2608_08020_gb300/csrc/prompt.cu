@@ -365,8 +365,8 @@ extern "C" gb_status gb_prompt_attention(const gb_prompt_args* a, gb_stream_t st
   // one and a half units per SM: 1300 tokens of 8 KV heads 25.5 -> 22.2 us, 1600 tokens 29.9 -> 27.7, but 2000 tokens 34.7 -> 36.1.
   const int few = a->dtype == GB_BF16 ? 3 * sms / (2 * a->num_kv_heads) : 0;
   const long long most = max_units(a->dtype, G, a->num_tokens, a->num_seqs);
-  PromptView view{ctl, a->cu_seqlens, (int)most, a->num_seqs, tokens, few ? flash::kRows / G : tokens, few, a->num_kv_heads, G, a->num_tokens, a->scale * 1.4426950408889634f,
-                  a->q_stride, a->k_stride, a->v_stride, a->out_stride};
+  PromptView view{ctl, a->cu_seqlens, (int)most, a->num_seqs, tokens, few ? flash::kRows / G : tokens, few,
+                  a->num_kv_heads, G, a->num_tokens, a->scale * 1.4426950408889634f, a->q_stride, a->k_stride, a->v_stride, a->out_stride};
   if (a->dtype == GB_BF16 && !flash::launches_with(reinterpret_cast<const void*>(k_prompt))) return GB_ERR_UNSUPPORTED;
   // The tensor maps first: nothing is enqueued when one cannot be made.
   PromptJob job;
