@@ -1220,7 +1220,10 @@ extern "C" gb_status gb_draft_attention(gb_pool* pool, int layer, const gb_draft
   // A captured plan is made when its graph runs: it serves the calls of the same capture only.
   cudaStreamCaptureStatus capturing = cudaStreamCaptureStatusNone;
   unsigned long long capture = 0;
-  if (cudaStreamGetCaptureInfo(s, &capturing, &capture) != cudaSuccess) return check_launch(pool, "draft: capture");
+  if (const cudaError_t e = cudaStreamGetCaptureInfo(s, &capturing, &capture); e != cudaSuccess) {
+    cudaGetLastError();
+    return fail(pool, GB_ERR_CUDA, cudaGetErrorString(e));
+  }
   if (capturing != cudaStreamCaptureStatusActive) capture = 0;
   if (layer > 0 && (pool->draft_epoch != pool->epoch || pool->draft_ws != d->workspace_dev || pool->draft_tokens != T ||
                     pool->draft_capture != capture))
