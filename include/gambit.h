@@ -575,6 +575,8 @@ gb_status gb_draft_workspace_bytes(gb_pool* pool, int n_draft, size_t* bytes);
  * result, whatever they are.  The pool's contexts are not changed.
  * Layer 0 plans the round; the other layers may follow in any order, and again, until the pool changes
  * (append, decode, accept, truncate, fork, prune, release); a plan captured into a graph serves that capture's calls.
+ * The host sees calls, not replays: when a replayed graph has changed the pool, or planned another round in this workspace, since
+ * the plan was made, a later layer computes nothing, leaves out_dev as it was and records GB_ERR_STATE in the device status.
  * Results are the same from call to call.  Launches: the attention and the join of its partial results, for layer 0 the
  * planner first (two launches in pools of more than 16 slots).
  * Errors: GB_ERR_INVALID for bad sizes, pointers or a scale that is not positive and finite; GB_ERR_STATE for an unseeded pool,

@@ -16,6 +16,7 @@
 // 16, 116 us with its plan and join (387 MB in 92 us inside the attention, 4.2 TB/s); 198 traces at 8000 tokens 258 us; a
 // layer of 128 traces of 190 tokens 46 us.
 #include <algorithm>
+#include <atomic>
 #include <type_traits>
 
 #include "flash.cuh"
@@ -30,7 +31,7 @@ constexpr int kTailRec = kMaxSegDepth;  // rec_off column of a beam's own units
 constexpr int kRecOffs = kMaxSegDepth + 1;
 
 // Workspace words of control.
-enum DraftCtl : int { kDrUnits = 0, kDrFew = 1, kDrWords = 64 };
+enum DraftCtl : int { kDrUnits = 0, kDrFew = 1, kDrChanges = 2, kDrToken = 4, kDrWords = 64 };
 
 struct DraftUnit {
   int seg;         // -1: a beam's own unit
@@ -83,6 +84,7 @@ DraftLayout draft_layout(const gb_pool_config& c, int num_sms, int T) {
 struct DraftView {
   int T, rows;              // tokens of a tree, rows of a beam and KV head (T x G)
   int rec_cap, max_units;
+  unsigned long long token; // the plan's name
   int* ctl;
   DraftUnit* units;
   unsigned long long* anc;  // [max_beams][T] ancestors and self
@@ -103,11 +105,12 @@ struct DraftView {
   float* rec;               // [rec_cap][Hkv][rows][D]
 };
 
-DraftView draft_view(const gb_pool* p, const DraftLayout& d, int T, void* ws) {
+DraftView draft_view(const gb_pool* p, const DraftLayout& d, int T, void* ws, unsigned long long token) {
   char* m = static_cast<char*>(ws);
   const size_t B = (size_t)p->cfg.max_beams;
   DraftView v{};
   v.T = T;
+  v.token = token;
   v.rows = ws_rows(p->cfg, T);
   v.rec_cap = d.rec_cap;
   v.max_units = d.max_units;
@@ -130,6 +133,26 @@ DraftView draft_view(const gb_pool* p, const DraftLayout& d, int T, void* ws) {
   v.ml = reinterpret_cast<float2*>(m + d.ml);
   v.rec = reinterpret_cast<float*>(m + d.rec);
   return v;
+}
+
+// Whether the workspace still holds the launch's own plan, of the pool as it is.  The host knows the calls, not the replays of
+// graphs, which change the pool or plan a round of their own in this workspace.
+__device__ __forceinline__ bool plan_holds(const PoolView& v, const DraftView& w) {
+  return *reinterpret_cast<const unsigned long long*>(w.ctl + kDrToken) == w.token && w.ctl[kDrChanges] == v.ctl[kCtlChanges];
+}
+
+// One warp, where the plan does not hold: says so, and leaves in its place one by which the join has nothing to write.  (A check
+// of its own would cost each of the join's many CTAs a load more: 36 layers 1657 -> 1690 us.)
+__device__ __forceinline__ void spoil_plan(const PoolView& v, const DraftView& w) {
+  const int lane = threadIdx.x & 31;
+  if (lane == 0) {
+    set_status(v.ctl, GB_ERR_STATE);
+    *reinterpret_cast<unsigned long long*>(w.ctl + kDrToken) = 0;
+  }
+  for (int b = lane; b < v.max_beams; b += 32) {
+    w.cnt[b] = w.T;
+    w.nrec[b] = 1;
+  }
 }
 
 // A warp's slot b: lane l's masks of tokens l and l + 32 (ancestors and self; 0 from `count` on), by
@@ -399,7 +422,11 @@ __global__ void __launch_bounds__(kListThreads) k_draft_plan(PoolView v, DraftVi
     per += 1 + per / 8;
     inv = 1.f / (float)per;
   }
-  if (tid == 0) w.ctl[kDrFew] = few;
+  if (tid == 0) {
+    w.ctl[kDrFew] = few;
+    w.ctl[kDrChanges] = v.ctl[kCtlChanges];
+    *reinterpret_cast<unsigned long long*>(w.ctl + kDrToken) = w.token;
+  }
 #pragma unroll 1
   for (;;) {
     mine = cnt > 0 ? pieces(tail) : 0;
@@ -539,8 +566,14 @@ struct DraftJob {
   __device__ __forceinline__ void error(int code) const { set_status(v.ctl, code); }
   struct Units {
     int count, few;
-    __device__ __forceinline__ explicit Units(const DraftJob& j) : count(j.w.ctl[kDrUnits]), few(j.w.ctl[kDrFew]) {}
+    __device__ __forceinline__ explicit Units(const DraftJob& j) : count(j.w.ctl[kDrUnits]), few(j.w.ctl[kDrFew]) {
+      count = plan_holds(j.v, j.w) ? count : 0;
+    }
   };
+  // A warp that has nothing to do yet, once what came before has completed.
+  __device__ __forceinline__ void begun() const {
+    if (blockIdx.x == 0 && !plan_holds(v, w)) spoil_plan(v, w);
+  }
   // Which rows share a unit, and where it stands in the list, follows the order in which segments were found, which may
   // differ from run to run: a row's result may not depend on it.  Where there are few units all of more than a tile are joint.
   __device__ __forceinline__ bool joins(const Units& all) const { return all.few != 0; }
@@ -774,7 +807,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_draft_f32(PoolView v, Draft
   pdl_launch_dependents();
   extern __shared__ __align__(16) unsigned char raw[];
   TileSmem& sm = *reinterpret_cast<TileSmem*>(raw);
-  const int total = w.ctl[kDrUnits] * v.Hkv;
+  const bool holds = plan_holds(v, w);
+  if (!holds && blockIdx.x == 0 && threadIdx.x < 32) spoil_plan(v, w);
+  const int total = holds ? w.ctl[kDrUnits] * v.Hkv : 0;
   for (int id = blockIdx.x; id < total; id += gridDim.x) {
     const DraftUnit u = w.units[id / v.Hkv];
     const int nctx = u.tok1 - u.tok0;
@@ -797,7 +832,8 @@ __global__ void __launch_bounds__(256) k_draft_merge(PoolView v, DraftView w, T*
   constexpr int per = D / 32;
   using Vec = typename std::conditional<per == 4, float4, float2>::type;
   const int lane = threadIdx.x & 31, i = blockIdx.x, b = blockIdx.y;
-  const int n = i < w.cnt[b] ? w.nrec[b] : 0;
+  const int there = w.cnt[b], records = w.nrec[b];  // (loaded together)
+  const int n = i < there ? records : 0;
   if (n == 1) return;
   const size_t step = (size_t)v.Hkv * w.rows;
   const size_t r1 = n > 0 ? (size_t)w.rec_base[b] * step + i * v.G : 0;
@@ -978,6 +1014,7 @@ __global__ void __launch_bounds__(1024) k_accept_plan(PoolView v, DraftView w, c
     return s_pages[r];
   };
   if (!fails) {
+    if (tid == 0) v.ctl[kCtlChanges] += 1;
     if (cow) {
       const int p = page_of(0);
       atomicSub(&v.refcnt[tail], 1);
@@ -1145,6 +1182,7 @@ __global__ void __launch_bounds__(1024) k_truncate(PoolView v, const int* length
   if (tid == 0) {
     v.ctl[kCtlCowJobs] = total;
     v.ctl[kCtlSegStale] = stale;
+    v.ctl[kCtlChanges] += 1;
     if (total > 0) atomicSub(&v.ctl[kCtlFree], total);
   }
 }
@@ -1228,7 +1266,9 @@ extern "C" gb_status gb_draft_attention(gb_pool* pool, int layer, const gb_draft
   if (layer > 0 && (pool->draft_epoch != pool->epoch || pool->draft_ws != d->workspace_dev || pool->draft_tokens != T ||
                     pool->draft_capture != capture))
     return fail(pool, GB_ERR_STATE, "draft: layer 0 plans the round, on the pool as it is, in this workspace and graph");
-  const DraftView w = draft_view(pool, draft_layout(pool->cfg, pool->num_sms, T), T, d->workspace_dev);
+  static std::atomic<unsigned long long> plans{0};
+  const unsigned long long token = layer == 0 ? ++plans : pool->draft_token;
+  const DraftView w = draft_view(pool, draft_layout(pool->cfg, pool->num_sms, T), T, d->workspace_dev, token);
   const float qscale = scale * 1.4426950408889634f;
   DraftJob job;
   if (bf16) {
@@ -1270,6 +1310,7 @@ extern "C" gb_status gb_draft_attention(gb_pool* pool, int layer, const gb_draft
     pool->draft_epoch = pool->epoch;
     pool->draft_ws = d->workspace_dev;
     pool->draft_tokens = T;
+    pool->draft_token = token;
     pool->draft_capture = capture;
   }
   cudaError_t e;
@@ -1305,7 +1346,7 @@ extern "C" gb_status gb_accept_draft(gb_pool* pool, const gb_draft* d, const voi
   if (!k_dev || !v_dev || !accepted_dev || (((uintptr_t)k_dev | (uintptr_t)v_dev) & 15))
     return fail(pool, GB_ERR_INVALID, "accept: bad arguments");
   const DraftView w =
-      draft_view(pool, draft_layout(pool->cfg, pool->num_sms, d->n_draft), d->n_draft, d->workspace_dev);
+      draft_view(pool, draft_layout(pool->cfg, pool->num_sms, d->n_draft), d->n_draft, d->workspace_dev, 0);
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   launch_pdl(k_accept_plan, 1, 1024, 0, s, pool->view, w, d->parent_dev, d->count_dev, accepted_dev, count_out_dev,
              path_out_dev);

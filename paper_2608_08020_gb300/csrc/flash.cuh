@@ -770,6 +770,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       const uint32_t o_addr = tmem + kTmemO + ((uint32_t)((warp & 3) * 32) << 16);
       const float2* xch = reinterpret_cast<const float2*>(sm + kXch);
       uint32_t c[2] = {0, 0};  // each group's units so far
+      if (warp == kOutWarp) job.begun();
       for (int u = 0;; ++u) {
         const int slot = u & (kSlots - 1);
         if (!wait_or_abort(ctl + kBarSched + 8 * slot, (u / kSlots) & 1, abort_flag)) break;

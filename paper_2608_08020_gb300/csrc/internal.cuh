@@ -56,7 +56,8 @@ enum Ctl : int {
   kCtlTailShared = 22, // 1 when a partial tail page may be shared (set by seed and forks, cleared by the planner)
   kCtlSegStale = 23,   // 1 when the last truncation took pages that segments cover
   kCtlCounters = 24,   // words 24-26 and 28-30: the two counter sets of the attention launches (Counters)
-  kCtlWords = 32
+  kCtlChanges = 32,    // calls that changed the beams' contexts, counted as they run (a graph's replays too)
+  kCtlWords = 40
 };
 
 // Control words of a call on caller-owned rows: its kernels record errors in kCtlStatus, the last one
@@ -352,6 +353,7 @@ struct gb_pool {
   unsigned long long epoch = 0;             // calls that changed the beams' contexts
   unsigned long long draft_capture = 0;     // the graph capture it belongs to, 0: none
   unsigned long long draft_epoch = ~0ull;   // the epoch, workspace and tree size of the round planned last
+  unsigned long long draft_token = 0;       // and its plan's name, no other plan's in this process
   const void* draft_ws = nullptr;
   int draft_tokens = 0;
   unsigned long long launches = 0;          // kernels launched by this pool

@@ -464,6 +464,7 @@ __global__ void __launch_bounds__(1024) k_step_begin(PoolView v, int n_tokens, c
   }
   if (b == 0) {
     if (tails_shared) v.ctl[kCtlTailShared] = 0;
+    v.ctl[kCtlChanges] += 1;
     v.ctl[kCtlStepOk] = 1;
   }
 }
@@ -553,6 +554,7 @@ __global__ void __launch_bounds__(1024) k_release(PoolView v, const int* slots, 
   __shared__ int s_take[1024];
   __shared__ int s_bad;               // (entry << 3) | code of the first bad entry
   const int tid = threadIdx.x;
+  if (tid == 0) v.ctl[kCtlChanges] += 1;
   for (int base = 0; base < n; base += 1024) {
     s_first[tid] = 0x7fffffff;
     if (tid == 0) s_bad = 0x7fffffff;

@@ -129,6 +129,7 @@ struct PromptJob : PromptView {
   };
 
   __device__ __forceinline__ void error(int code) const { atomicCAS(&ctl[kPrStatus], GB_OK, code); }
+  __device__ __forceinline__ void begun() const {}
   using Units = PromptUnits;  // what the warp that takes the units holds
   __device__ __forceinline__ int total(const Units& all) const { return all.count * Hkv; }
   __device__ __forceinline__ int capacity() const { return most_units * Hkv; }

@@ -168,6 +168,7 @@ __global__ void __launch_bounds__(kTourThreads, 1) k_tournament(PoolView v, Tour
   if (blockIdx.x == 0 && tid < 2 * kSegLenBuckets) v.seg_hist[tid] = 0;
   if (blockIdx.x == 0 && tid == 0) {
     v.ctl[kCtlSegGen] += 1;  // this rebuild's generation, read by every CTA after the first barrier
+    v.ctl[kCtlChanges] += 1;
     v.ctl[kCtlSegAlloc] = 0;  // segments (high word of the pair) and member slots (low word)
     v.ctl[kCtlSegAlloc + 1] = 0;
     v.ctl[kCtlSegRowTok] = 0;
