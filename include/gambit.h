@@ -552,7 +552,8 @@ gb_status gb_prompt_status(const void* workspace_dev, int* device_status, gb_str
  *                a count out of range records GB_ERR_INVALID and is clamped
  *   n_draft:     1 .. 64, the second dimension of every array below
  *   workspace_dev: gb_draft_workspace_bytes, 256-byte aligned, the caller's; calls using one workspace
- *                must be ordered, and a round uses one
+ *                must be ordered, and a round uses one.  It is known by its address: memory that has held anything else
+ *                since a round's layer 0 is a new workspace, whose first call is a layer 0
  */
 typedef struct {
   const int32_t* parent_dev;

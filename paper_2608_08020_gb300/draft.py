@@ -25,6 +25,9 @@ class DraftTrees:
         self.device = self.workspace.device
         self._index = self.device.index
         self._args = B.GbDraft(workspace_dev=self.workspace.data_ptr(), workspace_bytes=n, n_draft=n_draft)
+        # Whether a round was ever planned here: the library knows a workspace by its address, which an object before this one may
+        # have had.
+        self._planned = False
         self.dtype = TORCH_DT[pool.kv_dtype]
         self.q_shape = (pool.max_beams, n_draft, c.num_q_heads, c.head_dim)
         self.kv_shape = (pool.max_beams, n_draft, c.num_kv_heads, c.head_dim)
@@ -47,6 +50,8 @@ class DraftTrees:
         """One layer: q [max_beams][n_draft][q heads][D], k and v [max_beams][n_draft][kv heads][D], parent int32
         [max_beams][n_draft] (-1: the context's end), count int32 [max_beams] (None: n_draft each); returns out, like q (a new
         one belongs to `stream`, which then has to be a torch.cuda.Stream or None)."""
+        if layer > 0 and not self._planned:
+            raise B.GambitError(B.GB_ERR_STATE, "draft: layer 0 plans the round")
         if out is None:
             out = torch.empty_like(q) if stream is None else B.new_on(stream, lambda: torch.empty_like(q))
         qs, ks, dt, dev = self.q_shape, self.kv_shape, self.dtype, self._index
@@ -58,6 +63,7 @@ class DraftTrees:
                 self._check(name, x, shape, dt)
         B.gb_draft_attention(self.pool.handle, layer, self._draft(parent, count), q.data_ptr(), k.data_ptr(), v.data_ptr(),
                              scale, out.data_ptr(), stream)
+        self._planned = self._planned or layer == 0
         return out
 
     def accept(self, k, v, parent, accepted, count=None, stream=None):

@@ -86,3 +86,24 @@ def test_a_replay_that_plans_in_the_same_workspace(cuda, dtype):
         assert x.pool.status() == B.GB_OK
         assert torch.equal(kept[0], trees.attention(0, q, k, v, flat, x.scale))
         assert torch.equal(kept[1], trees.attention(1, q, k, v, flat, x.scale))
+
+
+def test_an_object_at_the_address_of_one_before(cuda):
+    """A new object has no plan, whatever the object whose memory it got had planned and wherever that memory has been."""
+    from paper_2608_08020_gb300 import binding as B
+    from paper_2608_08020_gb300.draft import DraftTrees
+    x = Trees("bf16", layers=2, seed=23)
+    q, k, v, chain, _ = rounds(x, 4)
+    trees = DraftTrees(x.pool, 4)
+    trees.attention(0, q, k, v, chain, x.scale)
+    at = trees.workspace.data_ptr()
+    del trees
+    trees = DraftTrees(x.pool, 4)
+    assert trees.workspace.data_ptr() == at
+    launches = B.gb_pool_launch_count(x.pool.handle)
+    with pytest.raises(B.GambitError, match="GB_ERR_STATE"):
+        trees.attention(1, q, k, v, chain, x.scale)
+    assert B.gb_pool_launch_count(x.pool.handle) == launches and x.pool.status() == B.GB_OK
+    trees.attention(0, q, k, v, chain, x.scale)
+    trees.attention(1, q, k, v, chain, x.scale)
+    assert x.pool.status() == B.GB_OK
