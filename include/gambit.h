@@ -575,7 +575,8 @@ gb_status gb_draft_workspace_bytes(gb_pool* pool, int n_draft, size_t* bytes);
  * count on are zero in out_dev and ignored in the inputs; values that a row does not see do not reach its
  * result, whatever they are.  The pool's contexts are not changed.
  * Layer 0 plans the round; the other layers may follow in any order, and again, until the pool changes
- * (append, decode, accept, truncate, fork, prune, release); a plan captured into a graph serves that capture's calls.
+ * (append, decode, accept, truncate, fork, prune, release); a plan captured into a graph serves that capture's calls.  Rounds in
+ * workspaces of their own do not disturb each other (the pool keeps the last 16).
  * The host sees calls, not replays: when a replayed graph has changed the pool, or planned another round in this workspace, since
  * the plan was made, a later layer computes nothing, leaves out_dev as it was and records GB_ERR_STATE in the device status.
  * Results are the same from call to call.  Launches: the attention and the join of its partial results, for layer 0 the

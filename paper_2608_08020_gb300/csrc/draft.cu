@@ -1224,6 +1224,25 @@ bool meets(const void* a, size_t an, const void* b, size_t bn) {
   return x < y + bn && y < x + an;
 }
 
+// The round that a layer above 0 belongs to, or nullptr.
+const gb_pool::DraftPlan* find_plan(const gb_pool* pool, const void* ws, int tokens, unsigned long long capture) {
+  if (pool->draft_epoch != pool->epoch) return nullptr;
+  for (const gb_pool::DraftPlan& p : pool->draft_plans)
+    if (p.token && p.ws == ws && p.tokens == tokens && p.capture == capture) return &p;
+  return nullptr;
+}
+
+// Takes the place of the plans whose memory it shares; where all entries are taken the oldest gives way.
+void keep_plan(gb_pool* pool, const gb_pool::DraftPlan& plan) {
+  gb_pool::DraftPlan* oldest = pool->draft_plans;  // (names grow; an entry without a plan has 0)
+  for (gb_pool::DraftPlan& p : pool->draft_plans) {
+    if (pool->draft_epoch != pool->epoch || meets(p.ws, p.bytes, plan.ws, plan.bytes)) p = {};
+    if (p.token < oldest->token) oldest = &p;
+  }
+  *oldest = plan;
+  pool->draft_epoch = pool->epoch;
+}
+
 }  // namespace
 }  // namespace gb
 
@@ -1263,12 +1282,13 @@ extern "C" gb_status gb_draft_attention(gb_pool* pool, int layer, const gb_draft
     return fail(pool, GB_ERR_CUDA, cudaGetErrorString(e));
   }
   if (capturing != cudaStreamCaptureStatusActive) capture = 0;
-  if (layer > 0 && (pool->draft_epoch != pool->epoch || pool->draft_ws != d->workspace_dev || pool->draft_tokens != T ||
-                    pool->draft_capture != capture))
+  const gb_pool::DraftPlan* planned = layer > 0 ? find_plan(pool, d->workspace_dev, T, capture) : nullptr;
+  if (layer > 0 && !planned)
     return fail(pool, GB_ERR_STATE, "draft: layer 0 plans the round, on the pool as it is, in this workspace and graph");
   static std::atomic<unsigned long long> plans{0};
-  const unsigned long long token = layer == 0 ? ++plans : pool->draft_token;
-  const DraftView w = draft_view(pool, draft_layout(pool->cfg, pool->num_sms, T), T, d->workspace_dev, token);
+  const unsigned long long token = planned ? planned->token : ++plans;
+  const DraftLayout layout = draft_layout(pool->cfg, pool->num_sms, T);
+  const DraftView w = draft_view(pool, layout, T, d->workspace_dev, token);
   const float qscale = scale * 1.4426950408889634f;
   DraftJob job;
   if (bf16) {
@@ -1307,11 +1327,7 @@ extern "C" gb_status gb_draft_attention(gb_pool* pool, int layer, const gb_draft
       pool->launches += 1;
     }
     if ((st = check_launch(pool, "draft_plan")) != GB_OK) return st;
-    pool->draft_epoch = pool->epoch;
-    pool->draft_ws = d->workspace_dev;
-    pool->draft_tokens = T;
-    pool->draft_token = token;
-    pool->draft_capture = capture;
+    keep_plan(pool, {d->workspace_dev, layout.total, T, capture, token});
   }
   cudaError_t e;
   const bool sparse = (long long)T * v.max_beams < 2 * pool->num_sms;

@@ -351,11 +351,16 @@ struct gb_pool {
   int tmap_oob = 0;                          // first row group past the tensor map (loads zeros)
   std::string last_error;
   unsigned long long epoch = 0;             // calls that changed the beams' contexts
-  unsigned long long draft_capture = 0;     // the graph capture it belongs to, 0: none
-  unsigned long long draft_epoch = ~0ull;   // the epoch, workspace and tree size of the round planned last
-  unsigned long long draft_token = 0;       // and its plan's name, no other plan's in this process
-  const void* draft_ws = nullptr;
-  int draft_tokens = 0;
+  // The rounds of drafts planned since `epoch` was draft_epoch (draft.cu): the latest in each workspace.
+  static constexpr int kDraftPlans = 16;
+  struct DraftPlan {
+    const void* ws = nullptr;
+    size_t bytes = 0;                       // of it that the plan's layout takes
+    int tokens = 0;                         // of a tree
+    unsigned long long capture = 0;         // the graph capture it belongs to, 0: none
+    unsigned long long token = 0;           // its name, no other plan's in this process; 0: no plan
+  } draft_plans[kDraftPlans];
+  unsigned long long draft_epoch = ~0ull;
   unsigned long long launches = 0;          // kernels launched by this pool
   cudaEvent_t prof_start[GB_PROF_SLOTS] = {};  // caller-owned instrumentation events
   cudaEvent_t prof_stop[GB_PROF_SLOTS] = {};

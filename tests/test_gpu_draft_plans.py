@@ -107,3 +107,58 @@ def test_an_object_at_the_address_of_one_before(cuda):
     trees.attention(0, q, k, v, chain, x.scale)
     trees.attention(1, q, k, v, chain, x.scale)
     assert x.pool.status() == B.GB_OK
+
+
+def test_rounds_side_by_side(cuda):
+    """Rounds in workspaces of their own, their layers by turns, one of them of shorter trees."""
+    import torch
+    from paper_2608_08020_gb300 import binding as B
+    from paper_2608_08020_gb300.draft import DraftTrees
+    x = Trees("bf16", layers=3, seed=24)
+    a, b = DraftTrees(x.pool, 4), DraftTrees(x.pool, 3)
+    qa, ka, va, chain, flat = rounds(x, 4)
+    qb, kb, vb, short, _ = rounds(x, 3)
+    want_a = [a.attention(layer, qa, ka, va, flat, x.scale) for layer in range(3)]
+    want_b = [b.attention(layer, qb, kb, vb, short, x.scale) for layer in range(3)]
+    got_a, got_b = [a.attention(0, qa, ka, va, flat, x.scale)], [b.attention(0, qb, kb, vb, short, x.scale)]
+    for layer in (1, 2):
+        got_a.append(a.attention(layer, qa, ka, va, flat, x.scale))
+        got_b.append(b.attention(layer, qb, kb, vb, short, x.scale))
+    assert all(torch.equal(g, w) for g, w in zip(got_a + got_b, want_a + want_b))
+    many = [DraftTrees(x.pool, 4) for _ in range(17)]
+    for m in many:
+        m.attention(0, qa, ka, va, chain, x.scale)
+    for m in many[1:]:
+        m.attention(1, qa, ka, va, chain, x.scale)
+    with pytest.raises(B.GambitError, match="GB_ERR_STATE"):
+        many[0].attention(1, qa, ka, va, chain, x.scale)
+    assert x.pool.status() == B.GB_OK
+    x.append(1)
+    for m in (a, b, many[5]):
+        q, k, v = (qb, kb, vb) if m is b else (qa, ka, va)
+        with pytest.raises(B.GambitError, match="GB_ERR_STATE"):
+            m.attention(1, q, k, v, short if m is b else chain, x.scale)
+    a.attention(0, qa, ka, va, chain, x.scale)
+    a.attention(1, qa, ka, va, chain, x.scale)
+    assert x.pool.status() == B.GB_OK
+
+
+def test_workspaces_that_overlap(cuda):
+    """A plan whose memory another one's shares gives way to it."""
+    import torch
+    from paper_2608_08020_gb300 import binding as B
+    x = Trees("bf16", layers=2, seed=25)
+    q, k, v, chain, _ = rounds(x, 4)
+    n = B.gb_draft_workspace_bytes(x.pool.handle, 4)
+    memory, out = torch.empty(n + 256, dtype=torch.uint8, device="cuda"), torch.empty_like(q)
+
+    def attention(layer, at):
+        d = B.GbDraft(parent_dev=chain.data_ptr(), workspace_dev=memory.data_ptr() + at, workspace_bytes=n, n_draft=4)
+        B.gb_draft_attention(x.pool.handle, layer, d, q, k, v, x.scale, out)
+
+    attention(0, 0)
+    attention(0, 256)
+    with pytest.raises(B.GambitError, match="GB_ERR_STATE"):
+        attention(1, 0)
+    attention(1, 256)
+    assert x.pool.status() == B.GB_OK
