@@ -228,7 +228,8 @@ inline bool launches_with(const void* kernel) try {
 } catch (...) {
   return false;
 }
-// A whole warp's wait_or_abort, whose lanes stay together.
+// A warp's wait: all lanes go on or, when it ran out or the CTA gave up meanwhile, none does.  (What follows takes whole warps:
+// lanes that part company here would wait for each other for ever.)
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
   uint64_t t0 = 0;
   for (uint32_t it = 1;; ++it) {
@@ -242,6 +243,11 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatil
       }
     }
   }
+}
+// The same with the lanes apart meanwhile, for the warps that write (8192 tokens: 384 us so, 388 with the other here too, 391 with
+// this one for the softmax too).
+__device__ __forceinline__ bool lanes_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  return __all_sync(0xffffffffu, wait_or_abort(bar, parity, abort_flag));
 }
 // One lane of the warp, the same each time.
 __device__ __forceinline__ bool elect_one() {
@@ -413,7 +419,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
         const uint32_t bar = ctl + kBarSched + 8 * slot, parity = (u_next / kSlots) & 1;
         if (!patient) {
           if (!__all_sync(0xffffffffu, mbar_test(bar, parity))) return true;
-        } else if (!wait_or_abort(bar, parity, abort_flag)) {
+        } else if (!warp_wait(bar, parity, abort_flag)) {
           return false;
         }
         if (units[slot].nt < 0) break;
@@ -453,7 +459,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       known = false;
       for (int i = 0; i < mine; ++i, ++n) {
         const int t = group_tile(mode, g, i);
-        if (!wait_or_abort(ctl + kBarS + 8 * g, n & 1, abort_flag)) { alive = false; break; }
+        if (!warp_wait(ctl + kBarS + 8 * g, n & 1, abort_flag)) { alive = false; break; }
         if (Job::kEarlyQ && i + 1 == mine && !(alive = begin_next(false))) break;
         tc_fence_after();
         uint32_t su[128];
@@ -527,7 +533,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       if (!(alive = begin_next(true))) break;
       if (units[sy].nt >= 0) job.loaded_q(r, ctl + kBarQ + 8 * g);
       // (m, l) go to the warps that write, once they have those of the group's unit before.
-      if (c_done > 0 && !(alive = wait_or_abort(ctl + kBarOFree + 8 * g, (c_done - 1) & 1, abort_flag))) break;
+      if (c_done > 0 && !(alive = warp_wait(ctl + kBarOFree + 8 * g, (c_done - 1) & 1, abort_flag))) break;
       ++c_done;
       xch[g * 128 + r] = make_float2(m_ref, l);
       __syncwarp();
@@ -773,7 +779,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       if (warp == kOutWarp) job.begun();
       for (int u = 0;; ++u) {
         const int slot = u & (kSlots - 1);
-        if (!wait_or_abort(ctl + kBarSched + 8 * slot, (u / kSlots) & 1, abort_flag)) break;
+        if (!lanes_wait(ctl + kBarSched + 8 * slot, (u / kSlots) & 1, abort_flag)) break;
         const Unit& x = units[slot];
         const int mode = x.mode;
         if (x.nt < 0) break;
@@ -782,7 +788,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
         if (mode == kJoint) {  // the two groups' sums
           job.find_row(x, 0, r, row);
           for (int g = 0; g < 2 && ok; ++g)
-            ok = wait_or_abort(ctl + kBarML + 8 * g, c[g] & 1, abort_flag) && wait_or_abort(ctl + kBarO + 8 * g, c[g] & 1, abort_flag);
+            ok = lanes_wait(ctl + kBarML + 8 * g, c[g] & 1, abort_flag) && lanes_wait(ctl + kBarO + 8 * g, c[g] & 1, abort_flag);
           if (!ok) break;
           const float2 p = xch[r], q = xch[128 + r];
           const float m = fmaxf(p.x, q.x), ref = m == -INFINITY ? 0.f : m, wp = exp2f(p.x - ref), wq = exp2f(q.x - ref);
@@ -798,7 +804,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
           for (int g = 0; g < 2; ++g) {
             if (!takes_part(mode, g)) continue;
             job.find_row(x, g, r, row);
-            ok = wait_or_abort(ctl + kBarML + 8 * g, c[g] & 1, abort_flag) && wait_or_abort(ctl + kBarO + 8 * g, c[g] & 1, abort_flag);
+            ok = lanes_wait(ctl + kBarML + 8 * g, c[g] & 1, abort_flag) && lanes_wait(ctl + kBarO + 8 * g, c[g] & 1, abort_flag);
             if (!ok) break;
             const float2 p = xch[g * 128 + r];
             tc_fence_after();
