@@ -750,7 +750,7 @@ struct DraftJob {
       }
     }
   }
-  __device__ __forceinline__ void drain_q(uint32_t, bool) const { asm volatile("cp.async.wait_all;" ::: "memory"); }
+  __device__ __forceinline__ void drain_q(uint32_t) const { asm volatile("cp.async.wait_all;" ::: "memory"); }
 };
 
 // A CTA per SM; what bounds it and its figures: the file's head, and flash.cuh for the split.

@@ -33,8 +33,8 @@
 // P overwrites the first half of its S tile.  O is rescaled by its own group, and only when a maximum
 // grows by more than 8 (p <= 2^8 meanwhile): when S(i) is complete so is P.V(i - 1), issued before it.
 //
-// Every wait is bounded; when one runs out the CTA records the timeout, every role stops issuing and waits
-// (bounded) for its own copies and products, the tensor memory is freed and the CTA leaves.
+// Every wait is bounded; when one runs out the CTA records the timeout, every role stops issuing and, once all have, waits
+// (bounded) for its own copies and products, then the tensor memory is freed and the CTA leaves.
 #pragma once
 #include <cuda.h>
 #include <mutex>
@@ -82,12 +82,19 @@ constexpr int kBarP = kBarS + 16;                 // [2 groups][2 halves] P of 6
 constexpr int kBarO = kBarP + 32;                 // [2] the unit's last P.V of the group is complete
 constexpr int kBarOFree = kBarO + 16;             // [2] the group's O has been read
 constexpr int kBarML = kBarOFree + 16;            // [2] the group's (m, l) are in
-constexpr int kBarPatch = kBarML + 16;            // a V tile that is mended before it is handed on
+constexpr int kBarDrained = kBarML + 16;          // [2] all of the group's products are complete (given up)
+constexpr int kBarPatch = kBarDrained + 16;       // a V tile that is mended before it is handed on
 constexpr int kBarSched = kBarPatch + 8;          // [kSlots]
 constexpr int kBarBegin = kBarSched + 8 * kSlots;  // [kSlots] K of the unit is on its way
 constexpr int kBarSchedFree = kBarBegin + 8 * kSlots;
 constexpr int kUnits = (kBarSchedFree + 8 * kSlots + 15) / 16 * 16;  // int [kSlots][kUnitWords]
-constexpr int kWordTmem = kUnits + 4 * kSlots * kUnitWords;
+// What the K and the V warp may have in flight at their end: the position loaded last, bit i of `seen` for the load i positions
+// before it, and of a V tile that waits to be mended its full barrier (else 0) and the patch barrier's phase.
+struct Flight {
+  uint32_t last, seen, patched, patch_parity;
+};
+constexpr int kFlights = kUnits + 4 * kSlots * kUnitWords;  // Flight [2]
+constexpr int kWordTmem = kFlights + 2 * (int)sizeof(Flight);
 constexpr int kWordAbort = kWordTmem + 4;
 static_assert(kUnits % 16 == 0 && kWordAbort + 4 <= 1024, "control area");
 constexpr int kSchedReaders = 15;  // eight softmax warps, two that issue products, one that loads V, four that write
@@ -358,6 +365,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
   const uint32_t sbase = smem_addr(sm), ctl = sbase + kBar;
   volatile int* abort_flag = reinterpret_cast<volatile int*>(sm + kBar + kWordAbort);
   Unit* units = reinterpret_cast<Unit*>(sm + kBar + kUnits);
+  Flight* flight = reinterpret_cast<Flight*>(sm + kBar + kFlights);
   if (sbase & 1023) {  // the swizzled layouts need a 1024-byte aligned base
     if (tid == 0) job.error(GB_ERR_UNSUPPORTED);
     return;
@@ -375,6 +383,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       mbar_init(ctl + kBarO + 8 * i, 1);
       mbar_init(ctl + kBarOFree + 8 * i, 4);
       mbar_init(ctl + kBarML + 8 * i, 4);
+      mbar_init(ctl + kBarDrained + 8 * i, 1);
     } else if (lane < kFulls + 2 + kSlots) {
       const int i = lane - kFulls - 2;
       mbar_init(ctl + kBarSched + 8 * i, 1);
@@ -543,7 +552,6 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       sx = sy;
       row = row_y;
     }
-    job.drain_q(ctl + kBarQ + 8 * g, *abort_flag != 0);
   } else {
     regs_dec<kOtherRegs>();
     if (warp == kKWarp) {
@@ -648,10 +656,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
         last = from - 2;
         seen = 0x155u & ((1u << min(from, 31u)) - 1);
       }
-      if (lane == 0 && *abort_flag)  // copies in flight land before the CTA leaves (bounded)
-        for (uint32_t i = 0; i < 2 * kStages; ++i)
-          if ((seen >> i) & 1)
-            mbar_wait_bounded(ctl + kBarFull + 8 * ((last - i) % kFulls), ((last - i) / kFulls) & 1, kWaitLimitNs / 8);
+      if (lane == 0) flight[0] = {last, seen, 0, 0};
     } else if (warp == kVWarp) {
       // ---------------------------------------------------------------- V tiles
       uint32_t from = 0, last = 0, seen = 0;  // as above
@@ -763,13 +768,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
         last = from - 1;
         seen = 0x155u & ((1u << min(from, 31u)) - 1);
       }
-      // Copies in flight land before the CTA leaves (bounded).
-      if (lane == 0 && *abort_flag) {
-        if (z0 < z1) mbar_wait_bounded(ctl + kBarPatch, patches & 1, kWaitLimitNs / 8);
-        for (uint32_t i = 0; i < 2 * kStages; ++i)
-          if (((seen >> i) & 1) && (ctl + kBarFull + 8 * ((last - i) % kFulls) != p_full || z0 >= z1))
-            mbar_wait_bounded(ctl + kBarFull + 8 * ((last - i) % kFulls), ((last - i) / kFulls) & 1, kWaitLimitNs / 8);
-      }
+      if (lane == 0) flight[1] = {last, seen, z0 < z1 ? p_full : 0, patches & 1};
     } else if (warp >= kOutWarp) {
       // ---------------------------------------------------------------- results
       const int r = tid & 127;
@@ -906,14 +905,34 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
         }
         ++c;
       }
-      if (leader && *abort_flag && n > 0)  // products in flight end before the tensor memory is freed (bounded)
-        mbar_wait_bounded(bars + kBarS + 8 * g, (n - 1) & 1, kWaitLimitNs / 8);
-      __syncwarp();
     }
   }
   if (*abort_flag && tid == 0) job.error(GB_ERR_TIMEOUT);
   tc_fence_before();
   __syncthreads();
+  // Given up: no role issues anything more.  What each has in flight ends before the tensor memory is freed and the CTA leaves
+  // (bounded).  (Only here does every role know: one that came to its end before another gave up would have looked too early.)
+  if (*abort_flag) {
+    if (warp < kKWarp) {
+      job.drain_q(ctl + kBarQ + 8 * (warp >> 2));
+    } else if ((warp == kKWarp || warp == kVWarp) && lane == 0) {
+      const Flight f = flight[warp == kVWarp];
+      if (f.patched) mbar_wait_bounded(ctl + kBarPatch, f.patch_parity, kWaitLimitNs / 8);
+      for (uint32_t i = 0; i < 2 * kStages; ++i) {
+        const uint32_t bar = ctl + kBarFull + 8 * ((f.last - i) % kFulls);
+        if (((f.seen >> i) & 1) && bar != f.patched) mbar_wait_bounded(bar, ((f.last - i) / kFulls) & 1, kWaitLimitNs / 8);
+      }
+    } else if (warp == kMmaWarp || warp == kMmaWarp + 1) {
+      // (a commit by the lane that issued them stands for all its products, S and P.V)
+      const uint32_t bar = ctl + kBarDrained + 8 * (warp - kMmaWarp);
+      if (elect_one()) {
+        mma_commit(bar);
+        mbar_wait_bounded(bar, 0, kWaitLimitNs / 8);
+      }
+      __syncwarp();
+    }
+    __syncthreads();
+  }
   tc_fence_after();
   if (warp == kMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));
 }

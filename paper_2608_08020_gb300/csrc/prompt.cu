@@ -230,9 +230,9 @@ struct PromptJob : PromptView {
         o[(s0 + tok) * out_stride + head * flash::kD + 4 * (threadIdx.x & 31) + i] = __float2bfloat16(acc[i] * ir);
     }
   }
-  __device__ __forceinline__ void drain_q(uint32_t bar, bool aborted) const {
-    // A copy in flight lands before the CTA leaves; without one the barrier's last phase passes at once.
-    if (aborted && (threadIdx.x & 127) == 0) {
+  __device__ __forceinline__ void drain_q(uint32_t bar) const {
+    // A copy in flight lands before the CTA leaves; without one the barrier's last phase passes at once and the other runs out.
+    if ((threadIdx.x & 127) == 0) {
       mbar_wait_bounded(bar, 0, kWaitLimitNs / 16);
       mbar_wait_bounded(bar, 1, kWaitLimitNs / 16);
     }
