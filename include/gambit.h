@@ -539,6 +539,14 @@ gb_status gb_prompt_attention(const gb_prompt_args* args, gb_stream_t stream);
 gb_status gb_prompt_status(const void* workspace_dev, int* device_status, gb_stream_t stream);
 
 /*
+ * Diagnostic of the failure path (not part of the method): gb_prompt_attention in GB_BF16, but one load never comes and the
+ * kernel's waits have a limit of 50 ms.  stalled: 0 the K, 1 the V of every unit's tile `at` (128 keys each), 2 the query rows of
+ * the units that begin with a sequence's token `at`.  The CTAs that wait for it give up and leave the rest of their rows as they
+ * were, the workspace's status becomes GB_ERR_TIMEOUT, and the context and the workspace stay usable.
+ */
+gb_status gb_prompt_wait_selftest(const gb_prompt_args* args, int stalled, int at, gb_stream_t stream);
+
+/*
  * Trees of drafted tokens (speculative decoding over the beams).  A round: a drafter proposes up to
  * n_draft tokens for every active slot, each the continuation of the context or of an earlier
  * drafted token; the model runs them all at once (gb_draft_attention, layer by layer); the caller picks a

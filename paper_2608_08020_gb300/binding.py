@@ -29,7 +29,7 @@ EXPORTS = ["gb_pool_workspace_bytes", "gb_pool_init", "gb_pool_destroy", "gb_poo
            "gb_append_kv", "gb_score_probe", "gb_push_scores", "gb_prune_branch", "gb_release", "gb_pool_status",
            "gb_pool_clear_status", "gb_pool_wait_selftest", "gb_pool_read_state", "gb_pool_set_profile_events", "gb_pool_launch_count",
            "gb_paged_decode_noalloc", "gb_paged_decode_noalloc_status", "gb_pool_read_step_stats", "gb_pool_set_capacity", "gb_pool_last_ranked", "gb_score_mlp", "gb_fork_slots", "gb_scorer_sizes", "gb_scorer_seed",
-           "gb_scorer_step", "gb_prompt_workspace_bytes", "gb_prompt_attention", "gb_prompt_status",
+           "gb_scorer_step", "gb_prompt_workspace_bytes", "gb_prompt_attention", "gb_prompt_status", "gb_prompt_wait_selftest",
            "gb_draft_workspace_bytes", "gb_draft_attention", "gb_accept_draft", "gb_truncate", "gb_last_error"]
 GB_PROF_DECODE, GB_PROF_PROBE, GB_PROF_PRUNE, GB_PROF_GROUPED = 0, 1, 2, 3
 GB_PROF_PLAN, GB_PROF_APPEND, GB_PROF_COMBINE, GB_PROF_ATTENTION = 4, 5, 6, 7
@@ -120,6 +120,7 @@ def load(path: Path | None = None) -> ctypes.CDLL:
         "gb_prompt_workspace_bytes": [I, I, I, I, I, I, P],
         "gb_prompt_attention": [P, V],
         "gb_prompt_status": [V, P, V],
+        "gb_prompt_wait_selftest": [P, I, I, V],
         "gb_draft_workspace_bytes": [V, I, P],
         "gb_draft_attention": [V, I, P, V, V, V, F, V, V],
         "gb_accept_draft": [V, P, V, V, V, V, V, V],
@@ -384,6 +385,10 @@ def gb_prompt_status(workspace, stream=None) -> int:
     st = ctypes.c_int()
     _check(None, load().gb_prompt_status(ptr(workspace), ctypes.byref(st), stream_handle(stream)), "gb_prompt_status")
     return st.value
+
+
+def gb_prompt_wait_selftest(args: GbPromptArgs, stalled: int, at: int, stream=None) -> None:
+    _check(None, load().gb_prompt_wait_selftest(ctypes.byref(args), stalled, at, stream_handle(stream)), "gb_prompt_wait_selftest")
 
 
 def gb_draft_workspace_bytes(pool: int, n_draft: int) -> int:

@@ -548,6 +548,7 @@ struct DraftJob {
   const __nv_bfloat16 *q, *k, *vv;  // this layer's [max_beams][T][heads][128]
   __nv_bfloat16* o;
 
+  static constexpr uint64_t kWaitNs = kWaitLimitNs;
   static constexpr bool kEarlyQ = true;
   // 64 traces x 4k 260 -> 240 us, 198 x 8k 295 -> 265; from two tiles on, 128 traces of 2 and 3 tiles a unit 1663 -> 1736 us.
   static constexpr int kLongPair = 4;

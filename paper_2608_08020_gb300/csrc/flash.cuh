@@ -237,6 +237,7 @@ inline bool launches_with(const void* kernel) try {
 }
 // A warp's wait: all lanes go on or, when it ran out or the CTA gave up meanwhile, none does.  (What follows takes whole warps:
 // lanes that part company here would wait for each other for ever.)
+template <class Job>
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
   uint64_t t0 = 0;
   for (uint32_t it = 1;; ++it) {
@@ -244,7 +245,7 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatil
     if ((it & 63) == 0) {
       const uint64_t now = globaltimer_ns();
       if (t0 == 0) t0 = now;
-      if (__any_sync(0xffffffffu, *abort_flag != 0 || now - t0 > kWaitLimitNs)) {
+      if (__any_sync(0xffffffffu, *abort_flag != 0 || now - t0 > Job::kWaitNs)) {
         *abort_flag = 1;
         return false;
       }
@@ -253,8 +254,9 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatil
 }
 // The same with the lanes apart meanwhile, for the warps that write (8192 tokens: 384 us so, 388 with the other here too, 391 with
 // this one for the softmax too).
+template <class Job>
 __device__ __forceinline__ bool lanes_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
-  return __all_sync(0xffffffffu, wait_or_abort(bar, parity, abort_flag));
+  return __all_sync(0xffffffffu, wait_or_abort(bar, parity, abort_flag, Job::kWaitNs));
 }
 // One lane of the warp, the same each time.
 __device__ __forceinline__ bool elect_one() {
@@ -367,6 +369,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
   Unit* units = reinterpret_cast<Unit*>(sm + kBar + kUnits);
   Flight* flight = reinterpret_cast<Flight*>(sm + kBar + kFlights);
   if (sbase & 1023) {  // the swizzled layouts need a 1024-byte aligned base
+    pdl_wait();
     if (tid == 0) job.error(GB_ERR_UNSUPPORTED);
     return;
   }
@@ -428,7 +431,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
         const uint32_t bar = ctl + kBarSched + 8 * slot, parity = (u_next / kSlots) & 1;
         if (!patient) {
           if (!__all_sync(0xffffffffu, mbar_test(bar, parity))) return true;
-        } else if (!warp_wait(bar, parity, abort_flag)) {
+        } else if (!warp_wait<Job>(bar, parity, abort_flag)) {
           return false;
         }
         if (units[slot].nt < 0) break;
@@ -468,7 +471,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       known = false;
       for (int i = 0; i < mine; ++i, ++n) {
         const int t = group_tile(mode, g, i);
-        if (!warp_wait(ctl + kBarS + 8 * g, n & 1, abort_flag)) { alive = false; break; }
+        if (!warp_wait<Job>(ctl + kBarS + 8 * g, n & 1, abort_flag)) { alive = false; break; }
         if (Job::kEarlyQ && i + 1 == mine && !(alive = begin_next(false))) break;
         tc_fence_after();
         uint32_t su[128];
@@ -542,7 +545,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       if (!(alive = begin_next(true))) break;
       if (units[sy].nt >= 0) job.loaded_q(r, ctl + kBarQ + 8 * g);
       // (m, l) go to the warps that write, once they have those of the group's unit before.
-      if (c_done > 0 && !(alive = warp_wait(ctl + kBarOFree + 8 * g, (c_done - 1) & 1, abort_flag))) break;
+      if (c_done > 0 && !(alive = warp_wait<Job>(ctl + kBarOFree + 8 * g, (c_done - 1) & 1, abort_flag))) break;
       ++c_done;
       xch[g * 128 + r] = make_float2(m_ref, l);
       __syncwarp();
@@ -573,7 +576,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       };
       auto publish = [&](int u, const Unit& x) {
         const int slot = u & (kSlots - 1);
-        if (u >= kSlots) ok = warp_wait(ctl + kBarSchedFree + 8 * slot, (u / kSlots - 1) & 1, abort_flag);
+        if (u >= kSlots) ok = warp_wait<Job>(ctl + kBarSchedFree + 8 * slot, (u / kSlots - 1) & 1, abort_flag);
         if (ok && lane == 0) {
           units[slot] = x;
           mbar_arrive(ctl + kBarSched + 8 * slot);
@@ -586,7 +589,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       auto load = [&](const Unit& z, const Places& at, int j, int page) {
         const uint32_t n = Job::kLongPair > 0 ? from + at.k(j) : from, st = n % kStages;
         if (n >= (uint32_t)kStages)
-          ok = warp_wait(ctl + kBarEmpty + 8 * ((n - kStages) % kFulls), ((n - kStages) / kFulls) & 1, abort_flag);
+          ok = warp_wait<Job>(ctl + kBarEmpty + 8 * ((n - kStages) % kFulls), ((n - kStages) / kFulls) & 1, abort_flag);
         if (!ok) return;
         const uint32_t bar = ctl + kBarFull + 8 * (n % kFulls);
         if (lane == 0) mbar_arrive_expect_tx(bar, kTile);
@@ -667,7 +670,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       auto fetch = [&](int u, Unit& to) {
         const int slot = u & (kSlots - 1);
         to.nt = -1;
-        if (!(ok = warp_wait(ctl + kBarSched + 8 * slot, (u / kSlots) & 1, abort_flag))) return;
+        if (!(ok = warp_wait<Job>(ctl + kBarSched + 8 * slot, (u / kSlots) & 1, abort_flag))) return;
         to = units[slot];
         __syncwarp();
         if (lane == 0) mbar_arrive(ctl + kBarSchedFree + 8 * slot);
@@ -685,7 +688,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       };
       // A stage's release, or with `landed` only the tile to be mended, which meanwhile is mended as soon as it is in.
       auto wait = [&](uint32_t bar, uint32_t parity, bool landed) {
-        if (z0 >= z1) return warp_wait(bar, parity, abort_flag);  // (a suspended wait leaves the issue slots to others)
+        if (z0 >= z1) return warp_wait<Job>(bar, parity, abort_flag);  // (a suspended wait leaves the issue slots to others)
         uint64_t t0 = 0;
         for (uint32_t it = 1;; ++it) {
           int f = 0;
@@ -695,7 +698,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
             else if ((it & 63) == 0) {
               const uint64_t now = globaltimer_ns();
               if (t0 == 0) t0 = now;
-              if (*abort_flag || now - t0 > kWaitLimitNs) {
+              if (*abort_flag || now - t0 > Job::kWaitNs) {
                 *abort_flag = 1;
                 f = 3;
               }
@@ -778,7 +781,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       if (warp == kOutWarp) job.begun();
       for (int u = 0;; ++u) {
         const int slot = u & (kSlots - 1);
-        if (!lanes_wait(ctl + kBarSched + 8 * slot, (u / kSlots) & 1, abort_flag)) break;
+        if (!lanes_wait<Job>(ctl + kBarSched + 8 * slot, (u / kSlots) & 1, abort_flag)) break;
         const Unit& x = units[slot];
         const int mode = x.mode;
         if (x.nt < 0) break;
@@ -787,7 +790,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
         if (mode == kJoint) {  // the two groups' sums
           job.find_row(x, 0, r, row);
           for (int g = 0; g < 2 && ok; ++g)
-            ok = lanes_wait(ctl + kBarML + 8 * g, c[g] & 1, abort_flag) && lanes_wait(ctl + kBarO + 8 * g, c[g] & 1, abort_flag);
+            ok = lanes_wait<Job>(ctl + kBarML + 8 * g, c[g] & 1, abort_flag) && lanes_wait<Job>(ctl + kBarO + 8 * g, c[g] & 1, abort_flag);
           if (!ok) break;
           const float2 p = xch[r], q = xch[128 + r];
           const float m = fmaxf(p.x, q.x), ref = m == -INFINITY ? 0.f : m, wp = exp2f(p.x - ref), wq = exp2f(q.x - ref);
@@ -803,7 +806,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
           for (int g = 0; g < 2; ++g) {
             if (!takes_part(mode, g)) continue;
             job.find_row(x, g, r, row);
-            ok = lanes_wait(ctl + kBarML + 8 * g, c[g] & 1, abort_flag) && lanes_wait(ctl + kBarO + 8 * g, c[g] & 1, abort_flag);
+            ok = lanes_wait<Job>(ctl + kBarML + 8 * g, c[g] & 1, abort_flag) && lanes_wait<Job>(ctl + kBarO + 8 * g, c[g] & 1, abort_flag);
             if (!ok) break;
             const float2 p = xch[g * 128 + r];
             tc_fence_after();
@@ -833,7 +836,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       uint32_t n = 0, c = 0;    // the group's tiles, and units in which it had any
       bool ok = true;
       auto wait = [&](uint32_t bar, uint32_t parity) {
-        ok = warp_wait(bar, parity, abort_flag);
+        ok = warp_wait<Job>(bar, parity, abort_flag);
         return ok;
       };
       for (int u = 0; ok; ++u) {
@@ -907,27 +910,27 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       }
     }
   }
-  if (*abort_flag && tid == 0) job.error(GB_ERR_TIMEOUT);
   tc_fence_before();
   __syncthreads();
   // Given up: no role issues anything more.  What each has in flight ends before the tensor memory is freed and the CTA leaves
   // (bounded).  (Only here does every role know: one that came to its end before another gave up would have looked too early.)
   if (*abort_flag) {
+    if (tid == 0) job.error(GB_ERR_TIMEOUT);
     if (warp < kKWarp) {
       job.drain_q(ctl + kBarQ + 8 * (warp >> 2));
     } else if ((warp == kKWarp || warp == kVWarp) && lane == 0) {
       const Flight f = flight[warp == kVWarp];
-      if (f.patched) mbar_wait_bounded(ctl + kBarPatch, f.patch_parity, kWaitLimitNs / 8);
+      if (f.patched) mbar_wait_bounded(ctl + kBarPatch, f.patch_parity, Job::kWaitNs / 8);
       for (uint32_t i = 0; i < 2 * kStages; ++i) {
         const uint32_t bar = ctl + kBarFull + 8 * ((f.last - i) % kFulls);
-        if (((f.seen >> i) & 1) && bar != f.patched) mbar_wait_bounded(bar, ((f.last - i) / kFulls) & 1, kWaitLimitNs / 8);
+        if (((f.seen >> i) & 1) && bar != f.patched) mbar_wait_bounded(bar, ((f.last - i) / kFulls) & 1, Job::kWaitNs / 8);
       }
     } else if (warp == kMmaWarp || warp == kMmaWarp + 1) {
       // (a commit by the lane that issued them stands for all its products, S and P.V)
       const uint32_t bar = ctl + kBarDrained + 8 * (warp - kMmaWarp);
       if (elect_one()) {
         mma_commit(bar);
-        mbar_wait_bounded(bar, 0, kWaitLimitNs / 8);
+        mbar_wait_bounded(bar, 0, Job::kWaitNs / 8);
       }
       __syncwarp();
     }

@@ -114,6 +114,7 @@ struct PromptJob : PromptView {
   const __nv_bfloat16 *q, *k, *v;
   __nv_bfloat16* o;
 
+  static constexpr uint64_t kWaitNs = kWaitLimitNs;
   static constexpr bool kEarlyQ = false;
   static constexpr int kLongPair = 0;  // none: K and V come from the L2 in time (24 packed prompts 78.2 us, with 4 tiles 79.4)
   static constexpr int kQArrivals = 1;
@@ -244,6 +245,25 @@ __global__ void __launch_bounds__(flash::kThreads, 1) k_prompt(const __grid_cons
   flash::body(job, sm);
 }
 
+// The self-test of the failure path: the tile `stalled` (0 K, 1 V, 2 the query rows; of the tile or unit `at`) never comes, and the
+// waits that this makes run out have a short limit.
+struct StalledJob : PromptJob {
+  static constexpr uint64_t kWaitNs = 50000000;
+  int stalled, at;
+  __device__ __forceinline__ void load_tile(const flash::Unit& x, int j, int kv, int page, uint32_t dst, uint32_t bar,
+                                            int lane) const {
+    if (kv != stalled || j != at) PromptJob::load_tile(x, j, kv, page, dst, bar, lane);
+  }
+  __device__ __forceinline__ void load_q(const flash::Unit& x, int g, int r, uint32_t dst, uint32_t bar, const Row& row) const {
+    if (stalled != 2 || x.w[1] != at) PromptJob::load_q(x, g, r, dst, bar, row);
+  }
+};
+
+__global__ void __launch_bounds__(flash::kThreads, 1) k_prompt_stalled(const __grid_constant__ StalledJob job) {
+  extern __shared__ __align__(1024) unsigned char sm[];
+  flash::body(job, sm);
+}
+
 // fp32: a CTA per (unit, KV head).
 struct PromptTile {
   const float *qp, *kp, *vp;  // the sequence's first row, this head
@@ -333,7 +353,8 @@ bool meets(const void* a, int64_t as, int aw, const void* b, int64_t bs, int bw,
 
 }  // namespace
 
-extern "C" gb_status gb_prompt_attention(const gb_prompt_args* a, gb_stream_t stream) {
+// stalled: see StalledJob; -1: the call itself.
+static gb_status launch_prompt(const gb_prompt_args* a, int stalled, int at, cudaStream_t s) {
   if (!a) return GB_ERR_INVALID;
   size_t need = 0;
   const gb_status st = gb_prompt_workspace_bytes(a->num_tokens, a->num_seqs, a->num_q_heads, a->num_kv_heads,
@@ -359,7 +380,6 @@ extern "C" gb_status gb_prompt_attention(const gb_prompt_args* a, gb_stream_t st
       cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess)
     return GB_ERR_CUDA;
   if (a->num_seqs == 0) return GB_OK;
-  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   int* ctl = static_cast<int*>(a->workspace);
   const int G = a->num_q_heads / a->num_kv_heads, tokens = unit_tokens(a->dtype, G);
   // Few units (a short prompt): half the rows each, so that twice as many SMs have work and the longest ends sooner.  Up to
@@ -368,11 +388,15 @@ extern "C" gb_status gb_prompt_attention(const gb_prompt_args* a, gb_stream_t st
   const long long most = max_units(a->dtype, G, a->num_tokens, a->num_seqs);
   PromptView view{ctl, a->cu_seqlens, (int)most, a->num_seqs, tokens, few ? flash::kRows / G : tokens, few,
                   a->num_kv_heads, G, a->num_tokens, a->scale * 1.4426950408889634f, a->q_stride, a->k_stride, a->v_stride, a->out_stride};
-  if (a->dtype == GB_BF16 && !flash::launches_with(reinterpret_cast<const void*>(k_prompt))) return GB_ERR_UNSUPPORTED;
+  if (a->dtype == GB_BF16 && (!flash::launches_with(reinterpret_cast<const void*>(k_prompt)) ||
+                              (stalled >= 0 && !flash::launches_with(reinterpret_cast<const void*>(k_prompt_stalled)))))
+    return GB_ERR_UNSUPPORTED;
   // The tensor maps first: nothing is enqueued when one cannot be made.
-  PromptJob job;
+  StalledJob job;
   if (a->dtype == GB_BF16) {
     static_cast<PromptView&>(job) = view;
+    job.stalled = stalled;
+    job.at = at;
     job.q = static_cast<const __nv_bfloat16*>(a->q);
     job.k = static_cast<const __nv_bfloat16*>(a->k);
     job.v = static_cast<const __nv_bfloat16*>(a->v);
@@ -393,8 +417,12 @@ extern "C" gb_status gb_prompt_attention(const gb_prompt_args* a, gb_stream_t st
     return GB_ERR_CUDA;
   cudaError_t e;
   if (a->dtype == GB_BF16) {
-    e = set_max_dynamic_smem(reinterpret_cast<const void*>(k_prompt), flash::kSmem);
-    if (e == cudaSuccess) e = launch_pdl(k_prompt, (unsigned)std::min<long long>(sms, most * a->num_kv_heads), flash::kThreads, flash::kSmem, s, job);
+    const void* kernel = stalled < 0 ? reinterpret_cast<const void*>(k_prompt) : reinterpret_cast<const void*>(k_prompt_stalled);
+    const unsigned grid = (unsigned)std::min<long long>(sms, most * a->num_kv_heads);
+    e = set_max_dynamic_smem(kernel, flash::kSmem);
+    if (e == cudaSuccess)
+      e = stalled < 0 ? launch_pdl(k_prompt, grid, flash::kThreads, flash::kSmem, s, job)
+                      : launch_pdl(k_prompt_stalled, grid, flash::kThreads, flash::kSmem, s, job);
   } else {
     e = set_max_dynamic_smem(reinterpret_cast<const void*>(k_prompt_f32), (int)sizeof(TileSmem));
     if (e == cudaSuccess)
@@ -403,6 +431,15 @@ extern "C" gb_status gb_prompt_attention(const gb_prompt_args* a, gb_stream_t st
                      static_cast<const float*>(a->v), static_cast<float*>(a->out));
   }
   return e == cudaSuccess ? GB_OK : GB_ERR_CUDA;
+}
+
+extern "C" gb_status gb_prompt_attention(const gb_prompt_args* args, gb_stream_t stream) {
+  return launch_prompt(args, -1, 0, reinterpret_cast<cudaStream_t>(stream));
+}
+
+extern "C" gb_status gb_prompt_wait_selftest(const gb_prompt_args* args, int stalled, int at, gb_stream_t stream) {
+  if (!args || args->dtype != GB_BF16 || stalled < 0 || stalled > 2 || at < 0) return GB_ERR_INVALID;
+  return launch_prompt(args, stalled, at, reinterpret_cast<cudaStream_t>(stream));
 }
 
 extern "C" gb_status gb_prompt_status(const void* workspace_dev, int* device_status, gb_stream_t stream) {
