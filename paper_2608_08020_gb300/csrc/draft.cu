@@ -598,13 +598,12 @@ struct DraftJob {
     x.w[kRec] = e.rec;
   }
   __device__ __forceinline__ bool draft_tile(const flash::Unit& x, int j) const { return x.w[kDrafts] && j == x.nt - 1; }
-  // Rows of the context's last page past its end hold whatever the pool's memory did.
-  __device__ __forceinline__ void stale_rows(const flash::Unit& x, int j, int& z0, int& z1) const {
+  // Rows of the context's last page past its end, and the drafted rows that are loaded (by eights) but lie past the count.
+  __device__ __forceinline__ uint32_t stale_rows(const flash::Unit& x, int j) const {
     const int n = x.w[kTok1] - x.w[kTok0] - j * flash::kTok;
-    if (n > 0 && n < flash::kTok && (n & (v.P - 1))) {
-      z0 = n;
-      z1 = (n + v.P - 1) & ~(v.P - 1);
-    }
+    const int page = n > 0 && n < flash::kTok ? -n & (v.P - 1) : 0;
+    const int drafts = draft_tile(x, j) ? min(w.T - x.w[kDrafts], -x.w[kDrafts] & 7) : 0;
+    return page + drafts > 0 ? flash::stale_word(n & 127, page, 64 + x.w[kDrafts], drafts) : 0;
   }
   // Evicted first: a layer's keys and values are read once or by units that run side by side, and should not push the records
   // that the join reads next out of the L2 (64 beams x 4k 284 -> 277 us, one beam of 20000 tokens 76 -> 70).
@@ -723,7 +722,7 @@ struct DraftJob {
       const size_t kv0 = ((size_t)x.w[kBeam] * w.T * v.Hkv + x.head) * flash::kD;
       const int nctx = x.w[kTok1] - x.w[kTok0];
       bool unseen = false;
-      for (int j = 0; j < min(w.T, (x.w[kDrafts] + 7) & ~7) && !unseen; ++j)
+      for (int j = 0; j < x.w[kDrafts] && !unseen; ++j)
         if (!((anc >> j) & 1)) unseen = flash::not_finite(vv + kv0 + (size_t)j * v.Hkv * flash::kD);
       if (!unseen) continue;
       const size_t qo = (((size_t)x.w[kBeam] * w.T + tok) * v.Hq + x.head * v.G + gg) * flash::kD;

@@ -323,6 +323,12 @@ __device__ __forceinline__ void walk_o(uint32_t a, uint32_t b, bool two, float w
   }
 }
 
+// Rows of a V tile that hold no token but whatever their memory did, up to 127 of them: `first` rows from row a on, then `second`
+// from row b on.  One word, 0: none.
+__device__ __forceinline__ uint32_t stale_word(int a, int first, int b, int second) {
+  return (uint32_t)a | (uint32_t)first << 8 | (uint32_t)b << 16 | (uint32_t)(first + second) << 24;
+}
+
 // Keys of a tile a row sees: all of them, the first `limit`, or the first `limit` (up to 64) and those of `bits`.
 struct Sees {
   bool all;                 // (the same for the warp)
@@ -664,8 +670,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       // ---------------------------------------------------------------- V tiles
       uint32_t from = 0, last = 0, seen = 0;  // as above
       uint32_t patches = 0;
-      uint32_t p_dst = 0, p_full = 0;  // the V tile that waits to be mended
-      int z0 = 0, z1 = 0;              // its rows that hold no token
+      uint32_t p_dst = 0, p_full = 0, stale = 0;  // the V tile that waits to be mended, and its rows (0: none waits)
       bool ok = true;
       auto fetch = [&](int u, Unit& to) {
         const int slot = u & (kSlots - 1);
@@ -677,23 +682,25 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       };
       // Whatever lies in the rows of a V tile that hold no token is made 0, since 0 x NaN is NaN.
       auto mend = [&]() {
-        for (int i = lane; i < (z1 - z0) * 16; i += 32)
-          *reinterpret_cast<uint4*>(sm + (p_dst - sbase) + Job::v_row(z0 + (i >> 4), (i >> 3) & 1) + (i & 7) * 16) =
-              make_uint4(0, 0, 0, 0);
+#pragma unroll 1
+        for (int i = lane; i < (int)(stale >> 24) * 16; i += 32) {
+          const int first = (stale >> 8) & 255, n = i >> 4, row = n < first ? (stale & 255) + n : ((stale >> 16) & 255) + n - first;
+          *reinterpret_cast<uint4*>(sm + (p_dst - sbase) + Job::v_row(row, (i >> 3) & 1) + (i & 7) * 16) = make_uint4(0, 0, 0, 0);
+        }
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(p_full);
         ++patches;
-        z0 = z1 = 0;
+        stale = 0;
       };
       // A stage's release, or with `landed` only the tile to be mended, which meanwhile is mended as soon as it is in.
       auto wait = [&](uint32_t bar, uint32_t parity, bool landed) {
-        if (z0 >= z1) return warp_wait<Job>(bar, parity, abort_flag);  // (a suspended wait leaves the issue slots to others)
+        if (!stale) return warp_wait<Job>(bar, parity, abort_flag);  // (a suspended wait leaves the issue slots to others)
         uint64_t t0 = 0;
         for (uint32_t it = 1;; ++it) {
           int f = 0;
           if (lane == 0) {
-            if (z0 < z1 && mbar_test(ctl + kBarPatch, patches & 1)) f = 2;
+            if (stale && mbar_test(ctl + kBarPatch, patches & 1)) f = 2;
             else if (!landed && mbar_test(bar, parity)) f = 1;
             else if ((it & 63) == 0) {
               const uint64_t now = globaltimer_ns();
@@ -717,12 +724,9 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
           ok = wait(ctl + kBarEmpty + 8 * ((n - kStages) % kFulls), ((n - kStages) / kFulls) & 1, false);
         if (!ok) return;
         uint32_t bar = full;
-        int s0 = 0, s1 = 0;
-        job.stale_rows(now, j, s0, s1);
-        if (s0 < s1) {
-          if (z0 < z1 && !(ok = wait(0, 0, true))) return;  // one at a time
-          z0 = s0;
-          z1 = s1;
+        if (const uint32_t rows = job.stale_rows(now, j)) {
+          if (stale && !(ok = wait(0, 0, true))) return;  // one at a time
+          stale = rows;
           p_dst = dst;
           p_full = full;
           bar = ctl + kBarPatch;
@@ -766,12 +770,12 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
         page_x = x.nt >= 0 ? job.page(x, 0, lane) : 0;
         page_y = pair ? job.page(y, 0, lane) : 0;
       }
-      if (ok && z0 < z1) ok = wait(0, 0, true);
+      if (ok && stale) ok = wait(0, 0, true);
       if (Job::kLongPair == 0) {
         last = from - 1;
         seen = 0x155u & ((1u << min(from, 31u)) - 1);
       }
-      if (lane == 0) flight[1] = {last, seen, z0 < z1 ? p_full : 0, patches & 1};
+      if (lane == 0) flight[1] = {last, seen, stale ? p_full : 0, patches & 1};
     } else if (warp >= kOutWarp) {
       // ---------------------------------------------------------------- results
       const int r = tid & 127;

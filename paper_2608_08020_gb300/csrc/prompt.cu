@@ -146,7 +146,7 @@ struct PromptJob : PromptView {
     x.w[3] = e.len;
   }
   // A tile's rows past the sequence are the next one's, or past the tensor and zeros.
-  __device__ __forceinline__ void stale_rows(const flash::Unit&, int, int&, int&) const {}
+  __device__ __forceinline__ uint32_t stale_rows(const flash::Unit&, int) const { return 0; }
   __device__ __forceinline__ int page(const flash::Unit&, int, int) const { return 0; }
   __device__ __forceinline__ void load_tile(const flash::Unit& x, int j, int kv, int, uint32_t dst, uint32_t bar,
                                             int lane) const {
