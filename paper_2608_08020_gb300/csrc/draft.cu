@@ -676,7 +676,7 @@ struct DraftJob {
   }
   template <class Done>
   __device__ __forceinline__ void out(const flash::Unit& x, const Row& row, uint32_t a, uint32_t b, bool two, float wa,
-                                      float wb, float m, float l, Done done) const {
+                                      float wb, float m, float l, Done done, volatile int* again) const {
     const bool final = row.rec < 0;
     const float inv = final ? 1.f / l : 1.f;
     const int head = x.head * v.G + row.gg;
@@ -710,43 +710,58 @@ struct DraftJob {
         },
         done);
     if (row.valid && !final) w.ml[rr] = make_float2(m, l);
-    unsigned redo = __ballot_sync(0xffffffffu, row.valid && x.w[kDrafts] && !fine && isfinite(m) && isfinite(l));
-    while (redo) {  // see sum_seen; only drafted tokens off the row's path share a tile with what it sees
-      const int src = __ffs(redo) - 1;
-      redo &= redo - 1;
-      const int tok = __shfl_sync(0xffffffffu, row.tok, src), gg = __shfl_sync(0xffffffffu, row.gg, src);
-      const float mr = __shfl_sync(0xffffffffu, m, src), ir = __shfl_sync(0xffffffffu, inv, src);
-      const unsigned long long anc = __shfl_sync(0xffffffffu, row.anc, src);
-      const bool fin = __shfl_sync(0xffffffffu, final, src);
-      const size_t at = __shfl_sync(0xffffffffu, rr, src);
-      const size_t kv0 = ((size_t)x.w[kBeam] * w.T * v.Hkv + x.head) * flash::kD;
-      const int nctx = x.w[kTok1] - x.w[kTok0];
-      bool unseen = false;
-      for (int j = 0; j < x.w[kDrafts] && !unseen; ++j)
-        if (!((anc >> j) & 1)) unseen = flash::not_finite(vv + kv0 + (size_t)j * v.Hkv * flash::kD);
-      if (!unseen) continue;
-      const size_t qo = (((size_t)x.w[kBeam] * w.T + tok) * v.Hq + x.head * v.G + gg) * flash::kD;
-      float acc[4];
-      flash::sum_seen(
-          q + qo, nctx + w.T,
-          [&](int j, const __nv_bfloat16*& kj, const __nv_bfloat16*& vj) {
-            if (j >= nctx) {
-              kj = k + kv0 + (size_t)(j - nctx) * v.Hkv * flash::kD;
-              vj = vv + kv0 + (size_t)(j - nctx) * v.Hkv * flash::kD;
-              return ((anc >> (j - nctx)) & 1) != 0;
-            }
-            const int pos = x.w[kTok0] + j, page = v.tables[(size_t)x.w[kBeam] * v.max_pages + pos / v.P];
-            if (page < 0 || page >= v.num_pages) return false;
-            const __nv_bfloat16* pool = reinterpret_cast<const __nv_bfloat16*>(v.kv);
-            kj = pool + kv_elem_offset(v, layer, page, 0, x.head, pos % v.P);
-            vj = pool + kv_elem_offset(v, layer, page, 1, x.head, pos % v.P);
-            return true;
-          },
-          qscale, mr, acc);
-      for (int i = 0; i < 4; ++i) {
-        const int c = 4 * (threadIdx.x & 31) + i;
-        if (fin) o[qo + c] = __float2bfloat16(acc[i] * ir);
-        else w.rec[at * flash::kD + c] = acc[i];
+    if (row.valid && x.w[kDrafts] && !fine && isfinite(m) && isfinite(l)) *again = 1;
+  }
+  // Rows that only met a value that is not finite in drafted tokens off their path, which alone share a tile with what they
+  // see; a row to a warp (see flash::one_row).
+  __device__ __forceinline__ void again(const flash::Unit& x, int warp) const {
+    if (!x.w[kDrafts]) return;
+    const int lane = threadIdx.x & 31, nctx = x.w[kTok1] - x.w[kTok0];
+    auto drafted_row = [&](const __nv_bfloat16* of, int i) {
+      return of + (((size_t)x.w[kBeam] * w.T + i) * v.Hkv + x.head) * flash::kD;
+    };
+    unsigned long long odd = 0;  // tokens whose V is not finite
+    bool looked = false;
+#pragma unroll 1
+    for (int i = warp; i < x.w[kNtok] * v.G; i += flash::kKWarp) {
+      Row row;
+      find_row(x, i / flash::kRows, i % flash::kRows, row);
+      const size_t qo = (((size_t)row.beam * w.T + row.tok) * v.Hq + x.head * v.G + row.gg) * flash::kD;
+      const size_t rr = ((size_t)max(row.rec, 0) * v.Hkv + x.head) * w.rows + row.tok * v.G + row.gg;
+      bool bad;
+      if (row.rec < 0) {
+        const uint2 y = reinterpret_cast<const uint2*>(o + qo)[lane];
+        bad = flash::not_finite(y.x) || flash::not_finite(y.y);
+      } else {
+        const float4 y = reinterpret_cast<const float4*>(w.rec + rr * flash::kD)[lane];
+        bad = !(isfinite(y.x) && isfinite(y.y) && isfinite(y.z) && isfinite(y.w));
+      }
+      if (!__any_sync(0xffffffffu, bad)) continue;
+      if (!looked) {
+        looked = true;
+        for (int t = 0; t < 64; t += 32)
+          odd |= (unsigned long long)__ballot_sync(0xffffffffu, t + lane < x.w[kDrafts] && flash::not_finite(drafted_row(vv, t + lane))) << t;
+      }
+      if (!(odd & ~row.anc)) continue;
+      float m, l, acc[4];
+      if (!flash::one_row(
+              q + qo, nctx + x.w[kDrafts],
+              [&](int j, int kv, const __nv_bfloat16*& to) {
+                if (j >= nctx) {
+                  to = drafted_row(kv ? vv : k, j - nctx);
+                  return ((row.anc >> (j - nctx)) & 1) != 0;
+                }
+                const int pos = x.w[kTok0] + j, page = v.tables[(size_t)x.w[kBeam] * v.max_pages + pos / v.P];
+                to = reinterpret_cast<const __nv_bfloat16*>(v.kv) + kv_elem_offset(v, layer, page, kv, x.head, pos % v.P);
+                return page >= 0 && page < v.num_pages;
+              },
+              qscale, m, l, acc))
+        continue;
+      if (row.rec < 0) {
+        for (int c = 0; c < 4; ++c) o[qo + 4 * lane + c] = __float2bfloat16(acc[c] / l);
+      } else {
+        reinterpret_cast<float4*>(w.rec + rr * flash::kD)[lane] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+        if (lane == 0) w.ml[rr] = make_float2(m, l);
       }
     }
   }

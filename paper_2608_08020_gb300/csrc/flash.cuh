@@ -22,7 +22,7 @@
 //
 // Warp roles (512 threads):
 //   warps 0-7    softmax: thread r of group g owns row r of its tile (tensor-memory lane r); also loads
-//                the row's query
+//                the row's query; at the end they answer rows anew that met unseen values (one_row)
 //   warp 8       takes the CTA's units from the sorted list, publishes them in a ring of eight and streams K
 //   warp 11      streams V; both go through one ring of five 32 KiB stages (K0 V0 K1 V1 ..., of a pair K K V V)
 //   warps 9-10   issue the products of a group each: S(i), then P.V(i) before S(i + 1), whose tile
@@ -96,7 +96,8 @@ struct Flight {
 constexpr int kFlights = kUnits + 4 * kSlots * kUnitWords;  // Flight [2]
 constexpr int kWordTmem = kFlights + 2 * (int)sizeof(Flight);
 constexpr int kWordAbort = kWordTmem + 4;
-static_assert(kUnits % 16 == 0 && kWordAbort + 4 <= 1024, "control area");
+constexpr int kWordAgain = kWordAbort + 4;  // some row was not finite
+static_assert(kUnits % 16 == 0 && kWordAgain + 4 <= 1024, "control area");
 constexpr int kSchedReaders = 15;  // eight softmax warps, two that issue products, one that loads V, four that write
 
 // What every role knows of a unit; w is the job's own.
@@ -337,33 +338,93 @@ struct Sees {
   unsigned long long bits;  // column 64 + i for bit i
 };
 
-// sum_j 2^(qscale q.k_j - m) v_j over the keys that key(j, k, v) says are seen, by a warp: lane l gets
-// columns 4 l on.  A product with P takes every key of a tile, with p = 0 for those the row does not see, and 0 x inf is
-// NaN: a row whose result is not finite although its maximum is, is summed again here where one of those keys' values is
-// not finite.
+// A product with P takes every key of a tile, with p = 0 for those the row does not see, and 0 x inf is NaN: a row whose result is
+// not finite although the maximum and the sum of its softmax are may only have met a value that it does not see.  The warps that
+// write make a note, and the softmax warps, once all else is done and nobody waits for them but the CTA's end, look through the
+// CTA's rows for those and answer them anew over the keys they see (Job::again).
+
+// One row's softmax over the keys that key(j, kv, row) says are seen (row: k_j or v_j), by a warp: lane l gets columns 4 l on of the
+// unnormalised sum.  32 keys at a time, a score to a lane, then eight values' loads at once (256 rows over 32768 keys by a CTA's eight
+// warps: 135 ms; by the four that write, with the registers they have, 280 to 700, and their units waited).  False where a score
+// seen is not finite.
 template <class Key>
-__device__ __forceinline__ void sum_seen(const __nv_bfloat16* q, int nkeys, Key key, float qscale, float m, float* acc) {
+__device__ __forceinline__ bool one_row(const __nv_bfloat16* q, int nkeys, Key key, float qscale, float& m, float& l, float* acc) {
   const int lane = threadIdx.x & 31;
-  float qv[4];
-  for (int i = 0; i < 4; ++i) {
-    qv[i] = __bfloat162float(q[4 * lane + i]);
-    acc[i] = 0.f;
+  constexpr int kAtOnce = 8;
+  m = -INFINITY;
+  l = 0.f;
+  for (int i = 0; i < 4; ++i) acc[i] = 0.f;
+#pragma unroll 1
+  for (int j0 = 0; j0 < nkeys; j0 += 32) {
+    const __nv_bfloat16* row;
+    const bool on = j0 + lane < nkeys && key(j0 + lane, 0, row);
+    float s = -INFINITY;
+    if (on) {
+      float part[4] = {};
+#pragma unroll 4
+      for (int c = 0; c < kD; c += 8) {
+        const uint4 a = *reinterpret_cast<const uint4*>(q + c), b = *reinterpret_cast<const uint4*>(row + c);
+        const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          part[i] = fmaf(__uint_as_float(x[i] << 16), __uint_as_float(y[i] << 16), part[i]);
+          part[i] = fmaf(__uint_as_float(x[i] & 0xffff0000u), __uint_as_float(y[i] & 0xffff0000u), part[i]);
+        }
+      }
+      s = ((part[0] + part[1]) + (part[2] + part[3])) * qscale;
+    }
+    float mx = s;
+#pragma unroll
+    for (int w = 16; w > 0; w >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
+    if (mx > m) {
+      const float f = exp2f(m - mx);
+      l *= f;
+      for (int i = 0; i < 4; ++i) acc[i] *= f;
+      m = mx;
+    }
+    const float p = on ? exp2f(s - m) : 0.f;
+    l += p;
+    const unsigned there = __ballot_sync(0xffffffffu, on);
+#pragma unroll 1
+    for (int e0 = 0; e0 < 32; e0 += kAtOnce) {
+      uint2 x[kAtOnce];
+#pragma unroll
+      for (int e = 0; e < kAtOnce; ++e)
+        if ((there >> (e0 + e)) & 1) {
+          key(j0 + e0 + e, 1, row);
+          x[e] = reinterpret_cast<const uint2*>(row)[lane];
+        }
+#pragma unroll
+      for (int e = 0; e < kAtOnce; ++e) {
+        const float f = __shfl_sync(0xffffffffu, p, e0 + e);
+        if ((there >> (e0 + e)) & 1) {
+          acc[0] = fmaf(f, __uint_as_float(x[e].x << 16), acc[0]);
+          acc[1] = fmaf(f, __uint_as_float(x[e].x & 0xffff0000u), acc[1]);
+          acc[2] = fmaf(f, __uint_as_float(x[e].y << 16), acc[2]);
+          acc[3] = fmaf(f, __uint_as_float(x[e].y & 0xffff0000u), acc[3]);
+        }
+      }
+    }
   }
-  for (int j = 0; j < nkeys; ++j) {
-    const __nv_bfloat16 *k, *v;
-    if (!key(j, k, v)) continue;
-    float s = 0.f;
-    for (int i = 0; i < 4; ++i) s = fmaf(qv[i], __bfloat162float(k[4 * lane + i]), s);
-    for (int w = 16; w > 0; w >>= 1) s += __shfl_xor_sync(0xffffffffu, s, w);
-    const float p = exp2f(fmaf(s, qscale, -m));
-    for (int i = 0; i < 4; ++i) acc[i] = fmaf(p, __bfloat162float(v[4 * lane + i]), acc[i]);
-  }
+#pragma unroll
+  for (int w = 16; w > 0; w >>= 1) l += __shfl_xor_sync(0xffffffffu, l, w);
+  return isfinite(m) && isfinite(l);
 }
-// Whether v has a value that is not finite (a warp's answer).
+// Whether two bf16 values, or a row of V (this lane's answer), are not all finite.
+__device__ __forceinline__ bool not_finite(uint32_t x) { return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u; }
 __device__ __forceinline__ bool not_finite(const __nv_bfloat16* v) {
   bool bad = false;
-  for (int i = 0; i < 4; ++i) bad |= !isfinite(__bfloat162float(v[4 * (threadIdx.x & 31) + i]));
-  return __any_sync(0xffffffffu, bad);
+#pragma unroll 4
+  for (int c = 0; c < kD; c += 8) {
+    const uint4 a = *reinterpret_cast<const uint4*>(v + c);
+    bad = bad || not_finite(a.x) || not_finite(a.y) || not_finite(a.z) || not_finite(a.w);
+  }
+  return bad;
+}
+
+// Entry of the list that is the CTA's u-th: b, 2 n - 1 - b, 2 n + b, ...
+__device__ __forceinline__ int unit_id(int u) {
+  return u * (int)gridDim.x + ((u & 1) ? (int)gridDim.x - 1 - (int)blockIdx.x : (int)blockIdx.x);
 }
 
 template <class Job>
@@ -372,6 +433,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const uint32_t sbase = smem_addr(sm), ctl = sbase + kBar;
   volatile int* abort_flag = reinterpret_cast<volatile int*>(sm + kBar + kWordAbort);
+  volatile int* again = reinterpret_cast<volatile int*>(sm + kBar + kWordAgain);
   Unit* units = reinterpret_cast<Unit*>(sm + kBar + kUnits);
   Flight* flight = reinterpret_cast<Flight*>(sm + kBar + kFlights);
   if (sbase & 1023) {  // the swizzled layouts need a 1024-byte aligned base
@@ -401,6 +463,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
     } else if (lane == 31) {
       mbar_init(ctl + kBarPatch, 1);
       *abort_flag = 0;
+      *reinterpret_cast<volatile int*>(sm + kBar + kWordAgain) = 0;
     }
     static_assert(kFulls + 2 + kSlots <= 31, "a lane each");
     fence_mbar_init();
@@ -417,151 +480,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
   pdl_launch_dependents();
 
   // The warpgroups share out the launch's registers; the others give theirs at once, so the groups' waits for them end.
-  if (warp < kKWarp) {
-    regs_inc<kSoftmaxRegs>();
-    // ---------------------------------------------------------------- softmax
-    const int g = warp >> 2, r = tid & 127;
-    const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t s_addr = tmem + kTmemS + g * 128 + lane_base, o_addr = tmem + kTmemO + lane_base;
-    float2* xch = reinterpret_cast<float2*>(sm + kXch);
-    const float qscale = job.qscale;
-    uint32_t n = 0, c_done = 0;   // tiles of this group, units it is done with
-    int u_next = 0;               // the unit read next
-    bool alive = true;
-    typename Job::Row row, row_y;
-    // The group's next unit: its words stay in shared memory until the group is done with it.
-    bool known = false;  // the next unit has been found (the same in a warp)
-    auto next_unit = [&](int& slot, bool patient) {
-      for (;; ++u_next) {
-        slot = u_next & (kSlots - 1);
-        const uint32_t bar = ctl + kBarSched + 8 * slot, parity = (u_next / kSlots) & 1;
-        if (!patient) {
-          if (!__all_sync(0xffffffffu, mbar_test(bar, parity))) return true;
-        } else if (!warp_wait<Job>(bar, parity, abort_flag)) {
-          return false;
-        }
-        if (units[slot].nt < 0) break;
-        if (takes_part(units[slot].mode, g)) {
-          ++u_next;
-          break;
-        }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(ctl + kBarSchedFree + 8 * slot);
-      }
-      known = true;
-      return true;
-    };
-    int sx = 0, sy = 0;
-    alive = next_unit(sx, true);
-    if (alive && units[sx].nt >= 0) {
-      job.find_row(units[sx], g, r, row);
-      job.load_q(units[sx], g, r, sbase + g * kTile, ctl + kBarQ + 8 * g, row);
-      job.loaded_q(r, ctl + kBarQ + 8 * g);
-    }
-    // The group's last S of a unit is complete: the next unit's query rows may come.  While P of that tile is due the
-    // group does not wait for the unit: where others without the group come first, it is made known only when they are
-    // loaded, to which the ring may need the stage of this tile's V.
-    auto begin_next = [&](bool patient) {
-      if (known) return true;
-      if (!next_unit(sy, patient)) return false;
-      if (known && units[sy].nt >= 0) {
-        job.find_row(units[sy], g, r, row_y);
-        job.load_q(units[sy], g, r, sbase + g * kTile, ctl + kBarQ + 8 * g, row_y);
-      }
-      return true;
-    };
-    while (alive && units[sx].nt >= 0) {
-      const Unit& x = units[sx];
-      const int mode = x.mode, mine = group_tiles(x.nt, mode, g);
-      float m_ref = -INFINITY, l = 0.f;
-      known = false;
-      for (int i = 0; i < mine; ++i, ++n) {
-        const int t = group_tile(mode, g, i);
-        if (!warp_wait<Job>(ctl + kBarS + 8 * g, n & 1, abort_flag)) { alive = false; break; }
-        if (Job::kEarlyQ && i + 1 == mine && !(alive = begin_next(false))) break;
-        tc_fence_after();
-        uint32_t su[128];
-#pragma unroll
-        for (int c = 0; c < 128; c += 32) ld32_issue(s_addr + c, su + c);
-#pragma unroll
-        for (int c = 0; c < 128; c += 32) ld32_wait(su + c);
-        float* s = reinterpret_cast<float*>(su);
-        const Sees see = job.sees(x, row, t);
-        if (!see.all) {
-#pragma unroll
-          for (int c = 0; c < 64; ++c) s[c] = c < see.limit ? s[c] : -INFINITY;
-          if (see.by_bits) {
-            const uint32_t half[2] = {(uint32_t)see.bits, (uint32_t)(see.bits >> 32)};
-#pragma unroll
-            for (int c = 64; c < 128; ++c) s[c] = (half[(c - 64) >> 5] & (1u << (c & 31))) ? s[c] : -INFINITY;
-          } else {
-#pragma unroll
-            for (int c = 64; c < 128; ++c) s[c] = c < see.limit ? s[c] : -INFINITY;
-          }
-        }
-        float mx[4] = {fmaxf(s[0], s[1]), fmaxf(s[2], s[3]), fmaxf(s[4], s[5]), fmaxf(s[6], s[7])};
-#pragma unroll
-        for (int c = 8; c < 128; c += 8)
-#pragma unroll
-          for (int k = 0; k < 4; ++k) mx[k] = max3(mx[k], s[c + 2 * k], s[c + 2 * k + 1]);
-        const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * qscale;
-        const bool raise = mt > m_ref + 8.f;
-        if (i > 0 && __any_sync(0xffffffffu, raise)) {
-          const float alpha = raise ? exp2f(m_ref - mt) : 1.f;
-#pragma unroll 1
-          for (int c0 = 0; c0 < 128; c0 += 32) {
-            float o[32];
-            tmem_ld32(o_addr + g * 128 + c0, o);
-#pragma unroll
-            for (int c = 0; c < 32; ++c) o[c] *= alpha;
-            tmem_st32(o_addr + g * 128 + c0, o);
-          }
-          l *= alpha;
-        }
-        if (raise) m_ref = mt;
-        const float neg_m = m_ref == -INFINITY ? 0.f : -m_ref;  // no key seen yet: every p is 0
-        const uint64_t sc2 = pack2(qscale, qscale), nm2 = pack2(neg_m, neg_m);
-        uint64_t ls[4] = {0ull, 0ull, 0ull, 0ull};  // pairs of fp32 sums
-#pragma unroll
-        for (int c = 0; c < 128; c += 32) {
-          uint32_t pw[16];
-#pragma unroll
-          for (int k = 0; k < 32; k += 2) {
-            float p0, p1;
-            unpack2(fma2(pack2(s[c + k], s[c + k + 1]), sc2, nm2), p0, p1);
-            p0 = ex2_approx(p0);
-            p1 = ex2_approx(p1);
-            ls[(k >> 1) & 3] = add2(ls[(k >> 1) & 3], pack2(p0, p1));
-            const __nv_bfloat162 a = __floats2bfloat162_rn(p0, p1);
-            pw[k / 2] = *reinterpret_cast<const uint32_t*>(&a);
-          }
-          st16(s_addr + c / 2, pw);
-          if (c == 32 || c == 96) {  // half of the tile's keys: the tensor core may begin on them
-            st_wait();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(ctl + kBarP + 16 * g + (c == 96 ? 8 : 0));
-          }
-        }
-        float l0, l1;
-        unpack2(add2(add2(ls[0], ls[1]), add2(ls[2], ls[3])), l0, l1);
-        l += l0 + l1;
-      }
-      if (!alive) break;
-      if (!(alive = begin_next(true))) break;
-      if (units[sy].nt >= 0) job.loaded_q(r, ctl + kBarQ + 8 * g);
-      // (m, l) go to the warps that write, once they have those of the group's unit before.
-      if (c_done > 0 && !(alive = warp_wait<Job>(ctl + kBarOFree + 8 * g, (c_done - 1) & 1, abort_flag))) break;
-      ++c_done;
-      xch[g * 128 + r] = make_float2(m_ref, l);
-      __syncwarp();
-      if (lane == 0) mbar_arrive(ctl + kBarML + 8 * g);
-      __syncwarp();
-      if (lane == 0) mbar_arrive(ctl + kBarSchedFree + 8 * sx);
-      sx = sy;
-      row = row_y;
-    }
-  } else {
+  if (warp >= kKWarp) {
     regs_dec<kOtherRegs>();
     if (warp == kKWarp) {
       // ---------------------------------------------------------------- units and K tiles
@@ -570,13 +489,10 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       uint32_t from = 0;            // ring position of the unit's (or pair's) first tile; without long pairs, of the next
       uint32_t last = 0, seen = 0;  // position loaded last; bit i: so was the one i before it
       bool ok = true;
-      auto id_of = [&](int u) {  // b, 2 n - 1 - b, 2 n + b, ...
-        return u * (int)gridDim.x + ((u & 1) ? (int)gridDim.x - 1 - (int)blockIdx.x : (int)blockIdx.x);
-      };
       auto find = [&](int u, Unit& x) {
         x.nt = -1;
         x.mate = 0;
-        const int id = id_of(u);
+        const int id = unit_id(u);
         if (id < cap) job.unit(all, id, x);  // (before the count of units is in: the list is there to its capacity)
         if (id >= total) x.nt = -1;
       };
@@ -803,7 +719,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
             tc_fence_before();
             __syncwarp();
             if (lane < 2) mbar_arrive(ctl + kBarOFree + 8 * lane);
-          });
+          }, again);
           ++c[0];
           ++c[1];
         } else {
@@ -818,7 +734,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
               tc_fence_before();
               __syncwarp();
               if (lane == 0) mbar_arrive(ctl + kBarOFree + 8 * g);
-            });
+            }, again);
             ++c[g];
           }
           if (!ok) break;
@@ -826,6 +742,8 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
         __syncwarp();
         if (lane == 0) mbar_arrive(ctl + kBarSchedFree + 8 * slot);
       }
+      __threadfence_block();
+      asm volatile("bar.arrive 1, %0;" ::"n"(32 * (kKWarp + 4)) : "memory");
     } else if (warp == kMmaWarp || warp == kMmaWarp + 1) {
       // ---------------------------------------------------------------- products, a warp per group
       // The whole warp walks the group's tiles and one lane issues: operands that are the same in every lane
@@ -911,6 +829,162 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
           }
         }
         ++c;
+      }
+    }
+  } else {
+    regs_inc<kSoftmaxRegs>();
+    // ---------------------------------------------------------------- softmax
+    const int g = warp >> 2, r = tid & 127;
+    const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t s_addr = tmem + kTmemS + g * 128 + lane_base, o_addr = tmem + kTmemO + lane_base;
+    float2* xch = reinterpret_cast<float2*>(sm + kXch);
+    const float qscale = job.qscale;
+    uint32_t n = 0, c_done = 0;   // tiles of this group, units it is done with
+    int u_next = 0;               // the unit read next
+    bool alive = true;
+    typename Job::Row row, row_y;
+    // The group's next unit: its words stay in shared memory until the group is done with it.
+    bool known = false;  // the next unit has been found (the same in a warp)
+    auto next_unit = [&](int& slot, bool patient) {
+      for (;; ++u_next) {
+        slot = u_next & (kSlots - 1);
+        const uint32_t bar = ctl + kBarSched + 8 * slot, parity = (u_next / kSlots) & 1;
+        if (!patient) {
+          if (!__all_sync(0xffffffffu, mbar_test(bar, parity))) return true;
+        } else if (!warp_wait<Job>(bar, parity, abort_flag)) {
+          return false;
+        }
+        if (units[slot].nt < 0) break;
+        if (takes_part(units[slot].mode, g)) {
+          ++u_next;
+          break;
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(ctl + kBarSchedFree + 8 * slot);
+      }
+      known = true;
+      return true;
+    };
+    int sx = 0, sy = 0;
+    alive = next_unit(sx, true);
+    if (alive && units[sx].nt >= 0) {
+      job.find_row(units[sx], g, r, row);
+      job.load_q(units[sx], g, r, sbase + g * kTile, ctl + kBarQ + 8 * g, row);
+      job.loaded_q(r, ctl + kBarQ + 8 * g);
+    }
+    // The group's last S of a unit is complete: the next unit's query rows may come.  While P of that tile is due the
+    // group does not wait for the unit: where others without the group come first, it is made known only when they are
+    // loaded, to which the ring may need the stage of this tile's V.
+    auto begin_next = [&](bool patient) {
+      if (known) return true;
+      if (!next_unit(sy, patient)) return false;
+      if (known && units[sy].nt >= 0) {
+        job.find_row(units[sy], g, r, row_y);
+        job.load_q(units[sy], g, r, sbase + g * kTile, ctl + kBarQ + 8 * g, row_y);
+      }
+      return true;
+    };
+    while (alive && units[sx].nt >= 0) {
+      const Unit& x = units[sx];
+      const int mode = x.mode, mine = group_tiles(x.nt, mode, g);
+      float m_ref = -INFINITY, l = 0.f;
+      known = false;
+      for (int i = 0; i < mine; ++i, ++n) {
+        const int t = group_tile(mode, g, i);
+        if (!warp_wait<Job>(ctl + kBarS + 8 * g, n & 1, abort_flag)) { alive = false; break; }
+        if (Job::kEarlyQ && i + 1 == mine && !(alive = begin_next(false))) break;
+        tc_fence_after();
+        uint32_t su[128];
+#pragma unroll
+        for (int c = 0; c < 128; c += 32) ld32_issue(s_addr + c, su + c);
+#pragma unroll
+        for (int c = 0; c < 128; c += 32) ld32_wait(su + c);
+        float* s = reinterpret_cast<float*>(su);
+        const Sees see = job.sees(x, row, t);
+        if (!see.all) {
+#pragma unroll
+          for (int c = 0; c < 64; ++c) s[c] = c < see.limit ? s[c] : -INFINITY;
+          if (see.by_bits) {
+            const uint32_t half[2] = {(uint32_t)see.bits, (uint32_t)(see.bits >> 32)};
+#pragma unroll
+            for (int c = 64; c < 128; ++c) s[c] = (half[(c - 64) >> 5] & (1u << (c & 31))) ? s[c] : -INFINITY;
+          } else {
+#pragma unroll
+            for (int c = 64; c < 128; ++c) s[c] = c < see.limit ? s[c] : -INFINITY;
+          }
+        }
+        float mx[4] = {fmaxf(s[0], s[1]), fmaxf(s[2], s[3]), fmaxf(s[4], s[5]), fmaxf(s[6], s[7])};
+#pragma unroll
+        for (int c = 8; c < 128; c += 8)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) mx[k] = max3(mx[k], s[c + 2 * k], s[c + 2 * k + 1]);
+        const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * qscale;
+        const bool raise = mt > m_ref + 8.f;
+        if (i > 0 && __any_sync(0xffffffffu, raise)) {
+          const float alpha = raise ? exp2f(m_ref - mt) : 1.f;
+#pragma unroll 1
+          for (int c0 = 0; c0 < 128; c0 += 32) {
+            float o[32];
+            tmem_ld32(o_addr + g * 128 + c0, o);
+#pragma unroll
+            for (int c = 0; c < 32; ++c) o[c] *= alpha;
+            tmem_st32(o_addr + g * 128 + c0, o);
+          }
+          l *= alpha;
+        }
+        if (raise) m_ref = mt;
+        const float neg_m = m_ref == -INFINITY ? 0.f : -m_ref;  // no key seen yet: every p is 0
+        const uint64_t sc2 = pack2(qscale, qscale), nm2 = pack2(neg_m, neg_m);
+        uint64_t ls[4] = {0ull, 0ull, 0ull, 0ull};  // pairs of fp32 sums
+#pragma unroll
+        for (int c = 0; c < 128; c += 32) {
+          uint32_t pw[16];
+#pragma unroll
+          for (int k = 0; k < 32; k += 2) {
+            float p0, p1;
+            unpack2(fma2(pack2(s[c + k], s[c + k + 1]), sc2, nm2), p0, p1);
+            p0 = ex2_approx(p0);
+            p1 = ex2_approx(p1);
+            ls[(k >> 1) & 3] = add2(ls[(k >> 1) & 3], pack2(p0, p1));
+            const __nv_bfloat162 a = __floats2bfloat162_rn(p0, p1);
+            pw[k / 2] = *reinterpret_cast<const uint32_t*>(&a);
+          }
+          st16(s_addr + c / 2, pw);
+          if (c == 32 || c == 96) {  // half of the tile's keys: the tensor core may begin on them
+            st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(ctl + kBarP + 16 * g + (c == 96 ? 8 : 0));
+          }
+        }
+        float l0, l1;
+        unpack2(add2(add2(ls[0], ls[1]), add2(ls[2], ls[3])), l0, l1);
+        l += l0 + l1;
+      }
+      if (!alive) break;
+      if (!(alive = begin_next(true))) break;
+      if (units[sy].nt >= 0) job.loaded_q(r, ctl + kBarQ + 8 * g);
+      // (m, l) go to the warps that write, once they have those of the group's unit before.
+      if (c_done > 0 && !(alive = warp_wait<Job>(ctl + kBarOFree + 8 * g, (c_done - 1) & 1, abort_flag))) break;
+      ++c_done;
+      xch[g * 128 + r] = make_float2(m_ref, l);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(ctl + kBarML + 8 * g);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(ctl + kBarSchedFree + 8 * sx);
+      sx = sy;
+      row = row_y;
+    }
+    // All rows are written (see one_row).
+    asm volatile("bar.sync 1, %0;" ::"n"(32 * (kKWarp + 4)) : "memory");
+    if (*again && !*abort_flag) {
+      const typename Job::Units all(job);
+      const int total = job.total(all);
+#pragma unroll 1
+      for (int u = 0; unit_id(u) < total; ++u) {
+        Unit x;
+        job.unit(all, unit_id(u), x);
+        job.again(x, warp);
       }
     }
   }

@@ -100,7 +100,12 @@ struct PromptUnits {
     len = start >= 0 && start <= end && end <= p.num_tokens ? end - start : 0;
     per = (len + p.tokens - 1) / p.tokens <= p.few ? p.small_tokens : p.tokens;
     count = (len + per - 1) / per;
-    if (blockIdx.x == 0 && threadIdx.x % 32 == 0) p.ctl[kPrStatus] = start >= 0 && start <= end && end <= p.num_tokens ? GB_OK : GB_ERR_INVALID;
+  }
+  // The planner's part of the status, where there is none: by one thread, once.
+  static __device__ __forceinline__ void status(const PromptView& p) {
+    if (p.num_seqs != 1) return;
+    const int start = p.cu[0], end = p.cu[1];
+    p.ctl[kPrStatus] = start >= 0 && start <= end && end <= p.num_tokens ? GB_OK : GB_ERR_INVALID;
   }
   __device__ __forceinline__ PromptUnit operator()(const PromptView& p, int i) const {
     if (p.num_seqs != 1) return reinterpret_cast<const PromptUnit*>(p.ctl + kPrWords)[i];
@@ -130,7 +135,9 @@ struct PromptJob : PromptView {
   };
 
   __device__ __forceinline__ void error(int code) const { atomicCAS(&ctl[kPrStatus], GB_OK, code); }
-  __device__ __forceinline__ void begun() const {}
+  __device__ __forceinline__ void begun() const {
+    if (blockIdx.x == 0 && threadIdx.x % 32 == 0) PromptUnits::status(*this);
+  }
   using Units = PromptUnits;  // what the warp that takes the units holds
   __device__ __forceinline__ int total(const Units& all) const { return all.count * Hkv; }
   __device__ __forceinline__ int capacity() const { return most_units * Hkv; }
@@ -184,7 +191,7 @@ struct PromptJob : PromptView {
   }
   template <class Done>
   __device__ __forceinline__ void out(const flash::Unit& x, const Row& row, uint32_t a, uint32_t b, bool two, float wa,
-                                      float wb, float m, float l, Done done) const {
+                                      float wb, float m, float l, Done done, volatile int* again) const {
     const float inv = 1.f / l;
     __nv_bfloat16* dst = o + (x.w[0] + row.tok) * out_stride + row.head * flash::kD;
     bool fine = true;
@@ -206,29 +213,39 @@ struct PromptJob : PromptView {
               *reinterpret_cast<uint4*>(dst + c + 2 * i) = make_uint4(u[i], u[i + 1], u[i + 2], u[i + 3]);
         },
         done);
-    unsigned redo = __ballot_sync(0xffffffffu, row.valid && !fine && isfinite(m) && isfinite(l));
-    while (redo) {  // see sum_seen
-      const int src = __ffs(redo) - 1;
-      redo &= redo - 1;
-      const int tok = __shfl_sync(0xffffffffu, row.tok, src), head = __shfl_sync(0xffffffffu, row.head, src);
-      const float mr = __shfl_sync(0xffffffffu, m, src), ir = __shfl_sync(0xffffffffu, inv, src);
-      const long long s0 = x.w[0];
-      const __nv_bfloat16 *kh = k + s0 * k_stride + x.head * flash::kD, *vh = v + s0 * v_stride + x.head * flash::kD;
-      bool unseen = false;
-      for (long long j = tok + 1; j < (long long)x.nt * flash::kTok && s0 + j < num_tokens && !unseen; ++j)
-        unseen = flash::not_finite(vh + j * v_stride);
-      if (!unseen) continue;
-      float acc[4];
-      flash::sum_seen(
-          q + (s0 + tok) * q_stride + head * flash::kD, tok + 1,
-          [&](int j, const __nv_bfloat16*& kj, const __nv_bfloat16*& vj) {
-            kj = kh + j * k_stride;
-            vj = vh + j * v_stride;
-            return true;
-          },
-          qscale, mr, acc);
-      for (int i = 0; i < 4; ++i)
-        o[(s0 + tok) * out_stride + head * flash::kD + 4 * (threadIdx.x & 31) + i] = __float2bfloat16(acc[i] * ir);
+    if (row.valid && !fine && isfinite(m) && isfinite(l)) *again = 1;
+  }
+  // Rows that only met a value that is not finite in tokens they do not see, a row to a warp (see flash::one_row): those before
+  // the last such token of the unit's tiles.
+  __device__ __forceinline__ void again(const flash::Unit& x, int warp) const {
+    const int lane = threadIdx.x & 31, end = (int)min((long long)x.nt * flash::kTok, num_tokens - (long long)x.w[0]);
+    const long long s0 = x.w[0];
+    int last = -2;  // not looked for yet
+#pragma unroll 1
+    for (int i = warp; i < (x.mode == flash::kDual ? 2 : 1) * flash::kRows; i += flash::kKWarp) {
+      Row row;
+      find_row(x, i / flash::kRows, i % flash::kRows, row);
+      if (!row.valid) continue;
+      __nv_bfloat16* dst = o + (s0 + row.tok) * out_stride + row.head * flash::kD;
+      const uint2 y = reinterpret_cast<const uint2*>(dst)[lane];
+      if (!__any_sync(0xffffffffu, flash::not_finite(y.x) || flash::not_finite(y.y))) continue;
+      if (last == -2) {
+        last = -1;
+        for (int j = first_token(x, 0) + 1 + lane; j < end; j += 32)
+          if (flash::not_finite(v + (s0 + j) * v_stride + x.head * flash::kD)) last = j;
+        last = __reduce_max_sync(0xffffffffu, last);
+      }
+      if (row.tok >= last) continue;
+      float m, l, acc[4];
+      if (!flash::one_row(
+              q + (s0 + row.tok) * q_stride + row.head * flash::kD, row.tok + 1,
+              [&](int j, int kv, const __nv_bfloat16*& to) {
+                to = (kv ? v + (s0 + j) * v_stride : k + (s0 + j) * k_stride) + x.head * flash::kD;
+                return true;
+              },
+              qscale, m, l, acc))
+        continue;
+      for (int c = 0; c < 4; ++c) dst[4 * lane + c] = __float2bfloat16(acc[c] / l);
     }
   }
   __device__ __forceinline__ void drain_q(uint32_t bar) const {
@@ -293,6 +310,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_prompt_f32(PromptView p, co
   extern __shared__ __align__(16) unsigned char raw[];
   TileSmem& sm = *reinterpret_cast<TileSmem*>(raw);
   const PromptUnits all(p);
+  if (blockIdx.x == 0 && threadIdx.x == 0) PromptUnits::status(p);
   const int total = all.count * p.Hkv;
   for (int id = blockIdx.x; id < total; id += gridDim.x) {
     const PromptUnit e = all(p, id / p.Hkv);

@@ -46,3 +46,86 @@ def test_drafted_rows_past_the_count(cuda, t):
     assert all(torch.equal(o, out[0]) for o in out)
     assert max(times) < 3 * times[0], times
     assert x.pool.status() == 0
+
+
+def rows_of(q, k, v, rows, scale):
+    """(softmax(scale q.k) v, the same of |v|) of some rows of one causal sequence, in 64 bits."""
+    import torch
+    g = q.shape[1] // k.shape[1]
+    o, a = [], []
+    for i in rows:
+        kk, vv = (x[:i + 1].double().repeat_interleave(g, 1) for x in (k, v))
+        p = torch.softmax(torch.einsum("hd,thd->ht", q[i].double(), kk) * scale, -1)
+        o.append(torch.einsum("ht,thd->hd", p, vv))
+        a.append(torch.einsum("ht,thd->hd", p, vv.abs()))
+    return torch.stack(o), torch.stack(a)
+
+
+def test_behind_a_long_prompt(cuda):
+    """131072 tokens whose last one, and the next sequence, hold NaN: every row of the last tile but one is summed again over
+    all its keys, which takes longer than the other warps' usual waits, and none runs out."""
+    import torch
+    from paper_2608_08020_gb300.prompt import PromptAttention
+    n = 1 << 17
+    q, k, v = make("bf16", n + 300, 2, 1, 41)
+    v[n - 1:] = float("nan")
+    op = PromptAttention(2, 1, 128, "bf16", max_tokens=n + 300, max_seqs=2)
+    cu = torch.tensor([0, n, n + 300], dtype=torch.int32, device="cuda")
+    out = op(q, k, v, cu, 1 / math.sqrt(128))
+    assert op.status() == 0
+    assert bool(out[:n - 1].isfinite().all()) and not bool(out[n - 1:].isfinite().any())
+    rows = [n - 2, n - 3, n - 64, n - 65, n - 100, n - 128, n - 129]
+    o, a = rows_of(q, k, v, rows, 1 / math.sqrt(128))
+    assert bool(((out[rows].double() - o).abs() <= bound(o, a, "bf16")).all())
+
+
+def test_a_token_of_nan_in_a_prompt(cuda):
+    """Rows before it do not see it, rows from it on do and have nothing to sum again: it costs little."""
+    import torch
+    from paper_2608_08020_gb300.prompt import PromptAttention
+    n, at = 6000, 1001
+    q, k, v = make("bf16", n, 8, 2, 42)
+    op = PromptAttention(8, 2, 128, "bf16", max_tokens=n, max_seqs=1)
+    cu = torch.tensor([0, n], dtype=torch.int32, device="cuda")
+    out = torch.empty_like(q)
+    times = []
+    for fill in (0.0, float("nan")):
+        v[at, :, 7] = fill
+        times.append(milliseconds(lambda: op(q, k, v, cu, 1 / math.sqrt(128), out)))
+    assert op.status() == 0
+    bad = torch.zeros_like(out, dtype=torch.bool)
+    bad[at:, :, 7] = True
+    assert torch.equal(out.isnan(), bad)
+    rows = [at - 1, at - 2, at - 20, 960, 959, at, 1100, 5999]
+    vv = v.clone()
+    vv[at, :, 7] = 0
+    o, a = rows_of(q, k, vv, rows, 1 / math.sqrt(128))
+    ok = (out[rows].double() - o).abs() <= bound(o, a, "bf16")
+    assert bool((ok | bad[rows]).all())
+    assert times[1] < times[0] + 5, times
+
+
+def test_a_drafted_token_of_nan(cuda):
+    """Over a long context: its descendants see it, the tree's other tokens do not."""
+    import torch
+    from paper_2608_08020_gb300.draft import DraftTrees
+    x = Trees("bf16", hq=16, hkv=4, slots=3, beams=2, prompt=9000, room=600, pages=1200, seed=43)
+    trees = DraftTrees(x.pool, 20)
+    x.append(33)
+    parent = np.array([[-1, 0, 1, -1, 3, 4, 0, 6, 7, 2, 9, 5, 11, 12, 13, -1, 15, 16, 17, 18]] * 3)
+    q, k, v = (x.rand(3, 20, h, 128) for h in (16, 4, 4))
+    bad = v.clone()
+    bad[:, 4, :, 3] = float("nan")
+    bad[:, 6] = float("inf")
+    out = trees.attention(0, q, k, bad, x.ints(parent), x.scale)
+    assert x.pool.status() == 0
+    sees = seen(parent[0], 0)
+    for s in range(2):
+        K, V = (torch.cat([c[0], y[s]]) for c, y in zip(x.ctx[s], (k, v)))
+        o, a = attend_tree(q[s], K, V, x.scale, seen(parent[s], K.shape[0] - 20))
+        nan, inf = sees[:, 4], sees[:, 6]
+        want = torch.zeros_like(out[s], dtype=torch.bool)
+        want[nan, :, 3] = True
+        want[inf] = True
+        assert torch.equal(~out[s].isfinite(), want)
+        assert bool((((out[s].double() - o).abs() <= bound(o, a, "bf16")) | want).all())
