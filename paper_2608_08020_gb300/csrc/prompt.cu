@@ -152,8 +152,12 @@ struct PromptJob : PromptView {
     x.w[2] = e.ntok;
     x.w[3] = e.len;
   }
-  // A tile's rows past the sequence are the next one's, or past the tensor and zeros.
-  __device__ __forceinline__ uint32_t stale_rows(const flash::Unit&, int) const { return 0; }
+  // A tile's rows past the sequence are another one's or nobody's (past the tensor: zeros).
+  __device__ __forceinline__ uint32_t stale_rows(const flash::Unit& x, int j) const {
+    const int n = x.w[3] - j * flash::kTok;  // of the sequence, in the tile
+    const int rows = min(flash::kTok - n, num_tokens - x.w[0] - x.w[3]);
+    return n < flash::kTok && rows > 0 ? flash::stale_word(n, rows, 0, 0) : 0;
+  }
   __device__ __forceinline__ int page(const flash::Unit&, int, int) const { return 0; }
   __device__ __forceinline__ void load_tile(const flash::Unit& x, int j, int kv, int, uint32_t dst, uint32_t bar,
                                             int lane) const {

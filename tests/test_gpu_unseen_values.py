@@ -129,3 +129,29 @@ def test_a_drafted_token_of_nan(cuda):
         want[inf] = True
         assert torch.equal(~out[s].isfinite(), want)
         assert bool((((out[s].double() - o).abs() <= bound(o, a, "bf16")) | want).all())
+
+
+@pytest.mark.parametrize("lengths", [[700, 33, 1, 129, 900, 64], [4000, 90]])
+def test_rows_behind_a_sequence(cuda, lengths):
+    """Padding behind each sequence of a batch: whatever it holds, the same bits in the same time (within a factor of 3, and
+    a millisecond for the padding's own rows, which are not finite; row by row it took some 100 times as long)."""
+    import torch
+    from paper_2608_08020_gb300.prompt import PromptAttention
+    pad = 37
+    total = sum(lengths) + pad * len(lengths)
+    q, k, v = make("bf16", total, 16, 4, 44)
+    cu, past, at = [0], torch.ones(total, dtype=torch.bool, device="cuda"), 0
+    for n in lengths:                          # a sequence, then its padding as a sequence of its own, whose results nobody wants
+        past[at:at + n] = False
+        cu += [at + n, at + n + pad]
+        at += n + pad
+    op = PromptAttention(16, 4, 128, "bf16", max_tokens=total, max_seqs=2 * len(lengths))
+    at = torch.tensor(cu, dtype=torch.int32, device="cuda")
+    out, times = [], []
+    for fill in (0.0, float("nan"), float("-inf")):
+        v[past] = fill
+        out.append(op(q, k, v, at, 1 / math.sqrt(128))[~past])
+        times.append(milliseconds(lambda: op(q, k, v, at, 1 / math.sqrt(128))))
+    assert op.status() == 0
+    assert all(torch.equal(o, out[0]) for o in out) and bool(out[0].isfinite().all())
+    assert max(times) < 3 * times[0] + 1, times
