@@ -71,7 +71,7 @@ enum Mode : int { kJoint, kDual, kFirst, kSecond, kAlone };
 // of p - 15.  It has ended if the load of p - 10 into its stage has been issued, and that follows from what the group has seen:
 // the K and V of its tiles before, or that p's unit has begun (kBarBegin), so that every K before it is out.  Each warp loads in
 // order, and a load at q says that q - 5 was consumed, hence landed, hence that all loads of its kind before it are out.  The
-// blocks K V and K K V V, in any order, leave no p without such a chain (all sequences over the last ten positions gone through);
+// blocks K V and K K V V, in any order, leave no p without such a chain (tests/test_ring_order.py goes through sequences of units);
 // a loading warp's wait, for the consumption of p - 5, has p - 20 behind it in the same way.
 constexpr int kFulls = 3 * kStages;
 constexpr int kBarFull = 0;                       // [kFulls]
