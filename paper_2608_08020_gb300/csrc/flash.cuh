@@ -236,24 +236,7 @@ inline bool launches_with(const void* kernel) try {
 } catch (...) {
   return false;
 }
-// A warp's wait: all lanes go on or, when it ran out or the CTA gave up meanwhile, none does.  (What follows takes whole warps:
-// lanes that part company here would wait for each other for ever.)
-template <class Job>
-__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
-  uint64_t t0 = 0;
-  for (uint32_t it = 1;; ++it) {
-    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
-    if ((it & 63) == 0) {
-      const uint64_t now = globaltimer_ns();
-      if (t0 == 0) t0 = now;
-      if (__any_sync(0xffffffffu, *abort_flag != 0 || now - t0 > Job::kWaitNs)) {
-        *abort_flag = 1;
-        return false;
-      }
-    }
-  }
-}
-// The same with the lanes apart meanwhile, for the warps that write (8192 tokens: 384 us so, 388 with the other here too, 391 with
+// warp_wait (tc.cuh) with the lanes apart meanwhile, for the warps that write (8192 tokens: 384 us so, 388 with the other here too, 391 with
 // this one for the softmax too).
 template <class Job>
 __device__ __forceinline__ bool lanes_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
@@ -498,7 +481,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       };
       auto publish = [&](int u, const Unit& x) {
         const int slot = u & (kSlots - 1);
-        if (u >= kSlots) ok = warp_wait<Job>(ctl + kBarSchedFree + 8 * slot, (u / kSlots - 1) & 1, abort_flag);
+        if (u >= kSlots) ok = warp_wait<Job::kWaitNs>(ctl + kBarSchedFree + 8 * slot, (u / kSlots - 1) & 1, abort_flag);
         if (ok && lane == 0) {
           units[slot] = x;
           mbar_arrive(ctl + kBarSched + 8 * slot);
@@ -511,7 +494,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       auto load = [&](const Unit& z, const Places& at, int j, int page) {
         const uint32_t n = Job::kLongPair > 0 ? from + at.k(j) : from, st = n % kStages;
         if (n >= (uint32_t)kStages)
-          ok = warp_wait<Job>(ctl + kBarEmpty + 8 * ((n - kStages) % kFulls), ((n - kStages) / kFulls) & 1, abort_flag);
+          ok = warp_wait<Job::kWaitNs>(ctl + kBarEmpty + 8 * ((n - kStages) % kFulls), ((n - kStages) / kFulls) & 1, abort_flag);
         if (!ok) return;
         const uint32_t bar = ctl + kBarFull + 8 * (n % kFulls);
         if (lane == 0) mbar_arrive_expect_tx(bar, kTile);
@@ -591,7 +574,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       auto fetch = [&](int u, Unit& to) {
         const int slot = u & (kSlots - 1);
         to.nt = -1;
-        if (!(ok = warp_wait<Job>(ctl + kBarSched + 8 * slot, (u / kSlots) & 1, abort_flag))) return;
+        if (!(ok = warp_wait<Job::kWaitNs>(ctl + kBarSched + 8 * slot, (u / kSlots) & 1, abort_flag))) return;
         to = units[slot];
         __syncwarp();
         if (lane == 0) mbar_arrive(ctl + kBarSchedFree + 8 * slot);
@@ -611,7 +594,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       };
       // A stage's release, or with `landed` only the tile to be mended, which meanwhile is mended as soon as it is in.
       auto wait = [&](uint32_t bar, uint32_t parity, bool landed) {
-        if (!stale) return warp_wait<Job>(bar, parity, abort_flag);  // (a suspended wait leaves the issue slots to others)
+        if (!stale) return warp_wait<Job::kWaitNs>(bar, parity, abort_flag);  // (a suspended wait leaves the issue slots to others)
         uint64_t t0 = 0;
         for (uint32_t it = 1;; ++it) {
           int f = 0;
@@ -758,7 +741,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       uint32_t n = 0, c = 0;    // the group's tiles, and units in which it had any
       bool ok = true;
       auto wait = [&](uint32_t bar, uint32_t parity) {
-        ok = warp_wait<Job>(bar, parity, abort_flag);
+        ok = warp_wait<Job::kWaitNs>(bar, parity, abort_flag);
         return ok;
       };
       for (int u = 0; ok; ++u) {
@@ -851,7 +834,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
         const uint32_t bar = ctl + kBarSched + 8 * slot, parity = (u_next / kSlots) & 1;
         if (!patient) {
           if (!__all_sync(0xffffffffu, mbar_test(bar, parity))) return true;
-        } else if (!warp_wait<Job>(bar, parity, abort_flag)) {
+        } else if (!warp_wait<Job::kWaitNs>(bar, parity, abort_flag)) {
           return false;
         }
         if (units[slot].nt < 0) break;
@@ -891,7 +874,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       known = false;
       for (int i = 0; i < mine; ++i, ++n) {
         const int t = group_tile(mode, g, i);
-        if (!warp_wait<Job>(ctl + kBarS + 8 * g, n & 1, abort_flag)) { alive = false; break; }
+        if (!warp_wait<Job::kWaitNs>(ctl + kBarS + 8 * g, n & 1, abort_flag)) { alive = false; break; }
         if (Job::kEarlyQ && i + 1 == mine && !(alive = begin_next(false))) break;
         tc_fence_after();
         uint32_t su[128];
@@ -965,7 +948,7 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       if (!(alive = begin_next(true))) break;
       if (units[sy].nt >= 0) job.loaded_q(r, ctl + kBarQ + 8 * g);
       // (m, l) go to the warps that write, once they have those of the group's unit before.
-      if (c_done > 0 && !(alive = warp_wait<Job>(ctl + kBarOFree + 8 * g, (c_done - 1) & 1, abort_flag))) break;
+      if (c_done > 0 && !(alive = warp_wait<Job::kWaitNs>(ctl + kBarOFree + 8 * g, (c_done - 1) & 1, abort_flag))) break;
       ++c_done;
       xch[g * 128 + r] = make_float2(m_ref, l);
       __syncwarp();

@@ -537,7 +537,7 @@ __device__ __forceinline__ void grouped_body(const PoolView& v, const Counters& 
     bool alive = true;
     for (;; ++uidx) {
       const int k = uidx & (kSchedSlots - 1);
-      if (!wait_or_abort(ctl + kBarSchedFull + 8 * k, (uidx / kSchedSlots) & 1, abort_flag)) break;
+      if (!warp_wait(ctl + kBarSchedFull + 8 * k, (uidx / kSchedSlots) & 1, abort_flag)) break;
       const int id = sched[k];
       __syncwarp();
       if (lane == 0) mbar_arrive(ctl + kBarSchedEmpty + 8 * k);
@@ -552,7 +552,7 @@ __device__ __forceinline__ void grouped_body(const PoolView& v, const Counters& 
       for (int j = 0; j < x.ntok; ++j, ++n) {
         const uint32_t sb = n % kSBufs;
         const uint32_t sp_addr = tmem + sb * 128 + grp * 64 + lane_base;
-        if (!wait_or_abort(ctl + kBarSFull + 8 * sb, (n / kSBufs) & 1, abort_flag)) { alive = false; break; }
+        if (!warp_wait(ctl + kBarSFull + 8 * sb, (n / kSBufs) & 1, abort_flag)) { alive = false; break; }
         tc_fence_after();
         const int valid = min(max(x.Ts - j * kTok - grp * kHalf, 0), kHalf);  // this group's tokens in the tile
         float sv[kHalf];
@@ -582,13 +582,13 @@ __device__ __forceinline__ void grouped_body(const PoolView& v, const Counters& 
         xch[(slot * 2 + grp) * 128 + r] = mt_own;
         __syncwarp();
         if (lane == 0) mbar_arrive(ctl + kBarMaxFull + 8 * slot);
-        if (!wait_or_abort(ctl + kBarMaxFull + 8 * slot, (n >> 1) & 1, abort_flag)) { alive = false; break; }
+        if (!warp_wait(ctl + kBarMaxFull + 8 * slot, (n >> 1) & 1, abort_flag)) { alive = false; break; }
         const float mt = fmaxf(mt_own, xch[(slot * 2 + 1 - grp) * 128 + r]);
         const bool raise = mt > m_ref + 8.f;
         if (j > 0 && __any_sync(0xffffffffu, raise)) {
           // O must hold P.V(n-1) and nothing newer before it is rescaled; each group
           // rescales its half of the columns.
-          if (!wait_or_abort(ctl + kBarPvDone + 8 * ((n - 1) % kSBufs), ((n - 1) / kSBufs) & 1, abort_flag)) {
+          if (!warp_wait(ctl + kBarPvDone + 8 * ((n - 1) % kSBufs), ((n - 1) / kSBufs) & 1, abort_flag)) {
             alive = false;
             break;
           }
@@ -639,13 +639,13 @@ __device__ __forceinline__ void grouped_body(const PoolView& v, const Counters& 
       // Unit end: O is final once P.V of the last tile has completed.  The groups add their
       // row sums (same max); slot n & 1 is free (its last reader passed the previous tile).
       const uint32_t last = n - 1;
-      if (!wait_or_abort(ctl + kBarPvDone + 8 * (last % kSBufs), (last / kSBufs) & 1, abort_flag)) break;
+      if (!warp_wait(ctl + kBarPvDone + 8 * (last % kSBufs), (last / kSBufs) & 1, abort_flag)) break;
       tc_fence_after();
       const int slot = n & 1;
       xch[(slot * 2 + grp) * 128 + r] = l;
       __syncwarp();
       if (lane == 0) mbar_arrive(ctl + kBarXchFull);
-      if (!wait_or_abort(ctl + kBarXchFull, uidx & 1, abort_flag)) break;
+      if (!warp_wait(ctl + kBarXchFull, uidx & 1, abort_flag)) break;
       const float l_all = l + xch[(slot * 2 + 1 - grp) * 128 + r];
       const int b = bk / kMaxSegDepth;
       const bool has = m < x.g && r_idx < kMaxSegRecords;
@@ -671,7 +671,7 @@ __device__ __forceinline__ void grouped_body(const PoolView& v, const Counters& 
       if (lane == 0) mbar_arrive(ctl + kBarOFree);
       // Every warp has read this unit's sums before the next unit's first tile rewrites
       // the exchange slot.
-      if (!wait_or_abort(ctl + kBarOFree, uidx & 1, abort_flag)) break;
+      if (!warp_wait(ctl + kBarOFree, uidx & 1, abort_flag)) break;
     }
   }
 

@@ -114,4 +114,22 @@ __device__ __forceinline__ bool wait_or_abort(uint32_t bar, uint32_t parity, vol
   }
 }
 
+// A warp's wait: all lanes go on or, when it ran out or the CTA gave up meanwhile, none does.  (What follows takes whole warps:
+// lanes that part company here would wait for each other for ever.)
+template <uint64_t kLimitNs = kWaitLimitNs>
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  uint64_t t0 = 0;
+  for (uint32_t it = 1;; ++it) {
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+    if ((it & 63) == 0) {
+      const uint64_t now = globaltimer_ns();
+      if (t0 == 0) t0 = now;
+      if (__any_sync(0xffffffffu, *abort_flag != 0 || now - t0 > kLimitNs)) {
+        *abort_flag = 1;
+        return false;
+      }
+    }
+  }
+}
+
 }  // namespace gb
