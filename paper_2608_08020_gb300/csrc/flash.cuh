@@ -221,7 +221,7 @@ __device__ __forceinline__ void st32(void* p, const uint32_t* u) {
                "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7])
                : "memory");
 }
-// Whether a kernel of this pipeline has the registers at launch that its warps then share out.
+// Whether a kernel of this pipeline has the registers at launch that its warps then share out (fewer, and they would wait for ever).
 inline bool launches_with(const void* kernel) try {
   static std::mutex mu;
   static std::set<std::pair<const void*, int>> fine;  // (kernel, device)
@@ -230,7 +230,8 @@ inline bool launches_with(const void* kernel) try {
   std::lock_guard<std::mutex> lock(mu);
   if (fine.count({kernel, device})) return true;
   cudaFuncAttributes a{};
-  if (cudaFuncGetAttributes(&a, kernel) != cudaSuccess || a.numRegs != kLaunchRegs) return false;
+  if (cudaFuncGetAttributes(&a, kernel) != cudaSuccess || a.numRegs * kThreads < 256 * (kSoftmaxRegs + kOtherRegs))
+    return false;
   fine.insert({kernel, device});
   return true;
 } catch (...) {
