@@ -536,13 +536,14 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
         begin(u);
         if (pair) begin(u + 1);
         for (int j = 0; j < tiles && ok; ++j) {
-          if (j < x.nt) {
-            load(x, at_x, j, page_x);
-            if (j + 1 < x.nt) page_x = job.page(x, j + 1, lane);
-          }
-          if (pair && j < y.nt && ok) {
-            load(y, at_y, j, page_y);
-            if (j + 1 < y.nt) page_y = job.page(y, j + 1, lane);
+#pragma unroll 1
+          for (int e = 0; e < (pair ? 2 : 1) && ok; ++e) {  // (one copy of a load's code)
+            const Unit z = e ? y : x;
+            if (j >= z.nt) continue;
+            load(z, e ? at_y : at_x, j, e ? page_y : page_x);
+            const int next = j + 1 < z.nt ? job.page(z, j + 1, lane) : 0;
+            if (e) page_y = next;
+            else page_x = next;
           }
           if (j == 0 && ok) {
             if (pair) find(u + 2, a);
@@ -620,12 +621,14 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
       auto load = [&](const Unit& now, const Places& at, int j, int page) {
         const uint32_t n = Job::kLongPair > 0 ? from + at.v(j) : from + 1;
         const uint32_t st = n % kStages, dst = sbase + kRing + st * kTile, full = ctl + kBarFull + 8 * (n % kFulls);
-        if (n >= (uint32_t)kStages)
-          ok = wait(ctl + kBarEmpty + 8 * ((n - kStages) % kFulls), ((n - kStages) / kFulls) & 1, false);
+        const uint32_t rows = job.stale_rows(now, j);
+        // The stage's release, then, since one tile waits at a time, the one before (one wait in the code: it is inlined).
+#pragma unroll 1
+        for (int landed = n < (uint32_t)kStages; ok && landed < (rows && stale ? 2 : 1); ++landed)
+          ok = wait(ctl + kBarEmpty + 8 * ((n - kStages) % kFulls), ((n - kStages) / kFulls) & 1, landed != 0);
         if (!ok) return;
         uint32_t bar = full;
-        if (const uint32_t rows = job.stale_rows(now, j)) {
-          if (stale && !(ok = wait(0, 0, true))) return;  // one at a time
+        if (rows) {
           stale = rows;
           p_dst = dst;
           p_full = full;
@@ -650,13 +653,14 @@ __device__ __forceinline__ void body(const Job& job, unsigned char* sm) {
         const int tiles = pair ? max(x.nt, y.nt) : x.nt, both = pair ? min(x.nt, y.nt) : 0;
         const Places at_x = places<Job>(both, false), at_y = places<Job>(both, true);
         for (int j = 0; j < tiles && ok; ++j) {
-          if (j < x.nt) {
-            load(x, at_x, j, page_x);
-            if (j + 1 < x.nt) page_x = job.page(x, j + 1, lane);
-          }
-          if (pair && j < y.nt && ok) {
-            load(y, at_y, j, page_y);
-            if (j + 1 < y.nt) page_y = job.page(y, j + 1, lane);
+#pragma unroll 1
+          for (int e = 0; e < (pair ? 2 : 1) && ok; ++e) {  // (one copy of a load's code)
+            const Unit z = e ? y : x;
+            if (j >= z.nt) continue;
+            load(z, e ? at_y : at_x, j, e ? page_y : page_x);
+            const int next = j + 1 < z.nt ? job.page(z, j + 1, lane) : 0;
+            if (e) page_y = next;
+            else page_x = next;
           }
         }
         if (!ok) break;
