@@ -500,7 +500,8 @@ gb_status gb_scorer_step(gb_pool* step_pool, const gb_scorer_config* cfg, const 
  *   num_tokens:    rows of q, k, v and out; rows outside every sequence are left as they were
  *   workspace:     gb_prompt_workspace_bytes, 256-byte aligned; calls using one workspace must be ordered
  * Values in rows a query does not see (later tokens, other sequences) do not reach its result, whatever
- * they are.  Launches: the attention, and before it, unless num_seqs is 1, a planner that lists the work longest first;
+ * they are; rows outside its sequence cost nothing, a later token of its own that is not finite costs the rows before it that
+ * share a tile of 128 keys with it a sum each of their own (milliseconds).  Launches: the attention, and before it, unless num_seqs is 1, a planner that lists the work longest first;
  * none, and the status stays, without tokens or sequences.
  * Errors: GB_ERR_INVALID for bad sizes, alignment, strides, overlap, a workspace that is too small or a
  * scale that is not positive and finite; GB_ERR_UNSUPPORTED unless (dtype, head_dim) is (GB_BF16, 128)
@@ -571,7 +572,11 @@ typedef struct {
   int n_draft;
 } gb_draft;
 
-/* Workspace of a pool's draft rounds of n_draft tokens (work lists and partial results). */
+/*
+ * Workspace of a pool's draft rounds of n_draft tokens (work lists and partial results): little more than
+ * (6 max_beams + 2 x multiprocessors) x n_draft x num_q_heads x (head_dim + 2) x 4 bytes, the records that long or shared
+ * contexts may be split into: 0.2 GiB for 64 slots, 16 tokens and 32 heads of 128; 1.8 GiB for 256 slots of 64 tokens.
+ */
 gb_status gb_draft_workspace_bytes(gb_pool* pool, int n_draft, size_t* bytes);
 
 /*

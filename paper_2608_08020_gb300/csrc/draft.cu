@@ -13,8 +13,8 @@
 //
 // Bound by the reads of the cache while rows x 2 flops a byte stay below the machine's ~280, i.e. up to some
 // 100 rows a shared token, and by the tensor cores beyond.  Measured (bf16): a layer of 64 traces at 4000 tokens, trees of up to
-// 16, 116 us with its plan and join (387 MB in 92 us inside the attention, 4.2 TB/s); 198 traces at 8000 tokens 258 us; a
-// layer of 128 traces of 190 tokens 46 us.
+// 16, 114 us with its plan and join (387 MB in 95 us inside the attention, 4.1 TB/s); 198 traces at 8000 tokens 255 us; a
+// layer of 128 traces of 190 tokens 44 us.
 #include <algorithm>
 #include <atomic>
 #include <type_traits>

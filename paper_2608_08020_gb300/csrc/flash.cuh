@@ -7,9 +7,10 @@
 //
 // A unit has one head's query rows and nt tiles of 128 keys.  Two groups of four softmax warps each hold
 // a Q tile of 128 rows, an accumulator O and an S tile in tensor memory (512 columns in all), so that two chains are in flight:
-// while one group takes the exponentials of its S tile the tensor core works for the other.  Per tile 1024
-// cycles of products (128^3 x 2 at 4096 multiply-adds a cycle) stand against 512 of ex2 (32 a cycle) and about 400 of
-// other instructions.  What a group works on:
+// while one group takes the exponentials of its S tile the tensor core works for the other.  A tile of each group is 2048
+// cycles of products (128^3 x 2 each at 4096 multiply-adds a cycle); a long prompt takes some 3300 for it, since the chain from an
+// S tile to the group's next one (scores read, maximum, 128 x 128 ex2 and their sums, P written, P.V, S) is longer than the
+// other group's products, and what of it the two groups do not cover the tensor core waits.  What a group works on:
 //   dual          129 to 256 rows: each group half of the rows, every K/V tile serves both
 //   first, second up to 128 rows: two units of the CTA's list, a group each, their tiles coming by turns
 //   joint         up to 128 rows and no second unit: the same rows in both groups, group g takes tiles g, g + 2, ...,
@@ -17,8 +18,9 @@
 //   alone         the same with a single tile, or where the job does not allow joint units: group 0
 // A row's sum goes over the keys in the same order in every mode but joint.
 //
-// P is rounded to bf16 for the tensor core (relative 2^-9 each, independent, so a result's error
-// is about that of its own rounding to bf16); the sum l is of the unrounded values.
+// P is rounded to bf16 for the tensor core: at most 2^-8 of each p, independent of one another, so a row's error is about that
+// of its own rounding to bf16 (1.2 to 1.4 times a result's whose p are fp32).  A second term of 8 bits would be a P.V more for each
+// tile, half as many products again.  The decode step's grouped role rounds the same way.  The sum l is of the unrounded values.
 //
 // Warp roles (512 threads):
 //   warps 0-7    softmax: thread r of group g owns row r of its tile (tensor-memory lane r); also loads

@@ -7,8 +7,9 @@
 // Bound by the tensor cores from a few hundred tokens on (2 D Hq n^2 flops against 4 D (Hq + Hkv) n bytes).
 // A planner CTA lists the units (sequence, run of tokens), longest first; a CTA per SM takes its (unit, KV head) pairs
 // in turn.  One prompt's units need no list.  bf16: flash.cuh; fp32: tile.cuh.
-// Measured (32 query heads, 8 KV heads, bf16): 8192 tokens 389 us, 1.41 PFLOP/s of the 1.88 of a large library product; 16384
-// tokens of 16 and 2 heads 745 us, 1.48 PFLOP/s; 333 tokens 12 us, of which the host's call is 10.
+// Measured (32 query heads, 8 KV heads, bf16): 8192 tokens 379 us, 1.45 PFLOP/s of the 1.88 of a large library product; 16384
+// tokens of 16 and 2 heads 716 us, 1.54 PFLOP/s; 24 packed prompts of up to 2048 tokens 73 us; 333 tokens 11 us, of which the
+// host's call is 9 to 10.
 #include <algorithm>
 #include <mutex>
 
@@ -86,8 +87,8 @@ struct PromptView {
   long long q_stride, k_stride, v_stride, out_stride;  // elements between tokens
 };
 
-// The units.  One prompt's are known from its bounds, longest first, without the planner's launch (5 us of a 16 us call
-// of 333 tokens).
+// The units.  One prompt's are known from its bounds, longest first, without the planner's launch (a call of 333 tokens took
+// 5 us more with it).
 struct PromptUnits {
   int start, len, per, count;
   __device__ __forceinline__ explicit PromptUnits(const PromptView& p) {
