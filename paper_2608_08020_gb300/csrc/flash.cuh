@@ -368,7 +368,7 @@ __device__ __forceinline__ bool one_row(const __nv_bfloat16* q, int nkeys, Key k
       for (int i = 0; i < 4; ++i) acc[i] *= f;
       m = mx;
     }
-    const float p = on ? exp2f(s - m) : 0.f;
+    const float p = on ? exp2f(s - (m == -INFINITY ? 0.f : m)) : 0.f;  // (scores of -inf alone so far: every p is 0)
     l += p;
     const unsigned there = __ballot_sync(0xffffffffu, on);
 #pragma unroll 1

@@ -155,3 +155,26 @@ def test_rows_behind_a_sequence(cuda, lengths):
     assert op.status() == 0
     assert all(torch.equal(o, out[0]) for o in out) and bool(out[0].isfinite().all())
     assert max(times) < 3 * times[0] + 1, times
+
+
+def test_scores_of_minus_infinity_first(cuda):
+    """Rows whose first keys all score minus infinity, answered anew because of a later token: those keys weigh nothing."""
+    import torch
+    from paper_2608_08020_gb300.prompt import PromptAttention
+    n, low, at = 300, 50, 200
+    q, k, v = make("bf16", n, 8, 2, 45)
+    q[:, :, 0] = q[:, :, 0].abs() + 0.5
+    k[:low, :, 0] = float("-inf")
+    v[at, 1] = float("nan")
+    op = PromptAttention(8, 2, 128, "bf16", max_tokens=n, max_seqs=1)
+    out = op(q, k, v, torch.tensor([0, n], dtype=torch.int32, device="cuda"), 1 / math.sqrt(128))
+    assert op.status() == 0
+    want = torch.zeros_like(out, dtype=torch.bool)
+    want[:low] = True                          # nothing but minus infinity
+    want[at:, 4:] = True                       # the heads that see the NaN
+    assert torch.equal(out.isnan(), want)
+    rows = [low, low + 1, 127, 128, 180, at - 1]
+    vv = v.clone()
+    vv[at, 1] = 0
+    o, a = rows_of(q[:, :, :], k, vv, rows, 1 / math.sqrt(128))
+    assert bool(((out[rows].double() - o).abs() <= bound(o, a, "bf16")).all())
