@@ -223,7 +223,7 @@ struct PromptJob : PromptView {
   // Rows that only met a value that is not finite in tokens they do not see, a row to a warp (see flash::one_row): those before
   // the last such token of the unit's tiles.
   __device__ __forceinline__ void again(const flash::Unit& x, int warp) const {
-    const int lane = threadIdx.x & 31, end = (int)min((long long)x.nt * flash::kTok, num_tokens - (long long)x.w[0]);
+    const int lane = threadIdx.x & 31, end = min(x.nt * flash::kTok, x.w[3]);  // (rows behind the sequence were made zero)
     const long long s0 = x.w[0];
     int last = -2;  // not looked for yet
 #pragma unroll 1

@@ -178,3 +178,21 @@ def test_scores_of_minus_infinity_first(cuda):
     vv[at, 1] = 0
     o, a = rows_of(q[:, :, :], k, vv, rows, 1 / math.sqrt(128))
     assert bool(((out[rows].double() - o).abs() <= bound(o, a, "bf16")).all())
+
+
+def test_nan_within_and_behind(cuda):
+    """Rows that are not finite by a token they see are not answered anew for what lies behind their sequence."""
+    import torch
+    from paper_2608_08020_gb300.prompt import PromptAttention
+    n = 8000
+    q, k, v = make("bf16", n + 40, 16, 4, 46)
+    op = PromptAttention(16, 4, 128, "bf16", max_tokens=n + 40, max_seqs=1)
+    cu = torch.tensor([0, n], dtype=torch.int32, device="cuda")
+    out = torch.empty_like(q)
+    times = []
+    for at in ([], [0], [0, n]):
+        for i in at:
+            v[i:n + 40 if i else 1] = float("nan")
+        times.append(milliseconds(lambda: op(q, k, v, cu, 1 / math.sqrt(128), out)))
+    assert op.status() == 0 and not bool(out[:n].isfinite().any())
+    assert times[2] < times[1] + 1, times
