@@ -239,8 +239,8 @@ inline bool launches_with(const void* kernel) try {
 } catch (...) {
   return false;
 }
-// warp_wait (tc.cuh) with the lanes apart meanwhile, for the warps that write (8192 tokens: 384 us so, 388 with the other here too, 391 with
-// this one for the softmax too).
+// warp_wait (tc.cuh) with the lanes apart meanwhile, for the warps that write (8192 tokens when it was chosen: 384 us so, 388 with
+// the other here too, 391 with this one for the softmax too).
 template <class Job>
 __device__ __forceinline__ bool lanes_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
   return __all_sync(0xffffffffu, wait_or_abort(bar, parity, abort_flag, Job::kWaitNs));
