@@ -53,6 +53,7 @@ typedef int gb_status;
 /* Element types. */
 #define GB_F32 0
 #define GB_BF16 1
+#define GB_FP8 2  /* a pool's K/V in 8 bits; its queries and new rows are GB_BF16 (gb_pool_config) */
 
 /* Decode path selection for gb_decode_attention(). */
 #define GB_PATH_AUTO 0      /* grouped tensor-core path where a shared segment is dense enough and the step is not tiny */
@@ -66,14 +67,25 @@ typedef struct {
   int num_layers;          /* layers sharing one page id space (a page spans all layers) */
   int num_q_heads;         /* Hq */
   int num_kv_heads;        /* Hkv; Hq % Hkv == 0 */
-  int head_dim;            /* D: 128 for GB_BF16, 64 for GB_F32 */
+  int head_dim;            /* D: 128 for GB_BF16 and GB_FP8, 64 for GB_F32 */
   int page_size;           /* P tokens per page: 16, 32 or 64 */
-  int kv_dtype;            /* GB_F32 or GB_BF16: K/V storage and the query dtype */
+  int kv_dtype;            /* GB_F32 or GB_BF16: K/V storage and the query dtype; GB_FP8: storage, rows given in GB_BF16 */
   int64_t num_pages;       /* pages in the pool */
   int max_beams;           /* slots = capacity C of the tournament, <= 1024 */
   int max_pages_per_beam;  /* block-table width */
   int group_min_beams;     /* grouped path only for segments shared by >= this many beams (0: default 2) */
 } gb_pool_config;
+
+/*
+ * Pools of 8 bits (kv_dtype GB_FP8; query heads per KV head 1, 2, 4 or 8).  The cache holds e4m3 values and, for each
+ * block of 16 tokens (by position, a part of a page) of one head's K or V, an exponent e that stands for a factor 2^e: the least
+ * e in [-60, 60] with every row written to the block within 448 2^e.  A row x is held as the e4m3 value nearest to x 2^-e (ties to
+ * even; past 448 where e would pass 60: 448), times 2^e; a value that is not finite is held as NaN.  A later row that does
+ * not fit raises its block's e, and the rows before it are rounded again; a block's first row begins its exponent anew, a cut
+ * (gb_truncate) keeps it.  Every call that takes or gives rows "in kv_dtype" takes or gives GB_BF16 ones.  All calls but gb_draft_* and
+ * gb_accept_draft (GB_ERR_UNSUPPORTED) take such pools; the sequence scorer's step pool is a GB_BF16 one.
+ * The paper's searches end where the KV cache fills the memory (Section 3.2): this holds twice the tokens.
+ */
 
 /* Host-side copies of the pool state, for tests and debugging (any member may be NULL). */
 typedef struct {
@@ -93,7 +105,8 @@ typedef struct {
 /*
  * Sizes of the two caller-allocated device buffers for a configuration.
  * kv_bytes: the paged KV pool, laid out [layer][page][K|V][kv_head][P][D] in
- * kv_dtype.  meta_bytes: block tables, refcounts, free bitmap, per-slot
+ * kv_dtype (GB_FP8: a byte a value, then from the next multiple of 256 bytes on the exponents, one signed byte each,
+ * [layer][page][K|V][kv_head][P / 16]).  meta_bytes: block tables, refcounts, free bitmap, per-slot
  * scores, decode plans and split-KV partials.  Either output may be NULL.
  * Paged KV and block tables: Section 3.1 (branching "via prefix caching",
  * pruning "frees their non-shared KV-cache blocks").
@@ -167,6 +180,50 @@ gb_status gb_decode_attention(gb_pool* pool, int layer, const void* q_dev, const
  */
 gb_status gb_append_kv(gb_pool* pool, int layer, int n_tokens, const void* k_dev,
                        const void* v_dev, gb_stream_t stream);
+
+/*
+ * Rotary position embedding, applied to keys (and queries) on their way: the pair (a, b) at position t becomes
+ *   (a cos - b sin, b cos + a sin) of the pair's angle at t,
+ * where the pairs are the values (i, i + rotary_dim / 2), or (2i, 2i + 1) when interleaved, of each head's first rotary_dim
+ * values; the rest stay.  Each result is rounded once, to the type that it goes on in (the cache's, the query's).
+ *   table_dev: fp32 [positions][rotary_dim / 2][4], 16-byte aligned: cos, its rounding error (the exact value minus the
+ *              rounded one, rounded), sin, its rounding error; any angles, and amplitudes too, as the caller fills it
+ *   rotary_dim: a multiple of 16, at most head_dim
+ * A token at a position that the table does not have is not rotated, and the device status records GB_ERR_INVALID.
+ */
+typedef struct {
+  const float* table_dev;
+  int positions;
+  int rotary_dim;
+  int interleaved;  /* 0 or 1 */
+} gb_rotation;
+
+/*
+ * gb_append_kv with the keys rotated to the positions that they are appended at.  Errors: as gb_append_kv, and
+ * GB_ERR_INVALID for a bad rotation or rows that do not start on 16 bytes, GB_ERR_STATE when the pool is on another device
+ * than the current one.
+ */
+gb_status gb_append_kv_rotated(gb_pool* pool, int layer, int n_tokens, const gb_rotation* rotation, const void* k_dev,
+                               const void* v_dev, gb_stream_t stream);
+
+/*
+ * gb_decode_attention with the step's queries and keys rotated to the step's position of each slot (the inputs are
+ * left as they are).  One launch more than gb_decode_attention on GB_F32 and GB_BF16 pools.  Errors: as
+ * gb_decode_attention and gb_append_kv_rotated.
+ */
+gb_status gb_decode_attention_rotated(gb_pool* pool, int layer, const gb_rotation* rotation, const void* q_dev,
+                                      const void* k_new_dev, const void* v_new_dev, float scale, float* out_dev, int flags,
+                                      gb_stream_t stream);
+
+/*
+ * What the cache holds: tokens first_dev[b] .. first_dev[b] + n_tokens - 1 (int32 [max_beams]) of every slot, one layer.
+ *   k_out_dev, v_out_dev: [n_tokens][max_beams][Hkv][D] in kv_dtype (GB_BF16 for GB_FP8 pools: exact), 16-byte aligned;
+ *                         zeros where a slot has no such token
+ * For moving a trace elsewhere, and for tests.  One launch.  Errors: GB_ERR_INVALID for bad arguments, GB_ERR_STATE for an
+ * unseeded pool, inside an open step, or when the pool is on another device than the current one.
+ */
+gb_status gb_read_kv(gb_pool* pool, int layer, const int32_t* first_dev, int n_tokens, void* k_out_dev, void* v_out_dev,
+                     gb_stream_t stream);
 
 /*
  * Scorer probe at a thought boundary and the running-mean update of

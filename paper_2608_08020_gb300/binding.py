@@ -20,13 +20,13 @@ GB_OK, GB_ERR_INVALID, GB_ERR_OOM, GB_ERR_CUDA, GB_ERR_STATE, GB_ERR_TIMEOUT, GB
 GB_ERR_TOO_LARGE = 7
 STATUS_NAMES = {0: "GB_OK", 1: "GB_ERR_INVALID", 2: "GB_ERR_OOM", 3: "GB_ERR_CUDA", 4: "GB_ERR_STATE",
                 5: "GB_ERR_TIMEOUT", 6: "GB_ERR_UNSUPPORTED", 7: "GB_ERR_TOO_LARGE"}
-GB_F32, GB_BF16 = 0, 1
+GB_F32, GB_BF16, GB_FP8 = 0, 1, 2
 STATS_WORDS = 10  # words per record of gb_pool_read_step_stats
 GB_PATH_AUTO, GB_PATH_PER_BEAM, GB_PATH_GROUPED = 0, 1, 2
 
 # Every symbol the header declares, in header order.
 EXPORTS = ["gb_pool_workspace_bytes", "gb_pool_init", "gb_pool_destroy", "gb_pool_seed", "gb_decode_attention",
-           "gb_append_kv", "gb_score_probe", "gb_push_scores", "gb_prune_branch", "gb_release", "gb_pool_status",
+           "gb_append_kv", "gb_append_kv_rotated", "gb_decode_attention_rotated", "gb_read_kv", "gb_score_probe", "gb_push_scores", "gb_prune_branch", "gb_release", "gb_pool_status",
            "gb_pool_clear_status", "gb_pool_wait_selftest", "gb_pool_read_state", "gb_pool_set_profile_events", "gb_pool_launch_count",
            "gb_paged_decode_noalloc", "gb_paged_decode_noalloc_status", "gb_pool_read_step_stats", "gb_pool_set_capacity", "gb_pool_last_ranked", "gb_score_mlp", "gb_fork_slots", "gb_scorer_sizes", "gb_scorer_seed",
            "gb_scorer_step", "gb_prompt_workspace_bytes", "gb_prompt_attention", "gb_prompt_status", "gb_prompt_wait_selftest",
@@ -71,6 +71,11 @@ class GbDraft(ctypes.Structure):
                 ("workspace_bytes", ctypes.c_size_t), ("n_draft", ctypes.c_int)]
 
 
+class GbRotation(ctypes.Structure):
+    _fields_ = [("table_dev", ctypes.c_void_p), ("positions", ctypes.c_int), ("rotary_dim", ctypes.c_int),
+                ("interleaved", ctypes.c_int)]
+
+
 class GambitError(RuntimeError):
     def __init__(self, code: int, what: str):
         super().__init__(f"{STATUS_NAMES.get(code, code)}: {what}")
@@ -97,6 +102,9 @@ def load(path: Path | None = None) -> ctypes.CDLL:
         "gb_pool_seed": [V, I, I, V, V, V],
         "gb_decode_attention": [V, I, V, V, V, F, V, I, V],
         "gb_append_kv": [V, I, I, V, V, V],
+        "gb_append_kv_rotated": [V, I, I, P, V, V, V],
+        "gb_decode_attention_rotated": [V, I, P, V, V, V, F, V, I, V],
+        "gb_read_kv": [V, I, V, I, V, V, V],
         "gb_score_probe": [V, V, I, I, V, F, V, V, V],
         "gb_push_scores": [V, V, V, V],
         "gb_prune_branch": [V, I, I, I, V, V, V, V, V],
@@ -240,6 +248,21 @@ def gb_decode_attention(pool: int, layer: int, q, k_new, v_new, scale: float, ou
 
 def gb_append_kv(pool: int, layer: int, n_tokens: int, k, v, stream=None) -> None:
     _check(pool, load().gb_append_kv(pool, layer, n_tokens, ptr(k), ptr(v), stream_handle(stream)), "gb_append_kv")
+
+
+def gb_append_kv_rotated(pool: int, layer: int, n_tokens: int, rotation: GbRotation, k, v, stream=None) -> None:
+    _check(pool, load().gb_append_kv_rotated(pool, layer, n_tokens, ctypes.byref(rotation), ptr(k), ptr(v), stream_handle(stream)),
+           "gb_append_kv_rotated")
+
+
+def gb_decode_attention_rotated(pool: int, layer: int, rotation: GbRotation, q, k_new, v_new, scale: float, out,
+                                flags: int = GB_PATH_AUTO, stream=None) -> None:
+    _check(pool, load().gb_decode_attention_rotated(pool, layer, ctypes.byref(rotation), ptr(q), ptr(k_new), ptr(v_new), float(scale),
+                                                    ptr(out), flags, stream_handle(stream)), "gb_decode_attention_rotated")
+
+
+def gb_read_kv(pool: int, layer: int, first, n_tokens: int, k_out, v_out, stream=None) -> None:
+    _check(pool, load().gb_read_kv(pool, layer, ptr(first), n_tokens, ptr(k_out), ptr(v_out), stream_handle(stream)), "gb_read_kv")
 
 
 def gb_score_probe(pool: int, hidden, hidden_dtype: int, hidden_dim: int, w, bias: float, mask=None,

@@ -20,6 +20,7 @@
 #include <type_traits>
 
 #include "flash.cuh"
+#include "rows.cuh"
 #include "tile.cuh"
 #include "worklist.cuh"
 
@@ -1202,27 +1203,41 @@ __global__ void __launch_bounds__(1024) k_truncate(PoolView v, const int* length
   }
 }
 
-// The rows of the pages that k_truncate replaced: a CTA per (layer, job).
+// The rows of the pages that k_truncate (in 8 bits also k_step_begin) replaced, and in 8 bits their blocks' exponents: a CTA per (layer, job).
 __global__ void __launch_bounds__(256) k_cow_rows(PoolView v) {
   pdl_wait();
   pdl_launch_dependents();
   const int jobs = v.ctl[kCtlCowJobs], layer = blockIdx.y;
   for (int j = blockIdx.x; j < jobs; j += gridDim.x) {
     const int old = v.cow[3 * j], page = v.cow[3 * j + 1], have = v.cow[3 * j + 2];
-    for (int i = threadIdx.x; i < 2 * v.Hkv * have * 16; i += 256) {
-      const int c = i & 15, row = (i >> 4) % have, kvh = (i >> 4) / have;
+    const int bits = v.dtype == GB_FP8 ? 3 : 4;  // 16-byte pieces of a row, as a power of two
+    if (v.dtype == GB_FP8) {
+      const int blks = (have + kBlockRows - 1) / kBlockRows;
+      for (int i = threadIdx.x; i < 2 * v.Hkv * blks; i += 256) {
+        const int row = i % blks * kBlockRows, kvh = i / blks;
+        v.kv_exp[exp_offset(v, layer, page, kvh / v.Hkv, kvh % v.Hkv, row)] =
+            v.kv_exp[exp_offset(v, layer, old, kvh / v.Hkv, kvh % v.Hkv, row)];
+      }
+    }
+    for (int i = threadIdx.x; i < (2 * v.Hkv * have) << bits; i += 256) {
+      const int c = i & ((1 << bits) - 1), row = (i >> bits) % have, kvh = (i >> bits) / have;
       reinterpret_cast<uint4*>(v.kv + kv_elem_offset(v, layer, page, kvh / v.Hkv, kvh % v.Hkv, row) * v.esize)[c] =
           reinterpret_cast<const uint4*>(v.kv + kv_elem_offset(v, layer, old, kvh / v.Hkv, kvh % v.Hkv, row) * v.esize)[c];
     }
   }
 }
 
-bool on_device(const gb_pool* pool) {
-  int d = -1;
-  return cudaGetDevice(&d) == cudaSuccess && d == pool->device;
+}  // namespace
+
+void launch_cow_rows(gb_pool* pool, cudaStream_t s) {
+  launch_pdl(k_cow_rows, dim3(std::min(pool->cfg.max_beams, 64), pool->cfg.num_layers), 256, 0, s, pool->view);
+  pool->launches += 1;
 }
 
+namespace {
+
 gb_status check_draft(gb_pool* pool, const gb_draft* d, const char* what) {
+  if (pool->cfg.kv_dtype == GB_FP8) return fail(pool, GB_ERR_UNSUPPORTED, "draft: pools of 8 bits have no drafts");
   if (!d || d->n_draft < 1 || d->n_draft > kMaxDraft || !d->parent_dev || !d->workspace_dev ||
       ((uintptr_t)d->workspace_dev & 255))
     return fail(pool, GB_ERR_INVALID, what);
@@ -1266,6 +1281,7 @@ using namespace gb;
 extern "C" gb_status gb_draft_workspace_bytes(gb_pool* pool, int n_draft, size_t* bytes) {
   if (!pool || !bytes) return GB_ERR_INVALID;
   if (n_draft < 1 || n_draft > kMaxDraft) return fail(pool, GB_ERR_INVALID, "draft: 1 to 64 tokens");
+  if (pool->cfg.kv_dtype == GB_FP8) return fail(pool, GB_ERR_UNSUPPORTED, "draft: pools of 8 bits have no drafts");
   *bytes = draft_layout(pool->cfg, pool->num_sms, n_draft).total;
   return GB_OK;
 }
@@ -1399,8 +1415,8 @@ extern "C" gb_status gb_truncate(gb_pool* pool, const int32_t* lengths_dev, gb_s
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   ++pool->epoch;
   launch_pdl(k_truncate, 1, 1024, 0, s, pool->view, lengths_dev);
-  launch_pdl(k_cow_rows, dim3(std::min(pool->cfg.max_beams, 64), pool->cfg.num_layers), 256, 0, s, pool->view);
-  pool->launches += 2;
+  pool->launches += 1;
+  launch_cow_rows(pool, s);
   const gb_status st = check_launch(pool, "truncate");
   if (st != GB_OK) return st;
   if (rebuild_segments(pool, s, pool->view.ctl + kCtlSegStale) != cudaSuccess) return check_launch(pool, "segments");

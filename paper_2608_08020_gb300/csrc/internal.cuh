@@ -83,6 +83,7 @@ struct MetaLayout {
   int words;            // free-bitmap words
   size_t mlp_scratch;   // MLP scorer partial sums
   int partial_records;  // split-KV partial records
+  size_t rotated;       // in the scratch above: a step's turned keys, then its turned queries
   int record_floats;    // floats per partial record: G*(D+2)
 };
 
@@ -93,6 +94,7 @@ struct PoolView {
   int layers, Hq, Hkv, D, P, G, dtype, esize, max_beams, max_pages, words;
   long long num_pages;
   char* kv;             // KV pool base
+  signed char* kv_exp;  // 8-bit pools: the blocks' exponents, [layer][page][K|V][kv_head][P / 16] (rows.cuh)
   long long page_elems; // elements of one (layer, page): 2*Hkv*P*D
   int* ctl;
   int* tables;          // [max_beams][max_pages]
@@ -384,12 +386,23 @@ inline void prof_end(gb_pool* p, int which, cudaStream_t s) {
   if (p->prof_stop[which]) prof_record(p->prof_stop[which], s);
 }
 gb_status check_launch(gb_pool* pool, const char* what);
+bool on_device(const gb_pool* pool);  // whether the pool's device is the current one
 // Raise a kernel's dynamic shared memory limit to `bytes` on the current device.  The
 // attribute belongs to the device, so it is set once per (kernel, device), under a lock.
 cudaError_t set_max_dynamic_smem(const void* kernel, int bytes);
 
 
+struct RotationView;
 // Kernel launchers implemented in the other translation units.
+cudaError_t launch_append_rows(gb_pool* pool, int layer, int n_tokens, const RotationView& rot, const void* k, const void* v,
+                               const void* q, void* qout, cudaStream_t s);
+cudaError_t launch_turn(gb_pool* pool, const RotationView& rot, const void* q, void* qout, const void* k, void* kout,
+                        cudaStream_t s);
+void launch_cow_rows(gb_pool* pool, cudaStream_t s);  // every layer's rows of the pages that were copied on write
+cudaError_t launch_seed_rows8(gb_pool* pool, int prompt_len, const void* k, const void* v, cudaStream_t s);
+// The attention of a layer-step of an 8-bit pool, whose new rows are in the cache already.
+cudaError_t launch_decode8(gb_pool* pool, int layer, const void* q, float scale, float* out, int mode, cudaStream_t s);
+bool make_tensor_map8(gb_pool* pool);
 // The attention of one layer-step on s, written to out: mode 0, the per-beam kernel; mode 1,
 // the attention kernel with the grouped and per-beam roles (launch_attention).  Every kernel
 // merges its records itself.

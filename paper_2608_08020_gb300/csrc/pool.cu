@@ -14,6 +14,7 @@
 #include <vector>
 
 #include "internal.cuh"
+#include "rows.cuh"
 #include "step_form.cuh"
 
 namespace gb {
@@ -22,7 +23,7 @@ static size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
 // One layer-step's new K (or V) rows.
 static size_t new_rows_bytes(const gb_pool_config& c) {
-  return (size_t)c.max_beams * c.num_kv_heads * c.head_dim * (c.kv_dtype == GB_BF16 ? 2 : 4);
+  return (size_t)c.max_beams * c.num_kv_heads * c.head_dim * (c.kv_dtype == GB_F32 ? 4 : 2);
 }
 
 MetaLayout meta_layout(const gb_pool_config& c) {
@@ -45,7 +46,7 @@ MetaLayout meta_layout(const gb_pool_config& c) {
   m.plan = take(2 * 3 * (B + 1) * sizeof(int));
   m.cow = take(kMaxCowJobs * 3 * sizeof(int));
   m.cow_old = take(B * sizeof(int));
-  m.record_floats = G * (c.head_dim + 2);
+  m.record_floats = (G * (c.head_dim + 2) + 3) / 4 * 4;  // records are read and written in pieces of 16 bytes
   m.partial_records = kMaxDecodeWarps + (int)B * c.num_kv_heads;  // record index: warp + b * Hkv + h
   m.partials = take((size_t)m.partial_records * m.record_floats * sizeof(float));
   const size_t BD = B * kMaxSegDepth;
@@ -70,15 +71,18 @@ MetaLayout meta_layout(const gb_pool_config& c) {
   m.seg_hist = take(2 * 256 * sizeof(int));
   m.pair_cnt = take(2 * B * c.num_kv_heads * sizeof(int));
   m.stats = take((size_t)kStatsRing * kStatsWords * sizeof(int));
-  // Also holds a step's new K and V rows where the caller's output overlaps them.
-  m.mlp_scratch = take(std::max((size_t)kMlpScratchFloats * sizeof(float), 2 * new_rows_bytes(c)));
+  // Also holds a step's new K and V rows where the caller's output overlaps them, and its turned keys and queries.
+  m.rotated = 2 * align256(new_rows_bytes(c));
+  m.mlp_scratch = take(std::max((size_t)kMlpScratchFloats * sizeof(float),
+                                m.rotated + align256(new_rows_bytes(c)) + G * new_rows_bytes(c)));
   m.total = o;
   return m;
 }
 
 bool decode_supported(int dtype, int D, int G) {
+  if (dtype == GB_FP8 && G == 1) return D == 128;
   if (!(G == 2 || G == 4 || G == 8)) return false;
-  if (dtype == GB_BF16) return D == 128;
+  if (dtype == GB_BF16 || dtype == GB_FP8) return D == 128;
   if (dtype == GB_F32) return D == 64;
   return false;
 }
@@ -99,6 +103,11 @@ cudaError_t set_max_dynamic_smem(const void* kernel, int bytes) {
   e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
   if (e == cudaSuccess) done.insert(std::make_tuple(kernel, device, bytes));
   return e;
+}
+
+bool on_device(const gb_pool* pool) {
+  int d = -1;
+  return cudaGetDevice(&d) == cudaSuccess && d == pool->device;
 }
 
 gb_status check_launch(gb_pool* pool, const char* what) {
@@ -608,16 +617,23 @@ static gb_status validate(const gb_pool_config* c) {
       c->max_pages_per_beam < 1 || c->group_min_beams < 0)
     return GB_ERR_INVALID;
   if (!(c->page_size == 16 || c->page_size == 32 || c->page_size == 64)) return GB_ERR_INVALID;
-  if (c->kv_dtype != GB_F32 && c->kv_dtype != GB_BF16) return GB_ERR_INVALID;
+  if (c->kv_dtype != GB_F32 && c->kv_dtype != GB_BF16 && c->kv_dtype != GB_FP8) return GB_ERR_INVALID;
   if (!decode_supported(c->kv_dtype, c->head_dim, c->num_q_heads / c->num_kv_heads))
     return GB_ERR_UNSUPPORTED;
   return GB_OK;
 }
 
+static int elem_size(int dtype) { return dtype == GB_F32 ? 4 : dtype == GB_BF16 ? 2 : 1; }
+
+// The cached values (8-bit pools: rounded up to 256 bytes, the blocks' exponents follow).
+static size_t kv_values_of(const gb_pool_config* c) {
+  return (size_t)c->num_layers * (size_t)c->num_pages * 2 * c->num_kv_heads * c->page_size * c->head_dim *
+         elem_size(c->kv_dtype);
+}
+
 static size_t kv_bytes_of(const gb_pool_config* c) {
-  const size_t es = c->kv_dtype == GB_BF16 ? 2 : 4;
-  return (size_t)c->num_layers * (size_t)c->num_pages * 2 * c->num_kv_heads * c->page_size *
-         c->head_dim * es;
+  const size_t n = kv_values_of(c);
+  return c->kv_dtype == GB_FP8 ? align256(n) + n / ((size_t)c->head_dim * kBlockRows) : n;
 }
 
 extern "C" gb_status gb_pool_workspace_bytes(const gb_pool_config* cfg, size_t* kv_bytes,
@@ -658,12 +674,13 @@ extern "C" gb_status gb_pool_init(const gb_pool_config* cfg, void* kv_dev, void*
   v.P = cfg->page_size;
   v.G = v.Hq / v.Hkv;
   v.dtype = cfg->kv_dtype;
-  v.esize = cfg->kv_dtype == GB_BF16 ? 2 : 4;
+  v.esize = elem_size(cfg->kv_dtype);
   v.max_beams = cfg->max_beams;
   v.max_pages = cfg->max_pages_per_beam;
   v.words = p->layout.words;
   v.num_pages = cfg->num_pages;
   v.kv = static_cast<char*>(kv_dev);
+  v.kv_exp = cfg->kv_dtype == GB_FP8 ? reinterpret_cast<signed char*>(v.kv + align256(kv_values_of(cfg))) : nullptr;
   v.page_elems = 2LL * v.Hkv * v.P * v.D;
   char* m = static_cast<char*>(meta_dev);
   const MetaLayout& L = p->layout;
@@ -713,6 +730,10 @@ extern "C" gb_status gb_pool_init(const gb_pool_config* cfg, void* kv_dev, void*
                   ? 1
                   : 0;
   make_kv_tensor_maps(p);
+  if (cfg->kv_dtype == GB_FP8 && !make_tensor_map8(p)) {
+    delete p;
+    return GB_ERR_UNSUPPORTED;
+  }
   // The grouped path runs as a role of the attention kernel beside the per-beam role, so it
   // needs both tensor maps.
   if (v.grouped && !(p->have_tmap && p->have_dtmap && p->num_sms * kMmaWarps <= kMaxDecodeWarps)) v.grouped = 0;
@@ -759,9 +780,12 @@ extern "C" gb_status gb_pool_seed(gb_pool* pool, int n_beams, int prompt_len, co
   const long long vecs = 2LL * pool->cfg.num_layers * prompt_len * pool->cfg.num_kv_heads *
                          (pool->view.D * pool->view.esize / 16);
   const int grid = (int)std::min<long long>((vecs + 255) / 256, pool->num_sms * 8LL);
-  k_seed_write<<<std::max(grid, 1), 256, 0, s>>>(pool->view, prompt_len,
-                                                 static_cast<const char*>(k_prompt_dev),
-                                                 static_cast<const char*>(v_prompt_dev));
+  if (pool->cfg.kv_dtype == GB_FP8)
+    launch_seed_rows8(pool, prompt_len, k_prompt_dev, v_prompt_dev, s);
+  else
+    k_seed_write<<<std::max(grid, 1), 256, 0, s>>>(pool->view, prompt_len,
+                                                   static_cast<const char*>(k_prompt_dev),
+                                                   static_cast<const char*>(v_prompt_dev));
   st = check_launch(pool, "seed_write");
   if (st != GB_OK) return st;
   pool->seeded = true;
@@ -769,10 +793,11 @@ extern "C" gb_status gb_pool_seed(gb_pool* pool, int n_beams, int prompt_len, co
   return GB_OK;
 }
 
-// Shared by gb_decode_attention and gb_append_kv: open the step at layer 0 and write the new
+// Shared by the decode and append calls: open the step at layer 0 and write the new
 // rows of `layer`, unless the attention launch that follows writes them itself (`fused`).
+// rot: turn the keys on the way, and with q also the queries, to qout.
 static gb_status append_layer(gb_pool* pool, int layer, int n_tokens, const void* k, const void* v, bool fused,
-                              cudaStream_t s) {
+                              const RotationView& rot, const void* q, void* qout, cudaStream_t s) {
   if (!pool->seeded) return fail(pool, GB_ERR_STATE, "pool not seeded");
   if (layer < 0 || layer >= pool->cfg.num_layers || n_tokens < 1 || !k || !v)
     return fail(pool, GB_ERR_INVALID, "append: bad arguments");
@@ -788,13 +813,16 @@ static gb_status append_layer(gb_pool* pool, int layer, int n_tokens, const void
     gb_status st = check_launch(pool, "step_begin");
     if (st != GB_OK) return st;
     pool->step_tokens = n_tokens;
+    if (pool->cfg.kv_dtype == GB_FP8) launch_cow_rows(pool, s);
   } else if (n_tokens != pool->step_tokens) {
     return fail(pool, GB_ERR_STATE, "token count differs from the one layer 0 reserved");
   }
   const int runs = (n_tokens + pool->cfg.page_size - 1) / pool->cfg.page_size + 1;  // pages a beam's new tokens meet
   const dim3 grid(pool->cfg.max_beams, std::min(2 * runs, 65535));
   prof_begin(pool, GB_PROF_APPEND, s);  // an empty interval when the attention launch appends
-  if (!fused) {
+  if (!fused && (rot.table || pool->cfg.kv_dtype == GB_FP8)) {
+    launch_append_rows(pool, layer, n_tokens, rot, k, v, q, qout, s);
+  } else if (!fused) {
     launch_pdl(k_append, grid, 256, 0, s, pool->view, layer, n_tokens, static_cast<const char*>(k),
                static_cast<const char*>(v));
     pool->launches += 1;
@@ -809,7 +837,28 @@ static gb_status append_layer(gb_pool* pool, int layer, int n_tokens, const void
 extern "C" gb_status gb_append_kv(gb_pool* pool, int layer, int n_tokens, const void* k_dev,
                                   const void* v_dev, gb_stream_t stream) {
   if (!pool) return GB_ERR_INVALID;
-  return append_layer(pool, layer, n_tokens, k_dev, v_dev, false, reinterpret_cast<cudaStream_t>(stream));
+  return append_layer(pool, layer, n_tokens, k_dev, v_dev, false, RotationView{}, nullptr, nullptr,
+                      reinterpret_cast<cudaStream_t>(stream));
+}
+
+// A caller's rotation as the kernels take it.
+static gb_status rotation_view(gb_pool* pool, const gb_rotation* r, RotationView* out) {
+  if (!r || !r->table_dev || ((uintptr_t)r->table_dev & 15) || r->positions < 1 || r->rotary_dim < 16 || r->rotary_dim % 16 != 0 ||
+      r->rotary_dim > pool->cfg.head_dim || (r->interleaved != 0 && r->interleaved != 1))
+    return fail(pool, GB_ERR_INVALID, "rotation: bad arguments");
+  if (!on_device(pool)) return fail(pool, GB_ERR_STATE, "rotation: the pool is on another device than the current one");
+  *out = {reinterpret_cast<const float4*>(r->table_dev), r->positions, r->rotary_dim / 2, r->interleaved};
+  return GB_OK;
+}
+
+extern "C" gb_status gb_append_kv_rotated(gb_pool* pool, int layer, int n_tokens, const gb_rotation* rotation,
+                                          const void* k_dev, const void* v_dev, gb_stream_t stream) {
+  if (!pool) return GB_ERR_INVALID;
+  RotationView rot;
+  const gb_status st = rotation_view(pool, rotation, &rot);
+  if (st != GB_OK) return st;
+  if (((uintptr_t)k_dev | (uintptr_t)v_dev) & 15) return fail(pool, GB_ERR_INVALID, "append: rows start on 16 bytes");
+  return append_layer(pool, layer, n_tokens, k_dev, v_dev, false, rot, nullptr, nullptr, reinterpret_cast<cudaStream_t>(stream));
 }
 
 static bool overlap(const void* a, size_t an, const void* b, size_t bn) {
@@ -817,15 +866,35 @@ static bool overlap(const void* a, size_t an, const void* b, size_t bn) {
   return x < y + bn && y < x + an;
 }
 
-extern "C" gb_status gb_decode_attention(gb_pool* pool, int layer, const void* q_dev,
-                                         const void* k_new_dev, const void* v_new_dev, float scale,
-                                         float* out_dev, int flags, gb_stream_t stream) {
-  if (!pool) return GB_ERR_INVALID;
+static gb_status decode_layer(gb_pool* pool, int layer, const RotationView& rot, const void* q_dev,
+                              const void* k_new_dev, const void* v_new_dev, float scale, float* out_dev, int flags,
+                              cudaStream_t s) {
   if (!q_dev || !out_dev) return fail(pool, GB_ERR_INVALID, "decode: null pointer");
   if (flags < GB_PATH_AUTO || flags > GB_PATH_GROUPED) return fail(pool, GB_ERR_INVALID, "decode: bad flags");
-  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  gb_status st = append_layer(pool, layer, 1, k_new_dev, v_new_dev, true, s);
+  char* turned = reinterpret_cast<char*>(pool->view.mlp_scratch) + pool->layout.rotated;  // keys, then queries
+  char* turned_q = turned + align256(new_rows_bytes(pool->cfg));
+  if (pool->cfg.kv_dtype == GB_FP8) {
+    // The new rows go to the cache in a launch of their own, which turns the queries too: a row may change its whole
+    // block's exponent, so the attention launch would have had to write what it reads.
+    if (((uintptr_t)q_dev | (uintptr_t)k_new_dev | (uintptr_t)v_new_dev) & 15)
+      return fail(pool, GB_ERR_INVALID, "decode: rows start on 16 bytes");
+    const gb_status st = append_layer(pool, layer, 1, k_new_dev, v_new_dev, false, rot, rot.table ? q_dev : nullptr, turned_q, s);
+    if (st != GB_OK) return st;
+    if (rot.table) q_dev = turned_q;
+    prof_begin(pool, GB_PROF_ATTENTION, s);
+    launch_decode8(pool, layer, q_dev, scale, out_dev, flags == GB_PATH_PER_BEAM || !pool->view.grouped ? 0 : 1, s);
+    prof_end(pool, GB_PROF_ATTENTION, s);
+    return check_launch(pool, "decode");
+  }
+  if (rot.table && (((uintptr_t)q_dev | (uintptr_t)k_new_dev | (uintptr_t)v_new_dev) & 15))
+    return fail(pool, GB_ERR_INVALID, "decode: rows start on 16 bytes");
+  gb_status st = append_layer(pool, layer, 1, k_new_dev, v_new_dev, true, RotationView{}, nullptr, nullptr, s);
   if (st != GB_OK) return st;
+  if (rot.table) {
+    launch_turn(pool, rot, q_dev, turned_q, k_new_dev, turned, s);
+    q_dev = turned_q;
+    k_new_dev = turned;
+  }
   // The launch writes a pair's output while other pairs' new rows are still to be read.
   const size_t rows = new_rows_bytes(pool->cfg);
   const size_t outb = (size_t)pool->cfg.max_beams * pool->cfg.num_q_heads * pool->cfg.head_dim * sizeof(float);
@@ -847,6 +916,24 @@ extern "C" gb_status gb_decode_attention(gb_pool* pool, int layer, const void* q
       cudaSuccess)
     return check_launch(pool, "decode");
   return check_launch(pool, "decode");
+}
+
+extern "C" gb_status gb_decode_attention(gb_pool* pool, int layer, const void* q_dev,
+                                         const void* k_new_dev, const void* v_new_dev, float scale,
+                                         float* out_dev, int flags, gb_stream_t stream) {
+  if (!pool) return GB_ERR_INVALID;
+  return decode_layer(pool, layer, RotationView{}, q_dev, k_new_dev, v_new_dev, scale, out_dev, flags,
+                      reinterpret_cast<cudaStream_t>(stream));
+}
+
+extern "C" gb_status gb_decode_attention_rotated(gb_pool* pool, int layer, const gb_rotation* rotation, const void* q_dev,
+                                                 const void* k_new_dev, const void* v_new_dev, float scale, float* out_dev,
+                                                 int flags, gb_stream_t stream) {
+  if (!pool) return GB_ERR_INVALID;
+  RotationView rot;
+  const gb_status st = rotation_view(pool, rotation, &rot);
+  if (st != GB_OK) return st;
+  return decode_layer(pool, layer, rot, q_dev, k_new_dev, v_new_dev, scale, out_dev, flags, reinterpret_cast<cudaStream_t>(stream));
 }
 
 extern "C" gb_status gb_release(gb_pool* pool, const int32_t* slots_dev, int n, gb_stream_t stream) {

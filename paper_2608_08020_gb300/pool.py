@@ -10,8 +10,8 @@ import torch
 
 from paper_2608_08020_gb300 import binding as B
 
-_DT = {"f32": B.GB_F32, "bf16": B.GB_BF16}
-TORCH_DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+_DT = {"f32": B.GB_F32, "bf16": B.GB_BF16, "fp8": B.GB_FP8}
+TORCH_DT = {"f32": torch.float32, "bf16": torch.bfloat16, "fp8": torch.bfloat16}   # of the rows that a caller gives
 
 
 class BeamPool:
@@ -54,11 +54,37 @@ class BeamPool:
     def seed(self, n_beams, prompt_len, k_prompt, v_prompt, stream=None):
         B.gb_pool_seed(self.handle, n_beams, prompt_len, k_prompt, v_prompt, stream)
 
-    def decode_attention(self, layer, q, k_new, v_new, scale, out, flags=B.GB_PATH_AUTO, stream=None):
-        B.gb_decode_attention(self.handle, layer, q, k_new, v_new, scale, out, flags, stream)
+    def decode_attention(self, layer, q, k_new, v_new, scale, out, flags=B.GB_PATH_AUTO, stream=None, rotation=None):
+        """`rotation`: a Rotation; q and k_new are then given as the projection leaves them."""
+        if rotation is None:
+            B.gb_decode_attention(self.handle, layer, q, k_new, v_new, scale, out, flags, stream)
+        else:
+            B.gb_decode_attention_rotated(self.handle, layer, self._rotation(rotation), q, k_new, v_new, scale, out, flags, stream)
 
-    def append_kv(self, layer, n_tokens, k, v, stream=None):
-        B.gb_append_kv(self.handle, layer, n_tokens, k, v, stream)
+    def append_kv(self, layer, n_tokens, k, v, stream=None, rotation=None):
+        """`rotation`: a Rotation; k is then given as the projection leaves it."""
+        if rotation is None:
+            B.gb_append_kv(self.handle, layer, n_tokens, k, v, stream)
+        else:
+            B.gb_append_kv_rotated(self.handle, layer, n_tokens, self._rotation(rotation), k, v, stream)
+
+    def read_kv(self, layer, first, n_tokens, stream=None):
+        """(keys, values) of tokens first[slot] .. first[slot] + n_tokens - 1 (first int32 [max_beams]) as the cache holds
+        them, each [n_tokens][max_beams][kv heads][head_dim]; zeros where a slot has no such token.  They belong to `stream`,
+        which has to be a torch.cuda.Stream or None."""
+        c = self.cfg
+        make = lambda: torch.empty(2, n_tokens, self.max_beams, c.num_kv_heads, c.head_dim, dtype=TORCH_DT[self.kv_dtype],  # noqa: E731
+                                   device=self.device)
+        first = self._slots("first", first)
+        k, v = make() if stream is None else B.new_on(stream, make)
+        B.gb_read_kv(self.handle, layer, first, n_tokens, k, v, stream)
+        return k, v
+
+    def _rotation(self, r):
+        if r.head_dim != self.cfg.head_dim or r.table.device != self.kv.device:
+            raise ValueError(f"rotation: of heads of {r.head_dim} on {r.table.device}, the pool's are of {self.cfg.head_dim} "
+                             f"on {self.kv.device}")
+        return r.args
 
     def score_probe(self, hidden, hidden_dtype: str, w, bias=0.0, mask=None, score_out=None, stream=None):
         B.gb_score_probe(self.handle, hidden, _DT[hidden_dtype], hidden.shape[-1], w, bias, mask, score_out, stream)
