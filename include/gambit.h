@@ -687,6 +687,46 @@ gb_status gb_accept_draft(gb_pool* pool, const gb_draft* draft, const void* k_de
  */
 gb_status gb_truncate(gb_pool* pool, const int32_t* lengths_dev, gb_stream_t stream);
 
+/*
+ * The next token of each row of logits, from a given random number (Algorithm 1, "Generate": every trace draws its own).
+ * With w_i = exp((x_i - max x) / temperature), tokens in descending order of x, equal ones by ascending index: top_k keeps the
+ * first top_k; min_p of these the ones with w_i >= min_p (so many times the likeliest one's probability); top_p of these the
+ * shortest head whose mass reaches top_p of theirs, one token at least.  The token is the first, by index, at which the
+ * cumulative mass of what is kept passes u times its total.
+ *   logits:      [rows] rows of vocab values in dtype (GB_F32, GB_BF16), row_stride elements apart; -infinity bans a token,
+ *                NaN counts as -infinity; where a row has +infinity its tokens share all of the mass
+ *   u:           fp32 [rows], in [0, 1); clamped to that (NaN: 0)
+ *   temperature: fp32 [rows], or NULL for all_temperature; not above 0 (or NaN): the likeliest token, the lowest index of equals
+ *   top_k:       int32 [rows], or NULL for all_top_k; below 1 or from vocab on: off
+ *   top_p, min_p: fp32 [rows], or NULL for all_top_p, all_min_p; top_p from 1 on (or NaN) and min_p up to 0 (or NaN): off;
+ *                min_p above 1 counts as 1
+ *   token:       int32 [rows]; -1 for a row that has only -infinity
+ *   logprob:     fp32 [rows] natural logarithm of the token's share of what is kept (-infinity with token -1), or NULL
+ * Masses are summed exactly (weights to 2^-33 of themselves), so a row's token does not depend on the other rows or the number of
+ * SMs.  Outputs must not overlap inputs.  No workspace; one launch, none without rows.
+ * Errors: GB_ERR_INVALID for bad sizes, pointers or alignment (each value's own), GB_ERR_UNSUPPORTED for a vocab above 524,288,
+ * GB_ERR_TOO_LARGE for more rows than a grid takes.
+ */
+typedef struct {
+  const void* logits;
+  int64_t row_stride;
+  const float* u;
+  const float* temperature;
+  const int32_t* top_k;
+  const float* top_p;
+  const float* min_p;
+  int32_t* token;
+  float* logprob;
+  int rows;
+  int vocab;
+  int dtype;
+  float all_temperature;
+  int all_top_k;
+  float all_top_p;
+  float all_min_p;
+} gb_sample_args;
+gb_status gb_sample(const gb_sample_args* args, gb_stream_t stream);
+
 /* Short description of the pool's last host-side failure ("" if none); static storage. */
 const char* gb_last_error(gb_pool* pool);
 

@@ -30,7 +30,7 @@ EXPORTS = ["gb_pool_workspace_bytes", "gb_pool_init", "gb_pool_destroy", "gb_poo
            "gb_pool_clear_status", "gb_pool_wait_selftest", "gb_pool_read_state", "gb_pool_set_profile_events", "gb_pool_launch_count",
            "gb_paged_decode_noalloc", "gb_paged_decode_noalloc_status", "gb_pool_read_step_stats", "gb_pool_set_capacity", "gb_pool_last_ranked", "gb_score_mlp", "gb_fork_slots", "gb_scorer_sizes", "gb_scorer_seed",
            "gb_scorer_step", "gb_prompt_workspace_bytes", "gb_prompt_attention", "gb_prompt_status", "gb_prompt_wait_selftest",
-           "gb_draft_workspace_bytes", "gb_draft_attention", "gb_accept_draft", "gb_truncate", "gb_last_error"]
+           "gb_draft_workspace_bytes", "gb_draft_attention", "gb_accept_draft", "gb_truncate", "gb_sample", "gb_last_error"]
 GB_PROF_DECODE, GB_PROF_PROBE, GB_PROF_PRUNE, GB_PROF_GROUPED = 0, 1, 2, 3
 GB_PROF_PLAN, GB_PROF_APPEND, GB_PROF_COMBINE, GB_PROF_ATTENTION = 4, 5, 6, 7
 
@@ -74,6 +74,14 @@ class GbDraft(ctypes.Structure):
 class GbRotation(ctypes.Structure):
     _fields_ = [("table_dev", ctypes.c_void_p), ("positions", ctypes.c_int), ("rotary_dim", ctypes.c_int),
                 ("interleaved", ctypes.c_int)]
+
+
+class GbSampleArgs(ctypes.Structure):
+    _fields_ = [("logits", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("u", ctypes.c_void_p), ("temperature", ctypes.c_void_p),
+                ("top_k", ctypes.c_void_p), ("top_p", ctypes.c_void_p), ("min_p", ctypes.c_void_p), ("token", ctypes.c_void_p),
+                ("logprob", ctypes.c_void_p), ("rows", ctypes.c_int), ("vocab", ctypes.c_int), ("dtype", ctypes.c_int),
+                ("all_temperature", ctypes.c_float), ("all_top_k", ctypes.c_int), ("all_top_p", ctypes.c_float),
+                ("all_min_p", ctypes.c_float)]
 
 
 class GambitError(RuntimeError):
@@ -133,6 +141,7 @@ def load(path: Path | None = None) -> ctypes.CDLL:
         "gb_draft_attention": [V, I, P, V, V, V, F, V, V],
         "gb_accept_draft": [V, P, V, V, V, V, V, V],
         "gb_truncate": [V, V, V],
+        "gb_sample": [P, V],
         "gb_last_error": [V],
     }
     for name, args in sig.items():
@@ -433,6 +442,13 @@ def gb_accept_draft(pool: int, draft: GbDraft, k, v, accepted, count_out=None, p
 
 def gb_truncate(pool: int, lengths, stream=None) -> None:
     _check(pool, load().gb_truncate(pool, ptr(lengths), stream_handle(stream)), "gb_truncate")
+
+
+def gb_sample(args: GbSampleArgs, stream=None, device: int | None = None) -> None:
+    """`device`: refuse when it is not the current one."""
+    code = load().gb_sample(ctypes.byref(args), stream_handle(stream) if device is None else stream_on(device, stream))
+    if code:
+        _check(None, code, "gb_sample")
 
 
 def gb_last_error(pool: int) -> str:
