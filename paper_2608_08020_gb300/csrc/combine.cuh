@@ -176,23 +176,16 @@ __device__ __forceinline__ void zero_all_pairs(const PoolView& v, int cta, int n
     zero_pair<G, D>(v, p / v.Hkv, p % v.Hkv, out);
 }
 
-// The merge phase of an attention launch, run by every warp of the merging CTAs after its own
-// work: `mode` selects the plan (0 per-beam, 1 with segments), W = warps of the per-beam
-// role, ng = CTAs of the grouped role (0 without one), out = [max_beams][Hq][128] fp32.
-// `claim`: the warps take pairs from the counter kCntPairNext as they finish (for CTAs
-// that start at different times) and fold a pair's segment records before they wait for its
-// split-KV records; otherwise merging CTA `cta` of `nctas` takes the pairs
-// p = cta + nctas * (warp + k * warps per CTA) and waits for all of a pair's records at once.
-template <int G>
-__device__ __forceinline__ void combine_pairs(const PoolView& v, const Counters& cnt, int mode, int W, int ng,
-                                              bool claim, int cta, int nctas, float* __restrict__ out) {
+// The same for shares of c chunks of the flat list (c = 0: whole pairs), by the first nw warps of each CTA.  Direct: a pair of a
+// single record has been written.
+template <int G, bool Direct>
+__device__ __forceinline__ void combine_shares(const PoolView& v, const Counters& cnt, int mode, int c, int ng, bool claim,
+                                               int cta, int nctas, int nw, float* __restrict__ out) {
   constexpr int D = 128;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nw = blockDim.x >> 5;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int npairs = v.max_beams * v.Hkv;
   const int* off = plan_off(v, mode);
   const int* nn = plan_n(v, mode);
-  const int Tot = off[v.max_beams];
-  const int c = Tot > 0 ? (Tot + W - 1) / W : 1;  // chunks per per-beam warp
   const size_t rf = (size_t)v.record_floats;
   for (int k = 0;; ++k) {
     int p = cta + nctas * (warp + k * nw);
@@ -206,8 +199,9 @@ __device__ __forceinline__ void combine_pairs(const PoolView& v, const Counters&
     const int n = act ? nn[b] : 0;
     const int nseg = (act && mode == 1 && v.grouped) ? v.seg_nrec[b] : 0;
     const int o0 = off[b] + h * n;
-    const int first = o0 / c;
-    const int npb = n > 0 ? (o0 + n - 1) / c - first + 1 : 0;
+    const int first = c > 0 ? o0 / c : 0;
+    const int npb = n == 0 ? 0 : c > 0 ? (o0 + n - 1) / c - first + 1 : 1;
+    if (Direct && npb == 1 && nseg == 0) continue;
     if (npb + nseg == 0) {
       zero_pair<G>(v, b, h, out);
       continue;
@@ -236,6 +230,20 @@ __device__ __forceinline__ void combine_pairs(const PoolView& v, const Counters&
       zero_pair<G, D>(v, b, h, out);
     }
   }
+}
+
+// The merge phase of an attention launch, run by every warp of the merging CTAs after its own
+// work: `mode` selects the plan (0 per-beam, 1 with segments), W = warps of the per-beam
+// role, ng = CTAs of the grouped role (0 without one), out = [max_beams][Hq][128] fp32.
+// `claim`: the warps take pairs from the counter kCntPairNext as they finish (for CTAs
+// that start at different times) and fold a pair's segment records before they wait for its
+// split-KV records; otherwise merging CTA `cta` of `nctas` takes the pairs
+// p = cta + nctas * (warp + k * warps per CTA) and waits for all of a pair's records at once.
+template <int G>
+__device__ __forceinline__ void combine_pairs(const PoolView& v, const Counters& cnt, int mode, int W, int ng,
+                                              bool claim, int cta, int nctas, float* __restrict__ out) {
+  const int Tot = plan_off(v, mode)[v.max_beams];
+  combine_shares<G, false>(v, cnt, mode, Tot > 0 ? (Tot + W - 1) / W : 1, ng, claim, cta, nctas, blockDim.x >> 5, out);
 }
 
 // Merge w records in shared memory, `stride` floats apart, into ob[g][:]: out = sum o 2^(m - M) /

@@ -2,8 +2,8 @@
 //
 //   out[b][h] = sum_t softmax_t(scale q . k_t) v_t,   k_t = 2^(e_K) c_t,  v_t = 2^(e_V) d_t
 // with one e_K and one e_V for each chunk of 16 tokens of a head (rows.cuh).  A chunk is 4 KiB, K and V, brought by one
-// TMA into a warp's ring of stages; its codes become pairs of fp16 in registers (exact) on their way into m16n8k16
-// products, the G query heads of the KV head being the N = 8 columns:
+// TMA into a CTA's ring; its codes become pairs of fp16 in registers (exact) on their way into m16n8k16 products, 8 query
+// rows being the N = 8 columns of a tile:
 //   S^T[16 tokens][8] = C Q'^T,   s = scale' 2^(e_K) S     (Q' = q times a power of two that brings a row below 2^15: exact
 //                                                           for a bf16 row but for values 2^-39 of its largest)
 //   O^T[128][8]      += D^T P^T
@@ -11,27 +11,64 @@
 //   p = 2^(t - m),   O += p d,   L += 2^(-e_V) p
 // so that the largest contribution to O has a weight near one whatever the blocks' scales, and out = O / L.  p enters the
 // products as two fp16 terms (22 bits): one term would be the largest error of the whole by a factor of 100.
-// m is set 7 below the largest t of a chunk, and raised only when a chunk exceeds it by more than 15: p stays under
-// fp16's 2^16, and the last place of a small p (2^-24) is 2^-31 of the largest.
+// m is set 7 below the largest t of a step of 32 tokens, and raised only when one exceeds it by more than 15: p stays under
+// fp16's 2^16, and the last place of a small p (2^-24) is 2^-31 of the largest.  The products' sums are cut off rather than
+// rounded, which adds up over a thousand chunks (to 8e-6 of the output), so each step's are added to O in fp32.
 //
 // Fragments are chosen so that a lane's operands are 16-byte pieces: the dims (the k of S) and the dims of O^T's rows
 // are permuted, which the queries and the output follow.  Lane (r = lane / 4, c = lane % 4) reads dims 32c .. 32c + 31 of
 // tokens r, r + 8 of K, and dims 16r .. 16r + 15 of tokens 2c, 2c + 1, 2c + 8, 2c + 9 of V, whose codes are
-// interleaved in pairs by byte permutes: 8 loads, 64 conversions, 16 permutes, 24 products a chunk.
+// interleaved in pairs by byte permutes: 8 loads, 64 conversions, 16 permutes and 24 products a chunk and tile.
+//
+// Work.  A unit is a run of chunks of one head's pages with the query rows that see them: a beam's own (its G heads), or a
+// shared segment's (up to 128 rows of its members; the lists that the grouped path of bf16 pools uses).  A CTA has a warp that
+// takes units from the launch's counters, two that stream their chunks through a ring, two chunks a stage, and
+// eight warps that share out a unit: row groups of 16 rows, and where those are fewer than eight, groups of stages
+// among the warps of a row group, whose softmax states are merged in shared memory when the unit ends.  Units' records are
+// merged at the end of the launch (combine.cuh); a beam whose whole context was one unit is written at once.
+#include <atomic>
+
 #include "decode_mma.cuh"
 #include "rows.cuh"
 
 namespace gb {
 namespace {
 
-constexpr int kWarps8 = 12;
-constexpr int kStages8 = 4;
-constexpr int kStageBytes8 = 2 * kChunk * 128;
+constexpr int kConsumers8 = 8;                     // warps that multiply
+constexpr int kLoaders8 = 2;                       // and that load: each has every second slot of the ring (one issues 34 GB/s an SM)
+constexpr int kThreads8 = (kConsumers8 + 4) * 32;  // one that plans, the loaders, and one idle (registers are shared out by fours)
+constexpr int kConsumerRegs8 = 216, kLoaderRegs8 = 72;
+static_assert((kConsumers8 * kConsumerRegs8 + 4 * kLoaderRegs8) * 32 <= kThreads8 * 168, "shares of the registers at launch");
+constexpr int kStages8 = 24;                       // 192 KiB on their way an SM: with 128 the unshared 64 x 16384 tokens take 365 us
+// A slot of the ring has the same warps for its stage n and its stage n + kStages8: others could look for the second
+// while the first is still on its way, and a barrier cannot tell a phase from the one before the last.
+static_assert(kStages8 % kConsumers8 == 0 && kStages8 % kLoaders8 == 0, "groups of stages keep their slots");
+constexpr int kChunkBytes8 = 2 * kChunk * 128;     // K and V
+constexpr int kStageBytes8 = 2 * kChunkBytes8;     // two chunks
+constexpr int kSlots8 = 4;                         // units known ahead
+constexpr int kRows8 = 64;                         // query rows of a unit: a tile for each warp
+constexpr int kRowFloats8 = 132;                   // of a row in the merge's memory
+
+enum UnitKind : int { kUnitEnd = 0, kUnitBeam = 1, kUnitSegment = 2 };
+struct Unit8 {
+  int kind, head, tokens, rows;
+  int record;    // beam: the record's index; segment: the split
+  int direct;    // beam: its only record, so its output
+  int source, tok0, again;  // whose table, the first token there, whether others read the pages too
+  int members[kRows8];  // the rows' beams; segment: x kMaxSegDepth + depth
+};
+
 struct Smem8 {
-  static constexpr int STAGES = kWarps8 * kStages8 * kStageBytes8;
-  static constexpr int BARS = kWarps8 * kStages8 * 8;
-  static constexpr int PLAN = 4 * (kMaxBeams + 1) * 4;  // offsets, chunk counts, start tokens, lengths
-  static constexpr int TOTAL = 1024 + STAGES + BARS + PLAN;
+  static constexpr int RING = kStages8 * kStageBytes8;
+  static constexpr int MERGE = RING;                                                  // float [8 warps][4 rows][132]
+  static constexpr int STATE = MERGE + kConsumers8 * 4 * kRowFloats8 * 4;             // float [8 warps][4 rows][m, l]
+  static constexpr int EXPS = STATE + kConsumers8 * 4 * 2 * 4;                        // int [stages][K, V of two chunks]
+  static constexpr int UNITS = EXPS + kStages8 * 16;
+  static constexpr int BARS = UNITS + kSlots8 * (int)sizeof(Unit8);
+  static constexpr int STOP = BARS + (2 * kStages8 + 2 * kSlots8) * 8;                // set when a wait ran out
+  static constexpr int PLAN = STOP + 8;                                               // offsets, chunk counts
+  static constexpr int TOTAL = 1024 + PLAN + 2 * (kMaxBeams + 1) * 4;
+  static_assert(BARS % 8 == 0 && EXPS % 16 == 0, "alignment");
   static_assert(TOTAL <= 232448, "shared memory per block");
 };
 
@@ -55,6 +92,38 @@ __device__ __forceinline__ uint4 ld_shared16(uint32_t addr) {
   return x;
 }
 
+__device__ __forceinline__ void mbar_arrive_n(uint32_t bar, uint32_t n) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(n) : "memory");
+}
+
+// The eight multiplying warps.
+__device__ __forceinline__ void consumers_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kConsumers8 * 32) : "memory"); }
+
+// The same, and whether any thread says so.
+__device__ __forceinline__ bool consumers_any(bool x) {
+  int any;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.s32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, 1, %2, p;\n\tselp.s32 %0, 1, 0, q;\n\t}"
+      : "=r"(any)
+      : "r"((int)x), "n"(kConsumers8 * 32)
+      : "memory");
+  return any != 0;
+}
+
+// A bounded wait that the CTA's other waits end too: the first that runs out stops them all.  The lanes may leave it apart:
+// callers bring them together again before an instruction of the whole warp, or one that takes uniform registers.
+__device__ __forceinline__ bool wait_or_stop(uint32_t bar, uint32_t parity, volatile int* stop) {
+  if (mbar_try_wait(bar, parity)) return true;
+  const uint64_t t0 = globaltimer_ns();
+  for (uint32_t it = 1;; ++it) {
+    if (mbar_try_wait(bar, parity)) return true;
+    if ((it & 63) == 0 && (*stop != 0 || globaltimer_ns() - t0 > kWaitLimitNs)) {
+      *stop = 1;
+      return false;
+    }
+  }
+}
+
 // K and V of one chunk of one head: box {128 bytes, 16 rows, K|V, 1} at row group g.
 __device__ __forceinline__ void tma_chunk8(uint32_t dst, const CUtensorMap* tm, int g, uint32_t bar, uint64_t pol) {
   asm volatile(
@@ -68,7 +137,7 @@ __device__ __forceinline__ void tma_chunk8(uint32_t dst, const CUtensorMap* tm, 
 struct Tile8 {
   uint32_t q[8][2];  // Q'^T: row r, dims 32c + 4j (+1), (+2, +3)
   float s0, s1;      // scale' of columns 2c, 2c + 1 over their rows' powers of two
-  float o[8][4];     // O^T: dims 16r + 2i of columns 2c, 2c + 1, then dims 16r + 2i + 1
+  float2 o[8][2];    // O^T: columns 2c, 2c + 1 of dims 16r + 2i, then 16r + 2i + 1
   float m0, m1, l0, l1;
 };
 
@@ -92,7 +161,7 @@ __device__ __forceinline__ void tile_begin(Tile8& t, const __nv_bfloat16* row, f
   }
   amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
   amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
-  // 2^sh brings the largest value into [2^14, 2^15); in two factors, as sh may pass fp32's exponents.
+  // 2^sh brings the largest value into [2^14, 2^15).
   const int ex = (int)(__float_as_uint(amax) >> 23) - 127, sh = min(max(14 - ex, -113), 126);
   const float up = pow2i(sh);
 #pragma unroll
@@ -102,105 +171,119 @@ __device__ __forceinline__ void tile_begin(Tile8& t, const __nv_bfloat16* row, f
   t.s0 = __shfl_sync(0xffffffffu, back, 8 * c);      // row 2c's first lane
   t.s1 = __shfl_sync(0xffffffffu, back, 8 * c + 4);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) t.o[i][0] = t.o[i][1] = t.o[i][2] = t.o[i][3] = 0.f;
+  for (int i = 0; i < 8; ++i) t.o[i][0] = t.o[i][1] = make_float2(0.f, 0.f);
   t.m0 = t.m1 = -INFINITY;
   t.l0 = t.l1 = 0.f;
 }
 
-// A landed chunk (its first nvalid >= 1 tokens) into NT tiles.  ek, ev: its exponents.
-template <int NT>
-__device__ __forceinline__ void chunk_attend8(Tile8 (&t)[NT], uint32_t sb, int nvalid, int ek, int ev, int r, int c) {
-  uint32_t w[2][8];  // K words: tokens r, r + 8; dims 32c + 4j .. + 3
+// K words of a landed stage's two chunks: tokens r, r + 8; dims 32c + 4j .. + 3.
+__device__ __forceinline__ void take_k(uint32_t (&w)[2][2][8], uint32_t sb, int r, int c) {
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int k = 0; k < 2; ++k)
 #pragma unroll
-    for (int z = 0; z < 2; ++z) {
-      const uint4 x = ld_shared16(sb + (r + 8 * i) * 128 + (((2 * c + z) ^ r) << 4));
-      w[i][4 * z] = x.x;
-      w[i][4 * z + 1] = x.y;
-      w[i][4 * z + 2] = x.z;
-      w[i][4 * z + 3] = x.w;
-    }
-  float s[NT][2][4];
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
-  for (int n = 0; n < NT; ++n)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) s[n][0][e] = s[n][1][e] = 0.f;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const uint32_t a0 = f16x2_of_e4m3x2(w[0][j]), a1 = f16x2_of_e4m3x2(w[1][j]);
-    const uint32_t a2 = f16x2_of_e4m3x2(w[0][j] >> 16), a3 = f16x2_of_e4m3x2(w[1][j] >> 16);
-#pragma unroll
-    for (int n = 0; n < NT; ++n) mma_f16(s[n][j & 1], a0, a1, a2, a3, t[n].q[j][0], t[n].q[j][1]);
-  }
-  uint4 x[4];  // V pieces of tokens 2c, 2c + 1, 2c + 8, 2c + 9
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int tok = 2 * c + (i & 1) + 8 * (i >> 1);
-    x[i] = ld_shared16(sb + kChunk * 128 + tok * 128 + ((r ^ (tok & 7)) << 4));
-    if (nvalid < kChunk && tok >= nvalid) x[i] = make_uint4(0u, 0u, 0u, 0u);  // whatever the page holds there
-  }
-  const float kscale = pow2i(ek), vback = pow2i(-ev), vexp = (float)ev;
-  uint32_t hi[NT][2], lo[NT][2];
-#pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    Tile8& u = t[n];
-    const float k0 = u.s0 * kscale, k1 = u.s1 * kscale;
-    float y[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = fmaf(s[n][0][e] + s[n][1][e], e & 1 ? k1 : k0, vexp);
-    if (nvalid < kChunk) {
-      if (r >= nvalid) y[0] = y[1] = -INFINITY;
-      if (r + 8 >= nvalid) y[2] = y[3] = -INFINITY;
-    }
-    float mx0 = fmaxf(y[0], y[2]), mx1 = fmaxf(y[1], y[3]);
-#pragma unroll
-    for (int o = 4; o < 32; o <<= 1) {
-      mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, o));
-      mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, o));
-    }
-    const bool up0 = mx0 > u.m0 + 15.f, up1 = mx1 > u.m1 + 15.f;
-    if (__any_sync(0xffffffffu, up0 || up1)) {
-      const float n0 = up0 ? mx0 - 7.f : u.m0, n1 = up1 ? mx1 - 7.f : u.m1;
-      const float f0 = up0 ? ex2_approx(u.m0 - n0) : 1.f, f1 = up1 ? ex2_approx(u.m1 - n1) : 1.f;
-      u.m0 = n0;
-      u.m1 = n1;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        u.o[i][0] *= f0;
-        u.o[i][1] *= f1;
-        u.o[i][2] *= f0;
-        u.o[i][3] *= f1;
+      for (int z = 0; z < 2; ++z) {
+        const uint4 x = ld_shared16(sb + k * kChunkBytes8 + (r + 8 * i) * 128 + (((2 * c + z) ^ r) << 4));
+        w[k][i][4 * z] = x.x;
+        w[k][i][4 * z + 1] = x.y;
+        w[k][i][4 * z + 2] = x.z;
+        w[k][i][4 * z + 3] = x.w;
       }
-      u.l0 *= f0;
-      u.l1 *= f1;
+}
+// V pieces: tokens 2c, 2c + 1, 2c + 8, 2c + 9; dims 16r .. + 15.
+__device__ __forceinline__ void take_v(uint4 (&x)[2][4], uint32_t sb, int nvalid, int r, int c) {
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int tok = 2 * c + (i & 1) + 8 * (i >> 1);
+      x[k][i] = ld_shared16(sb + k * kChunkBytes8 + kChunk * 128 + tok * 128 + ((r ^ (tok & 7)) << 4));
+      if (nvalid < 2 * kChunk && 16 * k + tok >= nvalid) x[k][i] = make_uint4(0u, 0u, 0u, 0u);  // whatever is there
     }
-    const float p0 = ex2_approx(y[0] - u.m0), p1 = ex2_approx(y[1] - u.m1);
-    const float p2 = ex2_approx(y[2] - u.m0), p3 = ex2_approx(y[3] - u.m1);
-    u.l0 = fmaf(p0 + p2, vback, u.l0);
-    u.l1 = fmaf(p1 + p3, vback, u.l1);
+}
+
+// A landed stage (its first nvalid >= 1 tokens) into a tile.  e: K's and V's exponent of each chunk.  leave() gives its slot back:
+// the stage is in registers before it is multiplied, which takes a warp a microsecond.
+template <class Leave>
+__device__ __forceinline__ void attend(Tile8& u, uint32_t sb, int nvalid, const int (&e)[2][2], int r, int c, Leave leave) {
+  uint32_t w[2][2][8];
+  uint4 x[2][4];
+  take_k(w, sb, r, c);
+  take_v(x, sb, nvalid, r, c);
+  leave();
+  float y[2][4];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    float s[2][4];  // two independent sums
+#pragma unroll
+    for (int z = 0; z < 4; ++z) s[0][z] = s[1][z] = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      mma_f16(s[j & 1], f16x2_of_e4m3x2(w[k][0][j]), f16x2_of_e4m3x2(w[k][1][j]), f16x2_of_e4m3x2(w[k][0][j] >> 16),
+              f16x2_of_e4m3x2(w[k][1][j] >> 16), u.q[j][0], u.q[j][1]);
+    const float ks = pow2i(e[k][0]), k0 = u.s0 * ks, k1 = u.s1 * ks, add = (float)e[k][1];
+#pragma unroll
+    for (int z = 0; z < 4; ++z) y[k][z] = fmaf(s[0][z] + s[1][z], z & 1 ? k1 : k0, add);
+    if (nvalid < 2 * kChunk) {
+      if (16 * k + r >= nvalid) y[k][0] = y[k][1] = -INFINITY;
+      if (16 * k + r + 8 >= nvalid) y[k][2] = y[k][3] = -INFINITY;
+    }
+  }
+  float mx0 = fmaxf(fmaxf(y[0][0], y[0][2]), fmaxf(y[1][0], y[1][2]));
+  float mx1 = fmaxf(fmaxf(y[0][1], y[0][3]), fmaxf(y[1][1], y[1][3]));
+#pragma unroll
+  for (int o = 4; o < 32; o <<= 1) {
+    mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, o));
+    mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, o));
+  }
+  const bool up0 = mx0 > u.m0 + 15.f, up1 = mx1 > u.m1 + 15.f;
+  if (__any_sync(0xffffffffu, up0 || up1)) {
+    const float n0 = up0 ? mx0 - 7.f : u.m0, n1 = up1 ? mx1 - 7.f : u.m1;
+    const float2 f = make_float2(up0 ? ex2_approx(u.m0 - n0) : 1.f, up1 ? ex2_approx(u.m1 - n1) : 1.f);
+    u.m0 = n0;
+    u.m1 = n1;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      u.o[i][0] = __fmul2_rn(u.o[i][0], f);
+      u.o[i][1] = __fmul2_rn(u.o[i][1], f);
+    }
+    u.l0 *= f.x;
+    u.l1 *= f.y;
+  }
+  uint32_t hi[2][2], lo[2][2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const float p0 = ex2_approx(y[k][0] - u.m0), p1 = ex2_approx(y[k][1] - u.m1);
+    const float p2 = ex2_approx(y[k][2] - u.m0), p3 = ex2_approx(y[k][3] - u.m1);
+    const float back = pow2i(-e[k][1]);
+    u.l0 = fmaf(p0 + p2, back, u.l0);
+    u.l1 = fmaf(p1 + p3, back, u.l1);
     const uint32_t h0 = pack_f16x2(p0, p1), h1 = pack_f16x2(p2, p3);
     const float2 g0 = float2_of_f16x2(h0), g1 = float2_of_f16x2(h1);
-    hi[n][0] = movmatrix_t(h0);
-    hi[n][1] = movmatrix_t(h1);
-    lo[n][0] = movmatrix_t(pack_f16x2(p0 - g0.x, p1 - g0.y));
-    lo[n][1] = movmatrix_t(pack_f16x2(p2 - g1.x, p3 - g1.y));
+    hi[k][0] = movmatrix_t(h0);
+    hi[k][1] = movmatrix_t(h1);
+    lo[k][0] = movmatrix_t(pack_f16x2(p0 - g0.x, p1 - g0.y));
+    lo[k][1] = movmatrix_t(pack_f16x2(p2 - g1.x, p3 - g1.y));
   }
-  const uint32_t* v0 = &x[0].x;
-  const uint32_t* v1 = &x[1].x;
-  const uint32_t* v2 = &x[2].x;
-  const uint32_t* v3 = &x[3].x;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const uint32_t sel = i & 1 ? 0x7362 : 0x5140;
-    const uint32_t a = __byte_perm(v0[i >> 1], v1[i >> 1], sel), b = __byte_perm(v2[i >> 1], v3[i >> 1], sel);
-    const uint32_t a0 = f16x2_of_e4m3x2(a), a1 = f16x2_of_e4m3x2(a >> 16);
-    const uint32_t a2 = f16x2_of_e4m3x2(b), a3 = f16x2_of_e4m3x2(b >> 16);
+    float d[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      mma_f16(t[n].o[i], a0, a1, a2, a3, hi[n][0], hi[n][1]);
-      mma_f16(t[n].o[i], a0, a1, a2, a3, lo[n][0], lo[n][1]);
+    for (int k = 0; k < 2; ++k) {
+      const uint32_t* v0 = &x[k][0].x;
+      const uint32_t* v1 = &x[k][1].x;
+      const uint32_t* v2 = &x[k][2].x;
+      const uint32_t* v3 = &x[k][3].x;
+      const uint32_t sel = i & 1 ? 0x7362 : 0x5140;
+      const uint32_t a = __byte_perm(v0[i >> 1], v1[i >> 1], sel), b = __byte_perm(v2[i >> 1], v3[i >> 1], sel);
+      const uint32_t a0 = f16x2_of_e4m3x2(a), a1 = f16x2_of_e4m3x2(a >> 16);
+      const uint32_t a2 = f16x2_of_e4m3x2(b), a3 = f16x2_of_e4m3x2(b >> 16);
+      mma_f16(d, a0, a1, a2, a3, lo[k][0], lo[k][1]);
+      mma_f16(d, a0, a1, a2, a3, hi[k][0], hi[k][1]);
     }
+    u.o[i][0] = __fadd2_rn(u.o[i][0], make_float2(d[0], d[1]));
+    u.o[i][1] = __fadd2_rn(u.o[i][1], make_float2(d[2], d[3]));
   }
 }
 
@@ -212,26 +295,384 @@ __device__ __forceinline__ void tile_finish(Tile8& t) {
   }
 }
 
-// Column 2c + z's record or output: 16 floats at `to` + 16 r.
-__device__ __forceinline__ void tile_store(const Tile8& t, float* to, int z, float by, uint64_t pol) {
-#pragma unroll
-  for (int i = 0; i < 8; i += 2)
-    st_hint4(to + 2 * i, make_float4(t.o[i][z] * by, t.o[i][z + 2] * by, t.o[i + 1][z] * by, t.o[i + 1][z + 2] * by), pol);
+// Four floats of column 2c + z: dims 16r + 4i ..
+__device__ __forceinline__ float4 tile_dims(const Tile8& t, int i, int z) {
+  const float2 a = t.o[2 * i][0], b = t.o[2 * i][1], c = t.o[2 * i + 1][0], d = t.o[2 * i + 1][1];
+  return z ? make_float4(a.y, b.y, c.y, d.y) : make_float4(a.x, b.x, c.x, d.x);
 }
 
-// The flat list of (beam, KV head, chunk) units, an even share for every warp (decode_mma.cuh); records are merged
-// in the launch (combine.cuh).
+// How a launch takes its beams' own chunks: whole (beam, KV head) pairs, or even ranges of `per` chunks of the flat list.
+struct Shares {
+  bool pairs;
+  int per, count;
+};
+
+__device__ __forceinline__ Shares shares_of(const PoolView& v, int mode, int nact, int total, int ctas) {
+  Shares s;
+  const int pairs = max(nact, 1) * v.Hkv;
+  s.pairs = false;
+  s.per = max(1, (total + ctas - 1) / ctas);
+  if (s.per > 160) s.per = (s.per + 3) / 4;
+  s.count = (total + s.per - 1) / s.per;
+  if (mode == 0) {
+    // Chunks that pass a CTA, and a unit's start and merge as so many more.
+    const int whole = (pairs + ctas - 1) / ctas * ((total + pairs - 1) / pairs + 16), even = (total + ctas - 1) / ctas + 48;
+    s.pairs = whole <= even;
+    if (s.pairs) s.count = v.max_beams * v.Hkv;
+  }
+  return s;
+}
+
+// ---- the loading warps -----------------------------------------------------------------------------
+
+// The stages of every unit whose ring slot is this loader's (number `own` of kLoaders8).
+__device__ void load_stages(const PoolView& v, const CUtensorMap* tm, int layer, unsigned char* smem, uint32_t bars, int own, int lane) {
+  const uint32_t full = bars, empty = bars + 8 * kStages8, ufull = bars + 16 * kStages8, uempty = ufull + 8 * kSlots8;
+  volatile int* stop = reinterpret_cast<volatile int*>(smem + Smem8::STOP);
+  const uint64_t once = policy_evict_first(), more = policy_evict_normal();
+  const int pg = v.P / kChunk;
+  const long long layer_pages = (long long)layer * v.num_pages;
+  const size_t gap = (size_t)v.Hkv * pg;  // exponents from K to V
+  uint32_t base = 0, top = 0;  // stages of earlier units; past the last that may be on its way
+  bool ok = true;
+  for (int k = 0; ok; ++k) {
+    const int slot = k % kSlots8;
+    ok = __all_sync(0xffffffffu, wait_or_stop(ufull + 8 * slot, (k / kSlots8) & 1, stop));
+    if (!ok) break;
+    const Unit8& u = reinterpret_cast<const Unit8*>(smem + Smem8::UNITS)[slot];
+    const int kind = u.kind, h = u.head, tok0 = u.tok0, n = (u.tokens + kChunk - 1) / kChunk, stages = (n + 1) / 2;
+    const int* table = v.tables + (size_t)u.source * v.max_pages;
+    const uint64_t pol = u.again ? more : once;
+    __syncwarp();
+    if (lane == 0) mbar_arrive_n(uempty + 8 * slot, 1);
+    __syncwarp();
+    if (kind == kUnitEnd) return;
+    // A chunk a lane: chunk lane % 2 of the loader's stage lane / 2, 16 of its stages at a time.
+    const int first = (int)((own - base) & (kLoaders8 - 1));
+    auto chunk_at = [&](int i0) { return 2 * (first + kLoaders8 * (i0 + (lane >> 1))) + (lane & 1); };
+    auto page_at = [&](int c) { return c < n ? table[(tok0 + c * kChunk) / v.P] : 0; };
+    auto group_at = [&](int c, int page) -> long long {  // row group of the chunk's K
+      if (page < 0 || page >= v.num_pages) {
+        if (c < n) set_status(v.ctl, GB_ERR_INVALID);
+        page = 0;
+      }
+      return ((layer_pages + page) * 2 * v.Hkv + h) * pg + ((tok0 + c * kChunk) & (v.P - 1)) / kChunk;
+    };
+    int c = chunk_at(0);
+    long long g = group_at(c, page_at(c));
+    int ek = v.kv_exp[g], ev = v.kv_exp[g + gap];
+    for (int i0 = 0; ok && first + kLoaders8 * i0 < stages; i0 += 16) {
+      const int next = chunk_at(i0 + 16), page = page_at(next);
+      const bool on = first + kLoaders8 * (i0 + 16) < stages;
+      long long gn = 0;
+      int ekn = 0, evn = 0;
+      const int i = c >> 1;  // the unit's stage
+      const uint32_t kk = base + i, st = kk % kStages8;
+      const bool in = c < n, there = i < stages;
+      top = base + min(stages, first + kLoaders8 * (i0 + 16));
+#pragma unroll 1
+      for (int z = 0; z < 4 && first + kLoaders8 * (i0 + 4 * z) < stages; ++z) {
+        if (z == 2 && on) {  // the page ids are there by now
+          gn = group_at(next, page);
+          ekn = v.kv_exp[gn];
+          evn = v.kv_exp[gn + gap];
+        }
+        // Eight lanes at a time.
+        const bool mine = lane >> 3 == z && there;
+        const bool good = !(mine && kk >= kStages8) || wait_or_stop(empty + 8 * st, (kk / kStages8 - 1) & 1, stop);
+        ok = __all_sync(0xffffffffu, good);
+        if (!ok) break;
+        if (mine) {
+          *reinterpret_cast<int2*>(smem + Smem8::EXPS + 16 * st + 8 * (lane & 1)) = in ? make_int2(ek, ev) : make_int2(0, 0);
+          const uint32_t bar = full + 8 * st;
+          if (in) {
+            mbar_arrive_expect_tx(bar, kChunkBytes8);
+            tma_chunk8(smem_addr(smem) + st * kStageBytes8 + (lane & 1) * kChunkBytes8, tm, (int)g, bar, pol);
+          } else {
+            mbar_arrive_n(bar, 1);
+          }
+        }
+        __syncwarp();
+      }
+      if (!ok) break;
+      c = next;
+      g = gn;
+      ek = ekn;
+      ev = evn;
+    }
+    base += stages;
+  }
+  // A wait ran out: leave no copy in flight.  (What was not issued runs out at once.)
+  for (int d = lane; d < 32 + kStages8; d += 32) {
+    const uint32_t last = top - 1 - d;
+    if ((int)last >= 0) mbar_wait_bounded(full + 8 * (last % kStages8), (last / kStages8) & 1, kWaitLimitNs / 100);
+  }
+}
+
+// ---- the planning warp -----------------------------------------------------------------------------
+
+struct Planner8 {
+  const int lane;
+  unsigned char* const smem;
+  const uint32_t ufull, uempty;
+  volatile int* const stop;
+  int units = 0;         // published
+  bool ok = true;
+
+  // The next unit's slot, once its last users have read it.
+  __device__ Unit8* slot() {
+    const int k = units % kSlots8;
+    const bool free = units < kSlots8 || wait_or_stop(uempty + 8 * k, (units / kSlots8 - 1) & 1, stop);
+    ok = __all_sync(0xffffffffu, free) && ok;
+    return reinterpret_cast<Unit8*>(smem + Smem8::UNITS) + k;
+  }
+  __device__ void publish() {
+    __syncwarp();
+    if (lane == 0) mbar_arrive_n(ufull + 8 * (units % kSlots8), 1);
+    __syncwarp();
+    ++units;
+  }
+};
+
 template <int G>
-__global__ void __launch_bounds__(kWarps8 * 32, 1)
+__device__ void plan_units(const PoolView& v, const Counters& cnt, int mode, const Shares& sh, unsigned char* smem, uint32_t bars, int lane) {
+  const int* s_off = reinterpret_cast<const int*>(smem + Smem8::PLAN);
+  const int* s_n = s_off + (kMaxBeams + 1);
+  Planner8 pl{lane, smem, bars + 16 * kStages8, bars + 16 * kStages8 + 8 * kSlots8, reinterpret_cast<volatile int*>(smem + Smem8::STOP)};
+  const bool shared = v.ctl[kCtlSegCount] > 0;
+  auto claim = [&](int word) {
+    int x = 0;
+    if (lane == 0) x = atomicAdd(&cnt.c[word], 1);
+    return x;
+  };
+  if (mode == 1) {
+    // The lists' tiles are of 128 rows: two units each, the second one empty where the members end before.
+    constexpr int members = kRows8 / G;
+    const int tiles = v.ctl[kCtlSegTiles], split = v.ctl[kCtlSegSplit];
+    const long long all = 2ll * tiles * v.Hkv;
+    int pending = (int)blockIdx.x;
+    while (pl.ok) {
+      const int u = __shfl_sync(0xffffffffu, pending, 0);
+      if (u >= all) break;
+      pending = (int)gridDim.x + claim(kCntGrpNext);
+      const int tq = u / (2 * v.Hkv), h = u / 2 % v.Hkv;
+      const int s = v.seg_tile_seg[tq], t = v.seg_tile_t[tq], sp = v.seg_tile_split[tq];
+      const int g = v.seg_g[s], moff = v.seg_mem_off[s], rep = v.seg_rep[s];
+      const int tok0 = sp * split, tokens = min(v.seg_len[s] * v.P - tok0, split);
+      const int m0 = (2 * t + (u & 1)) * members, have = min(members, g - m0);
+      if (have <= 0) continue;
+      Unit8* x = pl.slot();
+      if (!pl.ok) break;
+      for (int m = lane; m < have; m += 32) x->members[m] = v.seg_members[moff + m0 + m];
+      if (lane == 0) {
+        x->kind = kUnitSegment;
+        x->head = h;
+        x->tokens = tokens;
+        x->rows = have * G;
+        x->record = sp;
+        x->source = rep;
+        x->tok0 = v.seg_i0[s] * v.P + tok0;
+        x->again = g > members;
+      }
+      pl.publish();
+    }
+  }
+  // One (beam, head)'s chunks [i, i + n) of its list.
+  auto beam_unit = [&](int b, int h, int i, int n, int range) {
+    Unit8* x = pl.slot();
+    if (!pl.ok) return;
+    const int tok0 = plan_start(v, mode)[b] + i * kChunk, tokens = min(n * kChunk, v.seq_len[b] - tok0);
+    if (lane == 0) {
+      x->kind = kUnitBeam;
+      x->head = h;
+      x->tokens = tokens;
+      x->rows = G;
+      x->record = range + b * v.Hkv + h;
+      x->direct = n == s_n[b] && (mode == 0 || v.seg_nrec[b] == 0);
+      x->members[0] = b;
+      x->source = b;
+      x->tok0 = tok0;
+      x->again = mode == 0 && shared;
+    }
+    pl.publish();
+  };
+  // The first share is the CTA's own, the others are whoever's comes first.
+  int pending = (int)blockIdx.x;
+  while (pl.ok) {
+    const int u = __shfl_sync(0xffffffffu, pending, 0);
+    if (u >= sh.count) break;
+    if (sh.count > (int)gridDim.x) pending = (int)gridDim.x + claim(kCntRange);
+    else pending = sh.count;
+    if (sh.pairs) {
+      const int b = u / v.Hkv;
+      if (s_n[b] > 0) beam_unit(b, u - b * v.Hkv, 0, s_n[b], 0);
+      continue;
+    }
+    int x = u * sh.per;
+    const int end = min(s_off[v.max_beams], x + sh.per);
+    int b = 0, hi = v.max_beams;  // s_off[b] <= x < s_off[hi]
+    while (hi - b > 1) {
+      const int mid = (b + hi) >> 1;
+      if (s_off[mid] <= x) b = mid; else hi = mid;
+    }
+    while (x < end && pl.ok) {
+      while (s_off[b + 1] <= x) ++b;
+      const int h = (x - s_off[b]) / s_n[b], i = x - s_off[b] - h * s_n[b], n = min(s_n[b] - i, end - x);
+      beam_unit(b, h, i, n, u);
+      x += n;
+    }
+  }
+  if (pl.ok) {
+    Unit8* x = pl.slot();
+    if (pl.ok && lane == 0) x->kind = kUnitEnd;
+    if (pl.ok) pl.publish();
+  }
+}
+
+// ---- the multiplying warps --------------------------------------------------------------------------
+
+// Where a unit's row goes: its record, or its output.
+template <int G>
+__device__ __forceinline__ float* row_record(const PoolView& v, const Unit8& u, int row) {
+  if (u.kind == kUnitBeam) return v.partials + (size_t)u.record * v.record_floats;
+  const int e = u.members[row / G], b = e / kMaxSegDepth;
+  return v.grec + (((size_t)b * kMaxSegRecords + v.seg_rec_off[e] + u.record) * v.Hkv + u.head) * v.record_floats;
+}
+
+// One unit by the multiplying warps: row groups of 8 rows (1, 2, 4 or 8), and in each as many groups of stages as there are
+// warps for it.  A warp whose wait ran out still keeps step with the others; what the unit then leaves is nobody's, as the
+// status is set.
+template <int G>
+__device__ __forceinline__ void multiply(const PoolView& v, const Unit8& u, const __nv_bfloat16* q, float qscale, uint32_t base,
+                                         uint32_t bars, unsigned char* smem, float* out) {
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = lane >> 2, c = lane & 3;
+  const uint32_t full = bars, empty = bars + 8 * kStages8, ring = smem_addr(smem);
+  volatile int* stop = reinterpret_cast<volatile int*>(smem + Smem8::STOP);
+  const int rgroups = u.rows <= 8 ? 1 : u.rows <= 16 ? 2 : u.rows <= 32 ? 4 : 8, groups = kConsumers8 / rgroups;
+  const int rg = warp % rgroups, group = warp / rgroups;
+  Tile8 t;
+  {
+    const int row = rg * 8 + r;
+    const __nv_bfloat16* at = nullptr;
+    if (row < u.rows) {
+      const int e = u.members[row / G], b = u.kind == kUnitBeam ? e : e / kMaxSegDepth;
+      at = q + ((size_t)b * v.Hq + (size_t)u.head * G + row % G) * 128;
+    }
+    tile_begin(t, at, qscale, c);
+  }
+  const int stages = (u.tokens + 2 * kChunk - 1) / (2 * kChunk);
+  for (int i = group; i < stages; i += groups) {
+    const uint32_t k = base + i, s = k % kStages8;
+    if (!__all_sync(0xffffffffu, wait_or_stop(full + 8 * s, (k / kStages8) & 1, stop))) break;
+    const int4 e = *reinterpret_cast<const int4*>(smem + Smem8::EXPS + 16 * s);
+    const int eh[2][2] = {{e.x, e.y}, {e.z, e.w}};
+    attend(t, ring + s * kStageBytes8, min(2 * kChunk, u.tokens - i * 2 * kChunk), eh, r, c, [&] {
+      __syncwarp();
+      if (lane == 0) mbar_arrive_n(empty + 8 * s, groups);
+      __syncwarp();
+    });
+  }
+  tile_finish(t);
+  // The warps' states of the same rows, merged through shared memory four rows of each at a time.
+  float* left = reinterpret_cast<float*>(smem + Smem8::MERGE);
+  float2* ml = reinterpret_cast<float2*>(smem + Smem8::STATE);
+  const uint64_t pol = policy_evict_last();  // the launch's merge reads the records back from L2
+#pragma unroll
+  for (int f = 0; f < 2; ++f) {
+    if (f > 0 && 4 * f >= u.rows) break;
+    if (c >> 1 == f) {
+#pragma unroll
+      for (int z = 0; z < 2; ++z) {
+        const int in = warp * 4 + 2 * (c & 1) + z;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) *reinterpret_cast<float4*>(left + in * kRowFloats8 + 16 * r + 4 * i) = tile_dims(t, i, z);
+        if (r == 0) ml[in] = z ? make_float2(t.m1, t.l1) : make_float2(t.m0, t.l0);
+      }
+    }
+    consumers_sync();
+    for (int i = tid; i < rgroups * 4 * 32; i += kConsumers8 * 32) {
+      const int g = i >> 7, in = (i >> 5) & 3, row = g * 8 + 4 * f + in, d = 4 * (i & 31);
+      if (row >= u.rows) continue;
+      float M = -INFINITY;
+      for (int k = 0; k < groups; ++k) M = fmaxf(M, ml[(g + k * rgroups) * 4 + in].x);
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+      float L = 0.f;
+      for (int k = 0; k < groups; ++k) {
+        const int w = (g + k * rgroups) * 4 + in;
+        const float2 a = ml[w];
+        if (a.x == -INFINITY) continue;  // a warp without a stage
+        const float f2 = exp2f(a.x - M);
+        const float4 x = *reinterpret_cast<const float4*>(left + w * kRowFloats8 + d);
+        acc.x = fmaf(x.x, f2, acc.x);
+        acc.y = fmaf(x.y, f2, acc.y);
+        acc.z = fmaf(x.z, f2, acc.z);
+        acc.w = fmaf(x.w, f2, acc.w);
+        L = fmaf(a.y, f2, L);
+      }
+      if (u.kind == kUnitBeam && u.direct) {
+        float* to = out + ((size_t)u.members[0] * v.Hq + (size_t)u.head * G + row) * 128 + d;
+        to[0] = acc.x / L;
+        to[1] = acc.y / L;
+        to[2] = acc.z / L;
+        to[3] = acc.w / L;
+      } else {
+        float* rec = row_record<G>(v, u, row);
+        st_hint4(rec + row % G * 128 + d, acc, pol);
+        if (d == 0) {
+          st_hint(rec + G * 128 + row % G, M, pol);
+          st_hint(rec + G * 128 + G + row % G, L, pol);
+        }
+      }
+    }
+    consumers_sync();
+  }
+}
+
+template <int G>
+__device__ void multiply_units(const PoolView& v, const Counters& cnt, const __nv_bfloat16* q, float qscale, int mode, unsigned char* smem,
+                               uint32_t bars, float* out) {
+  const int tid = threadIdx.x, lane = tid & 31;
+  const uint32_t ufull = bars + 16 * kStages8, uempty = ufull + 8 * kSlots8;
+  volatile int* stop = reinterpret_cast<volatile int*>(smem + Smem8::STOP);
+  uint32_t base = 0;       // stages of earlier units
+  bool segments = mode == 1;
+  for (int k = 0;; ++k) {
+    const int slot = k % kSlots8;
+    const bool there = __all_sync(0xffffffffu, wait_or_stop(ufull + 8 * slot, (k / kSlots8) & 1, stop));
+    if (consumers_any(!there || *stop != 0)) {  // all leave together
+      if (tid == 0) set_status(v.ctl, GB_ERR_TIMEOUT);
+      return;
+    }
+    const Unit8& u = reinterpret_cast<const Unit8*>(smem + Smem8::UNITS)[slot];
+    if (segments && u.kind != kUnitSegment) {  // this CTA's segment records are written
+      if (tid == 0) {
+        fence_acq_rel_gpu();
+        atomicAdd(&cnt.c[kCntGrpDone], 1);
+      }
+      segments = false;
+    }
+    if (u.kind == kUnitEnd) return;
+    multiply<G>(v, u, q, qscale, base, bars, smem, out);
+    base += (u.tokens + 2 * kChunk - 1) / (2 * kChunk);
+    if (tid == 0 && u.kind == kUnitBeam && !u.direct) {
+      fence_acq_rel_gpu();
+      atomicAdd(&cnt.pair[u.members[0] * v.Hkv + u.head], 1);
+    }
+    __syncwarp();
+    if (lane == 0) mbar_arrive_n(uempty + 8 * slot, 1);
+  }
+}
+
+template <int G>
+__global__ void __launch_bounds__(kThreads8, 1)
     k_decode8(PoolView v, const __grid_constant__ CUtensorMap tm, int layer, const __nv_bfloat16* q, float qscale, int mode,
               float* __restrict__ out) {
   pdl_wait();
   pdl_launch_dependents();
-  using S = Smem8;
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   unsigned char* smem = smem_raw + ((1024 - (smem_addr(smem_raw) & 1023)) & 1023);
-  const int cta = (int)blockIdx.x, nctas = (int)gridDim.x;
-  const int step_ok = v.ctl[kCtlStepOk], steps = v.ctl[kCtlSteps];
+  const int cta = (int)blockIdx.x, nctas = (int)gridDim.x, tid = threadIdx.x;
+  const int step_ok = v.ctl[kCtlStepOk], steps = v.ctl[kCtlSteps], nact = v.ctl[kCtlActive];
   if (step_ok == 0) {
     zero_all_pairs<G>(v, cta, nctas, out);
     return;
@@ -239,154 +680,69 @@ __global__ void __launch_bounds__(kWarps8 * 32, 1)
   const int set = counter_set(v, layer, steps);
   const Counters cnt = counters(v, set);
   zero_counters(v, set ^ 1, cta, nctas);
-  int* s_off = reinterpret_cast<int*>(smem + S::STAGES + S::BARS);
-  int* s_n = s_off + (kMaxBeams + 1);
-  int* s_start = s_n + (kMaxBeams + 1);
-  int* s_len = s_start + (kMaxBeams + 1);
+  // mode 1: by segments; mode 2: by segments where that pays.  A segment's pages are read once for all of its members,
+  // but the multiplying warps do as much for a row either way, except that two or more members with few heads fill a tile that
+  // one would leave half empty.  So it pays where beams of up to 4 heads a KV head read far more than there is (us, beams alone /
+  // segments; MB read alone / there): 283 / 219 (1600 / 673, 128 x 6100), 281 / 229 (1844 / 491, 300 x 3000, G = 2); not 118 / 124
+  // (525 / 185, 64 x 4000), 146 / 156 (577 / 188, 256 x 1100), 283 / 438 (1623 / 359, 198 x 8000, G = 8).
+  if (v.ctl[kCtlSegTiles] == 0) mode = 0;
+  if (mode == 2) {
+    const long long all = (long long)plan_off(v, 0)[v.max_beams] * kChunkBytes8;
+    const long long there = plan_off(v, 1)[v.max_beams] * (long long)kChunkBytes8 + (long long)v.ctl[kCtlSegTok] * v.Hkv * (kChunkBytes8 / kChunk);
+    mode = G <= 4 && 5 * all - 6 * there > 3500000000ll ? 1 : 0;
+  }
+  const uint32_t bars = smem_addr(smem) + Smem8::BARS;
   {
+    int* s_off = reinterpret_cast<int*>(smem + Smem8::PLAN);
     const int* off = plan_off(v, mode);
     const int* nn = plan_n(v, mode);
-    const int* st = plan_start(v, mode);
-    for (int i = threadIdx.x; i <= v.max_beams; i += blockDim.x) {
+    for (int i = tid; i <= v.max_beams; i += kThreads8) {
       s_off[i] = off[i];
-      s_n[i] = i < v.max_beams ? nn[i] : 0;
-      s_start[i] = i < v.max_beams ? st[i] : 0;
-      s_len[i] = i < v.max_beams ? v.seq_len[i] : 0;
+      s_off[i + kMaxBeams + 1] = i < v.max_beams ? nn[i] : 0;
     }
+  }
+  if (tid == 0) {
+    for (int s = 0; s < kStages8; ++s) {
+      mbar_init(bars + 8 * s, 2);
+      mbar_init(bars + 8 * (kStages8 + s), kConsumers8);
+    }
+    for (int s = 0; s < kSlots8; ++s) {
+      mbar_init(bars + 8 * (2 * kStages8 + s), 1);
+      mbar_init(bars + 8 * (2 * kStages8 + kSlots8 + s), kConsumers8 + kLoaders8);
+    }
+    *reinterpret_cast<volatile int*>(smem + Smem8::STOP) = 0;
+    fence_mbar_init();
   }
   __syncthreads();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
-  const uint32_t stage0 = smem_addr(smem) + warp * kStages8 * kStageBytes8;
-  const uint32_t bar0 = smem_addr(smem) + S::STAGES + warp * kStages8 * 8;
-  const int W = nctas * kWarps8, w = cta * kWarps8 + warp, Tot = s_off[v.max_beams];
-  const int cw = (Tot + W - 1) / W;
-  const int x_begin = min(Tot, w * cw), x_end = min(Tot, x_begin + cw);
-  if (x_begin < x_end) {
-    if (lane == 0) {
-      for (int s = 0; s < kStages8; ++s) mbar_init(bar0 + 8 * s, 1);
-      fence_mbar_init();
-    }
-    __syncwarp();
-    ChunkIter it;
-    {
-      int lo = 0, hi = v.max_beams;  // invariant: s_off[lo] <= x < s_off[hi]
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (s_off[mid] <= x_begin) lo = mid; else hi = mid;
-      }
-      it.b = lo;
-      it.n = s_n[lo];
-      it.tok0 = s_start[lo];
-      const int rr = x_begin - s_off[lo];
-      it.h = rr / it.n;
-      it.i = rr % it.n;
-    }
-    const bool reread = mode == 0 && v.ctl[kCtlSegCount] > 0;
-    const uint64_t pol = reread || !v.grouped ? policy_evict_normal() : policy_evict_first();
-    int pw_b = -1, pw_i0 = 0, pw_lane = 0;
-    auto load_page = [&](const ChunkIter& qi) -> int {
-      if (qi.b != pw_b || qi.i < pw_i0 || qi.i >= pw_i0 + 32) {
-        pw_b = qi.b;
-        pw_i0 = qi.i;
-        const int i = pw_i0 + lane;
-        pw_lane = i >= qi.n ? 0 : v.tables[(size_t)qi.b * v.max_pages + (qi.tok0 + i * kChunk) / v.P];
-      }
-      return __shfl_sync(0xffffffffu, pw_lane, qi.i - pw_i0);
-    };
-    const int pg = v.P / kChunk;
-    const long long layer_pages = (long long)layer * v.num_pages;
-    const size_t kv_gap = (size_t)v.Hkv * pg;  // exponents from K to V
-    // Loads of the chunk at `qi` into a stage; lanes 0 and 1 of every warp also fetch its exponents, which wait in
-    // registers (`ex`, a slot a stage).
-    int ex[kStages8];
-    auto issue = [&](const ChunkIter& qi, int page, int stage) -> int {
-      if (page < 0 || page >= v.num_pages) {
-        if (lane == 0) set_status(v.ctl, GB_ERR_INVALID);
-        page = 0;
-      }
-      const int tok = qi.tok0 + qi.i * kChunk;
-      const long long g = ((layer_pages + page) * 2 * v.Hkv + qi.h) * pg + (tok & (v.P - 1)) / kChunk;
-      if (lane == 0) {
-        mbar_arrive_expect_tx(bar0 + 8 * stage, kStageBytes8);
-        tma_chunk8(stage0 + stage * kStageBytes8, &tm, (int)g, bar0 + 8 * stage, pol);
-      }
-      return lane < 2 ? v.kv_exp[g + lane * (long long)kv_gap] : 0;
-    };
-    ChunkIter ip = it;
-    int ip_x = x_begin, ip_page = load_page(ip);
-#pragma unroll
-    for (int s = 0; s < kStages8; ++s) {
-      ex[s] = 0;
-      if (ip_x < x_end) {
-        ex[s] = issue(ip, ip_page, s);
-        ++ip_x;
-        if (ip_x < x_end) {
-          iter_advance(ip, s_n, s_start, v.Hkv, v.max_beams);
-          ip_page = load_page(ip);
-        }
-      }
-    }
-    Tile8 t[1];
-    bool fresh = true, alive = true;
-    uint32_t parity = 0;
-    for (int x0 = x_begin; x0 < x_end && alive; x0 += kStages8, parity ^= 1u) {
-#pragma unroll
-      for (int s = 0; s < kStages8; ++s) {
-        const int x = x0 + s;
-        if (x >= x_end || !alive) break;
-        if (fresh) {
-          tile_begin(t[0], r < G ? q + ((size_t)it.b * v.Hq + it.h * G + r) * 128 : nullptr, qscale, c);
-          fresh = false;
-        }
-        if (!mbar_wait_bounded(bar0 + 8 * s, parity, kWaitLimitNs)) {
-          if (lane == 0) set_status(v.ctl, GB_ERR_TIMEOUT);
-          for (int z = 1; z < kStages8; ++z)  // a bounded chance for the copies in flight
-            if (x + z < ip_x) mbar_wait_bounded(bar0 + 8 * ((s + z) % kStages8), parity ^ (s + z >= kStages8 ? 1u : 0u), kWaitLimitNs / 4);
-          alive = false;
-          break;
-        }
-        const int nvalid = min(kChunk, s_len[it.b] - (it.tok0 + it.i * kChunk));
-        chunk_attend8<1>(t, stage0 + s * kStageBytes8, nvalid, __shfl_sync(0xffffffffu, ex[s], 0),
-                         __shfl_sync(0xffffffffu, ex[s], 1), r, c);
-        __syncwarp();
-        if (ip_x < x_end) {
-          if (lane == 0) fence_proxy_async_smem();
-          ex[s] = issue(ip, ip_page, s);
-          ++ip_x;
-          if (ip_x < x_end) {
-            iter_advance(ip, s_n, s_start, v.Hkv, v.max_beams);
-            ip_page = load_page(ip);
-          }
-        }
-        if (it.i == it.n - 1 || x + 1 == x_end) {
-          tile_finish(t[0]);
-          float* rec = v.partials + (size_t)(w + it.b * v.Hkv + it.h) * v.record_floats;
-          const uint64_t rpol = policy_evict_last();
-#pragma unroll
-          for (int z = 0; z < 2; ++z)
-            if (2 * c + z < G) {
-              tile_store(t[0], rec + (2 * c + z) * 128 + 16 * r, z, 1.f, rpol);
-              if (r == 0) {
-                st_hint(rec + G * 128 + 2 * c + z, z ? t[0].m1 : t[0].m0, rpol);
-                st_hint(rec + G * 128 + G + 2 * c + z, z ? t[0].l1 : t[0].l0, rpol);
-              }
-            }
-          record_arrive(cnt, it.b * v.Hkv + it.h, lane);
-          fresh = true;
-        }
-        if (x + 1 < x_end) iter_advance(it, s_n, s_start, v.Hkv, v.max_beams);
-      }
-    }
+  const Shares sh = shares_of(v, mode, nact, reinterpret_cast<const int*>(smem + Smem8::PLAN)[v.max_beams], nctas);
+  if (tid >> 5 >= kConsumers8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kLoaderRegs8));
+    const int w = (tid >> 5) - kConsumers8;
+    if (w == 0) plan_units<G>(v, cnt, mode, sh, smem, bars, tid & 31);
+    else if (w <= kLoaders8) load_stages(v, &tm, layer, smem, bars, w - 1, tid & 31);
+    return;
   }
-  combine_pairs<G>(v, cnt, mode, W, 0, false, cta, nctas, out);
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kConsumerRegs8));
+  multiply_units<G>(v, cnt, q, qscale, mode, smem, bars, out);
+  // Every CTA is resident with the others (one an SM), and each wait gives up once the status is set.
+  combine_shares<G, true>(v, cnt, mode, sh.pairs ? 0 : sh.per, nctas, false, cta, nctas, kConsumers8, out);
 }
 
 template <int G>
 cudaError_t launch_decode8_t(gb_pool* pool, int layer, const void* q, float scale, float* out, int mode, cudaStream_t s) {
   cudaError_t e = set_max_dynamic_smem(reinterpret_cast<const void*>(k_decode8<G>), Smem8::TOTAL);
   if (e != cudaSuccess) return e;
+  // With fewer registers at launch than its warps then share out the kernel would wait for ever.
+  static std::atomic<bool> fits{false};
+  if (!fits.load(std::memory_order_relaxed)) {
+    cudaFuncAttributes a{};
+    e = cudaFuncGetAttributes(&a, k_decode8<G>);
+    if (e != cudaSuccess) return e;
+    if (a.numRegs * kThreads8 < (kConsumers8 * kConsumerRegs8 + 4 * kLoaderRegs8) * 32) return cudaErrorInvalidConfiguration;
+    fits.store(true, std::memory_order_relaxed);
+  }
   prof_begin(pool, GB_PROF_DECODE, s);
-  e = launch_pdl(k_decode8<G>, pool->num_sms, kWarps8 * 32, Smem8::TOTAL, s, pool->view,
+  e = launch_pdl(k_decode8<G>, pool->num_sms, kThreads8, Smem8::TOTAL, s, pool->view,
                  *reinterpret_cast<const CUtensorMap*>(pool->dtmap), layer, static_cast<const __nv_bfloat16*>(q),
                  scale * 1.4426950408889634f, mode, out);
   prof_end(pool, GB_PROF_DECODE, s);
@@ -411,7 +767,7 @@ cudaError_t launch_decode8(gb_pool* pool, int layer, const void* q, float scale,
 bool make_tensor_map8(gb_pool* pool) {
   const PoolView& v = pool->view;
   const unsigned long long slab = (unsigned long long)v.Hkv * v.P / 16, groups = (unsigned long long)v.layers * v.num_pages * 2 * slab;
-  if (groups >= (1ull << 31) || pool->num_sms * kWarps8 > kMaxDecodeWarps) return false;
+  if (groups >= (1ull << 31)) return false;
   const cuuint64_t dims[4] = {64, 16, 2, groups - slab};
   const cuuint64_t strides[3] = {128, (cuuint64_t)v.Hkv * v.P * 128, 2048};
   const cuuint32_t box[4] = {64, 16, 2, 1};

@@ -737,6 +737,7 @@ extern "C" gb_status gb_pool_init(const gb_pool_config* cfg, void* kv_dev, void*
   // The grouped path runs as a role of the attention kernel beside the per-beam role, so it
   // needs both tensor maps.
   if (v.grouped && !(p->have_tmap && p->have_dtmap && p->num_sms * kMmaWarps <= kMaxDecodeWarps)) v.grouped = 0;
+  if (cfg->kv_dtype == GB_FP8) v.grouped = 1;  // (decode8.cu)
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   if (cudaMemsetAsync(m, 0, L.partials, s) != cudaSuccess ||
       cudaMemsetAsync(m + L.seg_cover, 0, L.seg_owner - L.seg_cover, s) != cudaSuccess ||
@@ -882,7 +883,7 @@ static gb_status decode_layer(gb_pool* pool, int layer, const RotationView& rot,
     if (st != GB_OK) return st;
     if (rot.table) q_dev = turned_q;
     prof_begin(pool, GB_PROF_ATTENTION, s);
-    launch_decode8(pool, layer, q_dev, scale, out_dev, flags == GB_PATH_PER_BEAM || !pool->view.grouped ? 0 : 1, s);
+    launch_decode8(pool, layer, q_dev, scale, out_dev, flags == GB_PATH_PER_BEAM ? 0 : flags == GB_PATH_GROUPED ? 1 : 2, s);
     prof_end(pool, GB_PROF_ATTENTION, s);
     return check_launch(pool, "decode");
   }
