@@ -26,6 +26,10 @@ constexpr int kUnit = 44;               // a weight of one is 2^44
 constexpr int kBins = 256, kDigits = 4, kDigitBits = 12;
 constexpr int kMaxCluster = 8;
 constexpr float kFar = 46.f;            // weights of 2^-46 and less count as none
+constexpr int kCap = 4096;              // tokens of a list
+constexpr int kSlices = 1024;           // of the weights' exponents, 22 to a power of two
+constexpr float kPerPower = 22.f;
+static_assert(kFar * kPerPower < kSlices, "every weight has a slice");
 typedef unsigned long long u64;
 
 // 2^(-j/256) in units of 2^-44: the power series of exp in 64 bits, as the compiler evaluates it.
@@ -113,6 +117,15 @@ __device__ __forceinline__ u64 weight(const Row& row, const u64* table, float x)
   return (w + ((1ull << n) >> 1)) >> n;
 }
 
+// The slice of a weight: y in steps of 1 / 22 (in a lower slice the weight is larger).
+__device__ __forceinline__ int slice_of(const Row& row, float x) {
+  if (x == row.max) return 0;
+  const float y = __fmul_rn(__fsub_rn(row.max, x), row.ch);
+  return y < kFar ? (int)(y * kPerPower) : kSlices - 1;
+}
+// Masses are summed in units of 2^shift by slice: 12 bits of a weight's 45.
+__device__ __forceinline__ int slice_shift(int b) { return max(0, 32 - b / (int)kPerPower); }
+
 __device__ __forceinline__ float value(const float* p) { return *p; }
 __device__ __forceinline__ float value(const __nv_bfloat16* p) { return __bfloat162float(*p); }
 __device__ __forceinline__ void values(const uint4& v, float (&x)[4]) {
@@ -154,8 +167,19 @@ struct Pieces {
 
 // ---- the row's CTAs ----------------------------------------------------------------------------------
 
+struct Entry {
+  float x;
+  int i;
+};
+
 struct Smem {
   u64 table[kBins];
+  Entry list[kCap];                      // the first CTA's holds all
+  uint32_t slice[kSlices];               // masses by slice, see top_p_cut
+  u64 slice_total[kSlices];
+  int listed, window[2];
+  uint32_t head_k;
+  int head_i;
   uint32_t hist[1 + kDigits][kBins];     // counts, then the masses' digits
   u64 total[kBins];
   float red[kWarps];
@@ -186,7 +210,9 @@ struct RowCtas {
   // f(value, token) of every token, spread over the row's CTAs.
   template <class F>
   __device__ __forceinline__ void each(F f) const {
-    for (int v = (int)(rank * kThreads + threadIdx.x); v < pieces.count; v += (int)(ctas * kThreads)) {
+    const int step = (int)(ctas * kThreads);
+#pragma unroll 2
+    for (int v = (int)(rank * kThreads + threadIdx.x); v < pieces.count; v += step) {
       float x[N];
       pieces.load(v, x);
 #pragma unroll
@@ -196,14 +222,20 @@ struct RowCtas {
       }
     }
   }
+  // The same of the first n tokens of this CTA's list.
+  template <class F>
+  __device__ __forceinline__ void each_listed(int n, F f) const {
+    for (int j = threadIdx.x; j < n; j += kThreads) f(sm.list[j].x, sm.list[j].i);
+  }
 
-  // One digit of a selection: the bin in which the running total (of counts or masses, by bin in ascending order) reaches
-  // `target` > 0, and the total before it.  bin(x, i): a token's bin, or -1; weigh: by mass.
+  // One digit of a selection among the row's tokens (n < 0) or this CTA's first n listed ones: the bin in which the running
+  // total (of counts or masses, by bin in ascending order) reaches `target` > 0, and the total before it.  bin(x, i): a token's
+  // bin, or -1; weigh: by mass.
   template <class B>
-  __device__ void digit(bool weigh, u64 target, B bin) {
+  __device__ void digit(int n, bool weigh, u64 target, B bin) {
     for (int t = threadIdx.x; t < (1 + kDigits) * kBins; t += kThreads) (&sm.hist[0][0])[t] = 0;
     __syncthreads();
-    each([&](float x, int i) {
+    auto count = [&](float x, int i) {
       const int b = bin(x, i);
       if (b < 0) return;
       if (!weigh) {
@@ -216,11 +248,18 @@ struct RowCtas {
         const uint32_t part = (uint32_t)(w >> (d * kDigitBits)) & ((1u << kDigitBits) - 1);
         if (part) atomicAdd(&sm.hist[1 + d][b], part);
       }
-    });
-    cluster_sync();
+    };
+    if (n < 0) {
+      each(count);
+      cluster_sync();
+    } else {
+      each_listed(n, count);
+      __syncthreads();
+    }
     for (int b = threadIdx.x; b < kBins; b += kThreads) {
       u64 t = 0;
-      for (unsigned c = 0; c < ctas; ++c) {
+      const unsigned first = n < 0 ? 0 : rank, last = n < 0 ? ctas : rank + 1;
+      for (unsigned c = first; c < last; ++c) {
         if (!weigh) {
           t += peer_load(peer_addr(&sm.hist[0][b], c));
         } else {
@@ -229,7 +268,8 @@ struct RowCtas {
       }
       sm.total[b] = t;
     }
-    cluster_sync();
+    if (n < 0) cluster_sync();
+    else __syncthreads();
     if (threadIdx.x < 32) {
       const int lane = threadIdx.x;
       u64 own = 0;
@@ -254,12 +294,12 @@ struct RowCtas {
     __syncthreads();
   }
 
-  // Cut the head where its running total (counts, or masses) reaches `target`, 1 <= target <= the head's total.
-  __device__ Head cut(const Head& h, bool weigh, u64 target) {
+  // Cut the head where its running total (counts, or masses) reaches `target`, 1 <= target <= the head's total.  n: digit()'s.
+  __device__ Head cut(const Head& h, int n, bool weigh, u64 target) {
     const uint32_t top = key_of(row.max);
     uint32_t at = 0;                       // of top - key, the digits chosen so far
     for (int s = 24; s >= 0; s -= 8) {
-      digit(weigh, target, [&](float x, int i) {
+      digit(n, weigh, target, [&](float x, int i) {
         const uint32_t key = key_of(x), rel = top - key;
         return kept(h, key, i) && (s == 24 || rel >> (s + 8) == at >> (s + 8)) ? (int)(rel >> s & 255u) : -1;
       });
@@ -274,17 +314,187 @@ struct RowCtas {
       const u64 w = weight(row, sm.table, key_value(to.k));
       most = w ? (target + w - 1) / w : target;
     }
+    to.i = min(to.i, by_index(n, false, most, [&](float x, int i) { return key_of(x) == to.k && i <= to.i; }));
+    return to;
+  }
+
+  // The index at which the running total of the tokens that in(x, i) says, taken by index, reaches `target`.
+  template <class In>
+  __device__ int by_index(int n, bool weigh, u64 target, In in) {
     int index = 0;
     for (int s = 16; s >= 0; s -= 8) {     // (indexes are below 2^19)
-      digit(false, most, [&](float x, int i) {
-        return key_of(x) == to.k && i <= to.i && (s == 16 || i >> (s + 8) == index >> (s + 8)) ? i >> s & 255 : -1;
+      digit(n, weigh, target, [&](float x, int i) {
+        return in(x, i) && (s == 16 || i >> (s + 8) == index >> (s + 8)) ? i >> s & 255 : -1;
       });
       index |= sm.bin << s;
-      most -= sm.before;
+      target -= sm.before;
       __syncthreads();
     }
-    to.i = min(to.i, index);
+    return index;
+  }
+
+  // This CTA's sum, in every thread.
+  __device__ u64 block_sum(u64 s) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if ((threadIdx.x & 31) == 0) sm.red64[threadIdx.x >> 5] = s;
+    __syncthreads();
+    u64 t = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) t += sm.red64[w];
+    __syncthreads();
+    return t;
+  }
+
+  // Puts the tokens that in(x, i) says into this CTA's list; then the first CTA's holds all of the row's (in no order).
+  // Returns how many there are: lists of more than kCap hold no more, and are none.
+  template <class In>
+  __device__ int gather(In in) {
+    if (threadIdx.x == 0) sm.listed = 0;
+    __syncthreads();
+    const int step = (int)(ctas * kThreads);
+    for (int v0 = (int)(rank * kThreads) + (int)(threadIdx.x & ~31u); v0 < pieces.count; v0 += step) {
+      const int v = v0 + (int)(threadIdx.x & 31);
+      float x[N];
+      pieces.load(v, x);
+      unsigned mine = 0;
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const int i = v * N - pieces.off + e;
+        if (v < pieces.count && i >= 0 && i < pieces.vocab && in(x[e], i)) mine |= 1u << e;
+      }
+      if (!__any_sync(0xffffffffu, mine != 0)) continue;
+      if (mine) {
+        int at = atomicAdd(&sm.listed, __popc(mine));
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+          if (mine >> e & 1) {
+            if (at < kCap) sm.list[at] = {x[e], v * N - pieces.off + e};
+            ++at;
+          }
+      }
+    }
+    cluster_sync();
+    int n = 0, before = 0;
+    for (unsigned c = 0; c < ctas; ++c) {
+      const int own = (int)peer_load(peer_addr(&sm.listed, c));
+      if (c < rank) before += own;
+      n += own;
+    }
+    if (n <= kCap && rank > 0) {
+      const int own = sm.listed;
+      for (int j = threadIdx.x; j < own; j += kThreads)
+        peer_store64(peer_addr(&sm.list[before + j], 0), (u64)__float_as_uint(sm.list[j].x) | (u64)(unsigned)sm.list[j].i << 32);
+    }
+    cluster_sync();
+    return n;
+  }
+
+  // The head that the first CTA has found, to all.
+  __device__ Head share(const Head& h) {
+    if (rank == 0 && threadIdx.x == 0) {
+      sm.head_k = h.k;
+      sm.head_i = h.i;
+    }
+    cluster_sync();
+    const Head to = {peer_load(peer_addr(&sm.head_k, 0)), (int)peer_load(peer_addr(&sm.head_i, 0))};
+    cluster_sync();
     return to;
+  }
+
+  // The k-th largest of the threads' largest tokens, of k <= kThreads: at least k of the row's tokens are as large.
+  __device__ uint32_t bound_of_top(int k, uint32_t key) {
+    uint32_t at = 0;  // the largest value that at least k keys reach
+    for (int b = 31; b >= 0; --b)
+      if (__syncthreads_count(key >= (at | 1u << b)) >= k) at |= 1u << b;
+    if (threadIdx.x == 0) sm.head_k = at;
+    cluster_sync();
+    for (unsigned c = 0; c < ctas; ++c) at = max(at, peer_load(peer_addr(&sm.head_k, c)));
+    cluster_sync();
+    return at;
+  }
+
+  // Cut the head where its mass reaches the share p of its total.  One pass sums the weights exactly, and by slices of their
+  // exponent to 12 bits each: the running total of the slices is then known from below, and from above within 2^-10 of itself,
+  // which leaves a slice or two in which the cut must lie.  A second pass sums what lies before them exactly and lists their
+  // tokens, among which the cut is found.  Tokens so light that all of them together could not be the share 1 - p that goes
+  // need no slice.
+  __device__ Head top_p_cut(const Head& h, float p) {
+    for (int b = threadIdx.x; b < kSlices; b += kThreads) sm.slice[b] = 0;
+    __syncthreads();
+    const float far = log2f((float)pieces.vocab / fmaxf(1.f - p, 5e-8f)) + 0.01f;
+    const int last = min(kSlices - 1, (int)(far * kPerPower) + 1);
+    u64 s = 0;
+    each([&](float x, int i) {
+      if (!kept(h, key_of(x), i)) return;
+      const u64 w = weight(row, sm.table, x);
+      s += w;
+      const int b = slice_of(row, x);
+      if (b <= last) atomicAdd(&sm.slice[b], (uint32_t)(w >> slice_shift(b)));
+    });
+    s = block_sum(s);
+    if (threadIdx.x == 0) sm.sum = s;
+    cluster_sync();
+    u64 all = 0;
+    for (unsigned c = 0; c < ctas; ++c) {
+      const uint32_t a = peer_addr(&sm.sum, c);
+      all += (u64)peer_load(a) | (u64)peer_load(a + 4) << 32;
+    }
+    for (int b = threadIdx.x; b < kSlices; b += kThreads) {
+      u64 t = 0;
+      for (unsigned c = 0; c < ctas; ++c) t += peer_load(peer_addr(&sm.slice[b], c));
+      sm.slice_total[b] = t << slice_shift(b);
+    }
+    cluster_sync();
+    const u64 target = max(1ull, min((u64)ceil(fmax((double)p, 0.0) * (double)all), all));
+    if (threadIdx.x < 32) {
+      constexpr int per = kSlices / 32;
+      const int lane = threadIdx.x;
+      u64 own = 0;
+      for (int b = 0; b < per; ++b) own += sm.slice_total[lane * per + b];
+      u64 inc = own;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const u64 y = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += y;
+      }
+      // First slice whose running total, from above, or from below, reaches the target.
+      u64 before = inc - own;
+      int lo = kSlices, hi = kSlices;
+      for (int b = lane * per; b < (lane + 1) * per; ++b) {
+        before += sm.slice_total[b];
+        if (lo == kSlices && before + (before >> 10) >= target) lo = b;
+        if (hi == kSlices && before >= target) hi = b;
+      }
+      lo = (int)__reduce_min_sync(0xffffffffu, (unsigned)lo);
+      hi = (int)__reduce_min_sync(0xffffffffu, (unsigned)hi);
+      if (lane == 0) {
+        sm.window[0] = min(lo, last);
+        sm.window[1] = min(hi, last);
+      }
+    }
+    __syncthreads();
+    const int lo = sm.window[0], hi = sm.window[1];
+    u64 above = 0;
+    const int n = gather([&](float x, int i) {
+      if (!kept(h, key_of(x), i)) return false;
+      const int b = slice_of(row, x);
+      if (b < lo) above += weight(row, sm.table, x);
+      return b >= lo && b <= hi;
+    });
+    above = block_sum(above);
+    if (threadIdx.x == 0) sm.sum = above;
+    cluster_sync();
+    above = 0;
+    for (unsigned c = 0; c < ctas; ++c) {
+      const uint32_t a = peer_addr(&sm.sum, c);
+      above += (u64)peer_load(a) | (u64)peer_load(a + 4) << 32;
+    }
+    cluster_sync();
+    if (n > kCap || above >= target) return cut(h, -1, true, target);   // (a run of equal weights)
+    Head to = h;
+    if (rank == 0) to = cut(h, n, true, target - above);
+    return share(to);
   }
   __device__ static float key_value(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
 
@@ -313,6 +523,17 @@ struct RowCtas {
   }
 };
 
+// The token drawn is the first at which the kept mass passes this.
+__device__ __forceinline__ u64 draw_at(float u, u64 total) {
+  const u64 t = u > 0.f ? (u64)fmin((double)u * (double)total, 9e18) : 0;
+  return min(t, total - 1);
+}
+// ln(w / total)
+__device__ __forceinline__ float share_of(float x, float m, float temperature, u64 total) {
+  const double y = x == m ? 0.0 : ((double)x - (double)m) / (double)temperature;
+  return (float)(y - log((double)total * 0x1p-44));
+}
+
 template <typename T>
 __global__ void __launch_bounds__(kThreads) k_sample(const __grid_constant__ Job job) {
   pdl_wait();
@@ -340,6 +561,7 @@ __global__ void __launch_bounds__(kThreads) k_sample(const __grid_constant__ Job
       at = v;
     }
   }
+  const uint32_t own_key = key_of(m);
 #pragma unroll
   for (int o = 16; o; o >>= 1) {
     const float y = __shfl_xor_sync(0xffffffffu, m, o);
@@ -399,20 +621,48 @@ __global__ void __launch_bounds__(kThreads) k_sample(const __grid_constant__ Job
   row.cl = (float)(c - (double)row.ch);
   RowCtas<T> ctx{sm, pieces, row, rank, ctas};
   Head head = {0u, 0x7fffffff};
-  if (top_k > 0 && top_k < job.vocab) head = ctx.cut(head, false, (u64)top_k);
+  Head least = head;  // min-p's
   if (min_p > 0.f) {
     // w >= min_p where x >= max + T ln(min_p): the least fp32 value that is.
-    const double least = (double)m + (double)temperature * log(fmin((double)min_p, 1.0));
-    float f = (float)least;
-    if ((double)f < least) f = nextafterf(f, INFINITY);
-    const uint32_t k = key_of(f);
-    if (k > head.k) head = {k, 0x7fffffff};
+    const double from = (double)m + (double)temperature * log(fmin((double)min_p, 1.0));
+    float f = (float)from;
+    if ((double)f < from) f = nextafterf(f, INFINITY);
+    least.k = key_of(f);
+    if (least.k > 0) {  // x >= f: key > key(f) - 1
+      --least.k;
+      least.i = -1;
+    }
   }
-  if (top_p < 1.f) {
-    const u64 all = ctx.sum([&](float x, int i) { return kept(head, key_of(x), i) ? weight(row, sm.table, x) : 0; });
-    const u64 target = (u64)ceil(fmax((double)top_p, 0.0) * (double)all);
-    head = ctx.cut(head, true, max(1ull, min(target, all)));
+  const bool by_k = top_k > 0 && top_k < job.vocab;
+  if (by_k && top_k <= kThreads) {
+    // The few tokens that can be among the first k, in one list.
+    const uint32_t bound = ctx.bound_of_top(top_k, own_key);
+    const int n = ctx.gather([&](float x, int i) { return key_of(x) >= bound && kept(least, key_of(x), i); });
+    if (n <= kCap) {
+      if (rank != 0) return;
+      if (n > top_k) head = ctx.cut(head, n, false, (u64)top_k);
+      u64 total = 0;
+      ctx.each_listed(n, [&](float x, int i) { total += kept(head, key_of(x), i) ? weight(row, sm.table, x) : 0; });
+      total = ctx.block_sum(total);
+      if (top_p < 1.f) {
+        const u64 target = (u64)ceil(fmax((double)top_p, 0.0) * (double)total);
+        head = ctx.cut(head, n, true, max(1ull, min(target, total)));
+        total = 0;
+        ctx.each_listed(n, [&](float x, int i) { total += kept(head, key_of(x), i) ? weight(row, sm.table, x) : 0; });
+        total = ctx.block_sum(total);
+      }
+      const int token = ctx.by_index(n, true, draw_at(job.u[r], total) + 1, [&](float x, int i) { return kept(head, key_of(x), i); });
+      if (tid == 0) job.token[r] = token;
+      if (job.logprob)
+        ctx.each_listed(n, [&](float x, int i) {
+          if (i == token) job.logprob[r] = share_of(x, m, temperature, total);
+        });
+      return;
+    }
   }
+  if (by_k) head = ctx.cut(head, -1, false, (u64)top_k);
+  if (least.k > head.k || (least.k == head.k && least.i < head.i)) head = least;
+  if (top_p < 1.f) head = ctx.top_p_cut(head, top_p);
   // The kept tokens' mass by runs of 32 pieces, to the first CTA.
   const int runs = (pieces.count + 31) / 32;
   for (int g = (int)rank * kWarps + warp; g < runs; g += (int)ctas * kWarps) {
@@ -440,9 +690,7 @@ __global__ void __launch_bounds__(kThreads) k_sample(const __grid_constant__ Job
     if (lane >= o) inc += y;
   }
   const u64 total = __shfl_sync(0xffffffffu, inc, 31);
-  const double u = job.u[r];
-  u64 target = u > 0 ? (u64)fmin(u * (double)total, 9e18) : 0;
-  target = min(target, total - 1);
+  const u64 target = draw_at(job.u[r], total);
   const int l = __ffs(__ballot_sync(0xffffffffu, inc > target)) - 1;
   int run = l * per;
   u64 before = __shfl_sync(0xffffffffu, inc - own, l);
@@ -473,10 +721,7 @@ __global__ void __launch_bounds__(kThreads) k_sample(const __grid_constant__ Job
     if (!found && sum > target) {
       found = true;
       job.token[r] = v * N - pieces.off + e;
-      if (job.logprob) {
-        const double y = x[e] == m ? 0.0 : ((double)x[e] - (double)m) / (double)temperature;
-        job.logprob[r] = (float)(y - log((double)total * 0x1p-44));
-      }
+      if (job.logprob) job.logprob[r] = share_of(x[e], m, temperature, total);
     }
   }
 }
@@ -500,7 +745,7 @@ extern "C" gb_status gb_sample(const gb_sample_args* a, gb_stream_t stream) {
     return GB_ERR_CUDA;
   // CTAs a row: as many as keep the GPU's SMs busy, and at least a few pieces for each thread.
   int cluster = 1;
-  while (cluster < kMaxCluster && (long long)a->rows * cluster * 2 <= 2ll * sms && a->vocab / (cluster * 2) >= kThreads * 8) cluster *= 2;
+  while (cluster < kMaxCluster && (long long)a->rows * cluster * 2 <= 2ll * sms && a->vocab / (cluster * 2) >= kThreads * 4) cluster *= 2;
   if ((long long)a->rows * cluster > 0x7fffffffll) return GB_ERR_TOO_LARGE;
   Job job = {a->logits, a->row_stride, a->rows, a->vocab, cluster, a->u, a->temperature, a->top_p, a->min_p, a->top_k,
              a->all_temperature, a->all_top_p, a->all_min_p, a->all_top_k, a->token, a->logprob};
