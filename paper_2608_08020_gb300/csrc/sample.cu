@@ -26,15 +26,16 @@ constexpr int kUnit = 44;               // a weight of one is 2^44
 constexpr int kBins = 256, kDigits = 4, kDigitBits = 12;
 constexpr int kMaxCluster = 8;
 constexpr float kFar = 46.f;            // weights of 2^-46 and less count as none
-constexpr int kCap = 4096;              // tokens of a list
+constexpr int kCap = 4096;              // tokens of the first CTA's list, in which a row is decided
+constexpr int kRanked = 256;            // lists up to this long are ranked by comparing every two entries
 constexpr int kSlices = 1024;           // of the weights' exponents, 22 to a power of two
-constexpr float kPerPower = 22.f;
+constexpr int kPerPower = 22;
 static_assert(kFar * kPerPower < kSlices, "every weight has a slice");
 typedef unsigned long long u64;
 
-// 2^(-j/256) in units of 2^-44: the power series of exp in 64 bits, as the compiler evaluates it.
+// 2^(-j/256) in units of 2^-31: the power series of exp in 64 bits, as the compiler evaluates it.
 struct PowerTable {
-  u64 t[kBins];
+  uint32_t t[kBins];
   constexpr PowerTable() : t() {
     for (int j = 0; j < kBins; ++j) {
       const double x = -0.69314718055994530942 * j / kBins;
@@ -43,7 +44,7 @@ struct PowerTable {
         sum += term;
         term *= x / n;
       }
-      t[j] = (u64)(sum * (double)(1ull << kUnit) + 0.5);
+      t[j] = (uint32_t)(sum * (double)(1u << 31) + 0.5);
     }
   }
 };
@@ -75,10 +76,20 @@ __device__ __forceinline__ uint32_t peer_addr(const void* p, unsigned rank) {
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
   return a;
 }
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ int peer_add(uint32_t a, int n) {
+  int x;
+  asm volatile("atom.shared::cluster.add.u32 %0, [%1], %2;" : "=r"(x) : "r"(a), "r"(n) : "memory");
+  return x;
+}
 __device__ __forceinline__ uint32_t peer_load(uint32_t a) {
   uint32_t x;
   asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(x) : "r"(a) : "memory");
   return x;
+}
+__device__ __forceinline__ void peer_store32(uint32_t a, uint32_t x) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(a), "r"(x) : "memory");
 }
 __device__ __forceinline__ void peer_store64(uint32_t a, u64 x) {
   asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(a), "l"(x) : "memory");
@@ -96,35 +107,49 @@ struct Row {
   float max, ch, cl;  // log2(e) / T in two terms
 };
 
-// exp((x - max) / T) in units of 2^-44.  y = (max - x) log2(e) / T to 2^-40 of itself or better; 2^-y is the table's
-// 2^(-j/256) times 1 + p, with p the third-order series of 2^-r, |r| <= 2^-9.
-__device__ __forceinline__ u64 weight(const Row& row, const u64* table, float x) {
-  if (!(x > -INFINITY)) return 0;
-  if (x == row.max) return 1ull << kUnit;
+// y = (max - x) log2(e) / T to fp32, which alone says a token's slice.
+__device__ __forceinline__ float exponent(const Row& row, float x) { return __fmul_rn(__fsub_rn(row.max, x), row.ch); }
+
+// exp((x - max) / T) = m 2^-31 2^-n with m in (2^30, 2^31], for a logit with exponent() below kFar; j = floor(256 y), n = j >> 8.
+// y is taken to 2^-40 of itself or better; m is the table's 2^(-(j & 255)/256) less its share 1 - 2^-r, 0 <= r < 2^-8, to the
+// third order.
+struct Weight {
+  uint32_t m;
+  int j;
+};
+__device__ __forceinline__ Weight weight_of(const Row& row, const uint32_t* table, float x) {
   const float d = __fsub_rn(row.max, x), b = __fsub_rn(d, row.max);
   const float e = __fadd_rn(__fsub_rn(row.max, __fsub_rn(d, b)), __fsub_rn(-x, b));
   const float yh = __fmul_rn(d, row.ch);
-  if (!(yh < kFar)) return 0;
   const float yl = __fadd_rn(__fmaf_rn(d, row.ch, -yh), __fmaf_rn(d, row.cl, __fmul_rn(e, row.ch)));
-  const float z = __fadd_rn(yh, 49152.f);                  // rounds to multiples of 2^-8
+  const float z = __fadd_rd(yh, 49152.f);                  // down to a multiple of 2^-8
   const int j = __float_as_int(z) - __float_as_int(49152.f);
   const float r = __fadd_rn(__fsub_rn(yh, __fsub_rn(z, 49152.f)), yl);
   constexpr float kLn2 = 0.69314718055994530942f;
-  const float p = r * __fmaf_rn(r, __fmaf_rn(r, -kLn2 * kLn2 * kLn2 / 6, kLn2 * kLn2 / 2), -kLn2);
-  const u64 t = table[j & 255];
-  const u64 w = t + (u64)(((long long)(int)(t >> 14) * __float2int_rn(p * 0x1p40f)) >> 26);
-  const int n = j >> 8;
-  return (w + ((1ull << n) >> 1)) >> n;
+  const float q = r * __fmaf_rn(r, __fmaf_rn(r, kLn2 * kLn2 * kLn2 / 6, -kLn2 * kLn2 / 2), kLn2);
+  const uint32_t t = table[j & 255];
+  const int less = __float2int_rn(q * 0x1p32f);            // (below 0 where yl pulls y under its multiple)
+  return {t - __umulhi(t, (uint32_t)less) + (t & (uint32_t)(less >> 31)), j};
+}
+// The same in units of 2^-44.
+__device__ __forceinline__ u64 mass_of(const Weight& w) {
+  const int n = w.j >> 8, sh = max(n - (kUnit - 31), 0);
+  const uint32_t m = (w.m + ((1u << sh) >> 1)) >> sh;      // (sh <= 32: a shift by 32 gives 0 on the GPU)
+  return (u64)m << max(kUnit - 31 - n, 0);
+}
+__device__ __forceinline__ u64 weight(const Row& row, const uint32_t* table, float x) {
+  if (!(x > -INFINITY)) return 0;
+  if (x == row.max) return 1ull << kUnit;
+  return exponent(row, x) < kFar ? mass_of(weight_of(row, table, x)) : 0;
 }
 
-// The slice of a weight: y in steps of 1 / 22 (in a lower slice the weight is larger).
-__device__ __forceinline__ int slice_of(const Row& row, float x) {
-  if (x == row.max) return 0;
-  const float y = __fmul_rn(__fsub_rn(row.max, x), row.ch);
-  return y < kFar ? (int)(y * kPerPower) : kSlices - 1;
-}
-// Masses are summed in units of 2^shift by slice: 12 bits of a weight's 45.
-__device__ __forceinline__ int slice_shift(int b) { return max(0, 32 - b / (int)kPerPower); }
+// Slices of the exponent, kPerPower to a power of two: floor(kPerPower j / 256).  Their masses are summed in units of
+// 2^slice_shift, 12 bits of a weight.
+__device__ __forceinline__ int slice_of(const Weight& w) { return w.j * kPerPower >> 8; }
+__device__ __forceinline__ uint32_t slice_part(const Weight& w) { return w.m >> max(19, (w.j >> 8) - (kUnit - 31)); }
+__device__ __forceinline__ int slice_shift(int b) { return max(0, 32 - b / kPerPower); }
+// The exponent that slice b begins at: tokens with exponent() below it are in the slices before.
+__device__ __forceinline__ float slice_begin(int b) { return (float)((b * 256 + kPerPower - 1) / kPerPower) * (1.f / 256); }
 
 __device__ __forceinline__ float value(const float* p) { return *p; }
 __device__ __forceinline__ float value(const __nv_bfloat16* p) { return __bfloat162float(*p); }
@@ -172,26 +197,6 @@ struct Entry {
   int i;
 };
 
-struct Smem {
-  u64 table[kBins];
-  Entry list[kCap];                      // the first CTA's holds all
-  uint32_t slice[kSlices];               // masses by slice, see top_p_cut
-  u64 slice_total[kSlices];
-  int listed, window[2];
-  uint32_t head_k;
-  int head_i;
-  uint32_t hist[1 + kDigits][kBins];     // counts, then the masses' digits
-  u64 total[kBins];
-  float red[kWarps];
-  int redi[kWarps];
-  u64 red64[kWarps];
-  u64 before;                            // of the bin chosen
-  int bin;
-  float max;                             // this CTA's, read by its peers
-  int arg;
-  u64 sum;
-};
-
 // What is kept: the tokens with key > k, and those with key = k and index <= i.
 struct Head {
   uint32_t k;
@@ -199,9 +204,110 @@ struct Head {
 };
 __device__ __forceinline__ bool kept(const Head& h, uint32_t key, int i) { return key > h.k || (key == h.k && i <= h.i); }
 
+struct Top {
+  float max;
+  int arg;
+  uint32_t bound;
+  uint32_t pad;
+};
+
+struct Smem {
+  uint32_t table[kBins];
+  Entry list[kCap];
+  union {
+    u64 weights[kCap];                   // of the list, once it is whole
+    u64 runs[(kMaxVocab / 4 + 2 + 31) / 32];  // the first CTA's: mass of each run of 32 pieces
+  };
+  float queue[kWarps][32 + 32 * 8];      // logits that wait for their weights
+  u64 order[kRanked];                    // a short list's entries: (key from above, index)
+  uint32_t slice[kSlices];               // masses by slice, see top_p_list
+  u64 slice_total[kSlices];
+  uint32_t hist[1 + kDigits][kBins];     // counts, then the masses' digits
+  u64 total[kBins];
+  Top tops[kMaxCluster];                 // of the row's CTAs
+  Head head;
+  double ahead;                          // T ln(min_p)
+  float least;
+  int listed, token;
+  int lo, hi, many;                      // top-p: the slices that its cut can lie in, whether it keeps more than a list holds
+  float red[kWarps];
+  int redi[kWarps];
+  u64 red64[kWarps];
+  u64 before;                            // of the bin chosen
+  int bin;
+  u64 sum;
+};
+
+// (The GPU's 64-bit floating point runs at a sixtieth of its 32-bit rate, so what every thread needs is in whole numbers.)
+// floor(f n) of 0 <= f < 1, exactly, and whether f n is more.
+__device__ __forceinline__ bool product(float f, u64 n, u64* below) {
+  const uint32_t b = __float_as_uint(f);
+  const int e = (int)(b >> 23), shift = 150 - (e ? e : 1);   // f = m 2^-shift
+  const u64 m = e ? (b & 0x7fffffu) | 0x800000u : b & 0x7fffffu;
+  const u64 lo = n * m, hi = __umul64hi(n, m);
+  if (shift >= 128) {
+    *below = 0;
+    return (lo | hi) != 0;
+  }
+  if (shift >= 64) {
+    *below = hi >> (shift - 64);
+    return lo != 0 || (hi & ((1ull << (shift - 64)) - 1)) != 0;
+  }
+  *below = (lo >> shift) | (hi << (64 - shift));
+  return (lo & ((1ull << shift) - 1)) != 0;
+}
+// The token drawn is the first at which the kept mass passes this.
+__device__ __forceinline__ u64 draw_at(float u, u64 total) {
+  if (!(u > 0.f)) return 0;
+  if (u >= 1.f) return total - 1;
+  u64 t;
+  product(u, total, &t);
+  return t;
+}
+// ln(w / total)
+__device__ __forceinline__ float log_share(float x, float m, float temperature, u64 total) {
+  const double y = x == m ? 0.0 : ((double)x - (double)m) / (double)temperature;
+  return (float)(y - log((double)total * 0x1p-44));
+}
+
+// A warp's queue of values.
+struct Queue {
+  float* at;
+  int n;
+  // Elements e of x where bit e of `mine` is set, lane after lane.
+  template <int N>
+  __device__ __forceinline__ void put(const float (&x)[N], unsigned mine) {
+    const int lane = threadIdx.x & 31, own = __popc(mine);
+    int inc = own;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += y;
+    }
+    int to = n + inc - own;
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if (mine >> e & 1) at[to++] = x[e];
+    n += __shfl_sync(0xffffffffu, inc, 31);
+    __syncwarp();
+  }
+  // f of the last `some` <= 32.
+  template <class F>
+  __device__ __forceinline__ void take(int some, F f) {
+    const int lane = threadIdx.x & 31;
+    if (lane < some) f(at[n - some + lane]);
+    n -= some;
+    __syncwarp();
+  }
+};
+
+// The kernel's shared memory, by its name: through a pointer that a function was given, the accesses of a function that is not
+// inlined are generic ones, whose atomics are ten times slower.
+extern __shared__ __align__(16) unsigned char sample_smem[];
+#define sm (*reinterpret_cast<Smem*>(sample_smem))
+
 template <typename T>
 struct RowCtas {
-  Smem& sm;
   const Pieces<T> pieces;
   const Row row;
   const unsigned rank, ctas;
@@ -307,6 +413,7 @@ struct RowCtas {
       target -= sm.before;
       __syncthreads();
     }
+    if (at > top || top - at < h.k) return h;   // (the total stays below the target: all of the head)
     // The key is chosen; of its tokens, all of one weight, the first ones by index.
     Head to = {top - at, h.k == top - at ? h.i : 0x7fffffff};
     u64 most = target;
@@ -346,172 +453,219 @@ struct RowCtas {
     return t;
   }
 
-  // Puts the tokens that in(x, i) says into this CTA's list; then the first CTA's holds all of the row's (in no order).
-  // Returns how many there are: lists of more than kCap hold no more, and are none.
+  // Room for the warp's `mine` entries each in the first CTA's list.
+  __device__ __forceinline__ int reserve(int mine) const {
+    const int lane = threadIdx.x & 31;
+    int inc = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += y;
+    }
+    int at = 0;
+    if (lane == 31) at = peer_add(peer_addr(&sm.listed, 0), inc);
+    return __shfl_sync(0xffffffffu, at, 31) + inc - mine;
+  }
+  __device__ __forceinline__ void put(int at, float x, int i) const {
+    if (at < kCap) peer_store64(peer_addr(&sm.list[at], 0), (u64)__float_as_uint(x) | (u64)(unsigned)i << 32);
+  }
+
+  // The row's tokens that in(x, i) says into the first CTA's list, in no order.
   template <class In>
-  __device__ int gather(In in) {
-    if (threadIdx.x == 0) sm.listed = 0;
-    __syncthreads();
+  __device__ __forceinline__ void gather(In in) const {
     const int step = (int)(ctas * kThreads);
+#pragma unroll 2
     for (int v0 = (int)(rank * kThreads) + (int)(threadIdx.x & ~31u); v0 < pieces.count; v0 += step) {
       const int v = v0 + (int)(threadIdx.x & 31);
       float x[N];
       pieces.load(v, x);
       unsigned mine = 0;
 #pragma unroll
+      for (int e = 0; e < N; ++e) mine |= x[e] > -INFINITY && in(x[e], v * N - pieces.off + e) ? 1u << e : 0u;
+      if (!__any_sync(0xffffffffu, mine != 0)) continue;
+      int at = reserve(__popc(mine));
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (mine >> e & 1) put(at++, x[e], v * N - pieces.off + e);
+    }
+  }
+
+  // Sums the weights of the tokens with x >= least, and those that top-p can keep by slices of their exponent, to 12 bits
+  // each.  Tokens below 2^-24 (`far`) are only summed, from the 22 bits of exp2f.  The others' weights take 60 instructions, so a warp puts
+  // their logits in a queue of its own and takes 32 at a time from it: as they lie in the row, most turns of a warp would have
+  // only a few.  Tokens so light that all of them together could not be the share 1 - p that goes need no slice (`can`).
+  __device__ u64 slice_masses(float p, float least, float own_max) {
+    for (int b = threadIdx.x; b < kSlices; b += kThreads) sm.slice[b] = 0;
+    // From below, log2 of all's mass: that of the threads' largest tokens.  (Each CTA has bounds of its own.)
+    float some = own_max >= least ? exp2f(-exponent(row, own_max)) : 0.f;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) some += __shfl_xor_sync(0xffffffffu, some, o);
+    if ((threadIdx.x & 31) == 0) sm.red[threadIdx.x >> 5] = some;
+    __syncthreads();
+    some = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) some += sm.red[w];
+    const float there = log2f(fmaxf(some, 1.f)) - 0.01f;
+    const float can = log2f((float)pieces.vocab / fmaxf(1.f - p, 5e-8f)) + 0.1f;
+    const float far = fminf(fmaxf(can, 24.f), kFar);   // (the same for every CTA, and however many there are)
+    const int reach = min((int)(fmaxf(can - there, 0.1f) * (float)kPerPower) + 1, kSlices - 1);
+    uint32_t light = 0;   // of 1024 tokens at most
+    u64 s = 0;
+    const int step = (int)(ctas * kThreads), lane = threadIdx.x & 31;
+    Queue queue{sm.queue[threadIdx.x >> 5], 0};
+    auto add = [&](float x) {
+      const Weight w = weight_of(row, sm.table, x);
+      s += mass_of(w);
+      const int b = slice_of(w);
+      if (b <= reach) atomicAdd(&sm.slice[b], slice_part(w));
+    };
+#pragma unroll 2
+    for (int v0 = (int)(rank * kThreads) + (int)(threadIdx.x & ~31u); v0 < pieces.count; v0 += step) {
+      float x[N];
+      pieces.load(v0 + lane, x);
+      unsigned mine = 0;
+#pragma unroll
       for (int e = 0; e < N; ++e) {
-        const int i = v * N - pieces.off + e;
-        if (v < pieces.count && i >= 0 && i < pieces.vocab && in(x[e], i)) mine |= 1u << e;
+        const float y = exponent(row, x[e]);
+        const bool in = x[e] >= least;
+        if (in && y < far) mine |= 1u << e;
+        else if (in && y < kFar) light += __float_as_uint(exp2f(-y) + 0x1p-21f) - __float_as_uint(0x1p-21f);  // 2^-44 each
       }
       if (!__any_sync(0xffffffffu, mine != 0)) continue;
-      if (mine) {
-        int at = atomicAdd(&sm.listed, __popc(mine));
-#pragma unroll
-        for (int e = 0; e < N; ++e)
-          if (mine >> e & 1) {
-            if (at < kCap) sm.list[at] = {x[e], v * N - pieces.off + e};
-            ++at;
-          }
-      }
+      queue.put(x, mine);
+      while (queue.n >= 32) queue.take(32, add);
     }
-    cluster_sync();
-    int n = 0, before = 0;
-    for (unsigned c = 0; c < ctas; ++c) {
-      const int own = (int)peer_load(peer_addr(&sm.listed, c));
-      if (c < rank) before += own;
-      n += own;
-    }
-    if (n <= kCap && rank > 0) {
-      const int own = sm.listed;
-      for (int j = threadIdx.x; j < own; j += kThreads)
-        peer_store64(peer_addr(&sm.list[before + j], 0), (u64)__float_as_uint(sm.list[j].x) | (u64)(unsigned)sm.list[j].i << 32);
-    }
-    cluster_sync();
-    return n;
+    queue.take(queue.n, add);
+    return s + light;
   }
 
-  // The head that the first CTA has found, to all.
-  __device__ Head share(const Head& h) {
-    if (rank == 0 && threadIdx.x == 0) {
-      sm.head_k = h.k;
-      sm.head_i = h.i;
-    }
-    cluster_sync();
-    const Head to = {peer_load(peer_addr(&sm.head_k, 0)), (int)peer_load(peer_addr(&sm.head_i, 0))};
-    cluster_sync();
-    return to;
-  }
-
-  // The k-th largest of the threads' largest tokens, of k <= kThreads: at least k of the row's tokens are as large.
-  __device__ uint32_t bound_of_top(int k, uint32_t key) {
-    uint32_t at = 0;  // the largest value that at least k keys reach
-    for (int b = 31; b >= 0; --b)
-      if (__syncthreads_count(key >= (at | 1u << b)) >= k) at |= 1u << b;
-    if (threadIdx.x == 0) sm.head_k = at;
-    cluster_sync();
-    for (unsigned c = 0; c < ctas; ++c) at = max(at, peer_load(peer_addr(&sm.head_k, c)));
-    cluster_sync();
-    return at;
-  }
-
-  // Cut the head where its mass reaches the share p of its total.  One pass sums the weights exactly, and by slices of their
-  // exponent to 12 bits each: the running total of the slices is then known from below, and from above within 2^-10 of itself,
-  // which leaves a slice or two in which the cut must lie.  A second pass sums what lies before them exactly and lists their
-  // tokens, among which the cut is found.  Tokens so light that all of them together could not be the share 1 - p that goes
-  // need no slice.
-  __device__ Head top_p_cut(const Head& h, float p) {
-    for (int b = threadIdx.x; b < kSlices; b += kThreads) sm.slice[b] = 0;
-    __syncthreads();
-    const float far = log2f((float)pieces.vocab / fmaxf(1.f - p, 5e-8f)) + 0.01f;
-    const int last = min(kSlices - 1, (int)(far * kPerPower) + 1);
-    u64 s = 0;
-    each([&](float x, int i) {
-      if (!kept(h, key_of(x), i)) return;
-      const u64 w = weight(row, sm.table, x);
-      s += w;
-      const int b = slice_of(row, x);
-      if (b <= last) atomicAdd(&sm.slice[b], (uint32_t)(w >> slice_shift(b)));
-    });
-    s = block_sum(s);
+  // What top-p keeps of the tokens with x >= least.  The slices' running total is short of the true one by 2^-11 of itself at
+  // most, so the cut lies in a slice from the one in which it reaches p of all with 2^-10 on top (sm.lo) to the one in which it
+  // does as it is (sm.hi).  Where few tokens lie that far they go into the first CTA's list, and all of their mass to *all: true.
+  __device__ bool top_p_list(float p, float least, float own_max, u64* all) {
+    u64 s = block_sum(slice_masses(p, least, own_max));
     if (threadIdx.x == 0) sm.sum = s;
     cluster_sync();
-    u64 all = 0;
-    for (unsigned c = 0; c < ctas; ++c) {
-      const uint32_t a = peer_addr(&sm.sum, c);
-      all += (u64)peer_load(a) | (u64)peer_load(a + 4) << 32;
-    }
-    for (int b = threadIdx.x; b < kSlices; b += kThreads) {
+    if (rank == 0) {
       u64 t = 0;
-      for (unsigned c = 0; c < ctas; ++c) t += peer_load(peer_addr(&sm.slice[b], c));
-      sm.slice_total[b] = t << slice_shift(b);
-    }
-    cluster_sync();
-    const u64 target = max(1ull, min((u64)ceil(fmax((double)p, 0.0) * (double)all), all));
-    if (threadIdx.x < 32) {
-      constexpr int per = kSlices / 32;
-      const int lane = threadIdx.x;
-      u64 own = 0;
-      for (int b = 0; b < per; ++b) own += sm.slice_total[lane * per + b];
-      u64 inc = own;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const u64 y = __shfl_up_sync(0xffffffffu, inc, o);
-        if (lane >= o) inc += y;
+      for (unsigned c = 0; c < ctas; ++c) {
+        const uint32_t a = peer_addr(&sm.sum, c);
+        t += (u64)peer_load(a) | (u64)peer_load(a + 4) << 32;
       }
-      // First slice whose running total, from above, or from below, reaches the target.
-      u64 before = inc - own;
-      int lo = kSlices, hi = kSlices;
-      for (int b = lane * per; b < (lane + 1) * per; ++b) {
-        before += sm.slice_total[b];
-        if (lo == kSlices && before + (before >> 10) >= target) lo = b;
-        if (hi == kSlices && before >= target) hi = b;
-      }
-      lo = (int)__reduce_min_sync(0xffffffffu, (unsigned)lo);
-      hi = (int)__reduce_min_sync(0xffffffffu, (unsigned)hi);
-      if (lane == 0) {
-        sm.window[0] = min(lo, last);
-        sm.window[1] = min(hi, last);
+      *all = t;
+      slice_totals();
+      if (threadIdx.x < 32) {
+        const int lane = threadIdx.x, lo = slice_reaching(share(p, t), 10), hi = slice_reaching(share(p, t), 0);
+        // At least so many tokens: a slice's mass over the most that one of it weighs.
+        u64 least_of = 0;
+        for (int b = lane; b <= hi; b += 32) least_of += sm.slice_total[b] >> max(kUnit - b / kPerPower, 0);
+        const unsigned count = __reduce_add_sync(0xffffffffu, (unsigned)least_of);
+        if ((unsigned)lane < ctas) {
+          peer_store32(peer_addr(&sm.lo, lane), lo);
+          peer_store32(peer_addr(&sm.hi, lane), hi);
+          peer_store32(peer_addr(&sm.many, lane), count > kCap);
+        }
       }
     }
-    __syncthreads();
-    const int lo = sm.window[0], hi = sm.window[1];
-    u64 above = 0;
-    const int n = gather([&](float x, int i) {
-      if (!kept(h, key_of(x), i)) return false;
-      const int b = slice_of(row, x);
-      if (b < lo) above += weight(row, sm.table, x);
-      return b >= lo && b <= hi;
-    });
-    above = block_sum(above);
-    if (threadIdx.x == 0) sm.sum = above;
     cluster_sync();
-    above = 0;
-    for (unsigned c = 0; c < ctas; ++c) {
-      const uint32_t a = peer_addr(&sm.sum, c);
-      above += (u64)peer_load(a) | (u64)peer_load(a + 4) << 32;
-    }
-    cluster_sync();
-    if (n > kCap || above >= target) return cut(h, -1, true, target);   // (a run of equal weights)
-    Head to = h;
-    if (rank == 0) to = cut(h, n, true, target - above);
-    return share(to);
+    if (sm.many) return false;
+    const float end = slice_begin(sm.hi + 1);
+    gather([&](float x, int) { return x >= least && exponent(row, x) < end; });
+    return true;
   }
-  __device__ static float key_value(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
 
-  // The sum of f over the row's tokens, in every thread.
-  template <class F>
-  __device__ u64 sum(F f) {
-    u64 s = 0;
-    each([&](float x, int i) { s += f(x, i); });
+  // The cut where that list would be too long: a pass that sums what lies before slice sm.lo, by runs of 32 pieces, and lists
+  // the slices up to sm.hi, in which the first CTA finds it.  (all: as from top_p_list; from: the head of
+  // the tokens with x >= least.)  It adds what the list keeps to the
+  // runs.  The other CTAs get no head; false where the list is too long even so (a long run of equal weights).
+  __device__ bool top_p_runs(float p, float least, const Head& from, u64 all, Head* head) {
+    if (threadIdx.x == 0) sm.listed = 0;
+    cluster_sync();
+    const float begin = slice_begin(sm.lo), end = slice_begin(sm.hi + 1);
+    const int runs = (pieces.count + 31) / 32, lane = threadIdx.x & 31;
+    Queue queue{sm.queue[threadIdx.x >> 5], 0};
+    for (int g = (int)rank * kWarps + (int)(threadIdx.x >> 5); g < runs; g += (int)ctas * kWarps) {
+      const int v = g * 32 + lane;
+      float x[N];
+      pieces.load(v, x);
+      unsigned above = 0, window = 0;
 #pragma unroll
-    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    if ((threadIdx.x & 31) == 0) sm.red64[threadIdx.x >> 5] = s;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      u64 t = 0;
-      for (int w = 0; w < kWarps; ++w) t += sm.red64[w];
-      sm.sum = t;
+      for (int e = 0; e < N; ++e) {
+        const float y = exponent(row, x[e]);
+        const bool in = x[e] >= least && y < end;
+        above |= in && y < begin ? 1u << e : 0u;
+        window |= in && y >= begin ? 1u << e : 0u;
+      }
+      u64 s = 0;
+      if (__any_sync(0xffffffffu, above != 0)) {
+        queue.put(x, above);
+        auto add = [&](float y) { s += mass_of(weight_of(row, sm.table, y)); };
+        while (queue.n > 0) queue.take(min(queue.n, 32), add);
+#pragma unroll
+        for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+      }
+      if (lane == 0) peer_store64(peer_addr(&sm.runs[g], 0), s);
+      if (__any_sync(0xffffffffu, window != 0)) {
+        int at = reserve(__popc(window));
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+          if (window >> e & 1) put(at++, x[e], v * N - pieces.off + e);
+      }
     }
+    cluster_sync();
+    const int n = (int)peer_load(peer_addr(&sm.listed, 0));
+    cluster_sync();
+    if (n > kCap) return false;
+    if (rank == 0) {
+      u64 s = 0;
+      for (int g = threadIdx.x; g < runs; g += kThreads) s += sm.runs[g];
+      s = block_sum(s);
+      const Head to = cut(from, n, true, share(p, all) - s);
+      each_listed(n, [&](float x, int i) {
+        if (kept(to, key_of(x), i)) atomicAdd(&sm.runs[(i + pieces.off) / (32 * N)], weight(row, sm.table, x));
+      });
+      __syncthreads();
+      *head = to;
+    }
+    return true;
+  }
+
+  // The row's masses by slice.
+  __device__ void slice_totals() {
+    for (int b = threadIdx.x; b < kSlices; b += kThreads) {
+      u64 m = 0;
+      for (unsigned c = 0; c < ctas; ++c) m += peer_load(peer_addr(&sm.slice[b], c));
+      sm.slice_total[b] = m << slice_shift(b);
+    }
+    __syncthreads();
+  }
+  // The first slice at which their running total, with 2^-over of itself on top (0: nothing), reaches the target; by a warp.
+  __device__ int slice_reaching(u64 target, int over) const {
+    constexpr int per = kSlices / 32;
+    const int lane = threadIdx.x & 31;
+    u64 own = 0;
+#pragma unroll 8
+    for (int b = 0; b < per; ++b) own += sm.slice_total[lane * per + b];
+    u64 inc = own;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const u64 y = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += y;
+    }
+    auto reaches = [&](u64 t) { return t + (over ? t >> over : 0) >= target; };
+    const unsigned past = __ballot_sync(0xffffffffu, reaches(inc));
+    int at = kSlices - 1;
+    if (past && lane == __ffs(past) - 1) {
+      u64 t = inc - own;
+      at = lane * per;
+      while (at < lane * per + per - 1 && !reaches(t + sm.slice_total[at])) t += sm.slice_total[at++];
+    }
+    return (int)__reduce_min_sync(0xffffffffu, (unsigned)at);
+  }
+
+  // The CTAs' sums added up.
+  __device__ u64 row_sum(u64 s) {
+    if (threadIdx.x == 0) sm.sum = s;
     cluster_sync();
     u64 t = 0;
     for (unsigned c = 0; c < ctas; ++c) {
@@ -521,35 +675,106 @@ struct RowCtas {
     cluster_sync();
     return t;
   }
+
+  // The mass at which top-p's head ends.
+  __device__ static u64 share(float p, u64 all) {
+    u64 below;
+    const bool more = product(fmaxf(p, 0.f), all, &below);
+    return max(1ull, min(below + (more ? 1 : 0), all));
+  }
+
+  // The token drawn, by the first CTA, whose list of n tokens holds every one that is kept: the first k of them (k < 1: all), of
+  // these top-p's head (p >= 1: all).  all: the mass that p is a share of, 0: that of the first k.  Every thread gets it, and the
+  // mass of what is kept.
+  __device__ int draw_listed(int n, int k, float p, u64 all, float u, u64* mass) {
+    if (n <= kRanked) {
+      // Every entry's rank and the mass before it, by comparing every two: some threads an entry.
+      for (int j = threadIdx.x; j < n; j += kThreads) {
+        const Entry e = sm.list[j];
+        sm.weights[j] = weight(row, sm.table, e.x);
+        sm.order[j] = (u64)~key_of(e.x) << 32 | (unsigned)e.i;
+      }
+      if (threadIdx.x == 0) sm.token = -1;
+      __syncthreads();
+      const int shift = n <= kRanked / 4 ? 3 : n <= kRanked / 2 ? 2 : 1, ways = 1 << shift;
+      const int j = threadIdx.x >> shift, way = threadIdx.x & (ways - 1);
+      const bool there = j < n, first = there && way == 0;
+      const u64 own = sm.order[there ? j : 0], w = there ? sm.weights[j] : 0;
+      int rank_in = 0;
+      u64 before = 0;
+#pragma unroll 4
+      for (int z = way; z < n; z += ways) {
+        const bool c = sm.order[z] < own;
+        const u64 wz = sm.weights[z];
+        rank_in += c ? 1 : 0;
+        before += c ? wz : 0;
+      }
+      for (int o = 1; o < ways; o <<= 1) {
+        rank_in += __shfl_xor_sync(0xffffffffu, rank_in, o);
+        before += __shfl_xor_sync(0xffffffffu, before, o);
+      }
+      bool in = there && (k < 1 || rank_in < k);
+      if (p < 1.f) {
+        if (all == 0) all = block_sum(in && first ? w : 0);
+        in = in && before < share(p, all);
+      }
+      const u64 total = block_sum(in && first ? w : 0);
+      if (first) sm.weights[j] = in ? w : 0;
+      __syncthreads();
+      const u64 at = draw_at(u, total);
+      u64 passed = 0;
+#pragma unroll 4
+      for (int z = way; z < n; z += ways) {
+        const u64 wz = sm.weights[z];
+        passed += (uint32_t)sm.order[z] < (uint32_t)own ? wz : 0;
+      }
+      for (int o = 1; o < ways; o <<= 1) passed += __shfl_xor_sync(0xffffffffu, passed, o);
+      if (in && first && passed <= at && at < passed + w) sm.token = (int)(uint32_t)own;
+      __syncthreads();
+      *mass = total;
+      return sm.token;
+    }
+    Head head = {0u, 0x7fffffff};
+    if (k > 0 && n > k) head = cut(head, n, false, (u64)k);
+    u64 total = listed_mass(n, head);
+    if (p < 1.f) {
+      head = cut(head, n, true, share(p, all ? all : total));
+      total = listed_mass(n, head);
+    }
+    *mass = total;
+    return by_index(n, true, draw_at(u, total) + 1, [&](float x, int i) { return kept(head, key_of(x), i); });
+  }
+  __device__ u64 listed_mass(int n, const Head& h) {
+    u64 s = 0;
+    each_listed(n, [&](float x, int i) { s += kept(h, key_of(x), i) ? weight(row, sm.table, x) : 0; });
+    return block_sum(s);
+  }
+  __device__ static float key_value(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
+
 };
 
-// The token drawn is the first at which the kept mass passes this.
-__device__ __forceinline__ u64 draw_at(float u, u64 total) {
-  const u64 t = u > 0.f ? (u64)fmin((double)u * (double)total, 9e18) : 0;
-  return min(t, total - 1);
-}
-// ln(w / total)
-__device__ __forceinline__ float share_of(float x, float m, float temperature, u64 total) {
-  const double y = x == m ? 0.0 : ((double)x - (double)m) / (double)temperature;
-  return (float)(y - log((double)total * 0x1p-44));
-}
-
 template <typename T>
-__global__ void __launch_bounds__(kThreads) k_sample(const __grid_constant__ Job job) {
+__global__ void __launch_bounds__(kThreads, 2) k_sample(const __grid_constant__ Job job) {
   pdl_wait();
   pdl_launch_dependents();
-  extern __shared__ __align__(16) unsigned char raw[];
-  Smem& sm = *reinterpret_cast<Smem*>(raw);
-  u64* chunk = reinterpret_cast<u64*>(raw + sizeof(Smem));  // the first CTA's: mass of each run of 32 pieces
   constexpr int N = Pieces<T>::N;
   const int r = (int)blockIdx.x / job.cluster, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const unsigned rank = cluster_rank(), ctas = (unsigned)job.cluster;
+  cluster_arrive();
   const Pieces<T> pieces(static_cast<const T*>(job.logits) + (size_t)r * job.stride, job.vocab);
+  const float temperature = job.temperature ? job.temperature[r] : job.all_temperature;
+  const int top_k = job.top_k ? job.top_k[r] : job.all_top_k;
+  const float top_p = job.top_p ? job.top_p[r] : job.all_top_p, min_p = job.min_p ? job.min_p[r] : job.all_min_p;
+  const bool by_k = top_k > 0 && top_k < job.vocab, greedy = !(temperature > 0.f) || top_k == 1;
   for (int j = tid; j < kBins; j += kThreads) sm.table[j] = kPowers.t[j];
+  if (tid == 0) sm.listed = 0;
+
+  if (min_p > 0.f && tid == kThreads - 1) sm.ahead = (double)temperature * log(fmin((double)min_p, 1.0));
 
   // The largest logit, and the piece that has it first.
   float m = -INFINITY;
   int at = 0x7fffffff;
+#pragma unroll 4
   for (int v = (int)(rank * kThreads + tid); v < pieces.count; v += (int)(ctas * kThreads)) {
     float x[N];
     pieces.load(v, x);
@@ -561,7 +786,15 @@ __global__ void __launch_bounds__(kThreads) k_sample(const __grid_constant__ Job
       at = v;
     }
   }
-  const uint32_t own_key = key_of(m);
+  // Where the first k tokens are asked for: a value that at least k of the threads' largest reach (to 14 bits of its key, a
+  // bit of it at a time).
+  uint32_t bound = 0;
+  if (by_k && !greedy && top_k <= kThreads) {
+    const uint32_t key = key_of(m);
+    for (int b = 31; b >= 18; --b)
+      if (__syncthreads_count(key >= (bound | 1u << b)) >= top_k) bound |= 1u << b;
+  }
+  const float own_max = m;
 #pragma unroll
   for (int o = 16; o; o >>= 1) {
     const float y = __shfl_xor_sync(0xffffffffu, m, o);
@@ -576,31 +809,37 @@ __global__ void __launch_bounds__(kThreads) k_sample(const __grid_constant__ Job
     sm.redi[warp] = at;
   }
   __syncthreads();
-  if (tid == 0) {
-    for (int w = 1; w < kWarps; ++w)
-      if (sm.red[w] > m || (sm.red[w] == m && sm.redi[w] < at)) {
-        m = sm.red[w];
-        at = sm.redi[w];
+  cluster_wait();  // every CTA of the row runs
+  if (warp == 0) {
+    m = lane < kWarps ? sm.red[lane] : -INFINITY;
+    at = lane < kWarps ? sm.redi[lane] : 0x7fffffff;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+      const float y = __shfl_xor_sync(0xffffffffu, m, o);
+      const int z = __shfl_xor_sync(0xffffffffu, at, o);
+      if (y > m || (y == m && z < at)) {
+        m = y;
+        at = z;
       }
-    sm.max = m;
-    sm.arg = at;
+    }
+    if ((unsigned)lane < ctas) {
+      const uint32_t to = peer_addr(&sm.tops[rank], lane);
+      peer_store64(to, (u64)__float_as_uint(m) | (u64)(unsigned)at << 32);
+      peer_store32(to + 8, bound);
+    }
   }
   cluster_sync();
   m = -INFINITY;
   at = 0x7fffffff;
   for (unsigned c = 0; c < ctas; ++c) {
-    const float y = __uint_as_float(peer_load(peer_addr(&sm.max, c)));
-    const int z = (int)peer_load(peer_addr(&sm.arg, c));
-    if (y > m || (y == m && z < at)) {
-      m = y;
-      at = z;
+    const Top& t = sm.tops[c];
+    if (t.max > m || (t.max == m && t.arg < at)) {
+      m = t.max;
+      at = t.arg;
     }
+    bound = max(bound, t.bound);
   }
-  cluster_sync();
-  float temperature = job.temperature ? job.temperature[r] : job.all_temperature;
-  const int top_k = job.top_k ? job.top_k[r] : job.all_top_k;
-  const float top_p = job.top_p ? job.top_p[r] : job.all_top_p, min_p = job.min_p ? job.min_p[r] : job.all_min_p;
-  if (m == -INFINITY || !(temperature > 0.f) || top_k == 1) {   // nothing to draw from, or the likeliest token
+  if (m == -INFINITY || greedy) {   // nothing to draw from, or the likeliest token
     if (rank == 0 && tid == 0) {
       int token = -1;
       if (m > -INFINITY) {
@@ -614,75 +853,89 @@ __global__ void __launch_bounds__(kThreads) k_sample(const __grid_constant__ Job
     }
     return;
   }
-  const double c = 1.4426950408889634074 / (double)temperature;
+  // log2(e) / T in two terms: the quotient, and its remainder's.
   Row row;
   row.max = m;
-  row.ch = (float)c;
-  row.cl = (float)(c - (double)row.ch);
-  RowCtas<T> ctx{sm, pieces, row, rank, ctas};
-  Head head = {0u, 0x7fffffff};
-  Head least = head;  // min-p's
+  row.ch = fminf(1.44269502f / temperature, 3e38f);   // (0 times it stays 0)
+  row.cl = row.ch < 1e30f && temperature < 1e30f ? (__fmaf_rn(-row.ch, temperature, 1.44269502f) + 1.92596299e-8f) / temperature : 0.f;
+  RowCtas<T> ctx{pieces, row, rank, ctas};
+  float least = -INFINITY;  // min-p's: w >= min_p where x >= max + T ln(min_p), the least fp32 value that is
   if (min_p > 0.f) {
-    // w >= min_p where x >= max + T ln(min_p): the least fp32 value that is.
-    const double from = (double)m + (double)temperature * log(fmin((double)min_p, 1.0));
-    float f = (float)from;
-    if ((double)f < from) f = nextafterf(f, INFINITY);
-    least.k = key_of(f);
-    if (least.k > 0) {  // x >= f: key > key(f) - 1
-      --least.k;
-      least.i = -1;
+    if (tid == 0) {
+      const double from = (double)m + sm.ahead;
+      least = (float)from;
+      if ((double)least < from) least = nextafterf(least, INFINITY);
+      sm.least = least;
     }
+    __syncthreads();
+    least = sm.least;
   }
-  const bool by_k = top_k > 0 && top_k < job.vocab;
-  if (by_k && top_k <= kThreads) {
-    // The few tokens that can be among the first k, in one list.
-    const uint32_t bound = ctx.bound_of_top(top_k, own_key);
-    const int n = ctx.gather([&](float x, int i) { return key_of(x) >= bound && kept(least, key_of(x), i); });
-    if (n <= kCap) {
-      if (rank != 0) return;
-      if (n > top_k) head = ctx.cut(head, n, false, (u64)top_k);
-      u64 total = 0;
-      ctx.each_listed(n, [&](float x, int i) { total += kept(head, key_of(x), i) ? weight(row, sm.table, x) : 0; });
-      total = ctx.block_sum(total);
-      if (top_p < 1.f) {
-        const u64 target = (u64)ceil(fmax((double)top_p, 0.0) * (double)total);
-        head = ctx.cut(head, n, true, max(1ull, min(target, total)));
-        total = 0;
-        ctx.each_listed(n, [&](float x, int i) { total += kept(head, key_of(x), i) ? weight(row, sm.table, x) : 0; });
-        total = ctx.block_sum(total);
+  // Where few tokens can be kept the first CTA decides in a list of them.
+  const Head from = least > -INFINITY ? Head{key_of(least) - 1, -1} : Head{0u, 0x7fffffff};  // x >= least: a key above its own less one
+  Head head = from;
+  bool summed = false;  // the kept tokens' mass lies in the first CTA's runs
+  if (m < INFINITY) {
+    u64 all = 0;
+    bool listed = true;
+    if (by_k && top_k <= kThreads) {
+      const float from = fmaxf(least, ctx.key_value(bound));  // (a NaN where the bound is below every number)
+      ctx.gather([&](float x, int) { return x >= from; });
+    } else if (!by_k && top_p < 1.f) {
+      listed = ctx.top_p_list(top_p, least, own_max, &all);
+    } else if (!by_k && min_p > 0.f) {
+      ctx.gather([&](float x, int) { return x >= least; });
+    } else {
+      listed = false;
+    }
+    if (listed) {
+      cluster_sync();
+      const int n = (int)peer_load(peer_addr(&sm.listed, 0));
+      if (n <= kCap) {
+        if (rank == 0) {
+          u64 total;
+          const int token = ctx.draw_listed(n, by_k ? top_k : 0, top_p, all, job.u[r], &total);
+          if (tid == 0) job.token[r] = token;
+          if (job.logprob)
+            ctx.each_listed(n, [&](float x, int i) {
+              if (i == token) job.logprob[r] = log_share(x, m, temperature, total);
+            });
+        }
+        cluster_sync();  // (the others have read this CTA's count)
+        return;
       }
-      const int token = ctx.by_index(n, true, draw_at(job.u[r], total) + 1, [&](float x, int i) { return kept(head, key_of(x), i); });
-      if (tid == 0) job.token[r] = token;
-      if (job.logprob)
-        ctx.each_listed(n, [&](float x, int i) {
-          if (i == token) job.logprob[r] = share_of(x, m, temperature, total);
-        });
-      return;
+      cluster_sync();
     }
+    if (!by_k && top_p < 1.f) summed = ctx.top_p_runs(top_p, least, from, all, &head);
   }
-  if (by_k) head = ctx.cut(head, -1, false, (u64)top_k);
-  if (least.k > head.k || (least.k == head.k && least.i < head.i)) head = least;
-  if (top_p < 1.f) head = ctx.top_p_cut(head, top_p);
-  // The kept tokens' mass by runs of 32 pieces, to the first CTA.
   const int runs = (pieces.count + 31) / 32;
-  for (int g = (int)rank * kWarps + warp; g < runs; g += (int)ctas * kWarps) {
-    const int v = g * 32 + lane;
-    float x[N];
-    pieces.load(v, x);
-    u64 s = 0;
+  if (!summed) {
+    head = by_k ? ctx.cut({0u, 0x7fffffff}, -1, false, (u64)top_k) : from;
+    if (from.k > head.k) head = from;
+    if (top_p < 1.f) {
+      u64 s = 0;
+      ctx.each([&](float x, int i) { s += kept(head, key_of(x), i) ? weight(row, sm.table, x) : 0; });
+      head = ctx.cut(head, -1, true, ctx.share(top_p, ctx.row_sum(ctx.block_sum(s))));
+    }
+    // The kept tokens' mass by runs of 32 pieces, to the first CTA.
+    for (int g = (int)rank * kWarps + warp; g < runs; g += (int)ctas * kWarps) {
+      const int v = g * 32 + lane;
+      float x[N];
+      pieces.load(v, x);
+      u64 s = 0;
 #pragma unroll
-    for (int e = 0; e < N; ++e)
-      if (kept(head, key_of(x[e]), v * N - pieces.off + e)) s += weight(row, sm.table, x[e]);
+      for (int e = 0; e < N; ++e)
+        if (kept(head, key_of(x[e]), v * N - pieces.off + e)) s += weight(row, sm.table, x[e]);
 #pragma unroll
-    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    if (lane == 0) peer_store64(peer_addr(&chunk[g], 0), s);
+      for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+      if (lane == 0) peer_store64(peer_addr(&sm.runs[g], 0), s);
+    }
+    cluster_sync();
   }
-  cluster_sync();
   if (rank != 0 || warp != 0) return;
   // Its first warp finds the run, then the token.
   const int per = (runs + 31) / 32;
   u64 own = 0;
-  for (int g = lane * per; g < min(runs, (lane + 1) * per); ++g) own += chunk[g];
+  for (int g = lane * per; g < min(runs, (lane + 1) * per); ++g) own += sm.runs[g];
   u64 inc = own;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -694,7 +947,7 @@ __global__ void __launch_bounds__(kThreads) k_sample(const __grid_constant__ Job
   const int l = __ffs(__ballot_sync(0xffffffffu, inc > target)) - 1;
   int run = l * per;
   u64 before = __shfl_sync(0xffffffffu, inc - own, l);
-  while (before + chunk[run] <= target) before += chunk[run++];
+  while (before + sm.runs[run] <= target) before += sm.runs[run++];
   const int v = run * 32 + lane;
   float x[N];
   pieces.load(v, x);
@@ -721,10 +974,12 @@ __global__ void __launch_bounds__(kThreads) k_sample(const __grid_constant__ Job
     if (!found && sum > target) {
       found = true;
       job.token[r] = v * N - pieces.off + e;
-      if (job.logprob) job.logprob[r] = share_of(x[e], m, temperature, total);
+      if (job.logprob) job.logprob[r] = log_share(x[e], m, temperature, total);
     }
   }
 }
+
+#undef sm
 
 }  // namespace
 }  // namespace gb
@@ -749,15 +1004,13 @@ extern "C" gb_status gb_sample(const gb_sample_args* a, gb_stream_t stream) {
   if ((long long)a->rows * cluster > 0x7fffffffll) return GB_ERR_TOO_LARGE;
   Job job = {a->logits, a->row_stride, a->rows, a->vocab, cluster, a->u, a->temperature, a->top_p, a->min_p, a->top_k,
              a->all_temperature, a->all_top_p, a->all_min_p, a->all_top_k, a->token, a->logprob};
-  const int n = 16 / es, runs = ((a->vocab + n - 1 + n - 1) / n + 31) / 32;
-  const size_t smem = sizeof(Smem) + (size_t)runs * sizeof(u64);
   void (*kernel)(const Job) = a->dtype == GB_F32 ? k_sample<float> : k_sample<__nv_bfloat16>;
-  if (set_max_dynamic_smem(reinterpret_cast<const void*>(kernel), (int)(sizeof(Smem) + (kMaxVocab / 128 + 2) * sizeof(u64))) != cudaSuccess)
+  if (set_max_dynamic_smem(reinterpret_cast<const void*>(kernel), (int)sizeof(Smem)) != cudaSuccess)
     return GB_ERR_CUDA;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(a->rows * cluster));
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = smem;
+  cfg.dynamicSmemBytes = sizeof(Smem);
   cfg.stream = reinterpret_cast<cudaStream_t>(stream);
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;

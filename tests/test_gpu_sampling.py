@@ -113,7 +113,7 @@ def test_random_numbers_at_the_ends(cuda):
     check(x, u, top_p=0.9)
 
 
-@pytest.mark.parametrize("name,values", [("temperature", [0.0, -1.0, math.nan, math.inf, 1e-30, 1e30]), ("top_k", [-5, 0, 500, 499, 1 << 30, 2]),
+@pytest.mark.parametrize("name,values", [("temperature", [0.0, -1.0, math.nan, math.inf, 1e-30, 1e-40]), ("top_k", [-5, 0, 500, 499, 1 << 30, 2]),
                                          ("top_p", [0.0, -1.0, 1.0, 2.0, math.nan, 1e-9]), ("min_p", [0.0, -1.0, 1.0, 2.0, math.nan, 1e-30])])
 def test_parameters_at_the_ends(cuda, name, values):
     g = torch.Generator().manual_seed(1)
