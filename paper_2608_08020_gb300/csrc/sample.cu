@@ -219,7 +219,8 @@ struct Smem {
     u64 runs[(kMaxVocab / 4 + 2 + 31) / 32];  // the first CTA's: mass of each run of 32 pieces
   };
   float queue[kWarps][32 + 32 * 8];      // logits that wait for their weights
-  u64 order[kRanked];                    // a short list's entries: (key from above, index)
+  u64 order[kRanked];                    // tokens to be ranked, (key from above, index), and their weights
+  u64 ranked[kRanked];
   uint32_t slice[kSlices];               // masses by slice, see top_p_list
   u64 slice_total[kSlices];
   uint32_t hist[1 + kDigits][kBins];     // counts, then the masses' digits
@@ -228,7 +229,7 @@ struct Smem {
   Head head;
   double ahead;                          // T ln(min_p)
   float least;
-  int listed, token;
+  int listed, ranks, token;
   int lo, hi, many;                      // top-p: the slices that its cut can lie in, whether it keeps more than a list holds
   float red[kWarps];
   int redi[kWarps];
@@ -333,6 +334,14 @@ struct RowCtas {
   __device__ __forceinline__ void each_listed(int n, F f) const {
     for (int j = threadIdx.x; j < n; j += kThreads) f(sm.list[j].x, sm.list[j].i);
   }
+  // f(value, token, weight), of those with a weight in sm.weights.
+  template <class F>
+  __device__ __forceinline__ void each_weighed(int n, F f) const {
+    for (int j = threadIdx.x; j < n; j += kThreads) {
+      const u64 w = sm.weights[j];
+      if (w) f(sm.list[j].x, sm.list[j].i, w);
+    }
+  }
 
   // One digit of a selection among the row's tokens (n < 0) or this CTA's first n listed ones: the bin in which the running
   // total (of counts or masses, by bin in ascending order) reaches `target` > 0, and the total before it.  bin(x, i): a token's
@@ -404,6 +413,7 @@ struct RowCtas {
   __device__ Head cut(const Head& h, int n, bool weigh, u64 target) {
     const uint32_t top = key_of(row.max);
     uint32_t at = 0;                       // of top - key, the digits chosen so far
+    u64 of = 0;                            // the last one's bin's total
     for (int s = 24; s >= 0; s -= 8) {
       digit(n, weigh, target, [&](float x, int i) {
         const uint32_t key = key_of(x), rel = top - key;
@@ -411,18 +421,69 @@ struct RowCtas {
       });
       at |= (uint32_t)sm.bin << s;
       target -= sm.before;
+      of = sm.total[sm.bin];
       __syncthreads();
     }
     if (at > top || top - at < h.k) return h;   // (the total stays below the target: all of the head)
     // The key is chosen; of its tokens, all of one weight, the first ones by index.
     Head to = {top - at, h.k == top - at ? h.i : 0x7fffffff};
+    if (target >= of) return to;
     u64 most = target;
     if (weigh) {
       const u64 w = weight(row, sm.table, key_value(to.k));
-      most = w ? (target + w - 1) / w : target;
+      most = (target + w - 1) / w;
+      if (most * w >= of) return to;
     }
     to.i = min(to.i, by_index(n, false, most, [&](float x, int i) { return key_of(x) == to.k && i <= to.i; }));
     return to;
+  }
+
+  // The order of this CTA's sm.ranks <= kRanked tokens in sm.order: f(token's number, the mass of those before it, its own),
+  // for each by one thread, which compares it with all the others, together with its neighbours.
+  template <class F>
+  __device__ __forceinline__ void rank_each(F f) const {
+    const int n = sm.ranks, shift = n <= kRanked / 4 ? 3 : n <= kRanked / 2 ? 2 : 1, ways = 1 << shift;
+    const int j = threadIdx.x >> shift, way = threadIdx.x & (ways - 1);
+    const u64 own = sm.order[j < n ? j : 0];
+    u64 before = 0;
+#pragma unroll 4
+    for (int z = way; z < n; z += ways) {
+      const u64 w = sm.ranked[z];
+      before += sm.order[z] < own ? w : 0;
+    }
+    for (int o = 1; o < ways; o <<= 1) before += __shfl_xor_sync(0xffffffffu, before, o);
+    if (j < n && way == 0) f(j, before, sm.ranked[j]);
+  }
+  __device__ __forceinline__ void to_rank(u64 order, u64 w) const {
+    const int at = atomicAdd(&sm.ranks, 1);
+    if (at < kRanked) {
+      sm.order[at] = order;
+      sm.ranked[at] = w;
+    }
+  }
+
+  // cut() by mass of the head h of this CTA's list (each(f): f(value, token, weight) of its tokens in h) where the tokens with
+  // an exponent below `begin` are known to stay.
+  template <class Each>
+  __device__ Head cut_listed(const Head& h, int n, float begin, u64 target, Each each_of) {
+    if (threadIdx.x == 0) {
+      sm.ranks = 0;
+      sm.head = h;
+    }
+    __syncthreads();
+    u64 above = 0;
+    each_of([&](float x, int i, u64 w) {
+      if (exponent(row, x) < begin) above += w;
+      else to_rank((u64)~key_of(x) << 32 | (unsigned)i, w);
+    });
+    above = block_sum(above);
+    if (sm.ranks > kRanked) return cut(h, n, true, target);
+    rank_each([&](int j, u64 before, u64 w) {
+      before += above;
+      if (before < target && target <= before + w) sm.head = {~(uint32_t)(sm.order[j] >> 32), (int)(uint32_t)sm.order[j]};
+    });
+    __syncthreads();
+    return sm.head;
   }
 
   // The index at which the running total of the tokens that in(x, i) says, taken by index, reaches `target`.
@@ -531,7 +592,14 @@ struct RowCtas {
         if (in && y < far) mine |= 1u << e;
         else if (in && y < kFar) light += __float_as_uint(exp2f(-y) + 0x1p-21f) - __float_as_uint(0x1p-21f);  // 2^-44 each
       }
-      if (!__any_sync(0xffffffffu, mine != 0)) continue;
+      const unsigned some = __reduce_add_sync(0xffffffffu, __popc(mine));
+      if (some == 0) continue;
+      if (some >= 16 * N) {
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+          if (mine >> e & 1) add(x[e]);
+        continue;
+      }
       queue.put(x, mine);
       while (queue.n >= 32) queue.take(32, add);
     }
@@ -597,10 +665,17 @@ struct RowCtas {
         window |= in && y >= begin ? 1u << e : 0u;
       }
       u64 s = 0;
-      if (__any_sync(0xffffffffu, above != 0)) {
-        queue.put(x, above);
+      const unsigned some = __reduce_add_sync(0xffffffffu, __popc(above));
+      if (some != 0) {
         auto add = [&](float y) { s += mass_of(weight_of(row, sm.table, y)); };
-        while (queue.n > 0) queue.take(min(queue.n, 32), add);
+        if (some >= 16 * N) {
+#pragma unroll
+          for (int e = 0; e < N; ++e)
+            if (above >> e & 1) add(x[e]);
+        } else {
+          queue.put(x, above);
+          while (queue.n > 0) queue.take(min(queue.n, 32), add);
+        }
 #pragma unroll
         for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
       }
@@ -620,7 +695,9 @@ struct RowCtas {
       u64 s = 0;
       for (int g = threadIdx.x; g < runs; g += kThreads) s += sm.runs[g];
       s = block_sum(s);
-      const Head to = cut(from, n, true, share(p, all) - s);
+      const Head to = cut_listed(from, n, -1.f, share(p, all) - s, [&](auto f) {
+        each_listed(n, [&](float x, int i) { f(x, i, weight(row, sm.table, x)); });
+      });
       each_listed(n, [&](float x, int i) {
         if (kept(to, key_of(x), i)) atomicAdd(&sm.runs[(i + pieces.off) / (32 * N)], weight(row, sm.table, x));
       });
@@ -736,17 +813,40 @@ struct RowCtas {
     }
     Head head = {0u, 0x7fffffff};
     if (k > 0 && n > k) head = cut(head, n, false, (u64)k);
-    u64 total = listed_mass(n, head);
+    u64 total = weigh_listed(n, head);
+    auto weighed = [&](auto f) { each_weighed(n, f); };
     if (p < 1.f) {
-      head = cut(head, n, true, share(p, all ? all : total));
-      total = listed_mass(n, head);
+      head = cut_listed(head, n, k > 0 ? -1.f : slice_begin(sm.lo), share(p, all ? all : total), weighed);
+      total = weigh_listed(n, head);
     }
     *mass = total;
-    return by_index(n, true, draw_at(u, total) + 1, [&](float x, int i) { return kept(head, key_of(x), i); });
+    // A digit of the index, then the tokens that share it.
+    const u64 at = draw_at(u, total);
+    const int shift = max(0, 24 - __clz(pieces.vocab));
+    if (threadIdx.x == 0) sm.ranks = 0;
+    digit(n, true, at + 1, [&](float x, int i) { return kept(head, key_of(x), i) ? i >> shift : -1; });
+    const int bin = sm.bin;
+    const u64 rest = at - sm.before;
+    each_weighed(n, [&](float, int i, u64 w) {
+      if (i >> shift == bin) to_rank((u64)(unsigned)i, w);
+    });
+    __syncthreads();
+    if (sm.ranks > kRanked) return by_index(n, true, at + 1, [&](float x, int i) { return kept(head, key_of(x), i); });
+    rank_each([&](int j, u64 before, u64 w) {
+      if (before <= rest && rest < before + w) sm.token = (int)sm.order[j];
+    });
+    __syncthreads();
+    return sm.token;
   }
-  __device__ u64 listed_mass(int n, const Head& h) {
+  // The weights of the list's tokens, 0 where the head does not keep them, and their sum.
+  __device__ u64 weigh_listed(int n, const Head& h) {
     u64 s = 0;
-    each_listed(n, [&](float x, int i) { s += kept(h, key_of(x), i) ? weight(row, sm.table, x) : 0; });
+    for (int j = threadIdx.x; j < n; j += kThreads) {
+      const Entry e = sm.list[j];
+      const u64 w = kept(h, key_of(e.x), e.i) ? weight(row, sm.table, e.x) : 0;
+      sm.weights[j] = w;
+      s += w;
+    }
     return block_sum(s);
   }
   __device__ static float key_value(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
