@@ -78,11 +78,6 @@ __device__ __forceinline__ uint32_t peer_addr(const void* p, unsigned rank) {
 }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-__device__ __forceinline__ int peer_add(uint32_t a, int n) {
-  int x;
-  asm volatile("atom.shared::cluster.add.u32 %0, [%1], %2;" : "=r"(x) : "r"(a), "r"(n) : "memory");
-  return x;
-}
 __device__ __forceinline__ uint32_t peer_load(uint32_t a) {
   uint32_t x;
   asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(x) : "r"(a) : "memory");
@@ -112,24 +107,32 @@ __device__ __forceinline__ float exponent(const Row& row, float x) { return __fm
 
 // exp((x - max) / T) = m 2^-31 2^-n with m in (2^30, 2^31], for a logit with exponent() below kFar; j = floor(256 y), n = j >> 8.
 // y is taken to 2^-40 of itself or better; m is the table's 2^(-(j & 255)/256) less its share 1 - 2^-r, 0 <= r < 2^-8, to the
-// third order.
+// third order and in units of 2^-31.  Two at a time, as the fp32 units take them; of other logits something without meaning.
 struct Weight {
   uint32_t m;
   int j;
 };
-__device__ __forceinline__ Weight weight_of(const Row& row, const uint32_t* table, float x) {
-  const float d = __fsub_rn(row.max, x), b = __fsub_rn(d, row.max);
-  const float e = __fadd_rn(__fsub_rn(row.max, __fsub_rn(d, b)), __fsub_rn(-x, b));
-  const float yh = __fmul_rn(d, row.ch);
-  const float yl = __fadd_rn(__fmaf_rn(d, row.ch, -yh), __fmaf_rn(d, row.cl, __fmul_rn(e, row.ch)));
-  const float z = __fadd_rd(yh, 49152.f);                  // down to a multiple of 2^-8
-  const int j = __float_as_int(z) - __float_as_int(49152.f);
-  const float r = __fadd_rn(__fsub_rn(yh, __fsub_rn(z, 49152.f)), yl);
-  constexpr float kLn2 = 0.69314718055994530942f;
-  const float q = r * __fmaf_rn(r, __fmaf_rn(r, kLn2 * kLn2 * kLn2 / 6, -kLn2 * kLn2 / 2), kLn2);
-  const uint32_t t = table[j & 255];
-  const int less = __float2int_rn(q * 0x1p32f);            // (below 0 where yl pulls y under its multiple)
-  return {t - __umulhi(t, (uint32_t)less) + (t & (uint32_t)(less >> 31)), j};
+__device__ __forceinline__ float2 two(float x) { return make_float2(x, x); }
+__device__ __forceinline__ float2 minus(float2 x) { return make_float2(-x.x, -x.y); }
+__device__ __forceinline__ void weights_of(const Row& row, const uint32_t* table, float2 x, Weight (&w)[2]) {
+  const float2 top = two(row.max), ch = two(row.ch), nx = minus(x);
+  const float2 d = __fadd2_rn(top, nx), b = __fadd2_rn(d, minus(top));
+  const float2 e = __fadd2_rn(__fadd2_rn(top, __fadd2_rn(b, minus(d))), __fadd2_rn(nx, minus(b)));
+  const float2 yh = __fmul2_rn(d, ch);
+  const float2 yl = __fadd2_rn(__ffma2_rn(d, ch, minus(yh)), __ffma2_rn(d, two(row.cl), __fmul2_rn(e, ch)));
+  const float2 z = __fadd2_rd(yh, two(49152.f));           // down to a multiple of 2^-8
+  const float2 r = __fadd2_rn(__fadd2_rn(yh, minus(__fadd2_rn(z, two(-49152.f)))), yl);
+  constexpr float kLn2 = 0.69314718055994530942f, k31 = 0x1p31f, kBase = 0x1.4p23f;
+  float2 q = __ffma2_rn(r, two(k31 * kLn2 * kLn2 * kLn2 / 6), two(-k31 * kLn2 * kLn2 / 2));
+  q = __fadd2_rn(__fmul2_rn(r, __ffma2_rn(r, q, two(k31 * kLn2))), two(kBase));  // rounds; q < 0 where yl pulls y under its multiple
+  const float zs[2] = {z.x, z.y}, qs[2] = {q.x, q.y};
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int less = 2 * (__float_as_int(qs[i]) - __float_as_int(kBase));
+    w[i].j = __float_as_int(zs[i]) - __float_as_int(49152.f);
+    const uint32_t t = table[w[i].j & 255];
+    w[i].m = t + (uint32_t)__mulhi(-(int)t, less);         // (-t: at least -2^31)
+  }
 }
 // The same in units of 2^-44.
 __device__ __forceinline__ u64 mass_of(const Weight& w) {
@@ -140,7 +143,10 @@ __device__ __forceinline__ u64 mass_of(const Weight& w) {
 __device__ __forceinline__ u64 weight(const Row& row, const uint32_t* table, float x) {
   if (!(x > -INFINITY)) return 0;
   if (x == row.max) return 1ull << kUnit;
-  return exponent(row, x) < kFar ? mass_of(weight_of(row, table, x)) : 0;
+  if (!(exponent(row, x) < kFar)) return 0;
+  Weight w[2];
+  weights_of(row, table, two(x), w);
+  return mass_of(w[0]);
 }
 
 // Slices of the exponent, kPerPower to a power of two: floor(kPerPower j / 256).  Their masses are summed in units of
@@ -151,8 +157,8 @@ __device__ __forceinline__ int slice_shift(int b) { return max(0, 32 - b / kPerP
 // The exponent that slice b begins at: tokens with exponent() below it are in the slices before.
 __device__ __forceinline__ float slice_begin(int b) { return (float)((b * 256 + kPerPower - 1) / kPerPower) * (1.f / 256); }
 
-__device__ __forceinline__ float value(const float* p) { return *p; }
-__device__ __forceinline__ float value(const __nv_bfloat16* p) { return __bfloat162float(*p); }
+__device__ __forceinline__ unsigned value(const float* p) { return __float_as_uint(*p); }
+__device__ __forceinline__ unsigned value(const __nv_bfloat16* p) { return __bfloat16_as_ushort(*p); }
 __device__ __forceinline__ void values(const uint4& v, float (&x)[4]) {
   x[0] = __uint_as_float(v.x);
   x[1] = __uint_as_float(v.y);
@@ -179,13 +185,35 @@ struct Pieces {
     off = (int)(((uintptr_t)row & 15) / sizeof(T));
     count = (off + n + N - 1) / N;
   }
-  __device__ __forceinline__ void load(int v, float (&f)[N]) const {
+  __device__ __forceinline__ uint4 bits(int v) const {
     const int i0 = v * N - off;
-    if (v < count && i0 >= 0 && i0 + N <= vocab) {
-      values(__ldg(reinterpret_cast<const uint4*>(x + i0)), f);
-    } else {
+    if (v < count && i0 >= 0 && i0 + N <= vocab) return __ldg(reinterpret_cast<const uint4*>(x + i0));
+    constexpr unsigned kNone = sizeof(T) == 4 ? 0xff800000u : 0xff80u;  // -infinity
+    uint32_t w[4] = {};
 #pragma unroll
-      for (int e = 0; e < N; ++e) f[e] = v < count && i0 + e >= 0 && i0 + e < vocab ? value(x + i0 + e) : -INFINITY;
+    for (int e = 0; e < N; ++e) {
+      const bool in = v < count && i0 + e >= 0 && i0 + e < vocab;
+      w[e * (int)sizeof(T) / 4] |= (in ? value(x + i0 + e) : kNone) << (e * (int)sizeof(T) % 4 * 8);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  __device__ __forceinline__ void load(int v, float (&f)[N]) const { values(bits(v), f); }
+  // f(v, its values) of the pieces v = first, first + step, ... below `end`, the same number for every lane of a warp (end: for
+  // lane 0); `Ahead` loads at a time.
+  template <int Ahead, class F>
+  __device__ __forceinline__ void scan(int first, int end, int step, F f) const {
+    const int lane = threadIdx.x & 31;
+    for (int v0 = first; v0 < end; v0 += Ahead * step) {
+      uint4 b[Ahead];
+#pragma unroll
+      for (int a = 0; a < Ahead; ++a) b[a] = bits(v0 + a * step + lane);
+#pragma unroll
+      for (int a = 0; a < Ahead; ++a) {
+        if (v0 + a * step >= end) break;
+        float y[N];
+        values(b[a], y);
+        f(v0 + a * step + lane, y);
+      }
     }
   }
 };
@@ -218,11 +246,10 @@ struct Smem {
     u64 weights[kCap];                   // of the list, once it is whole
     u64 runs[(kMaxVocab / 4 + 2 + 31) / 32];  // the first CTA's: mass of each run of 32 pieces
   };
-  float queue[kWarps][32 + 32 * 8];      // logits that wait for their weights
+  float queue[kWarps][64 + 32 * 8];      // logits that wait for their weights
   u64 order[kRanked];                    // tokens to be ranked, (key from above, index), and their weights
   u64 ranked[kRanked];
   uint32_t slice[kSlices];               // masses by slice, see top_p_list
-  u64 slice_total[kSlices];
   uint32_t hist[1 + kDigits][kBins];     // counts, then the masses' digits
   u64 total[kBins];
   Top tops[kMaxCluster];                 // of the row's CTAs
@@ -292,11 +319,16 @@ struct Queue {
     n += __shfl_sync(0xffffffffu, inc, 31);
     __syncwarp();
   }
-  // f of the last `some` <= 32.
+  // f of the last `some` <= 64, two at a time: f(two values, which of them).
   template <class F>
   __device__ __forceinline__ void take(int some, F f) {
     const int lane = threadIdx.x & 31;
-    if (lane < some) f(at[n - some + lane]);
+    const float* from = at + n - some;
+    if (lane < some) {
+      const bool both = lane + 32 < some;
+      const float x = from[lane];
+      f(make_float2(x, both ? from[lane + 32] : x), both ? 3u : 1u);
+    }
     n -= some;
     __syncwarp();
   }
@@ -514,7 +546,7 @@ struct RowCtas {
     return t;
   }
 
-  // Room for the warp's `mine` entries each in the first CTA's list.
+  // Room for the warp's `mine` entries each in this CTA's list.
   __device__ __forceinline__ int reserve(int mine) const {
     const int lane = threadIdx.x & 31;
     int inc = mine;
@@ -524,31 +556,43 @@ struct RowCtas {
       if (lane >= o) inc += y;
     }
     int at = 0;
-    if (lane == 31) at = peer_add(peer_addr(&sm.listed, 0), inc);
+    if (lane == 31) at = atomicAdd(&sm.listed, inc);
     return __shfl_sync(0xffffffffu, at, 31) + inc - mine;
   }
   __device__ __forceinline__ void put(int at, float x, int i) const {
-    if (at < kCap) peer_store64(peer_addr(&sm.list[at], 0), (u64)__float_as_uint(x) | (u64)(unsigned)i << 32);
+    if (at < kCap) sm.list[at] = {x, i};
   }
-
-  // The row's tokens that in(x, i) says into the first CTA's list, in no order.
+  // The row's tokens that in(x, i) says into the lists of the CTAs that read them, in no order.
   template <class In>
   __device__ __forceinline__ void gather(In in) const {
-    const int step = (int)(ctas * kThreads);
-#pragma unroll 2
-    for (int v0 = (int)(rank * kThreads) + (int)(threadIdx.x & ~31u); v0 < pieces.count; v0 += step) {
-      const int v = v0 + (int)(threadIdx.x & 31);
-      float x[N];
-      pieces.load(v, x);
+    pieces.template scan<4>((int)(rank * kThreads) + (int)(threadIdx.x & ~31u), pieces.count, (int)(ctas * kThreads), [&](int v, const float (&x)[N]) {
       unsigned mine = 0;
 #pragma unroll
       for (int e = 0; e < N; ++e) mine |= x[e] > -INFINITY && in(x[e], v * N - pieces.off + e) ? 1u << e : 0u;
-      if (!__any_sync(0xffffffffu, mine != 0)) continue;
+      if (!__any_sync(0xffffffffu, mine != 0)) return;
       int at = reserve(__popc(mine));
 #pragma unroll
       for (int e = 0; e < N; ++e)
         if (mine >> e & 1) put(at++, x[e], v * N - pieces.off + e);
+    });
+  }
+  // The CTAs' lists behind the first one's.  Their length together, and where it is above kCap only that.
+  __device__ int join_lists() const {
+    cluster_sync();
+    int n = 0, own = 0, at = 0;
+    for (unsigned c = 0; c < ctas; ++c) {
+      const int there = (int)peer_load(peer_addr(&sm.listed, c));
+      if (c < rank) at += there;
+      if (c == rank) own = there;
+      n += there;
     }
+    if (rank != 0 && n <= kCap) {
+      const uint32_t to = peer_addr(&sm.list[at], 0);
+      for (int j = threadIdx.x; j < own; j += kThreads)
+        peer_store64(to + j * (uint32_t)sizeof(Entry), (u64)__float_as_uint(sm.list[j].x) | (u64)(unsigned)sm.list[j].i << 32);
+    }
+    cluster_sync();
+    return n;
   }
 
   // Sums the weights of the tokens with x >= least, and those that top-p can keep by slices of their exponent, to 12 bits
@@ -572,18 +616,20 @@ struct RowCtas {
     const int reach = min((int)(fmaxf(can - there, 0.1f) * (float)kPerPower) + 1, kSlices - 1);
     uint32_t light = 0;   // of 1024 tokens at most
     u64 s = 0;
-    const int step = (int)(ctas * kThreads), lane = threadIdx.x & 31;
+    const int step = (int)(ctas * kThreads);
     Queue queue{sm.queue[threadIdx.x >> 5], 0};
-    auto add = [&](float x) {
-      const Weight w = weight_of(row, sm.table, x);
-      s += mass_of(w);
-      const int b = slice_of(w);
-      if (b <= reach) atomicAdd(&sm.slice[b], slice_part(w));
+    auto add = [&](float2 x, unsigned which) {
+      Weight w[2];
+      weights_of(row, sm.table, x, w);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        if (!(which >> i & 1)) continue;
+        s += mass_of(w[i]);
+        const int b = slice_of(w[i]);
+        if (b <= reach) atomicAdd(&sm.slice[b], slice_part(w[i]));
+      }
     };
-#pragma unroll 2
-    for (int v0 = (int)(rank * kThreads) + (int)(threadIdx.x & ~31u); v0 < pieces.count; v0 += step) {
-      float x[N];
-      pieces.load(v0 + lane, x);
+    pieces.template scan<2>((int)(rank * kThreads) + (int)(threadIdx.x & ~31u), pieces.count, step, [&](int, const float (&x)[N]) {
       unsigned mine = 0;
 #pragma unroll
       for (int e = 0; e < N; ++e) {
@@ -593,16 +639,15 @@ struct RowCtas {
         else if (in && y < kFar) light += __float_as_uint(exp2f(-y) + 0x1p-21f) - __float_as_uint(0x1p-21f);  // 2^-44 each
       }
       const unsigned some = __reduce_add_sync(0xffffffffu, __popc(mine));
-      if (some == 0) continue;
+      if (some == 0) return;
       if (some >= 16 * N) {
 #pragma unroll
-        for (int e = 0; e < N; ++e)
-          if (mine >> e & 1) add(x[e]);
-        continue;
+        for (int e = 0; e < N; e += 2) add(make_float2(x[e], x[e + 1]), mine >> e);
+        return;
       }
       queue.put(x, mine);
-      while (queue.n >= 32) queue.take(32, add);
-    }
+      while (queue.n >= 64) queue.take(64, add);
+    });
     queue.take(queue.n, add);
     return s + light;
   }
@@ -621,25 +666,73 @@ struct RowCtas {
         t += (u64)peer_load(a) | (u64)peer_load(a + 4) << 32;
       }
       *all = t;
-      slice_totals();
-      if (threadIdx.x < 32) {
-        const int lane = threadIdx.x, lo = slice_reaching(share(p, t), 10), hi = slice_reaching(share(p, t), 0);
-        // At least so many tokens: a slice's mass over the most that one of it weighs.
-        u64 least_of = 0;
-        for (int b = lane; b <= hi; b += 32) least_of += sm.slice_total[b] >> max(kUnit - b / kPerPower, 0);
-        const unsigned count = __reduce_add_sync(0xffffffffu, (unsigned)least_of);
-        if ((unsigned)lane < ctas) {
-          peer_store32(peer_addr(&sm.lo, lane), lo);
-          peer_store32(peer_addr(&sm.hi, lane), hi);
-          peer_store32(peer_addr(&sm.many, lane), count > kCap);
-        }
-      }
+      window(share(p, t));
     }
     cluster_sync();
+    if (rank != 0 && threadIdx.x == 0) {
+      sm.lo = (int)peer_load(peer_addr(&sm.lo, 0));
+      sm.hi = (int)peer_load(peer_addr(&sm.hi, 0));
+      sm.many = (int)peer_load(peer_addr(&sm.many, 0));
+    }
+    __syncthreads();
     if (sm.many) return false;
     const float end = slice_begin(sm.hi + 1);
     gather([&](float x, int) { return x >= least && exponent(row, x) < end; });
     return true;
+  }
+  // By the first CTA: sm.lo, sm.hi, and sm.many, whether more than kCap tokens lie so far: at least a slice's mass over the most
+  // that one of it weighs.
+  __device__ void window(u64 target) {
+    constexpr int per = kSlices / kThreads;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    u64 mass[per], m = 0;
+    unsigned count[per], n = 0;
+#pragma unroll
+    for (int i = 0; i < per; ++i) {
+      const int b = threadIdx.x * per + i;
+      u64 t = 0;
+      for (unsigned c = 0; c < ctas; ++c) t += peer_load(peer_addr(&sm.slice[b], c));
+      t <<= slice_shift(b);
+      mass[i] = m += t;
+      count[i] = n += (unsigned)(t >> max(kUnit - b / kPerPower, 0));
+    }
+    const u64 own = m;
+    const unsigned owned = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const u64 x = __shfl_up_sync(0xffffffffu, m, o);
+      const unsigned y = __shfl_up_sync(0xffffffffu, n, o);
+      if (lane >= o) {
+        m += x;
+        n += y;
+      }
+    }
+    if (lane == 31) {
+      sm.red64[warp] = m;
+      sm.redi[warp] = (int)n;
+    }
+    if (threadIdx.x == 0) {
+      sm.lo = sm.hi = kSlices - 1;
+      sm.many = 0;
+    }
+    __syncthreads();
+    m -= own;
+    n -= owned;
+    for (int w = 0; w < warp; ++w) {
+      m += sm.red64[w];
+      n += (unsigned)sm.redi[w];
+    }
+    u64 before = m;
+#pragma unroll
+    for (int i = 0; i < per; ++i) {
+      const u64 with = m + mass[i];
+      if (before + (before >> 10) < target && with + (with >> 10) >= target) sm.lo = threadIdx.x * per + i;
+      if (before < target && with >= target) {
+        sm.hi = threadIdx.x * per + i;
+        sm.many = n + count[i] > kCap;
+      }
+      before = with;
+    }
   }
 
   // The cut where that list would be too long: a pass that sums what lies before slice sm.lo, by runs of 32 pieces, and lists
@@ -652,10 +745,8 @@ struct RowCtas {
     const float begin = slice_begin(sm.lo), end = slice_begin(sm.hi + 1);
     const int runs = (pieces.count + 31) / 32, lane = threadIdx.x & 31;
     Queue queue{sm.queue[threadIdx.x >> 5], 0};
-    for (int g = (int)rank * kWarps + (int)(threadIdx.x >> 5); g < runs; g += (int)ctas * kWarps) {
-      const int v = g * 32 + lane;
-      float x[N];
-      pieces.load(v, x);
+    pieces.template scan<2>((int)(rank * kThreads) + (int)(threadIdx.x & ~31u), pieces.count, (int)(ctas * kThreads), [&](int v, const float (&x)[N]) {
+      const int g = v >> 5;
       unsigned above = 0, window = 0;
 #pragma unroll
       for (int e = 0; e < N; ++e) {
@@ -667,14 +758,17 @@ struct RowCtas {
       u64 s = 0;
       const unsigned some = __reduce_add_sync(0xffffffffu, __popc(above));
       if (some != 0) {
-        auto add = [&](float y) { s += mass_of(weight_of(row, sm.table, y)); };
+        auto add = [&](float2 y, unsigned which) {
+          Weight w[2];
+          weights_of(row, sm.table, y, w);
+          s += (which & 1 ? mass_of(w[0]) : 0) + (which & 2 ? mass_of(w[1]) : 0);
+        };
         if (some >= 16 * N) {
 #pragma unroll
-          for (int e = 0; e < N; ++e)
-            if (above >> e & 1) add(x[e]);
+          for (int e = 0; e < N; e += 2) add(make_float2(x[e], x[e + 1]), above >> e);
         } else {
           queue.put(x, above);
-          while (queue.n > 0) queue.take(min(queue.n, 32), add);
+          while (queue.n > 0) queue.take(min(queue.n, 64), add);
         }
 #pragma unroll
         for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
@@ -686,10 +780,8 @@ struct RowCtas {
         for (int e = 0; e < N; ++e)
           if (window >> e & 1) put(at++, x[e], v * N - pieces.off + e);
       }
-    }
-    cluster_sync();
-    const int n = (int)peer_load(peer_addr(&sm.listed, 0));
-    cluster_sync();
+    });
+    const int n = join_lists();
     if (n > kCap) return false;
     if (rank == 0) {
       u64 s = 0;
@@ -705,39 +797,6 @@ struct RowCtas {
       *head = to;
     }
     return true;
-  }
-
-  // The row's masses by slice.
-  __device__ void slice_totals() {
-    for (int b = threadIdx.x; b < kSlices; b += kThreads) {
-      u64 m = 0;
-      for (unsigned c = 0; c < ctas; ++c) m += peer_load(peer_addr(&sm.slice[b], c));
-      sm.slice_total[b] = m << slice_shift(b);
-    }
-    __syncthreads();
-  }
-  // The first slice at which their running total, with 2^-over of itself on top (0: nothing), reaches the target; by a warp.
-  __device__ int slice_reaching(u64 target, int over) const {
-    constexpr int per = kSlices / 32;
-    const int lane = threadIdx.x & 31;
-    u64 own = 0;
-#pragma unroll 8
-    for (int b = 0; b < per; ++b) own += sm.slice_total[lane * per + b];
-    u64 inc = own;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const u64 y = __shfl_up_sync(0xffffffffu, inc, o);
-      if (lane >= o) inc += y;
-    }
-    auto reaches = [&](u64 t) { return t + (over ? t >> over : 0) >= target; };
-    const unsigned past = __ballot_sync(0xffffffffu, reaches(inc));
-    int at = kSlices - 1;
-    if (past && lane == __ffs(past) - 1) {
-      u64 t = inc - own;
-      at = lane * per;
-      while (at < lane * per + per - 1 && !reaches(t + sm.slice_total[at])) t += sm.slice_total[at++];
-    }
-    return (int)__reduce_min_sync(0xffffffffu, (unsigned)at);
   }
 
   // The CTAs' sums added up.
@@ -988,8 +1047,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(const __grid_constant__ 
       listed = false;
     }
     if (listed) {
-      cluster_sync();
-      const int n = (int)peer_load(peer_addr(&sm.listed, 0));
+      const int n = ctx.join_lists();
       if (n <= kCap) {
         if (rank == 0) {
           u64 total;
@@ -1000,10 +1058,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(const __grid_constant__ 
               if (i == token) job.logprob[r] = log_share(x, m, temperature, total);
             });
         }
-        cluster_sync();  // (the others have read this CTA's count)
         return;
       }
-      cluster_sync();
     }
     if (!by_k && top_p < 1.f) summed = ctx.top_p_runs(top_p, least, from, all, &head);
   }
@@ -1017,18 +1073,22 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(const __grid_constant__ 
       head = ctx.cut(head, -1, true, ctx.share(top_p, ctx.row_sum(ctx.block_sum(s))));
     }
     // The kept tokens' mass by runs of 32 pieces, to the first CTA.
-    for (int g = (int)rank * kWarps + warp; g < runs; g += (int)ctas * kWarps) {
-      const int v = g * 32 + lane;
-      float x[N];
-      pieces.load(v, x);
+    pieces.template scan<2>(((int)rank * kWarps + warp) * 32, pieces.count, (int)(ctas * kThreads), [&](int v, const float (&x)[N]) {
       u64 s = 0;
 #pragma unroll
-      for (int e = 0; e < N; ++e)
-        if (kept(head, key_of(x[e]), v * N - pieces.off + e)) s += weight(row, sm.table, x[e]);
+      for (int e = 0; e < N; e += 2) {
+        Weight w[2];
+        weights_of(row, sm.table, make_float2(x[e], x[e + 1]), w);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const bool in = kept(head, key_of(x[e + i]), v * N - pieces.off + e + i);
+          s += in && x[e + i] == m ? 1ull << kUnit : in && exponent(row, x[e + i]) < kFar ? mass_of(w[i]) : 0;
+        }
+      }
 #pragma unroll
       for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-      if (lane == 0) peer_store64(peer_addr(&sm.runs[g], 0), s);
-    }
+      if (lane == 0) peer_store64(peer_addr(&sm.runs[v >> 5], 0), s);
+    });
     cluster_sync();
   }
   if (rank != 0 || warp != 0) return;
@@ -1098,9 +1158,12 @@ extern "C" gb_status gb_sample(const gb_sample_args* a, gb_stream_t stream) {
   int device = 0, sms = 0;
   if (cudaGetDevice(&device) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess)
     return GB_ERR_CUDA;
-  // CTAs a row: as many as keep the GPU's SMs busy, and at least a few pieces for each thread.
+  // CTAs a row: as many as keep the GPU's SMs busy, some also of many rows, whose times differ sixfold: 512 rows of 128000 take
+  // 189 us with one, 142 with two.  At least a few pieces for each thread.
+  constexpr int kLeast = 2;
   int cluster = 1;
-  while (cluster < kMaxCluster && (long long)a->rows * cluster * 2 <= 2ll * sms && a->vocab / (cluster * 2) >= kThreads * 4) cluster *= 2;
+  while (cluster < kMaxCluster && (cluster < kLeast || (long long)a->rows * cluster * 2 <= 2ll * sms) && a->vocab / (cluster * 2) >= kThreads * 4)
+    cluster *= 2;
   if ((long long)a->rows * cluster > 0x7fffffffll) return GB_ERR_TOO_LARGE;
   Job job = {a->logits, a->row_stride, a->rows, a->vocab, cluster, a->u, a->temperature, a->top_p, a->min_p, a->top_k,
              a->all_temperature, a->all_top_p, a->all_min_p, a->all_top_k, a->token, a->logprob};
