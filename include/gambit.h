@@ -186,8 +186,8 @@ gb_status gb_append_kv(gb_pool* pool, int layer, int n_tokens, const void* k_dev
  *   (a cos - b sin, b cos + a sin) of the pair's angle at t,
  * where the pairs are the values (i, i + rotary_dim / 2), or (2i, 2i + 1) when interleaved, of each head's first rotary_dim
  * values; the rest stay.  Each result is rounded once, to the type that it goes on in (the cache's, the query's).
- *   table_dev: fp32 [positions][rotary_dim / 2][4], 16-byte aligned: cos, its rounding error (the exact value minus the
- *              rounded one, rounded), sin, its rounding error; any angles, and amplitudes too, as the caller fills it
+ *   table_dev: fp32 [positions][4][rotary_dim / 2], 16-byte aligned: cos, its rounding errors (the exact values minus the
+ *              rounded ones, rounded), sin, its rounding errors; any angles, and amplitudes too, as the caller fills it
  *   rotary_dim: a multiple of 16, at most head_dim
  * A token at a position that the table does not have is not rotated, and the device status records GB_ERR_INVALID.
  */

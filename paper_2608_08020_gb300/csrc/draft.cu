@@ -1230,7 +1230,8 @@ __global__ void __launch_bounds__(256) k_cow_rows(PoolView v) {
 }  // namespace
 
 void launch_cow_rows(gb_pool* pool, cudaStream_t s) {
-  launch_pdl(k_cow_rows, dim3(std::min(pool->cfg.max_beams, 64), pool->cfg.num_layers), 256, 0, s, pool->view);
+  const int most = std::max(1, (4 * pool->num_sms + pool->cfg.num_layers - 1) / pool->cfg.num_layers);
+  launch_pdl(k_cow_rows, dim3(std::min(pool->cfg.max_beams, most), pool->cfg.num_layers), 256, 0, s, pool->view);
   pool->launches += 1;
 }
 

@@ -848,7 +848,7 @@ static gb_status rotation_view(gb_pool* pool, const gb_rotation* r, RotationView
       r->rotary_dim > pool->cfg.head_dim || (r->interleaved != 0 && r->interleaved != 1))
     return fail(pool, GB_ERR_INVALID, "rotation: bad arguments");
   if (!on_device(pool)) return fail(pool, GB_ERR_STATE, "rotation: the pool is on another device than the current one");
-  *out = {reinterpret_cast<const float4*>(r->table_dev), r->positions, r->rotary_dim / 2, r->interleaved};
+  *out = {r->table_dev, r->positions, r->rotary_dim / 2, r->interleaved};
   return GB_OK;
 }
 

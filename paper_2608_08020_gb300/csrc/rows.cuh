@@ -55,17 +55,19 @@ __device__ __forceinline__ long long exp_offset(const PoolView& v, int layer, lo
 
 // ---- rotation ----------------------------------------------------------------------------------
 
-// By value to kernels: the table [positions][half] of (cos, its rounding error, sin, its rounding error).
+// By value to kernels: the table [positions][4][half] of cos, its rounding errors, sin, its rounding errors.  Each apart, so that
+// a half warp's lanes read neighbouring values: with the four side by side a row took 32 lines of L1 a load instead of eight.
 struct RotationView {
-  const float4* table;  // nullptr: none
+  const float* table;   // nullptr: none
   int positions, half, interleaved;
 };
 
-// a cos - b sin, rounded once: the products' and the sum's rounding errors are carried along.  What follows
-// rounds to 16 or 8 bits, and a result that is off in its last place can end on the other side of a tie there.
-__device__ __forceinline__ float turn(float a, float c, float ce, float b, float s, float se) {
-  const float p = __fmul_rn(a, c), q = __fmul_rn(-b, s);
-  const float pe = __fmaf_rn(a, ce, __fmaf_rn(a, c, -p)), qe = __fmaf_rn(-b, se, __fmaf_rn(-b, s, -q));
+// a cos + g sin (g: minus the pair's other value, or it), rounded once: the products' and the sum's rounding errors are carried
+// along.  What follows rounds to 16 or 8 bits, and a result that is off in its last place can end on the other side of a tie
+// there.
+__device__ __forceinline__ float turn(float a, float c, float ce, float g, float s, float se) {
+  const float p = __fmul_rn(a, c), q = __fmul_rn(g, s);
+  const float pe = __fmaf_rn(a, ce, __fmaf_rn(a, c, -p)), qe = __fmaf_rn(g, se, __fmaf_rn(g, s, -q));
   const float d = __fadd_rn(p, q), t = __fsub_rn(d, p);
   const float err = __fadd_rn(__fsub_rn(p, __fsub_rn(d, t)), __fsub_rn(q, t));
   return __fadd_rn(d, __fadd_rn(err, __fadd_rn(pe, qe)));
@@ -105,6 +107,29 @@ __device__ __forceinline__ uint4 row_bits(const float (&f)[RowTraits<DT>::N]) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// The M angles from i0 on of a position (i0: a multiple of M).
+template <int M>
+__device__ __forceinline__ void angles(const RotationView& rot, int pos, int i0, float (&c)[4][M]) {
+  const float* t = rot.table + (size_t)pos * 4 * rot.half + i0;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    if constexpr (M == 2) {
+      const float2 x = __ldg(reinterpret_cast<const float2*>(t + k * rot.half));
+      c[k][0] = x.x;
+      c[k][1] = x.y;
+    } else {
+#pragma unroll
+      for (int i = 0; i < M; i += 4) {
+        const float4 x = __ldg(reinterpret_cast<const float4*>(t + k * rot.half + i));
+        c[k][i] = x.x;
+        c[k][i + 1] = x.y;
+        c[k][i + 2] = x.z;
+        c[k][i + 3] = x.w;
+      }
+    }
+  }
+}
+
 // Turn the row that lanes 16h .. 16h + 15 hold (h: this lane's half of the warp) to position pos.  Every lane of
 // the warp calls it; pos may differ between the halves.  A position past the table leaves the row as it is.
 template <int DT>
@@ -115,13 +140,13 @@ __device__ __forceinline__ void turn_row(float (&f)[RowTraits<DT>::N], const Rot
   if (rot.interleaved) {
     const int i0 = N / 2 * j;                        // this lane's first pair
     if (in && i0 < rot.half) {
-      const float4* t = rot.table + (size_t)pos * rot.half + i0;
+      float c[4][N / 2];
+      angles(rot, pos, i0, c);
 #pragma unroll
       for (int i = 0; i < N / 2; ++i) {
-        const float4 cs = __ldg(t + i);
         const float a = f[2 * i], b = f[2 * i + 1];
-        f[2 * i] = turn(a, cs.x, cs.y, b, cs.z, cs.w);
-        f[2 * i + 1] = turn(b, cs.x, cs.y, -a, cs.z, cs.w);
+        f[2 * i] = turn(a, c[0][i], c[1][i], -b, c[2][i], c[3][i]);
+        f[2 * i + 1] = turn(b, c[0][i], c[1][i], a, c[2][i], c[3][i]);
       }
     }
     return;
@@ -133,12 +158,10 @@ __device__ __forceinline__ void turn_row(float (&f)[RowTraits<DT>::N], const Rot
 #pragma unroll
   for (int i = 0; i < N; ++i) g[i] = __shfl_sync(0xffffffffu, f[i], from);
   if (in && turns) {
-    const float4* t = rot.table + (size_t)pos * rot.half + N * (low ? j : j - away);
+    float c[4][N];
+    angles(rot, pos, N * (low ? j : j - away), c);
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const float4 cs = __ldg(t + i);
-      f[i] = turn(f[i], cs.x, cs.y, low ? g[i] : -g[i], cs.z, cs.w);
-    }
+    for (int i = 0; i < N; ++i) f[i] = turn(f[i], c[0][i], c[1][i], low ? -g[i] : g[i], c[2][i], c[3][i]);
   }
 }
 

@@ -73,10 +73,10 @@ class BeamPool:
         them, each [n_tokens][max_beams][kv heads][head_dim]; zeros where a slot has no such token.  They belong to `stream`,
         which has to be a torch.cuda.Stream or None."""
         c = self.cfg
-        make = lambda: torch.empty(2, n_tokens, self.max_beams, c.num_kv_heads, c.head_dim, dtype=TORCH_DT[self.kv_dtype],  # noqa: E731
+        make = lambda: torch.empty((n_tokens, self.max_beams, c.num_kv_heads, c.head_dim), dtype=TORCH_DT[self.kv_dtype],  # noqa: E731
                                    device=self.device)
         first = self._slots("first", first)
-        k, v = make() if stream is None else B.new_on(stream, make)
+        k, v = (make(), make()) if stream is None else B.new_on(stream, lambda: (make(), make()))
         B.gb_read_kv(self.handle, layer, first, n_tokens, k, v, stream)
         return k, v
 

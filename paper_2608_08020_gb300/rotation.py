@@ -32,13 +32,13 @@ class Rotation:
         self.head_dim, self.rotary_dim, self.max_positions, self.interleaved = head_dim, r, max_positions, bool(interleaved)
         # (cos, its rounding error, sin, its rounding error): the angles of far positions need 64 bits, and results are
         # rounded to 16 or 8 bits once, which a table of 32 bits alone would move across ties.
-        self.table = torch.empty(max_positions, r // 2, 4, dtype=torch.float32, device=self.device)
+        self.table = torch.empty(max_positions, 4, r // 2, dtype=torch.float32, device=self.device)
         for at in range(0, max_positions, 1 << 16):
             part = self.table[at:at + (1 << 16)]
             angle = torch.arange(at, at + part.shape[0], dtype=torch.float64, device=self.device)[:, None] * f
             for i, exact in enumerate((angle.cos() * amplitude, angle.sin() * amplitude)):
-                part[..., 2 * i] = exact
-                part[..., 2 * i + 1] = exact - part[..., 2 * i].double()
+                part[:, 2 * i] = exact
+                part[:, 2 * i + 1] = exact - part[:, 2 * i].double()
         self.device = self.table.device
         if self.device.type == "cuda" and not torch.cuda.is_current_stream_capturing():
             torch.cuda.current_stream(self.device).synchronize()       # calls may be on any stream

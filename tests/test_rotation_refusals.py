@@ -24,12 +24,12 @@ def test_rotation_table():
     r = Rotation(128, max_positions=70000, base=1e4, rotary_dim=32, amplitude=0.5, device="cpu")
     t = torch.arange(70000, dtype=torch.float64)[:, None] * 1e4 ** (-torch.arange(0, 32, 2, dtype=torch.float64) / 32)
     table = r.table.double()
-    assert r.table.shape == (70000, 16, 4)
+    assert r.table.shape == (70000, 4, 16)
     # Two fp32 terms: the second is rounded to 2^-24 of the first's rounding error, 2^-25 of the value.
-    assert ((table[..., 0] + table[..., 1]) - 0.5 * t.cos()).abs().max() <= 2.0 ** -49
-    assert ((table[..., 2] + table[..., 3]) - 0.5 * t.sin()).abs().max() <= 2.0 ** -49
+    assert ((table[:, 0] + table[:, 1]) - 0.5 * t.cos()).abs().max() <= 2.0 ** -49
+    assert ((table[:, 2] + table[:, 3]) - 0.5 * t.sin()).abs().max() <= 2.0 ** -49
     f = Rotation(64, max_positions=3, frequencies=torch.arange(32), device="cpu")
-    assert torch.allclose(f.table[2, 3, 0], torch.tensor(6.0).cos())
+    assert torch.allclose(f.table[2, 0, 3], torch.tensor(6.0).cos())
 
 
 @pytest.mark.parametrize("g,d,ok", [(1, 128, True), (2, 128, True), (4, 128, True), (8, 128, True), (16, 128, False), (3, 128, False),
