@@ -219,8 +219,8 @@ __device__ __forceinline__ void combine_shares(const PoolView& v, const Counters
     } else {
       good = wait_pair_records(v, cnt, p, npb, nseg > 0 ? ng : 0);
       if (good) {
-        merge_fold(st, prec, rf, npb);
-        merge_fold(st, grec, (size_t)v.Hkv * rf, nseg);
+#pragma unroll 1
+        for (int s = 0; s < 2; ++s) merge_fold(st, s ? grec : prec, s ? (size_t)v.Hkv * rf : rf, s ? nseg : npb);
       }
     }
     if (good) {

@@ -314,12 +314,14 @@ __device__ __forceinline__ Shares shares_of(const PoolView& v, int mode, int nac
   s.per = max(1, (total + ctas - 1) / ctas);
   if (s.per > 160) s.per = (s.per + 3) / 4;
   s.count = (total + s.per - 1) / s.per;
-  if (mode == 0) {
+  if (mode == 1) {  // whoever is done with its segments takes the next one
+    s.pairs = total <= 64ll * pairs;
+  } else {
     // Chunks that pass a CTA, and a unit's start and merge as so many more.
     const int whole = (pairs + ctas - 1) / ctas * ((total + pairs - 1) / pairs + 16), even = (total + ctas - 1) / ctas + 48;
     s.pairs = whole <= even;
-    if (s.pairs) s.count = v.max_beams * v.Hkv;
   }
+  if (s.pairs) s.count = v.max_beams * v.Hkv;
   return s;
 }
 
@@ -496,12 +498,13 @@ __device__ void plan_units(const PoolView& v, const Counters& cnt, int mode, con
     }
     pl.publish();
   };
-  // The first share is the CTA's own, the others are whoever's comes first.
-  int pending = (int)blockIdx.x;
+  // The first share is the CTA's own, the others are whoever's comes first; behind segments, all of them.
+  const int own = mode == 1 ? 0 : (int)gridDim.x;
+  int pending = own ? (int)blockIdx.x : claim(kCntRange);
   while (pl.ok) {
     const int u = __shfl_sync(0xffffffffu, pending, 0);
     if (u >= sh.count) break;
-    if (sh.count > (int)gridDim.x) pending = (int)gridDim.x + claim(kCntRange);
+    if (sh.count > own) pending = own + claim(kCntRange);
     else pending = sh.count;
     if (sh.pairs) {
       const int b = u / v.Hkv;
@@ -573,11 +576,26 @@ __device__ __forceinline__ void multiply(const PoolView& v, const Unit8& u, cons
     });
   }
   tile_finish(t);
+  const uint64_t pol = policy_evict_last();  // the launch's merge reads the records back from L2
+  if (groups == 1) {                         // nobody else has these rows
+#pragma unroll
+    for (int z = 0; z < 2; ++z) {
+      const int row = rg * 8 + 2 * c + z;
+      if (row >= u.rows) continue;
+      float* rec = row_record<G>(v, u, row);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) st_hint4(rec + row % G * 128 + 16 * r + 4 * i, tile_dims(t, i, z), pol);
+      if (r == 0) {
+        st_hint(rec + G * 128 + row % G, z ? t.m1 : t.m0, pol);
+        st_hint(rec + G * 128 + G + row % G, z ? t.l1 : t.l0, pol);
+      }
+    }
+    return;
+  }
   // The warps' states of the same rows, merged through shared memory four rows of each at a time.
   float* left = reinterpret_cast<float*>(smem + Smem8::MERGE);
   float2* ml = reinterpret_cast<float2*>(smem + Smem8::STATE);
-  const uint64_t pol = policy_evict_last();  // the launch's merge reads the records back from L2
-#pragma unroll
+#pragma unroll 1
   for (int f = 0; f < 2; ++f) {
     if (f > 0 && 4 * f >= u.rows) break;
     if (c >> 1 == f) {
@@ -667,11 +685,22 @@ template <int G>
 __global__ void __launch_bounds__(kThreads8, 1)
     k_decode8(PoolView v, const __grid_constant__ CUtensorMap tm, int layer, const __nv_bfloat16* q, float qscale, int mode,
               float* __restrict__ out) {
-  pdl_wait();
-  pdl_launch_dependents();
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   unsigned char* smem = smem_raw + ((1024 - (smem_addr(smem_raw) & 1023)) & 1023);
   const int cta = (int)blockIdx.x, nctas = (int)gridDim.x, tid = threadIdx.x;
+  const uint32_t bars = smem_addr(smem) + Smem8::BARS;
+  if (tid < kStages8) {
+    mbar_init(bars + 8 * tid, 2);
+    mbar_init(bars + 8 * (kStages8 + tid), kConsumers8);
+  }
+  if (tid < kSlots8) {
+    mbar_init(bars + 8 * (2 * kStages8 + tid), 1);
+    mbar_init(bars + 8 * (2 * kStages8 + kSlots8 + tid), kConsumers8 + kLoaders8);
+  }
+  if (tid == 0) *reinterpret_cast<volatile int*>(smem + Smem8::STOP) = 0;
+  if (tid < 32) fence_mbar_init();
+  pdl_wait();
+  pdl_launch_dependents();
   const int step_ok = v.ctl[kCtlStepOk], steps = v.ctl[kCtlSteps], nact = v.ctl[kCtlActive];
   if (step_ok == 0) {
     zero_all_pairs<G>(v, cta, nctas, out);
@@ -680,18 +709,18 @@ __global__ void __launch_bounds__(kThreads8, 1)
   const int set = counter_set(v, layer, steps);
   const Counters cnt = counters(v, set);
   zero_counters(v, set ^ 1, cta, nctas);
-  // mode 1: by segments; mode 2: by segments where that pays.  A segment's pages are read once for all of its members,
-  // but the multiplying warps do as much for a row either way, except that two or more members with few heads fill a tile that
-  // one would leave half empty.  So it pays where beams of up to 4 heads a KV head read far more than there is (us, beams alone /
-  // segments; MB read alone / there): 283 / 219 (1600 / 673, 128 x 6100), 281 / 229 (1844 / 491, 300 x 3000, G = 2); not 118 / 124
-  // (525 / 185, 64 x 4000), 146 / 156 (577 / 188, 256 x 1100), 283 / 438 (1623 / 359, 198 x 8000, G = 8).
+  // mode 1: by segments; mode 2: by segments where that pays.  A segment's pages are read once for all of its members, but a
+  // tile's step takes a warp as long for members as for a beam alone, and the records more to merge.  So it pays where beams of up
+  // to 4 heads a KV head, two or more of which fill a tile that one would leave half empty, read far more than there is (us, beams
+  // alone / segments; MB read alone / there): 115 / 99 (525 / 185, 64 x 4000), 278 / 195 (1600 / 673, 128 x 6100), 185 / 138 (1024 /
+  // 369, 200 x 2500, G = 2), 109 / 98 (410 / 142, 100 x 2000); not 85 / 86 (328 / 109, 40 x 4000), 93 / 110 (164 / 61, 256 x 313), 278 /
+  // 290 (1623 / 359, 198 x 8000, G = 8).
   if (v.ctl[kCtlSegTiles] == 0) mode = 0;
   if (mode == 2) {
     const long long all = (long long)plan_off(v, 0)[v.max_beams] * kChunkBytes8;
     const long long there = plan_off(v, 1)[v.max_beams] * (long long)kChunkBytes8 + (long long)v.ctl[kCtlSegTok] * v.Hkv * (kChunkBytes8 / kChunk);
-    mode = G <= 4 && 5 * all - 6 * there > 3500000000ll ? 1 : 0;
+    mode = G <= 4 && all - there > 260000000ll ? 1 : 0;
   }
-  const uint32_t bars = smem_addr(smem) + Smem8::BARS;
   {
     int* s_off = reinterpret_cast<int*>(smem + Smem8::PLAN);
     const int* off = plan_off(v, mode);
@@ -700,18 +729,6 @@ __global__ void __launch_bounds__(kThreads8, 1)
       s_off[i] = off[i];
       s_off[i + kMaxBeams + 1] = i < v.max_beams ? nn[i] : 0;
     }
-  }
-  if (tid == 0) {
-    for (int s = 0; s < kStages8; ++s) {
-      mbar_init(bars + 8 * s, 2);
-      mbar_init(bars + 8 * (kStages8 + s), kConsumers8);
-    }
-    for (int s = 0; s < kSlots8; ++s) {
-      mbar_init(bars + 8 * (2 * kStages8 + s), 1);
-      mbar_init(bars + 8 * (2 * kStages8 + kSlots8 + s), kConsumers8 + kLoaders8);
-    }
-    *reinterpret_cast<volatile int*>(smem + Smem8::STOP) = 0;
-    fence_mbar_init();
   }
   __syncthreads();
   const Shares sh = shares_of(v, mode, nact, reinterpret_cast<const int*>(smem + Smem8::PLAN)[v.max_beams], nctas);
