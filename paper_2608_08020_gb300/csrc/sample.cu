@@ -249,6 +249,7 @@ struct Smem {
   float queue[kWarps][64 + 32 * 8];      // logits that wait for their weights
   u64 order[kRanked];                    // tokens to be ranked, (key from above, index), and their weights
   u64 ranked[kRanked];
+  Entry places[kRanked];                 // a short list in order
   uint32_t slice[kSlices];               // masses by slice, see top_p_list
   uint32_t hist[1 + kDigits][kBins];     // counts, then the masses' digits
   u64 total[kBins];
@@ -546,6 +547,29 @@ struct RowCtas {
     return t;
   }
 
+  // The sum of the threads' before this one, and of all.
+  __device__ u64 block_before(u64 s, u64* all) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    u64 inc = s;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const u64 y = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += y;
+    }
+    if (lane == 31) sm.red64[warp] = inc;
+    __syncthreads();
+    u64 before = inc - s, t = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      const u64 x = sm.red64[w];
+      before += w < warp ? x : 0;
+      t += x;
+    }
+    *all = t;
+    __syncthreads();
+    return before;
+  }
+
   // Room for the warp's `mine` entries each in this CTA's list.
   __device__ __forceinline__ int reserve(int mine) const {
     const int lane = threadIdx.x & 31;
@@ -824,50 +848,46 @@ struct RowCtas {
   // mass of what is kept.
   __device__ int draw_listed(int n, int k, float p, u64 all, float u, u64* mass) {
     if (n <= kRanked) {
-      // Every entry's rank and the mass before it, by comparing every two: some threads an entry.
-      for (int j = threadIdx.x; j < n; j += kThreads) {
-        const Entry e = sm.list[j];
-        sm.weights[j] = weight(row, sm.table, e.x);
-        sm.order[j] = (u64)~key_of(e.x) << 32 | (unsigned)e.i;
+      // Every entry's rank, by comparing every two, puts it in its place; the masses before the places say what is kept.
+      if (threadIdx.x < n) {
+        const Entry e = sm.list[threadIdx.x];
+        sm.order[threadIdx.x] = (u64)~key_of(e.x) << 32 | (unsigned)e.i;
       }
-      if (threadIdx.x == 0) sm.token = -1;
+      if (threadIdx.x == 0) {
+        sm.ranks = 0;
+        sm.token = -1;
+      }
       __syncthreads();
       const int shift = n <= kRanked / 4 ? 3 : n <= kRanked / 2 ? 2 : 1, ways = 1 << shift;
       const int j = threadIdx.x >> shift, way = threadIdx.x & (ways - 1);
-      const bool there = j < n, first = there && way == 0;
-      const u64 own = sm.order[there ? j : 0], w = there ? sm.weights[j] : 0;
-      int rank_in = 0;
-      u64 before = 0;
-#pragma unroll 4
-      for (int z = way; z < n; z += ways) {
-        const bool c = sm.order[z] < own;
-        const u64 wz = sm.weights[z];
-        rank_in += c ? 1 : 0;
-        before += c ? wz : 0;
-      }
-      for (int o = 1; o < ways; o <<= 1) {
-        rank_in += __shfl_xor_sync(0xffffffffu, rank_in, o);
-        before += __shfl_xor_sync(0xffffffffu, before, o);
-      }
-      bool in = there && (k < 1 || rank_in < k);
+      const u64 own = sm.order[j < n ? j : 0];
+      int place = 0;
+#pragma unroll 8
+      for (int z = way; z < n; z += ways) place += sm.order[z] < own ? 1 : 0;
+      for (int o = 1; o < ways; o <<= 1) place += __shfl_xor_sync(0xffffffffu, place, o);
+      if (j < n && way == 0) sm.places[place] = sm.list[j];
+      __syncthreads();
+      const int some = k < 1 ? n : min(n, k);
+      const bool there = (int)threadIdx.x < some;
+      const Entry e = sm.places[there ? threadIdx.x : 0];
+      const u64 w = there ? weight(row, sm.table, e.x) : 0;
+      u64 sum;
+      const u64 before = block_before(w, &sum);
       if (p < 1.f) {
-        if (all == 0) all = block_sum(in && first ? w : 0);
-        in = in && before < share(p, all);
+        const u64 to = share(p, all ? all : sum);
+        const bool in = there && before < to;
+        if (in) to_rank((u64)(unsigned)e.i, w);
+        sum = block_sum(in ? w : 0);
+      } else {
+        if (there) to_rank((u64)(unsigned)e.i, w);
+        __syncthreads();
       }
-      const u64 total = block_sum(in && first ? w : 0);
-      if (first) sm.weights[j] = in ? w : 0;
+      const u64 at = draw_at(u, sum);
+      rank_each([&](int z, u64 passed, u64 own_w) {
+        if (passed <= at && at < passed + own_w) sm.token = (int)sm.order[z];
+      });
       __syncthreads();
-      const u64 at = draw_at(u, total);
-      u64 passed = 0;
-#pragma unroll 4
-      for (int z = way; z < n; z += ways) {
-        const u64 wz = sm.weights[z];
-        passed += (uint32_t)sm.order[z] < (uint32_t)own ? wz : 0;
-      }
-      for (int o = 1; o < ways; o <<= 1) passed += __shfl_xor_sync(0xffffffffu, passed, o);
-      if (in && first && passed <= at && at < passed + w) sm.token = (int)(uint32_t)own;
-      __syncthreads();
-      *mass = total;
+      *mass = sum;
       return sm.token;
     }
     Head head = {0u, 0x7fffffff};
