@@ -21,11 +21,16 @@
 // interleaved in pairs by byte permutes: 8 loads, 64 conversions, 16 permutes and 24 products a chunk and tile.
 //
 // Work.  A unit is a run of chunks of one head's pages with the query rows that see them: a beam's own (its G heads), or a
-// shared segment's (up to 128 rows of its members; the lists that the grouped path of bf16 pools uses).  A CTA has a warp that
+// shared segment's (up to 64 rows of its members; the lists that the grouped path of bf16 pools uses).  A CTA has a warp that
 // takes units from the launch's counters, two that stream their chunks through a ring, two chunks a stage, and
-// eight warps that share out a unit: row groups of 16 rows, and where those are fewer than eight, groups of stages
+// eight warps that share out a unit: row groups of 8 rows, and where those are fewer than eight, groups of stages
 // among the warps of a row group, whose softmax states are merged in shared memory when the unit ends.  Units' records are
 // merged at the end of the launch (combine.cuh); a beam whose whole context was one unit is written at once.
+//
+// What bounds it (a launch alone, one layer): unshared caches, memory: 64 x 16384 tokens in 385 us, 5.6 TB/s; the same bytes from
+// L2 in 313 (6.7 TB/s: what two warps' copies of 4 KiB bring in).  Segments, the products, of which a tile of 8 rows takes 48 for 32
+// tokens, 0.056 us of an SM's: with twelve warps, or two tiles a warp that share their conversions, as much.  Small calls, a chain:
+// barriers, plan, page ids and exponents, first chunks, merge: 13-15 us cold for 8 or 13 beams, 2.5 of them before the first copy.
 #include <atomic>
 
 #include "decode_mma.cuh"

@@ -141,7 +141,8 @@ __device__ __forceinline__ void turn_queries(const PoolView& v, const RotationVi
 // n_tokens new rows of every active slot at positions [seq_len - n_tokens, seq_len) of one layer, like k_append, but
 // turned on the way, or held in 8 bits; and, with q, the slots' queries turned to the last of these positions.
 // kin/vin: [n_tokens][max_beams][Hkv] rows of 256 bytes.  Two warps take a block of 16 positions of `heads` heads of
-// K or V (heads divides Hkv), one after the other so that the rotation's table comes from L1.
+// K or V (heads divides Hkv), one after the other so that the rotation's table comes from L1.  256 slots x 199 tokens x 8 heads
+// in 8 bits: 73 us (208 MB in, 104 out, 4.3 TB/s), 115 turned: 13 operations a value, half of the issue slots, 16 warps an SM.
 template <int DT, bool E8>
 __global__ void __launch_bounds__(32 * kCtaWarps, 2) k_append_rows(PoolView v, int layer, int n_tokens, int heads, RotationView rot, const char* kin,
                                                      const char* vin, const uint4* q, uint4* qout) {
@@ -237,7 +238,8 @@ __global__ void __launch_bounds__(32 * kCtaWarps, 2) k_seed_rows8(PoolView v, in
 }
 
 // Tokens first[b] .. first[b] + n - 1 of every slot as the cache holds them, in the type that rows are given in;
-// zeros where a slot has no such token.  A warp takes a block of 16 positions of a (K|V, head), two rows at a time.
+// zeros where a slot has no such token.  A warp takes a block of 16 positions of a (K|V, head), two rows at a time: memory, 256
+// slots x 199 tokens x 8 heads of 8 bits in 52 us (6.0 TB/s; 16 bytes a thread, with a page lookup each, took 165).
 template <bool E8>
 __global__ void __launch_bounds__(256) k_read_kv(PoolView v, int layer, const int* first, int n, uint4* kout, uint4* vout) {
   pdl_wait();
