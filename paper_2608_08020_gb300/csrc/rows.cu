@@ -308,8 +308,8 @@ cudaError_t launch_append_rows(gb_pool* pool, int layer, int n_tokens, const Rot
   const int blks = (n_tokens + 2 * kBlockRows - 2) / kBlockRows;  // at most, of a slot
   // Heads one after the other where there are blocks enough without (two CTAs an SM), else side by side.
   int heads = v.Hkv;
-  while (heads % 2 == 0 && (long long)blks * v.max_beams * 2 * (v.Hkv / heads) < 2ll * kTeams * 2 * pool->num_sms) heads /= 2;
-  if ((long long)blks * v.max_beams * 2 * (v.Hkv / heads) < 2ll * kTeams * 2 * pool->num_sms) heads = 1;
+  while (heads % 2 == 0 && (long long)blks * v.max_beams * 2 * (v.Hkv / heads) < (long long)kTeams * 2 * pool->num_sms) heads /= 2;
+  if ((long long)blks * v.max_beams * 2 * (v.Hkv / heads) < (long long)kTeams * 2 * pool->num_sms) heads = 1;
   const long long units = (long long)blks * 2 * (v.Hkv / heads) + (q ? (v.Hq + 2 * kBlockWarps - 1) / (2 * kBlockWarps) : 0);
   const dim3 grid(v.max_beams, (unsigned)std::min((units + kTeams - 1) / kTeams, 65535ll));
   pool->launches += 1;
