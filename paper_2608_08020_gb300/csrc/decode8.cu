@@ -57,10 +57,11 @@ constexpr int kRowFloats8 = 132;                   // of a row in the merge's me
 enum UnitKind : int { kUnitEnd = 0, kUnitBeam = 1, kUnitSegment = 2 };
 struct Unit8 {
   int kind, head, tokens, rows;
-  int record;    // beam: the record's index; segment: the split
+  int record;    // beam: the record's index
   int direct;    // beam: its only record, so its output
   int source, tok0, again;  // whose table, the first token there, whether others read the pages too
-  int members[kRows8];  // the rows' beams; segment: x kMaxSegDepth + depth
+  int members[kRows8];  // the rows' beams
+  int records[kRows8];  // segment: their records (of grec, in all heads)
 };
 
 struct Smem8 {
@@ -146,17 +147,21 @@ struct Tile8 {
   float m0, m1, l0, l1;
 };
 
-// row: this lane's query row (128 bf16), or nullptr for a column without one.
-__device__ __forceinline__ void tile_begin(Tile8& t, const __nv_bfloat16* row, float qscale, int c) {
-  uint32_t w[16];
+// This lane's part of a query row (128 bf16; nullptr: zeros), into the tile's own registers until tile_begin.
+__device__ __forceinline__ void tile_load(Tile8& t, const __nv_bfloat16* row, int c) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const uint4 x = row ? *reinterpret_cast<const uint4*>(row + 32 * c + 8 * i) : make_uint4(0u, 0u, 0u, 0u);
-    w[4 * i] = x.x;
-    w[4 * i + 1] = x.y;
-    w[4 * i + 2] = x.z;
-    w[4 * i + 3] = x.w;
+    t.q[2 * i][0] = x.x;
+    t.q[2 * i][1] = x.y;
+    t.q[2 * i + 1][0] = x.z;
+    t.q[2 * i + 1][1] = x.w;
   }
+}
+__device__ __forceinline__ void tile_begin(Tile8& t, float qscale, int c) {
+  uint32_t w[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) w[i] = t.q[i >> 1][i & 1];
   float amax = 0.f;
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
@@ -470,13 +475,16 @@ __device__ void plan_units(const PoolView& v, const Counters& cnt, int mode, con
       if (have <= 0) continue;
       Unit8* x = pl.slot();
       if (!pl.ok) break;
-      for (int m = lane; m < have; m += 32) x->members[m] = v.seg_members[moff + m0 + m];
+      for (int m = lane; m < have; m += 32) {
+        const int e = v.seg_members[moff + m0 + m], b = e / kMaxSegDepth;
+        x->members[m] = b;
+        x->records[m] = b * kMaxSegRecords + v.seg_rec_off[e] + sp;
+      }
       if (lane == 0) {
         x->kind = kUnitSegment;
         x->head = h;
         x->tokens = tokens;
         x->rows = have * G;
-        x->record = sp;
         x->source = rep;
         x->tok0 = v.seg_i0[s] * v.P + tok0;
         x->again = g > members;
@@ -543,43 +551,50 @@ __device__ void plan_units(const PoolView& v, const Counters& cnt, int mode, con
 template <int G>
 __device__ __forceinline__ float* row_record(const PoolView& v, const Unit8& u, int row) {
   if (u.kind == kUnitBeam) return v.partials + (size_t)u.record * v.record_floats;
-  const int e = u.members[row / G], b = e / kMaxSegDepth;
-  return v.grec + (((size_t)b * kMaxSegRecords + v.seg_rec_off[e] + u.record) * v.Hkv + u.head) * v.record_floats;
+  return v.grec + ((size_t)u.records[row / G] * v.Hkv + u.head) * v.record_floats;
 }
 
-// One unit by the multiplying warps: row groups of 8 rows (1, 2, 4 or 8), and in each as many groups of stages as there are
-// warps for it.  A warp whose wait ran out still keeps step with the others; what the unit then leaves is nobody's, as the
-// status is set.
+// How the multiplying warps share out a unit: row groups of 8 rows (1, 2, 4 or 8), and in each as many groups of stages as
+// there are warps for it.
+__device__ __forceinline__ int row_groups(int rows) { return rows <= 8 ? 1 : rows <= 16 ? 2 : rows <= 32 ? 4 : 8; }
+
+// This warp's query rows of a unit, on their way.
 template <int G>
-__device__ __forceinline__ void multiply(const PoolView& v, const Unit8& u, const __nv_bfloat16* q, float qscale, uint32_t base,
-                                         uint32_t bars, unsigned char* smem, float* out) {
+__device__ __forceinline__ void load_queries(Tile8& t, const PoolView& v, const Unit8& u, const __nv_bfloat16* q, int warp, int r, int c) {
+  if (u.kind == kUnitEnd) return;
+  const int row = warp % row_groups(u.rows) * 8 + r;
+  tile_load(t, row < u.rows ? q + ((size_t)u.members[row / G] * v.Hq + (size_t)u.head * G + row % G) * 128 : nullptr, c);
+}
+
+// One unit by the multiplying warps.  A warp whose wait ran out still keeps step with the others; what the unit then leaves is
+// nobody's, as the status is set.  next(): called when the queries are no longer needed.
+template <int G, class Next>
+__device__ __forceinline__ void multiply(Tile8& t, const PoolView& v, const Unit8& u, float qscale, uint32_t base, uint32_t bars,
+                                         unsigned char* smem, float* out, Next next) {
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = lane >> 2, c = lane & 3;
   const uint32_t full = bars, empty = bars + 8 * kStages8, ring = smem_addr(smem);
   volatile int* stop = reinterpret_cast<volatile int*>(smem + Smem8::STOP);
-  const int rgroups = u.rows <= 8 ? 1 : u.rows <= 16 ? 2 : u.rows <= 32 ? 4 : 8, groups = kConsumers8 / rgroups;
-  const int rg = warp % rgroups, group = warp / rgroups;
-  Tile8 t;
-  {
-    const int row = rg * 8 + r;
-    const __nv_bfloat16* at = nullptr;
-    if (row < u.rows) {
-      const int e = u.members[row / G], b = u.kind == kUnitBeam ? e : e / kMaxSegDepth;
-      at = q + ((size_t)b * v.Hq + (size_t)u.head * G + row % G) * 128;
-    }
-    tile_begin(t, at, qscale, c);
-  }
+  const int rgroups = row_groups(u.rows), groups = kConsumers8 / rgroups, rg = warp % rgroups, group = warp / rgroups;
+  tile_begin(t, qscale, c);
   const int stages = (u.tokens + 2 * kChunk - 1) / (2 * kChunk);
+  const bool any = rg * 8 < u.rows;
   for (int i = group; i < stages; i += groups) {
     const uint32_t k = base + i, s = k % kStages8;
     if (!__all_sync(0xffffffffu, wait_or_stop(full + 8 * s, (k / kStages8) & 1, stop))) break;
-    const int4 e = *reinterpret_cast<const int4*>(smem + Smem8::EXPS + 16 * s);
-    const int eh[2][2] = {{e.x, e.y}, {e.z, e.w}};
-    attend(t, ring + s * kStageBytes8, min(2 * kChunk, u.tokens - i * 2 * kChunk), eh, r, c, [&] {
+    auto leave = [&] {
       __syncwarp();
       if (lane == 0) mbar_arrive_n(empty + 8 * s, groups);
       __syncwarp();
-    });
+    };
+    if (!any) {
+      leave();
+      continue;
+    }
+    const int4 e = *reinterpret_cast<const int4*>(smem + Smem8::EXPS + 16 * s);
+    const int eh[2][2] = {{e.x, e.y}, {e.z, e.w}};
+    attend(t, ring + s * kStageBytes8, min(2 * kChunk, u.tokens - i * 2 * kChunk), eh, r, c, leave);
   }
+  next();
   tile_finish(t);
   const uint64_t pol = policy_evict_last();  // the launch's merge reads the records back from L2
   if (groups == 1) {                         // nobody else has these rows
@@ -658,15 +673,22 @@ __device__ void multiply_units(const PoolView& v, const Counters& cnt, const __n
   const uint32_t ufull = bars + 16 * kStages8, uempty = ufull + 8 * kSlots8;
   volatile int* stop = reinterpret_cast<volatile int*>(smem + Smem8::STOP);
   uint32_t base = 0;       // stages of earlier units
-  bool segments = mode == 1;
+  bool segments = mode == 1, there = false;
+  const Unit8* units = reinterpret_cast<const Unit8*>(smem + Smem8::UNITS);
+  Tile8 t;
+  // Unit k's queries, asked for while the unit before it is merged (its slot is filled by then, or soon: kSlots8).
+  auto arrive_at = [&](int k) {
+    there = __all_sync(0xffffffffu, wait_or_stop(ufull + 8 * (k % kSlots8), (k / kSlots8) & 1, stop));
+    if (there) load_queries<G>(t, v, units[k % kSlots8], q, tid >> 5, lane >> 2, lane & 3);
+  };
+  arrive_at(0);
   for (int k = 0;; ++k) {
     const int slot = k % kSlots8;
-    const bool there = __all_sync(0xffffffffu, wait_or_stop(ufull + 8 * slot, (k / kSlots8) & 1, stop));
     if (consumers_any(!there || *stop != 0)) {  // all leave together
       if (tid == 0) set_status(v.ctl, GB_ERR_TIMEOUT);
       return;
     }
-    const Unit8& u = reinterpret_cast<const Unit8*>(smem + Smem8::UNITS)[slot];
+    const Unit8& u = units[slot];
     if (segments && u.kind != kUnitSegment) {  // this CTA's segment records are written
       if (tid == 0) {
         fence_acq_rel_gpu();
@@ -675,7 +697,7 @@ __device__ void multiply_units(const PoolView& v, const Counters& cnt, const __n
       segments = false;
     }
     if (u.kind == kUnitEnd) return;
-    multiply<G>(v, u, q, qscale, base, bars, smem, out);
+    multiply<G>(t, v, u, qscale, base, bars, smem, out, [&] { arrive_at(k + 1); });
     base += (u.tokens + 2 * kChunk - 1) / (2 * kChunk);
     if (tid == 0 && u.kind == kUnitBeam && !u.direct) {
       fence_acq_rel_gpu();
