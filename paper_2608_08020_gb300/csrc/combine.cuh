@@ -176,10 +176,10 @@ __device__ __forceinline__ void zero_all_pairs(const PoolView& v, int cta, int n
     zero_pair<G, D>(v, p / v.Hkv, p % v.Hkv, out);
 }
 
-// The same for shares of c chunks of the flat list (c = 0: whole pairs), by the first nw warps of each CTA.  Direct: a pair of a
+// The same for any shares of the flat list (share(x): that of chunk x), by the first nw warps of each CTA.  Direct: a pair of a
 // single record has been written.
-template <int G, bool Direct>
-__device__ __forceinline__ void combine_shares(const PoolView& v, const Counters& cnt, int mode, int c, int ng, bool claim,
+template <int G, bool Direct, class Share>
+__device__ __forceinline__ void combine_shares(const PoolView& v, const Counters& cnt, int mode, Share share, int ng, bool claim,
                                                int cta, int nctas, int nw, float* __restrict__ out) {
   constexpr int D = 128;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -199,8 +199,8 @@ __device__ __forceinline__ void combine_shares(const PoolView& v, const Counters
     const int n = act ? nn[b] : 0;
     const int nseg = (act && mode == 1 && v.grouped) ? v.seg_nrec[b] : 0;
     const int o0 = off[b] + h * n;
-    const int first = c > 0 ? o0 / c : 0;
-    const int npb = n == 0 ? 0 : c > 0 ? (o0 + n - 1) / c - first + 1 : 1;
+    const int first = n == 0 ? 0 : share(o0);
+    const int npb = n == 0 ? 0 : share(o0 + n - 1) - first + 1;
     if (Direct && npb == 1 && nseg == 0) continue;
     if (npb + nseg == 0) {
       zero_pair<G>(v, b, h, out);
@@ -242,8 +242,8 @@ __device__ __forceinline__ void combine_shares(const PoolView& v, const Counters
 template <int G>
 __device__ __forceinline__ void combine_pairs(const PoolView& v, const Counters& cnt, int mode, int W, int ng,
                                               bool claim, int cta, int nctas, float* __restrict__ out) {
-  const int Tot = plan_off(v, mode)[v.max_beams];
-  combine_shares<G, false>(v, cnt, mode, Tot > 0 ? (Tot + W - 1) / W : 1, ng, claim, cta, nctas, blockDim.x >> 5, out);
+  const int Tot = plan_off(v, mode)[v.max_beams], c = Tot > 0 ? (Tot + W - 1) / W : 1;
+  combine_shares<G, false>(v, cnt, mode, [c](int x) { return x / c; }, ng, claim, cta, nctas, blockDim.x >> 5, out);
 }
 
 // Merge w records in shared memory, `stride` floats apart, into ob[g][:]: out = sum o 2^(m - M) /

@@ -27,10 +27,11 @@
 // among the warps of a row group, whose softmax states are merged in shared memory when the unit ends.  Units' records are
 // merged at the end of the launch (combine.cuh); a beam whose whole context was one unit is written at once.
 //
-// What bounds it (a launch alone, one layer): unshared caches, memory: 64 x 16384 tokens in 385 us, 5.6 TB/s; the same bytes from
-// L2 in 313 (6.7 TB/s: what two warps' copies of 4 KiB bring in).  Segments, the products, of which a tile of 8 rows takes 48 for 32
-// tokens, 0.056 us of an SM's: with twelve warps, or two tiles a warp that share their conversions, as much.  Small calls, a chain:
-// barriers, plan, page ids and exponents, first chunks, merge: 13-15 us cold for 8 or 13 beams, 2.5 of them before the first copy.
+// What bounds it (a launch alone, one layer): unshared caches, memory: 64 x 16384 tokens in 351 us, 6.1 TB/s (without the products
+// 339).  Shared ones, the multiplying warps: the same bytes from L2 take 285 us, 7.4 TB/s, without the products 162.  A tile's 32
+// tokens are 48 products (413 cycles of a scheduler's) and 534 instructions, for which a warp takes 2100 cycles, two a scheduler; with
+// twelve warps, or two tiles a warp that share their conversions, the SM does as much.  Small calls, a chain: barriers, plan, page
+// ids and exponents, first chunks, merge: 13-15 us cold for 8 or 13 beams, 2.5 of them before the first copy.
 #include <atomic>
 
 #include "decode_mma.cuh"
@@ -213,42 +214,47 @@ __device__ __forceinline__ void take_v(uint4 (&x)[2][4], uint32_t sb, int nvalid
     }
 }
 
-// A landed stage (its first nvalid >= 1 tokens) into a tile.  e: K's and V's exponent of each chunk.  leave() gives its slot back:
-// the stage is in registers before it is multiplied, which takes a warp a microsecond.
-template <class Leave>
-__device__ __forceinline__ void attend(Tile8& u, uint32_t sb, int nvalid, const int (&e)[2][2], int r, int c, Leave leave) {
-  uint32_t w[2][2][8];
+// A landed stage (its first nvalid >= 1 tokens) into a tile.  w: its K words (take_k); e: K's and V's exponent of each chunk.
+// leave() gives its slot back; ahead() may load the next stage's K words, behind which V's products then run.
+template <class Leave, class Ahead>
+__device__ __forceinline__ void attend(Tile8& u, const uint32_t (&w)[2][2][8], uint32_t sb, int nvalid, const int (&e)[2][2], int r, int c,
+                                       Leave leave, Ahead ahead) {
   uint4 x[2][4];
-  take_k(w, sb, r, c);
   take_v(x, sb, nvalid, r, c);
-  leave();
   float y[2][4];
+  {
+    float s[2][2][4];  // two independent sums a chunk: a product waits for the one before it for as long as four others take
 #pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    float s[2][4];  // two independent sums
+    for (int k = 0; k < 2; ++k)
 #pragma unroll
-    for (int z = 0; z < 4; ++z) s[0][z] = s[1][z] = 0.f;
+      for (int z = 0; z < 4; ++z) s[k][0][z] = s[k][1][z] = 0.f;
 #pragma unroll
     for (int j = 0; j < 8; ++j)
-      mma_f16(s[j & 1], f16x2_of_e4m3x2(w[k][0][j]), f16x2_of_e4m3x2(w[k][1][j]), f16x2_of_e4m3x2(w[k][0][j] >> 16),
-              f16x2_of_e4m3x2(w[k][1][j] >> 16), u.q[j][0], u.q[j][1]);
-    const float ks = pow2i(e[k][0]), k0 = u.s0 * ks, k1 = u.s1 * ks, add = (float)e[k][1];
 #pragma unroll
-    for (int z = 0; z < 4; ++z) y[k][z] = fmaf(s[0][z] + s[1][z], z & 1 ? k1 : k0, add);
-    if (nvalid < 2 * kChunk) {
-      if (16 * k + r >= nvalid) y[k][0] = y[k][1] = -INFINITY;
-      if (16 * k + r + 8 >= nvalid) y[k][2] = y[k][3] = -INFINITY;
+      for (int k = 0; k < 2; ++k)
+        mma_f16(s[k][j & 1], f16x2_of_e4m3x2(w[k][0][j]), f16x2_of_e4m3x2(w[k][1][j]), f16x2_of_e4m3x2(w[k][0][j] >> 16),
+                f16x2_of_e4m3x2(w[k][1][j] >> 16), u.q[j][0], u.q[j][1]);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const float ks = pow2i(e[k][0]), k0 = u.s0 * ks, k1 = u.s1 * ks, add = (float)e[k][1];
+#pragma unroll
+      for (int z = 0; z < 4; ++z) y[k][z] = fmaf(s[k][0][z] + s[k][1][z], z & 1 ? k1 : k0, add);
+      if (nvalid < 2 * kChunk) {
+        if (16 * k + r >= nvalid) y[k][0] = y[k][1] = -INFINITY;
+        if (16 * k + r + 8 >= nvalid) y[k][2] = y[k][3] = -INFINITY;
+      }
     }
   }
+  leave();
   float mx0 = fmaxf(fmaxf(y[0][0], y[0][2]), fmaxf(y[1][0], y[1][2]));
   float mx1 = fmaxf(fmaxf(y[0][1], y[0][3]), fmaxf(y[1][1], y[1][3]));
+  if (__any_sync(0xffffffffu, mx0 > u.m0 + 15.f || mx1 > u.m1 + 15.f)) {
 #pragma unroll
-  for (int o = 4; o < 32; o <<= 1) {
-    mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, o));
-    mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, o));
-  }
-  const bool up0 = mx0 > u.m0 + 15.f, up1 = mx1 > u.m1 + 15.f;
-  if (__any_sync(0xffffffffu, up0 || up1)) {
+    for (int o = 4; o < 32; o <<= 1) {
+      mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, o));
+      mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, o));
+    }
+    const bool up0 = mx0 > u.m0 + 15.f, up1 = mx1 > u.m1 + 15.f;
     const float n0 = up0 ? mx0 - 7.f : u.m0, n1 = up1 ? mx1 - 7.f : u.m1;
     const float2 f = make_float2(up0 ? ex2_approx(u.m0 - n0) : 1.f, up1 ? ex2_approx(u.m1 - n1) : 1.f);
     u.m0 = n0;
@@ -276,24 +282,39 @@ __device__ __forceinline__ void attend(Tile8& u, uint32_t sb, int nvalid, const 
     lo[k][0] = movmatrix_t(pack_f16x2(p0 - g0.x, p1 - g0.y));
     lo[k][1] = movmatrix_t(pack_f16x2(p2 - g1.x, p3 - g1.y));
   }
+  ahead();
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    float d[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int i0 = 0; i0 < 8; i0 += 4) {
+    float d[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) d[i][0] = d[i][1] = d[i][2] = d[i][3] = 0.f;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       const uint32_t* v0 = &x[k][0].x;
       const uint32_t* v1 = &x[k][1].x;
       const uint32_t* v2 = &x[k][2].x;
       const uint32_t* v3 = &x[k][3].x;
-      const uint32_t sel = i & 1 ? 0x7362 : 0x5140;
-      const uint32_t a = __byte_perm(v0[i >> 1], v1[i >> 1], sel), b = __byte_perm(v2[i >> 1], v3[i >> 1], sel);
-      const uint32_t a0 = f16x2_of_e4m3x2(a), a1 = f16x2_of_e4m3x2(a >> 16);
-      const uint32_t a2 = f16x2_of_e4m3x2(b), a3 = f16x2_of_e4m3x2(b >> 16);
-      mma_f16(d, a0, a1, a2, a3, lo[k][0], lo[k][1]);
-      mma_f16(d, a0, a1, a2, a3, hi[k][0], hi[k][1]);
+      uint32_t a[4][4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int at = (i0 + i) >> 1;
+        const uint32_t sel = i & 1 ? 0x7362 : 0x5140;
+        const uint32_t f = __byte_perm(v0[at], v1[at], sel), g = __byte_perm(v2[at], v3[at], sel);
+        a[i][0] = f16x2_of_e4m3x2(f);
+        a[i][1] = f16x2_of_e4m3x2(f >> 16);
+        a[i][2] = f16x2_of_e4m3x2(g);
+        a[i][3] = f16x2_of_e4m3x2(g >> 16);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) mma_f16(d[i], a[i][0], a[i][1], a[i][2], a[i][3], lo[k][0], lo[k][1]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) mma_f16(d[i], a[i][0], a[i][1], a[i][2], a[i][3], hi[k][0], hi[k][1]);
     }
-    u.o[i][0] = __fadd2_rn(u.o[i][0], make_float2(d[0], d[1]));
-    u.o[i][1] = __fadd2_rn(u.o[i][1], make_float2(d[2], d[3]));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      u.o[i0 + i][0] = __fadd2_rn(u.o[i0 + i][0], make_float2(d[i][0], d[i][1]));
+      u.o[i0 + i][1] = __fadd2_rn(u.o[i0 + i][1], make_float2(d[i][2], d[i][3]));
+    }
   }
 }
 
@@ -311,25 +332,36 @@ __device__ __forceinline__ float4 tile_dims(const Tile8& t, int i, int z) {
   return z ? make_float4(a.y, b.y, c.y, d.y) : make_float4(a.x, b.x, c.x, d.x);
 }
 
-// How a launch takes its beams' own chunks: whole (beam, KV head) pairs, or even ranges of `per` chunks of the flat list.
+// How a launch takes its beams' own chunks: whole (beam, KV head) pairs, or ranges of the flat list: one of `large` chunks for each
+// CTA, and the others of `small` for whoever is done first.
 struct Shares {
   bool pairs;
-  int per, count;
+  int large, small, ctas, count;
+  __device__ __forceinline__ int begin(int u) const { return u < ctas ? u * large : ctas * large + (u - ctas) * small; }
+  __device__ __forceinline__ int of(int x) const {
+    if (pairs) return 0;
+    return x < ctas * large ? x / large : ctas + (x - ctas * large) / small;
+  }
 };
 
 __device__ __forceinline__ Shares shares_of(const PoolView& v, int mode, int nact, int total, int ctas) {
   Shares s;
-  const int pairs = max(nact, 1) * v.Hkv;
+  const int pairs = max(nact, 1) * v.Hkv, even = max(1, (total + ctas - 1) / ctas);
   s.pairs = false;
-  s.per = max(1, (total + ctas - 1) / ctas);
-  if (s.per > 160) s.per = (s.per + 3) / 4;
-  s.count = (total + s.per - 1) / s.per;
+  s.ctas = ctas;
+  // SMs differ, so a tenth of long shares is left for the end.  (In four parts each, a CTA that took a fifth one held up the others
+  // for a fifth of the time.  us of 64 x 16384 unshared tokens and 198 x 8000, G = 8: four parts 385, 280; four fifths and parts of a
+  // twentieth 354, 261; nine tenths and a thirty-second 351, 256; two thirds and a sixteenth 347, 274.)
+  s.large = even > 160 ? even * 9 / 10 : even;
+  s.small = even > 160 ? max(32, even / 32) : 1;
+  const int rest = total - ctas * s.large;
+  s.count = rest > 0 ? ctas + (rest + s.small - 1) / s.small : (total + s.large - 1) / s.large;
   if (mode == 1) {  // whoever is done with its segments takes the next one
     s.pairs = total <= 64ll * pairs;
   } else {
     // Chunks that pass a CTA, and a unit's start and merge as so many more.
-    const int whole = (pairs + ctas - 1) / ctas * ((total + pairs - 1) / pairs + 16), even = (total + ctas - 1) / ctas + 48;
-    s.pairs = whole <= even;
+    const int whole = (pairs + ctas - 1) / ctas * ((total + pairs - 1) / pairs + 16);
+    s.pairs = whole <= even + 48;
   }
   if (s.pairs) s.count = v.max_beams * v.Hkv;
   return s;
@@ -524,8 +556,8 @@ __device__ void plan_units(const PoolView& v, const Counters& cnt, int mode, con
       if (s_n[b] > 0) beam_unit(b, u - b * v.Hkv, 0, s_n[b], 0);
       continue;
     }
-    int x = u * sh.per;
-    const int end = min(s_off[v.max_beams], x + sh.per);
+    int x = sh.begin(u);
+    const int end = min(s_off[v.max_beams], sh.begin(u + 1));
     int b = 0, hi = v.max_beams;  // s_off[b] <= x < s_off[hi]
     while (hi - b > 1) {
       const int mid = (b + hi) >> 1;
@@ -577,22 +609,40 @@ __device__ __forceinline__ void multiply(Tile8& t, const PoolView& v, const Unit
   const int rgroups = row_groups(u.rows), groups = kConsumers8 / rgroups, rg = warp % rgroups, group = warp / rgroups;
   tile_begin(t, qscale, c);
   const int stages = (u.tokens + 2 * kChunk - 1) / (2 * kChunk);
-  const bool any = rg * 8 < u.rows;
-  for (int i = group; i < stages; i += groups) {
-    const uint32_t k = base + i, s = k % kStages8;
-    if (!__all_sync(0xffffffffu, wait_or_stop(full + 8 * s, (k / kStages8) & 1, stop))) break;
-    auto leave = [&] {
-      __syncwarp();
+  if (rg * 8 < u.rows) {
+    uint32_t w[2][2][8];
+    int4 e = make_int4(0, 0, 0, 0);
+    bool ok = true;
+    auto arrive = [&](int i) {  // stage i: wait for it, its exponents and K
+      const uint32_t k = base + i, s = k % kStages8;
+      ok = __all_sync(0xffffffffu, wait_or_stop(full + 8 * s, (k / kStages8) & 1, stop));
+      if (!ok) return;
+      e = *reinterpret_cast<const int4*>(smem + Smem8::EXPS + 16 * s);
+      take_k(w, ring + s * kStageBytes8, r, c);
+    };
+    if (group < stages) arrive(group);
+#pragma unroll 1
+    for (int i = group; ok && i < stages; i += groups) {
+      const uint32_t s = (base + i) % kStages8;
+      const int eh[2][2] = {{e.x, e.y}, {e.z, e.w}};
+      attend(
+          t, w, ring + s * kStageBytes8, min(2 * kChunk, u.tokens - i * 2 * kChunk), eh, r, c,
+          [&] {
+            __syncwarp();
+            if (lane == 0) mbar_arrive_n(empty + 8 * s, groups);
+            __syncwarp();
+          },
+          [&] {
+            if (i + groups < stages) arrive(i + groups);
+          });
+    }
+  } else {
+    for (int i = group; i < stages; i += groups) {  // no rows: the stages' slots are given back
+      const uint32_t k = base + i, s = k % kStages8;
+      if (!__all_sync(0xffffffffu, wait_or_stop(full + 8 * s, (k / kStages8) & 1, stop))) break;
       if (lane == 0) mbar_arrive_n(empty + 8 * s, groups);
       __syncwarp();
-    };
-    if (!any) {
-      leave();
-      continue;
     }
-    const int4 e = *reinterpret_cast<const int4*>(smem + Smem8::EXPS + 16 * s);
-    const int eh[2][2] = {{e.x, e.y}, {e.z, e.w}};
-    attend(t, ring + s * kStageBytes8, min(2 * kChunk, u.tokens - i * 2 * kChunk), eh, r, c, leave);
   }
   next();
   tile_finish(t);
@@ -739,14 +789,14 @@ __global__ void __launch_bounds__(kThreads8, 1)
   // mode 1: by segments; mode 2: by segments where that pays.  A segment's pages are read once for all of its members, but a
   // tile's step takes a warp as long for members as for a beam alone, and the records more to merge.  So it pays where beams of up
   // to 4 heads a KV head, two or more of which fill a tile that one would leave half empty, read far more than there is (us, beams
-  // alone / segments; MB read alone / there): 115 / 99 (525 / 185, 64 x 4000), 278 / 195 (1600 / 673, 128 x 6100), 185 / 138 (1024 /
-  // 369, 200 x 2500, G = 2), 109 / 98 (410 / 142, 100 x 2000); not 85 / 86 (328 / 109, 40 x 4000), 93 / 110 (164 / 61, 256 x 313), 278 /
-  // 290 (1623 / 359, 198 x 8000, G = 8).
+  // alone / segments; MB read alone / there): 104 / 99 (525 / 185, 64 x 4000), 250 / 198 (1600 / 673, 128 x 6100), 184 / 135 (1024 /
+  // 369, 200 x 2500, G = 2), 244 / 203 (1660 / 554, 90 x 9000); not 76 / 85 (328 / 109, 40 x 4000), 93 / 97 (410 / 142, 100 x 2000), 140 /
+  // 146 (577 / 188, 256 x 1100), 256 / 302 (1623 / 359, 198 x 8000, G = 8).
   if (v.ctl[kCtlSegTiles] == 0) mode = 0;
   if (mode == 2) {
     const long long all = (long long)plan_off(v, 0)[v.max_beams] * kChunkBytes8;
     const long long there = plan_off(v, 1)[v.max_beams] * (long long)kChunkBytes8 + (long long)v.ctl[kCtlSegTok] * v.Hkv * (kChunkBytes8 / kChunk);
-    mode = G <= 4 && all - there > 260000000ll ? 1 : 0;
+    mode = G <= 4 && all - there > 330000000ll ? 1 : 0;
   }
   {
     int* s_off = reinterpret_cast<int*>(smem + Smem8::PLAN);
@@ -769,7 +819,7 @@ __global__ void __launch_bounds__(kThreads8, 1)
   asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kConsumerRegs8));
   multiply_units<G>(v, cnt, q, qscale, mode, smem, bars, out);
   // Every CTA is resident with the others (one an SM), and each wait gives up once the status is set.
-  combine_shares<G, true>(v, cnt, mode, sh.pairs ? 0 : sh.per, nctas, false, cta, nctas, kConsumers8, out);
+  combine_shares<G, true>(v, cnt, mode, [sh](int x) { return sh.of(x); }, nctas, false, cta, nctas, kConsumers8, out);
 }
 
 template <int G>
