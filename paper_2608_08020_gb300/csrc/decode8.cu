@@ -214,12 +214,13 @@ __device__ __forceinline__ void take_v(uint4 (&x)[2][4], uint32_t sb, int nvalid
     }
 }
 
-// A landed stage (its first nvalid >= 1 tokens) into a tile.  w: its K words (take_k); e: K's and V's exponent of each chunk.
-// leave() gives its slot back; ahead() may load the next stage's K words, behind which V's products then run.
-template <class Leave, class Ahead>
-__device__ __forceinline__ void attend(Tile8& u, const uint32_t (&w)[2][2][8], uint32_t sb, int nvalid, const int (&e)[2][2], int r, int c,
-                                       Leave leave, Ahead ahead) {
+// A landed stage (its first nvalid >= 1 tokens) into a tile.  e: K's and V's exponent of each chunk.  leave() gives its slot back: V
+// is in registers before it is multiplied.
+template <class Leave>
+__device__ __forceinline__ void attend(Tile8& u, uint32_t sb, int nvalid, const int (&e)[2][2], int r, int c, Leave leave) {
+  uint32_t w[2][2][8];
   uint4 x[2][4];
+  take_k(w, sb, r, c);
   take_v(x, sb, nvalid, r, c);
   float y[2][4];
   {
@@ -282,7 +283,6 @@ __device__ __forceinline__ void attend(Tile8& u, const uint32_t (&w)[2][2][8], u
     lo[k][0] = movmatrix_t(pack_f16x2(p0 - g0.x, p1 - g0.y));
     lo[k][1] = movmatrix_t(pack_f16x2(p2 - g1.x, p3 - g1.y));
   }
-  ahead();
 #pragma unroll
   for (int i0 = 0; i0 < 8; i0 += 4) {
     float d[4][4];
@@ -609,39 +609,22 @@ __device__ __forceinline__ void multiply(Tile8& t, const PoolView& v, const Unit
   const int rgroups = row_groups(u.rows), groups = kConsumers8 / rgroups, rg = warp % rgroups, group = warp / rgroups;
   tile_begin(t, qscale, c);
   const int stages = (u.tokens + 2 * kChunk - 1) / (2 * kChunk);
-  if (rg * 8 < u.rows) {
-    uint32_t w[2][2][8];
-    int4 e = make_int4(0, 0, 0, 0);
-    bool ok = true;
-    auto arrive = [&](int i) {  // stage i: wait for it, its exponents and K
-      const uint32_t k = base + i, s = k % kStages8;
-      ok = __all_sync(0xffffffffu, wait_or_stop(full + 8 * s, (k / kStages8) & 1, stop));
-      if (!ok) return;
-      e = *reinterpret_cast<const int4*>(smem + Smem8::EXPS + 16 * s);
-      take_k(w, ring + s * kStageBytes8, r, c);
-    };
-    if (group < stages) arrive(group);
+  const bool any = rg * 8 < u.rows;  // (without rows the stages' slots are only given back)
 #pragma unroll 1
-    for (int i = group; ok && i < stages; i += groups) {
-      const uint32_t s = (base + i) % kStages8;
-      const int eh[2][2] = {{e.x, e.y}, {e.z, e.w}};
-      attend(
-          t, w, ring + s * kStageBytes8, min(2 * kChunk, u.tokens - i * 2 * kChunk), eh, r, c,
-          [&] {
-            __syncwarp();
-            if (lane == 0) mbar_arrive_n(empty + 8 * s, groups);
-            __syncwarp();
-          },
-          [&] {
-            if (i + groups < stages) arrive(i + groups);
-          });
-    }
-  } else {
-    for (int i = group; i < stages; i += groups) {  // no rows: the stages' slots are given back
-      const uint32_t k = base + i, s = k % kStages8;
-      if (!__all_sync(0xffffffffu, wait_or_stop(full + 8 * s, (k / kStages8) & 1, stop))) break;
+  for (int i = group; i < stages; i += groups) {
+    const uint32_t k = base + i, s = k % kStages8;
+    if (!__all_sync(0xffffffffu, wait_or_stop(full + 8 * s, (k / kStages8) & 1, stop))) break;
+    auto leave = [&] {
+      __syncwarp();
       if (lane == 0) mbar_arrive_n(empty + 8 * s, groups);
       __syncwarp();
+    };
+    if (any) {
+      const int4 e = *reinterpret_cast<const int4*>(smem + Smem8::EXPS + 16 * s);
+      const int eh[2][2] = {{e.x, e.y}, {e.z, e.w}};
+      attend(t, ring + s * kStageBytes8, min(2 * kChunk, u.tokens - i * 2 * kChunk), eh, r, c, leave);
+    } else {
+      leave();
     }
   }
   next();
