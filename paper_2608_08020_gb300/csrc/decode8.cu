@@ -27,10 +27,10 @@
 // among the warps of a row group, whose softmax states are merged in shared memory when the unit ends.  Units' records are
 // merged at the end of the launch (combine.cuh); a beam whose whole context was one unit is written at once.
 //
-// What bounds it (a launch alone, one layer): unshared caches, memory: 64 x 16384 tokens in 351 us, 6.1 TB/s (without the products
-// 339).  Shared ones, the multiplying warps: the same bytes from L2 take 285 us, 7.4 TB/s, without the products 162.  A tile's 32
-// tokens are 48 products (413 cycles of a scheduler's) and 534 instructions, for which a warp takes 2100 cycles, two a scheduler; with
-// twelve warps, or two tiles a warp that share their conversions, the SM does as much.  Small calls, a chain: barriers, plan, page
+// What bounds it (a launch alone, one layer): unshared caches, memory: 64 x 16384 tokens in 355 us, 6.1 TB/s (without the products
+// 339).  Shared ones, the multiplying warps: the same bytes from L2 take 263 us, 8.0 TB/s, without the products 162.  A tile's 32
+// tokens are 48 products (413 cycles of a scheduler's) and 530 instructions, for which a warp takes 2000 cycles, two a scheduler; with
+// twelve warps, two tiles a warp that share their conversions, or the next stage's K asked for early, the SM does no more.  Small calls, a chain: barriers, plan, page
 // ids and exponents, first chunks, merge: 13-15 us cold for 8 or 13 beams, 2.5 of them before the first copy.
 #include <atomic>
 
@@ -350,8 +350,8 @@ __device__ __forceinline__ Shares shares_of(const PoolView& v, int mode, int nac
   s.pairs = false;
   s.ctas = ctas;
   // SMs differ, so a tenth of long shares is left for the end.  (In four parts each, a CTA that took a fifth one held up the others
-  // for a fifth of the time.  us of 64 x 16384 unshared tokens and 198 x 8000, G = 8: four parts 385, 280; four fifths and parts of a
-  // twentieth 354, 261; nine tenths and a thirty-second 351, 256; two thirds and a sixteenth 347, 274.)
+  // for a fifth of the time.  us of 64 x 16384 unshared tokens and 198 x 8000, G = 8, as measured then: four parts 385, 280; four fifths
+  // and parts of a twentieth 354, 261; nine tenths and a thirty-second 351, 256; two thirds and a sixteenth 347, 274.)
   s.large = even > 160 ? even * 9 / 10 : even;
   s.small = even > 160 ? max(32, even / 32) : 1;
   const int rest = total - ctas * s.large;
@@ -772,9 +772,9 @@ __global__ void __launch_bounds__(kThreads8, 1)
   // mode 1: by segments; mode 2: by segments where that pays.  A segment's pages are read once for all of its members, but a
   // tile's step takes a warp as long for members as for a beam alone, and the records more to merge.  So it pays where beams of up
   // to 4 heads a KV head, two or more of which fill a tile that one would leave half empty, read far more than there is (us, beams
-  // alone / segments; MB read alone / there): 104 / 99 (525 / 185, 64 x 4000), 250 / 198 (1600 / 673, 128 x 6100), 184 / 135 (1024 /
-  // 369, 200 x 2500, G = 2), 244 / 203 (1660 / 554, 90 x 9000); not 76 / 85 (328 / 109, 40 x 4000), 93 / 97 (410 / 142, 100 x 2000), 140 /
-  // 146 (577 / 188, 256 x 1100), 256 / 302 (1623 / 359, 198 x 8000, G = 8).
+  // alone / segments; MB read alone / there): 99 / 93 (525 / 185, 64 x 4000), 242 / 186 (1600 / 673, 128 x 6100), 173 / 128 (1024 /
+  // 369, 200 x 2500, G = 2), 228 / 187 (1660 / 554, 90 x 9000); not 72 / 80 (328 / 109, 40 x 4000), 88 / 93 (410 / 142, 100 x 2000), 132 /
+  // 136 (577 / 188, 256 x 1100, on the wrong side), 238 / 280 (1623 / 359, 198 x 8000, G = 8).
   if (v.ctl[kCtlSegTiles] == 0) mode = 0;
   if (mode == 2) {
     const long long all = (long long)plan_off(v, 0)[v.max_beams] * kChunkBytes8;

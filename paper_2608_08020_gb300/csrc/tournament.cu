@@ -552,7 +552,7 @@ __global__ void __launch_bounds__(kTourThreads, 1) k_tournament(PoolView v, Tour
     const long long work = (long long)v.ctl[kCtlSegTileTok] * v.Hkv;  // tile-tokens over all heads
     long long target_units = (long long)GB_SEG_UNITS_PCT * (v.num_sms > 0 ? v.num_sms : 1) / 100;
     // 8 bits: k_decode8's units are of half a tile, and taken by whoever is free, so four times as many fill the SMs evenly
-    // (64 x 4000 tokens with twice, four and eight times: 104, 100 and 116 us; 198 x 8000: 348, 300, 315).
+    // (64 x 4000 tokens with twice, four and eight times as many, when this was chosen: 104, 100 and 116 us; 198 x 8000: 348, 300, 315).
     if (v.dtype == GB_FP8) target_units = max(target_units, min(4 * target_units, 32ll * cap * v.Hkv));
     int split = (int)(((work + target_units - 1) / target_units + 127) / 128 * 128);
     const int max_tokens = v.max_pages * v.P;
