@@ -75,3 +75,36 @@ def test_traces_with_shared_prefixes(cuda, hq, hkv, slots):
         length += 1
         _check(pool, [length] * slots, q, out, 128 ** -0.5)
     assert pool.status() == 0
+
+
+def test_offsets_past_32_bits(cuda):
+    """The last layer of a pool of 25 GB: its rows and scales written, copied on write, read and attended to."""
+    from paper_2608_08020_gb300.pool import BeamPool
+    from paper_2608_08020_gb300.rotation import Rotation
+    layers, hq, hkv, slots = 40, 16, 8, 4
+    pool = BeamPool(num_layers=layers, num_q_heads=hq, num_kv_heads=hkv, head_dim=128, page_size=16, kv_dtype="fp8", num_pages=19000,
+                    max_beams=slots, max_pages_per_beam=16)
+    assert pool.kv.numel() > 5 << 32
+    g = torch.Generator(device="cuda").manual_seed(0)
+    rand = lambda *s: torch.randn(s, generator=g, device="cuda").to(torch.bfloat16)  # noqa: E731
+    rotation = Rotation(128, max_positions=300)
+    seed, new = rand(2, layers, 70, hkv, 128), rand(2, layers, 30, slots, hkv, 128)
+    pool.seed(slots, 70, seed[0], seed[1])
+    for i in range(layers):
+        pool.append_kv(i, 30, new[0, i], new[1, i], rotation=rotation)
+    first = torch.zeros(slots, dtype=torch.int32, device="cuda")
+    top = pool.read_kv(layers - 1, first, 100)
+    for b in range(slots):                                  # 4 significant bits, and those of a block whose scale rose
+        exact = torch.cat([seed[1, -1], new[1, -1, :, b]]).double()
+        assert ((top[1][:, b].double() - exact).abs() <= 2.0 ** -3 * exact.abs() + 2.0 ** -8).all()
+    q, k, v = rand(layers, slots, hq, 128), rand(layers, slots, hkv, 128), rand(layers, slots, hkv, 128)
+    out = torch.empty(slots, hq, 128, device="cuda")
+    for i in range(layers):
+        pool.decode_attention(i, q[i], k[i], v[i], 128 ** -0.5, out)
+    kc, vc = (x.double() for x in pool.read_kv(layers - 1, first, 101))
+    for b in range(slots):
+        kk, vv = (x[:, b].transpose(0, 1).repeat_interleave(2, 0) for x in (kc, vc))
+        p = ((kk @ q[-1, b].double()[:, :, None])[..., 0] * 128 ** -0.5).softmax(-1)[:, None]
+        # Scores are right to 2^-16 of sizes up to some tens, weights to 2^-18.
+        assert ((out[b].double() - (p @ vv)[:, 0]).abs() <= 2.0 ** -11 * (p @ vv.abs())[:, 0]).all()
+    assert pool.status() == 0

@@ -62,3 +62,14 @@ def test_a_row_alone_and_among_many(cuda, dtype, vocab):
         for r in range(rows):
             t, p = _sampler(1, vocab)(x[r:r + 1], u[r:r + 1], **kw)
             assert (token[r::rows] == t).all() and (logprob[r::rows] == p).all(), f"row {r} {kw}"
+
+
+def test_rows_past_32_bits(cuda):
+    """Rows so far apart that the last one begins behind 2^31 logits."""
+    rows, vocab, stride = 3, 5000, 1_100_000_003
+    buf = torch.empty(2 * stride + vocab, dtype=torch.bfloat16, device="cuda")
+    x = buf.as_strided((rows, vocab), (stride, 1))
+    g = torch.Generator().manual_seed(0)
+    x.copy_(_logits(g, rows, vocab, torch.bfloat16))
+    check(x, torch.rand(rows, generator=g).cuda(), top_p=0.9)
+    check(x, torch.rand(rows, generator=g).cuda(), top_k=20)
