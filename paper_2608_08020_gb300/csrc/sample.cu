@@ -633,8 +633,8 @@ struct RowCtas {
   }
 
   // Sums the weights of the tokens with x >= least, and those that top-p can keep by slices of their exponent, to 12 bits
-  // each.  Tokens below 2^-24 (`far`) are only summed, from the 22 bits of exp2f.  The others' weights take 60 instructions, so a warp puts
-  // their logits in a queue of its own and takes 32 at a time from it: as they lie in the row, most turns of a warp would have
+  // each.  Tokens below 2^-24 (`far`) are only summed, from the 22 bits of exp2f.  The others' weights take 36 issue slots, so a warp
+  // puts their logits in a queue of its own and takes 64 at a time from it: as they lie in the row, most turns of a warp would have
   // only a few.  Tokens so light that all of them together could not be the share 1 - p that goes need no slice (`can`).
   __device__ u64 slice_masses(float p, float least, float own_max) {
     for (int b = threadIdx.x; b < kSlices; b += kThreads) sm.slice[b] = 0;
