@@ -1099,7 +1099,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(const __grid_constant__ 
   const int runs = (pieces.count + 31) / 32;
   if (!summed) {
     head = by_k ? ctx.cut({0u, 0x7fffffff}, -1, false, (u64)top_k) : from;
-    if (from.k > head.k) head = from;
+    if (least > -INFINITY && from.k >= head.k) head = from;  // (of one key, min-p's: it keeps none of that key's tokens)
     if (top_p < 1.f) {
       u64 s = 0;
       ctx.each([&](float x, int i) { s += kept(head, key_of(x), i) ? weight(row, sm.table, x) : 0; });
