@@ -961,7 +961,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(const __grid_constant__ 
   for (int j = tid; j < kBins; j += kThreads) sm.table[j] = kPowers.t[j];
   if (tid == 0) sm.listed = 0;
 
-  if (min_p > 0.f && tid == kThreads - 1) sm.ahead = (double)temperature * log(fmin((double)min_p, 1.0));
+  if (min_p > 0.f && tid == kThreads - 1)  // (an endless temperature makes every weight one, and times ln 1 it is no number)
+    sm.ahead = temperature < INFINITY ? (double)temperature * log(fmin((double)min_p, 1.0)) : -INFINITY;
 
   // The largest logit, and the piece that has it first.
   float m = -INFINITY;

@@ -31,6 +31,26 @@ def test_top_k_ends_in_a_run_just_below_min_p(cuda, dtype, vocab, c):
     check(x, torch.full((6,), 1 - 2.0 ** -24, device="cuda"), top_k=700, min_p=p)
 
 
+@pytest.mark.parametrize("vocab", [5, 500, 40000])
+@pytest.mark.parametrize("min_p", [0.0, 1e-30, 0.5, 1.0, 2.0, math.inf])
+def test_endless_temperatures(cuda, vocab, min_p):
+    """They make a row flat: every token stays, and comes up as often as the others.  (The largest finite one says the same.)"""
+    g = torch.Generator().manual_seed(vocab)
+    x, u = _logits(g, 7, vocab, torch.float32, banned=0.2), torch.rand(7, generator=g).cuda()
+    x[:, 0] = 1.0
+    s = _sampler(7, vocab)
+    inf = torch.full((7,), math.inf, device="cuda")
+    for kw in ({}, {"top_k": 3}, {"top_k": 600}, {"top_p": 0.7}, {"top_k": 4, "top_p": 0.5}):
+        token, logprob = s(x, u, temperature=inf, min_p=min_p, **kw)
+        kept = (x > -math.inf).sum(1)
+        if kw.get("top_k", vocab) < vocab:
+            kept = kept.clamp(max=kw["top_k"])
+        if "top_p" in kw:
+            kept = torch.ceil(kept.double() * float(np.float32(kw["top_p"])) - 1e-9).long()
+        assert (token >= 0).all() and (x.gather(1, token.long()[:, None]) > -math.inf).all()
+        assert ((logprob.double() + kept.double().log()).abs() <= 2.0 ** -24 * kept.double().log() + 2.0 ** -30).all()
+
+
 def test_parameters_at_the_ends_together(cuda):
     """Every pairing of extremes, a row each."""
     temps = [1e-40, 1e-30, 1e-6, 0.5, 1.0, 1e6, 1e30, 3e38]
