@@ -548,6 +548,21 @@ __global__ void __launch_bounds__(kTourThreads, 1) k_tournament(PoolView v, Tour
     v.ctl[kCtlSegCount] = nseg_all;
     v.ctl[kCtlSegMembers] = v.ctl[kCtlSegAlloc];
   }
+  if (v.dtype == GB_FP8) {
+    // Each list's members in ascending order, whoever came first: k_decode8 shares out the last 64 query rows of a list otherwise
+    // than full ones, so the same step would differ in its last places from one rebuild to the next.
+    for (int s = blockIdx.x; s < nseg_all; s += gridDim.x) {
+      int* list = v.seg_members + v.seg_mem_off[s];
+      const int g = min(v.seg_g[s], cap * kMaxSegDepth - v.seg_mem_off[s]);
+      const int e = tid < g ? list[tid] : 0;
+      s_pref[tid] = e;
+      __syncthreads();
+      int rank = 0;
+      for (int i = 0; i < (tid < g ? g : 0); ++i) rank += s_pref[i] < e ? 1 : 0;
+      if (tid < g) list[rank] = e;
+      __syncthreads();
+    }
+  }
   if (tid == 0) {
     const long long work = (long long)v.ctl[kCtlSegTileTok] * v.Hkv;  // tile-tokens over all heads
     long long target_units = (long long)GB_SEG_UNITS_PCT * (v.num_sms > 0 ? v.num_sms : 1) / 100;
