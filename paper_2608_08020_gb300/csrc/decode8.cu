@@ -32,6 +32,8 @@
 // tokens are 48 products (413 cycles of a scheduler's) and 530 instructions, for which a warp takes 2000 cycles, two a scheduler; with
 // twelve warps, two tiles a warp that share their conversions, or the next stage's K asked for early, the SM does no more.  Small calls, a chain: barriers, plan, page
 // ids and exponents, first chunks, merge: 13-15 us cold for 8 or 13 beams, 2.5 of them before the first copy.
+#include <float.h>
+
 #include <atomic>
 
 #include "decode_mma.cuh"
@@ -183,7 +185,7 @@ __device__ __forceinline__ void tile_begin(Tile8& t, float qscale, int c) {
   t.s1 = __shfl_sync(0xffffffffu, back, 8 * c + 4);
 #pragma unroll
   for (int i = 0; i < 8; ++i) t.o[i][0] = t.o[i][1] = make_float2(0.f, 0.f);
-  t.m0 = t.m1 = -INFINITY;
+  t.m0 = t.m1 = -FLT_MAX;  // not -infinity: a warp whose scores are all NaN has a state, which the merges keep
   t.l0 = t.l1 = 0.f;
 }
 
@@ -664,15 +666,14 @@ __device__ __forceinline__ void multiply(Tile8& t, const PoolView& v, const Unit
     for (int i = tid; i < rgroups * 4 * 32; i += kConsumers8 * 32) {
       const int g = i >> 7, in = (i >> 5) & 3, row = g * 8 + 4 * f + in, d = 4 * (i & 31);
       if (row >= u.rows) continue;
-      float M = -INFINITY;
+      float M = -FLT_MAX;
       for (int k = 0; k < groups; ++k) M = fmaxf(M, ml[(g + k * rgroups) * 4 + in].x);
       float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
       float L = 0.f;
       for (int k = 0; k < groups; ++k) {
         const int w = (g + k * rgroups) * 4 + in;
         const float2 a = ml[w];
-        if (a.x == -INFINITY) continue;  // a warp without a stage
-        const float f2 = exp2f(a.x - M);
+        const float f2 = exp2f(a.x - M);  // (a warp without a stage adds zeros)
         const float4 x = *reinterpret_cast<const float4*>(left + w * kRowFloats8 + d);
         acc.x = fmaf(x.x, f2, acc.x);
         acc.y = fmaf(x.y, f2, acc.y);
