@@ -24,6 +24,7 @@
 // are warp-wide so rescaling is a warp-uniform branch.
 #include <cuda.h>
 #include <cuda_bf16.h>
+#include <float.h>
 #include <math.h>
 
 #include "decode_mma.cuh"
@@ -252,7 +253,7 @@ __device__ __forceinline__ bool decode_range(const PoolView& v, int layer, const
           qr[g][d] = make_float2(qr[g][d].x * qscale, qr[g][d].y * qscale);
           o[g][d] = make_float2(0.f, 0.f);
         }
-        m_run[g] = -INFINITY;
+        m_run[g] = -FLT_MAX;  // (pair_begin)
       }
 #pragma unroll
       for (int kk = 0; kk < NS; ++kk) l_lane[kk] = 0.f;

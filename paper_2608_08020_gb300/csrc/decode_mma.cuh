@@ -4,6 +4,7 @@
 #pragma once
 #include <cuda.h>
 #include <cuda_bf16.h>
+#include <float.h>
 #include <math.h>
 
 #include "combine.cuh"
@@ -137,7 +138,9 @@ __device__ __forceinline__ void pair_begin(PairState& st, const PoolView& v, con
   }
 #pragma unroll
   for (int mt = 0; mt < 8; ++mt) st.o[mt][0] = st.o[mt][1] = st.o[mt][2] = st.o[mt][3] = 0.f;
-  st.m0 = st.m1 = -INFINITY;
+  // Not -infinity: scores of minus infinity alone weigh 2^-inf, and a warp whose scores are all NaN has a state, which the
+  // merges keep (a record with m = -infinity is one without tokens).
+  st.m0 = st.m1 = -FLT_MAX;
   st.l0 = st.l1 = 0.f;
 }
 

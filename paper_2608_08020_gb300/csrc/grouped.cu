@@ -548,7 +548,7 @@ __device__ __forceinline__ void grouped_body(const PoolView& v, const Counters& 
       const int m = x.t * members_per_tile + r / G, gg = r % G;
       const int bk = m < x.g ? v.seg_members[x.moff + m] : 0;
       const int r_idx = v.seg_rec_off[bk] + x.sp;
-      float m_ref = -INFINITY, l = 0.f;
+      float m_ref = -FLT_MAX, l = 0.f;  // (not -infinity: pair_begin)
       for (int j = 0; j < x.ntok; ++j, ++n) {
         const uint32_t sb = n % kSBufs;
         const uint32_t sp_addr = tmem + sb * 128 + grp * 64 + lane_base;

@@ -1,5 +1,5 @@
 """Keys that are not finite in a decode step's context.  A key that makes a score NaN makes every head that sees it NaN, wherever in the
-context it lies and however the context is split."""
+context it lies and however the context is split; a key that scores minus infinity weighs nothing, whatever was met before it."""
 import pytest
 import torch
 
@@ -33,7 +33,7 @@ class Step:
         return out
 
 
-@pytest.mark.parametrize("dtype,hq", [("fp8", 2), ("fp8", 8), ("fp8", 16)])
+@pytest.mark.parametrize("dtype,hq", [("fp8", 2), ("fp8", 8), ("fp8", 16), ("bf16", 4), ("bf16", 8), ("bf16", 16), ("f32", 4), ("f32", 16)])
 @pytest.mark.parametrize("slots,length", [(3, 1), (3, 33), (3, 65), (2, 300), (1, 4000), (40, 1500)])
 @pytest.mark.parametrize("flags", [0, 1, 2])
 def test_a_key_that_is_not_a_number(cuda, dtype, hq, slots, length, flags):
@@ -58,3 +58,23 @@ def test_a_key_that_is_not_a_number(cuda, dtype, hq, slots, length, flags):
             want[sees, g:] = True
             assert torch.equal(out.isnan(), want), f"token {at}"
             assert torch.equal(out[~want], clean[~want]), f"token {at}"
+
+
+@pytest.mark.parametrize("dtype,hq", [("bf16", 4), ("bf16", 8), ("bf16", 16), ("f32", 4), ("f32", 16)])
+@pytest.mark.parametrize("slots,length", [(3, 33), (3, 65), (2, 300), (1, 4000), (40, 1500)])
+@pytest.mark.parametrize("flags", [0, 1, 2])
+def test_scores_of_minus_infinity(cuda, dtype, hq, slots, length, flags):
+    """The context's first tokens, a range inside it, all but the newest, all: as with scores so low that they weigh nothing."""
+    t = Step(dtype, hq, slots, length)
+    t.q[..., 0] = t.q[..., 0].abs() + 0.5
+    for lo, hi in ((0, 1), (0, 16), (0, 31), (0, length // 2), (length // 3, length - 1), (0, length - 1)):
+        was = t.kv[0, 0, lo:hi, :, 0].clone()
+        outs = []
+        # 0.5 x -1e6 / sqrt(128) is below -40000: its weight is 0 in fp32, too, beside scores of some tens.
+        for low in (float("-inf"), -1e6):
+            t.kv[0, 0, lo:hi, :, 0] = low
+            outs.append(t.run(flags))
+        t.kv[0, 0, lo:hi, :, 0] = was
+        assert bool(outs[1].isfinite().all()) and torch.equal(*outs), f"tokens {lo} to {hi}"
+    t.kv[0, 0, :, :, 0] = t.new[0, :, :, 0] = float("-inf")
+    assert bool(t.run(flags).isnan().all())
