@@ -1420,6 +1420,5 @@ extern "C" gb_status gb_truncate(gb_pool* pool, const int32_t* lengths_dev, gb_s
   launch_cow_rows(pool, s);
   const gb_status st = check_launch(pool, "truncate");
   if (st != GB_OK) return st;
-  if (rebuild_segments(pool, s, pool->view.ctl + kCtlSegStale) != cudaSuccess) return check_launch(pool, "segments");
-  return GB_OK;
+  return check_launch(pool, "segments", rebuild_segments(pool, s, pool->view.ctl + kCtlSegStale));
 }

@@ -386,7 +386,8 @@ inline void prof_begin(gb_pool* p, int which, cudaStream_t s) {
 inline void prof_end(gb_pool* p, int which, cudaStream_t s) {
   if (p->prof_stop[which]) prof_record(p->prof_stop[which], s);
 }
-gb_status check_launch(gb_pool* pool, const char* what);
+// The last error of the runtime, or `e`: what a launcher returned, which need not be one (a check of its own).
+gb_status check_launch(gb_pool* pool, const char* what, cudaError_t e = cudaSuccess);
 bool on_device(const gb_pool* pool);  // whether the pool's device is the current one
 // Raise a kernel's dynamic shared memory limit to `bytes` on the current device.  The
 // attribute belongs to the device, so it is set once per (kernel, device), under a lock.

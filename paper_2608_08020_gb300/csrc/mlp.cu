@@ -113,8 +113,6 @@ extern "C" gb_status gb_score_mlp(gb_pool* pool, const void* hidden_dev, int hid
   if ((size_t)pool->view.max_beams * d_h > (size_t)kMlpScratchFloats)
     return fail(pool, GB_ERR_TOO_LARGE, "score_mlp: max_beams x d_h exceeds the partial-sum buffer");
   if (pool->next_layer != 0) return fail(pool, GB_ERR_STATE, "score_mlp inside an open step");
-  if (launch_mlp(pool, hidden_dev, hidden_dim, w1_dev, b1_dev, w2_dev, b2, d_h, boundary_mask_dev, score_out_dev,
-                 reinterpret_cast<cudaStream_t>(stream)) != cudaSuccess)
-    return check_launch(pool, "score_mlp");
-  return check_launch(pool, "score_mlp");
+  return check_launch(pool, "score_mlp", launch_mlp(pool, hidden_dev, hidden_dim, w1_dev, b1_dev, w2_dev, b2, d_h, boundary_mask_dev,
+                                                    score_out_dev, reinterpret_cast<cudaStream_t>(stream)));
 }

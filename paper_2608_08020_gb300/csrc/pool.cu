@@ -110,8 +110,9 @@ bool on_device(const gb_pool* pool) {
   return cudaGetDevice(&d) == cudaSuccess && d == pool->device;
 }
 
-gb_status check_launch(gb_pool* pool, const char* what) {
-  cudaError_t e = cudaGetLastError();
+gb_status check_launch(gb_pool* pool, const char* what, cudaError_t e) {
+  const cudaError_t last = cudaGetLastError();
+  if (e == cudaSuccess) e = last;
   if (e != cudaSuccess) {
     if (pool) pool->last_error = std::string(what) + ": " + cudaGetErrorString(e);
     return GB_ERR_CUDA;
@@ -781,17 +782,17 @@ extern "C" gb_status gb_pool_seed(gb_pool* pool, int n_beams, int prompt_len, co
   const long long vecs = 2LL * pool->cfg.num_layers * prompt_len * pool->cfg.num_kv_heads *
                          (pool->view.D * pool->view.esize / 16);
   const int grid = (int)std::min<long long>((vecs + 255) / 256, pool->num_sms * 8LL);
+  cudaError_t e = cudaSuccess;
   if (pool->cfg.kv_dtype == GB_FP8)
-    launch_seed_rows8(pool, prompt_len, k_prompt_dev, v_prompt_dev, s);
+    e = launch_seed_rows8(pool, prompt_len, k_prompt_dev, v_prompt_dev, s);
   else
     k_seed_write<<<std::max(grid, 1), 256, 0, s>>>(pool->view, prompt_len,
                                                    static_cast<const char*>(k_prompt_dev),
                                                    static_cast<const char*>(v_prompt_dev));
-  st = check_launch(pool, "seed_write");
+  st = check_launch(pool, "seed_write", e);
   if (st != GB_OK) return st;
   pool->seeded = true;
-  if (rebuild_segments(pool, s) != cudaSuccess) return check_launch(pool, "segments");
-  return GB_OK;
+  return check_launch(pool, "segments", rebuild_segments(pool, s));
 }
 
 // Shared by the decode and append calls: open the step at layer 0 and write the new
@@ -820,16 +821,17 @@ static gb_status append_layer(gb_pool* pool, int layer, int n_tokens, const void
   }
   const int runs = (n_tokens + pool->cfg.page_size - 1) / pool->cfg.page_size + 1;  // pages a beam's new tokens meet
   const dim3 grid(pool->cfg.max_beams, std::min(2 * runs, 65535));
+  cudaError_t e = cudaSuccess;
   prof_begin(pool, GB_PROF_APPEND, s);  // an empty interval when the attention launch appends
   if (!fused && (rot.table || pool->cfg.kv_dtype == GB_FP8)) {
-    launch_append_rows(pool, layer, n_tokens, rot, k, v, q, qout, s);
+    e = launch_append_rows(pool, layer, n_tokens, rot, k, v, q, qout, s);
   } else if (!fused) {
-    launch_pdl(k_append, grid, 256, 0, s, pool->view, layer, n_tokens, static_cast<const char*>(k),
-               static_cast<const char*>(v));
+    e = launch_pdl(k_append, grid, 256, 0, s, pool->view, layer, n_tokens, static_cast<const char*>(k),
+                   static_cast<const char*>(v));
     pool->launches += 1;
   }
   prof_end(pool, GB_PROF_APPEND, s);
-  gb_status st = check_launch(pool, "append");
+  gb_status st = check_launch(pool, "append", e);
   if (st != GB_OK) return st;
   pool->next_layer = (layer + 1) % pool->cfg.num_layers;
   return GB_OK;
@@ -883,16 +885,18 @@ static gb_status decode_layer(gb_pool* pool, int layer, const RotationView& rot,
     if (st != GB_OK) return st;
     if (rot.table) q_dev = turned_q;
     prof_begin(pool, GB_PROF_ATTENTION, s);
-    launch_decode8(pool, layer, q_dev, scale, out_dev, flags == GB_PATH_PER_BEAM ? 0 : flags == GB_PATH_GROUPED ? 1 : 2, s);
+    const cudaError_t e =
+        launch_decode8(pool, layer, q_dev, scale, out_dev, flags == GB_PATH_PER_BEAM ? 0 : flags == GB_PATH_GROUPED ? 1 : 2, s);
     prof_end(pool, GB_PROF_ATTENTION, s);
-    return check_launch(pool, "decode");
+    return check_launch(pool, "decode", e);
   }
   if (rot.table && (((uintptr_t)q_dev | (uintptr_t)k_new_dev | (uintptr_t)v_new_dev) & 15))
     return fail(pool, GB_ERR_INVALID, "decode: rows start on 16 bytes");
   gb_status st = append_layer(pool, layer, 1, k_new_dev, v_new_dev, true, RotationView{}, nullptr, nullptr, s);
   if (st != GB_OK) return st;
   if (rot.table) {
-    launch_turn(pool, rot, q_dev, turned_q, k_new_dev, turned, s);
+    st = check_launch(pool, "turn", launch_turn(pool, rot, q_dev, turned_q, k_new_dev, turned, s));
+    if (st != GB_OK) return st;
     q_dev = turned_q;
     k_new_dev = turned;
   }
@@ -913,10 +917,8 @@ static gb_status decode_layer(gb_pool* pool, int layer, const RotationView& rot,
   // shares of the SMs (decode_ctas), or one after the other on every SM.
   const int mode = (flags == GB_PATH_PER_BEAM || !pool->view.grouped) ? 0 : 1;
   prof_begin(pool, GB_PROF_ATTENTION, s);
-  if (launch_decode(pool, layer, q_dev, k_new_dev, v_new_dev, scale, out_dev, mode, flags != GB_PATH_GROUPED, s) !=
-      cudaSuccess)
-    return check_launch(pool, "decode");
-  return check_launch(pool, "decode");
+  return check_launch(pool, "decode", launch_decode(pool, layer, q_dev, k_new_dev, v_new_dev, scale, out_dev, mode,
+                                                    flags != GB_PATH_GROUPED, s));
 }
 
 extern "C" gb_status gb_decode_attention(gb_pool* pool, int layer, const void* q_dev,
@@ -947,9 +949,7 @@ extern "C" gb_status gb_release(gb_pool* pool, const int32_t* slots_dev, int n, 
   pool->launches += 1;
   gb_status st = check_launch(pool, "release");
   if (st != GB_OK) return st;
-  if (rebuild_segments(pool, reinterpret_cast<cudaStream_t>(stream)) != cudaSuccess)
-    return check_launch(pool, "segments");
-  return GB_OK;
+  return check_launch(pool, "segments", rebuild_segments(pool, reinterpret_cast<cudaStream_t>(stream)));
 }
 
 extern "C" gb_status gb_pool_status(gb_pool* pool, int* device_status, gb_stream_t stream) {
@@ -999,10 +999,8 @@ extern "C" gb_status gb_pool_launch_count(gb_pool* pool, uint64_t* count) {
 
 extern "C" gb_status gb_pool_wait_selftest(gb_pool* pool, gb_stream_t stream) {
   if (!pool) return GB_ERR_INVALID;
-  if (launch_wait_selftest(pool, reinterpret_cast<cudaStream_t>(stream)) != cudaSuccess)
-    return check_launch(pool, "wait_selftest");
   pool->launches += 1;
-  return check_launch(pool, "wait_selftest");
+  return check_launch(pool, "wait_selftest", launch_wait_selftest(pool, reinterpret_cast<cudaStream_t>(stream)));
 }
 
 extern "C" gb_status gb_pool_clear_status(gb_pool* pool, gb_stream_t stream) {
