@@ -134,7 +134,8 @@ gb_status gb_pool_destroy(gb_pool* pool);
  * [num_layers][prompt_len][Hkv][D] in kv_dtype.  Running means start at 0
  * with n = 0.  Slots get lineage ids in order.
  * Errors: GB_ERR_STATE unless every slot is inactive; GB_ERR_INVALID for a
- * bad count or length; out of pages is reported in the device status.
+ * bad count or length, or rows that do not start on 16 bytes; out of pages is
+ * reported in the device status.
  */
 gb_status gb_pool_seed(gb_pool* pool, int n_beams, int prompt_len, const void* k_prompt_dev,
                        const void* v_prompt_dev, gb_stream_t stream);
@@ -162,9 +163,11 @@ gb_status gb_pool_seed(gb_pool* pool, int n_beams, int prompt_len, const void* k
  * the pool is bf16 and the step is not a small one, so they must all get an SM
  * within the wait limit (2 s): nothing else should hold the GPU's SMs for that
  * long meanwhile.  An fp32 pool's CTAs never wait on one another.
- * Errors: GB_ERR_STATE for a layer out of order; out of pages is reported in
- * the device status and makes the whole step a no-op; a wait that runs out
- * records GB_ERR_TIMEOUT and zeroes the outputs it could not complete.
+ * Errors: GB_ERR_STATE for a layer out of order; GB_ERR_INVALID for q, k_new
+ * or v_new that do not start on 16 bytes (GB_PATH_PER_BEAM of a GB_BF16 pool: q
+ * on 4); out of pages is reported in the device status and makes the whole step
+ * a no-op; a wait that runs out records GB_ERR_TIMEOUT and zeroes the outputs it
+ * could not complete.
  */
 gb_status gb_decode_attention(gb_pool* pool, int layer, const void* q_dev, const void* k_new_dev,
                               const void* v_new_dev, float scale, float* out_dev, int flags,
@@ -200,8 +203,7 @@ typedef struct {
 
 /*
  * gb_append_kv with the keys rotated to the positions that they are appended at.  Errors: as gb_append_kv, and
- * GB_ERR_INVALID for a bad rotation or rows that do not start on 16 bytes, GB_ERR_STATE when the pool is on another device
- * than the current one.
+ * GB_ERR_INVALID for a bad rotation, GB_ERR_STATE when the pool is on another device than the current one.
  */
 gb_status gb_append_kv_rotated(gb_pool* pool, int layer, int n_tokens, const gb_rotation* rotation, const void* k_dev,
                                const void* v_dev, gb_stream_t stream);

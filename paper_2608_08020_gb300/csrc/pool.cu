@@ -766,12 +766,16 @@ extern "C" const char* gb_last_error(gb_pool* pool) {
   return pool ? pool->last_error.c_str() : "";
 }
 
+// Every kernel reads rows in pieces of 16 bytes.
+static bool on_16_bytes(const void* a, const void* b) { return (((uintptr_t)a | (uintptr_t)b) & 15) == 0; }
+
 extern "C" gb_status gb_pool_seed(gb_pool* pool, int n_beams, int prompt_len, const void* k_prompt_dev,
                                   const void* v_prompt_dev, gb_stream_t stream) {
   if (!pool) return GB_ERR_INVALID;
   if (pool->seeded) return fail(pool, GB_ERR_STATE, "seed: pool already seeded");
   if (n_beams < 1 || n_beams > pool->cfg.max_beams || prompt_len < 1 || !k_prompt_dev || !v_prompt_dev)
     return fail(pool, GB_ERR_INVALID, "seed: bad arguments");
+  if (!on_16_bytes(k_prompt_dev, v_prompt_dev)) return fail(pool, GB_ERR_INVALID, "seed: rows start on 16 bytes");
   if ((prompt_len + pool->cfg.page_size - 1) / pool->cfg.page_size > 2048)
     return fail(pool, GB_ERR_UNSUPPORTED, "seed: prompt longer than 2048 pages");
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
@@ -803,6 +807,7 @@ static gb_status append_layer(gb_pool* pool, int layer, int n_tokens, const void
   if (!pool->seeded) return fail(pool, GB_ERR_STATE, "pool not seeded");
   if (layer < 0 || layer >= pool->cfg.num_layers || n_tokens < 1 || !k || !v)
     return fail(pool, GB_ERR_INVALID, "append: bad arguments");
+  if (!on_16_bytes(k, v)) return fail(pool, GB_ERR_INVALID, "append: rows start on 16 bytes");
   if (layer != pool->next_layer) return fail(pool, GB_ERR_STATE, "layers of a step must be called in order");
   if (layer == 0) {
     ++pool->epoch;
@@ -860,7 +865,6 @@ extern "C" gb_status gb_append_kv_rotated(gb_pool* pool, int layer, int n_tokens
   RotationView rot;
   const gb_status st = rotation_view(pool, rotation, &rot);
   if (st != GB_OK) return st;
-  if (((uintptr_t)k_dev | (uintptr_t)v_dev) & 15) return fail(pool, GB_ERR_INVALID, "append: rows start on 16 bytes");
   return append_layer(pool, layer, n_tokens, k_dev, v_dev, false, rot, nullptr, nullptr, reinterpret_cast<cudaStream_t>(stream));
 }
 
@@ -874,13 +878,13 @@ static gb_status decode_layer(gb_pool* pool, int layer, const RotationView& rot,
                               cudaStream_t s) {
   if (!q_dev || !out_dev) return fail(pool, GB_ERR_INVALID, "decode: null pointer");
   if (flags < GB_PATH_AUTO || flags > GB_PATH_GROUPED) return fail(pool, GB_ERR_INVALID, "decode: bad flags");
+  const bool words = pool->cfg.kv_dtype == GB_BF16 && flags == GB_PATH_PER_BEAM && !rot.table;  // reads q by words
+  if ((uintptr_t)q_dev & (words ? 3 : 15)) return fail(pool, GB_ERR_INVALID, "decode: rows start on 16 bytes");
   char* turned = reinterpret_cast<char*>(pool->view.mlp_scratch) + pool->layout.rotated;  // keys, then queries
   char* turned_q = turned + align256(new_rows_bytes(pool->cfg));
   if (pool->cfg.kv_dtype == GB_FP8) {
     // The new rows go to the cache in a launch of their own, which turns the queries too: a row may change its whole
     // block's exponent, so the attention launch would have had to write what it reads.
-    if (((uintptr_t)q_dev | (uintptr_t)k_new_dev | (uintptr_t)v_new_dev) & 15)
-      return fail(pool, GB_ERR_INVALID, "decode: rows start on 16 bytes");
     const gb_status st = append_layer(pool, layer, 1, k_new_dev, v_new_dev, false, rot, rot.table ? q_dev : nullptr, turned_q, s);
     if (st != GB_OK) return st;
     if (rot.table) q_dev = turned_q;
@@ -890,8 +894,6 @@ static gb_status decode_layer(gb_pool* pool, int layer, const RotationView& rot,
     prof_end(pool, GB_PROF_ATTENTION, s);
     return check_launch(pool, "decode", e);
   }
-  if (rot.table && (((uintptr_t)q_dev | (uintptr_t)k_new_dev | (uintptr_t)v_new_dev) & 15))
-    return fail(pool, GB_ERR_INVALID, "decode: rows start on 16 bytes");
   gb_status st = append_layer(pool, layer, 1, k_new_dev, v_new_dev, true, RotationView{}, nullptr, nullptr, s);
   if (st != GB_OK) return st;
   if (rot.table) {
