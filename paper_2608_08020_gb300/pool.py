@@ -59,14 +59,16 @@ class BeamPool:
         if rotation is None:
             B.gb_decode_attention(self.handle, layer, q, k_new, v_new, scale, out, flags, stream)
         else:
-            B.gb_decode_attention_rotated(self.handle, layer, self._rotation(rotation), q, k_new, v_new, scale, out, flags, stream)
+            on = self._rotate_on(rotation, stream)
+            B.gb_decode_attention_rotated(self.handle, layer, rotation.args, q, k_new, v_new, scale, out, flags, on)
 
     def append_kv(self, layer, n_tokens, k, v, stream=None, rotation=None):
         """`rotation`: a Rotation; k is then given as the projection leaves it."""
         if rotation is None:
             B.gb_append_kv(self.handle, layer, n_tokens, k, v, stream)
         else:
-            B.gb_append_kv_rotated(self.handle, layer, n_tokens, self._rotation(rotation), k, v, stream)
+            on = self._rotate_on(rotation, stream)
+            B.gb_append_kv_rotated(self.handle, layer, n_tokens, rotation.args, k, v, on)
 
     def read_kv(self, layer, first, n_tokens, stream=None):
         """(keys, values) of tokens first[slot] .. first[slot] + n_tokens - 1 (first int32 [max_beams]) as the cache holds
@@ -80,11 +82,11 @@ class BeamPool:
         B.gb_read_kv(self.handle, layer, first, n_tokens, k, v, stream)
         return k, v
 
-    def _rotation(self, r):
+    def _rotate_on(self, r, stream):
         if r.head_dim != self.cfg.head_dim or r.table.device != self.kv.device:
             raise ValueError(f"rotation: of heads of {r.head_dim} on {r.table.device}, the pool's are of {self.cfg.head_dim} "
                              f"on {self.kv.device}")
-        return r.args
+        return r.used_on(stream)
 
     def score_probe(self, hidden, hidden_dtype: str, w, bias=0.0, mask=None, score_out=None, stream=None):
         B.gb_score_probe(self.handle, hidden, _DT[hidden_dtype], hidden.shape[-1], w, bias, mask, score_out, stream)

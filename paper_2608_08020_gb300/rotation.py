@@ -2,7 +2,9 @@
 
 ``BeamPool.append_kv`` and ``BeamPool.decode_attention`` take one: keys (and a decode step's queries) are then given as
 the projection leaves them, and the library turns them to the positions that they are appended at, which only the pool
-on the device knows.  The object is the table of angles; it belongs to no pool and may serve many.
+on the device knows.  The object is the table of angles; it belongs to no pool and may serve many.  It may be dropped while
+calls that use it are still to run, but for those on a raw stream handle and those in a captured graph, which reads the table
+at each replay: for these the caller keeps it.
 """
 from __future__ import annotations
 
@@ -42,4 +44,14 @@ class Rotation:
         self.device = self.table.device
         if self.device.type == "cuda" and not torch.cuda.is_current_stream_capturing():
             torch.cuda.current_stream(self.device).synchronize()       # calls may be on any stream
+        # Streams that the table's memory waits for before others get it: the one that it comes from, and each that used it.
+        self._streams = {torch.cuda.current_stream(self.device).cuda_stream} if self.device.type == "cuda" else set()
         self.args = B.GbRotation(self.table.data_ptr(), max_positions, r, int(self.interleaved))
+
+    def used_on(self, stream) -> int:
+        """The handle of `stream` (as BeamPool's calls take it), on which a call is about to read the table."""
+        handle = B.stream_handle(stream)
+        if handle not in self._streams and not isinstance(stream, int):
+            self.table.record_stream(torch.cuda.current_stream(self.device) if stream is None else stream)
+            self._streams.add(handle)
+        return handle
