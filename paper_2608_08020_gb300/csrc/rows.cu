@@ -73,7 +73,7 @@ __device__ __forceinline__ void write_block(const PoolView& v, int layer, const 
       if (h + 1 < heads) load();
 #pragma unroll
       for (int i = 0; i < kMine; ++i) {
-        if (turns && row(i) - half < cnt) turn_row<DT>(f[i], rot, row(i) < cnt ? t0 + row(i) : -1);
+        if (turns && row(i) - half < cnt) turn_row<DT, false>(f[i], rot, row(i) < cnt ? t0 + row(i) : -1);
 #pragma unroll
         for (int e = 0; e < N; ++e) amax = fmaxf(amax, fabsf(f[i][e]));  // (passes over NaN)
       }

@@ -64,13 +64,15 @@ struct RotationView {
 
 // a cos + g sin (g: minus the pair's other value, or it), rounded once: the products' and the sum's rounding errors are carried
 // along.  What follows rounds to 16 or 8 bits, and a result that is off in its last place can end on the other side of a tie
-// there.
+// there.  Where the plain sum is infinite the errors are no numbers, and it stays (Inf; 8 bits hold neither).
+template <bool Inf>
 __device__ __forceinline__ float turn(float a, float c, float ce, float g, float s, float se) {
   const float p = __fmul_rn(a, c), q = __fmul_rn(g, s);
   const float pe = __fmaf_rn(a, ce, __fmaf_rn(a, c, -p)), qe = __fmaf_rn(g, se, __fmaf_rn(g, s, -q));
   const float d = __fadd_rn(p, q), t = __fsub_rn(d, p);
   const float err = __fadd_rn(__fsub_rn(p, __fsub_rn(d, t)), __fsub_rn(q, t));
-  return __fadd_rn(d, __fadd_rn(err, __fadd_rn(pe, qe)));
+  const float r = __fadd_rn(d, __fadd_rn(err, __fadd_rn(pe, qe)));
+  return Inf && r != r ? d : r;
 }
 
 template <int DT>
@@ -132,7 +134,7 @@ __device__ __forceinline__ void angles(const RotationView& rot, int pos, int i0,
 
 // Turn the row that lanes 16h .. 16h + 15 hold (h: this lane's half of the warp) to position pos.  Every lane of
 // the warp calls it; pos may differ between the halves.  A position past the table leaves the row as it is.
-template <int DT>
+template <int DT, bool Inf = true>
 __device__ __forceinline__ void turn_row(float (&f)[RowTraits<DT>::N], const RotationView& rot, int pos) {
   constexpr int N = RowTraits<DT>::N;
   const int j = threadIdx.x & 15;
@@ -145,8 +147,8 @@ __device__ __forceinline__ void turn_row(float (&f)[RowTraits<DT>::N], const Rot
 #pragma unroll
       for (int i = 0; i < N / 2; ++i) {
         const float a = f[2 * i], b = f[2 * i + 1];
-        f[2 * i] = turn(a, c[0][i], c[1][i], -b, c[2][i], c[3][i]);
-        f[2 * i + 1] = turn(b, c[0][i], c[1][i], a, c[2][i], c[3][i]);
+        f[2 * i] = turn<Inf>(a, c[0][i], c[1][i], -b, c[2][i], c[3][i]);
+        f[2 * i + 1] = turn<Inf>(b, c[0][i], c[1][i], a, c[2][i], c[3][i]);
       }
     }
     return;
@@ -161,7 +163,7 @@ __device__ __forceinline__ void turn_row(float (&f)[RowTraits<DT>::N], const Rot
     float c[4][N];
     angles(rot, pos, N * (low ? j : j - away), c);
 #pragma unroll
-    for (int i = 0; i < N; ++i) f[i] = turn(f[i], c[0][i], c[1][i], low ? -g[i] : g[i], c[2][i], c[3][i]);
+    for (int i = 0; i < N; ++i) f[i] = turn<Inf>(f[i], c[0][i], c[1][i], low ? -g[i] : g[i], c[2][i], c[3][i]);
   }
 }
 
