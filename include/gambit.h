@@ -158,11 +158,13 @@ gb_status gb_pool_seed(gb_pool* pool, int n_beams, int prompt_len, const void* k
  * v_new_dev (the rows are then copied first).
  * Launches: one attention launch that also appends the new rows and merges
  * the split and shared-prefix partial results into out_dev; layer 0 adds the
- * step's planner first.  The
+ * step's planner first.  (GB_FP8: the rows are appended by a launch before it,
+ * and layer 0 adds one more, the copies of shared tail pages.)  The
  * attention launch's CTAs wait (bounded) on each other's partial results where
- * the pool is bf16 and the step is not a small one, so they must all get an SM
- * within the wait limit (2 s): nothing else should hold the GPU's SMs for that
- * long meanwhile.  An fp32 pool's CTAs never wait on one another.
+ * the pool is bf16 and the step is not a small one, or the pool is GB_FP8, so
+ * they must all get an SM within the wait limit (2 s): nothing else should hold
+ * the GPU's SMs for that long meanwhile.  An fp32 pool's CTAs never wait on one
+ * another.
  * Errors: GB_ERR_STATE for a layer out of order; GB_ERR_INVALID for q, k_new
  * or v_new that do not start on 16 bytes (GB_PATH_PER_BEAM of a GB_BF16 pool: q
  * on 4); out of pages is reported in the device status and makes the whole step
@@ -192,7 +194,8 @@ gb_status gb_append_kv(gb_pool* pool, int layer, int n_tokens, const void* k_dev
  *   table_dev: fp32 [positions][4][rotary_dim / 2], 16-byte aligned: cos, its rounding errors (the exact values minus the
  *              rounded ones, rounded), sin, its rounding errors; any angles, and amplitudes too, as the caller fills it
  *   rotary_dim: a multiple of 16, at most head_dim
- * A token at a position that the table does not have is not rotated, and the device status records GB_ERR_INVALID.
+ * A token at a position that the table does not have is not rotated, and the device status records GB_ERR_INVALID.  What passes
+ * fp32's range in a rotation is infinite.
  */
 typedef struct {
   const float* table_dev;
@@ -704,8 +707,9 @@ gb_status gb_truncate(gb_pool* pool, const int32_t* lengths_dev, gb_stream_t str
  *                min_p above 1 counts as 1
  *   token:       int32 [rows]; -1 for a row that has only -infinity
  *   logprob:     fp32 [rows] natural logarithm of the token's share of what is kept (-infinity with token -1), or NULL
- * Masses are summed exactly (weights to 2^-33 of themselves), so a row's token does not depend on the other rows or the number of
- * SMs.  Outputs must not overlap inputs.  No workspace; one launch, none without rows.
+ * Masses are whole numbers, so a row's token does not depend on the other rows or the number of SMs.  A weight is held to 2^-28 of
+ * itself and 2^-45 of the largest one, and counts as none below 2^-46 of it; top-p's total takes those below 2^-24 of the largest to
+ * 2^-17 of themselves.  Outputs must not overlap inputs.  No workspace; one launch, none without rows.
  * Errors: GB_ERR_INVALID for bad sizes, pointers or alignment (each value's own), GB_ERR_UNSUPPORTED for a vocab above 524,288,
  * GB_ERR_TOO_LARGE for more rows than a grid takes.
  */

@@ -7,9 +7,10 @@
 // so what is kept is always a head of that order: the tokens with x > K, and those with x = K up to some index.  The token is
 // the first, by index, at which the kept tokens' mass passes u times its total.
 //
-// A token is compared against sums over the whole vocabulary, so masses are whole numbers: w in units of 2^-44, right to about
-// 2^-31 of itself, summed in 64 bits.  Sums are then the same in any order, and no draw depends on how the row was split.
-// (Tokens below 2^-24 of the largest enter top-p's total by the 22 bits of exp2f.)
+// A token is compared against sums over the whole vocabulary, so masses are whole numbers: w in units of 2^-44, right to 2^-28 of
+// itself (weights_of) and half a unit, summed in 64 bits.  Sums are then the same in any order, and no draw depends on how the row
+// was split.  (Tokens below 2^-24 of the largest enter top-p's total by exp2f of an fp32 exponent: right to 2^-17 of themselves, as
+// the exponent, up to 46, has three roundings of 2^-24.)
 //
 // A cluster of CTAs a row, which reads it two to four times; all but the first time from L2:
 //   1. the largest logit; with top-k a value that at least k tokens reach, of the threads' largest,
@@ -120,7 +121,9 @@ __device__ __forceinline__ float exponent(const Row& row, float x) { return __fm
 
 // exp((x - max) / T) = m 2^-31 2^-n with m in (2^30, 2^31], for a logit with exponent() below kFar; j = floor(256 y), n = j >> 8.
 // y is taken to 2^-40 of itself or better; m is the table's 2^(-(j & 255)/256) less its share 1 - 2^-r, 0 <= r < 2^-8, to the
-// third order and in units of 2^-31.  Two at a time, as the fp32 units take them; of other logits something without meaning.
+// third order and in units of 2^-31.  Together within 3 units: half of one in the table, one that the product's floor cuts off, half
+// in q and as much in its terms' roundings; 2^-29.0 of the weight is the most that 40 million of them were off.
+// Two at a time, as the fp32 units take them; of other logits something without meaning.
 struct Weight {
   uint32_t m;
   int j;

@@ -622,7 +622,8 @@ __global__ void __launch_bounds__(kTourThreads, 1) k_tournament(PoolView v, Tour
     }
   }
   // The list holds at most 9 * max_beams + 2 * SMs entries (each beam sits in at most
-  // kMaxSegDepth segments of >= 2 sharers) and a beam at most kMaxSegDepth + 32 records,
+  // kMaxSegDepth segments of >= 2 sharers; of an 8-bit pool, where 2 * SMs is 32 * max_beams
+  // if that is more) and a beam at most kMaxSegDepth + 32 records,
   // so neither limit is reached for pools of 8 beams or more.  Should the list still
   // overflow, the step is left entirely to the per-beam path.
   const bool overflow = total > wcap;
