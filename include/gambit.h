@@ -345,6 +345,15 @@ gb_status gb_pool_clear_status(gb_pool* pool, gb_stream_t stream);
  */
 gb_status gb_pool_wait_selftest(gb_pool* pool, gb_stream_t stream);
 
+/*
+ * Diagnostic of the failure path (not part of the method): gb_decode_attention of a GB_FP8 pool, but in each CTA of the attention
+ * launch one load never comes, that of the CTA's `stalled`-th 32 tokens (from 0, over all that it reads).  The CTAs that read so
+ * many wait for it (2 s), give up and leave; the outputs that the launch could not complete are zero, the device status becomes
+ * GB_ERR_TIMEOUT, and the context and the pool stay usable.  Errors: as gb_decode_attention, GB_ERR_UNSUPPORTED for other pools.
+ */
+gb_status gb_decode_wait_selftest(gb_pool* pool, int layer, const void* q_dev, const void* k_new_dev, const void* v_new_dev,
+                                  float scale, float* out_dev, int flags, int stalled, gb_stream_t stream);
+
 /* Synchronise `stream` and copy the pool state into host arrays (see gb_pool_state). */
 gb_status gb_pool_read_state(gb_pool* pool, const gb_pool_state* state, gb_stream_t stream);
 

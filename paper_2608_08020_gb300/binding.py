@@ -27,7 +27,7 @@ GB_PATH_AUTO, GB_PATH_PER_BEAM, GB_PATH_GROUPED = 0, 1, 2
 # Every symbol the header declares, in header order.
 EXPORTS = ["gb_pool_workspace_bytes", "gb_pool_init", "gb_pool_destroy", "gb_pool_seed", "gb_decode_attention",
            "gb_append_kv", "gb_append_kv_rotated", "gb_decode_attention_rotated", "gb_read_kv", "gb_score_probe", "gb_push_scores", "gb_prune_branch", "gb_release", "gb_pool_status",
-           "gb_pool_clear_status", "gb_pool_wait_selftest", "gb_pool_read_state", "gb_pool_set_profile_events", "gb_pool_launch_count",
+           "gb_pool_clear_status", "gb_pool_wait_selftest", "gb_decode_wait_selftest", "gb_pool_read_state", "gb_pool_set_profile_events", "gb_pool_launch_count",
            "gb_paged_decode_noalloc", "gb_paged_decode_noalloc_status", "gb_pool_read_step_stats", "gb_pool_set_capacity", "gb_pool_last_ranked", "gb_score_mlp", "gb_fork_slots", "gb_scorer_sizes", "gb_scorer_seed",
            "gb_scorer_step", "gb_prompt_workspace_bytes", "gb_prompt_attention", "gb_prompt_status", "gb_prompt_wait_selftest",
            "gb_draft_workspace_bytes", "gb_draft_attention", "gb_accept_draft", "gb_truncate", "gb_sample", "gb_last_error"]
@@ -120,6 +120,7 @@ def load(path: Path | None = None) -> ctypes.CDLL:
         "gb_pool_status": [V, P, V],
         "gb_pool_clear_status": [V, V],
         "gb_pool_wait_selftest": [V, V],
+        "gb_decode_wait_selftest": [V, I, V, V, V, F, V, I, I, V],
         "gb_pool_read_state": [V, P, V],
         "gb_pool_set_profile_events": [V, I, V, V],
         "gb_pool_launch_count": [V, P],
@@ -347,6 +348,11 @@ def gb_pool_clear_status(pool: int, stream=None) -> None:
 
 def gb_pool_wait_selftest(pool: int, stream=None) -> None:
     _check(pool, load().gb_pool_wait_selftest(pool, stream_handle(stream)), "gb_pool_wait_selftest")
+
+
+def gb_decode_wait_selftest(pool: int, layer: int, q, k_new, v_new, scale: float, out, flags: int, stalled: int, stream=None) -> None:
+    _check(pool, load().gb_decode_wait_selftest(pool, layer, ptr(q), ptr(k_new), ptr(v_new), float(scale), ptr(out), flags, stalled,
+                                                stream_handle(stream)), "gb_decode_wait_selftest")
 
 
 def gb_pool_read_state(pool: int, state: GbPoolState, stream=None) -> None:

@@ -371,8 +371,10 @@ __device__ __forceinline__ Shares shares_of(const PoolView& v, int mode, int nac
 
 // ---- the loading warps -----------------------------------------------------------------------------
 
-// The stages of every unit whose ring slot is this loader's (number `own` of kLoaders8).
-__device__ void load_stages(const PoolView& v, const CUtensorMap* tm, int layer, unsigned char* smem, uint32_t bars, int own, int lane) {
+// The stages of every unit whose ring slot is this loader's (number `own` of kLoaders8), but for the CTA's stage `stalled`, which never
+// comes (-1: none, but in a self-test).
+__device__ void load_stages(const PoolView& v, const CUtensorMap* tm, int layer, int stalled, unsigned char* smem, uint32_t bars, int own,
+                            int lane) {
   const uint32_t full = bars, empty = bars + 8 * kStages8, ufull = bars + 16 * kStages8, uempty = ufull + 8 * kSlots8;
   volatile int* stop = reinterpret_cast<volatile int*>(smem + Smem8::STOP);
   const uint64_t once = policy_evict_first(), more = policy_evict_normal();
@@ -428,7 +430,7 @@ __device__ void load_stages(const PoolView& v, const CUtensorMap* tm, int layer,
         const bool good = !(mine && kk >= kStages8) || wait_or_stop(empty + 8 * st, (kk / kStages8 - 1) & 1, stop);
         ok = __all_sync(0xffffffffu, good);
         if (!ok) break;
-        if (mine) {
+        if (mine && (int)kk != stalled) {
           *reinterpret_cast<int2*>(smem + Smem8::EXPS + 16 * st + 8 * (lane & 1)) = in ? make_int2(ek, ev) : make_int2(0, 0);
           const uint32_t bar = full + 8 * st;
           if (in) {
@@ -600,10 +602,10 @@ __device__ __forceinline__ void load_queries(Tile8& t, const PoolView& v, const 
   tile_load(t, row < u.rows ? q + ((size_t)u.members[row / G] * v.Hq + (size_t)u.head * G + row % G) * 128 : nullptr, c);
 }
 
-// One unit by the multiplying warps.  A warp whose wait ran out still keeps step with the others; what the unit then leaves is
-// nobody's, as the status is set.  next(): called when the queries are no longer needed.
+// One unit by the multiplying warps.  A warp whose wait ran out still keeps step with the others, and none of the unit's outputs is
+// written (its records may be: nobody counts them): false.  next(): called when the queries are no longer needed.
 template <int G, class Next>
-__device__ __forceinline__ void multiply(Tile8& t, const PoolView& v, const Unit8& u, float qscale, uint32_t base, uint32_t bars,
+__device__ __forceinline__ bool multiply(Tile8& t, const PoolView& v, const Unit8& u, float qscale, uint32_t base, uint32_t bars,
                                          unsigned char* smem, float* out, Next next) {
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = lane >> 2, c = lane & 3;
   const uint32_t full = bars, empty = bars + 8 * kStages8, ring = smem_addr(smem);
@@ -612,10 +614,14 @@ __device__ __forceinline__ void multiply(Tile8& t, const PoolView& v, const Unit
   tile_begin(t, qscale, c);
   const int stages = (u.tokens + 2 * kChunk - 1) / (2 * kChunk);
   const bool any = rg * 8 < u.rows;  // (without rows the stages' slots are only given back)
+  bool whole = true;
 #pragma unroll 1
   for (int i = group; i < stages; i += groups) {
     const uint32_t k = base + i, s = k % kStages8;
-    if (!__all_sync(0xffffffffu, wait_or_stop(full + 8 * s, (k / kStages8) & 1, stop))) break;
+    if (!__all_sync(0xffffffffu, wait_or_stop(full + 8 * s, (k / kStages8) & 1, stop))) {
+      whole = false;
+      break;
+    }
     auto leave = [&] {
       __syncwarp();
       if (lane == 0) mbar_arrive_n(empty + 8 * s, groups);
@@ -645,7 +651,7 @@ __device__ __forceinline__ void multiply(Tile8& t, const PoolView& v, const Unit
         st_hint(rec + G * 128 + G + row % G, z ? t.l1 : t.l0, pol);
       }
     }
-    return;
+    return whole;
   }
   // The warps' states of the same rows, merged through shared memory four rows of each at a time.
   float* left = reinterpret_cast<float*>(smem + Smem8::MERGE);
@@ -662,7 +668,7 @@ __device__ __forceinline__ void multiply(Tile8& t, const PoolView& v, const Unit
         if (r == 0) ml[in] = z ? make_float2(t.m1, t.l1) : make_float2(t.m0, t.l0);
       }
     }
-    consumers_sync();
+    if (consumers_any(!whole)) return false;
     for (int i = tid; i < rgroups * 4 * 32; i += kConsumers8 * 32) {
       const int g = i >> 7, in = (i >> 5) & 3, row = g * 8 + 4 * f + in, d = 4 * (i & 31);
       if (row >= u.rows) continue;
@@ -698,10 +704,12 @@ __device__ __forceinline__ void multiply(Tile8& t, const PoolView& v, const Unit
     }
     consumers_sync();
   }
+  return true;
 }
 
+// Every unit that the CTA takes; false where a wait ran out.
 template <int G>
-__device__ void multiply_units(const PoolView& v, const Counters& cnt, const __nv_bfloat16* q, float qscale, int mode, unsigned char* smem,
+__device__ bool multiply_units(const PoolView& v, const Counters& cnt, const __nv_bfloat16* q, float qscale, int mode, unsigned char* smem,
                                uint32_t bars, float* out) {
   const int tid = threadIdx.x, lane = tid & 31;
   const uint32_t ufull = bars + 16 * kStages8, uempty = ufull + 8 * kSlots8;
@@ -720,7 +728,7 @@ __device__ void multiply_units(const PoolView& v, const Counters& cnt, const __n
     const int slot = k % kSlots8;
     if (consumers_any(!there || *stop != 0)) {  // all leave together
       if (tid == 0) set_status(v.ctl, GB_ERR_TIMEOUT);
-      return;
+      return false;
     }
     const Unit8& u = units[slot];
     if (segments && u.kind != kUnitSegment) {  // this CTA's segment records are written
@@ -730,11 +738,11 @@ __device__ void multiply_units(const PoolView& v, const Counters& cnt, const __n
       }
       segments = false;
     }
-    if (u.kind == kUnitEnd) return;
-    multiply<G>(t, v, u, qscale, base, bars, smem, out, [&] { arrive_at(k + 1); });
+    if (u.kind == kUnitEnd) return true;
+    const bool done = multiply<G>(t, v, u, qscale, base, bars, smem, out, [&] { arrive_at(k + 1); });
     base += (u.tokens + 2 * kChunk - 1) / (2 * kChunk);
-    if (tid == 0 && u.kind == kUnitBeam && !u.direct) {
-      fence_acq_rel_gpu();
+    if (tid == 0 && u.kind == kUnitBeam && done) {  // (a pair written at once is counted for zero_unwritten alone)
+      if (!u.direct) fence_acq_rel_gpu();
       atomicAdd(&cnt.pair[u.members[0] * v.Hkv + u.head], 1);
     }
     __syncwarp();
@@ -742,9 +750,21 @@ __device__ void multiply_units(const PoolView& v, const Counters& cnt, const __n
   }
 }
 
+// A CTA gave up, with units that it had taken: zeros for every pair that was to be written at once and has not been.  (The
+// others' merges give them zeros.)
+template <int G>
+__device__ void zero_unwritten(const PoolView& v, const Counters& cnt, int mode, const Shares& sh, float* out) {
+  for (int p = threadIdx.x >> 5; p < v.max_beams * v.Hkv; p += kConsumers8) {
+    const int b = p / v.Hkv, h = p - b * v.Hkv, n = v.active[b] ? plan_n(v, mode)[b] : 0;
+    if (n == 0 || (mode == 1 && v.seg_nrec[b] > 0)) continue;
+    const int o0 = plan_off(v, mode)[b] + h * n;
+    if (sh.of(o0) == sh.of(o0 + n - 1) && ld_acquire_gpu(&cnt.pair[p]) == 0) zero_pair<G>(v, b, h, out);
+  }
+}
+
 template <int G>
 __global__ void __launch_bounds__(kThreads8, 1)
-    k_decode8(PoolView v, const __grid_constant__ CUtensorMap tm, int layer, const __nv_bfloat16* q, float qscale, int mode,
+    k_decode8(PoolView v, const __grid_constant__ CUtensorMap tm, int layer, const __nv_bfloat16* q, float qscale, int mode, int stalled,
               float* __restrict__ out) {
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   unsigned char* smem = smem_raw + ((1024 - (smem_addr(smem_raw) & 1023)) & 1023);
@@ -797,17 +817,17 @@ __global__ void __launch_bounds__(kThreads8, 1)
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kLoaderRegs8));
     const int w = (tid >> 5) - kConsumers8;
     if (w == 0) plan_units<G>(v, cnt, mode, sh, smem, bars, tid & 31);
-    else if (w <= kLoaders8) load_stages(v, &tm, layer, smem, bars, w - 1, tid & 31);
+    else if (w <= kLoaders8) load_stages(v, &tm, layer, stalled, smem, bars, w - 1, tid & 31);
     return;
   }
   asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kConsumerRegs8));
-  multiply_units<G>(v, cnt, q, qscale, mode, smem, bars, out);
+  if (!multiply_units<G>(v, cnt, q, qscale, mode, smem, bars, out)) zero_unwritten<G>(v, cnt, mode, sh, out);
   // Every CTA is resident with the others (one an SM), and each wait gives up once the status is set.
   combine_shares<G, true>(v, cnt, mode, [sh](int x) { return sh.of(x); }, nctas, false, cta, nctas, kConsumers8, out);
 }
 
 template <int G>
-cudaError_t launch_decode8_t(gb_pool* pool, int layer, const void* q, float scale, float* out, int mode, cudaStream_t s) {
+cudaError_t launch_decode8_t(gb_pool* pool, int layer, const void* q, float scale, float* out, int mode, int stalled, cudaStream_t s) {
   cudaError_t e = set_max_dynamic_smem(reinterpret_cast<const void*>(k_decode8<G>), Smem8::TOTAL);
   if (e != cudaSuccess) return e;
   // With fewer registers at launch than its warps then share out the kernel would wait for ever.
@@ -822,7 +842,7 @@ cudaError_t launch_decode8_t(gb_pool* pool, int layer, const void* q, float scal
   prof_begin(pool, GB_PROF_DECODE, s);
   e = launch_pdl(k_decode8<G>, pool->num_sms, kThreads8, Smem8::TOTAL, s, pool->view,
                  *reinterpret_cast<const CUtensorMap*>(pool->dtmap), layer, static_cast<const __nv_bfloat16*>(q),
-                 scale * 1.4426950408889634f, mode, out);
+                 scale * 1.4426950408889634f, mode, stalled, out);
   prof_end(pool, GB_PROF_DECODE, s);
   pool->launches += 1;
   return e;
@@ -830,12 +850,12 @@ cudaError_t launch_decode8_t(gb_pool* pool, int layer, const void* q, float scal
 
 }  // namespace
 
-cudaError_t launch_decode8(gb_pool* pool, int layer, const void* q, float scale, float* out, int mode, cudaStream_t s) {
+cudaError_t launch_decode8(gb_pool* pool, int layer, const void* q, float scale, float* out, int mode, int stalled, cudaStream_t s) {
   switch (pool->view.G) {
-    case 1: return launch_decode8_t<1>(pool, layer, q, scale, out, mode, s);
-    case 2: return launch_decode8_t<2>(pool, layer, q, scale, out, mode, s);
-    case 4: return launch_decode8_t<4>(pool, layer, q, scale, out, mode, s);
-    case 8: return launch_decode8_t<8>(pool, layer, q, scale, out, mode, s);
+    case 1: return launch_decode8_t<1>(pool, layer, q, scale, out, mode, stalled, s);
+    case 2: return launch_decode8_t<2>(pool, layer, q, scale, out, mode, stalled, s);
+    case 4: return launch_decode8_t<4>(pool, layer, q, scale, out, mode, stalled, s);
+    case 8: return launch_decode8_t<8>(pool, layer, q, scale, out, mode, stalled, s);
   }
   return cudaErrorInvalidValue;
 }

@@ -403,8 +403,8 @@ cudaError_t launch_turn(gb_pool* pool, const RotationView& rot, const void* q, v
 void launch_cow_rows(gb_pool* pool, cudaStream_t s);  // every layer's rows of the pages that were copied on write
 cudaError_t launch_seed_rows8(gb_pool* pool, int prompt_len, const void* k, const void* v, cudaStream_t s);
 // The attention of a layer-step of an 8-bit pool, whose new rows are in the cache already.  mode 0: every beam for itself, 1: by
-// shared segments, 2: whichever is the faster.
-cudaError_t launch_decode8(gb_pool* pool, int layer, const void* q, float scale, float* out, int mode, cudaStream_t s);
+// shared segments, 2: whichever is the faster.  stalled: -1, or the stage of each CTA that is not loaded (a self-test).
+cudaError_t launch_decode8(gb_pool* pool, int layer, const void* q, float scale, float* out, int mode, int stalled, cudaStream_t s);
 bool make_tensor_map8(gb_pool* pool);
 // The attention of one layer-step on s, written to out: mode 0, the per-beam kernel; mode 1,
 // the attention kernel with the grouped and per-beam roles (launch_attention).  Every kernel

@@ -875,7 +875,7 @@ static bool overlap(const void* a, size_t an, const void* b, size_t bn) {
 
 static gb_status decode_layer(gb_pool* pool, int layer, const RotationView& rot, const void* q_dev,
                               const void* k_new_dev, const void* v_new_dev, float scale, float* out_dev, int flags,
-                              cudaStream_t s) {
+                              cudaStream_t s, int stalled = -1) {
   if (!q_dev || !out_dev) return fail(pool, GB_ERR_INVALID, "decode: null pointer");
   if (flags < GB_PATH_AUTO || flags > GB_PATH_GROUPED) return fail(pool, GB_ERR_INVALID, "decode: bad flags");
   const bool words = pool->cfg.kv_dtype == GB_BF16 && flags == GB_PATH_PER_BEAM && !rot.table;  // reads q by words
@@ -890,7 +890,7 @@ static gb_status decode_layer(gb_pool* pool, int layer, const RotationView& rot,
     if (rot.table) q_dev = turned_q;
     prof_begin(pool, GB_PROF_ATTENTION, s);
     const cudaError_t e =
-        launch_decode8(pool, layer, q_dev, scale, out_dev, flags == GB_PATH_PER_BEAM ? 0 : flags == GB_PATH_GROUPED ? 1 : 2, s);
+        launch_decode8(pool, layer, q_dev, scale, out_dev, flags == GB_PATH_PER_BEAM ? 0 : flags == GB_PATH_GROUPED ? 1 : 2, stalled, s);
     prof_end(pool, GB_PROF_ATTENTION, s);
     return check_launch(pool, "decode", e);
   }
@@ -929,6 +929,15 @@ extern "C" gb_status gb_decode_attention(gb_pool* pool, int layer, const void* q
   if (!pool) return GB_ERR_INVALID;
   return decode_layer(pool, layer, RotationView{}, q_dev, k_new_dev, v_new_dev, scale, out_dev, flags,
                       reinterpret_cast<cudaStream_t>(stream));
+}
+
+extern "C" gb_status gb_decode_wait_selftest(gb_pool* pool, int layer, const void* q_dev, const void* k_new_dev, const void* v_new_dev,
+                                             float scale, float* out_dev, int flags, int stalled, gb_stream_t stream) {
+  if (!pool) return GB_ERR_INVALID;
+  if (pool->cfg.kv_dtype != GB_FP8) return fail(pool, GB_ERR_UNSUPPORTED, "decode_wait_selftest: of 8-bit pools");
+  if (stalled < 0) return fail(pool, GB_ERR_INVALID, "decode_wait_selftest: bad stage");
+  return decode_layer(pool, layer, RotationView{}, q_dev, k_new_dev, v_new_dev, scale, out_dev, flags,
+                      reinterpret_cast<cudaStream_t>(stream), stalled);
 }
 
 extern "C" gb_status gb_decode_attention_rotated(gb_pool* pool, int layer, const gb_rotation* rotation, const void* q_dev,
