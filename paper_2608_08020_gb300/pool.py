@@ -28,6 +28,7 @@ class BeamPool:
         kv_bytes, meta_bytes = B.gb_pool_workspace_bytes(self.cfg)
         self.kv = torch.empty(kv_bytes, dtype=torch.uint8, device=self.device)
         self.meta = torch.empty(meta_bytes, dtype=torch.uint8, device=self.device)
+        self._rotates = head_dim, self.kv.device          # what a Rotation has to be of
         self.handle = B.gb_pool_init(self.cfg, self.kv, self.meta, stream)
 
     @classmethod
@@ -83,7 +84,7 @@ class BeamPool:
         return k, v
 
     def _rotate_on(self, r, stream):
-        if r.head_dim != self.cfg.head_dim or r.table.device != self.kv.device:
+        if r.head_dim != self._rotates[0] or r.device != self._rotates[1]:
             raise ValueError(f"rotation: of heads of {r.head_dim} on {r.table.device}, the pool's are of {self.cfg.head_dim} "
                              f"on {self.kv.device}")
         return r.used_on(stream)

@@ -46,6 +46,8 @@ class TokenSampler:
         row = {}                                   # a parameter's address, or None
         for name, x in (("temperature", temperature), ("top_k", top_k), ("top_p", top_p), ("min_p", min_p)):
             row[name] = self._row(name, x, rows, _TYPE[name]) if isinstance(x, torch.Tensor) else None
+        if row["top_k"] is None and top_k is not None and not 0 < top_k < self.vocab:
+            top_k = 0                              # off, also where the number has more than 32 bits
         number = lambda name, x: _OFF[name] if x is None or row[name] is not None else x  # noqa: E731
         # (In the order of the structure's fields: by name takes three times as long.)
         a = B.GbSampleArgs(logits.data_ptr(), stride[0] if rows > 1 else self.vocab, self._row("u", u, rows, torch.float32),

@@ -63,3 +63,11 @@ def test_parameters_at_the_ends_together(cuda):
         x[:, 3] = 11.0                                    # one likeliest token: no draw by a share of a tie
         check(x.cuda(), torch.rand(len(combos), generator=g).cuda(), temperature=[c[0] for c in combos], top_p=[c[1] for c in combos],
               min_p=[c[2] for c in combos], top_k=k)
+
+
+@pytest.mark.parametrize("top_k", [1 << 31, (1 << 32) + 1, 1 << 40, -(1 << 31) - 1, -(1 << 32) + 2, 0, -3, 500, 501])
+def test_numbers_that_keep_every_token(cuda, top_k):
+    g = torch.Generator().manual_seed(5)
+    x, u = _logits(g, 6, 500, torch.float32), torch.rand(6, generator=g).cuda()
+    a, b = _sampler(6, 500)(x, u, top_k=top_k), _sampler(6, 500)(x, u)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
