@@ -29,7 +29,7 @@
 //
 // What bounds it (a launch alone, one layer): unshared caches, memory: 64 x 16384 tokens in 355 us, 6.1 TB/s (without the products
 // 339).  Shared ones, the multiplying warps: the same bytes from L2 take 263 us, 8.0 TB/s, without the products 162.  A tile's 32
-// tokens are 48 products (413 cycles of a scheduler's) and 530 instructions, for which a warp takes 2000 cycles, two a scheduler; with
+// tokens are 48 products (384 cycles of a scheduler's) and 540 instructions, for which a warp takes 2200 cycles, two a scheduler; with
 // twelve warps, two tiles a warp that share their conversions, or the next stage's K asked for early, the SM does no more.  Small calls, a chain: barriers, plan, page
 // ids and exponents, first chunks, merge: 13-15 us cold for 8 or 13 beams, 2.5 of them before the first copy.
 #include <float.h>
