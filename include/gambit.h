@@ -181,7 +181,7 @@ gb_status gb_decode_attention(gb_pool* pool, int layer, const void* q_dev, const
  * decode steps' appends: page allocation follows the same order (token by
  * token, slots ascending).  k_dev/v_dev: [n_tokens][max_beams][Hkv][D].
  * Layer 0 reserves the positions; layers 1.. must follow in order.
- * Errors as gb_decode_attention.
+ * Errors as gb_decode_attention, and GB_ERR_INVALID for more than 2^30 tokens.
  */
 gb_status gb_append_kv(gb_pool* pool, int layer, int n_tokens, const void* k_dev,
                        const void* v_dev, gb_stream_t stream);

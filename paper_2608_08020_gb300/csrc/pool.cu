@@ -805,7 +805,8 @@ extern "C" gb_status gb_pool_seed(gb_pool* pool, int n_beams, int prompt_len, co
 static gb_status append_layer(gb_pool* pool, int layer, int n_tokens, const void* k, const void* v, bool fused,
                               const RotationView& rot, const void* q, void* qout, cudaStream_t s) {
   if (!pool->seeded) return fail(pool, GB_ERR_STATE, "pool not seeded");
-  if (layer < 0 || layer >= pool->cfg.num_layers || n_tokens < 1 || !k || !v)
+  // (More tokens than the limit would pass 32 bits together with a context's length.)
+  if (layer < 0 || layer >= pool->cfg.num_layers || n_tokens < 1 || n_tokens > 1 << 30 || !k || !v)
     return fail(pool, GB_ERR_INVALID, "append: bad arguments");
   if (!on_16_bytes(k, v)) return fail(pool, GB_ERR_INVALID, "append: rows start on 16 bytes");
   if (layer != pool->next_layer) return fail(pool, GB_ERR_STATE, "layers of a step must be called in order");
